@@ -326,6 +326,135 @@ int retopk_profile_end(retopk_ctx* ctx, double ms_host[3], int64_t launches_host
 /* Number of kernels the last decode call of this context launched (host-side count). */
 int retopk_last_launch_count(const retopk_ctx* ctx);
 
+/* =========================================================================================
+ * Around the KV cache: rotary positions, append, read-back, attention over a 4-bit cache.
+ *
+ * These calls need no context: they keep nothing between calls and allocate nothing.  Each
+ * enqueues its kernels on `stream` on the CURRENT device, to which all device pointers must
+ * belong; none synchronises, all may be captured into a graph.  Conventions as above, except:
+ *   - 16-bit tensors are bf16 or fp16 (`dtype`), d is 64 or 128.
+ *   - Token-major inputs may be slices of a wider row (one projection's output): a stride counts
+ *     ELEMENTS from one token to the next, the heads of a token lie d apart.  Pointers are
+ *     16-byte aligned, strides multiples of 8 and not below heads * d.
+ *   - Lengths, positions and page numbers live on the device (int32) and are checked there: what
+ *     points outside the cache is skipped, never followed.
+ * ========================================================================================= */
+enum { RETOPK_BF16 = 0, RETOPK_FP16 = 1, RETOPK_FP32 = 2 };
+
+/*
+ * Rotary positions.  Pair i of rot_dim / 2 turns by angle position * w_i:
+ *     (x, y) -> a * (x cos - y sin, x sin + y cos)
+ * RETOPK_ROPE_HALF pairs channel i with i + rot_dim / 2, RETOPK_ROPE_INTERLEAVED 2i with 2i + 1;
+ * channels from rot_dim on pass through.  w_i = base^(-2i / rot_dim), a = 1, then by `scaling`
+ *   RETOPK_ROPE_LINEAR  w_i / factor
+ *   RETOPK_ROPE_NTK     base * factor^(rot_dim / (rot_dim - 2)) as the base   (rot_dim > 2)
+ *   RETOPK_ROPE_LLAMA3  w_i / factor where the wavelength 2 pi / w_i is above original_len /
+ *                       low_freq_factor, w_i where it is below original_len / high_freq_factor,
+ *                       between them the blend linear in original_len / wavelength
+ *   RETOPK_ROPE_YARN    w_i / factor for pairs that turn fewer than beta_slow times over
+ *                       original_len, w_i above beta_fast turns, a linear ramp over the pair index
+ *                       between; a = 0.1 ln(factor) + 1
+ * attn_factor > 0 replaces a.  Zero in low_freq_factor, high_freq_factor, beta_fast or beta_slow
+ * stands for 1, 4, 32 and 1.  Angle and rotation are computed in 64 bits (at position 1 Mi an
+ * angle in 32 bits is 0.06 rad off) and rounded once to the tensor's type.
+ */
+typedef struct retopk_rope retopk_rope;
+enum { RETOPK_ROPE_HALF = 0, RETOPK_ROPE_INTERLEAVED = 1 };
+enum { RETOPK_ROPE_PLAIN = 0, RETOPK_ROPE_LINEAR = 1, RETOPK_ROPE_NTK = 2, RETOPK_ROPE_LLAMA3 = 3, RETOPK_ROPE_YARN = 4 };
+typedef struct {
+    int d, rot_dim;      /* head dimension; rotated channels, even, 2..d */
+    int layout;          /* RETOPK_ROPE_HALF / _INTERLEAVED */
+    int scaling;         /* RETOPK_ROPE_PLAIN ... */
+    double base, factor, original_len, low_freq_factor, high_freq_factor, beta_fast, beta_slow, attn_factor;
+} retopk_rope_config_t;
+
+/* The handle holds host memory only: it serves every device and stream, from several threads too. */
+int retopk_rope_create(retopk_rope** rope, const retopk_rope_config_t* config);
+int retopk_rope_destroy(retopk_rope* rope);
+/* The frequencies w_i [rot_dim / 2] (radians per position) and a, on the host; either may be NULL. */
+int retopk_rope_frequencies(const retopk_rope* rope, double* inv_freq_host, double* attn_factor_host);
+
+/*
+ * Rotate q [n_tokens,H_q,d] and k [n_tokens,H_k,d] at positions [n_tokens] (int32, any sign) in one
+ * launch.  Either tensor may be NULL.  An output may be its own input (same pointer and stride);
+ * other overlaps are EINVAL.  inverse = 1 applies the transpose: the gradient with respect to the
+ * input, given the gradient of the output, and for a = 1 the rotation back.
+ */
+int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, const int32_t* positions, const void* q,
+                      int64_t q_stride, void* q_out, int64_t q_out_stride, int H_q, const void* k, int64_t k_stride,
+                      void* k_out, int64_t k_out_stride, int H_k, int inverse, void* stream);
+
+/*
+ * A cache in pages.  Row p of sequence b is row p % page_size of page block_table[b][p / page_size];
+ * block_table [B,max_pages] int32 on the device.  block_table = NULL: sequence b owns page b (then
+ * n_pages >= B), so that k and v with page_size = max_seq_len are the cache of retopk_decode_step.
+ *   RETOPK_PAGES_BF16 / _FP16: k, v [n_pages,H_kv,page_size,d].
+ *   RETOPK_PAGES_Q4: k, v [n_pages,H_kv,page_size,d/2] bytes, the even channel in the low four bits;
+ *     k_scale, v_scale [n_pages,H_kv,page_size,d/64,2] bf16: step s and minimum m of each group of 64
+ *     channels.  Code n stands for s * n + m.  4.5 bits a value.  page_size % 16 == 0.
+ * All four 16-byte aligned.  page_size and max_pages >= 1; their product at most 2^31 - 1.
+ */
+enum { RETOPK_PAGES_BF16 = 0, RETOPK_PAGES_FP16 = 1, RETOPK_PAGES_Q4 = 2 };
+typedef struct {
+    int format, H_kv, d, page_size;
+    int64_t n_pages;
+    void *k, *v, *k_scale, *v_scale;
+    const int32_t* block_table;
+    int64_t max_pages;
+} retopk_pages_t;
+
+/*
+ * Append new keys and values, rotated on the way.  seq_lens [B] counts the keys of each sequence
+ * INCLUDING the new ones.  The new tokens of sequence b are rows cu_new[b] .. cu_new[b+1]-1 of k_new /
+ * v_new [n_new,H_kv,d] (cu_new [B+1] int32, ascending from 0); cu_new = NULL: n_new / B rows each.
+ * Row i of n new ones goes to position seq_lens[b] - n + i.  With `rope` keys are rotated there and,
+ * if q is given, q [n_new,H_q,d] into q_out as by retopk_rope_apply; rope = NULL stores keys as they
+ * are (then q = NULL).
+ * RETOPK_PAGES_Q4 rounds the rotated key to `dtype` and then quantises each group of 64 channels:
+ * m = bf16(min), s = bf16((max - m) / 15), n = round((x - m) / s) to nearest, ties to even, within
+ * 0..15, n = 0 where s = 0; 32-bit arithmetic, IEEE rounding.  A span max - m above the fp32 range is
+ * unspecified.  16-bit pages hold `dtype`.
+ * Rows of k_new from cu_new[B] on, and tokens whose position is negative (an idle sequence of length
+ * 0), are left out, their q_out rows too.  A key whose page is not in 0..n_pages-1 or whose position is
+ * beyond the block table is not stored.  All other rows of the cache stay as they are.  Two new
+ * tokens that share a row of a page leave that row unspecified.
+ * Limits: B <= 65535; EUNSUPPORTED beyond.
+ */
+int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* cu_new, int64_t n_new,
+                     int dtype, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                     const retopk_rope* rope, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int H_q,
+                     void* stream);
+
+/*
+ * Read rows back: k_out / v_out [B,H_kv,max_rows,d], contiguous, row i of sequence b = the cache's row
+ * first[b] + i for rows below seq_lens[b] (first [B] int32, NULL = 0).  Other rows of the outputs, and
+ * those whose page is out of range, are left as they were.  Either output may be NULL.
+ * dtype: any for 4-bit pages (fp32 holds s * n + m with one rounding), the pages' own type or
+ * RETOPK_FP32 for 16-bit ones.  With max_rows = max_seq_len this fills the cache of
+ * retopk_decode_step from pages.  Limits: B, H_kv <= 65535.
+ */
+int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* first, int64_t max_rows,
+                     int dtype, void* k_out, void* v_out, void* stream);
+
+/*
+ * Decode attention over 4-bit pages (RETOPK_PAGES_Q4), all keys, no selection:
+ *     out[b,t,h] = sum_j softmax_j(scale * q . k_j) v_j,  k_j, v_j = s * n + m
+ * for T query tokens per sequence (1 = a decode step, more = draft tokens checked at once), which are
+ * its last T positions: token t sees keys j < seq_lens[b] - T + 1 + t, with window > 0 only the last
+ * `window` of those.  q row b * T + t with q_stride, out [B,T,H_q,d] contiguous, lse [B,T,H_q] fp32 or
+ * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf.  Keys of pages
+ * out of range do not count.  Scores, weights, sums and outputs are held in fp32 (weights enter the
+ * product with the codes as a sum of two bf16 parts), rounded once to dtype.  What rows behind
+ * seq_lens hold, NaN patterns among it, has no influence.  Results are bit-reproducible.
+ * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant
+ * before and after; calls that may overlap on the GPU (two streams, two captured graphs) need one each.
+ * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096; EUNSUPPORTED beyond.
+ */
+int64_t retopk_q4_attention_workspace(int B, int T, int H_q, int H_kv, int d);   /* bytes, or a negative code */
+int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int dtype,
+                        const void* q, int64_t q_stride, float scale, int64_t window, void* out, float* lse,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Static description of an error code. */
 const char* retopk_strerror(int code);
 

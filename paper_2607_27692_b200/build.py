@@ -1,4 +1,4 @@
-"""Compile the CUDA library in-tree: ``csrc/retopk_api.cu`` -> ``libretopk.so`` (sm_100a)."""
+"""Compile the CUDA library in-tree: ``csrc/*.cu`` -> ``libretopk.so`` (sm_100a)."""
 from __future__ import annotations
 
 import fcntl

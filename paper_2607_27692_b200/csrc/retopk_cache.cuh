@@ -1,0 +1,970 @@
+// Device code around the KV cache (sm_100a): rotary positions, append to 16-bit or 4-bit pages,
+// read-back of pages, and decode attention over 4-bit pages.
+//
+//   rows_kernel       rotates rows of q and k and stores k and v (rotation alone, append to 16-bit
+//                     pages and append to 4-bit pages are three instances of it)
+//   gather_kernel     rows of a paged cache -> contiguous [B,H_kv,rows,d]
+//   q4_attend_kernel  streams the 4-bit pages once through the tensor cores
+//   q4_combine_kernel joins the parts of sequences that several CTAs shared
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace retopk_cache {
+
+constexpr int TYPE_BF16 = 0, TYPE_FP16 = 1, TYPE_FP32 = 2;
+constexpr int GROUP = 64;                // channels that share a step and a minimum
+constexpr int MAX_PAIRS = 64;            // rotated pairs of a head (d <= 128)
+
+// ---------------------------------------------------------------------------------------
+// Small helpers
+// ---------------------------------------------------------------------------------------
+template <int DT> __device__ __forceinline__ float to_f32(uint16_t u) {
+    if (DT == TYPE_BF16) return __uint_as_float((uint32_t)u << 16);
+    return __half2float(__ushort_as_half(u));
+}
+template <int DT> __device__ __forceinline__ float2 unpack2(uint32_t u) {
+    if (DT == TYPE_BF16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    if (DT == TYPE_BF16) {
+        __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<uint32_t*>(&v);
+    }
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+template <int DT> __device__ __forceinline__ void unpack8(const uint4& x, float* f) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 p = unpack2<DT>(w[i]);
+        f[2 * i] = p.x;
+        f[2 * i + 1] = p.y;
+    }
+}
+template <int DT> __device__ __forceinline__ uint4 pack8(const float* f) {
+    return make_uint4(pack2<DT>(f[0], f[1]), pack2<DT>(f[2], f[3]), pack2<DT>(f[4], f[5]), pack2<DT>(f[6], f[7]));
+}
+
+__device__ __forceinline__ void cp_async16_zfill(uint32_t smem_dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The cache as the kernels see it (retopk_pages_t with 64-bit strides worked out).
+struct Pages {
+    unsigned char *k, *v, *ks, *vs;
+    const int32_t* table;       // null: sequence b owns page b
+    long long n_pages, max_pages, capacity;   // capacity: rows a sequence can have
+    int H_kv, page_size;
+};
+
+// Row index of position `pos` of sequence b for KV head 0 (head h: + h * page_size), or -1 when
+// the position is outside the cache or its page number is not a page.
+__device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long pos) {
+    if (pos < 0 || pos >= pg.capacity) return -1;
+    const int slot = (int)pos / pg.page_size, off = (int)pos - slot * pg.page_size;
+    long long page = b;
+    if (pg.table) page = pg.table[(long long)b * pg.max_pages + slot];
+    if (page < 0 || page >= pg.n_pages) return -1;
+    return page * pg.H_kv * pg.page_size + off;
+}
+
+// ---------------------------------------------------------------------------------------
+// rows_kernel: rotate and store
+// ---------------------------------------------------------------------------------------
+enum { ROT_NONE = 0, ROT_HALF = 1, ROT_INTERLEAVED = 2, ROT_HALF_ANY = 3 };
+enum { DEST_ROWS = 0, DEST_PAGES16 = 1, DEST_PAGES4 = 2 };
+constexpr int ROWS_THREADS = 256;
+constexpr int ROWS_MAX_TOKENS = 8;       // tokens per CTA
+
+struct RowsArgs {
+    double turns[MAX_PAIRS];    // turns per position of each pair: w_i / (2 pi)
+    double amp;                 // factor on cosine and sine
+    int pairs, rot_mode, inverse;
+    int tokens_per_cta, units;  // a CTA takes `tokens_per_cta` tokens; blockIdx.y of `units` shares their rows
+    long long n_tokens;
+    const int32_t* positions;   // DEST_ROWS
+    const int32_t *seq_lens, *cu;
+    int B, T;                   // T: new tokens per sequence when cu is null
+    const uint16_t *q, *k, *v;
+    uint16_t *q_out, *k_out;
+    long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+    int Hq, Hk, Hv;
+    Pages pg;
+};
+
+// One row is held by D / 16 lanes, two chunks of 8 channels each.  Where a half-layout rotation
+// covers a multiple of 16 channels, a lane's chunks are partners of each other (c and c + rot/2), so
+// that no value crosses lanes; otherwise they are channels 8l and D/2 + 8l.
+//
+// Bound: HBM (two bytes read and written per value).  The angle and the rotation are done in fp64:
+// at far positions an fp32 angle is useless, and a key that is quantised afterwards must round to the
+// same 16-bit value however it is computed.
+template <int DT, int D, int DEST>
+__global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constant__ RowsArgs a) {
+    constexpr int LANES = D / 16, RPW = 32 / LANES;      // lanes per row, rows per warp
+    __shared__ double2 s_tab[ROWS_MAX_TOKENS][MAX_PAIRS];
+    __shared__ long long s_row[ROWS_MAX_TOKENS];
+    __shared__ int s_pos[ROWS_MAX_TOKENS];
+    __shared__ int s_live[ROWS_MAX_TOKENS];
+
+    const int tid = threadIdx.x;
+    const long long tok0 = (long long)blockIdx.x * a.tokens_per_cta;
+    const int n_tok = (int)(a.n_tokens - tok0 < a.tokens_per_cta ? a.n_tokens - tok0 : a.tokens_per_cta);
+
+    if (tid < n_tok) {
+        const long long tok = tok0 + tid;
+        int live = 1, pos = 0;
+        long long row = -1;
+        if (DEST == DEST_ROWS) {
+            pos = a.positions[tok];
+        } else {
+            int b = 0, i = 0, n = 0;
+            if (a.cu) {
+                int lo = 0, hi = a.B;                    // largest b with cu[b] <= tok
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (a.cu[mid] <= tok) lo = mid; else hi = mid;
+                }
+                b = lo;
+                const int first = a.cu[b], last = a.cu[b + 1];
+                live = tok >= first && tok < last;
+                i = (int)(tok - first);
+                n = last - first;
+            } else {
+                b = (int)(tok / a.T);
+                i = (int)(tok - (long long)b * a.T);
+                n = a.T;
+            }
+            if (live) {
+                const long long p = (long long)a.seq_lens[b] - n + i;
+                live = p >= 0;
+                pos = (int)p;
+                row = cache_row(a.pg, b, p);
+            }
+        }
+        s_pos[tid] = pos;
+        s_row[tid] = row;
+        s_live[tid] = live;
+    }
+    __syncthreads();
+    if (a.rot_mode != ROT_NONE) {
+        for (int x = tid; x < n_tok * a.pairs; x += ROWS_THREADS) {
+            const int t = x / a.pairs, i = x - t * a.pairs;
+            // angle in turns, reduced before it is rounded: position * turns as a product and its rest
+            const double p = (double)s_pos[t], w = a.turns[i];
+            const double hi = p * w, lo = fma(p, w, -hi);
+            const double r = (hi - rint(hi)) + lo;
+            double sn, cs;
+            sincospi(2.0 * r, &sn, &cs);
+            sn *= a.amp;
+            cs *= a.amp;
+            // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the 8 lanes
+            // of a row in different banks
+            s_tab[t][i ^ ((i >> 3) & 7)] = make_double2(cs, a.inverse ? -sn : sn);
+        }
+    }
+    __syncthreads();
+
+    const int lane = tid & 31, warp = tid >> 5, sub = lane % LANES;
+    const int rows_per_tok = a.Hq + a.Hk + a.Hv, total = n_tok * rows_per_tok;
+    const int step = (ROWS_THREADS / 32) * RPW * a.units;
+    for (int base = ((int)blockIdx.y * (ROWS_THREADS / 32) + warp) * RPW; base < total; base += step) {
+        const int rid = base + lane / LANES;
+        const int t = rid < total ? rid / rows_per_tok : 0;
+        int h = rid - t * rows_per_tok;
+        const bool active = rid < total && s_live[t];
+        const int which = h < a.Hq ? 0 : (h < a.Hq + a.Hk ? 1 : 2);       // q, k or v
+        h -= which == 0 ? 0 : (which == 1 ? a.Hq : a.Hq + a.Hk);
+        const int mode = which == 2 ? ROT_NONE : a.rot_mode;
+        const long long tok = tok0 + t;
+        const uint16_t* src = which == 0 ? a.q + tok * a.q_stride : (which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
+        src += (long long)h * D;
+        const int half = a.pairs;                                         // rot / 2
+        int ca = 8 * sub, cb = D / 2 + 8 * sub;
+        if (mode == ROT_HALF) {
+            if (8 * sub < half) cb = half + 8 * sub;
+            else { ca = 16 * sub; cb = ca + 8; }                          // behind the rotated part
+        }
+        float xa[8], xb[8];
+        float pa[8], pb[8];                                               // partners, ROT_HALF_ANY only
+        if (active) {
+            unpack8<DT>(*reinterpret_cast<const uint4*>(src + ca), xa);
+            unpack8<DT>(*reinterpret_cast<const uint4*>(src + cb), xb);
+            if (mode == ROT_HALF_ANY) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int c = ca + e, c2 = cb + e;
+                    pa[e] = c < half ? to_f32<DT>(src[c + half]) : (c < 2 * half ? to_f32<DT>(src[c - half]) : 0.f);
+                    pb[e] = c2 < half ? to_f32<DT>(src[c2 + half]) : (c2 < 2 * half ? to_f32<DT>(src[c2 - half]) : 0.f);
+                }
+            }
+        }
+        __syncwarp();                     // in place: every lane of the row has read before one writes
+        if (active && mode == ROT_HALF && 8 * sub < half) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double2 cs = s_tab[t][(ca + e) ^ (sub & 7)];
+                const double x = xa[e], y = xb[e];
+                xa[e] = (float)(x * cs.x - y * cs.y);
+                xb[e] = (float)(y * cs.x + x * cs.y);
+            }
+        } else if (active && mode == ROT_INTERLEAVED) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                int i = (ca + e) >> 1;
+                if (i < a.pairs) {
+                    const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
+                    const double x = xa[e], y = xa[e + 1];
+                    xa[e] = (float)(x * cs.x - y * cs.y);
+                    xa[e + 1] = (float)(y * cs.x + x * cs.y);
+                }
+                i = (cb + e) >> 1;
+                if (i < a.pairs) {
+                    const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
+                    const double x = xb[e], y = xb[e + 1];
+                    xb[e] = (float)(x * cs.x - y * cs.y);
+                    xb[e + 1] = (float)(y * cs.x + x * cs.y);
+                }
+            }
+        } else if (active && mode == ROT_HALF_ANY) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int c = (s ? cb : ca) + e;
+                    float& x = s ? xb[e] : xa[e];
+                    const double own = x, other = s ? pb[e] : pa[e];
+                    if (c < 2 * half) {
+                        const int i = c < half ? c : c - half;
+                        const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
+                        x = (float)(own * cs.x + (c < half ? -other : other) * cs.y);
+                    }
+                }
+            }
+        }
+        const uint4 ya = pack8<DT>(xa), yb = pack8<DT>(xb);
+        if (DEST == DEST_ROWS || which == 0) {
+            if (active) {
+                uint16_t* dst = (which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + (long long)h * D;
+                *reinterpret_cast<uint4*>(dst + ca) = ya;
+                *reinterpret_cast<uint4*>(dst + cb) = yb;
+            }
+            if (DEST != DEST_PAGES4) continue;
+        }
+        const long long row = s_row[t] + (long long)h * a.pg.page_size;
+        const bool store = active && which != 0 && s_row[t] >= 0;
+        if (DEST == DEST_PAGES16) {
+            if (store) {
+                uint16_t* dst = reinterpret_cast<uint16_t*>(which == 1 ? a.pg.k : a.pg.v) + row * D;
+                *reinterpret_cast<uint4*>(dst + ca) = ya;
+                *reinterpret_cast<uint4*>(dst + cb) = yb;
+            }
+        } else if (DEST == DEST_PAGES4) {
+            // quantise the 16-bit values: minimum and maximum of each group over the lanes of the row
+            constexpr int NG = D / GROUP;
+            unpack8<DT>(ya, xa);
+            unpack8<DT>(yb, xb);
+            float mna = xa[0], mxa = xa[0], mnb = xb[0], mxb = xb[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) {
+                mna = fminf(mna, xa[e]); mxa = fmaxf(mxa, xa[e]);
+                mnb = fminf(mnb, xb[e]); mxb = fmaxf(mxb, xb[e]);
+            }
+            const int ga = ca / GROUP, gb = cb / GROUP;
+            float low[NG], step_[NG];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float mn = fminf(ga == g ? mna : INFINITY, gb == g ? mnb : INFINITY);
+                float mx = fmaxf(ga == g ? mxa : -INFINITY, gb == g ? mxb : -INFINITY);
+#pragma unroll
+                for (int o = 1; o < LANES; o <<= 1) {
+                    mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                }
+                low[g] = __bfloat162float(__float2bfloat16_rn(mn));
+                // the minimum may have been rounded up past the maximum of a narrow group
+                step_[g] = __bfloat162float(__float2bfloat16_rn(fmaxf(__fdiv_rn(mx - low[g], 15.f), 0.f)));
+            }
+            uint32_t wa = 0, wb = 0;
+            const float la = low[ga < NG ? ga : 0], sa = step_[ga < NG ? ga : 0], lb = low[gb < NG ? gb : 0], sb = step_[gb < NG ? gb : 0];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float na = sa > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(xa[e] - la, sa)), 0.f), 15.f) : 0.f;
+                const float nb = sb > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(xb[e] - lb, sb)), 0.f), 15.f) : 0.f;
+                wa |= (uint32_t)(int)na << (4 * e);
+                wb |= (uint32_t)(int)nb << (4 * e);
+            }
+            if (store) {
+                unsigned char* dst = (which == 1 ? a.pg.k : a.pg.v) + row * (D / 2);
+                *reinterpret_cast<uint32_t*>(dst + ca / 2) = wa;
+                *reinterpret_cast<uint32_t*>(dst + cb / 2) = wb;
+                if (sub < NG) {
+                    const float s = sub == 0 ? step_[0] : step_[NG - 1], m = sub == 0 ? low[0] : low[NG - 1];
+                    uint32_t* sc = reinterpret_cast<uint32_t*>(which == 1 ? a.pg.ks : a.pg.vs) + row * NG;
+                    sc[sub] = pack2<TYPE_BF16>(s, m);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// gather_kernel: rows of a paged cache -> contiguous rows
+// ---------------------------------------------------------------------------------------
+constexpr int GATHER_THREADS = 256;
+constexpr int GATHER_ROWS = 64;          // rows per CTA
+
+struct GatherArgs {
+    Pages pg;
+    const int32_t *seq_lens, *first;
+    long long max_rows;
+    void *k_out, *v_out;
+};
+
+template <int SRC /* 0 bf16, 1 fp16, 2: four bits */, int DT, int D>
+__global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_constant__ GatherArgs a) {
+    constexpr int LANES = D / 8, RPP = GATHER_THREADS / LANES, PASSES = GATHER_ROWS / RPP;
+    const int b = blockIdx.z, h = blockIdx.y;
+    const long long row0 = (long long)blockIdx.x * GATHER_ROWS;
+    const long long first = a.first ? a.first[b] : 0;
+    long long len = a.seq_lens[b];
+    if (len > a.pg.capacity) len = a.pg.capacity;
+    if (first + row0 >= len) return;
+    const int sub = threadIdx.x % LANES, r0 = threadIdx.x / LANES;
+    long long src_row[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const long long i = row0 + r0 + p * RPP;
+        src_row[p] = -1;
+        if (i < a.max_rows && first + i < len) {
+            src_row[p] = cache_row(a.pg, b, first + i);
+            if (src_row[p] >= 0) src_row[p] += (long long)h * a.pg.page_size;
+        }
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        void* out = kv ? a.v_out : a.k_out;
+        if (!out) continue;
+        const unsigned char* base = kv ? a.pg.v : a.pg.k;
+        const unsigned char* sbase = kv ? a.pg.vs : a.pg.ks;
+        uint4 raw[PASSES];
+        uint32_t sc[PASSES];
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            if (src_row[p] < 0) continue;
+            if (SRC == 2) {
+                raw[p].x = *reinterpret_cast<const uint32_t*>(base + src_row[p] * (D / 2) + sub * 4);
+                sc[p] = *reinterpret_cast<const uint32_t*>(sbase + (src_row[p] * (D / GROUP) + sub * 8 / GROUP) * 4);
+            } else {
+                raw[p] = *reinterpret_cast<const uint4*>(base + (src_row[p] * D + sub * 8) * 2);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            if (src_row[p] < 0) continue;
+            const long long i = row0 + r0 + p * RPP;
+            const long long at = (((long long)b * a.pg.H_kv + h) * a.max_rows + i) * D + sub * 8;
+            float f[8];
+            if (SRC == 2) {
+                const float2 sm = unpack2<TYPE_BF16>(sc[p]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = fmaf((float)((raw[p].x >> (4 * e)) & 15u), sm.x, sm.y);
+            } else if (DT == TYPE_FP32) {
+                unpack8<SRC == 2 ? 0 : SRC>(raw[p], f);
+            }
+            if (DT == TYPE_FP32) {
+                float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
+                o[0] = make_float4(f[0], f[1], f[2], f[3]);
+                o[1] = make_float4(f[4], f[5], f[6], f[7]);
+            } else {
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = SRC == 2 ? pack8<DT>(f) : raw[p];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// q4_attend_kernel
+// ---------------------------------------------------------------------------------------
+constexpr int Q4_THREADS = 256, Q4_WARPS = Q4_THREADS / 32;
+constexpr int Q4_TILE = 16;              // keys of one warp tile
+constexpr int Q4_UNIT = Q4_TILE * Q4_WARPS;
+constexpr int Q4_STAGES = 4;             // tiles a warp has in flight or in use
+constexpr float Q4_NONE = -3.0e38f;      // reference of a column that has seen no key
+
+// Columns (query token, head of the group) of one CTA by shape: four columns, each as two parts of
+// its weights, or 8 or 16 columns.
+enum { COLS_4 = 0, COLS_8 = 1, COLS_16 = 2 };
+__host__ __device__ constexpr int q4_cols(int shape) { return shape == COLS_4 ? 4 : (shape == COLS_8 ? 8 : 16); }
+// bytes of one stage of one warp: key codes, value codes, key scales, value scales of 16 rows
+__host__ __device__ constexpr int q4_stage_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
+__host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
+    const int ring = Q4_WARPS * Q4_STAGES * q4_stage_bytes(d);
+    const int merge = Q4_WARPS * q4_cols(shape) * (d + 2) * 4;
+    return ring > merge ? ring : merge;
+}
+
+struct Q4Args {
+    Pages pg;
+    const int32_t* seq_lens;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    float* part;                // [2 * grid][cols][d + 2]
+    long long q_stride, window;
+    float scale_log2;
+    int B, T, Hq, G, col_tiles, grid;
+};
+
+struct Span { int lo, len, units; };     // keys of a sequence: first one read (multiple of 16), end, units
+__device__ __forceinline__ Span q4_span(const Q4Args& a, int b) {
+    Span s;
+    long long len = a.seq_lens[b];
+    if (len > a.pg.capacity) len = a.pg.capacity;
+    s.len = len > 0 ? (int)len : 0;
+    long long lo = a.window > 0 ? (long long)s.len - a.T + 1 - a.window : 0;
+    if (lo < 0) lo = 0;
+    s.lo = (int)lo & ~(Q4_TILE - 1);
+    s.units = s.len > s.lo ? (s.len - s.lo + Q4_UNIT - 1) / Q4_UNIT : 0;
+    return s;
+}
+// Share c of `grid` in U >= grid units begins here (no share is empty).
+__device__ __forceinline__ long long q4_share(long long U, int grid, int c) { return U * c / grid; }
+
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <int DT>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (DT == TYPE_BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Codes I and I + 4 of a word of eight (or of two half words of four) as two 16-bit numbers OFFSET + n:
+// the code is put where the mantissa of OFFSET counts ones.
+template <int DT, int I> __device__ __forceinline__ uint32_t codes2(uint32_t x) {
+    if (DT == TYPE_BF16) return ((x >> (4 * I)) & 0x000f000fu) | 0x43004300u;          // 128 + n
+    return ((I == 0 ? x << 4 : x >> (4 * I - 4)) & 0x00f000f0u) | 0x54005400u;         // 64 + n
+}
+template <int DT> __host__ __device__ constexpr float code_offset() { return DT == TYPE_BF16 ? 128.f : 64.f; }
+
+// One warp's running state over the keys that it has seen.
+template <int D, int NT, bool PACKED>
+struct Q4State {
+    static constexpr int NG = D / GROUP, NC = PACKED ? 1 : 2;
+    float o[NG][4][NT][4];      // codes times weights: channel pairs x columns
+    float off[NG][NT][4];       // OFFSET times the sum of the weights, by the same products
+    float msum[NG][NT][NC];     // weights times minima, over this lane's rows
+    float l[NT][NC], ref[NT][NC];
+};
+
+// Mathematics.  With a key row held as s_g n_c + m_g per group g of 64 channels,
+//     q . k = sum_g ( s_g (q . n)_g + m_g (sum of q)_g )
+// so the codes go into the tensor core as they are (OFFSET + n, exact in 16 bits, the offset taken out
+// through the accumulator's start value) and step and minimum are applied to the 16 x 8 result.  The
+// same for values: sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j, the weight p_j s_j entering as
+// two bf16 parts (hi + lo, 2^-17 relative) and OFFSET * sum_j p_j s_j taken out by one product with a
+// constant matrix, from the very same rounded weights.  Keys are the M side of both products (16 keys
+// or 16 channels), the columns the N side: with 4 columns the two parts of a weight fill the 8 columns
+// of one product, so the second part is free.
+//
+// A warp works alone on tiles of 16 keys (2.3 KB at d = 128) through its own ring of cp.async stages;
+// warps meet only when a sequence's share ends.  The reference of the exponentials moves only when a
+// score exceeds it by 2^8: one vote per tile instead of a reduction.
+//
+// Channels are matched to the fragments so that no code moves between lanes: key codes of lane quarter
+// t are channels 64 g + 16 t .. + 15, value codes of lane group r channels 64 g + 8 r .. + 7.
+template <int DT, int D, int SHAPE>
+__global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_attend_kernel(const __grid_constant__ Q4Args a) {
+    constexpr bool PACKED = SHAPE == COLS_4;
+    constexpr int NT = SHAPE == COLS_16 ? 2 : 1;
+    constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2;
+    constexpr int STAGE = q4_stage_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4;
+    constexpr uint32_t ONES = 0x43004300u;               // 128, 128 in bf16
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int s_start[3];                           // sequence, units before it (two words: 64 bits are not needed)
+    __shared__ int s_scan[Q4_WARPS + 1];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, t4 = lane & 3, r8 = lane >> 2;
+    const int per_seq = a.pg.H_kv * a.col_tiles;
+
+    // Units before each sequence: every CTA adds up the lengths itself.  First the total, then the
+    // sequence in which this CTA's share begins.
+    long long U = 0, u = 0, u_end = 0, before = 0;
+    int b = 0, shares = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        long long run = 0;
+        for (int b0 = 0; b0 < a.B; b0 += Q4_THREADS) {
+            const int bb = b0 + tid;
+            int v = bb < a.B ? q4_span(a, bb).units * per_seq : 0;
+            int incl = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int w = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += w;
+            }
+            if (lane == 31) s_scan[warp] = incl;
+            __syncthreads();
+            int base = 0, tot = 0;
+#pragma unroll
+            for (int w = 0; w < Q4_WARPS; ++w) {
+                if (w < warp) base += s_scan[w];
+                tot += s_scan[w];
+            }
+            if (pass == 1) {
+                const long long lo = run + base + incl - v;
+                if (v > 0 && u >= lo && u < lo + v) { s_start[0] = bb; s_start[1] = (int)(u - lo); }
+            }
+            run += tot;
+            __syncthreads();
+        }
+        if (pass == 0) {
+            U = run;
+            shares = U < a.grid ? (int)U : a.grid;
+            if ((int)blockIdx.x >= shares) return;
+            u = q4_share(U, shares, blockIdx.x);
+            u_end = q4_share(U, shares, blockIdx.x + 1);
+        }
+    }
+    b = s_start[0];
+    before = u - s_start[1];                             // units before sequence b
+    Span sp = q4_span(a, b);
+    const long long u_begin = u;
+
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (Q4_STAGES * STAGE);
+    unsigned char* ring_p = smem + warp * (Q4_STAGES * STAGE);
+    float* s_merge = reinterpret_cast<float*>(smem);
+
+    while (u < u_end) {
+        while (u >= before + (long long)sp.units * per_seq) {
+            before += (long long)sp.units * per_seq;
+            ++b;
+            sp = q4_span(a, b);
+        }
+        const int in_seq = (int)(u - before);
+        const int item = in_seq / sp.units, k_unit = in_seq - item * sp.units;
+        const int h = item / a.col_tiles, ct = item - h * a.col_tiles;
+        int n_units = sp.units - k_unit;
+        if (u_end - u < n_units) n_units = (int)(u_end - u);
+        const long long item_start = before + (long long)item * sp.units;
+        const int key0 = sp.lo + k_unit * Q4_UNIT;
+        int key_end = key0 + n_units * Q4_UNIT;
+        if (key_end > sp.len) key_end = sp.len;
+        // this warp's tiles: key0 + (i * warps + warp) * 16
+        const int n_all = (key_end - key0 + Q4_TILE - 1) / Q4_TILE;
+        const int n_tiles = n_all > warp ? (n_all - warp + Q4_WARPS - 1) / Q4_WARPS : 0;
+
+        // ---- page rows of the next 32 tiles, one per lane ------------------------------------
+        auto tile_row = [&](int i) -> long long {
+            if (i >= n_tiles) return -1;
+            const long long r = cache_row(a.pg, b, key0 + ((long long)i * Q4_WARPS + warp) * Q4_TILE);
+            return r < 0 ? -1 : r + (long long)h * a.pg.page_size;
+        };
+        long long rows_now = tile_row(lane), rows_next = tile_row(32 + lane);
+        uint32_t bad_now = 0;                            // stages whose page was out of range, one bit each
+
+        auto issue = [&](int i) {
+            if (i < n_tiles) {
+                if (i > 0 && (i & 31) == 0) {
+                    rows_now = rows_next;
+                    rows_next = tile_row(i + 32 + lane);
+                }
+                const long long row = __shfl_sync(0xffffffffu, rows_now, i & 31);
+                const int st = i % Q4_STAGES;
+                const uint32_t dst = ring + st * STAGE;
+                const bool ok = row >= 0;
+                bad_now = (bad_now & ~(1u << st)) | (ok ? 0u : 1u << st);
+                const long long rr = ok ? row : 0;
+                const uint32_t nb = ok ? 16u : 0u;
+                const unsigned char* kp = a.pg.k + rr * (D / 2);
+                const unsigned char* vp = a.pg.v + rr * (D / 2);
+#pragma unroll
+                for (int c = lane; c < KB / 16; c += 32) {
+                    // 128-byte lines with their 16-byte slots exchanged by line: the fragment reads
+                    // below then touch every bank once
+                    const uint32_t o = (uint32_t)((c >> 3) * 128 + (((c & 7) ^ (2 * ((c >> 3) & 3))) * 16));
+                    cp_async16_zfill(dst + o, kp + c * 16, nb);
+                    cp_async16_zfill(dst + KB + o, vp + c * 16, nb);
+                }
+                if (lane < SB / 16) cp_async16_zfill(dst + 2 * KB + lane * 16, a.pg.ks + rr * (NG * 4) + lane * 16, nb);
+                else if (lane < SB / 8) cp_async16_zfill(dst + 2 * KB + lane * 16, a.pg.vs + rr * (NG * 4) + (lane - SB / 16) * 16, nb);
+            }
+            cp_async_commit();
+        };
+#pragma unroll
+        for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i);
+
+        // ---- queries of this column tile ------------------------------------------------------
+        // fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n)
+        uint32_t qf[NT][NG][4][2];
+        float qsum[NT][NG][NC];
+        int lim[NT][NC], low[NT][NC];                    // keys [low, lim) count for a column
+        const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int col = PACKED ? r8 >> 1 : nt * 8 + r8;
+            const int cc = ct * COLS + (col < cols_here ? col : 0);
+            const int tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
+            const uint16_t* qp = a.q + ((long long)b * a.T + tok) * a.q_stride + (long long)head * D;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j);
+                    // channels (0,4) (1,5) (2,6) (3,7) of the eight
+                    qf[nt][g][2 * j][0] = __byte_perm(x.x, x.z, 0x5410);
+                    qf[nt][g][2 * j][1] = __byte_perm(x.x, x.z, 0x7632);
+                    qf[nt][g][2 * j + 1][0] = __byte_perm(x.y, x.w, 0x5410);
+                    qf[nt][g][2 * j + 1][1] = __byte_perm(x.y, x.w, 0x7632);
+                    float f[8];
+                    unpack8<DT>(x, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s += f[e];
+                }
+                s += __shfl_xor_sync(0xffffffffu, s, 1);
+                s += __shfl_xor_sync(0xffffffffu, s, 2);
+                // lanes hold columns 2 t4 + c of the result
+#pragma unroll
+                for (int c = 0; c < NC; ++c) qsum[nt][g][c] = __shfl_sync(0xffffffffu, s, (2 * t4 + c) * 4);
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
+                const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
+                lim[nt][c] = sp.len - a.T + 1 + tk;
+                low[nt][c] = a.window > 0 && lim[nt][c] > a.window ? (int)(lim[nt][c] - a.window) : 0;
+            }
+        }
+        // keys below safe_end and from safe_lo on count for every column
+        const int safe_end = sp.len - a.T + 1;
+        const int safe_lo = a.window > 0 && sp.len > a.window ? (int)(sp.len - a.window) : 0;
+
+        Q4State<D, NT, PACKED> st;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) st.o[g][m][nt][e] = 0.f;
+                    st.off[g][nt][e] = 0.f;
+                }
+#pragma unroll
+                for (int c = 0; c < NC; ++c) st.msum[g][nt][c] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) { st.l[nt][c] = 0.f; st.ref[nt][c] = Q4_NONE; }
+        }
+
+        for (int i = 0; i < n_tiles; ++i) {
+            cp_async_wait<Q4_STAGES - 2>();
+            __syncwarp();
+            const int sidx = i % Q4_STAGES;
+            const bool bad = (bad_now >> sidx) & 1u;
+            issue(i + Q4_STAGES - 1);                    // into the stage that the previous tile left
+            const unsigned char* sk = ring_p + sidx * STAGE;
+            const unsigned char* sv = sk + KB;
+            const uint32_t* ssk = reinterpret_cast<const uint32_t*>(sk + 2 * KB);
+            const uint32_t* ssv = ssk + Q4_TILE * NG;
+            const int kbase = key0 + (i * Q4_WARPS + warp) * Q4_TILE;
+            // offset of byte x of row r in a swizzled block
+            auto sw = [](int r, int x) -> int {
+                const int lin = r * (D / 2) + x, line = lin >> 7;
+                return (line << 7) + ((((lin >> 4) & 7) ^ (2 * (line & 3))) << 4) + (lin & 15);
+            };
+
+            // ---- scores of 16 keys ------------------------------------------------------------
+            float sc[NT][2][NC];                         // rows r8 and r8 + 8
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) sc[nt][r][c] = 0.f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint2 x = *reinterpret_cast<const uint2*>(sk + sw(r8, g * 32 + 8 * t4));
+                const uint2 y = *reinterpret_cast<const uint2*>(sk + sw(r8 + 8, g * 32 + 8 * t4));
+                float acc[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[nt][e] = -code_offset<DT>() * qsum[nt][g][PACKED ? 0 : (e & 1)];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t xw = j ? x.y : x.x, yw = j ? y.y : y.x;
+                    const uint32_t x0 = codes2<DT, 0>(xw), x1 = codes2<DT, 1>(xw), x2 = codes2<DT, 2>(xw), x3 = codes2<DT, 3>(xw);
+                    const uint32_t y0 = codes2<DT, 0>(yw), y1 = codes2<DT, 1>(yw), y2 = codes2<DT, 2>(yw), y3 = codes2<DT, 3>(yw);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma16816<DT>(acc[nt], x0, y0, x1, y1, qf[nt][g][2 * j][0], qf[nt][g][2 * j][1]);
+                        mma16816<DT>(acc[nt], x2, y2, x3, y3, qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
+                    }
+                }
+                const float2 s0 = unpack2<TYPE_BF16>(ssk[r8 * NG + g]), s1 = unpack2<TYPE_BF16>(ssk[(r8 + 8) * NG + g]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        sc[nt][0][c] += s0.x * acc[nt][c] + s0.y * qsum[nt][g][c];
+                        sc[nt][1][c] += s1.x * acc[nt][2 + c] + s1.y * qsum[nt][g][c];
+                    }
+            }
+
+            // ---- weights -----------------------------------------------------------------------
+            const bool edge = bad || kbase + Q4_TILE > safe_end || kbase < safe_lo;
+            bool grow = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        float x = sc[nt][r][c] * a.scale_log2;
+                        if (edge) {
+                            const int key = kbase + r8 + 8 * r;
+                            if (bad || key >= lim[nt][c] || key < low[nt][c]) x = -INFINITY;
+                        }
+                        sc[nt][r][c] = x;
+                        grow |= x > st.ref[nt][c] + 8.f;
+                    }
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float f[NC];
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        float mx = fmaxf(sc[nt][0][c], sc[nt][1][c]);
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                        mx = fmaxf(mx, st.ref[nt][c]);
+                        f[c] = exp2f(st.ref[nt][c] - mx);
+                        st.ref[nt][c] = mx;
+                        st.l[nt][c] *= f[c];
+                    }
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) st.msum[g][nt][c] *= f[c];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float fe = f[PACKED ? 0 : (e & 1)];
+                            st.off[g][nt][e] *= fe;
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) st.o[g][m][nt][e] *= fe;
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    sc[nt][0][c] = exp2f(sc[nt][0][c] - st.ref[nt][c]);
+                    sc[nt][1][c] = exp2f(sc[nt][1][c] - st.ref[nt][c]);
+                    st.l[nt][c] += sc[nt][0][c] + sc[nt][1][c];
+                }
+
+            // ---- values ------------------------------------------------------------------------
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                float2 v0 = unpack2<TYPE_BF16>(ssv[r8 * NG + g]), v1 = unpack2<TYPE_BF16>(ssv[(r8 + 8) * NG + g]);
+                if (edge) {                              // rows that hold no key may hold anything
+                    if (bad || kbase + r8 >= sp.len) v0 = make_float2(0.f, 0.f);
+                    if (bad || kbase + r8 + 8 >= sp.len) v1 = make_float2(0.f, 0.f);
+                }
+                uint32_t bw[NT][PACKED ? 1 : 2][2];      // [part][rows 0-7, 8-15], transposed to the N side
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 v = r ? v1 : v0;
+                        if (PACKED) {
+                            const float w = sc[nt][r][0] * v.x;
+                            const float hi = __bfloat162float(__float2bfloat16_rn(w));
+                            bw[nt][0][r] = movmatrix(pack2<TYPE_BF16>(hi, w - hi));
+                            st.msum[g][nt][0] += sc[nt][r][0] * v.y;
+                        } else {
+                            const float w0 = sc[nt][r][0] * v.x, w1 = sc[nt][r][NC - 1] * v.x;
+                            const uint32_t hi = pack2<TYPE_BF16>(w0, w1);
+                            const float2 hf = unpack2<TYPE_BF16>(hi);
+                            bw[nt][0][r] = movmatrix(hi);
+                            bw[nt][PACKED ? 0 : 1][r] = movmatrix(pack2<TYPE_BF16>(w0 - hf.x, w1 - hf.y));
+                            st.msum[g][nt][0] += sc[nt][r][0] * v.y;
+                            st.msum[g][nt][NC - 1] += sc[nt][r][NC - 1] * v.y;
+                        }
+                    }
+                }
+                // codes of keys 2 t4, 2 t4 + 1, + 8, + 9 for channels 64 g + 8 r8 .. + 7
+                const int x = g * 32 + 4 * r8;
+                const uint32_t w0 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4, x));
+                const uint32_t w1 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 1, x));
+                const uint32_t w8 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 8, x));
+                const uint32_t w9 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 9, x));
+                const uint32_t lo01 = __byte_perm(w0, w1, 0x5410), hi01 = __byte_perm(w0, w1, 0x7632);
+                const uint32_t lo89 = __byte_perm(w8, w9, 0x5410), hi89 = __byte_perm(w8, w9, 0x7632);
+                constexpr int BF = TYPE_BF16;
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const uint32_t p01 = hh ? hi01 : lo01, p89 = hh ? hi89 : lo89;
+                    const uint32_t c0 = codes2<BF, 0>(p01), c1 = codes2<BF, 1>(p01), c2 = codes2<BF, 2>(p01), c3 = codes2<BF, 3>(p01);
+                    const uint32_t e0 = codes2<BF, 0>(p89), e1 = codes2<BF, 1>(p89), e2 = codes2<BF, 2>(p89), e3 = codes2<BF, 3>(p89);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int part = 0; part < (PACKED ? 1 : 2); ++part) {
+                            mma16816<BF>(st.o[g][2 * hh][nt], c0, c1, e0, e1, bw[nt][part][0], bw[nt][part][1]);
+                            mma16816<BF>(st.o[g][2 * hh + 1][nt], c2, c3, e2, e3, bw[nt][part][0], bw[nt][part][1]);
+                        }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int part = 0; part < (PACKED ? 1 : 2); ++part)
+                        mma16816<BF>(st.off[g][nt], ONES, ONES, ONES, ONES, bw[nt][part][0], bw[nt][part][1]);
+            }
+        }
+        cp_async_wait<0>();
+
+        // ---- join the warps ---------------------------------------------------------------------
+        // sums over the lanes that share columns (rows of the tiles)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    st.l[nt][c] += __shfl_xor_sync(0xffffffffu, st.l[nt][c], o);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) st.msum[g][nt][c] += __shfl_xor_sync(0xffffffffu, st.msum[g][nt][c], o);
+                }
+            }
+        __syncthreads();                                 // every warp is done with its ring
+        // [warp][col][D], then [warp][col] reference and sum
+        float* s_ref = s_merge + Q4_WARPS * COLS * D;
+        float* s_l = s_ref + Q4_WARPS * COLS;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = PACKED ? t4 : nt * 8 + 2 * t4 + c;
+                float* dst = s_merge + (warp * COLS + col) * D;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {    // accumulator rows r8 and r8 + 8: channels 2 m and 2 m + 1
+                            float x = st.o[g][m][nt][2 * e + c] - st.off[g][nt][2 * e + c];
+                            if (PACKED) x += st.o[g][m][nt][2 * e + 1] - st.off[g][nt][2 * e + 1];
+                            dst[g * GROUP + 8 * r8 + 2 * m + e] = x + st.msum[g][nt][c];
+                        }
+                if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
+            }
+        __syncthreads();
+        const bool whole = n_units == sp.units;
+        float* part = a.part + (long long)(2 * blockIdx.x + (item_start > u_begin ? 1 : 0)) * COLS * (D + 2);
+        for (int x = tid; x < cols_here * D; x += Q4_THREADS) {
+            const int col = x / D, ch = x - col * D;
+            float mx = Q4_NONE;
+#pragma unroll
+            for (int w = 0; w < Q4_WARPS; ++w) mx = fmaxf(mx, s_ref[w * COLS + col]);
+            float l = 0.f, o = 0.f;
+#pragma unroll
+            for (int w = 0; w < Q4_WARPS; ++w) {
+                const float f = exp2f(s_ref[w * COLS + col] - mx);
+                l += f * s_l[w * COLS + col];
+                o += f * s_merge[(w * COLS + col) * D + ch];
+            }
+            if (whole) {
+                const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
+                const long long row = ((long long)b * a.T + tok) * a.Hq + head;
+                const float y = l > 0.f ? o / l : 0.f;
+                a.out[row * D + ch] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
+                if (a.lse && ch == 0) a.lse[row] = l > 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            } else {
+                part[col * (D + 2) + ch] = o;
+                if (ch == 0) { part[col * (D + 2) + D] = mx; part[col * (D + 2) + D + 1] = l; }
+            }
+        }
+        __syncthreads();                                 // the ring is free for the next share
+        u += n_units;
+    }
+}
+
+// Joins the parts of items (sequence, KV head, column tile) that more than one CTA worked on, and
+// writes the rows of sequences without keys.  One CTA of D threads per item.
+template <int DT, int D, int SHAPE>
+__global__ void __launch_bounds__(D) q4_combine_kernel(const __grid_constant__ Q4Args a) {
+    constexpr int COLS = q4_cols(SHAPE);
+    __shared__ long long s_sum[2];
+    const int tid = threadIdx.x, per_seq = a.pg.H_kv * a.col_tiles;
+    const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
+    const int h = item / a.col_tiles, ct = item - h * a.col_tiles;
+    if (tid < 2) s_sum[tid] = 0;
+    __syncthreads();
+    long long mine = 0, all = 0;
+    for (int bb = tid; bb < a.B; bb += D) {
+        const int n = q4_span(a, bb).units;
+        all += n;
+        if (bb < b) mine += n;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        mine += __shfl_down_sync(0xffffffffu, mine, o);
+        all += __shfl_down_sync(0xffffffffu, all, o);
+    }
+    if ((tid & 31) == 0) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s_sum[0]), (unsigned long long)mine);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&s_sum[1]), (unsigned long long)all);
+    }
+    __syncthreads();
+    const int units = q4_span(a, b).units;
+    const long long U = s_sum[1] * per_seq, ua = s_sum[0] * per_seq + (long long)item * units, ub = ua + units;
+    const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
+    const int shares = U < a.grid ? (int)U : a.grid;
+    int c0 = 0, c1 = -1;
+    if (units > 0) {
+        // CTA whose share holds unit x: the largest c with U * c / shares <= x
+        c0 = (int)(((ua + 1) * shares + U - 1) / U) - 1;
+        c1 = (int)((ub * shares + U - 1) / U) - 1;
+        if (c0 == c1) return;                            // one CTA had it all and wrote it
+    }
+    for (int col = 0; col < cols_here; ++col) {
+        float mx = Q4_NONE;
+        for (int c = c0; c <= c1; ++c) {
+            const float* p = a.part + ((long long)(2 * c + (ua > q4_share(U, shares, c) ? 1 : 0)) * COLS + col) * (D + 2);
+            mx = fmaxf(mx, p[D]);
+        }
+        float l = 0.f, o = 0.f;
+        for (int c = c0; c <= c1; ++c) {
+            const float* p = a.part + ((long long)(2 * c + (ua > q4_share(U, shares, c) ? 1 : 0)) * COLS + col) * (D + 2);
+            const float f = exp2f(p[D] - mx);
+            l += f * p[D + 1];
+            o += f * p[tid];
+        }
+        const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
+        const long long row = ((long long)b * a.T + tok) * a.Hq + head;
+        const float y = l > 0.f ? o / l : 0.f;
+        a.out[row * D + tid] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
+        if (a.lse && tid == 0) a.lse[row] = l > 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+}  // namespace retopk_cache

@@ -60,6 +60,15 @@ SIGNATURES = {
     "retopk_profile_begin": (_i32, [_vp, _i32]),
     "retopk_profile_end": (_i32, [_vp, C.POINTER(C.c_double), C.POINTER(_i64)]),
     "retopk_last_launch_count": (_i32, [_vp]),
+    # around the KV cache (bound in paged.py)
+    "retopk_rope_create": (_i32, [C.POINTER(_vp), _vp]),
+    "retopk_rope_destroy": (_i32, [_vp]),
+    "retopk_rope_frequencies": (_i32, [_vp, C.POINTER(C.c_double), C.POINTER(C.c_double)]),
+    "retopk_rope_apply": (_i32, [_vp, _i32, _i64, _vp, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _i32, _i32, _vp]),
+    "retopk_kv_append": (_i32, [_vp, _i32, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i32, _vp]),
+    "retopk_kv_gather": (_i32, [_vp, _i32, _vp, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "retopk_q4_attention_workspace": (_i64, [_i32] * 5),
+    "retopk_q4_attention": (_i32, [_vp, _i32, _i32, _i32, _vp, _i32, _vp, _i64, _f32, _i64, _vp, _vp, _vp, _i64, _vp]),
     "retopk_strerror": (C.c_char_p, [_i32]),
 }
 
