@@ -151,7 +151,7 @@ int check_q4_shape(int B, int T, int H_q, int H_kv, int d) {
 template <int DT, int D, int SHAPE> int launch_q4(const Q4Args& a, int items, cudaStream_t s) {
     q4_attend_kernel<DT, D, SHAPE><<<a.grid, Q4_THREADS, q4_smem_bytes(D, SHAPE), s>>>(a);
     if (cudaGetLastError() != cudaSuccess) return RETOPK_ECUDA;
-    q4_combine_kernel<DT, D, SHAPE><<<items, D, 0, s>>>(a);
+    q4_combine_kernel<DT, D, SHAPE><<<dim3((unsigned)items, (unsigned)q4_cols(SHAPE)), D, 0, s>>>(a);
     return launched();
 }
 template <int DT, int D> int launch_q4_shape(const Q4Args& a, int shape, int items, cudaStream_t s) {

@@ -50,8 +50,8 @@ template <int DT> __device__ __forceinline__ uint4 pack8(const float* f) {
     return make_uint4(pack2<DT>(f[0], f[1]), pack2<DT>(f[2], f[3]), pack2<DT>(f[4], f[5]), pack2<DT>(f[6], f[7]));
 }
 
-__device__ __forceinline__ void cp_async16_zfill(uint32_t smem_dst, const void* src, uint32_t bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -394,19 +394,20 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
 // q4_attend_kernel
 // ---------------------------------------------------------------------------------------
 constexpr int Q4_THREADS = 256, Q4_WARPS = Q4_THREADS / 32;
-constexpr int Q4_TILE = 16;              // keys of one warp tile
+constexpr int Q4_TILE = 16;              // keys of one tile
+constexpr int Q4_PAIR = 2;               // tiles that a warp takes in one step
 constexpr int Q4_UNIT = Q4_TILE * Q4_WARPS;
-constexpr int Q4_STAGES = 4;             // tiles a warp has in flight or in use
+constexpr int Q4_STAGES = 3;             // steps a warp has in flight or in use
 constexpr float Q4_NONE = -3.0e38f;      // reference of a column that has seen no key
 
 // Columns (query token, head of the group) of one CTA by shape: four columns, each as two parts of
 // its weights, or 8 or 16 columns.
 enum { COLS_4 = 0, COLS_8 = 1, COLS_16 = 2 };
 __host__ __device__ constexpr int q4_cols(int shape) { return shape == COLS_4 ? 4 : (shape == COLS_8 ? 8 : 16); }
-// bytes of one stage of one warp: key codes, value codes, key scales, value scales of 16 rows
-__host__ __device__ constexpr int q4_stage_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
+// bytes of one tile: key codes, value codes, key scales, value scales of 16 rows
+__host__ __device__ constexpr int q4_tile_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
 __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
-    const int ring = Q4_WARPS * Q4_STAGES * q4_stage_bytes(d);
+    const int ring = Q4_WARPS * Q4_STAGES * Q4_PAIR * q4_tile_bytes(d);
     const int merge = Q4_WARPS * q4_cols(shape) * (d + 2) * 4;
     return ring > merge ? ring : merge;
 }
@@ -424,9 +425,9 @@ struct Q4Args {
 };
 
 struct Span { int lo, len, units; };     // keys of a sequence: first one read (multiple of 16), end, units
-__device__ __forceinline__ Span q4_span(const Q4Args& a, int b) {
+__device__ __forceinline__ Span q4_span(const Q4Args& a, int seq_len) {
     Span s;
-    long long len = a.seq_lens[b];
+    long long len = seq_len;
     if (len > a.pg.capacity) len = a.pg.capacity;
     s.len = len > 0 ? (int)len : 0;
     long long lo = a.window > 0 ? (long long)s.len - a.T + 1 - a.window : 0;
@@ -438,6 +439,11 @@ __device__ __forceinline__ Span q4_span(const Q4Args& a, int b) {
 // Share c of `grid` in U >= grid units begins here (no share is empty).
 __device__ __forceinline__ long long q4_share(long long U, int grid, int c) { return U * c / grid; }
 
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -453,106 +459,139 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Codes I and I + 4 of a word of eight (or of two half words of four) as two 16-bit numbers OFFSET + n:
-// the code is put where the mantissa of OFFSET counts ones.
-template <int DT, int I> __device__ __forceinline__ uint32_t codes2(uint32_t x) {
-    if (DT == TYPE_BF16) return ((x >> (4 * I)) & 0x000f000fu) | 0x43004300u;          // 128 + n
-    return ((I == 0 ? x << 4 : x >> (4 * I - 4)) & 0x00f000f0u) | 0x54005400u;         // 64 + n
+// Codes as operands.  A code n in the low bits of a 16-bit number IS a number: the subnormal n * 2^-133
+// in bf16 (n * 2^-24 in fp16), which the tensor core multiplies exactly.  In bf16 bits 0..7 count up
+// linearly across the first normal exponent, so the second code of a byte stands for 16 n * 2^-133
+// where it is: one mask each and one shift for four pairs.  (fp16 keeps 16 times smaller queries from
+// becoming subnormal by shifting instead.)  No offset, hence no cancellation in the sums.
+template <int DT> __device__ __forceinline__ void codes8(uint32_t x, uint32_t (&c)[4]) {
+    if (DT == TYPE_BF16) {
+        const uint32_t y = x >> 8;
+        c[0] = x & 0x000f000fu;
+        c[1] = x & 0x00f000f0u;          // times 16
+        c[2] = y & 0x000f000fu;
+        c[3] = y & 0x00f000f0u;          // times 16
+    } else {
+        c[0] = x & 0x000f000fu;
+        c[1] = (x >> 4) & 0x000f000fu;
+        c[2] = (x >> 8) & 0x000f000fu;
+        c[3] = (x >> 12) & 0x000f000fu;
+    }
 }
-template <int DT> __host__ __device__ constexpr float code_offset() { return DT == TYPE_BF16 ? 128.f : 64.f; }
+// Powers of two that keep products with subnormals in the middle of the fp32 range: bf16 queries are
+// multiplied by 2^64, weights carry 2^64 through the reference of their exponential.
+constexpr float TWO64 = 18446744073709551616.f, TWO69 = 32.f * TWO64;     // 2^-133 * 2^64 = 1 / TWO69
+template <int DT> __host__ __device__ constexpr float q_scale() { return DT == TYPE_BF16 ? TWO64 : 1.f; }
+template <int DT> __host__ __device__ constexpr float score_unit() { return DT == TYPE_BF16 ? TWO69 : 16777216.f; }
 
 // One warp's running state over the keys that it has seen.
 template <int D, int NT, bool PACKED>
 struct Q4State {
     static constexpr int NG = D / GROUP, NC = PACKED ? 1 : 2;
     float o[NG][4][NT][4];      // codes times weights: channel pairs x columns
-    float off[NG][NT][4];       // OFFSET times the sum of the weights, by the same products
     float msum[NG][NT][NC];     // weights times minima, over this lane's rows
-    float l[NT][NC], ref[NT][NC];
+    float l[NT][NC], ref[NT][NC];   // sum of weights; reference of the exponentials minus 64
 };
 
 // Mathematics.  With a key row held as s_g n_c + m_g per group g of 64 channels,
 //     q . k = sum_g ( s_g (q . n)_g + m_g (sum of q)_g )
-// so the codes go into the tensor core as they are (OFFSET + n, exact in 16 bits, the offset taken out
-// through the accumulator's start value) and step and minimum are applied to the 16 x 8 result.  The
-// same for values: sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j, the weight p_j s_j entering as
-// two bf16 parts (hi + lo, 2^-17 relative) and OFFSET * sum_j p_j s_j taken out by one product with a
-// constant matrix, from the very same rounded weights.  Keys are the M side of both products (16 keys
+// so the codes go into the tensor core as they are and step and minimum are applied to the 16 x 8
+// result.  The same for values: sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j, the weight p_j s_j
+// entering as two bf16 parts (hi + lo, 2^-16 relative).  Keys are the M side of both products (16 keys
 // or 16 channels), the columns the N side: with 4 columns the two parts of a weight fill the 8 columns
 // of one product, so the second part is free.
 //
-// A warp works alone on tiles of 16 keys (2.3 KB at d = 128) through its own ring of cp.async stages;
-// warps meet only when a sequence's share ends.  The reference of the exponentials moves only when a
-// score exceeds it by 2^8: one vote per tile instead of a reduction.
+// A warp works alone on tiles of 16 keys (2.3 KB at d = 128), two at a time, through its own ring of
+// cp.async stages; warps meet only when a sequence's share ends.  The reference of the exponentials
+// moves only when a score exceeds it by 2^8: one vote per step instead of a reduction.
 //
 // Channels are matched to the fragments so that no code moves between lanes: key codes of lane quarter
 // t are channels 64 g + 16 t .. + 15, value codes of lane group r channels 64 g + 8 r .. + 7.
 template <int DT, int D, int SHAPE>
 __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_attend_kernel(const __grid_constant__ Q4Args a) {
     constexpr bool PACKED = SHAPE == COLS_4;
-    constexpr int NT = SHAPE == COLS_16 ? 2 : 1;
-    constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2;
-    constexpr int STAGE = q4_stage_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4;
-    constexpr uint32_t ONES = 0x43004300u;               // 128, 128 in bf16
+    constexpr int NT = SHAPE == COLS_16 ? 2 : 1, U = Q4_PAIR;
+    constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2, PARTS = PACKED ? 1 : 2;
+    constexpr int TILE = q4_tile_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4, RING = Q4_STAGES * U * TILE;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int s_start[3];                           // sequence, units before it (two words: 64 bits are not needed)
-    __shared__ int s_scan[Q4_WARPS + 1];
+    __shared__ int s_start[3];                           // sequence, its units before this share, its length
+    __shared__ int s_scan[Q4_WARPS];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, t4 = lane & 3, r8 = lane >> 2;
     const int per_seq = a.pg.H_kv * a.col_tiles;
 
     // Units before each sequence: every CTA adds up the lengths itself.  First the total, then the
-    // sequence in which this CTA's share begins.
-    long long U = 0, u = 0, u_end = 0, before = 0;
-    int b = 0, shares = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        long long run = 0;
-        for (int b0 = 0; b0 < a.B; b0 += Q4_THREADS) {
-            const int bb = b0 + tid;
-            int v = bb < a.B ? q4_span(a, bb).units * per_seq : 0;
-            int incl = v;
+    // sequence in which this CTA's share begins (the lengths are still in registers for up to 256
+    // sequences).
+    long long total = 0, u = 0, u_end = 0;
+    int shares = 0;
+    {
+        int len = 0, v = 0, before_me = 0;
+        for (int pass = 0; pass < 2; ++pass) {
+            long long run = 0;
+            for (int b0 = 0; b0 < a.B; b0 += Q4_THREADS) {
+                const int bb = b0 + tid;
+                if (pass == 0 || a.B > Q4_THREADS) {
+                    len = bb < a.B ? a.seq_lens[bb] : 0;
+                    v = q4_span(a, len).units * per_seq;
+                    int incl = v;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int w = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += w;
-            }
-            if (lane == 31) s_scan[warp] = incl;
-            __syncthreads();
-            int base = 0, tot = 0;
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int w = __shfl_up_sync(0xffffffffu, incl, o);
+                        if (lane >= o) incl += w;
+                    }
+                    if (lane == 31) s_scan[warp] = incl;
+                    __syncthreads();
+                    int base = 0, all = 0;
 #pragma unroll
-            for (int w = 0; w < Q4_WARPS; ++w) {
-                if (w < warp) base += s_scan[w];
-                tot += s_scan[w];
+                    for (int w = 0; w < Q4_WARPS; ++w) {
+                        if (w < warp) base += s_scan[w];
+                        all += s_scan[w];
+                    }
+                    before_me = base + incl - v;
+                    if (pass == 0) total += all;
+                    else if (u >= run + before_me && u < run + before_me + v) { s_start[0] = bb; s_start[1] = (int)(u - run) - before_me; s_start[2] = len; }
+                    run += all;
+                    __syncthreads();
+                } else if (u >= before_me && u < before_me + v) {
+                    s_start[0] = bb; s_start[1] = (int)u - before_me; s_start[2] = len;
+                }
             }
-            if (pass == 1) {
-                const long long lo = run + base + incl - v;
-                if (v > 0 && u >= lo && u < lo + v) { s_start[0] = bb; s_start[1] = (int)(u - lo); }
+            if (pass == 0) {
+                shares = total < a.grid ? (int)total : a.grid;
+                if ((int)blockIdx.x >= shares) return;
+                u = q4_share(total, shares, blockIdx.x);
+                u_end = q4_share(total, shares, blockIdx.x + 1);
             }
-            run += tot;
-            __syncthreads();
         }
-        if (pass == 0) {
-            U = run;
-            shares = U < a.grid ? (int)U : a.grid;
-            if ((int)blockIdx.x >= shares) return;
-            u = q4_share(U, shares, blockIdx.x);
-            u_end = q4_share(U, shares, blockIdx.x + 1);
-        }
+        __syncthreads();
     }
-    b = s_start[0];
-    before = u - s_start[1];                             // units before sequence b
-    Span sp = q4_span(a, b);
+    int b = s_start[0];
+    long long before = u - s_start[1];                   // units before sequence b
+    Span sp = q4_span(a, s_start[2]);
     const long long u_begin = u;
 
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (Q4_STAGES * STAGE);
-    unsigned char* ring_p = smem + warp * (Q4_STAGES * STAGE);
+    unsigned char* ring = smem + warp * RING;
+    const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
     float* s_merge = reinterpret_cast<float*>(smem);
+
+    // Where this lane's codes lie in a block of 16 rows whose 128-byte lines have their 16-byte slots
+    // exchanged by line (slot ^ 2 (line mod 4)), so that every read below touches each bank once.
+    // Keys: row r8, byte 8 t4 of a group's 32.  Values: row 2 t4, byte 4 r8.
+    auto swz = [](int r, int x) -> int {
+        const int lin = r * (D / 2) + x, line = lin >> 7;
+        return (line << 7) + ((((lin >> 4) & 7) ^ (2 * (line & 3))) << 4) + (lin & 15);
+    };
+    const int k_off = swz(r8, 8 * t4), v_off = swz(2 * t4, 4 * r8);
+    constexpr int ROW8 = 8 * D / 2;                      // 8 rows on: for d = 64 the exchange differs by 4 slots
+    constexpr int ROW8_X = D == 64 ? 64 : 0;
+    constexpr int ROW1_X = D / 2;                        // the odd row of a pair: its slot bit
 
     while (u < u_end) {
         while (u >= before + (long long)sp.units * per_seq) {
             before += (long long)sp.units * per_seq;
             ++b;
-            sp = q4_span(a, b);
+            sp = q4_span(a, a.seq_lens[b]);
         }
         const int in_seq = (int)(u - before);
         const int item = in_seq / sp.units, k_unit = in_seq - item * sp.units;
@@ -574,44 +613,44 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             return r < 0 ? -1 : r + (long long)h * a.pg.page_size;
         };
         long long rows_now = tile_row(lane), rows_next = tile_row(32 + lane);
-        uint32_t bad_now = 0;                            // stages whose page was out of range, one bit each
+        uint32_t bad_bits = 0;                           // tiles of the ring that hold no keys
 
-        auto issue = [&](int i) {
-            if (i < n_tiles) {
-                if (i > 0 && (i & 31) == 0) {
+        auto issue = [&](int step, int st) {             // tiles of `step` into stage st
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const int i = step * U + x;
+                if (x == 0 && step > 0 && (i & 31) == 0) {
                     rows_now = rows_next;
                     rows_next = tile_row(i + 32 + lane);
                 }
                 const long long row = __shfl_sync(0xffffffffu, rows_now, i & 31);
-                const int st = i % Q4_STAGES;
-                const uint32_t dst = ring + st * STAGE;
-                const bool ok = row >= 0;
-                bad_now = (bad_now & ~(1u << st)) | (ok ? 0u : 1u << st);
-                const long long rr = ok ? row : 0;
-                const uint32_t nb = ok ? 16u : 0u;
-                const unsigned char* kp = a.pg.k + rr * (D / 2);
-                const unsigned char* vp = a.pg.v + rr * (D / 2);
+                const uint32_t bit = 1u << (st * U + x);
+                bad_bits = row < 0 ? bad_bits | bit : bad_bits & ~bit;
+                if (row >= 0) {
+                    const uint32_t dst = ring_s + (st * U + x) * TILE;
+                    const unsigned char* kp = a.pg.k + row * (D / 2) + lane * 16;
+                    const unsigned char* vp = a.pg.v + row * (D / 2) + lane * 16;
 #pragma unroll
-                for (int c = lane; c < KB / 16; c += 32) {
-                    // 128-byte lines with their 16-byte slots exchanged by line: the fragment reads
-                    // below then touch every bank once
-                    const uint32_t o = (uint32_t)((c >> 3) * 128 + (((c & 7) ^ (2 * ((c >> 3) & 3))) * 16));
-                    cp_async16_zfill(dst + o, kp + c * 16, nb);
-                    cp_async16_zfill(dst + KB + o, vp + c * 16, nb);
+                    for (int c = 0; c < KB / 512; ++c) {
+                        const int cc = lane + 32 * c;
+                        const uint32_t o = (uint32_t)((cc >> 3) * 128 + (((cc & 7) ^ (2 * ((cc >> 3) & 3))) * 16));
+                        cp_async16(dst + o, kp + c * 512);
+                        cp_async16(dst + KB + o, vp + c * 512);
+                    }
+                    if (lane < SB / 8)
+                        cp_async16(dst + 2 * KB + lane * 16, (lane < SB / 16 ? a.pg.ks : a.pg.vs - SB) + row * (NG * 4) + lane * 16);
                 }
-                if (lane < SB / 16) cp_async16_zfill(dst + 2 * KB + lane * 16, a.pg.ks + rr * (NG * 4) + lane * 16, nb);
-                else if (lane < SB / 8) cp_async16_zfill(dst + 2 * KB + lane * 16, a.pg.vs + rr * (NG * 4) + (lane - SB / 16) * 16, nb);
             }
             cp_async_commit();
         };
+        const int n_steps = (n_tiles + U - 1) / U;
 #pragma unroll
-        for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i);
+        for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i, i);
 
         // ---- queries of this column tile ------------------------------------------------------
         // fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n)
         uint32_t qf[NT][NG][4][2];
         float qsum[NT][NG][NC];
-        int lim[NT][NC], low[NT][NC];                    // keys [low, lim) count for a column
         const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -624,34 +663,28 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                 float s = 0.f;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j);
-                    // channels (0,4) (1,5) (2,6) (3,7) of the eight
-                    qf[nt][g][2 * j][0] = __byte_perm(x.x, x.z, 0x5410);
-                    qf[nt][g][2 * j][1] = __byte_perm(x.x, x.z, 0x7632);
-                    qf[nt][g][2 * j + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-                    qf[nt][g][2 * j + 1][1] = __byte_perm(x.y, x.w, 0x7632);
                     float f[8];
-                    unpack8<DT>(x, f);
+                    unpack8<DT>(*reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j), f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s += f[e];
+                    // channels (0,4) (1,5) (2,6) (3,7) of the eight, in the units of their codes
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float c = q_scale<DT>() * (DT == TYPE_BF16 && (e & 1) ? 0.0625f : 1.f);
+                        qf[nt][g][2 * j + (e >> 1)][e & 1] = pack2<DT>(f[e] * c, f[e + 4] * c);
+                    }
                 }
                 s += __shfl_xor_sync(0xffffffffu, s, 1);
                 s += __shfl_xor_sync(0xffffffffu, s, 2);
                 // lanes hold columns 2 t4 + c of the result
 #pragma unroll
-                for (int c = 0; c < NC; ++c) qsum[nt][g][c] = __shfl_sync(0xffffffffu, s, (2 * t4 + c) * 4);
-            }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
-                const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
-                lim[nt][c] = sp.len - a.T + 1 + tk;
-                low[nt][c] = a.window > 0 && lim[nt][c] > a.window ? (int)(lim[nt][c] - a.window) : 0;
+                for (int c = 0; c < NC; ++c) qsum[nt][g][c] = __shfl_sync(0xffffffffu, s, (2 * t4 + c) * 4) / score_unit<DT>();
             }
         }
         // keys below safe_end and from safe_lo on count for every column
         const int safe_end = sp.len - a.T + 1;
         const int safe_lo = a.window > 0 && sp.len > a.window ? (int)(sp.len - a.window) : 0;
+        const float unit = a.scale_log2 * score_unit<DT>();
 
         Q4State<D, NT, PACKED> st;
 #pragma unroll
@@ -659,11 +692,9 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int m = 0; m < 4; ++m)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) st.o[g][m][nt][e] = 0.f;
-                    st.off[g][nt][e] = 0.f;
-                }
+                    for (int e = 0; e < 4; ++e) st.o[g][m][nt][e] = 0.f;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) st.msum[g][nt][c] = 0.f;
             }
@@ -671,90 +702,98 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             for (int c = 0; c < NC; ++c) { st.l[nt][c] = 0.f; st.ref[nt][c] = Q4_NONE; }
         }
 
-        for (int i = 0; i < n_tiles; ++i) {
+        int stage = 0;
+        for (int step = 0; step < n_steps; ++step) {
             cp_async_wait<Q4_STAGES - 2>();
             __syncwarp();
-            const int sidx = i % Q4_STAGES;
-            const bool bad = (bad_now >> sidx) & 1u;
-            issue(i + Q4_STAGES - 1);                    // into the stage that the previous tile left
-            const unsigned char* sk = ring_p + sidx * STAGE;
-            const unsigned char* sv = sk + KB;
-            const uint32_t* ssk = reinterpret_cast<const uint32_t*>(sk + 2 * KB);
-            const uint32_t* ssv = ssk + Q4_TILE * NG;
-            const int kbase = key0 + (i * Q4_WARPS + warp) * Q4_TILE;
-            // offset of byte x of row r in a swizzled block
-            auto sw = [](int r, int x) -> int {
-                const int lin = r * (D / 2) + x, line = lin >> 7;
-                return (line << 7) + ((((lin >> 4) & 7) ^ (2 * (line & 3))) << 4) + (lin & 15);
-            };
+            const uint32_t bad2 = (bad_bits >> (stage * U)) & ((1u << U) - 1);
+            const unsigned char* blk = ring + stage * (U * TILE);
+            // the next tiles go into the stage that the previous step left
+            issue(step + Q4_STAGES - 1, stage == 0 ? Q4_STAGES - 1 : stage - 1);
+            stage = stage == Q4_STAGES - 1 ? 0 : stage + 1;
+            const int kbase = key0 + (step * U * Q4_WARPS + warp) * Q4_TILE;
 
-            // ---- scores of 16 keys ------------------------------------------------------------
-            float sc[NT][2][NC];                         // rows r8 and r8 + 8
+            // ---- scores --------------------------------------------------------------------------
+            float sc[U][NT][2][NC];                      // rows r8 and r8 + 8, in powers of two
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int x = 0; x < U; ++x) {
+                const unsigned char* sk = blk + x * TILE;
+                const uint32_t* ssk = reinterpret_cast<const uint32_t*>(sk + 2 * KB);
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int g = 0; g < NG; ++g) {
+                    const uint2 w0 = *reinterpret_cast<const uint2*>(sk + (k_off ^ (32 * g)));
+                    const uint2 w8 = *reinterpret_cast<const uint2*>(sk + ((k_off ^ (32 * g) ^ ROW8_X) + ROW8));
+                    float acc[NT][4];
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) sc[nt][r][c] = 0.f;
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const uint2 x = *reinterpret_cast<const uint2*>(sk + sw(r8, g * 32 + 8 * t4));
-                const uint2 y = *reinterpret_cast<const uint2*>(sk + sw(r8 + 8, g * 32 + 8 * t4));
-                float acc[NT][4];
+                        for (int e = 0; e < 4; ++e) acc[nt][e] = 0.f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t c0[4], c8[4];
+                        codes8<DT>(j ? w0.y : w0.x, c0);
+                        codes8<DT>(j ? w8.y : w8.x, c8);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[nt][e] = -code_offset<DT>() * qsum[nt][g][PACKED ? 0 : (e & 1)];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t xw = j ? x.y : x.x, yw = j ? y.y : y.x;
-                    const uint32_t x0 = codes2<DT, 0>(xw), x1 = codes2<DT, 1>(xw), x2 = codes2<DT, 2>(xw), x3 = codes2<DT, 3>(xw);
-                    const uint32_t y0 = codes2<DT, 0>(yw), y1 = codes2<DT, 1>(yw), y2 = codes2<DT, 2>(yw), y3 = codes2<DT, 3>(yw);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma16816<DT>(acc[nt], x0, y0, x1, y1, qf[nt][g][2 * j][0], qf[nt][g][2 * j][1]);
-                        mma16816<DT>(acc[nt], x2, y2, x3, y3, qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma16816<DT>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2 * j][0], qf[nt][g][2 * j][1]);
+                            mma16816<DT>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
+                        }
                     }
+                    const float2 s0 = unpack2<TYPE_BF16>(ssk[r8 * NG + g]), s8 = unpack2<TYPE_BF16>(ssk[(r8 + 8) * NG + g]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const float p0 = fmaf(s0.x, acc[nt][c], s0.y * qsum[nt][g][c]);
+                            const float p8 = fmaf(s8.x, acc[nt][2 + c], s8.y * qsum[nt][g][c]);
+                            sc[x][nt][0][c] = g == 0 ? p0 : sc[x][nt][0][c] + p0;
+                            sc[x][nt][1][c] = g == 0 ? p8 : sc[x][nt][1][c] + p8;
+                        }
                 }
-                const float2 s0 = unpack2<TYPE_BF16>(ssk[r8 * NG + g]), s1 = unpack2<TYPE_BF16>(ssk[(r8 + 8) * NG + g]);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        sc[nt][0][c] += s0.x * acc[nt][c] + s0.y * qsum[nt][g][c];
-                        sc[nt][1][c] += s1.x * acc[nt][2 + c] + s1.y * qsum[nt][g][c];
-                    }
             }
 
-            // ---- weights -----------------------------------------------------------------------
-            const bool edge = bad || kbase + Q4_TILE > safe_end || kbase < safe_lo;
+            // ---- weights -------------------------------------------------------------------------
+            const int last = kbase + (U - 1) * Q4_UNIT + Q4_TILE;
+            const bool edge = bad2 != 0 || last > safe_end || kbase < safe_lo;
             bool grow = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int c = 0; c < NC; ++c) {
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        float x = sc[nt][r][c] * a.scale_log2;
-                        if (edge) {
-                            const int key = kbase + r8 + 8 * r;
-                            if (bad || key >= lim[nt][c] || key < low[nt][c]) x = -INFINITY;
-                        }
-                        sc[nt][r][c] = x;
-                        grow |= x > st.ref[nt][c] + 8.f;
+                    for (int x = 0; x < U; ++x) { sc[x][nt][0][c] *= unit; sc[x][nt][1][c] *= unit; }
+                    if (edge) {
+                        const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
+                        const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
+                        const int lim = sp.len - a.T + 1 + tk;              // keys [low, lim) count
+                        const int low = a.window > 0 && lim > a.window ? (int)(lim - a.window) : 0;
+#pragma unroll
+                        for (int x = 0; x < U; ++x)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const int key = kbase + x * Q4_UNIT + r8 + 8 * r;
+                                if (((bad2 >> x) & 1u) || key >= lim || key < low) sc[x][nt][r][c] = -INFINITY;
+                            }
                     }
+                    float mx = fmaxf(sc[0][nt][0][c], sc[0][nt][1][c]);
+#pragma unroll
+                    for (int x = 1; x < U; ++x) mx = fmaxf(mx, fmaxf(sc[x][nt][0][c], sc[x][nt][1][c]));
+                    grow |= mx > st.ref[nt][c] + 72.f;                      // 8 above the reference
+                }
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float f[NC];
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
-                        float mx = fmaxf(sc[nt][0][c], sc[nt][1][c]);
+                        float mx = fmaxf(sc[0][nt][0][c], sc[0][nt][1][c]);
+#pragma unroll
+                        for (int x = 1; x < U; ++x) mx = fmaxf(mx, fmaxf(sc[x][nt][0][c], sc[x][nt][1][c]));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        mx = fmaxf(mx, st.ref[nt][c]);
-                        f[c] = exp2f(st.ref[nt][c] - mx);
+                        mx = fmaxf(mx - 64.f, st.ref[nt][c]);
+                        f[c] = ex2(st.ref[nt][c] - mx);
                         st.ref[nt][c] = mx;
                         st.l[nt][c] *= f[c];
                     }
@@ -763,87 +802,84 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
 #pragma unroll
                         for (int c = 0; c < NC; ++c) st.msum[g][nt][c] *= f[c];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float fe = f[PACKED ? 0 : (e & 1)];
-                            st.off[g][nt][e] *= fe;
+                        for (int m = 0; m < 4; ++m)
 #pragma unroll
-                            for (int m = 0; m < 4; ++m) st.o[g][m][nt][e] *= fe;
-                        }
+                            for (int e = 0; e < 4; ++e) st.o[g][m][nt][e] *= f[PACKED ? 0 : (e & 1)];
                     }
                 }
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    sc[nt][0][c] = exp2f(sc[nt][0][c] - st.ref[nt][c]);
-                    sc[nt][1][c] = exp2f(sc[nt][1][c] - st.ref[nt][c]);
-                    st.l[nt][c] += sc[nt][0][c] + sc[nt][1][c];
-                }
-
-            // ---- values ------------------------------------------------------------------------
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                float2 v0 = unpack2<TYPE_BF16>(ssv[r8 * NG + g]), v1 = unpack2<TYPE_BF16>(ssv[(r8 + 8) * NG + g]);
-                if (edge) {                              // rows that hold no key may hold anything
-                    if (bad || kbase + r8 >= sp.len) v0 = make_float2(0.f, 0.f);
-                    if (bad || kbase + r8 + 8 >= sp.len) v1 = make_float2(0.f, 0.f);
-                }
-                uint32_t bw[NT][PACKED ? 1 : 2][2];      // [part][rows 0-7, 8-15], transposed to the N side
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float2 v = r ? v1 : v0;
-                        if (PACKED) {
-                            const float w = sc[nt][r][0] * v.x;
-                            const float hi = __bfloat162float(__float2bfloat16_rn(w));
-                            bw[nt][0][r] = movmatrix(pack2<TYPE_BF16>(hi, w - hi));
-                            st.msum[g][nt][0] += sc[nt][r][0] * v.y;
-                        } else {
-                            const float w0 = sc[nt][r][0] * v.x, w1 = sc[nt][r][NC - 1] * v.x;
-                            const uint32_t hi = pack2<TYPE_BF16>(w0, w1);
-                            const float2 hf = unpack2<TYPE_BF16>(hi);
-                            bw[nt][0][r] = movmatrix(hi);
-                            bw[nt][PACKED ? 0 : 1][r] = movmatrix(pack2<TYPE_BF16>(w0 - hf.x, w1 - hf.y));
-                            st.msum[g][nt][0] += sc[nt][r][0] * v.y;
-                            st.msum[g][nt][NC - 1] += sc[nt][r][NC - 1] * v.y;
-                        }
-                    }
-                }
-                // codes of keys 2 t4, 2 t4 + 1, + 8, + 9 for channels 64 g + 8 r8 .. + 7
-                const int x = g * 32 + 4 * r8;
-                const uint32_t w0 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4, x));
-                const uint32_t w1 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 1, x));
-                const uint32_t w8 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 8, x));
-                const uint32_t w9 = *reinterpret_cast<const uint32_t*>(sv + sw(2 * t4 + 9, x));
-                const uint32_t lo01 = __byte_perm(w0, w1, 0x5410), hi01 = __byte_perm(w0, w1, 0x7632);
-                const uint32_t lo89 = __byte_perm(w8, w9, 0x5410), hi89 = __byte_perm(w8, w9, 0x7632);
-                constexpr int BF = TYPE_BF16;
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const uint32_t p01 = hh ? hi01 : lo01, p89 = hh ? hi89 : lo89;
-                    const uint32_t c0 = codes2<BF, 0>(p01), c1 = codes2<BF, 1>(p01), c2 = codes2<BF, 2>(p01), c3 = codes2<BF, 3>(p01);
-                    const uint32_t e0 = codes2<BF, 0>(p89), e1 = codes2<BF, 1>(p89), e2 = codes2<BF, 2>(p89), e3 = codes2<BF, 3>(p89);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int part = 0; part < (PACKED ? 1 : 2); ++part) {
-                            mma16816<BF>(st.o[g][2 * hh][nt], c0, c1, e0, e1, bw[nt][part][0], bw[nt][part][1]);
-                            mma16816<BF>(st.o[g][2 * hh + 1][nt], c2, c3, e2, e3, bw[nt][part][0], bw[nt][part][1]);
-                        }
-                }
+            for (int x = 0; x < U; ++x)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int part = 0; part < (PACKED ? 1 : 2); ++part)
-                        mma16816<BF>(st.off[g][nt], ONES, ONES, ONES, ONES, bw[nt][part][0], bw[nt][part][1]);
+                    for (int c = 0; c < NC; ++c) {
+                        sc[x][nt][0][c] = ex2(sc[x][nt][0][c] - st.ref[nt][c]);
+                        sc[x][nt][1][c] = ex2(sc[x][nt][1][c] - st.ref[nt][c]);
+                        st.l[nt][c] += sc[x][nt][0][c] + sc[x][nt][1][c];
+                    }
+
+            // ---- values --------------------------------------------------------------------------
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const unsigned char* sv = blk + x * TILE + KB;
+                const uint32_t* ssv = reinterpret_cast<const uint32_t*>(blk + x * TILE + 2 * KB + SB);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float2 v0 = unpack2<TYPE_BF16>(ssv[r8 * NG + g]), v8 = unpack2<TYPE_BF16>(ssv[(r8 + 8) * NG + g]);
+                    if (edge) {                          // rows that hold no key may hold anything
+                        const int key = kbase + x * Q4_UNIT + r8;
+                        if (((bad2 >> x) & 1u) || key >= sp.len) v0 = make_float2(0.f, 0.f);
+                        if (((bad2 >> x) & 1u) || key + 8 >= sp.len) v8 = make_float2(0.f, 0.f);
+                    }
+                    // weights transposed to the N side: [part][rows 0-7, 8-15]; the second part is what
+                    // cutting the first to 16 bits left over
+                    uint32_t bw[NT][PARTS][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float2 v = r ? v8 : v0;
+                            const float w0 = sc[x][nt][r][0] * v.x;
+                            const float d0 = w0 - __uint_as_float(__float_as_uint(w0) & 0xffff0000u);
+                            st.msum[g][nt][0] = fmaf(sc[x][nt][r][0], v.y, st.msum[g][nt][0]);
+                            if (PACKED) {
+                                bw[nt][0][r] = movmatrix(__byte_perm(__float_as_uint(w0), __float_as_uint(d0), 0x7632));
+                            } else {
+                                const float w1 = sc[x][nt][r][NC - 1] * v.x;
+                                const float d1 = w1 - __uint_as_float(__float_as_uint(w1) & 0xffff0000u);
+                                st.msum[g][nt][NC - 1] = fmaf(sc[x][nt][r][NC - 1], v.y, st.msum[g][nt][NC - 1]);
+                                bw[nt][0][r] = movmatrix(__byte_perm(__float_as_uint(w0), __float_as_uint(w1), 0x7632));
+                                bw[nt][PARTS - 1][r] = movmatrix(__byte_perm(__float_as_uint(d0), __float_as_uint(d1), 0x7632));
+                            }
+                        }
+                    // codes of keys 2 t4, 2 t4 + 1, + 8, + 9 for channels 64 g + 8 r8 .. + 7
+                    const int o = v_off ^ (32 * g);
+                    const uint32_t w0 = *reinterpret_cast<const uint32_t*>(sv + o);
+                    const uint32_t w1 = *reinterpret_cast<const uint32_t*>(sv + (o ^ ROW1_X));
+                    const uint32_t w8 = *reinterpret_cast<const uint32_t*>(sv + ((o ^ ROW8_X) + ROW8));
+                    const uint32_t w9 = *reinterpret_cast<const uint32_t*>(sv + ((o ^ ROW1_X ^ ROW8_X) + ROW8));
+                    constexpr int BF = TYPE_BF16;
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        uint32_t c0[4], c8[4];
+                        codes8<BF>(__byte_perm(w0, w1, hh ? 0x7632 : 0x5410), c0);
+                        codes8<BF>(__byte_perm(w8, w9, hh ? 0x7632 : 0x5410), c8);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int part = 0; part < PARTS; ++part) {
+                                mma16816<BF>(st.o[g][2 * hh][nt], c0[0], c0[1], c8[0], c8[1], bw[nt][part][0], bw[nt][part][1]);
+                                mma16816<BF>(st.o[g][2 * hh + 1][nt], c0[2], c0[3], c8[2], c8[3], bw[nt][part][0], bw[nt][part][1]);
+                            }
+                    }
+                }
             }
         }
         cp_async_wait<0>();
 
         // ---- join the warps ---------------------------------------------------------------------
-        // sums over the lanes that share columns (rows of the tiles)
+        // sums over the lanes that share columns (rows of the tiles); the 2^64 of the weights goes here
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -854,6 +890,9 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
 #pragma unroll
                     for (int g = 0; g < NG; ++g) st.msum[g][nt][c] += __shfl_xor_sync(0xffffffffu, st.msum[g][nt][c], o);
                 }
+                st.l[nt][c] *= 1.f / TWO64;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) st.msum[g][nt][c] *= 1.f / TWO64;
             }
         __syncthreads();                                 // every warp is done with its ring
         // [warp][col][D], then [warp][col] reference and sum
@@ -871,9 +910,9 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                     for (int m = 0; m < 4; ++m)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {    // accumulator rows r8 and r8 + 8: channels 2 m and 2 m + 1
-                            float x = st.o[g][m][nt][2 * e + c] - st.off[g][nt][2 * e + c];
-                            if (PACKED) x += st.o[g][m][nt][2 * e + 1] - st.off[g][nt][2 * e + 1];
-                            dst[g * GROUP + 8 * r8 + 2 * m + e] = x + st.msum[g][nt][c];
+                            float x = st.o[g][m][nt][2 * e + c];
+                            if (PACKED) x += st.o[g][m][nt][2 * e + 1];
+                            dst[g * GROUP + 8 * r8 + 2 * m + e] = fmaf(x, e ? TWO69 / 16.f : TWO69, st.msum[g][nt][c]);
                         }
                 if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
             }
@@ -888,7 +927,7 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             float l = 0.f, o = 0.f;
 #pragma unroll
             for (int w = 0; w < Q4_WARPS; ++w) {
-                const float f = exp2f(s_ref[w * COLS + col] - mx);
+                const float f = ex2(s_ref[w * COLS + col] - mx);
                 l += f * s_l[w * COLS + col];
                 o += f * s_merge[(w * COLS + col) * D + ch];
             }
@@ -897,7 +936,7 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                 const long long row = ((long long)b * a.T + tok) * a.Hq + head;
                 const float y = l > 0.f ? o / l : 0.f;
                 a.out[row * D + ch] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
-                if (a.lse && ch == 0) a.lse[row] = l > 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                if (a.lse && ch == 0) a.lse[row] = l > 0.f ? (mx + 64.f + log2f(l)) * 0.6931471805599453f : -INFINITY;
             } else {
                 part[col * (D + 2) + ch] = o;
                 if (ch == 0) { part[col * (D + 2) + D] = mx; part[col * (D + 2) + D + 1] = l; }
@@ -909,62 +948,76 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
 }
 
 // Joins the parts of items (sequence, KV head, column tile) that more than one CTA worked on, and
-// writes the rows of sequences without keys.  One CTA of D threads per item.
+// writes the rows of sequences without keys.  One CTA of D threads per item and column.
 template <int DT, int D, int SHAPE>
 __global__ void __launch_bounds__(D) q4_combine_kernel(const __grid_constant__ Q4Args a) {
-    constexpr int COLS = q4_cols(SHAPE);
-    __shared__ long long s_sum[2];
+    constexpr int COLS = q4_cols(SHAPE), WARPS = D / 32, AHEAD = 8;
+    __shared__ long long s_sum[2][WARPS];
     const int tid = threadIdx.x, per_seq = a.pg.H_kv * a.col_tiles;
     const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
-    const int h = item / a.col_tiles, ct = item - h * a.col_tiles;
-    if (tid < 2) s_sum[tid] = 0;
-    __syncthreads();
+    const int h = item / a.col_tiles, ct = item - h * a.col_tiles, col = blockIdx.y;
+    const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
+    if (col >= cols_here) return;
     long long mine = 0, all = 0;
     for (int bb = tid; bb < a.B; bb += D) {
-        const int n = q4_span(a, bb).units;
+        const int n = q4_span(a, a.seq_lens[bb]).units;
         all += n;
         if (bb < b) mine += n;
     }
+    const int units = q4_span(a, a.seq_lens[b]).units;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         mine += __shfl_down_sync(0xffffffffu, mine, o);
         all += __shfl_down_sync(0xffffffffu, all, o);
     }
-    if ((tid & 31) == 0) {
-        atomicAdd(reinterpret_cast<unsigned long long*>(&s_sum[0]), (unsigned long long)mine);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&s_sum[1]), (unsigned long long)all);
-    }
+    if ((tid & 31) == 0) { s_sum[0][tid >> 5] = mine; s_sum[1][tid >> 5] = all; }
     __syncthreads();
-    const int units = q4_span(a, b).units;
-    const long long U = s_sum[1] * per_seq, ua = s_sum[0] * per_seq + (long long)item * units, ub = ua + units;
-    const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
-    const int shares = U < a.grid ? (int)U : a.grid;
+    mine = all = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) { mine += s_sum[0][w]; all += s_sum[1][w]; }
+    const long long total = all * per_seq, ua = mine * per_seq + (long long)item * units, ub = ua + units;
+    const int shares = total < a.grid ? (int)total : a.grid;
     int c0 = 0, c1 = -1;
     if (units > 0) {
-        // CTA whose share holds unit x: the largest c with U * c / shares <= x
-        c0 = (int)(((ua + 1) * shares + U - 1) / U) - 1;
-        c1 = (int)((ub * shares + U - 1) / U) - 1;
+        // CTA whose share holds unit x: the largest c with total * c / shares <= x
+        c0 = (int)(((ua + 1) * shares + total - 1) / total) - 1;
+        c1 = (int)((ub * shares + total - 1) / total) - 1;
         if (c0 == c1) return;                            // one CTA had it all and wrote it
     }
-    for (int col = 0; col < cols_here; ++col) {
-        float mx = Q4_NONE;
-        for (int c = c0; c <= c1; ++c) {
-            const float* p = a.part + ((long long)(2 * c + (ua > q4_share(U, shares, c) ? 1 : 0)) * COLS + col) * (D + 2);
-            mx = fmaxf(mx, p[D]);
+    // only the first CTA can have begun another item before this one
+    const float* p0 = a.part + ((long long)(2 * c0 + (units > 0 && ua > q4_share(total, shares, c0) ? 1 : 0)) * COLS + col) * (D + 2);
+    const float* p1 = a.part + ((long long)(2 * (c0 + 1)) * COLS + col) * (D + 2);
+    constexpr long long NEXT = 2ll * COLS * (D + 2);
+    float mx = Q4_NONE, l = 0.f, o = 0.f;
+    for (int c = c0; c <= c1; c += AHEAD) {
+        float m[AHEAD], s[AHEAD], x[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const bool in = c + i <= c1;
+            const float* p = c + i == c0 ? p0 : p1 + (long long)(c + i - c0 - 1) * NEXT;
+            m[i] = in ? p[D] : Q4_NONE;
+            s[i] = in ? p[D + 1] : 0.f;
+            x[i] = in ? p[tid] : 0.f;
         }
-        float l = 0.f, o = 0.f;
-        for (int c = c0; c <= c1; ++c) {
-            const float* p = a.part + ((long long)(2 * c + (ua > q4_share(U, shares, c) ? 1 : 0)) * COLS + col) * (D + 2);
-            const float f = exp2f(p[D] - mx);
-            l += f * p[D + 1];
-            o += f * p[tid];
+        float top = mx;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, m[i]);
+        const float f = ex2(mx - top);
+        l *= f;
+        o *= f;
+        mx = top;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float g = ex2(m[i] - top);
+            l = fmaf(g, s[i], l);
+            o = fmaf(g, x[i], o);
         }
-        const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
-        const long long row = ((long long)b * a.T + tok) * a.Hq + head;
-        const float y = l > 0.f ? o / l : 0.f;
-        a.out[row * D + tid] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
-        if (a.lse && tid == 0) a.lse[row] = l > 0.f ? (mx + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
+    const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
+    const long long row = ((long long)b * a.T + tok) * a.Hq + head;
+    const float y = l > 0.f ? o / l : 0.f;
+    a.out[row * D + tid] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
+    if (a.lse && tid == 0) a.lse[row] = l > 0.f ? (mx + 64.f + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 }  // namespace retopk_cache
