@@ -102,7 +102,24 @@ int device_sms(int* num_sms) {
     return RETOPK_OK;
 }
 
-int launched() { return cudaGetLastError() == cudaSuccess ? RETOPK_OK : RETOPK_ECUDA; }
+// Launch with programmatic stream serialisation: the kernel may be set up while its predecessor in
+// the stream still runs; it waits (pdl_wait) before it touches memory.
+template <class Args>
+int launch(void (*kernel)(Args), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, const Args& a) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) { cudaGetLastError(); return RETOPK_ECUDA; }
+    return RETOPK_OK;
+}
 
 void set_rotation(RowsArgs& a, const retopk_rope* rope, int inverse) {
     if (!rope) return;
@@ -123,24 +140,20 @@ template <int DEST> int launch_rows(RowsArgs& a, int dtype, int d, int num_sms, 
     const long long gx = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
     if (gx > 2147483647ll || a.units > 65535) return RETOPK_EUNSUPPORTED;
     const dim3 grid((unsigned)gx, (unsigned)a.units);
-    if (dtype == RETOPK_BF16) {
-        if (d == 128) rows_kernel<TYPE_BF16, 128, DEST><<<grid, ROWS_THREADS, 0, s>>>(a);
-        else rows_kernel<TYPE_BF16, 64, DEST><<<grid, ROWS_THREADS, 0, s>>>(a);
-    } else {
-        if (d == 128) rows_kernel<TYPE_FP16, 128, DEST><<<grid, ROWS_THREADS, 0, s>>>(a);
-        else rows_kernel<TYPE_FP16, 64, DEST><<<grid, ROWS_THREADS, 0, s>>>(a);
-    }
-    return launched();
+    if (dtype == RETOPK_BF16)
+        return d == 128 ? launch(rows_kernel<TYPE_BF16, 128, DEST>, grid, ROWS_THREADS, 0, s, a)
+                        : launch(rows_kernel<TYPE_BF16, 64, DEST>, grid, ROWS_THREADS, 0, s, a);
+    return d == 128 ? launch(rows_kernel<TYPE_FP16, 128, DEST>, grid, ROWS_THREADS, 0, s, a)
+                    : launch(rows_kernel<TYPE_FP16, 64, DEST>, grid, ROWS_THREADS, 0, s, a);
 }
 
 template <int SRC, int DT> int launch_gather(const GatherArgs& a, int d, dim3 grid, cudaStream_t s) {
-    if (d == 128) gather_kernel<SRC, DT, 128><<<grid, GATHER_THREADS, 0, s>>>(a);
-    else gather_kernel<SRC, DT, 64><<<grid, GATHER_THREADS, 0, s>>>(a);
-    return launched();
+    return d == 128 ? launch(gather_kernel<SRC, DT, 128>, grid, GATHER_THREADS, 0, s, a)
+                    : launch(gather_kernel<SRC, DT, 64>, grid, GATHER_THREADS, 0, s, a);
 }
 
 int q4_shape(int columns) { return columns <= 4 ? COLS_4 : (columns <= 8 ? COLS_8 : COLS_16); }
-int q4_ctas(int shape, int num_sms) { return num_sms * (shape == COLS_16 ? 1 : 2); }
+int q4_ctas(int d, int shape, int num_sms) { return num_sms * q4_ctas_per_sm(d, shape); }
 
 int check_q4_shape(int B, int T, int H_q, int H_kv, int d) {
     if (B < 1 || T < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv != 0) return RETOPK_EINVAL;
@@ -149,10 +162,9 @@ int check_q4_shape(int B, int T, int H_q, int H_kv, int d) {
 }
 
 template <int DT, int D, int SHAPE> int launch_q4(const Q4Args& a, int items, cudaStream_t s) {
-    q4_attend_kernel<DT, D, SHAPE><<<a.grid, Q4_THREADS, q4_smem_bytes(D, SHAPE), s>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return RETOPK_ECUDA;
-    q4_combine_kernel<DT, D, SHAPE><<<dim3((unsigned)items, (unsigned)q4_cols(SHAPE)), D, 0, s>>>(a);
-    return launched();
+    const int rc = launch(q4_attend_kernel<DT, D, SHAPE>, dim3((unsigned)a.grid), Q4_THREADS, q4_smem_bytes(D, SHAPE), s, a);
+    if (rc != RETOPK_OK) return rc;
+    return launch(q4_combine_kernel<DT, D, SHAPE>, dim3((unsigned)items, (unsigned)q4_cols(SHAPE)), D, 0, s, a);
 }
 template <int DT, int D> int launch_q4_shape(const Q4Args& a, int shape, int items, cudaStream_t s) {
     if (shape == COLS_4) return launch_q4<DT, D, COLS_4>(a, items, s);
@@ -344,7 +356,7 @@ int64_t retopk_q4_attention_workspace(int B, int T, int H_q, int H_kv, int d) {
     if (rc == RETOPK_OK) rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
     const int shape = q4_shape(T * (H_q / H_kv));
-    return 2ll * q4_ctas(shape, num_sms) * q4_cols(shape) * (d + 2) * 4;
+    return 2ll * q4_ctas(d, shape, num_sms) * q4_cols(shape) * (d + 2) * 4;
 }
 
 int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int dtype,
@@ -360,7 +372,7 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
     Q4Args a;
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
-    if (a.pg.capacity > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    if (a.pg.capacity > MAX_KEYS || pages->n_pages > 0xfffffffell / ((long long)pages->H_kv * pages->page_size)) return RETOPK_EUNSUPPORTED;
     int num_sms = 0;
     rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
@@ -371,13 +383,14 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
     a.part = static_cast<float*>(workspace);
     a.q_stride = q_stride;
     a.window = window;
+    a.two16 = 1u << 16;
     a.scale_log2 = (float)((double)scale * 1.44269504088896340736);
     a.B = B; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv;
     const int columns = T * a.G, shape = q4_shape(columns);
     a.col_tiles = (columns + q4_cols(shape) - 1) / q4_cols(shape);
-    if (workspace_bytes < 2ll * q4_ctas(shape, num_sms) * q4_cols(shape) * (pages->d + 2) * 4) return RETOPK_EINVAL;
+    if (workspace_bytes < 2ll * q4_ctas(pages->d, shape, num_sms) * q4_cols(shape) * (pages->d + 2) * 4) return RETOPK_EINVAL;
     const long long most = (long long)B * pages->H_kv * a.col_tiles * ((a.pg.capacity + Q4_UNIT - 1) / Q4_UNIT);
-    const int ctas = q4_ctas(shape, num_sms);
+    const int ctas = q4_ctas(pages->d, shape, num_sms);
     a.grid = (int)(most < ctas ? most : ctas);
     const int items = B * pages->H_kv * a.col_tiles;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

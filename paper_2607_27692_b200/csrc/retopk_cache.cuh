@@ -53,6 +53,10 @@ template <int DT> __device__ __forceinline__ uint4 pack8(const float* f) {
 __device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
 }
+// Programmatic dependent launch: every kernel here is launched with the stream-serialisation attribute
+// and waits before it touches memory; a kernel that lets its successor start does so after its own wait.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -117,6 +121,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constan
     const int tid = threadIdx.x;
     const long long tok0 = (long long)blockIdx.x * a.tokens_per_cta;
     const int n_tok = (int)(a.n_tokens - tok0 < a.tokens_per_cta ? a.n_tokens - tok0 : a.tokens_per_cta);
+    pdl_wait();
 
     if (tid < n_tok) {
         const long long tok = tok0 + tid;
@@ -331,6 +336,7 @@ struct GatherArgs {
 template <int SRC /* 0 bf16, 1 fp16, 2: four bits */, int DT, int D>
 __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_constant__ GatherArgs a) {
     constexpr int LANES = D / 8, RPP = GATHER_THREADS / LANES, PASSES = GATHER_ROWS / RPP;
+    pdl_wait();
     const int b = blockIdx.z, h = blockIdx.y;
     const long long row0 = (long long)blockIdx.x * GATHER_ROWS;
     const long long first = a.first ? a.first[b] : 0;
@@ -412,6 +418,9 @@ __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
     return ring > merge ? ring : merge;
 }
 
+// Accumulators and queries of 16 columns of 128 channels need more than the 128 registers of two CTAs an SM.
+__host__ __device__ constexpr int q4_ctas_per_sm(int d, int shape) { return shape == COLS_16 && d == 128 ? 1 : 2; }
+
 struct Q4Args {
     Pages pg;
     const int32_t* seq_lens;
@@ -422,9 +431,16 @@ struct Q4Args {
     long long q_stride, window;
     float scale_log2;
     int B, T, Hq, G, col_tiles, grid;
+    uint32_t two16;             // 2^16: a shift as a product
 };
 
-struct Span { int lo, len, units; };     // keys of a sequence: first one read (multiple of 16), end, units
+// What beginning an item costs a CTA (page look-up, queries, first tiles, join), in units: a share counts
+// that much more for every item that begins in it, else the CTAs that get the short sequences of a mixed
+// batch finish last.
+constexpr int Q4_BEGIN = 4;
+
+// keys of a sequence: first one read (multiple of 16), end, units, and what an item counts (0 if empty)
+struct Span { int lo, len, units, weight; };
 __device__ __forceinline__ Span q4_span(const Q4Args& a, int seq_len) {
     Span s;
     long long len = seq_len;
@@ -434,6 +450,7 @@ __device__ __forceinline__ Span q4_span(const Q4Args& a, int seq_len) {
     if (lo < 0) lo = 0;
     s.lo = (int)lo & ~(Q4_TILE - 1);
     s.units = s.len > s.lo ? (s.len - s.lo + Q4_UNIT - 1) / Q4_UNIT : 0;
+    s.weight = s.units > 0 ? s.units + Q4_BEGIN : 0;
     return s;
 }
 // Share c of `grid` in U >= grid units begins here (no share is empty).
@@ -446,49 +463,66 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-template <int DT>
+// c += a * b; FIRST: c = a * b
+template <int DT, bool FIRST = false>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    const float i0 = FIRST ? 0.f : c[0], i1 = FIRST ? 0.f : c[1], i2 = FIRST ? 0.f : c[2], i3 = FIRST ? 0.f : c[3];
     if (DT == TYPE_BF16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(i0), "f"(i1), "f"(i2), "f"(i3));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(i0), "f"(i1), "f"(i2), "f"(i3));
 }
-
-// Codes as operands.  A code n in the low bits of a 16-bit number IS a number: the subnormal n * 2^-133
-// in bf16 (n * 2^-24 in fp16), which the tensor core multiplies exactly.  In bf16 bits 0..7 count up
-// linearly across the first normal exponent, so the second code of a byte stands for 16 n * 2^-133
-// where it is: one mask each and one shift for four pairs.  (fp16 keeps 16 times smaller queries from
-// becoming subnormal by shifting instead.)  No offset, hence no cancellation in the sums.
-template <int DT> __device__ __forceinline__ void codes8(uint32_t x, uint32_t (&c)[4]) {
-    if (DT == TYPE_BF16) {
-        const uint32_t y = x >> 8;
-        c[0] = x & 0x000f000fu;
-        c[1] = x & 0x00f000f0u;          // times 16
-        c[2] = y & 0x000f000fu;
-        c[3] = y & 0x00f000f0u;          // times 16
-    } else {
-        c[0] = x & 0x000f000fu;
-        c[1] = (x >> 4) & 0x000f000fu;
-        c[2] = (x >> 8) & 0x000f000fu;
-        c[3] = (x >> 12) & 0x000f000fu;
-    }
+// Codes as operands: the bits of a code ARE a small number.  In bf16 bits 0..7 count in steps of 2^-133
+// (subnormals, then the first exponent), in fp16 bits 0..10 in steps of 2^-24, and the tensor core
+// multiplies subnormals exactly.  So a mask makes the operand and no offset has to be taken out of the
+// sums again.  A byte b = n0 + 16 n1 goes in as n0 and as b: four instructions for the eight codes of a
+// word instead of the seven of four masks and three shifts.  What b brings too much is put right in the
+// other operand (keys) or once at the end (values).  The kernel is bound by the ALU, where masks,
+// shifts and byte permutations go; measured at 4 x 128K keys: 132 us with n0, 16 n1 and a shift for
+// the upper bytes, 142 us with that shift as a product (its two issue slots cost more), 143 us with
+// e4m3 operands (mma converts them to fp16, on the ALU).
+__device__ __forceinline__ void code_bytes(uint32_t x, uint32_t (&c)[4]) {
+    c[0] = x & 0x000f000fu;                      // codes (0,4)
+    c[1] = __byte_perm(x, 0u, 0x4240);           // bytes 0 and 2: (0,4) + 16 (1,5)
+    c[3] = __byte_perm(x, 0u, 0x4341);           // bytes 1 and 3: (2,6) + 16 (3,7)
+    c[2] = c[3] & 0x000f000fu;                   // codes (2,6)
 }
-// Powers of two that keep products with subnormals in the middle of the fp32 range: bf16 queries are
-// multiplied by 2^64, weights carry 2^64 through the reference of their exponential.
+// The same for the lower or upper half words of two keys: codes 0..3 of the first, of the second.
+__device__ __forceinline__ void pair_bytes(uint32_t z, uint32_t (&c)[4]) {
+    c[0] = z & 0x000f000fu;
+    c[1] = z & 0x00ff00ffu;
+    c[3] = __byte_perm(z, 0u, 0x4341);
+    c[2] = c[3] & 0x000f000fu;
+}
+__device__ __forceinline__ float2 step_min(uint32_t x, uint32_t two16) {
+    return make_float2(__uint_as_float(x * two16), __uint_as_float(x & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+    uint2 x;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(addr) : "memory");
+    return x;
+}
+// Weights carry 2^64 through the reference of their exponentials: it keeps their products with the
+// subnormals in the middle of the fp32 range.
 constexpr float TWO64 = 18446744073709551616.f, TWO69 = 32.f * TWO64;     // 2^-133 * 2^64 = 1 / TWO69
-template <int DT> __host__ __device__ constexpr float q_scale() { return DT == TYPE_BF16 ? TWO64 : 1.f; }
-template <int DT> __host__ __device__ constexpr float score_unit() { return DT == TYPE_BF16 ? TWO69 : 16777216.f; }
 
 // One warp's running state over the keys that it has seen.
 template <int D, int NT, bool PACKED>
 struct Q4State {
     static constexpr int NG = D / GROUP, NC = PACKED ? 1 : 2;
-    float o[NG][4][NT][4];      // codes times weights: channel pairs x columns
+    float o[NG][4][NT][4];      // codes and bytes times weights: channel pairs x columns
     float msum[NG][NT][NC];     // weights times minima, over this lane's rows
     float l[NT][NC], ref[NT][NC];   // sum of weights; reference of the exponentials minus 64
 };
@@ -508,19 +542,21 @@ struct Q4State {
 // Channels are matched to the fragments so that no code moves between lanes: key codes of lane quarter
 // t are channels 64 g + 16 t .. + 15, value codes of lane group r channels 64 g + 8 r .. + 7.
 template <int DT, int D, int SHAPE>
-__global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_attend_kernel(const __grid_constant__ Q4Args a) {
+__global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_attend_kernel(const __grid_constant__ Q4Args a) {
     constexpr bool PACKED = SHAPE == COLS_4;
     constexpr int NT = SHAPE == COLS_16 ? 2 : 1, U = Q4_PAIR;
     constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2, PARTS = PACKED ? 1 : 2;
     constexpr int TILE = q4_tile_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4, RING = Q4_STAGES * U * TILE;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int s_start[3];                           // sequence, its units before this share, its length
+    __shared__ int s_start[3];                           // sequence, its weight before this share, its length
     __shared__ int s_scan[Q4_WARPS];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, t4 = lane & 3, r8 = lane >> 2;
     const int per_seq = a.pg.H_kv * a.col_tiles;
 
-    // Units before each sequence: every CTA adds up the lengths itself.  First the total, then the
+    pdl_wait();
+    pdl_start_next();
+    // Weights before each sequence: every CTA adds up the lengths itself.  First the total, then the
     // sequence in which this CTA's share begins (the lengths are still in registers for up to 256
     // sequences).
     long long total = 0, u = 0, u_end = 0;
@@ -533,7 +569,7 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                 const int bb = b0 + tid;
                 if (pass == 0 || a.B > Q4_THREADS) {
                     len = bb < a.B ? a.seq_lens[bb] : 0;
-                    v = q4_span(a, len).units * per_seq;
+                    v = q4_span(a, len).weight * per_seq;
                     int incl = v;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
@@ -567,12 +603,11 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
         __syncthreads();
     }
     int b = s_start[0];
-    long long before = u - s_start[1];                   // units before sequence b
+    long long before = u - s_start[1];                   // weight before sequence b
     Span sp = q4_span(a, s_start[2]);
     const long long u_begin = u;
 
-    unsigned char* ring = smem + warp * RING;
-    const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * RING;
     float* s_merge = reinterpret_cast<float*>(smem);
 
     // Where this lane's codes lie in a block of 16 rows whose 128-byte lines have their 16-byte slots
@@ -582,23 +617,42 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
         const int lin = r * (D / 2) + x, line = lin >> 7;
         return (line << 7) + ((((lin >> 4) & 7) ^ (2 * (line & 3))) << 4) + (lin & 15);
     };
-    const int k_off = swz(r8, 8 * t4), v_off = swz(2 * t4, 4 * r8);
     constexpr int ROW8 = 8 * D / 2;                      // 8 rows on: for d = 64 the exchange differs by 4 slots
     constexpr int ROW8_X = D == 64 ? 64 : 0;
     constexpr int ROW1_X = D / 2;                        // the odd row of a pair: its slot bit
+    const uint32_t k_at = ring + swz(r8, 8 * t4), v_at = ring + KB + swz(2 * t4, 4 * r8);
+    // the same with the exchanged slots, relative to the first: group 1, the odd row, 8 rows on
+    auto moved = [](uint32_t at, uint32_t base, int x) { return base + ((at - base) ^ x); };
+    uint32_t k_addr[NG][2], v_addr[NG][2][2];            // [group][8 rows on], [group][odd row][8 rows on]
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            k_addr[g][e] = moved(k_at, ring, 32 * g ^ (e ? ROW8_X : 0));
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) v_addr[g][odd][e] = moved(v_at, ring + KB, 32 * g ^ (odd ? ROW1_X : 0) ^ (e ? ROW8_X : 0));
+        }
+    const uint32_t s_addr = ring + 2 * KB + r8 * (NG * 4);
+    // what this lane copies: 16 bytes of every 512 of the codes, and a piece of the scales
+    const uint32_t c_dst = ring + swz(lane * 16 / (D / 2), lane * 16 % (D / 2));
+    const unsigned char* const k_src = a.pg.k + lane * 16;
+    const unsigned char* const v_src = a.pg.v + lane * 16;
+    const unsigned char* const s_src = (lane < SB / 16 ? a.pg.ks : a.pg.vs - SB) + lane * 16;
 
     while (u < u_end) {
-        while (u >= before + (long long)sp.units * per_seq) {
-            before += (long long)sp.units * per_seq;
+        while (u >= before + (long long)sp.weight * per_seq) {
+            before += (long long)sp.weight * per_seq;
             ++b;
             sp = q4_span(a, a.seq_lens[b]);
         }
         const int in_seq = (int)(u - before);
-        const int item = in_seq / sp.units, k_unit = in_seq - item * sp.units;
+        const int item = in_seq / sp.weight, at = in_seq - item * sp.weight;
         const int h = item / a.col_tiles, ct = item - h * a.col_tiles;
-        int n_units = sp.units - k_unit;
-        if (u_end - u < n_units) n_units = (int)(u_end - u);
-        const long long item_start = before + (long long)item * sp.units;
+        const int here = u_end - u < sp.weight - at ? (int)(u_end - u) : sp.weight - at;
+        u += here;
+        const int k_unit = at > Q4_BEGIN ? at - Q4_BEGIN : 0, n_units = at + here - Q4_BEGIN - k_unit;
+        if (n_units <= 0) continue;                      // a share that ends within an item's beginning
+        const long long item_start = before + (long long)item * sp.weight;
         const int key0 = sp.lo + k_unit * Q4_UNIT;
         int key_end = key0 + n_units * Q4_UNIT;
         if (key_end > sp.len) key_end = sp.len;
@@ -607,38 +661,39 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
         const int n_tiles = n_all > warp ? (n_all - warp + Q4_WARPS - 1) / Q4_WARPS : 0;
 
         // ---- page rows of the next 32 tiles, one per lane ------------------------------------
-        auto tile_row = [&](int i) -> long long {
-            if (i >= n_tiles) return -1;
-            const long long r = cache_row(a.pg, b, key0 + ((long long)i * Q4_WARPS + warp) * Q4_TILE);
-            return r < 0 ? -1 : r + (long long)h * a.pg.page_size;
+        // (32 bits: the host refuses caches of 2^32 rows or more.)  A tile whose page is out of range
+        // is read from row 0 and masked; that such a tile exists is remembered for the whole share.
+        bool bad = false;
+        auto row_of = [&](int i) -> long long { return cache_row(a.pg, b, key0 + ((long long)i * Q4_WARPS + warp) * Q4_TILE); };
+        auto tile_row = [&](int i) -> uint32_t {
+            if (i >= n_tiles) return 0u;
+            const long long r = row_of(i);
+            bad |= r < 0;
+            return r < 0 ? 0u : (uint32_t)(r + (long long)h * a.pg.page_size);
         };
-        long long rows_now = tile_row(lane), rows_next = tile_row(32 + lane);
-        uint32_t bad_bits = 0;                           // tiles of the ring that hold no keys
+        uint32_t rows_now = tile_row(lane), rows_next = tile_row(32 + lane);
+        bool some_bad = __any_sync(0xffffffffu, bad);
 
         auto issue = [&](int step, int st) {             // tiles of `step` into stage st
+            if (step > 0 && (step * U & 31) == 0) {
+                rows_now = rows_next;
+                rows_next = tile_row(step * U + 32 + lane);
+                some_bad = __any_sync(0xffffffffu, bad);
+            }
 #pragma unroll
             for (int x = 0; x < U; ++x) {
                 const int i = step * U + x;
-                if (x == 0 && step > 0 && (i & 31) == 0) {
-                    rows_now = rows_next;
-                    rows_next = tile_row(i + 32 + lane);
-                }
-                const long long row = __shfl_sync(0xffffffffu, rows_now, i & 31);
-                const uint32_t bit = 1u << (st * U + x);
-                bad_bits = row < 0 ? bad_bits | bit : bad_bits & ~bit;
-                if (row >= 0) {
-                    const uint32_t dst = ring_s + (st * U + x) * TILE;
-                    const unsigned char* kp = a.pg.k + row * (D / 2) + lane * 16;
-                    const unsigned char* vp = a.pg.v + row * (D / 2) + lane * 16;
+                const uint32_t row = __shfl_sync(0xffffffffu, rows_now, i & 31);
+                if (i < n_tiles) {
+                    const uint32_t dst = c_dst + (st * U + x) * TILE;
+                    const unsigned char* kp = k_src + (uint64_t)row * (D / 2);
+                    const unsigned char* vp = v_src + (uint64_t)row * (D / 2);
 #pragma unroll
                     for (int c = 0; c < KB / 512; ++c) {
-                        const int cc = lane + 32 * c;
-                        const uint32_t o = (uint32_t)((cc >> 3) * 128 + (((cc & 7) ^ (2 * ((cc >> 3) & 3))) * 16));
-                        cp_async16(dst + o, kp + c * 512);
-                        cp_async16(dst + KB + o, vp + c * 512);
+                        cp_async16(dst + c * 512, kp + c * 512);
+                        cp_async16(dst + KB + c * 512, vp + c * 512);
                     }
-                    if (lane < SB / 8)
-                        cp_async16(dst + 2 * KB + lane * 16, (lane < SB / 16 ? a.pg.ks : a.pg.vs - SB) + row * (NG * 4) + lane * 16);
+                    if (lane < SB / 8) cp_async16(ring + (st * U + x) * TILE + 2 * KB + lane * 16, s_src + (uint64_t)row * (NG * 4));
                 }
             }
             cp_async_commit();
@@ -648,9 +703,11 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
         for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i, i);
 
         // ---- queries of this column tile ------------------------------------------------------
-        // fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n)
+        // Fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n).  Queries enter as
+        // fp16, scaled by the power of two that brings the column's largest element to 2^14..2^15: exact
+        // for both types, but for elements below 2^-24 of the largest (off by 2^-36 of it).
         uint32_t qf[NT][NG][4][2];
-        float qsum[NT][NG][NC];
+        float qsum[NT][NG][NC], unit[NT][NC];            // sum of q in units of the products; their value in powers of two
         const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -658,33 +715,65 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             const int cc = ct * COLS + (col < cols_here ? col : 0);
             const int tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
             const uint16_t* qp = a.q + ((long long)b * a.T + tok) * a.q_stride + (long long)head * D;
+            float f[NG][2][8], big = 0.f, sum[NG];
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                float s = 0.f;
+                sum[g] = 0.f;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float f[8];
-                    unpack8<DT>(*reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j), f);
+                    unpack8<DT>(*reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j), f[g][j]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s += f[e];
-                    // channels (0,4) (1,5) (2,6) (3,7) of the eight, in the units of their codes
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float c = q_scale<DT>() * (DT == TYPE_BF16 && (e & 1) ? 0.0625f : 1.f);
-                        qf[nt][g][2 * j + (e >> 1)][e & 1] = pack2<DT>(f[e] * c, f[e + 4] * c);
-                    }
+                    for (int e = 0; e < 8; ++e) { sum[g] += f[g][j][e]; big = fmaxf(big, fabsf(f[g][j][e])); }
                 }
-                s += __shfl_xor_sync(0xffffffffu, s, 1);
-                s += __shfl_xor_sync(0xffffffffu, s, 2);
-                // lanes hold columns 2 t4 + c of the result
+                sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
+                sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
+            }
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            // 2^(14 - exponent of the largest), kept within what a float can hold both ways
+            int e2 = 141 - (int)(__float_as_uint(big) >> 23);
+            e2 = e2 > 100 ? 100 : (e2 < -100 ? -100 : e2);
+            const float to_unit = __uint_as_float((uint32_t)(127 + e2) << 23);
+            const float of_unit = __uint_as_float((uint32_t)(127 + 24 - e2) << 23);      // products: n q 2^-24
+            // q0 n0 + q1 n1 = (q0 - q1 / 16) n0 + (q1 / 16) b.  The difference needs more bits than fp16
+            // has: PACKED, the odd columns take what it leaves over; else a second product would be
+            // dearer than the mask it saves, and the second operand is 16 n1.
 #pragma unroll
-                for (int c = 0; c < NC; ++c) qsum[nt][g][c] = __shfl_sync(0xffffffffu, s, (2 * t4 + c) * 4) / score_unit<DT>();
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {        // channels (0,4) (1,5), then (2,6) (3,7) of the eight
+                        float q0[2], q1[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            q0[i] = f[g][j][2 * e + 4 * i] * to_unit;
+                            q1[i] = f[g][j][2 * e + 4 * i + 1] * (0.0625f * to_unit);
+                        }
+                        if (PACKED) {
+                            const float d0 = q0[0] - q1[0], d1 = q0[1] - q1[1];
+                            const uint32_t hi = pack2<TYPE_FP16>(d0, d1);
+                            const float2 hf = unpack2<TYPE_FP16>(hi);
+                            const bool rest = r8 & 1;
+                            qf[nt][g][2 * j + e][0] = rest ? pack2<TYPE_FP16>(d0 - hf.x, d1 - hf.y) : hi;
+                            qf[nt][g][2 * j + e][1] = rest ? 0u : pack2<TYPE_FP16>(q1[0], q1[1]);
+                        } else {
+                            qf[nt][g][2 * j + e][0] = pack2<TYPE_FP16>(q0[0], q0[1]);
+                            qf[nt][g][2 * j + e][1] = pack2<TYPE_FP16>(q1[0], q1[1]);
+                        }
+                    }
+            // lanes hold columns 2 t4 + c of the result
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const float of = __shfl_sync(0xffffffffu, of_unit, (2 * t4 + c) * 4);
+                unit[nt][c] = a.scale_log2 * of;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) qsum[nt][g][c] = __shfl_sync(0xffffffffu, sum[g], (2 * t4 + c) * 4) / of;
             }
         }
-        // keys below safe_end and from safe_lo on count for every column
-        const int safe_end = sp.len - a.T + 1;
+        // keys below safe_end and from safe_lo on count for every column, and are in the ring
+        const int safe_end = sp.len - a.T + 1 < key_end ? sp.len - a.T + 1 : key_end;
         const int safe_lo = a.window > 0 && sp.len > a.window ? (int)(sp.len - a.window) : 0;
-        const float unit = a.scale_log2 * score_unit<DT>();
 
         Q4State<D, NT, PACKED> st;
 #pragma unroll
@@ -703,11 +792,11 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
         }
 
         int stage = 0;
+#pragma unroll 1
         for (int step = 0; step < n_steps; ++step) {
             cp_async_wait<Q4_STAGES - 2>();
             __syncwarp();
-            const uint32_t bad2 = (bad_bits >> (stage * U)) & ((1u << U) - 1);
-            const unsigned char* blk = ring + stage * (U * TILE);
+            const int ring_at = stage * (U * TILE);
             // the next tiles go into the stage that the previous step left
             issue(step + Q4_STAGES - 1, stage == 0 ? Q4_STAGES - 1 : stage - 1);
             stage = stage == Q4_STAGES - 1 ? 0 : stage + 1;
@@ -717,62 +806,81 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             float sc[U][NT][2][NC];                      // rows r8 and r8 + 8, in powers of two
 #pragma unroll
             for (int x = 0; x < U; ++x) {
-                const unsigned char* sk = blk + x * TILE;
-                const uint32_t* ssk = reinterpret_cast<const uint32_t*>(sk + 2 * KB);
+                constexpr int NGW = NG;
+                const int blk = ring_at + x * TILE;
+                uint32_t w_s[2][NGW];                    // step and minimum of rows r8 and r8 + 8, per group
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t at = s_addr + blk + r * (8 * NG * 4);
+                    if (NG == 2) {
+                        const uint2 z = lds64(at);
+                        w_s[r][0] = z.x;
+                        w_s[r][NG - 1] = z.y;
+                    } else {
+                        w_s[r][0] = lds32(at);
+                    }
+                }
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const uint2 w0 = *reinterpret_cast<const uint2*>(sk + (k_off ^ (32 * g)));
-                    const uint2 w8 = *reinterpret_cast<const uint2*>(sk + ((k_off ^ (32 * g) ^ ROW8_X) + ROW8));
+                    const uint2 w0 = lds64(k_addr[g][0] + blk), w8 = lds64(k_addr[g][1] + blk + ROW8);
                     float acc[NT][4];
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[nt][e] = 0.f;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         uint32_t c0[4], c8[4];
-                        codes8<DT>(j ? w0.y : w0.x, c0);
-                        codes8<DT>(j ? w8.y : w8.x, c8);
+                        code_bytes(j ? w0.y : w0.x, c0);
+                        code_bytes(j ? w8.y : w8.x, c8);
+                        if (!PACKED) {
+                            c0[1] &= 0x00f000f0u; c0[3] &= 0x00f000f0u;
+                            c8[1] &= 0x00f000f0u; c8[3] &= 0x00f000f0u;
+                        }
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            mma16816<DT>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2 * j][0], qf[nt][g][2 * j][1]);
-                            mma16816<DT>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
+                            if (j == 0) mma16816<TYPE_FP16, true>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][0][0], qf[nt][g][0][1]);
+                            else mma16816<TYPE_FP16>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2][0], qf[nt][g][2][1]);
+                            mma16816<TYPE_FP16>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
                         }
                     }
-                    const float2 s0 = unpack2<TYPE_BF16>(ssk[r8 * NG + g]), s8 = unpack2<TYPE_BF16>(ssk[(r8 + 8) * NG + g]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 s = step_min(w_s[r][g], a.two16);
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) {
-                            const float p0 = fmaf(s0.x, acc[nt][c], s0.y * qsum[nt][g][c]);
-                            const float p8 = fmaf(s8.x, acc[nt][2 + c], s8.y * qsum[nt][g][c]);
-                            sc[x][nt][0][c] = g == 0 ? p0 : sc[x][nt][0][c] + p0;
-                            sc[x][nt][1][c] = g == 0 ? p8 : sc[x][nt][1][c] + p8;
-                        }
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < NC; ++c)
+                                sc[x][nt][r][c] = fmaf(s.x, PACKED ? acc[nt][2 * r] + acc[nt][2 * r + 1] : acc[nt][2 * r + c],
+                                                       g == 0 ? s.y * qsum[nt][g][c] : fmaf(s.y, qsum[nt][g][c], sc[x][nt][r][c]));
+                    }
                 }
             }
 
             // ---- weights -------------------------------------------------------------------------
-            const int last = kbase + (U - 1) * Q4_UNIT + Q4_TILE;
-            const bool edge = bad2 != 0 || last > safe_end || kbase < safe_lo;
+            const bool edge = some_bad || kbase + (U - 1) * Q4_UNIT + Q4_TILE > safe_end || kbase < safe_lo;
+            bool none[U];                                // tiles that hold no keys
+#pragma unroll
+            for (int x = 0; x < U; ++x) none[x] = false;
+            if (some_bad) {
+#pragma unroll
+                for (int x = 0; x < U; ++x) none[x] = row_of(step * U + x) < 0;
+            }
             bool grow = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
 #pragma unroll
-                    for (int x = 0; x < U; ++x) { sc[x][nt][0][c] *= unit; sc[x][nt][1][c] *= unit; }
+                    for (int x = 0; x < U; ++x) { sc[x][nt][0][c] *= unit[nt][c]; sc[x][nt][1][c] *= unit[nt][c]; }
                     if (edge) {
                         const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
                         const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
                         const int lim = sp.len - a.T + 1 + tk;              // keys [low, lim) count
                         const int low = a.window > 0 && lim > a.window ? (int)(lim - a.window) : 0;
+                        const int end = lim < key_end ? lim : key_end;      // beyond key_end the ring holds no tile
 #pragma unroll
                         for (int x = 0; x < U; ++x)
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
                                 const int key = kbase + x * Q4_UNIT + r8 + 8 * r;
-                                if (((bad2 >> x) & 1u) || key >= lim || key < low) sc[x][nt][r][c] = -INFINITY;
+                                if (none[x] || key >= end || key < low) sc[x][nt][r][c] = -INFINITY;
                             }
                     }
                     float mx = fmaxf(sc[0][nt][0][c], sc[0][nt][1][c]);
@@ -822,16 +930,25 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             // ---- values --------------------------------------------------------------------------
 #pragma unroll
             for (int x = 0; x < U; ++x) {
-                const unsigned char* sv = blk + x * TILE + KB;
-                const uint32_t* ssv = reinterpret_cast<const uint32_t*>(blk + x * TILE + 2 * KB + SB);
+                const int blk = ring_at + x * TILE;
+                uint32_t w_s[2][NG];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint32_t at = s_addr + blk + SB + r * (8 * NG * 4);
+                    if (NG == 2) {
+                        const uint2 z = lds64(at);
+                        w_s[r][0] = z.x;
+                        w_s[r][NG - 1] = z.y;
+                    } else {
+                        w_s[r][0] = lds32(at);
+                    }
+                    if (edge) {                          // rows that hold no key may hold anything
+                        if (none[x] || kbase + x * Q4_UNIT + r8 + 8 * r >= key_end) w_s[r][0] = w_s[r][NG - 1] = 0u;
+                    }
+                }
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    float2 v0 = unpack2<TYPE_BF16>(ssv[r8 * NG + g]), v8 = unpack2<TYPE_BF16>(ssv[(r8 + 8) * NG + g]);
-                    if (edge) {                          // rows that hold no key may hold anything
-                        const int key = kbase + x * Q4_UNIT + r8;
-                        if (((bad2 >> x) & 1u) || key >= sp.len) v0 = make_float2(0.f, 0.f);
-                        if (((bad2 >> x) & 1u) || key + 8 >= sp.len) v8 = make_float2(0.f, 0.f);
-                    }
+                    const float2 v0 = step_min(w_s[0][g], a.two16), v8 = step_min(w_s[1][g], a.two16);
                     // weights transposed to the N side: [part][rows 0-7, 8-15]; the second part is what
                     // cutting the first to 16 bits left over
                     uint32_t bw[NT][PARTS][2];
@@ -854,23 +971,19 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                             }
                         }
                     // codes of keys 2 t4, 2 t4 + 1, + 8, + 9 for channels 64 g + 8 r8 .. + 7
-                    const int o = v_off ^ (32 * g);
-                    const uint32_t w0 = *reinterpret_cast<const uint32_t*>(sv + o);
-                    const uint32_t w1 = *reinterpret_cast<const uint32_t*>(sv + (o ^ ROW1_X));
-                    const uint32_t w8 = *reinterpret_cast<const uint32_t*>(sv + ((o ^ ROW8_X) + ROW8));
-                    const uint32_t w9 = *reinterpret_cast<const uint32_t*>(sv + ((o ^ ROW1_X ^ ROW8_X) + ROW8));
-                    constexpr int BF = TYPE_BF16;
+                    const uint32_t w0 = lds32(v_addr[g][0][0] + blk), w1 = lds32(v_addr[g][1][0] + blk);
+                    const uint32_t w8 = lds32(v_addr[g][0][1] + blk + ROW8), w9 = lds32(v_addr[g][1][1] + blk + ROW8);
 #pragma unroll
                     for (int hh = 0; hh < 2; ++hh) {
                         uint32_t c0[4], c8[4];
-                        codes8<BF>(__byte_perm(w0, w1, hh ? 0x7632 : 0x5410), c0);
-                        codes8<BF>(__byte_perm(w8, w9, hh ? 0x7632 : 0x5410), c8);
+                        pair_bytes(__byte_perm(w0, w1, hh ? 0x7632 : 0x5410), c0);
+                        pair_bytes(__byte_perm(w8, w9, hh ? 0x7632 : 0x5410), c8);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int part = 0; part < PARTS; ++part) {
-                                mma16816<BF>(st.o[g][2 * hh][nt], c0[0], c0[1], c8[0], c8[1], bw[nt][part][0], bw[nt][part][1]);
-                                mma16816<BF>(st.o[g][2 * hh + 1][nt], c0[2], c0[3], c8[2], c8[3], bw[nt][part][0], bw[nt][part][1]);
+                                mma16816<TYPE_BF16>(st.o[g][2 * hh][nt], c0[0], c0[1], c8[0], c8[1], bw[nt][part][0], bw[nt][part][1]);
+                                mma16816<TYPE_BF16>(st.o[g][2 * hh + 1][nt], c0[2], c0[3], c8[2], c8[3], bw[nt][part][0], bw[nt][part][1]);
                             }
                     }
                 }
@@ -908,12 +1021,12 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int m = 0; m < 4; ++m)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {    // accumulator rows r8 and r8 + 8: channels 2 m and 2 m + 1
-                            float x = st.o[g][m][nt][2 * e + c];
-                            if (PACKED) x += st.o[g][m][nt][2 * e + 1];
-                            dst[g * GROUP + 8 * r8 + 2 * m + e] = fmaf(x, e ? TWO69 / 16.f : TWO69, st.msum[g][nt][c]);
-                        }
+                    {                                    // accumulator rows r8 and r8 + 8: n0 and n0 + 16 n1 of
+                        float x = st.o[g][m][nt][c], y = st.o[g][m][nt][2 + c];              // channels 2 m, 2 m + 1
+                        if (PACKED) { x += st.o[g][m][nt][1]; y += st.o[g][m][nt][3]; }
+                        dst[g * GROUP + 8 * r8 + 2 * m] = fmaf(x, TWO69, st.msum[g][nt][c]);
+                        dst[g * GROUP + 8 * r8 + 2 * m + 1] = fmaf(y - x, TWO69 / 16.f, st.msum[g][nt][c]);
+                    }
                 if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
             }
         __syncthreads();
@@ -943,7 +1056,6 @@ __global__ void __launch_bounds__(Q4_THREADS, SHAPE == COLS_16 ? 1 : 2) q4_atten
             }
         }
         __syncthreads();                                 // the ring is free for the next share
-        u += n_units;
     }
 }
 
@@ -957,14 +1069,14 @@ __global__ void __launch_bounds__(D) q4_combine_kernel(const __grid_constant__ Q
     const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
     const int h = item / a.col_tiles, ct = item - h * a.col_tiles, col = blockIdx.y;
     const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
-    if (col >= cols_here) return;
+    if (col >= cols_here) { pdl_wait(); return; }        // (a grid that ends is one whose predecessor has)
     long long mine = 0, all = 0;
     for (int bb = tid; bb < a.B; bb += D) {
-        const int n = q4_span(a, a.seq_lens[bb]).units;
+        const int n = q4_span(a, a.seq_lens[bb]).weight;
         all += n;
         if (bb < b) mine += n;
     }
-    const int units = q4_span(a, a.seq_lens[b]).units;
+    const int weight = q4_span(a, a.seq_lens[b]).weight;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         mine += __shfl_down_sync(0xffffffffu, mine, o);
@@ -975,19 +1087,20 @@ __global__ void __launch_bounds__(D) q4_combine_kernel(const __grid_constant__ Q
     mine = all = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) { mine += s_sum[0][w]; all += s_sum[1][w]; }
-    const long long total = all * per_seq, ua = mine * per_seq + (long long)item * units, ub = ua + units;
+    const long long total = all * per_seq, ua = mine * per_seq + (long long)item * weight, ub = ua + weight;
     const int shares = total < a.grid ? (int)total : a.grid;
     int c0 = 0, c1 = -1;
-    if (units > 0) {
-        // CTA whose share holds unit x: the largest c with total * c / shares <= x
-        c0 = (int)(((ua + 1) * shares + total - 1) / total) - 1;
+    if (weight > 0) {
+        // CTA whose share holds x: the largest c with total * c / shares <= x; the first key's, the last key's
+        c0 = (int)(((ua + Q4_BEGIN + 1) * shares + total - 1) / total) - 1;
         c1 = (int)((ub * shares + total - 1) / total) - 1;
-        if (c0 == c1) return;                            // one CTA had it all and wrote it
     }
     // only the first CTA can have begun another item before this one
-    const float* p0 = a.part + ((long long)(2 * c0 + (units > 0 && ua > q4_share(total, shares, c0) ? 1 : 0)) * COLS + col) * (D + 2);
+    const float* p0 = a.part + ((long long)(2 * c0 + (weight > 0 && ua > q4_share(total, shares, c0) ? 1 : 0)) * COLS + col) * (D + 2);
     const float* p1 = a.part + ((long long)(2 * (c0 + 1)) * COLS + col) * (D + 2);
     constexpr long long NEXT = 2ll * COLS * (D + 2);
+    pdl_wait();                                          // (the lengths were there before the first kernel began)
+    if (weight > 0 && c0 == c1) return;                  // one CTA had it all and wrote it
     float mx = Q4_NONE, l = 0.f, o = 0.f;
     for (int c = c0; c <= c1; c += AHEAD) {
         float m[AHEAD], s[AHEAD], x[AHEAD];
