@@ -399,11 +399,12 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
 // ---------------------------------------------------------------------------------------
 // q4_attend_kernel
 // ---------------------------------------------------------------------------------------
-constexpr int Q4_THREADS = 256, Q4_WARPS = Q4_THREADS / 32;
+constexpr int Q4_THREADS = 128, Q4_WARPS = Q4_THREADS / 32;
 constexpr int Q4_TILE = 16;              // keys of one tile
-constexpr int Q4_PAIR = 2;               // tiles that a warp takes in one step
+constexpr int Q4_STEP = 3;               // tiles that a warp takes in one step
 constexpr int Q4_UNIT = Q4_TILE * Q4_WARPS;
-constexpr int Q4_STAGES = 3;             // steps a warp has in flight or in use
+constexpr int Q4_STAGES = 2;             // steps a warp has in flight or in use
+constexpr int Q4_AHEAD = 32 / Q4_STEP * Q4_STEP;   // tiles whose rows the lanes of a warp look up at once
 constexpr float Q4_NONE = -3.0e38f;      // reference of a column that has seen no key
 
 // Columns (query token, head of the group) of one CTA by shape: four columns, each as two parts of
@@ -413,13 +414,15 @@ __host__ __device__ constexpr int q4_cols(int shape) { return shape == COLS_4 ? 
 // bytes of one tile: key codes, value codes, key scales, value scales of 16 rows
 __host__ __device__ constexpr int q4_tile_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
 __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
-    const int ring = Q4_WARPS * Q4_STAGES * Q4_PAIR * q4_tile_bytes(d);
+    const int ring = Q4_WARPS * Q4_STAGES * Q4_STEP * q4_tile_bytes(d);
     const int merge = Q4_WARPS * q4_cols(shape) * (d + 2) * 4;
     return ring > merge ? ring : merge;
 }
 
-// Accumulators and queries of 16 columns of 128 channels need more than the 128 registers of two CTAs an SM.
-__host__ __device__ constexpr int q4_ctas_per_sm(int d, int shape) { return shape == COLS_16 && d == 128 ? 1 : 2; }
+// Few warps with many registers: three tiles at a time keep the ALU and the tensor cores busier than
+// more warps with one or two tiles would (4 x 128K keys: 107 us; 16 warps an SM with two tiles 112, 20
+// with one 130).  Accumulators and queries of 16 columns of 128 channels take what two CTAs leave.
+__host__ __device__ constexpr int q4_ctas_per_sm(int d, int shape) { return shape == COLS_16 && d == 128 ? 2 : 3; }
 
 struct Q4Args {
     Pages pg;
@@ -437,7 +440,7 @@ struct Q4Args {
 // What beginning an item costs a CTA (page look-up, queries, first tiles, join), in units: a share counts
 // that much more for every item that begins in it, else the CTAs that get the short sequences of a mixed
 // batch finish last.
-constexpr int Q4_BEGIN = 4;
+constexpr int Q4_BEGIN = 10;
 
 // keys of a sequence: first one read (multiple of 16), end, units, and what an item counts (0 if empty)
 struct Span { int lo, len, units, weight; };
@@ -466,19 +469,21 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-// c += a * b; FIRST: c = a * b
-template <int DT, bool FIRST = false>
+// c += a * b, and c = a * b
+template <int DT>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    const float i0 = FIRST ? 0.f : c[0], i1 = FIRST ? 0.f : c[1], i2 = FIRST ? 0.f : c[2], i3 = FIRST ? 0.f : c[3];
     if (DT == TYPE_BF16)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(i0), "f"(i1), "f"(i2), "f"(i3));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(i0), "f"(i1), "f"(i2), "f"(i3));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 // Codes as operands: the bits of a code ARE a small number.  In bf16 bits 0..7 count in steps of 2^-133
 // (subnormals, then the first exponent), in fp16 bits 0..10 in steps of 2^-24, and the tensor core
 // multiplies subnormals exactly.  So a mask makes the operand and no offset has to be taken out of the
@@ -509,6 +514,7 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
     return x;
 }
+__device__ __forceinline__ void sts32(uint32_t addr, uint32_t x) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(x) : "memory"); }
 __device__ __forceinline__ uint2 lds64(uint32_t addr) {
     uint2 x;
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(addr) : "memory");
@@ -535,7 +541,7 @@ struct Q4State {
 // or 16 channels), the columns the N side: with 4 columns the two parts of a weight fill the 8 columns
 // of one product, so the second part is free.
 //
-// A warp works alone on tiles of 16 keys (2.3 KB at d = 128), two at a time, through its own ring of
+// A warp works alone on tiles of 16 keys (2.3 KB at d = 128), three at a time, through its own ring of
 // cp.async stages; warps meet only when a sequence's share ends.  The reference of the exponentials
 // moves only when a score exceeds it by 2^8: one vote per step instead of a reduction.
 //
@@ -544,7 +550,7 @@ struct Q4State {
 template <int DT, int D, int SHAPE>
 __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_attend_kernel(const __grid_constant__ Q4Args a) {
     constexpr bool PACKED = SHAPE == COLS_4;
-    constexpr int NT = SHAPE == COLS_16 ? 2 : 1, U = Q4_PAIR;
+    constexpr int NT = SHAPE == COLS_16 ? 2 : 1, U = Q4_STEP;
     constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2, PARTS = PACKED ? 1 : 2;
     constexpr int TILE = q4_tile_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4, RING = Q4_STAGES * U * TILE;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -557,7 +563,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
     pdl_wait();
     pdl_start_next();
     // Weights before each sequence: every CTA adds up the lengths itself.  First the total, then the
-    // sequence in which this CTA's share begins (the lengths are still in registers for up to 256
+    // sequence in which this CTA's share begins (the lengths are still in registers for up to 128
     // sequences).
     long long total = 0, u = 0, u_end = 0;
     int shares = 0;
@@ -660,7 +666,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
         const int n_all = (key_end - key0 + Q4_TILE - 1) / Q4_TILE;
         const int n_tiles = n_all > warp ? (n_all - warp + Q4_WARPS - 1) / Q4_WARPS : 0;
 
-        // ---- page rows of the next 32 tiles, one per lane ------------------------------------
+        // ---- page rows of the next tiles, one per lane ---------------------------------------
         // (32 bits: the host refuses caches of 2^32 rows or more.)  A tile whose page is out of range
         // is read from row 0 and masked; that such a tile exists is remembered for the whole share.
         bool bad = false;
@@ -671,19 +677,21 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             bad |= r < 0;
             return r < 0 ? 0u : (uint32_t)(r + (long long)h * a.pg.page_size);
         };
-        uint32_t rows_now = tile_row(lane), rows_next = tile_row(32 + lane);
+        uint32_t rows_now = tile_row(lane), rows_next = tile_row(Q4_AHEAD + lane);
         bool some_bad = __any_sync(0xffffffffu, bad);
+        int ahead = 0;                                   // tiles issued from rows_now
 
         auto issue = [&](int step, int st) {             // tiles of `step` into stage st
-            if (step > 0 && (step * U & 31) == 0) {
+            if (ahead == Q4_AHEAD) {
+                ahead = 0;
                 rows_now = rows_next;
-                rows_next = tile_row(step * U + 32 + lane);
+                rows_next = tile_row(step * U + Q4_AHEAD + lane);
                 some_bad = __any_sync(0xffffffffu, bad);
             }
 #pragma unroll
             for (int x = 0; x < U; ++x) {
                 const int i = step * U + x;
-                const uint32_t row = __shfl_sync(0xffffffffu, rows_now, i & 31);
+                const uint32_t row = __shfl_sync(0xffffffffu, rows_now, ahead + x);
                 if (i < n_tiles) {
                     const uint32_t dst = c_dst + (st * U + x) * TILE;
                     const unsigned char* kp = k_src + (uint64_t)row * (D / 2);
@@ -696,6 +704,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                     if (lane < SB / 8) cp_async16(ring + (st * U + x) * TILE + 2 * KB + lane * 16, s_src + (uint64_t)row * (NG * 4));
                 }
             }
+            ahead += U;
             cp_async_commit();
         };
         const int n_steps = (n_tiles + U - 1) / U;
@@ -835,7 +844,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                         }
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            if (j == 0) mma16816<TYPE_FP16, true>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][0][0], qf[nt][g][0][1]);
+                            if (j == 0) mma16816_first(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][0][0], qf[nt][g][0][1]);
                             else mma16816<TYPE_FP16>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2][0], qf[nt][g][2][1]);
                             mma16816<TYPE_FP16>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
                         }
@@ -854,35 +863,45 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             }
 
             // ---- weights -------------------------------------------------------------------------
-            const bool edge = some_bad || kbase + (U - 1) * Q4_UNIT + Q4_TILE > safe_end || kbase < safe_lo;
-            bool none[U];                                // tiles that hold no keys
 #pragma unroll
-            for (int x = 0; x < U; ++x) none[x] = false;
-            if (some_bad) {
+            for (int x = 0; x < U; ++x)
 #pragma unroll
-                for (int x = 0; x < U; ++x) none[x] = row_of(step * U + x) < 0;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) { sc[x][nt][0][c] *= unit[nt][c]; sc[x][nt][1][c] *= unit[nt][c]; }
+            if (some_bad || kbase + (U - 1) * Q4_UNIT + Q4_TILE > safe_end || kbase < safe_lo) {
+                // Keys that do not count for a column: score -inf.  Rows that hold no key may hold
+                // anything: their value scales are cleared in the ring.
+#pragma unroll
+                for (int x = 0; x < U; ++x) {
+                    const int key = kbase + x * Q4_UNIT + r8;
+                    const bool none = some_bad && row_of(step * U + x) < 0;
+                    if (t4 < 2 && (none || key + 8 * t4 >= key_end)) {
+                        const uint32_t at = s_addr + ring_at + x * TILE + SB + t4 * (8 * NG * 4);
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) sts32(at + 4 * g, 0u);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
+                            const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
+                            const int lim = sp.len - a.T + 1 + tk;          // keys [low, lim) count
+                            const int low = a.window > 0 && lim > a.window ? (int)(lim - a.window) : 0;
+                            const int end = lim < key_end ? lim : key_end;  // beyond key_end the ring holds no tile
+#pragma unroll
+                            for (int r = 0; r < 2; ++r)
+                                if (none || key + 8 * r >= end || key + 8 * r < low) sc[x][nt][r][c] = -INFINITY;
+                        }
+                }
+                __syncwarp();
             }
             bool grow = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-#pragma unroll
-                    for (int x = 0; x < U; ++x) { sc[x][nt][0][c] *= unit[nt][c]; sc[x][nt][1][c] *= unit[nt][c]; }
-                    if (edge) {
-                        const int mycol = PACKED ? t4 : nt * 8 + 2 * t4 + c;
-                        const int tk = (ct * COLS + (mycol < cols_here ? mycol : 0)) / a.G;
-                        const int lim = sp.len - a.T + 1 + tk;              // keys [low, lim) count
-                        const int low = a.window > 0 && lim > a.window ? (int)(lim - a.window) : 0;
-                        const int end = lim < key_end ? lim : key_end;      // beyond key_end the ring holds no tile
-#pragma unroll
-                        for (int x = 0; x < U; ++x)
-#pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                const int key = kbase + x * Q4_UNIT + r8 + 8 * r;
-                                if (none[x] || key >= end || key < low) sc[x][nt][r][c] = -INFINITY;
-                            }
-                    }
                     float mx = fmaxf(sc[0][nt][0][c], sc[0][nt][1][c]);
 #pragma unroll
                     for (int x = 1; x < U; ++x) mx = fmaxf(mx, fmaxf(sc[x][nt][0][c], sc[x][nt][1][c]));
@@ -941,9 +960,6 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                         w_s[r][NG - 1] = z.y;
                     } else {
                         w_s[r][0] = lds32(at);
-                    }
-                    if (edge) {                          // rows that hold no key may hold anything
-                        if (none[x] || kbase + x * Q4_UNIT + r8 + 8 * r >= key_end) w_s[r][0] = w_s[r][NG - 1] = 0u;
                     }
                 }
 #pragma unroll
