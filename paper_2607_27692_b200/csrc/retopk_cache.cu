@@ -69,6 +69,7 @@ Pages device_pages(const retopk_pages_t* p) {
     g.capacity = g.max_pages * p->page_size;
     g.H_kv = p->H_kv;
     g.page_size = p->page_size;
+    g.page_shift = (p->page_size & (p->page_size - 1)) == 0 ? __builtin_ctz((unsigned)p->page_size) : -1;
     return g;
 }
 

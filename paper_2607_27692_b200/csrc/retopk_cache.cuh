@@ -65,14 +65,14 @@ struct Pages {
     unsigned char *k, *v, *ks, *vs;
     const int32_t* table;       // null: sequence b owns page b
     long long n_pages, max_pages, capacity;   // capacity: rows a sequence can have
-    int H_kv, page_size;
+    int H_kv, page_size, page_shift;          // page_shift: log2 of page_size, or -1
 };
 
 // Row index of position `pos` of sequence b for KV head 0 (head h: + h * page_size), or -1 when
 // the position is outside the cache or its page number is not a page.
 __device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long pos) {
     if (pos < 0 || pos >= pg.capacity) return -1;
-    const int slot = (int)pos / pg.page_size, off = (int)pos - slot * pg.page_size;
+    const int slot = pg.page_shift >= 0 ? (int)pos >> pg.page_shift : (int)pos / pg.page_size, off = (int)pos - slot * pg.page_size;
     long long page = b;
     if (pg.table) page = pg.table[(long long)b * pg.max_pages + slot];
     if (page < 0 || page >= pg.n_pages) return -1;
@@ -415,7 +415,7 @@ __host__ __device__ constexpr int q4_cols(int shape) { return shape == COLS_4 ? 
 __host__ __device__ constexpr int q4_tile_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
 __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
     const int ring = Q4_WARPS * Q4_STAGES * Q4_STEP * q4_tile_bytes(d);
-    const int merge = Q4_WARPS * q4_cols(shape) * (d + 2) * 4;
+    const int merge = Q4_WARPS * q4_cols(shape) * (d + 4) * 4;
     return ring > merge ? ring : merge;
 }
 
@@ -554,63 +554,68 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
     constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2, PARTS = PACKED ? 1 : 2;
     constexpr int TILE = q4_tile_bytes(D), KB = Q4_TILE * D / 2, SB = Q4_TILE * NG * 4, RING = Q4_STAGES * U * TILE;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int s_start[3];                           // sequence, its weight before this share, its length
-    __shared__ int s_scan[Q4_WARPS];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, t4 = lane & 3, r8 = lane >> 2;
     const int per_seq = a.pg.H_kv * a.col_tiles;
 
     pdl_wait();
     pdl_start_next();
-    // Weights before each sequence: every CTA adds up the lengths itself.  First the total, then the
-    // sequence in which this CTA's share begins (the lengths are still in registers for up to 128
-    // sequences).
-    long long total = 0, u = 0, u_end = 0;
-    int shares = 0;
+    // Every warp adds up the weights of the sequences by itself, 128 at a time: first the total, then
+    // the sequence in which this CTA's share begins (up to 128 lengths are still in registers then).
+    long long total = 0, u = 0, u_end = 0, before = 0;   // before: weight before sequence b
+    int shares = 0, b = 0, b_len = 0;
     {
-        int len = 0, v = 0, before_me = 0;
+        constexpr int EACH = 4;
+        int len[EACH], w[EACH], mine = 0, incl = 0;
         for (int pass = 0; pass < 2; ++pass) {
             long long run = 0;
-            for (int b0 = 0; b0 < a.B; b0 += Q4_THREADS) {
-                const int bb = b0 + tid;
-                if (pass == 0 || a.B > Q4_THREADS) {
-                    len = bb < a.B ? a.seq_lens[bb] : 0;
-                    v = q4_span(a, len).weight * per_seq;
-                    int incl = v;
+            for (int b0 = 0; b0 < a.B; b0 += 32 * EACH) {
+                const int first = b0 + lane * EACH;
+                if (pass == 0 || a.B > 32 * EACH) {
+                    mine = 0;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) len[i] = first + i < a.B ? a.seq_lens[first + i] : 0;
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) {
+                        w[i] = q4_span(a, len[i]).weight * per_seq;
+                        mine += w[i];
+                    }
+                    incl = mine;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
-                        const int w = __shfl_up_sync(0xffffffffu, incl, o);
-                        if (lane >= o) incl += w;
+                        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                        if (lane >= o) incl += x;
                     }
-                    if (lane == 31) s_scan[warp] = incl;
-                    __syncthreads();
-                    int base = 0, all = 0;
-#pragma unroll
-                    for (int w = 0; w < Q4_WARPS; ++w) {
-                        if (w < warp) base += s_scan[w];
-                        all += s_scan[w];
-                    }
-                    before_me = base + incl - v;
-                    if (pass == 0) total += all;
-                    else if (u >= run + before_me && u < run + before_me + v) { s_start[0] = bb; s_start[1] = (int)(u - run) - before_me; s_start[2] = len; }
-                    run += all;
-                    __syncthreads();
-                } else if (u >= before_me && u < before_me + v) {
-                    s_start[0] = bb; s_start[1] = (int)u - before_me; s_start[2] = len;
                 }
+                const int all = __shfl_sync(0xffffffffu, incl, 31);
+                if (pass == 1) {
+                    const long long lo = run + incl - mine;
+                    const uint32_t hit = __ballot_sync(0xffffffffu, u >= lo && u < lo + mine);
+                    if (hit) {                           // one lane has it
+                        long long at = lo;
+                        int bb = first, ll = len[0];
+#pragma unroll
+                        for (int i = 0; i < EACH - 1; ++i)
+                            if (bb == first + i && u >= at + w[i]) { at += w[i]; bb = first + i + 1; ll = len[i + 1]; }
+                        const int src = __ffs(hit) - 1;
+                        before = __shfl_sync(0xffffffffu, at, src);
+                        b = __shfl_sync(0xffffffffu, bb, src);
+                        b_len = __shfl_sync(0xffffffffu, ll, src);
+                        break;
+                    }
+                }
+                run += all;
             }
             if (pass == 0) {
+                total = run;
                 shares = total < a.grid ? (int)total : a.grid;
                 if ((int)blockIdx.x >= shares) return;
                 u = q4_share(total, shares, blockIdx.x);
                 u_end = q4_share(total, shares, blockIdx.x + 1);
             }
         }
-        __syncthreads();
     }
-    int b = s_start[0];
-    long long before = u - s_start[1];                   // weight before sequence b
-    Span sp = q4_span(a, s_start[2]);
+    Span sp = q4_span(a, b_len);
     const long long u_begin = u;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * RING;
@@ -666,6 +671,21 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
         const int n_all = (key_end - key0 + Q4_TILE - 1) / Q4_TILE;
         const int n_tiles = n_all > warp ? (n_all - warp + Q4_WARPS - 1) / Q4_WARPS : 0;
 
+        // ---- queries of this column tile: asked for here, used below ---------------------------
+        const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
+        uint4 q_raw[NT][NG][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int col = PACKED ? r8 >> 1 : nt * 8 + r8;
+            const int cc = ct * COLS + (col < cols_here ? col : 0);
+            const int tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
+            const uint16_t* qp = a.q + ((long long)b * a.T + tok) * a.q_stride + (long long)head * D;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) q_raw[nt][g][j] = *reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j);
+        }
+
         // ---- page rows of the next tiles, one per lane ---------------------------------------
         // (32 bits: the host refuses caches of 2^32 rows or more.)  A tile whose page is out of range
         // is read from row 0 and masked; that such a tile exists is remembered for the whole share.
@@ -711,26 +731,21 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
 #pragma unroll
         for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i, i);
 
-        // ---- queries of this column tile ------------------------------------------------------
+        // ---- query fragments --------------------------------------------------------------------
         // Fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n).  Queries enter as
         // fp16, scaled by the power of two that brings the column's largest element to 2^14..2^15: exact
         // for both types, but for elements below 2^-24 of the largest (off by 2^-36 of it).
         uint32_t qf[NT][NG][4][2];
         float qsum[NT][NG][NC], unit[NT][NC];            // sum of q in units of the products; their value in powers of two
-        const int cols_here = a.T * a.G - ct * COLS < COLS ? a.T * a.G - ct * COLS : COLS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int col = PACKED ? r8 >> 1 : nt * 8 + r8;
-            const int cc = ct * COLS + (col < cols_here ? col : 0);
-            const int tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
-            const uint16_t* qp = a.q + ((long long)b * a.T + tok) * a.q_stride + (long long)head * D;
             float f[NG][2][8], big = 0.f, sum[NG];
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 sum[g] = 0.f;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    unpack8<DT>(*reinterpret_cast<const uint4*>(qp + g * GROUP + 16 * t4 + 8 * j), f[g][j]);
+                    unpack8<DT>(q_raw[nt][g][j], f[g][j]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) { sum[g] += f[g][j][e]; big = fmaxf(big, fabsf(f[g][j][e])); }
                 }
@@ -1024,15 +1039,17 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                 for (int g = 0; g < NG; ++g) st.msum[g][nt][c] *= 1.f / TWO64;
             }
         __syncthreads();                                 // every warp is done with its ring
-        // [warp][col][D], then [warp][col] reference and sum
-        float* s_ref = s_merge + Q4_WARPS * COLS * D;
+        // [warp][col][D + 2] (the two keep the columns of a store in different banks), then [warp][col]
+        // reference and sum
+        constexpr int LD = D + 2;
+        float* s_ref = s_merge + Q4_WARPS * COLS * LD;
         float* s_l = s_ref + Q4_WARPS * COLS;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = PACKED ? t4 : nt * 8 + 2 * t4 + c;
-                float* dst = s_merge + (warp * COLS + col) * D;
+                float* dst = s_merge + (warp * COLS + col) * LD + 8 * r8;
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -1040,8 +1057,8 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                     {                                    // accumulator rows r8 and r8 + 8: n0 and n0 + 16 n1 of
                         float x = st.o[g][m][nt][c], y = st.o[g][m][nt][2 + c];              // channels 2 m, 2 m + 1
                         if (PACKED) { x += st.o[g][m][nt][1]; y += st.o[g][m][nt][3]; }
-                        dst[g * GROUP + 8 * r8 + 2 * m] = fmaf(x, TWO69, st.msum[g][nt][c]);
-                        dst[g * GROUP + 8 * r8 + 2 * m + 1] = fmaf(y - x, TWO69 / 16.f, st.msum[g][nt][c]);
+                        *reinterpret_cast<float2*>(dst + g * GROUP + 2 * m) =
+                            make_float2(fmaf(x, TWO69, st.msum[g][nt][c]), fmaf(y - x, TWO69 / 16.f, st.msum[g][nt][c]));
                     }
                 if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
             }
@@ -1058,7 +1075,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             for (int w = 0; w < Q4_WARPS; ++w) {
                 const float f = ex2(s_ref[w * COLS + col] - mx);
                 l += f * s_l[w * COLS + col];
-                o += f * s_merge[(w * COLS + col) * D + ch];
+                o += f * s_merge[(w * COLS + col) * LD + ch];
             }
             if (whole) {
                 const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);

@@ -46,23 +46,18 @@ class _Pages(C.Structure):
                 [(n, _vp) for n in ("k", "v", "k_scale", "v_scale", "block_table")] + [("max_pages", C.c_int64)])
 
 
-class _on:
-    """Make the device current for a call; free when it is already."""
+# Both cost a tenth of a microsecond; the public forms cost three, as much as a launch.
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
 
-    __slots__ = ("index", "prev")
 
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.prev = torch.cuda.current_device()
-        if self.prev != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.prev != self.index:
-            torch.cuda.set_device(self.prev)
+def _call(device, fn, *args):
+    """fn(*args, stream) on the current stream of `device`, which is made current for the call."""
+    index = device.index
+    if _current_device() == index:
+        return fn(*args, _current_stream(index))
+    with torch.cuda.device(device):
+        return fn(*args, _current_stream(index))
 
 
 def _rows(t, what, device, dtype, n, heads, d):
@@ -136,26 +131,29 @@ class Rope:
     def apply_pair(self, q, k, positions, q_out=None, k_out=None, inverse=False):
         """Rotate queries and keys in one launch.  ``inverse``: the transpose, i.e. the gradient."""
         _half_rows(q, "q")
-        n, dev, dt, d = q.shape[0], q.device, q.dtype, self.d
+        (n, H_q, d), dev, dt = q.shape, q.device, q.dtype
+        qp, qs = _rows(q, "q", dev, dt, n, H_q, self.d)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=dev)
-        H_q = q.shape[1]
-        qp, qs = _rows(q, "q", dev, dt, n, H_q, d)
-        qop, qos = _rows(q_out, "q_out", dev, dt, n, H_q, d)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            qop, qos = q_out.data_ptr(), H_q * d
+        else:
+            qop, qos = _rows(q_out, "q_out", dev, dt, n, H_q, d)
         kp, ks, kop, kos, H_k = None, 0, None, 0, 0
         if k is not None:
-            if k_out is None:
-                k_out = torch.empty(k.shape, dtype=dt, device=dev)
-            H_k = k.shape[1]
+            H_k = k.shape[1] if k.dim() == 3 else 0
             kp, ks = _rows(k, "k", dev, dt, n, H_k, d)
-            kop, kos = _rows(k_out, "k_out", dev, dt, n, H_k, d)
+            if k_out is None:
+                k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+                kop, kos = k_out.data_ptr(), H_k * d
+            else:
+                kop, kos = _rows(k_out, "k_out", dev, dt, n, H_k, d)
         pos = _ints(positions, "positions", dev, (n,))
         if n == 0:
             return q_out, k_out
-        with _on(dev) as stream:
-            rc = self.lib.retopk_rope_apply(self.h, _TYPE[dt], n, pos, qp, qs, qop, qos, H_q, kp, ks, kop, kos, H_k,
-                                            int(inverse), stream)
-        _check(rc, "retopk_rope_apply")
+        rc = _call(dev, self.lib.retopk_rope_apply, self.h, _TYPE[dt], n, pos, qp, qs, qop, qos, H_q, kp, ks, kop, kos,
+                   H_k, 1 if inverse else 0)
+        if rc:
+            _check(rc, "retopk_rope_apply")
         return q_out, k_out
 
 
@@ -205,6 +203,7 @@ class KVPages:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.fmt = "q4" if q4 else ("bf16" if k.dtype == torch.bfloat16 else "fp16")
         self.device = k.device
+        self._needs = {}             # workspace bytes by (B, T, H_q)
         self._head = (_FORMATS[self.fmt][0], self.H_kv, self.d, self.page_size, self.n_pages, k.data_ptr(), v.data_ptr(),
                       k_scale.data_ptr() if q4 else None, v_scale.data_ptr() if q4 else None)
 
@@ -241,17 +240,19 @@ class KVPages:
                 raise ValueError("q is rotated with the keys: pass rope")
             _half_rows(q, "q")
             H_q = q.shape[1]
-            if q_out is None:
-                q_out = torch.empty(q.shape, dtype=dt, device=dev)
             qp, qs = _rows(q, "q", dev, dt, n, H_q, d)
-            qop, qos = _rows(q_out, "q_out", dev, dt, n, H_q, d)
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                qop, qos = q_out.data_ptr(), H_q * d
+            else:
+                qop, qos = _rows(q_out, "q_out", dev, dt, n, H_q, d)
         pages = self._pages(B, block_table)
         if n == 0:
             return q_out
-        with _on(dev) as stream:
-            rc = self.lib.retopk_kv_append(pages, B, lens, cu, n, _TYPE[dt], kp, ks, vp, vs, None if rope is None else rope.h,
-                                           qp, qs, qop, qos, H_q, stream)
-        _check(rc, "retopk_kv_append")
+        rc = _call(dev, self.lib.retopk_kv_append, pages, B, lens, cu, n, _TYPE[dt], kp, ks, vp, vs,
+                   None if rope is None else rope.h, qp, qs, qop, qos, H_q)
+        if rc:
+            _check(rc, "retopk_kv_append")
         return q_out
 
     def gather(self, k_out, v_out, seq_lens, block_table=None, first=None):
@@ -275,11 +276,10 @@ class KVPages:
         pages = self._pages(B, block_table)
         if ref.numel() == 0:
             return k_out, v_out
-        with _on(self.device) as stream:
-            rc = self.lib.retopk_kv_gather(pages, B, lens, start, rows, _TYPE[dt],
-                                           None if k_out is None else k_out.data_ptr(),
-                                           None if v_out is None else v_out.data_ptr(), stream)
-        _check(rc, "retopk_kv_gather")
+        rc = _call(self.device, self.lib.retopk_kv_gather, pages, B, lens, start, rows, _TYPE[dt],
+                   None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr())
+        if rc:
+            _check(rc, "retopk_kv_gather")
         return k_out, v_out
 
     def attend(self, q, seq_lens, block_table=None, scale=None, window=0, out=None, lse=None):
@@ -302,7 +302,7 @@ class KVPages:
             raise ValueError(f"q: tokens have to lie one stride apart and heads {self.d} elements apart, strides are {s}")
         q_stride = H_q * self.d if B * T <= 1 else (s[0] if q.dim() == 3 or T == 1 else s[1])
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.device != dev or out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
             raise TypeError(f"out: contiguous {q.dtype} {tuple(q.shape)} on {dev}")
         if lse is not None and (lse.device != dev or lse.dtype != torch.float32 or lse.shape != q.shape[:-1] or
@@ -312,13 +312,20 @@ class KVPages:
         pages = self._pages(B, block_table)
         if B == 0:
             return out
-        with _on(dev) as stream:
-            need = self.lib.retopk_q4_attention_workspace(B, T, H_q, self.H_kv, self.d)
-            _check(int(min(need, 0)), "retopk_q4_attention_workspace")
-            # from torch's allocator: tied to this stream (and, under capture, to the graph's own pool)
-            ws = torch.empty(need, dtype=torch.uint8, device=dev)
-            rc = self.lib.retopk_q4_attention(pages, B, T, H_q, lens, _TYPE[q.dtype], q.data_ptr(), q_stride,
-                                              self.d ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                              None if lse is None else lse.data_ptr(), ws.data_ptr(), need, stream)
-        _check(rc, "retopk_q4_attention")
+        rc = _call(dev, self._attend, pages, B, T, H_q, lens, _TYPE[q.dtype], q.data_ptr(), q_stride,
+                   self.d ** -0.5 if scale is None else scale, window, out.data_ptr(), None if lse is None else lse.data_ptr())
+        if rc:
+            _check(rc, "retopk_q4_attention")
         return out
+
+    def _attend(self, pages, B, T, H_q, *rest):
+        # (with the device current: the workspace's size depends on it)
+        need = self._needs.get((B, T, H_q))
+        if need is None:
+            need = self.lib.retopk_q4_attention_workspace(B, T, H_q, self.H_kv, self.d)
+            if need < 0:
+                return int(need)
+            self._needs[B, T, H_q] = need
+        # from torch's allocator: tied to this stream (and, under capture, to the graph's own pool)
+        ws = self.k.new_empty(need)
+        return self.lib.retopk_q4_attention(pages, B, T, H_q, *rest[:-1], ws.data_ptr(), need, rest[-1])
