@@ -128,24 +128,34 @@ void set_rotation(RowsArgs& a, const retopk_rope* rope, int inverse) {
     a.amp = rope->amp;
     a.pairs = rope->rot_dim / 2;
     a.inverse = inverse;
-    a.rot_mode = rope->layout == RETOPK_ROPE_INTERLEAVED ? ROT_INTERLEAVED : (rope->rot_dim % 16 == 0 ? ROT_HALF : ROT_HALF_ANY);
 }
 
-// CTAs for n tokens of R rows each: several tokens per CTA where there are many (the sine table and
-// the page look-up then serve more rows), several CTAs per token where there are few.
-template <int DEST> int launch_rows(RowsArgs& a, int dtype, int d, int num_sms, cudaStream_t s) {
-    const int R = a.Hq + a.Hk + a.Hv, at_once = ROWS_THREADS / (d / 16);
-    a.tokens_per_cta = a.n_tokens >= 16ll * num_sms ? 4 : 1;
-    const int fill = (a.tokens_per_cta * R + at_once - 1) / at_once;
-    a.units = a.n_tokens >= 4ll * num_sms ? 1 : fill;
+// CTAs for n tokens of R rows each: a warp per token where that gives every SM warps enough, several
+// warps or CTAs per token below.
+template <int DEST> int launch_rows(RowsArgs& a, const retopk_rope* rope, int dtype, int d, int num_sms, cudaStream_t s) {
+    const int rpw = 32 / (d / 16), groups = (a.Hq + rpw - 1) / rpw + (a.Hk + rpw - 1) / rpw + (a.Hv + rpw - 1) / rpw;
+    const long long want = 16ll * num_sms;               // warps
+    a.tokens_per_cta = a.n_tokens >= want ? 4 : (2 * a.n_tokens >= want ? 2 : 1);
+    // two groups of rows to a warp, if the tokens alone do not fill the device
+    const int per_tok = ROWS_WARPS / a.tokens_per_cta, most = (groups + 2 * per_tok - 1) / (2 * per_tok);
+    const long long need = (want + a.n_tokens * per_tok - 1) / (a.n_tokens * per_tok);
+    a.units = (int)(need < most ? need : most);
+    if (a.units < 1) a.units = 1;
     const long long gx = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
     if (gx > 2147483647ll || a.units > 65535) return RETOPK_EUNSUPPORTED;
     const dim3 grid((unsigned)gx, (unsigned)a.units);
-    if (dtype == RETOPK_BF16)
-        return d == 128 ? launch(rows_kernel<TYPE_BF16, 128, DEST>, grid, ROWS_THREADS, 0, s, a)
-                        : launch(rows_kernel<TYPE_BF16, 64, DEST>, grid, ROWS_THREADS, 0, s, a);
-    return d == 128 ? launch(rows_kernel<TYPE_FP16, 128, DEST>, grid, ROWS_THREADS, 0, s, a)
-                    : launch(rows_kernel<TYPE_FP16, 64, DEST>, grid, ROWS_THREADS, 0, s, a);
+    auto go = [&](auto bf128, auto bf64, auto fp128, auto fp64) {
+        return launch(dtype == RETOPK_BF16 ? (d == 128 ? bf128 : bf64) : (d == 128 ? fp128 : fp64), grid, ROWS_THREADS, 0, s, a);
+    };
+    constexpr int BF = TYPE_BF16, FP = TYPE_FP16;
+    if (!rope || (rope->layout == RETOPK_ROPE_HALF && rope->rot_dim % 16 != 0))
+        return go(rows_kernel<BF, 128, DEST, ROT_OTHER>, rows_kernel<BF, 64, DEST, ROT_OTHER>,
+                  rows_kernel<FP, 128, DEST, ROT_OTHER>, rows_kernel<FP, 64, DEST, ROT_OTHER>);
+    if (rope->layout == RETOPK_ROPE_HALF)
+        return go(rows_kernel<BF, 128, DEST, ROT_HALF>, rows_kernel<BF, 64, DEST, ROT_HALF>,
+                  rows_kernel<FP, 128, DEST, ROT_HALF>, rows_kernel<FP, 64, DEST, ROT_HALF>);
+    return go(rows_kernel<BF, 128, DEST, ROT_INTERLEAVED>, rows_kernel<BF, 64, DEST, ROT_INTERLEAVED>,
+              rows_kernel<FP, 128, DEST, ROT_INTERLEAVED>, rows_kernel<FP, 64, DEST, ROT_INTERLEAVED>);
 }
 
 template <int SRC, int DT> int launch_gather(const GatherArgs& a, int d, dim3 grid, cudaStream_t s) {
@@ -278,7 +288,7 @@ int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, cons
     a.k_out = static_cast<uint16_t*>(k_out); a.k_out_stride = k_out_stride;
     a.Hq = q ? H_q : 0;
     a.Hk = k ? H_k : 0;
-    return launch_rows<DEST_ROWS>(a, dtype, d, num_sms, static_cast<cudaStream_t>(stream));
+    return launch_rows<DEST_ROWS>(a, rope, dtype, d, num_sms, static_cast<cudaStream_t>(stream));
 }
 
 int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* cu_new, int64_t n_new,
@@ -316,8 +326,8 @@ int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     a.Hk = a.Hv = H;
     a.pg = device_pages(pages);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (pages->format == RETOPK_PAGES_Q4) return launch_rows<DEST_PAGES4>(a, dtype, d, num_sms, s);
-    return launch_rows<DEST_PAGES16>(a, dtype, d, num_sms, s);
+    if (pages->format == RETOPK_PAGES_Q4) return launch_rows<DEST_PAGES4>(a, rope, dtype, d, num_sms, s);
+    return launch_rows<DEST_PAGES16>(a, rope, dtype, d, num_sms, s);
 }
 
 int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* first, int64_t max_rows,

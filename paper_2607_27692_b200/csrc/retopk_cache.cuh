@@ -82,16 +82,15 @@ __device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long
 // ---------------------------------------------------------------------------------------
 // rows_kernel: rotate and store
 // ---------------------------------------------------------------------------------------
-enum { ROT_NONE = 0, ROT_HALF = 1, ROT_INTERLEAVED = 2, ROT_HALF_ANY = 3 };
+enum { ROT_HALF = 0, ROT_INTERLEAVED = 1, ROT_OTHER = 2 };    // OTHER: none (pairs = 0), or a half layout of any even size
 enum { DEST_ROWS = 0, DEST_PAGES16 = 1, DEST_PAGES4 = 2 };
-constexpr int ROWS_THREADS = 256;
-constexpr int ROWS_MAX_TOKENS = 8;       // tokens per CTA
+constexpr int ROWS_THREADS = 128, ROWS_WARPS = ROWS_THREADS / 32;
 
 struct RowsArgs {
     double turns[MAX_PAIRS];    // turns per position of each pair: w_i / (2 pi)
     double amp;                 // factor on cosine and sine
-    int pairs, rot_mode, inverse;
-    int tokens_per_cta, units;  // a CTA takes `tokens_per_cta` tokens; blockIdx.y of `units` shares their rows
+    int pairs, inverse;         // pairs = 0: no rotation
+    int tokens_per_cta, units;  // a CTA takes 1, 2 or 4 tokens; blockIdx.y of `units` shares their rows
     long long n_tokens;
     const int32_t* positions;   // DEST_ROWS
     const int32_t *seq_lens, *cu;
@@ -103,48 +102,81 @@ struct RowsArgs {
     Pages pg;
 };
 
-// One row is held by D / 16 lanes, two chunks of 8 channels each.  Where a half-layout rotation
-// covers a multiple of 16 channels, a lane's chunks are partners of each other (c and c + rot/2), so
-// that no value crosses lanes; otherwise they are channels 8l and D/2 + 8l.
+// One row is held by D / 16 lanes, two chunks of 8 channels each, so that a warp has 4 rows (d = 128) or
+// 8; a warp stays with one token and keeps that token's cosines and sines in registers while it goes
+// through the heads, the next two groups of rows on their way.  Where a half-layout rotation covers a multiple of 16
+// channels, a lane's chunks are partners of each other (c and c + rot/2), so that no value crosses
+// lanes; otherwise they are channels 8l and D/2 + 8l.
 //
 // Bound: HBM (two bytes read and written per value).  The angle and the rotation are done in fp64:
 // at far positions an fp32 angle is useless, and a key that is quantised afterwards must round to the
 // same 16-bit value however it is computed.
-template <int DT, int D, int DEST>
-__global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constant__ RowsArgs a) {
+template <int DT, int D, int DEST, int ROT>
+__global__ void __launch_bounds__(ROWS_THREADS, 5) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int LANES = D / 16, RPW = 32 / LANES;      // lanes per row, rows per warp
-    __shared__ double2 s_tab[ROWS_MAX_TOKENS][MAX_PAIRS];
-    __shared__ long long s_row[ROWS_MAX_TOKENS];
-    __shared__ int s_pos[ROWS_MAX_TOKENS];
-    __shared__ int s_live[ROWS_MAX_TOKENS];
+    __shared__ double2 s_tab[ROWS_WARPS][MAX_PAIRS];
+    __shared__ long long s_row[ROWS_WARPS];
+    __shared__ int s_pos[ROWS_WARPS];
+    __shared__ int s_live[ROWS_WARPS];
 
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LANES, row_in = lane / LANES;
     const long long tok0 = (long long)blockIdx.x * a.tokens_per_cta;
     const int n_tok = (int)(a.n_tokens - tok0 < a.tokens_per_cta ? a.n_tokens - tok0 : a.tokens_per_cta);
     pdl_wait();
 
+    // ---- groups of RPW rows: which tensor, which heads; asked for early -------------------------
+    const int per_tok = ROWS_WARPS / a.tokens_per_cta;   // warps per token
+    const int t = warp / per_tok;
+    const bool mine = t < n_tok;
+    const long long tok = tok0 + (mine ? t : 0);
+    const int gq = (a.Hq + RPW - 1) / RPW, gk = (a.Hk + RPW - 1) / RPW, gv = (a.Hv + RPW - 1) / RPW, groups = mine ? gq + gk + gv : 0;
+    const int step = per_tok * a.units;
+    const int half = a.pairs;                            // rot / 2
+    int ca = 8 * sub, cb = D / 2 + 8 * sub;
+    if (ROT == ROT_HALF) {
+        if (8 * sub < half) cb = half + 8 * sub;
+        else { ca = 16 * sub; cb = ca + 8; }             // behind the rotated part
+    }
+    // values keep the same chunks: a row's channels are where they are whichever lane holds them
+    struct Group { int which, h; bool on; uint4 xa, xb; };
+    auto load = [&](int g, Group& r) {
+        r.which = g < gq ? 0 : (g < gq + gk ? 1 : 2);    // q, k or v
+        r.h = (g - (r.which == 0 ? 0 : (r.which == 1 ? gq : gq + gk))) * RPW + row_in;
+        r.on = g < groups && r.h < (r.which == 0 ? a.Hq : (r.which == 1 ? a.Hk : a.Hv));
+        if (!r.on) return;
+        const uint16_t* src = r.which == 0 ? a.q + tok * a.q_stride : (r.which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
+        src += r.h * D;
+        r.xa = *reinterpret_cast<const uint4*>(src + ca);
+        r.xb = *reinterpret_cast<const uint4*>(src + cb);
+    };
+    const int g0 = (int)blockIdx.y * per_tok + warp % per_tok;
+    Group now, next;
+    load(g0, now);
+    load(g0 + step, next);
+
+    // ---- positions, page rows, cosines and sines ------------------------------------------------
     if (tid < n_tok) {
-        const long long tok = tok0 + tid;
+        const long long tk = tok0 + tid;
         int live = 1, pos = 0;
         long long row = -1;
         if (DEST == DEST_ROWS) {
-            pos = a.positions[tok];
+            pos = a.positions[tk];
         } else {
             int b = 0, i = 0, n = 0;
             if (a.cu) {
-                int lo = 0, hi = a.B;                    // largest b with cu[b] <= tok
+                int lo = 0, hi = a.B;                    // largest b with cu[b] <= tk
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
-                    if (a.cu[mid] <= tok) lo = mid; else hi = mid;
+                    if (a.cu[mid] <= tk) lo = mid; else hi = mid;
                 }
                 b = lo;
                 const int first = a.cu[b], last = a.cu[b + 1];
-                live = tok >= first && tok < last;
-                i = (int)(tok - first);
+                live = tk >= first && tk < last;
+                i = (int)(tk - first);
                 n = last - first;
             } else {
-                b = (int)(tok / a.T);
-                i = (int)(tok - (long long)b * a.T);
+                b = (int)(tk / a.T);
+                i = (int)(tk - (long long)b * a.T);
                 n = a.T;
             }
             if (live) {
@@ -159,115 +191,108 @@ __global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constan
         s_live[tid] = live;
     }
     __syncthreads();
-    if (a.rot_mode != ROT_NONE) {
+    if (a.pairs > 0) {
         for (int x = tid; x < n_tok * a.pairs; x += ROWS_THREADS) {
-            const int t = x / a.pairs, i = x - t * a.pairs;
+            const int tt = x / a.pairs, i = x - tt * a.pairs;
             // angle in turns, reduced before it is rounded: position * turns as a product and its rest
-            const double p = (double)s_pos[t], w = a.turns[i];
+            const double p = (double)s_pos[tt], w = a.turns[i];
             const double hi = p * w, lo = fma(p, w, -hi);
             const double r = (hi - rint(hi)) + lo;
             double sn, cs;
             sincospi(2.0 * r, &sn, &cs);
             sn *= a.amp;
             cs *= a.amp;
-            // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the 8 lanes
-            // of a row in different banks
-            s_tab[t][i ^ ((i >> 3) & 7)] = make_double2(cs, a.inverse ? -sn : sn);
+            // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the lanes of
+            // a row in different banks
+            s_tab[tt][i ^ ((i >> 3) & 7)] = make_double2(cs, a.inverse ? -sn : sn);
+        }
+        __syncthreads();
+    }
+    if (!mine) return;
+    const bool live = s_live[t];
+    const long long row0 = s_row[t];
+
+    // pairs of this lane: half layout ca .. ca + 7; interleaved ca/2 .. + 3 and cb/2 .. + 3
+    double2 cs[8];
+    auto tab = [&](int i) { return s_tab[t][i ^ ((i >> 3) & 7)]; };
+    if (ROT == ROT_HALF && 8 * sub < half) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cs[e] = tab(ca + e);
+    } else if (ROT == ROT_INTERLEAVED) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = ca / 2 + e, j = cb / 2 + e;
+            cs[e] = i < half ? tab(i) : make_double2(1.0, 0.0);
+            cs[4 + e] = j < half ? tab(j) : make_double2(1.0, 0.0);
         }
     }
-    __syncthreads();
 
-    const int lane = tid & 31, warp = tid >> 5, sub = lane % LANES;
-    const int rows_per_tok = a.Hq + a.Hk + a.Hv, total = n_tok * rows_per_tok;
-    const int step = (ROWS_THREADS / 32) * RPW * a.units;
-    for (int base = ((int)blockIdx.y * (ROWS_THREADS / 32) + warp) * RPW; base < total; base += step) {
-        const int rid = base + lane / LANES;
-        const int t = rid < total ? rid / rows_per_tok : 0;
-        int h = rid - t * rows_per_tok;
-        const bool active = rid < total && s_live[t];
-        const int which = h < a.Hq ? 0 : (h < a.Hq + a.Hk ? 1 : 2);       // q, k or v
-        h -= which == 0 ? 0 : (which == 1 ? a.Hq : a.Hq + a.Hk);
-        const int mode = which == 2 ? ROT_NONE : a.rot_mode;
-        const long long tok = tok0 + t;
-        const uint16_t* src = which == 0 ? a.q + tok * a.q_stride : (which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
-        src += (long long)h * D;
-        const int half = a.pairs;                                         // rot / 2
-        int ca = 8 * sub, cb = D / 2 + 8 * sub;
-        if (mode == ROT_HALF) {
-            if (8 * sub < half) cb = half + 8 * sub;
-            else { ca = 16 * sub; cb = ca + 8; }                          // behind the rotated part
-        }
+    auto turn = [](double2 c, float& x, float& y) {
+        const double u = x, v = y;
+        x = (float)(u * c.x - v * c.y);
+        y = (float)(v * c.x + u * c.y);
+    };
+    auto finish = [&](const Group& r) {
+        const bool on = r.on && live;
         float xa[8], xb[8];
-        float pa[8], pb[8];                                               // partners, ROT_HALF_ANY only
-        if (active) {
-            unpack8<DT>(*reinterpret_cast<const uint4*>(src + ca), xa);
-            unpack8<DT>(*reinterpret_cast<const uint4*>(src + cb), xb);
-            if (mode == ROT_HALF_ANY) {
+        uint4 ya = r.xa, yb = r.xb;
+        if (r.which != 2 && (ROT != ROT_OTHER || a.pairs > 0)) {
+            unpack8<DT>(r.xa, xa);
+            unpack8<DT>(r.xb, xb);
+            if (ROT == ROT_HALF) {
+                if (8 * sub < half) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int c = ca + e, c2 = cb + e;
-                    pa[e] = c < half ? to_f32<DT>(src[c + half]) : (c < 2 * half ? to_f32<DT>(src[c - half]) : 0.f);
-                    pb[e] = c2 < half ? to_f32<DT>(src[c2 + half]) : (c2 < 2 * half ? to_f32<DT>(src[c2 - half]) : 0.f);
+                    for (int e = 0; e < 8; ++e) turn(cs[e], xa[e], xb[e]);
                 }
-            }
-        }
-        __syncwarp();                     // in place: every lane of the row has read before one writes
-        if (active && mode == ROT_HALF && 8 * sub < half) {
+            } else if (ROT == ROT_INTERLEAVED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double2 cs = s_tab[t][(ca + e) ^ (sub & 7)];
-                const double x = xa[e], y = xb[e];
-                xa[e] = (float)(x * cs.x - y * cs.y);
-                xb[e] = (float)(y * cs.x + x * cs.y);
-            }
-        } else if (active && mode == ROT_INTERLEAVED) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                int i = (ca + e) >> 1;
-                if (i < a.pairs) {
-                    const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
-                    const double x = xa[e], y = xa[e + 1];
-                    xa[e] = (float)(x * cs.x - y * cs.y);
-                    xa[e + 1] = (float)(y * cs.x + x * cs.y);
+                for (int e = 0; e < 4; ++e) {
+                    // (pairs behind the rotated part: 1 * x - 0 * y, but an infinity must pass through)
+                    if (ca / 2 + e < half) turn(cs[e], xa[2 * e], xa[2 * e + 1]);
+                    if (cb / 2 + e < half) turn(cs[4 + e], xb[2 * e], xb[2 * e + 1]);
                 }
-                i = (cb + e) >> 1;
-                if (i < a.pairs) {
-                    const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
-                    const double x = xb[e], y = xb[e + 1];
-                    xb[e] = (float)(x * cs.x - y * cs.y);
-                    xb[e + 1] = (float)(y * cs.x + x * cs.y);
+            } else {
+                // a rotated part that is no multiple of 16 channels: partners lie in other lanes
+                float pa[8], pb[8];
+                if (on) {
+                    const uint16_t* src = (r.which == 0 ? a.q + tok * a.q_stride : a.k + tok * a.k_stride) + r.h * D;
+                    auto partner = [&](int c) { return c < half ? to_f32<DT>(src[c + half]) : (c < 2 * half ? to_f32<DT>(src[c - half]) : 0.f); };
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { pa[e] = partner(ca + e); pb[e] = partner(cb + e); }
                 }
-            }
-        } else if (active && mode == ROT_HALF_ANY) {
+                __syncwarp();             // in place: every lane of the row has read before one writes
+                if (on) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < 8; ++e) {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int c = (s ? cb : ca) + e;
-                    float& x = s ? xb[e] : xa[e];
-                    const double own = x, other = s ? pb[e] : pa[e];
-                    if (c < 2 * half) {
-                        const int i = c < half ? c : c - half;
-                        const double2 cs = s_tab[t][i ^ ((i >> 3) & 7)];
-                        x = (float)(own * cs.x + (c < half ? -other : other) * cs.y);
+                        for (int s = 0; s < 2; ++s) {
+                            const int c = (s ? cb : ca) + e;
+                            float& x = s ? xb[e] : xa[e];
+                            const double own = x, other = s ? pb[e] : pa[e];
+                            if (c < 2 * half) {
+                                const double2 z = tab(c < half ? c : c - half);
+                                x = (float)(own * z.x + (c < half ? -other : other) * z.y);
+                            }
+                        }
                     }
                 }
             }
+            ya = pack8<DT>(xa);
+            yb = pack8<DT>(xb);
         }
-        const uint4 ya = pack8<DT>(xa), yb = pack8<DT>(xb);
-        if (DEST == DEST_ROWS || which == 0) {
-            if (active) {
-                uint16_t* dst = (which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + (long long)h * D;
+        if (DEST == DEST_ROWS || r.which == 0) {
+            if (on) {
+                uint16_t* dst = (r.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + r.h * D;
                 *reinterpret_cast<uint4*>(dst + ca) = ya;
                 *reinterpret_cast<uint4*>(dst + cb) = yb;
             }
-            if (DEST != DEST_PAGES4) continue;
+            return;                       // (a group is of one tensor: the whole warp returns)
         }
-        const long long row = s_row[t] + (long long)h * a.pg.page_size;
-        const bool store = active && which != 0 && s_row[t] >= 0;
+        const long long row = row0 + (long long)r.h * a.pg.page_size;
+        const bool store = on && row0 >= 0;
         if (DEST == DEST_PAGES16) {
             if (store) {
-                uint16_t* dst = reinterpret_cast<uint16_t*>(which == 1 ? a.pg.k : a.pg.v) + row * D;
+                uint16_t* dst = reinterpret_cast<uint16_t*>(r.which == 1 ? a.pg.k : a.pg.v) + row * D;
                 *reinterpret_cast<uint4*>(dst + ca) = ya;
                 *reinterpret_cast<uint4*>(dst + cb) = yb;
             }
@@ -297,8 +322,9 @@ __global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constan
                 // the minimum may have been rounded up past the maximum of a narrow group
                 step_[g] = __bfloat162float(__float2bfloat16_rn(fmaxf(__fdiv_rn(mx - low[g], 15.f), 0.f)));
             }
+            const float la = ga == 0 ? low[0] : low[NG - 1], sa = ga == 0 ? step_[0] : step_[NG - 1];
+            const float lb = gb == 0 ? low[0] : low[NG - 1], sb = gb == 0 ? step_[0] : step_[NG - 1];
             uint32_t wa = 0, wb = 0;
-            const float la = low[ga < NG ? ga : 0], sa = step_[ga < NG ? ga : 0], lb = low[gb < NG ? gb : 0], sb = step_[gb < NG ? gb : 0];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float na = sa > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(xa[e] - la, sa)), 0.f), 15.f) : 0.f;
@@ -307,16 +333,23 @@ __global__ void __launch_bounds__(ROWS_THREADS) rows_kernel(const __grid_constan
                 wb |= (uint32_t)(int)nb << (4 * e);
             }
             if (store) {
-                unsigned char* dst = (which == 1 ? a.pg.k : a.pg.v) + row * (D / 2);
+                unsigned char* dst = (r.which == 1 ? a.pg.k : a.pg.v) + row * (D / 2);
                 *reinterpret_cast<uint32_t*>(dst + ca / 2) = wa;
                 *reinterpret_cast<uint32_t*>(dst + cb / 2) = wb;
                 if (sub < NG) {
-                    const float s = sub == 0 ? step_[0] : step_[NG - 1], m = sub == 0 ? low[0] : low[NG - 1];
-                    uint32_t* sc = reinterpret_cast<uint32_t*>(which == 1 ? a.pg.ks : a.pg.vs) + row * NG;
-                    sc[sub] = pack2<TYPE_BF16>(s, m);
+                    uint32_t* sc = reinterpret_cast<uint32_t*>(r.which == 1 ? a.pg.ks : a.pg.vs) + row * NG;
+                    sc[sub] = pack2<TYPE_BF16>(sub == 0 ? step_[0] : step_[NG - 1], sub == 0 ? low[0] : low[NG - 1]);
                 }
             }
         }
+    };
+#pragma unroll 1
+    for (int g = g0; g < groups; g += step) {
+        Group later;
+        load(g + 2 * step, later);
+        finish(now);
+        now = next;
+        next = later;
     }
 }
 
