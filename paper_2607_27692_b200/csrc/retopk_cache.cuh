@@ -84,7 +84,7 @@ __device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long
 // ---------------------------------------------------------------------------------------
 enum { ROT_HALF = 0, ROT_INTERLEAVED = 1, ROT_OTHER = 2 };    // OTHER: none (pairs = 0), or a half layout of any even size
 enum { DEST_ROWS = 0, DEST_PAGES16 = 1, DEST_PAGES4 = 2 };
-constexpr int ROWS_THREADS = 128, ROWS_WARPS = ROWS_THREADS / 32;
+constexpr int ROWS_THREADS = 128, ROWS_WARPS = ROWS_THREADS / 32, ROWS_CTAS = 6;
 
 struct RowsArgs {
     double turns[MAX_PAIRS];    // turns per position of each pair: w_i / (2 pi)
@@ -104,201 +104,189 @@ struct RowsArgs {
 
 // One row is held by D / 16 lanes, two chunks of 8 channels each, so that a warp has 4 rows (d = 128) or
 // 8; a warp stays with one token and keeps that token's cosines and sines in registers while it goes
-// through the heads, the next two groups of rows on their way.  Where a half-layout rotation covers a multiple of 16
+// through the heads, two groups of rows at a time.  Where a half-layout rotation covers a multiple of 16
 // channels, a lane's chunks are partners of each other (c and c + rot/2), so that no value crosses
 // lanes; otherwise they are channels 8l and D/2 + 8l.
 //
-// Bound: HBM (two bytes read and written per value).  The angle and the rotation are done in fp64:
-// at far positions an fp32 angle is useless, and a key that is quantised afterwards must round to the
-// same 16-bit value however it is computed.
+// Bound: HBM (two bytes read and written per value).  The angle is reduced and its cosine and sine are
+// taken in fp64: at far positions an fp32 angle is useless.  The rotation itself: cosine and sine are
+// split into a head of so few bits that its product with a 16-bit value is exact in fp32 (16 bits for
+// bf16, 13 for fp16) and a rest, so that x ch - y sh is rounded once, whatever cancels, and the rests
+// add what is missing: 2^-23 of the result, before it is rounded to 16 bits.  Keys that are quantised
+// afterwards are rotated in fp64: a 16-bit value that is one step off could change a code.  (All in
+// fp64, 16K tokens of 40 heads took 71 us: the conversions from and to fp32 fill their pipe.)
 template <int DT, int D, int DEST, int ROT>
-__global__ void __launch_bounds__(ROWS_THREADS, 5) rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int LANES = D / 16, RPW = 32 / LANES;      // lanes per row, rows per warp
-    __shared__ double2 s_tab[ROWS_WARPS][MAX_PAIRS];
-    __shared__ long long s_row[ROWS_WARPS];
-    __shared__ int s_pos[ROWS_WARPS];
-    __shared__ int s_live[ROWS_WARPS];
+    __shared__ float4 s_tab[ROWS_WARPS][MAX_PAIRS];      // heads and rests of cosine and sine
+    __shared__ double2 s_tab64[DEST == DEST_PAGES4 ? ROWS_WARPS : 1][MAX_PAIRS];
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane % LANES, row_in = lane / LANES;
-    const long long tok0 = (long long)blockIdx.x * a.tokens_per_cta;
-    const int n_tok = (int)(a.n_tokens - tok0 < a.tokens_per_cta ? a.n_tokens - tok0 : a.tokens_per_cta);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES, row_in = lane / LANES;
+    const int per_tok = ROWS_WARPS / a.tokens_per_cta;   // warps per token; each keeps a table of its own
+    const long long tok = (long long)blockIdx.x * a.tokens_per_cta + warp / per_tok;
     pdl_wait();
+    if (tok >= a.n_tokens) return;
 
-    // ---- groups of RPW rows: which tensor, which heads; asked for early -------------------------
-    const int per_tok = ROWS_WARPS / a.tokens_per_cta;   // warps per token
-    const int t = warp / per_tok;
-    const bool mine = t < n_tok;
-    const long long tok = tok0 + (mine ? t : 0);
-    const int gq = (a.Hq + RPW - 1) / RPW, gk = (a.Hk + RPW - 1) / RPW, gv = (a.Hv + RPW - 1) / RPW, groups = mine ? gq + gk + gv : 0;
-    const int step = per_tok * a.units;
     const int half = a.pairs;                            // rot / 2
     int ca = 8 * sub, cb = D / 2 + 8 * sub;
     if (ROT == ROT_HALF) {
         if (8 * sub < half) cb = half + 8 * sub;
         else { ca = 16 * sub; cb = ca + 8; }             // behind the rotated part
     }
-    // values keep the same chunks: a row's channels are where they are whichever lane holds them
-    struct Group { int which, h; bool on; uint4 xa, xb; };
-    auto load = [&](int g, Group& r) {
-        r.which = g < gq ? 0 : (g < gq + gk ? 1 : 2);    // q, k or v
-        r.h = (g - (r.which == 0 ? 0 : (r.which == 1 ? gq : gq + gk))) * RPW + row_in;
-        r.on = g < groups && r.h < (r.which == 0 ? a.Hq : (r.which == 1 ? a.Hk : a.Hv));
-        if (!r.on) return;
-        const uint16_t* src = r.which == 0 ? a.q + tok * a.q_stride : (r.which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
-        src += r.h * D;
-        r.xa = *reinterpret_cast<const uint4*>(src + ca);
-        r.xb = *reinterpret_cast<const uint4*>(src + cb);
-    };
-    const int g0 = (int)blockIdx.y * per_tok + warp % per_tok;
-    Group now, next;
-    load(g0, now);
-    load(g0 + step, next);
 
-    // ---- positions, page rows, cosines and sines ------------------------------------------------
-    if (tid < n_tok) {
-        const long long tk = tok0 + tid;
-        int live = 1, pos = 0;
-        long long row = -1;
-        if (DEST == DEST_ROWS) {
-            pos = a.positions[tk];
+    // ---- where this warp's rows are -------------------------------------------------------------
+    // Groups of RPW rows of q, then k, then v are dealt out in turn to the warps of a token.  A cursor is
+    // a tensor and a group in it; PER groups of one tensor are taken at a time, the next ones on their way.
+    constexpr int PER = DEST == DEST_PAGES4 ? 1 : 2;     // (quantising twice over is too much code: 40 against 31 us, 6K tokens)
+    const int step = per_tok * a.units;
+    struct Cursor { int which, g; };
+    auto heads_of = [&](int which) { return which == 0 ? a.Hq : (which == 1 ? a.Hk : a.Hv); };
+    auto settle = [&](Cursor& c) {                       // to the first tensor that has group c.g
+        while (c.which < 3) {
+            const int groups = (heads_of(c.which) + RPW - 1) / RPW;
+            if (c.g < groups) break;
+            c.g -= groups;
+            ++c.which;
+        }
+    };
+    auto advance = [&](Cursor c) {
+        const int groups = (heads_of(c.which) + RPW - 1) / RPW;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (c.g < groups) c.g += step;
+        settle(c);
+        return c;
+    };
+    auto source = [&](int which) {
+        return which == 0 ? a.q + tok * a.q_stride : (which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
+    };
+    auto fetch = [&](Cursor c, uint4 (&fa)[PER], uint4 (&fb)[PER]) {
+        if (c.which >= 3) return;
+        const int heads = heads_of(c.which), h = c.g * RPW + row_in;
+        const uint16_t* src = source(c.which) + h * D;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (h + i * step * RPW < heads) {
+                fa[i] = *reinterpret_cast<const uint4*>(src + i * step * (RPW * D) + ca);
+                fb[i] = *reinterpret_cast<const uint4*>(src + i * step * (RPW * D) + cb);
+            }
+    };
+    uint4 ya[PER], yb[PER];
+    Cursor cur = {0, (int)blockIdx.y * per_tok + warp % per_tok};
+    settle(cur);
+    fetch(cur, ya, yb);                                  // on their way while position and page are looked up
+
+    // ---- position and page row, by the whole warp -----------------------------------------------
+    int pos = 0;
+    long long row0 = -1;                                 // page row for head 0, -1: not stored
+    if (DEST == DEST_ROWS) {
+        pos = a.positions[tok];
+    } else {
+        long long p = -1;
+        int b = 0;
+        if (a.cu) {
+            // largest b < B with cu[b] <= tok, 32 candidates at a time
+            int lo = 0, n = a.B;
+            while (n > 1) {
+                const int hop = (n + 31) / 32, at = lane * hop;
+                const uint32_t le = __ballot_sync(0xffffffffu, at < n && a.cu[lo + at] <= tok);
+                const int last = le ? 31 - __clz((int)le) : 0;
+                lo += last * hop;
+                n = n - last * hop < hop ? n - last * hop : hop;
+            }
+            b = lo;
+            const int first = a.cu[b], end = a.cu[b + 1], len = a.seq_lens[b];
+            if (tok >= first && tok < end) p = (long long)len - end + tok;
         } else {
-            int b = 0, i = 0, n = 0;
-            if (a.cu) {
-                int lo = 0, hi = a.B;                    // largest b with cu[b] <= tk
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (a.cu[mid] <= tk) lo = mid; else hi = mid;
-                }
-                b = lo;
-                const int first = a.cu[b], last = a.cu[b + 1];
-                live = tk >= first && tk < last;
-                i = (int)(tk - first);
-                n = last - first;
-            } else {
-                b = (int)(tk / a.T);
-                i = (int)(tk - (long long)b * a.T);
-                n = a.T;
-            }
-            if (live) {
-                const long long p = (long long)a.seq_lens[b] - n + i;
-                live = p >= 0;
-                pos = (int)p;
-                row = cache_row(a.pg, b, p);
-            }
+            b = (int)(tok / a.T);
+            p = (long long)a.seq_lens[b] - a.T + (tok - (long long)b * a.T);
         }
-        s_pos[tid] = pos;
-        s_row[tid] = row;
-        s_live[tid] = live;
-    }
-    __syncthreads();
-    if (a.pairs > 0) {
-        for (int x = tid; x < n_tok * a.pairs; x += ROWS_THREADS) {
-            const int tt = x / a.pairs, i = x - tt * a.pairs;
-            // angle in turns, reduced before it is rounded: position * turns as a product and its rest
-            const double p = (double)s_pos[tt], w = a.turns[i];
-            const double hi = p * w, lo = fma(p, w, -hi);
-            const double r = (hi - rint(hi)) + lo;
-            double sn, cs;
-            sincospi(2.0 * r, &sn, &cs);
-            sn *= a.amp;
-            cs *= a.amp;
-            // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the lanes of
-            // a row in different banks
-            s_tab[tt][i ^ ((i >> 3) & 7)] = make_double2(cs, a.inverse ? -sn : sn);
-        }
-        __syncthreads();
-    }
-    if (!mine) return;
-    const bool live = s_live[t];
-    const long long row0 = s_row[t];
-
-    // pairs of this lane: half layout ca .. ca + 7; interleaved ca/2 .. + 3 and cb/2 .. + 3
-    double2 cs[8];
-    auto tab = [&](int i) { return s_tab[t][i ^ ((i >> 3) & 7)]; };
-    if (ROT == ROT_HALF && 8 * sub < half) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) cs[e] = tab(ca + e);
-    } else if (ROT == ROT_INTERLEAVED) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = ca / 2 + e, j = cb / 2 + e;
-            cs[e] = i < half ? tab(i) : make_double2(1.0, 0.0);
-            cs[4 + e] = j < half ? tab(j) : make_double2(1.0, 0.0);
-        }
+        if (p < 0) return;                               // belongs to no sequence, or has no place
+        pos = (int)p;
+        row0 = cache_row(a.pg, b, p);
     }
 
-    auto turn = [](double2 c, float& x, float& y) {
-        const double u = x, v = y;
-        x = (float)(u * c.x - v * c.y);
-        y = (float)(v * c.x + u * c.y);
+    // ---- cosines and sines of this position -----------------------------------------------------
+    for (int i = lane; i < a.pairs; i += 32) {
+        // angle in turns, reduced before it is rounded: position * turns as a product and its rest
+        const double p = (double)pos, w = a.turns[i];
+        const double hi = p * w, lo = fma(p, w, -hi);
+        const double r = (hi - rint(hi)) + lo;
+        double sn, cs;
+        sincospi(2.0 * r, &sn, &cs);
+        sn *= a.amp;
+        cs *= a.amp;
+        if (a.inverse) sn = -sn;
+        // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the lanes of a
+        // row in different banks
+        const int at = i ^ ((i >> 3) & 7);
+        constexpr uint32_t HEAD = DT == TYPE_BF16 ? 0xffffff00u : 0xfffff800u;
+        const float ch = __uint_as_float(__float_as_uint((float)cs) & HEAD), sh = __uint_as_float(__float_as_uint((float)sn) & HEAD);
+        s_tab[warp][at] = make_float4(ch, (float)(cs - ch), sh, (float)(sn - sh));
+        if (DEST == DEST_PAGES4) s_tab64[DEST == DEST_PAGES4 ? warp : 0][at] = make_double2(cs, sn);
+    }
+    __syncwarp();
+
+    // pair i turned: (x, y) -> (x c - y s, y c + x s)
+    auto turn = [&](bool exact, int i, float& x, float& y) {
+        const int at = i ^ ((i >> 3) & 7);
+        if (DEST == DEST_PAGES4 && exact) {
+            const double2 c = s_tab64[DEST == DEST_PAGES4 ? warp : 0][at];
+            const double u = x, v = y;
+            x = (float)(u * c.x - v * c.y);
+            y = (float)(v * c.x + u * c.y);
+        } else {
+            const float4 c = s_tab[warp][at];
+            const float u = x, v = y;
+            x = fmaf(-v, c.z, u * c.x) + fmaf(-v, c.w, u * c.y);
+            y = fmaf(u, c.z, v * c.x) + fmaf(u, c.w, v * c.y);
+        }
     };
-    auto finish = [&](const Group& r) {
-        const bool on = r.on && live;
+    // 16 channels of one row, in place; src: the row itself (for partners in other lanes), on: it exists
+    auto rotate = [&](bool exact, uint4& ya, uint4& yb, const uint16_t* src, bool on) {
+        if (ROT == ROT_OTHER && a.pairs == 0) return;
         float xa[8], xb[8];
-        uint4 ya = r.xa, yb = r.xb;
-        if (r.which != 2 && (ROT != ROT_OTHER || a.pairs > 0)) {
-            unpack8<DT>(r.xa, xa);
-            unpack8<DT>(r.xb, xb);
-            if (ROT == ROT_HALF) {
-                if (8 * sub < half) {
+        unpack8<DT>(ya, xa);
+        unpack8<DT>(yb, xb);
+        if (ROT == ROT_HALF) {
+            if (8 * sub >= half) return;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) turn(cs[e], xa[e], xb[e]);
-                }
-            } else if (ROT == ROT_INTERLEAVED) {
+            for (int e = 0; e < 8; ++e) turn(exact, ca + e, xa[e], xb[e]);
+        } else if (ROT == ROT_INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    // (pairs behind the rotated part: 1 * x - 0 * y, but an infinity must pass through)
-                    if (ca / 2 + e < half) turn(cs[e], xa[2 * e], xa[2 * e + 1]);
-                    if (cb / 2 + e < half) turn(cs[4 + e], xb[2 * e], xb[2 * e + 1]);
-                }
-            } else {
-                // a rotated part that is no multiple of 16 channels: partners lie in other lanes
-                float pa[8], pb[8];
-                if (on) {
-                    const uint16_t* src = (r.which == 0 ? a.q + tok * a.q_stride : a.k + tok * a.k_stride) + r.h * D;
-                    auto partner = [&](int c) { return c < half ? to_f32<DT>(src[c + half]) : (c < 2 * half ? to_f32<DT>(src[c - half]) : 0.f); };
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { pa[e] = partner(ca + e); pb[e] = partner(cb + e); }
-                }
-                __syncwarp();             // in place: every lane of the row has read before one writes
-                if (on) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            const int c = (s ? cb : ca) + e;
-                            float& x = s ? xb[e] : xa[e];
-                            const double own = x, other = s ? pb[e] : pa[e];
-                            if (c < 2 * half) {
-                                const double2 z = tab(c < half ? c : c - half);
-                                x = (float)(own * z.x + (c < half ? -other : other) * z.y);
-                            }
-                        }
-                    }
-                }
+            for (int e = 0; e < 4; ++e) {
+                if (ca / 2 + e < half) turn(exact, ca / 2 + e, xa[2 * e], xa[2 * e + 1]);
+                if (cb / 2 + e < half) turn(exact, cb / 2 + e, xb[2 * e], xb[2 * e + 1]);
             }
-            ya = pack8<DT>(xa);
-            yb = pack8<DT>(xb);
-        }
-        if (DEST == DEST_ROWS || r.which == 0) {
+        } else {
+            // a rotated part that is no multiple of 16 channels: partners lie in other lanes
+            float pa[8], pb[8];
             if (on) {
-                uint16_t* dst = (r.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + r.h * D;
-                *reinterpret_cast<uint4*>(dst + ca) = ya;
-                *reinterpret_cast<uint4*>(dst + cb) = yb;
+                auto partner = [&](int c) { return c < half ? to_f32<DT>(src[c + half]) : (c < 2 * half ? to_f32<DT>(src[c - half]) : 0.f); };
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { pa[e] = partner(ca + e); pb[e] = partner(cb + e); }
             }
-            return;                       // (a group is of one tensor: the whole warp returns)
+            __syncwarp();                 // in place: every lane of the row has read before one writes
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int c = (s ? cb : ca) + e;
+                    float& x = s ? xb[e] : xa[e];
+                    float other = s ? pb[e] : pa[e];
+                    if (on && c < half) turn(exact, c, x, other);
+                    else if (on && c < 2 * half) turn(exact, c - half, other, x);
+                }
+            }
         }
-        const long long row = row0 + (long long)r.h * a.pg.page_size;
-        const bool store = on && row0 >= 0;
-        if (DEST == DEST_PAGES16) {
-            if (store) {
-                uint16_t* dst = reinterpret_cast<uint16_t*>(r.which == 1 ? a.pg.k : a.pg.v) + row * D;
-                *reinterpret_cast<uint4*>(dst + ca) = ya;
-                *reinterpret_cast<uint4*>(dst + cb) = yb;
-            }
-        } else if (DEST == DEST_PAGES4) {
-            // quantise the 16-bit values: minimum and maximum of each group over the lanes of the row
+        ya = pack8<DT>(xa);
+        yb = pack8<DT>(xb);
+    };
+    // quantise one row's 16-bit values and store codes, step and minimum
+    auto quantise = [&](const uint4& ya, const uint4& yb, unsigned char* codes, unsigned char* scales, long long row, bool store) {
             constexpr int NG = D / GROUP;
+            float xa[8], xb[8];
+            // quantise the 16-bit values: minimum and maximum of each group over the lanes of the row
             unpack8<DT>(ya, xa);
             unpack8<DT>(yb, xb);
             float mna = xa[0], mxa = xa[0], mnb = xb[0], mxb = xb[0];
@@ -333,23 +321,47 @@ __global__ void __launch_bounds__(ROWS_THREADS, 5) rows_kernel(const __grid_cons
                 wb |= (uint32_t)(int)nb << (4 * e);
             }
             if (store) {
-                unsigned char* dst = (r.which == 1 ? a.pg.k : a.pg.v) + row * (D / 2);
+                unsigned char* dst = codes + row * (D / 2);
                 *reinterpret_cast<uint32_t*>(dst + ca / 2) = wa;
                 *reinterpret_cast<uint32_t*>(dst + cb / 2) = wb;
-                if (sub < NG) {
-                    uint32_t* sc = reinterpret_cast<uint32_t*>(r.which == 1 ? a.pg.ks : a.pg.vs) + row * NG;
-                    sc[sub] = pack2<TYPE_BF16>(sub == 0 ? step_[0] : step_[NG - 1], sub == 0 ? low[0] : low[NG - 1]);
+                if (sub < NG)
+                    reinterpret_cast<uint32_t*>(scales)[row * NG + sub] = pack2<TYPE_BF16>(sub == 0 ? step_[0] : step_[NG - 1], sub == 0 ? low[0] : low[NG - 1]);
+            }
+    };
+
+#pragma unroll 1
+    while (cur.which < 3) {
+        const Cursor next = advance(cur);
+        uint4 na[PER], nb[PER];
+        fetch(next, na, nb);
+        const int heads = heads_of(cur.which), h0 = cur.g * RPW + row_in;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int h = h0 + i * step * RPW;
+            const bool on = h < heads;
+            // (values go in as they are; their chunks are where the lane's are)
+            if (cur.which != 2) rotate(DEST == DEST_PAGES4 && cur.which == 1, ya[i], yb[i], source(cur.which) + h * D, on);
+            if (DEST == DEST_ROWS || cur.which == 0) {
+                if (on) {
+                    uint16_t* dst = (cur.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + h * D;
+                    *reinterpret_cast<uint4*>(dst + ca) = ya[i];
+                    *reinterpret_cast<uint4*>(dst + cb) = yb[i];
+                }
+            } else {
+                const long long row = row0 + (long long)h * a.pg.page_size;
+                unsigned char* pages = cur.which == 1 ? a.pg.k : a.pg.v;
+                if (DEST == DEST_PAGES4) {
+                    quantise(ya[i], yb[i], pages, cur.which == 1 ? a.pg.ks : a.pg.vs, row, on && row0 >= 0);
+                } else if (on && row0 >= 0) {
+                    uint16_t* dst = reinterpret_cast<uint16_t*>(pages) + row * D;
+                    *reinterpret_cast<uint4*>(dst + ca) = ya[i];
+                    *reinterpret_cast<uint4*>(dst + cb) = yb[i];
                 }
             }
+            ya[i] = na[i];
+            yb[i] = nb[i];
         }
-    };
-#pragma unroll 1
-    for (int g = g0; g < groups; g += step) {
-        Group later;
-        load(g + 2 * step, later);
-        finish(now);
-        now = next;
-        next = later;
+        cur = next;
     }
 }
 
@@ -366,9 +378,13 @@ struct GatherArgs {
     void *k_out, *v_out;
 };
 
+// One row is held by D / 8 lanes with 8 channels each, for fp32 results 4 in each half of the row, so
+// that every store instruction writes whole sectors.  All of a thread's loads, keys and values, are
+// asked for before the first is used.  Bound: HBM, mostly the writes.
 template <int SRC /* 0 bf16, 1 fp16, 2: four bits */, int DT, int D>
 __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_constant__ GatherArgs a) {
     constexpr int LANES = D / 8, RPP = GATHER_THREADS / LANES, PASSES = GATHER_ROWS / RPP;
+    constexpr bool SPLIT = DT == TYPE_FP32;              // 4 + 4 channels instead of 8
     pdl_wait();
     const int b = blockIdx.z, h = blockIdx.y;
     const long long row0 = (long long)blockIdx.x * GATHER_ROWS;
@@ -377,6 +393,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
     if (len > a.pg.capacity) len = a.pg.capacity;
     if (first + row0 >= len) return;
     const int sub = threadIdx.x % LANES, r0 = threadIdx.x / LANES;
+    const int c0 = SPLIT ? 4 * sub : 8 * sub, c1 = SPLIT ? D / 2 + 4 * sub : 8 * sub + 4;
     long long src_row[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
@@ -387,43 +404,68 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
             if (src_row[p] >= 0) src_row[p] += (long long)h * a.pg.page_size;
         }
     }
+    uint2 x0[2][PASSES], x1[2][PASSES];                  // 16 bits: four values each; 4 bits: codes and scale
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        if (!(kv ? a.v_out : a.k_out)) continue;
+        const unsigned char* base = kv ? a.pg.v : a.pg.k;
+        const unsigned char* sbase = kv ? a.pg.vs : a.pg.ks;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            if (src_row[p] < 0) continue;
+            if (SRC == 2) {
+                const unsigned char* row = base + src_row[p] * (D / 2);
+                const unsigned char* sc = sbase + src_row[p] * (D / GROUP * 4);
+                if (SPLIT) {
+                    x0[kv][p].x = *reinterpret_cast<const uint16_t*>(row + c0 / 2);
+                    x1[kv][p].x = *reinterpret_cast<const uint16_t*>(row + c1 / 2);
+                } else {
+                    x0[kv][p].x = *reinterpret_cast<const uint32_t*>(row + c0 / 2);
+                    x1[kv][p].x = x0[kv][p].x >> 16;
+                }
+                x0[kv][p].y = *reinterpret_cast<const uint32_t*>(sc + c0 / GROUP * 4);
+                x1[kv][p].y = SPLIT ? *reinterpret_cast<const uint32_t*>(sc + c1 / GROUP * 4) : x0[kv][p].y;
+            } else {
+                const unsigned char* row = base + src_row[p] * (D * 2);
+                if (SPLIT) {
+                    x0[kv][p] = *reinterpret_cast<const uint2*>(row + c0 * 2);
+                    x1[kv][p] = *reinterpret_cast<const uint2*>(row + c1 * 2);
+                } else {
+                    const uint4 x = *reinterpret_cast<const uint4*>(row + c0 * 2);
+                    x0[kv][p] = make_uint2(x.x, x.y);
+                    x1[kv][p] = make_uint2(x.z, x.w);
+                }
+            }
+        }
+    }
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
         void* out = kv ? a.v_out : a.k_out;
         if (!out) continue;
-        const unsigned char* base = kv ? a.pg.v : a.pg.k;
-        const unsigned char* sbase = kv ? a.pg.vs : a.pg.ks;
-        uint4 raw[PASSES];
-        uint32_t sc[PASSES];
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             if (src_row[p] < 0) continue;
-            if (SRC == 2) {
-                raw[p].x = *reinterpret_cast<const uint32_t*>(base + src_row[p] * (D / 2) + sub * 4);
-                sc[p] = *reinterpret_cast<const uint32_t*>(sbase + (src_row[p] * (D / GROUP) + sub * 8 / GROUP) * 4);
-            } else {
-                raw[p] = *reinterpret_cast<const uint4*>(base + (src_row[p] * D + sub * 8) * 2);
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            if (src_row[p] < 0) continue;
-            const long long i = row0 + r0 + p * RPP;
-            const long long at = (((long long)b * a.pg.H_kv + h) * a.max_rows + i) * D + sub * 8;
+            const long long at = (((long long)b * a.pg.H_kv + h) * a.max_rows + row0 + r0 + p * RPP) * D;
             float f[8];
-            if (SRC == 2) {
-                const float2 sm = unpack2<TYPE_BF16>(sc[p]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = fmaf((float)((raw[p].x >> (4 * e)) & 15u), sm.x, sm.y);
-            } else if (DT == TYPE_FP32) {
-                unpack8<SRC == 2 ? 0 : SRC>(raw[p], f);
+            for (int half = 0; half < 2; ++half) {
+                const uint2 x = half ? x1[kv][p] : x0[kv][p];
+                if (SRC == 2) {
+                    const float2 sm = unpack2<TYPE_BF16>(x.y);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[4 * half + e] = fmaf((float)((x.x >> (4 * e)) & 15u), sm.x, sm.y);
+                } else if (SPLIT) {
+                    const float2 lo = unpack2<SRC == 2 ? 0 : SRC>(x.x), hi = unpack2<SRC == 2 ? 0 : SRC>(x.y);
+                    f[4 * half] = lo.x; f[4 * half + 1] = lo.y; f[4 * half + 2] = hi.x; f[4 * half + 3] = hi.y;
+                }
             }
-            if (DT == TYPE_FP32) {
-                float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + at);
-                o[0] = make_float4(f[0], f[1], f[2], f[3]);
-                o[1] = make_float4(f[4], f[5], f[6], f[7]);
+            if (SPLIT) {
+                float* o = static_cast<float*>(out) + at;
+                *reinterpret_cast<float4*>(o + c0) = make_float4(f[0], f[1], f[2], f[3]);
+                *reinterpret_cast<float4*>(o + c1) = make_float4(f[4], f[5], f[6], f[7]);
             } else {
-                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = SRC == 2 ? pack8<DT>(f) : raw[p];
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c0) =
+                    SRC == 2 ? pack8<SPLIT ? 0 : DT>(f) : make_uint4(x0[kv][p].x, x0[kv][p].y, x1[kv][p].x, x1[kv][p].y);
             }
         }
     }
