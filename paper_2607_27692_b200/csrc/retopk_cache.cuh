@@ -50,6 +50,17 @@ template <int DT> __device__ __forceinline__ uint4 pack8(const float* f) {
     return make_uint4(pack2<DT>(f[0], f[1]), pack2<DT>(f[2], f[3]), pack2<DT>(f[4], f[5]), pack2<DT>(f[6], f[7]));
 }
 
+__device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16x2_sub(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
 __device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(src) : "memory");
 }
@@ -380,7 +391,9 @@ struct GatherArgs {
 
 // One row is held by D / 8 lanes with 8 channels each, for fp32 results 4 in each half of the row, so
 // that every store instruction writes whole sectors.  All of a thread's loads, keys and values, are
-// asked for before the first is used.  Bound: HBM, mostly the writes.
+// asked for before the first is used.  Bound: HBM, mostly the writes; but a code at a time through
+// integer conversion it was the ALU (4 x 32K rows to bf16: 127 us at 76% ALU).  bf16 results take two
+// codes to a packed multiply-add, s n + m with its one rounding; 128 + n is a mask away.
 template <int SRC /* 0 bf16, 1 fp16, 2: four bits */, int DT, int D>
 __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_constant__ GatherArgs a) {
     constexpr int LANES = D / 8, RPP = GATHER_THREADS / LANES, PASSES = GATHER_ROWS / RPP;
@@ -446,6 +459,19 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
         for (int p = 0; p < PASSES; ++p) {
             if (src_row[p] < 0) continue;
             const long long at = (((long long)b * a.pg.H_kv + h) * a.max_rows + row0 + r0 + p * RPP) * D;
+            if (SRC == 2 && DT == TYPE_BF16) {
+                const uint32_t x = x0[kv][p].x, sm = x0[kv][p].y;
+                uint32_t v[4];                           // values (0,4) (1,5) (2,6) (3,7)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t n = ((x >> (4 * e)) & 0x000f000fu) | 0x43004300u;
+                    v[e] = bf16x2_fma(bf16x2_sub(n, 0x43004300u), __byte_perm(sm, sm, 0x1010), __byte_perm(sm, sm, 0x3232));
+                }
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c0) =
+                    make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
+                               __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+                continue;
+            }
             float f[8];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -453,7 +479,10 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
                 if (SRC == 2) {
                     const float2 sm = unpack2<TYPE_BF16>(x.y);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[4 * half + e] = fmaf((float)((x.x >> (4 * e)) & 15u), sm.x, sm.y);
+                    for (int e = 0; e < 4; ++e) {        // 2^23 + n is a mask away too
+                        const float n = __uint_as_float(((x.x >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.f;
+                        f[4 * half + e] = fmaf(n, sm.x, sm.y);
+                    }
                 } else if (SPLIT) {
                     const float2 lo = unpack2<SRC == 2 ? 0 : SRC>(x.x), hi = unpack2<SRC == 2 ? 0 : SRC>(x.y);
                     f[4 * half] = lo.x; f[4 * half + 1] = lo.y; f[4 * half + 2] = hi.x; f[4 * half + 3] = hi.y;
