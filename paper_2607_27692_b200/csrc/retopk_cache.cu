@@ -133,11 +133,14 @@ void set_rotation(RowsArgs& a, const retopk_rope* rope, int inverse) {
 // CTAs for n tokens of R rows each: a warp per token where that gives every SM warps enough, several
 // warps or CTAs per token below.
 template <int DEST> int launch_rows(RowsArgs& a, const retopk_rope* rope, int dtype, int d, int num_sms, cudaStream_t s) {
-    const int rpw = 32 / (d / 16), groups = (a.Hq + rpw - 1) / rpw + (a.Hk + rpw - 1) / rpw + (a.Hv + rpw - 1) / rpw;
+    const int rpw = 32 / (d / 16);
+    a.gq = (a.Hq + rpw - 1) / rpw;
+    a.gqk = a.gq + (a.Hk + rpw - 1) / rpw;
+    a.groups = a.gqk + (a.Hv + rpw - 1) / rpw;
     const long long want = 16ll * num_sms;               // warps
     a.tokens_per_cta = a.n_tokens >= want ? 4 : (2 * a.n_tokens >= want ? 2 : 1);
     // two groups of rows to a warp, if the tokens alone do not fill the device
-    const int per_tok = ROWS_WARPS / a.tokens_per_cta, most = (groups + 2 * per_tok - 1) / (2 * per_tok);
+    const int per_tok = ROWS_WARPS / a.tokens_per_cta, most = (a.groups + 2 * per_tok - 1) / (2 * per_tok);
     const long long need = (want + a.n_tokens * per_tok - 1) / (a.n_tokens * per_tok);
     a.units = (int)(need < most ? need : most);
     if (a.units < 1) a.units = 1;

@@ -110,6 +110,7 @@ struct RowsArgs {
     uint16_t *q_out, *k_out;
     long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
     int Hq, Hk, Hv;
+    int gq, gqk, groups;        // groups of rows of q; of q and k; of all three
     Pages pg;
 };
 
@@ -132,7 +133,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     __shared__ float4 s_tab[ROWS_WARPS][MAX_PAIRS];      // heads and rests of cosine and sine
     __shared__ double2 s_tab64[DEST == DEST_PAGES4 ? ROWS_WARPS : 1][MAX_PAIRS];
 
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES, row_in = lane / LANES;
+    const int lane = threadIdx.x & 31, sub = lane % LANES, row_in = lane / LANES;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0);      // (known to be the same for all lanes)
     const int per_tok = ROWS_WARPS / a.tokens_per_cta;   // warps per token; each keeps a table of its own
     const long long tok = (long long)blockIdx.x * a.tokens_per_cta + warp / per_tok;
     pdl_wait();
@@ -146,46 +148,33 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     }
 
     // ---- where this warp's rows are -------------------------------------------------------------
-    // Groups of RPW rows of q, then k, then v are dealt out in turn to the warps of a token.  A cursor is
-    // a tensor and a group in it; PER groups of one tensor are taken at a time, the next ones on their way.
+    // Groups of RPW rows of q, then k, then v are dealt out in turn to the warps of a token, which take
+    // PER of them at a time, the next ones on their way.
     constexpr int PER = DEST == DEST_PAGES4 ? 1 : 2;     // (quantising twice over is too much code: 40 against 31 us, 6K tokens)
     const int step = per_tok * a.units;
-    struct Cursor { int which, g; };
-    auto heads_of = [&](int which) { return which == 0 ? a.Hq : (which == 1 ? a.Hk : a.Hv); };
-    auto settle = [&](Cursor& c) {                       // to the first tensor that has group c.g
-        while (c.which < 3) {
-            const int groups = (heads_of(c.which) + RPW - 1) / RPW;
-            if (c.g < groups) break;
-            c.g -= groups;
-            ++c.which;
+    const uint16_t *const q_src = a.q + tok * a.q_stride, *const k_src = a.k + tok * a.k_stride, *const v_src = a.v + tok * a.v_stride;
+    struct Rows { int which, h; bool on; const uint16_t* src; };
+    auto rows_of = [&](int g) {                          // this lane's row of group g
+        Rows r;
+        r.which = g < a.gq ? 0 : (g < a.gqk ? 1 : 2);
+        r.h = (g - (r.which == 0 ? 0 : (r.which == 1 ? a.gq : a.gqk))) * RPW + row_in;
+        r.on = g < a.groups && r.h < (r.which == 0 ? a.Hq : (r.which == 1 ? a.Hk : a.Hv));
+        r.src = (r.which == 0 ? q_src : (r.which == 1 ? k_src : v_src)) + r.h * D;
+        return r;
+    };
+    auto fetch = [&](int g, uint4 (&fa)[PER], uint4 (&fb)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const Rows r = rows_of(g + i * step);
+            if (r.on) {
+                fa[i] = *reinterpret_cast<const uint4*>(r.src + ca);
+                fb[i] = *reinterpret_cast<const uint4*>(r.src + cb);
+            }
         }
     };
-    auto advance = [&](Cursor c) {
-        const int groups = (heads_of(c.which) + RPW - 1) / RPW;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (c.g < groups) c.g += step;
-        settle(c);
-        return c;
-    };
-    auto source = [&](int which) {
-        return which == 0 ? a.q + tok * a.q_stride : (which == 1 ? a.k + tok * a.k_stride : a.v + tok * a.v_stride);
-    };
-    auto fetch = [&](Cursor c, uint4 (&fa)[PER], uint4 (&fb)[PER]) {
-        if (c.which >= 3) return;
-        const int heads = heads_of(c.which), h = c.g * RPW + row_in;
-        const uint16_t* src = source(c.which) + h * D;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (h + i * step * RPW < heads) {
-                fa[i] = *reinterpret_cast<const uint4*>(src + i * step * (RPW * D) + ca);
-                fb[i] = *reinterpret_cast<const uint4*>(src + i * step * (RPW * D) + cb);
-            }
-    };
     uint4 ya[PER], yb[PER];
-    Cursor cur = {0, (int)blockIdx.y * per_tok + warp % per_tok};
-    settle(cur);
-    fetch(cur, ya, yb);                                  // on their way while position and page are looked up
+    const int g0 = (int)blockIdx.y * per_tok + warp % per_tok;
+    fetch(g0, ya, yb);                                   // on their way while position and page are looked up
 
     // ---- position and page row, by the whole warp -----------------------------------------------
     int pos = 0;
@@ -341,29 +330,27 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     };
 
 #pragma unroll 1
-    while (cur.which < 3) {
-        const Cursor next = advance(cur);
+    for (int g = g0; g < a.groups; g += PER * step) {
         uint4 na[PER], nb[PER];
-        fetch(next, na, nb);
-        const int heads = heads_of(cur.which), h0 = cur.g * RPW + row_in;
+        fetch(g + PER * step, na, nb);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int h = h0 + i * step * RPW;
-            const bool on = h < heads;
+            const Rows r = rows_of(g + i * step);
             // (values go in as they are; their chunks are where the lane's are)
-            if (cur.which != 2) rotate(DEST == DEST_PAGES4 && cur.which == 1, ya[i], yb[i], source(cur.which) + h * D, on);
-            if (DEST == DEST_ROWS || cur.which == 0) {
-                if (on) {
-                    uint16_t* dst = (cur.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + h * D;
+            if (r.which != 2) rotate(DEST == DEST_PAGES4 && r.which == 1, ya[i], yb[i], r.src, r.on);
+            if (DEST == DEST_ROWS || r.which == 0) {
+                if (r.on) {
+                    uint16_t* dst = (r.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + r.h * D;
                     *reinterpret_cast<uint4*>(dst + ca) = ya[i];
                     *reinterpret_cast<uint4*>(dst + cb) = yb[i];
                 }
             } else {
-                const long long row = row0 + (long long)h * a.pg.page_size;
-                unsigned char* pages = cur.which == 1 ? a.pg.k : a.pg.v;
+                const long long row = row0 + (long long)r.h * a.pg.page_size;
+                unsigned char* pages = r.which == 1 ? a.pg.k : a.pg.v;
+                const bool store = r.on && row0 >= 0;
                 if (DEST == DEST_PAGES4) {
-                    quantise(ya[i], yb[i], pages, cur.which == 1 ? a.pg.ks : a.pg.vs, row, on && row0 >= 0);
-                } else if (on && row0 >= 0) {
+                    quantise(ya[i], yb[i], pages, r.which == 1 ? a.pg.ks : a.pg.vs, row, store);
+                } else if (store) {
                     uint16_t* dst = reinterpret_cast<uint16_t*>(pages) + row * D;
                     *reinterpret_cast<uint4*>(dst + ca) = ya[i];
                     *reinterpret_cast<uint4*>(dst + cb) = yb[i];
@@ -372,7 +359,6 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
             ya[i] = na[i];
             yb[i] = nb[i];
         }
-        cur = next;
     }
 }
 
