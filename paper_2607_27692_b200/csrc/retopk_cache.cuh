@@ -90,6 +90,23 @@ __device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long
     return page * pg.H_kv * pg.page_size + off;
 }
 
+// Codes round((x - m) / s) within 0..15 of eight values, the first in the low bits.  The quotient is
+// rounded as the division is (P. Markstein's theorem: from the rounded reciprocal y and a quotient q
+// within one unit, q + (a - b q) y rounds correctly), one reciprocal for all; both sides are scaled so
+// that reciprocal and remainder stay in range.  Adding 1.5 * 2^23 rounds to a whole number, ties to
+// even, and leaves it in the low bits.
+__device__ __forceinline__ uint32_t eight_codes(const float* x, float m, float s) {
+    const float c = s < 8.6736174e-19f ? 18446744073709551616.f : (s > 1.1529215e18f ? 5.4210109e-20f : 1.f);   // 2^-60: 2^64, 2^60: 2^-64
+    const float b = s * c, y = s > 0.f ? __frcp_rn(b) : 0.f;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 7; e >= 0; --e) {
+        const float a = (x[e] - m) * c, q0 = a * y, q = fmaf(fmaf(-q0, b, a), y, q0);
+        w = w * 16u + (__float_as_uint(fminf(fmaxf(q, 0.f), 15.f) + 12582912.f) - 0x4b400000u);
+    }
+    return w;
+}
+
 // ---------------------------------------------------------------------------------------
 // rows_kernel: rotate and store
 // ---------------------------------------------------------------------------------------
@@ -310,16 +327,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
                 // the minimum may have been rounded up past the maximum of a narrow group
                 step_[g] = __bfloat162float(__float2bfloat16_rn(fmaxf(__fdiv_rn(mx - low[g], 15.f), 0.f)));
             }
-            const float la = ga == 0 ? low[0] : low[NG - 1], sa = ga == 0 ? step_[0] : step_[NG - 1];
-            const float lb = gb == 0 ? low[0] : low[NG - 1], sb = gb == 0 ? step_[0] : step_[NG - 1];
-            uint32_t wa = 0, wb = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float na = sa > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(xa[e] - la, sa)), 0.f), 15.f) : 0.f;
-                const float nb = sb > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(xb[e] - lb, sb)), 0.f), 15.f) : 0.f;
-                wa |= (uint32_t)(int)na << (4 * e);
-                wb |= (uint32_t)(int)nb << (4 * e);
-            }
+            const uint32_t wa = eight_codes(xa, ga == 0 ? low[0] : low[NG - 1], ga == 0 ? step_[0] : step_[NG - 1]);
+            const uint32_t wb = eight_codes(xb, gb == 0 ? low[0] : low[NG - 1], gb == 0 ? step_[0] : step_[NG - 1]);
             if (store) {
                 unsigned char* dst = codes + row * (D / 2);
                 *reinterpret_cast<uint32_t*>(dst + ca / 2) = wa;
@@ -335,6 +344,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
         fetch(g + PER * step, na, nb);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
+            if (i > 0 && g + i * step >= a.groups) break;
             const Rows r = rows_of(g + i * step);
             // (values go in as they are; their chunks are where the lane's are)
             if (r.which != 2) rotate(DEST == DEST_PAGES4 && r.which == 1, ya[i], yb[i], r.src, r.on);

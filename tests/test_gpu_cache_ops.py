@@ -212,6 +212,34 @@ def test_quantiser_corners(paged, dtype):
     assert step[0].item() == 0 and codes[0].max() == 0
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
+def test_quantiser_many_values(paged, dtype, d):
+    """Four million values of steps from 2^-100 to 2^100: every code as a 64-bit division rounds it, ties among them."""
+    n, H, page = 4096, 8 * 64 // d * 2, 64
+    g = gen(d)
+    x = torch.randn(n, H, d, generator=g, device="cuda")
+    if dtype == BF:
+        x = x * torch.exp2(torch.randint(-100, 100, (n, H, 1), generator=g, device="cuda").float())
+    else:
+        x = x * torch.exp2(torch.randint(-12, 12, (n, H, 1), generator=g, device="cuda").float())
+    x[: n // 2] = (x[: n // 2] * 4).round() / 4 * x[: n // 2, :, :1].abs().clamp_min(2.0 ** -90)     # coarse grids: ties
+    x[::3] += 5 * x[::3, :, :1]                                                                       # minima far from zero
+    x = x.to(dtype)
+    cache = paged.KVPages(n // page, H, page, d, "q4")
+    cache.append(x, x.flip(0).contiguous(), ints([n]), torch.arange(n // page, dtype=torch.int32, device="cuda")[None])
+    codes, step, low = ref.quantise(x)
+    # infinities, and spans beyond the fp32 range, are outside what is specified: their groups are left out
+    span = x.float().unflatten(-1, (-1, 64)).amax(-1) - low.float()
+    fine = torch.isfinite(x).unflatten(-1, (-1, 64)).all(-1) & torch.isfinite(span)
+    assert fine.float().mean().item() > 0.8
+    for name, c, s, m, ok in (("k", codes, step, low, fine), ("v", codes.flip(0), step.flip(0), low.flip(0), fine.flip(0))):
+        got = getattr(cache, name).transpose(1, 2).reshape(n, H, d // 64, 32)
+        scale = getattr(cache, name + "_scale").transpose(1, 2).reshape(n, H, d // 64, 2).double()
+        assert torch.equal(scale[..., 0][ok], s[ok]) and torch.equal(scale[..., 1][ok], m[ok])
+        assert torch.equal(got[ok], ref.pack(c).unflatten(-1, (-1, 32))[ok])
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "q4"])
 def test_append_what_points_outside_is_left_out(paged, fmt):
     """Idle sequences, bad pages and positions beyond the table: skipped, nothing else changes."""
