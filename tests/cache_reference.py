@@ -107,17 +107,30 @@ def attention(q, k, v, scale, window=0, ok=None):
 
 
 def attention_bounds(q, k_scale, v_scale, v, scale, n, dtype):
-    """(bound on |lse error|, absolute part of the bound on |out error|).
+    """(bound on |lse error|, absolute part of the bound on |out error|); q [.., d].
 
-    Scores: per group the tensor core adds (OFFSET + code) * q, OFFSET <= 128, code <= 15, in fp32:
-    partial sums stay below 143 * sum |q|, at most 8 additions each way off by 2^-23 (truncation) of
-    that; then a handful of fp32 operations on values up to |s| * 15 * sum |q| + |m| * sum |q|.
-    Weights: exp of a score off by e is off by a factor 1 + e; as two bf16 parts 2^-16; the sums of
-    codes times weights carry OFFSET as well, (n / 128 + 64) additions of 2^-23 each.
+    Scores.  Queries may become whole numbers of a unit that puts the largest element of a row between
+    2^13.99 and 2^15 of them: element c is off by e_c = |q_c - unit * round(q_c / unit)|, worked out here,
+    and a group's sum of codes (at most 15) times step by 15 * step * sum of e_c.  Whole-number sums are
+    exact.  Or they stay 16-bit numbers: at most 8 additions in fp32, each off by 2^-23 (truncation) of
+    partial sums below 15 * sum |q|.  Then a conversion and at most 7 fp32 operations, 2^-24 each, on
+    values up to (15 * step + |minimum|) * sum |q|: 16 * 2^-24 in all cover both.
+    The exponential: off by e in the score is off by the factor 1 + e; lse adds its own fp32 steps.
+
+    Output.  Weights off by 1 + e on both sides of the quotient: 2 e * max |v|; weights as two truncated
+    bf16 parts: 2^-16, likewise.  Sums: a warp adds at most n / 16 + 64 products, each addition off by
+    2^-23 of a partial sum below 16 * step (bytes up to 255, divided by 16 at the end) or |minimum|, for
+    weights that sum to 1; joining warps and CTAs is within the 64.
     """
-    sumq = q.double().abs().sum(-1).max().item()
+    q = q.double()
+    sumq = q.abs().sum(-1).max().item()
+    big = q.abs().amax(-1, keepdim=True).clamp_min(2.0 ** -126)
+    unit = torch.exp2(torch.floor(torch.log2(big)) - 14)
+    unit = torch.where(big / unit > 32512, 2 * unit, unit)
+    rounded = (q - unit * torch.round(q / unit)).abs().sum(-1).max().item()
     ks, km = k_scale[..., 0].double().abs().max().item(), k_scale[..., 1].double().abs().max().item()
-    vs = v_scale[..., 0].double().abs().max().item()
-    err = abs(scale) * sumq * 2.0 ** -23 * (8 * 143 * ks + 8 * (15 * ks + km))
+    vs, vm = v_scale[..., 0].double().abs().max().item(), v_scale[..., 1].double().abs().max().item()
+    err = abs(scale) * (15 * ks * rounded + 2.0 ** -20 * sumq * (15 * ks + km))
     vmax = v.abs().max().item() if v.numel() else 0.0
-    return err + 2.0 ** -20 * (1 + abs(math.log(max(n, 2)))), 2 * (err + 2.0 ** -16) * vmax + (n / 128 + 64) * 2.0 ** -23 * 143 * vs
+    out = 2 * (err + 2.0 ** -16) * vmax + (n / 16 + 64) * 2.0 ** -23 * (16 * vs + vm)
+    return err + 2.0 ** -20 * (1 + abs(math.log(max(n, 2)))), out
