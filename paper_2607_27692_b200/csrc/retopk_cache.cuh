@@ -1125,16 +1125,16 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                         for (int r = 0; r < 2; ++r) {
                             const float2 v = r ? v8 : v0;
                             const float w0 = sc[x][nt][r][0] * v.x;
-                            const float d0 = w0 - __uint_as_float(__float_as_uint(w0) & 0xffff0000u);
+                            const float h0 = __uint_as_float(__float_as_uint(w0) & 0xffff0000u), d0 = w0 - h0;
                             st.msum[g][nt][0] = fmaf(sc[x][nt][r][0], v.y, st.msum[g][nt][0]);
                             if (PACKED) {
-                                bw[nt][0][r] = movmatrix(__byte_perm(__float_as_uint(w0), __float_as_uint(d0), 0x7632));
+                                bw[nt][0][r] = movmatrix(pack2<TYPE_BF16>(h0, d0));
                             } else {
                                 const float w1 = sc[x][nt][r][NC - 1] * v.x;
                                 const float d1 = w1 - __uint_as_float(__float_as_uint(w1) & 0xffff0000u);
                                 st.msum[g][nt][NC - 1] = fmaf(sc[x][nt][r][NC - 1], v.y, st.msum[g][nt][NC - 1]);
                                 bw[nt][0][r] = movmatrix(__byte_perm(__float_as_uint(w0), __float_as_uint(w1), 0x7632));
-                                bw[nt][PARTS - 1][r] = movmatrix(__byte_perm(__float_as_uint(d0), __float_as_uint(d1), 0x7632));
+                                bw[nt][PARTS - 1][r] = movmatrix(pack2<TYPE_BF16>(d0, d1));
                             }
                         }
                     // codes of keys 2 t4, 2 t4 + 1, + 8, + 9 for channels 64 g + 8 r8 .. + 7
