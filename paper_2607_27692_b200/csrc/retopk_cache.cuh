@@ -513,11 +513,16 @@ enum { COLS_4 = 0, COLS_8 = 1, COLS_16 = 2 };
 __host__ __device__ constexpr int q4_cols(int shape) { return shape == COLS_4 ? 4 : (shape == COLS_8 ? 8 : 16); }
 // bytes of one tile: key codes, value codes, key scales, value scales of 16 rows
 __host__ __device__ constexpr int q4_tile_bytes(int d) { return Q4_TILE * (d + d / GROUP * 8); }
-__host__ __device__ constexpr int q4_smem_bytes(int d, int shape) {
+__host__ __device__ constexpr int q4_ring_bytes(int d, int shape) {      // the ring, later the join of the warps
     const int ring = Q4_WARPS * Q4_STAGES * Q4_STEP * q4_tile_bytes(d);
     const int merge = Q4_WARPS * q4_cols(shape) * (d + 4) * 4;
     return ring > merge ? ring : merge;
 }
+// The tensor core cuts what it adds to an accumulator off at that accumulator's last place: after 150
+// tiles the sums were 5e-6 too small, and where many keys average out to little that is the first thing
+// wrong with the result.  Every Q4_FLUSH steps the sums move on to shared memory, by rounded additions.
+constexpr int Q4_FLUSH = 8;
+__host__ __device__ constexpr int q4_smem_bytes(int d, int shape) { return q4_ring_bytes(d, shape) + Q4_WARPS * q4_cols(shape) * d * 4; }
 
 // Few warps with many registers: three tiles at a time keep the ALU and the tensor cores busier than
 // more warps with one or two tiles would (4 x 128K keys: 107 us; 16 warps an SM with two tiles 112, 20
@@ -738,6 +743,8 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * RING;
     float* s_merge = reinterpret_cast<float*>(smem);
+    // this lane's sums over the earlier steps: pairs of channels, [group][pair][tile][column][lane]
+    float2* const s_sum = reinterpret_cast<float2*>(smem + q4_ring_bytes(D, SHAPE)) + warp * (COLS * D / 2) + lane;
 
     // Where this lane's codes lie in a block of 16 rows whose 128-byte lines have their 16-byte slots
     // exchanged by line (slot ^ 2 (line mod 4)), so that every read below touches each bank once.
@@ -942,9 +949,33 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             for (int c = 0; c < NC; ++c) { st.l[nt][c] = 0.f; st.ref[nt][c] = Q4_NONE; }
         }
 
-        int stage = 0;
+        int stage = 0, since = 0;
+        bool flushed = false;
+        auto flush = [&]() {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {    // accumulator rows r8 and r8 + 8: n0 and n0 + 16 n1 of
+                            float (&o)[4] = st.o[g][m][nt];          // channels 2 m, 2 m + 1
+                            float x = o[c], y = o[2 + c];
+                            if (PACKED) { x += o[1]; y += o[3]; }
+                            float2* at = s_sum + (((g * 4 + m) * NT + nt) * NC + c) * 32;
+                            float2 v = make_float2(x * TWO69, (y - x) * (TWO69 / 16.f));
+                            if (flushed) { const float2 w = *at; v.x += w.x; v.y += w.y; }
+                            *at = v;
+                            if (PACKED) { o[0] = o[1] = o[2] = o[3] = 0.f; } else { o[c] = o[2 + c] = 0.f; }
+                        }
+            flushed = true;
+            since = 0;
+        };
 #pragma unroll 1
         for (int step = 0; step < n_steps; ++step) {
+            if (since == Q4_FLUSH) flush();
+            ++since;
             cp_async_wait<Q4_STAGES - 2>();
             __syncwarp();
             const int ring_at = stage * (U * TILE);
@@ -1083,6 +1114,16 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                         for (int m = 0; m < 4; ++m)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) st.o[g][m][nt][e] *= f[PACKED ? 0 : (e & 1)];
+                        if (flushed) {
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                                for (int c = 0; c < NC; ++c) {
+                                    float2* at = s_sum + (((g * 4 + m) * NT + nt) * NC + c) * 32;
+                                    const float2 w = *at;
+                                    *at = make_float2(w.x * f[c], w.y * f[c]);
+                                }
+                        }
                     }
                 }
             }
@@ -1157,6 +1198,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             }
         }
         cp_async_wait<0>();
+        flush();
 
         // ---- join the warps ---------------------------------------------------------------------
         // sums over the lanes that share columns (rows of the tiles); the 2^64 of the weights goes here
@@ -1190,11 +1232,9 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int m = 0; m < 4; ++m)
-                    {                                    // accumulator rows r8 and r8 + 8: n0 and n0 + 16 n1 of
-                        float x = st.o[g][m][nt][c], y = st.o[g][m][nt][2 + c];              // channels 2 m, 2 m + 1
-                        if (PACKED) { x += st.o[g][m][nt][1]; y += st.o[g][m][nt][3]; }
-                        *reinterpret_cast<float2*>(dst + g * GROUP + 2 * m) =
-                            make_float2(fmaf(x, TWO69, st.msum[g][nt][c]), fmaf(y - x, TWO69 / 16.f, st.msum[g][nt][c]));
+                    {
+                        const float2 v = s_sum[(((g * 4 + m) * NT + nt) * NC + c) * 32];
+                        *reinterpret_cast<float2*>(dst + g * GROUP + 2 * m) = make_float2(v.x + st.msum[g][nt][c], v.y + st.msum[g][nt][c]);
                     }
                 if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
             }

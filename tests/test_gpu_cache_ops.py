@@ -412,6 +412,22 @@ def test_attention_weights_of_far_keys(paged):
     check_attention(cache, q, lens, table, out, lse, d ** -0.5)
 
 
+@pytest.mark.parametrize("dtype,G", [(FP, 4), (BF, 4), (FP, 7)])
+def test_attention_long_flat(paged, dtype, G):
+    """A quarter of a million keys of much the same weight: the result is the little that is left of large sums."""
+    lens, page, d = [262144], 128, 128
+    cache, table = filled(paged, lens, page, 1, d, 85)
+    q = (0.05 * torch.randn(1, 1, G, d, generator=gen(86), device="cuda")).to(dtype)
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    out = cache.attend(q, ints(lens), table, lse=lse)
+    check_attention(cache, q, lens, table, out, lse, d ** -0.5)
+    want, _ = ref.attention(q[0], *(ref.rows_of(t, s, table, 0, lens[0], page) for t, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale))), d ** -0.5)
+    # systematic part: 24 additions cut off by 2^-23 at most, of sums that grow to 16 steps (half on
+    # average); steps are 0.21 on average here
+    rms = (out[0].double() - want).square().mean().sqrt().item()
+    assert rms <= ref.half_step(dtype) * want.square().mean().sqrt().item() + 24 * 2.0 ** -23 * 8 * 0.21
+
+
 def test_attention_pages_out_of_range(paged):
     lens, page, d = [200, 64, 33], 16, 128
     cache, table = filled(paged, lens, page, 2, d, 91)
