@@ -356,7 +356,8 @@ enum { RETOPK_BF16 = 0, RETOPK_FP16 = 1, RETOPK_FP32 = 2 };
  *                       between; a = 0.1 ln(factor) + 1
  * attn_factor > 0 replaces a.  Zero in low_freq_factor, high_freq_factor, beta_fast or beta_slow
  * stands for 1, 4, 32 and 1.  Angle and rotation are computed in 64 bits (at position 1 Mi an
- * angle in 32 bits is 0.06 rad off) and rounded once to the tensor's type.
+ * angle in 32 bits is 0.06 rad off) or, the rotation, to within 2^-23 of that; rounded once to the tensor's
+ * type.
  */
 typedef struct retopk_rope retopk_rope;
 enum { RETOPK_ROPE_HALF = 0, RETOPK_ROPE_INTERLEAVED = 1 };
@@ -378,7 +379,7 @@ int retopk_rope_frequencies(const retopk_rope* rope, double* inv_freq_host, doub
  * Rotate q [n_tokens,H_q,d] and k [n_tokens,H_k,d] at positions [n_tokens] (int32, any sign) in one
  * launch.  Either tensor may be NULL.  An output may be its own input (same pointer and stride);
  * other overlaps are EINVAL.  inverse = 1 applies the transpose: the gradient with respect to the
- * input, given the gradient of the output, and for a = 1 the rotation back.
+ * input, given the gradient of the output, and for a = 1 the rotation back.  Limit: 65535 heads.
  */
 int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, const int32_t* positions, const void* q,
                       int64_t q_stride, void* q_out, int64_t q_out_stride, int H_q, const void* k, int64_t k_stride,
@@ -413,12 +414,13 @@ typedef struct {
  * RETOPK_PAGES_Q4 rounds the rotated key to `dtype` and then quantises each group of 64 channels:
  * m = bf16(min), s = bf16((max - m) / 15), n = round((x - m) / s) to nearest, ties to even, within
  * 0..15, n = 0 where s = 0; 32-bit arithmetic, IEEE rounding.  A span max - m above the fp32 range is
- * unspecified.  16-bit pages hold `dtype`.
+ * unspecified.  16-bit pages hold `dtype`; q and keys that stay 16-bit are rounded once from a rotation
+ * within 2^-23 of the exact one, keys that are quantised from one in 64 bits.
  * Rows of k_new from cu_new[B] on, and tokens whose position is negative (an idle sequence of length
  * 0), are left out, their q_out rows too.  A key whose page is not in 0..n_pages-1 or whose position is
  * beyond the block table is not stored.  All other rows of the cache stay as they are.  Two new
  * tokens that share a row of a page leave that row unspecified.
- * Limits: B <= 65535; EUNSUPPORTED beyond.
+ * Limits: B, H_kv, H_q <= 65535; EUNSUPPORTED beyond.
  */
 int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* cu_new, int64_t n_new,
                      int dtype, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
@@ -443,12 +445,15 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * its last T positions: token t sees keys j < seq_lens[b] - T + 1 + t, with window > 0 only the last
  * `window` of those.  q row b * T + t with q_stride, out [B,T,H_q,d] contiguous, lse [B,T,H_q] fp32 or
  * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf.  Keys of pages
- * out of range do not count.  Scores, weights, sums and outputs are held in fp32 (weights enter the
- * product with the codes as a sum of two bf16 parts), rounded once to dtype.  What rows behind
- * seq_lens hold, NaN patterns among it, has no influence.  Results are bit-reproducible.
+ * out of range do not count.  Scores, weights, sums and outputs are held in fp32 and rounded once to
+ * dtype; weights enter the product with the codes as a sum of two bf16 parts (2^-17).  Queries enter, up
+ * to 4 columns T * H_q / H_kv, as whole numbers of a unit of at most 2^-13.99 of the row's largest element
+ * (exact above 2^-7 of it in bf16, 2^-4 in fp16), beyond that exactly; elements of q below 2^117.  What
+ * rows behind seq_lens hold, NaN patterns among it, has no influence.  Results are bit-reproducible.
  * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant
  * before and after; calls that may overlap on the GPU (two streams, two captured graphs) need one each.
- * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096; EUNSUPPORTED beyond.
+ * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096, at most 2^20 keys of a sequence (max_pages *
+ * page_size) and 2^32 - 2 rows n_pages * H_kv * page_size; EUNSUPPORTED beyond.
  */
 int64_t retopk_q4_attention_workspace(int B, int T, int H_q, int H_kv, int d);   /* bytes, or a negative code */
 int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int dtype,

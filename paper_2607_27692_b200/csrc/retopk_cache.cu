@@ -22,6 +22,7 @@ namespace {
 constexpr double PI = 3.14159265358979323846;
 constexpr long long MAX_KEYS = 1048576;  // keys of one sequence in the attention, as in retopk_create
 constexpr int MAX_SEQ_GROUPS = 4096;     // B * H_kv, as in retopk_create
+constexpr int MAX_HEADS = 65535;         // of a tensor that is rotated or appended
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool bad_half_type(int dtype) { return dtype != RETOPK_BF16 && dtype != RETOPK_FP16; }
@@ -273,6 +274,7 @@ int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, cons
     const int d = rope->d;
     if (q && (!rows_ok(q, q_stride, H_q, d) || !rows_ok(q_out, q_out_stride, H_q, d))) return RETOPK_EINVAL;
     if (k && (!rows_ok(k, k_stride, H_k, d) || !rows_ok(k_out, k_out_stride, H_k, d))) return RETOPK_EINVAL;
+    if ((q && H_q > MAX_HEADS) || (k && H_k > MAX_HEADS)) return RETOPK_EUNSUPPORTED;
     if (n_tokens == 0) return RETOPK_OK;
     if (!positions) return RETOPK_EINVAL;
     if (q && !rows_apart(q, q_stride, q_out, q_out_stride, n_tokens, H_q, d)) return RETOPK_EINVAL;
@@ -307,7 +309,7 @@ int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     if (!rows_ok(k_new, k_stride, H, d) || !rows_ok(v_new, v_stride, H, d)) return RETOPK_EINVAL;
     if (rope && rope->d != d) return RETOPK_EINVAL;
     if (q && (!rope || !rows_ok(q, q_stride, H_q, d) || !rows_ok(q_out, q_out_stride, H_q, d))) return RETOPK_EINVAL;
-    if (B > 65535 || n_new > 2147483647ll) return RETOPK_EUNSUPPORTED;
+    if (B > 65535 || n_new > 2147483647ll || H > MAX_HEADS || (q && H_q > MAX_HEADS)) return RETOPK_EUNSUPPORTED;
     if (n_new == 0) return RETOPK_OK;
     if (q && !rows_apart(q, q_stride, q_out, q_out_stride, n_new, H_q, d)) return RETOPK_EINVAL;
     int num_sms = 0;
@@ -351,8 +353,9 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     a.max_rows = max_rows;
     a.k_out = k_out;
     a.v_out = v_out;
-    // no sequence has more rows than the cache holds
-    const long long rows = max_rows < a.pg.capacity ? max_rows : a.pg.capacity;
+    // no sequence has more rows than the cache holds (unless it begins before the first)
+    const long long rows = first || max_rows < a.pg.capacity ? max_rows : a.pg.capacity;
+    if (rows > 2147483647ll * GATHER_ROWS) return RETOPK_EUNSUPPORTED;
     const dim3 grid((unsigned)((rows + GATHER_ROWS - 1) / GATHER_ROWS), (unsigned)pages->H_kv, (unsigned)B);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (q4) {

@@ -883,7 +883,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
             // 2^(14 - exponent of the largest), kept within what a float can hold both ways
             int e2 = 141 - (int)(__float_as_uint(big) >> 23);
             if (PACKED && (__float_as_uint(big) & 0x7fffffu) > 0x7e0000u) --e2;      // at most 32512
-            e2 = e2 > 100 ? 100 : (e2 < -100 ? -100 : e2);
+            e2 = e2 > 100 ? 100 : (e2 < -103 ? -103 : e2);
             const float to_unit = __uint_as_float((uint32_t)(127 + e2) << 23);
             const float of_unit = __uint_as_float((uint32_t)(127 + (PACKED ? -4 : 24) - e2) << 23);  // products: 16 n q, or n q 2^-24
             if (PACKED) {

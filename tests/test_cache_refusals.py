@@ -138,6 +138,7 @@ def test_append_refusals(lib):
                dict(rope=h, q=A, qs=512, qo=A, qos=512, Hq=0), dict(pg=pages(format=1)), dict(pg=pages(format=0), dtype=1)):
         assert call(**kw) == EINVAL, kw
     assert call(B=70000, n=70000) == EUNSUPPORTED
+    assert call(rope=h, q=A, qs=70000 * 128, qo=A, qos=70000 * 128, Hq=70000) == EUNSUPPORTED
     assert call(n=0) == OK
     lib.retopk_rope_destroy(h)
     lib.retopk_rope_destroy(h64)

@@ -293,6 +293,10 @@ def test_gather(paged, fmt, src, out, d):
             else:
                 close_to_rounding(got[b, :, :m], want, out)
             assert (got[b, :, m:] == 7.0).all(), "rows beyond the sequence were written"
+    # rows before the first: left alone, the rest of the sequence behind them, beyond the table's width too
+    wide = torch.full((len(lens), H, 400, d), 7.0, dtype=out, device="cuda")
+    cache.gather(wide, None, ints(lens), table, first=ints([-60] * len(lens)))
+    assert (wide[:, :, :60] == 7.0).all() and torch.equal(wide[5, :, 160:360], ko[5]) and (wide[5, :, 393:] == 7.0).all()
     # one output alone, and pages that do not exist
     ko2 = torch.full_like(ko, 7.0)
     cache.gather(ko2, None, ints(lens), table, first=ints(first))
@@ -426,6 +430,20 @@ def test_attention_long_flat(paged, dtype, G):
     # average); steps are 0.21 on average here
     rms = (out[0].double() - want).square().mean().sqrt().item()
     assert rms <= ref.half_step(dtype) * want.square().mean().sqrt().item() + 24 * 2.0 ** -23 * 8 * 0.21
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+@pytest.mark.parametrize("G", [1, 7])
+def test_attention_scales(paged, scale, G):
+    lens = [5, 260]
+    cache, table = filled(paged, lens, 16, 2, 64, 89)
+    q = torch.randn(2, 1, 2 * G, 64, generator=gen(90), device="cuda").to(BF)
+    q[0, 0, 0] = 0.0
+    q[1, 0, 0] *= 2.0 ** -40
+    q[1, 0, G] *= 2.0 ** 20 if scale == 0.0 else 1.0
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    out = cache.attend(q, ints(lens), table, scale=scale, lse=lse)
+    check_attention(cache, q, lens, table, out, lse, scale)
 
 
 def test_attention_pages_out_of_range(paged):
