@@ -663,3 +663,19 @@ def test_binding_refusals(paged):
         paged.KVPages.wrap(cache.k, cache.v)
     with pytest.raises(TypeError):
         cache.gather(torch.zeros(2, 2, 4, 64, device="cuda", dtype=torch.float64), None, lens, table)
+    with pytest.raises(ValueError):
+        cache.gather(None, None, lens, table)
+    with pytest.raises(TypeError):
+        cache.attend(q, [1, 1], table)
+    rope = paged.Rope(64)
+    wide = torch.zeros(3, 4, 64, dtype=BF, device="cuda")
+    with pytest.raises(ValueError):
+        cache.append(k, k, lens, table, rope=paged.Rope(128))
+    with pytest.raises(ValueError):
+        rope.apply(q, ints([0]))
+    with pytest.raises(paged._rt.RetopkError):
+        rope.apply(wide[:2], lens, out=wide[1:])            # overlaps without being the same
+    rope.close()
+    for call in (lambda: rope.apply(q, lens), lambda: cache.append(k, k, lens, table, rope=rope), rope.frequencies):
+        with pytest.raises(paged._rt.RetopkError):
+            call()
