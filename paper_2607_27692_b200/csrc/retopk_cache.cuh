@@ -90,21 +90,34 @@ __device__ __forceinline__ long long cache_row(const Pages& pg, int b, long long
     return page * pg.H_kv * pg.page_size + off;
 }
 
-// Codes round((x - m) / s) within 0..15 of eight values, the first in the low bits.  The quotient is
-// rounded as the division is (P. Markstein's theorem: from the rounded reciprocal y and a quotient q
-// within one unit, q + (a - b q) y rounds correctly), one reciprocal for all; both sides are scaled so
-// that reciprocal and remainder stay in range.  Adding 1.5 * 2^23 rounds to a whole number, ties to
-// even, and leaves it in the low bits.
-__device__ __forceinline__ uint32_t eight_codes(const float* x, float m, float s) {
-    const float c = s < 8.6736174e-19f ? 18446744073709551616.f : (s > 1.1529215e18f ? 5.4210109e-20f : 1.f);   // 2^-60: 2^64, 2^60: 2^-64
-    const float b = s * c, y = s > 0.f ? __frcp_rn(b) : 0.f;
+// Codes round((x - m) / s) within 0..15 of eight values, the first in the low bits; c: a power of two
+// that brings s well into the normal range, y: 1 / (s c) rounded, 0 if s is.  The quotient is rounded as
+// the division is (P. Markstein's theorem: from the rounded reciprocal y and a quotient q within one unit,
+// q + (a - b q) y rounds correctly).  Adding 1.5 * 2^23 rounds to a whole number, ties to even, and leaves
+// it in the low bits.  A step that is not subnormal is at least (1 - 2^-8) of a fifteenth of the span, so
+// no quotient reaches 15.5; below 0 it can be, if the minimum was rounded up.
+template <bool SCALED>
+__device__ __forceinline__ uint32_t eight_codes(const float* x, float m, float s, float y, float c) {
+    const float b = SCALED ? s * c : s;
     uint32_t w = 0;
 #pragma unroll
     for (int e = 7; e >= 0; --e) {
-        const float a = (x[e] - m) * c, q0 = a * y, q = fmaf(fmaf(-q0, b, a), y, q0);
-        w = w * 16u + (__float_as_uint(fminf(fmaxf(q, 0.f), 15.f) + 12582912.f) - 0x4b400000u);
+        const float a = SCALED ? (x[e] - m) * c : x[e] - m, q0 = a * y;
+        float q = fmaxf(fmaf(fmaf(-q0, b, a), y, q0), 0.f);
+        if (SCALED) q = fminf(q, 15.f);
+        w = w * 16u + (__float_as_uint(q + 12582912.f) - 0x4b400000u);
     }
     return w;
+}
+// The rare steps below 2^-60 or above 2^60, out of line.
+__device__ __noinline__ uint32_t eight_codes_scaled(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float m, float s) {
+    const float c = s < 1.f ? 18446744073709551616.f : 5.4210109e-20f;       // 2^64, 2^-64
+    const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
+    return eight_codes<true>(x, m, s, s > 0.f ? __frcp_rn(s * c) : 0.f, c);
+}
+__device__ __forceinline__ uint32_t codes_of(const float* x, float m, float s) {
+    if (s > 8.6736174e-19f && s < 1.1529215e18f) return eight_codes<false>(x, m, s, __frcp_rn(s), 1.f);
+    return eight_codes_scaled(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7], m, s);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -179,19 +192,20 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
         r.src = (r.which == 0 ? q_src : (r.which == 1 ? k_src : v_src)) + r.h * D;
         return r;
     };
-    auto fetch = [&](int g, uint4 (&fa)[PER], uint4 (&fb)[PER]) {
+    auto fetch = [&](int g, Rows (&r)[PER], uint4 (&fa)[PER], uint4 (&fb)[PER]) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const Rows r = rows_of(g + i * step);
-            if (r.on) {
-                fa[i] = *reinterpret_cast<const uint4*>(r.src + ca);
-                fb[i] = *reinterpret_cast<const uint4*>(r.src + cb);
+            r[i] = rows_of(g + i * step);
+            if (r[i].on) {
+                fa[i] = *reinterpret_cast<const uint4*>(r[i].src + ca);
+                fb[i] = *reinterpret_cast<const uint4*>(r[i].src + cb);
             }
         }
     };
+    Rows here[PER];
     uint4 ya[PER], yb[PER];
     const int g0 = (int)blockIdx.y * per_tok + warp % per_tok;
-    fetch(g0, ya, yb);                                   // on their way while position and page are looked up
+    fetch(g0, here, ya, yb);                                   // on their way while position and page are looked up
 
     // ---- position and page row, by the whole warp -----------------------------------------------
     int pos = 0;
@@ -215,8 +229,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
             const int first = a.cu[b], end = a.cu[b + 1], len = a.seq_lens[b];
             if (tok >= first && tok < end) p = (long long)len - end + tok;
         } else {
-            b = (int)(tok / a.T);
-            p = (long long)a.seq_lens[b] - a.T + (tok - (long long)b * a.T);
+            b = (int)tok / a.T;
+            p = (long long)a.seq_lens[b] - a.T + ((int)tok - b * a.T);
         }
         if (p < 0) return;                               // belongs to no sequence, or has no place
         pos = (int)p;
@@ -327,8 +341,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
                 // the minimum may have been rounded up past the maximum of a narrow group
                 step_[g] = __bfloat162float(__float2bfloat16_rn(fmaxf(__fdiv_rn(mx - low[g], 15.f), 0.f)));
             }
-            const uint32_t wa = eight_codes(xa, ga == 0 ? low[0] : low[NG - 1], ga == 0 ? step_[0] : step_[NG - 1]);
-            const uint32_t wb = eight_codes(xb, gb == 0 ? low[0] : low[NG - 1], gb == 0 ? step_[0] : step_[NG - 1]);
+            const uint32_t wa = codes_of(xa, ga == 0 ? low[0] : low[NG - 1], ga == 0 ? step_[0] : step_[NG - 1]);
+            const uint32_t wb = codes_of(xb, gb == 0 ? low[0] : low[NG - 1], gb == 0 ? step_[0] : step_[NG - 1]);
             if (store) {
                 unsigned char* dst = codes + row * (D / 2);
                 *reinterpret_cast<uint32_t*>(dst + ca / 2) = wa;
@@ -340,12 +354,13 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
 
 #pragma unroll 1
     for (int g = g0; g < a.groups; g += PER * step) {
+        Rows next[PER];
         uint4 na[PER], nb[PER];
-        fetch(g + PER * step, na, nb);
+        fetch(g + PER * step, next, na, nb);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (i > 0 && g + i * step >= a.groups) break;
-            const Rows r = rows_of(g + i * step);
+            const Rows r = here[i];
             // (values go in as they are; their chunks are where the lane's are)
             if (r.which != 2) rotate(DEST == DEST_PAGES4 && r.which == 1, ya[i], yb[i], r.src, r.on);
             if (DEST == DEST_ROWS || r.which == 0) {
@@ -366,6 +381,10 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
                     *reinterpret_cast<uint4*>(dst + cb) = yb[i];
                 }
             }
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            here[i] = next[i];
             ya[i] = na[i];
             yb[i] = nb[i];
         }
