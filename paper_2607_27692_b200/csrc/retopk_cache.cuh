@@ -1258,20 +1258,29 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_atten
                 if (r8 == 0) { s_ref[warp * COLS + col] = st.ref[nt][c]; s_l[warp * COLS + col] = st.l[nt][c]; }
             }
         __syncthreads();
-        const bool whole = n_units == sp.units;
-        float* part = a.part + (long long)(2 * blockIdx.x + (item_start > u_begin ? 1 : 0)) * COLS * (D + 2);
-        for (int x = tid; x < cols_here * D; x += Q4_THREADS) {
-            const int col = x / D, ch = x - col * D;
-            float mx = Q4_NONE;
+        // per column: common reference, the warps' factors to it (in place of their references), sum
+        if (tid < COLS) {
+            float mx = Q4_NONE, l = 0.f;
 #pragma unroll
-            for (int w = 0; w < Q4_WARPS; ++w) mx = fmaxf(mx, s_ref[w * COLS + col]);
-            float l = 0.f, o = 0.f;
+            for (int w = 0; w < Q4_WARPS; ++w) mx = fmaxf(mx, s_ref[w * COLS + tid]);
 #pragma unroll
             for (int w = 0; w < Q4_WARPS; ++w) {
-                const float f = ex2(s_ref[w * COLS + col] - mx);
-                l += f * s_l[w * COLS + col];
-                o += f * s_merge[(w * COLS + col) * LD + ch];
+                const float f = ex2(s_ref[w * COLS + tid] - mx);
+                l = fmaf(f, s_l[w * COLS + tid], l);
+                s_ref[w * COLS + tid] = f;
             }
+            s_l[tid] = l;
+            s_l[COLS + tid] = mx;
+        }
+        __syncthreads();
+        const bool whole = n_units == sp.units;
+        float* part = a.part + (long long)(2 * blockIdx.x + (item_start > u_begin ? 1 : 0)) * COLS * (D + 2);
+        const int ch = tid % D;                          // a thread keeps its channel
+        for (int col = tid / D; col < cols_here; col += Q4_THREADS / D) {
+            float o = 0.f;
+#pragma unroll
+            for (int w = 0; w < Q4_WARPS; ++w) o = fmaf(s_ref[w * COLS + col], s_merge[(w * COLS + col) * LD + ch], o);
+            const float l = s_l[col], mx = s_l[COLS + col];
             if (whole) {
                 const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
                 const long long row = ((long long)b * a.T + tok) * a.Hq + head;
