@@ -378,7 +378,7 @@ int retopk_rope_frequencies(const retopk_rope* rope, double* inv_freq_host, doub
 /*
  * Rotate q [n_tokens,H_q,d] and k [n_tokens,H_k,d] at positions [n_tokens] (int32, any sign) in one
  * launch.  Either tensor may be NULL.  An output may be its own input (same pointer and stride);
- * other overlaps are EINVAL.  inverse = 1 applies the transpose: the gradient with respect to the
+ * other overlaps among inputs and outputs are EINVAL.  inverse = 1 applies the transpose: the gradient with respect to the
  * input, given the gradient of the output, and for a = 1 the rotation back.  Limit: 65535 heads.
  */
 int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, const int32_t* positions, const void* q,

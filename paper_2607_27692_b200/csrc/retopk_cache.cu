@@ -31,13 +31,20 @@ inline bool bad_half_type(int dtype) { return dtype != RETOPK_BF16 && dtype != R
 bool rows_ok(const void* p, long long stride, int heads, int d) {
     return p && aligned16(p) && heads >= 1 && stride % 8 == 0 && stride >= (long long)heads * d;
 }
-// An output may be its input exactly, or must not touch it.
-bool rows_apart(const void* in, long long si, const void* out, long long so, long long n, int heads, int d) {
-    if (in == out && si == so) return true;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(in), b0 = reinterpret_cast<uintptr_t>(out);
-    const uintptr_t a1 = a0 + (uintptr_t)((n - 1) * si + (long long)heads * d) * 2;
-    const uintptr_t b1 = b0 + (uintptr_t)((n - 1) * so + (long long)heads * d) * 2;
-    return a1 <= b0 || b1 <= a0;
+// Whether two such tensors of n tokens share no element: apart altogether, or with one stride and side by
+// side within it (slices of one projection's output).
+struct Strided { const void* p; long long stride; int heads; };
+bool rows_apart(const Strided& x, const Strided& y, long long n, int d) {
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x.p), y0 = reinterpret_cast<uintptr_t>(y.p);
+    const uintptr_t wx = (uintptr_t)x.heads * d * 2, wy = (uintptr_t)y.heads * d * 2;
+    if (x0 + (uintptr_t)(n - 1) * x.stride * 2 + wx <= y0 || y0 + (uintptr_t)(n - 1) * y.stride * 2 + wy <= x0) return true;
+    if (x.stride != y.stride) return false;
+    const uintptr_t step = (uintptr_t)x.stride * 2, off = y0 >= x0 ? (y0 - x0) % step : (step - (x0 - y0) % step) % step;
+    return off >= wx && off + wy <= step;
+}
+// An output may be its own input exactly, or must not touch it.
+bool in_place_or_apart(const Strided& in, const Strided& out, long long n, int d) {
+    return (in.p == out.p && in.stride == out.stride) || rows_apart(in, out, n, d);
 }
 
 int check_pages(const retopk_pages_t* p, int B) {
@@ -277,8 +284,10 @@ int retopk_rope_apply(const retopk_rope* rope, int dtype, int64_t n_tokens, cons
     if ((q && H_q > MAX_HEADS) || (k && H_k > MAX_HEADS)) return RETOPK_EUNSUPPORTED;
     if (n_tokens == 0) return RETOPK_OK;
     if (!positions) return RETOPK_EINVAL;
-    if (q && !rows_apart(q, q_stride, q_out, q_out_stride, n_tokens, H_q, d)) return RETOPK_EINVAL;
-    if (k && !rows_apart(k, k_stride, k_out, k_out_stride, n_tokens, H_k, d)) return RETOPK_EINVAL;
+    const Strided qi = {q, q_stride, H_q}, qo = {q_out, q_out_stride, H_q}, ki = {k, k_stride, H_k}, ko = {k_out, k_out_stride, H_k};
+    if (q && !in_place_or_apart(qi, qo, n_tokens, d)) return RETOPK_EINVAL;
+    if (k && !in_place_or_apart(ki, ko, n_tokens, d)) return RETOPK_EINVAL;
+    if (q && k && !(rows_apart(qo, ki, n_tokens, d) && rows_apart(ko, qi, n_tokens, d) && rows_apart(qo, ko, n_tokens, d))) return RETOPK_EINVAL;
     int num_sms = 0;
     const int rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
@@ -311,7 +320,8 @@ int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     if (q && (!rope || !rows_ok(q, q_stride, H_q, d) || !rows_ok(q_out, q_out_stride, H_q, d))) return RETOPK_EINVAL;
     if (B > 65535 || n_new > 2147483647ll || H > MAX_HEADS || (q && H_q > MAX_HEADS)) return RETOPK_EUNSUPPORTED;
     if (n_new == 0) return RETOPK_OK;
-    if (q && !rows_apart(q, q_stride, q_out, q_out_stride, n_new, H_q, d)) return RETOPK_EINVAL;
+    const Strided qi = {q, q_stride, H_q}, qo = {q_out, q_out_stride, H_q}, ki = {k_new, k_stride, H}, vi = {v_new, v_stride, H};
+    if (q && !(in_place_or_apart(qi, qo, n_new, d) && rows_apart(qo, ki, n_new, d) && rows_apart(qo, vi, n_new, d))) return RETOPK_EINVAL;
     int num_sms = 0;
     rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;

@@ -145,8 +145,8 @@ struct RowsArgs {
 };
 
 // One row is held by D / 16 lanes, two chunks of 8 channels each, so that a warp has 4 rows (d = 128) or
-// 8; a warp stays with one token and keeps that token's cosines and sines in registers while it goes
-// through the heads, two groups of rows at a time.  Where a half-layout rotation covers a multiple of 16
+// 8; a warp stays with one token, whose cosines and sines it keeps in shared memory, and goes through the
+// heads, the next groups of rows on their way.  Where a half-layout rotation covers a multiple of 16
 // channels, a lane's chunks are partners of each other (c and c + rot/2), so that no value crosses
 // lanes; otherwise they are channels 8l and D/2 + 8l.
 //
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     Rows here[PER];
     uint4 ya[PER], yb[PER];
     const int g0 = (int)blockIdx.y * per_tok + warp % per_tok;
-    fetch(g0, here, ya, yb);                                   // on their way while position and page are looked up
+    fetch(g0, here, ya, yb);                             // on their way while position and page are looked up
 
     // ---- position and page row, by the whole warp -----------------------------------------------
     int pos = 0;

@@ -86,6 +86,12 @@ def apply_args(**kw):
     dict(dtype=2), dict(dtype=-1), dict(n=-1), dict(pos=None), dict(q=None), dict(q=A + 2), dict(qs=500), dict(qs=504),
     dict(qo=None), dict(qo=A + 8 + (1 << 16)), dict(qos=256), dict(Hq=0), dict(inv=2), dict(qo=A + 64), dict(qo=A, qos=1024),
     dict(k=A, ks=512, ko=None, kos=512, Hk=4), dict(k=A, ks=512, ko=A + 16, kos=512, Hk=4),
+    # an output on the other tensor's input or output: all of it, part of each token, another stride
+    dict(k=A + (1 << 16), ks=512, ko=A + (1 << 17), kos=512, Hk=4), dict(k=A + (1 << 17), ks=512, ko=A, kos=512, Hk=4),
+    dict(k=A + (1 << 17), ks=512, ko=A + (1 << 16), kos=512, Hk=4),
+    dict(qs=1024, qo=A, qos=1024, k=A + 512, ks=1024, ko=A + 512, kos=1024, Hk=2),
+    dict(qs=1024, qo=A, qos=1024, k=A + 1024, ks=1536, ko=A + 1024, kos=1536, Hk=2),
+    dict(qs=1024, qo=A, qos=1024, k=A + 1024 - 2048, ks=1024, ko=A + 1024 - 2048, kos=1024, Hk=5),
 ])
 def test_rope_apply_refusals(lib, kw):
     rc, h = create(lib)
@@ -137,6 +143,8 @@ def test_append_refusals(lib):
                dict(rope=h, q=A, qs=512, qo=None, qos=512, Hq=4), dict(rope=h, q=A, qs=512, qo=A + 64, qos=512, Hq=4),
                dict(rope=h, q=A, qs=512, qo=A, qos=512, Hq=0), dict(pg=pages(format=1)), dict(pg=pages(format=0), dtype=1)):
         assert call(**kw) == EINVAL, kw
+    for kw in (dict(k=A + 4096), dict(v=A + 4096), dict(k=A + 1024, ks=512), dict(v=A + 512, vs=512)):     # q_out on k_new, v_new
+        assert call(**{**dict(rope=h, q=A, qs=512, qo=A, qos=512, Hq=4, n=30, B=30, k=A + (1 << 20), v=A + (1 << 20)), **kw}) == EINVAL, kw
     assert call(B=70000, n=70000) == EUNSUPPORTED
     assert call(rope=h, q=A, qs=70000 * 128, qo=A, qos=70000 * 128, Hq=70000) == EUNSUPPORTED
     assert call(n=0) == OK

@@ -401,6 +401,36 @@ def test_attention_shares(paged, page, lens):
     assert torch.equal(out, again), "not bit-reproducible"
 
 
+@pytest.mark.parametrize("B", [129, 300, 2000])
+def test_many_sequences(paged, B):
+    """More sequences than a warp looks at at once: append, read back and attend, empty and idle ones among them."""
+    H, d, page = 2, 64, 16
+    g = torch.Generator().manual_seed(B)
+    news = torch.randint(0, 4, (B,), generator=g).tolist()
+    pasts = [0 if i % 7 == 0 else int(x) for i, x in enumerate(torch.randint(0, 90, (B,), generator=g))]
+    news[0] = news[-1] = 0
+    lens = [a + b for a, b in zip(news, pasts)]
+    cache, table = filled(paged, [100] * B, page, H, d, 111, wild=False)
+    _, k, v = new_rows(news, 1, H, d, BF, 112)
+    cu = ints([0] + torch.tensor(news).cumsum(0).tolist())
+    cache.append(k, v, ints(lens), table, cu)
+    most = max(news)
+    ko, vo = torch.zeros(B, H, most, d, device="cuda"), torch.zeros(B, H, most, d, device="cuda")
+    cache.gather(ko, vo, ints(lens), table, first=ints(pasts))
+    at = torch.cat([torch.arange(n) for n in news]).cuda()
+    seq = torch.repeat_interleave(torch.arange(B), torch.tensor(news)).cuda()
+    for x, out in ((k, ko), (v, vo)):
+        c, st, m = ref.quantise(x)
+        want = ref.values(ref.pack(c), torch.stack((st, m), -1))
+        assert ((out[seq, :, at].double() - want).abs() <= 2.0 ** -23 * want.abs()).all()
+    q = torch.randn(B, 1, 2 * H, d, generator=gen(113), device="cuda").to(BF)
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    out = cache.attend(q, ints(lens), table, lse=lse)
+    some = sorted({0, 1, 2, 127, 128, B // 2, B - 2, B - 1} | set(range(0, B, 97)))
+    check_attention(cache, q[some], [lens[b] for b in some], table[some], out[some], lse[some], d ** -0.5)
+    assert torch.equal(out, cache.attend(q, ints(lens), table)) and torch.isfinite(out.float()).all()
+
+
 def test_attention_weights_of_far_keys(paged):
     """Scores that grow along the sequence and others that fall: the running reference has to move, late and often."""
     lens, page, d = [3000, 3000, 3000], 32, 64
