@@ -143,8 +143,7 @@ void set_rotation(RowsArgs& a, const retopk_rope* rope, int inverse) {
 template <int DEST> int launch_rows(RowsArgs& a, const retopk_rope* rope, int dtype, int d, int num_sms, cudaStream_t s) {
     const int rpw = 32 / (d / 16);
     a.gq = (a.Hq + rpw - 1) / rpw;
-    a.gqk = a.gq + (a.Hk + rpw - 1) / rpw;
-    a.groups = a.gqk + (a.Hv + rpw - 1) / rpw;
+    a.groups = a.gq + (a.Hk + a.Hv + rpw - 1) / rpw;
     const long long want = 16ll * num_sms;               // warps
     a.tokens_per_cta = a.n_tokens >= want ? 4 : (2 * a.n_tokens >= want ? 2 : 1);
     // two groups of rows to a warp, if the tokens alone do not fill the device

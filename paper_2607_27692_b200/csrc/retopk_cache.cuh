@@ -140,7 +140,7 @@ struct RowsArgs {
     uint16_t *q_out, *k_out;
     long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
     int Hq, Hk, Hv;
-    int gq, gqk, groups;        // groups of rows of q; of q and k; of all three
+    int gq, groups;             // groups of rows of q; of q, and of k and v one after the other
     Pages pg;
 };
 
@@ -178,17 +178,20 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     }
 
     // ---- where this warp's rows are -------------------------------------------------------------
-    // Groups of RPW rows of q, then k, then v are dealt out in turn to the warps of a token, which take
-    // PER of them at a time, the next ones on their way.
-    constexpr int PER = DEST == DEST_PAGES4 ? 1 : 2;     // (quantising twice over is too much code: 40 against 31 us, 6K tokens)
+    // Groups of RPW rows of q, then of k and v one after the other (a group may end in k and begin in v),
+    // are dealt out in turn to the warps of a token, which take PER of them at a time, the next ones on
+    // their way.
+    // (quantising twice over is too much code: 40 against 31 us, 6K tokens; so are partners in other lanes)
+    constexpr int PER = DEST == DEST_PAGES4 || ROT == ROT_OTHER ? 1 : 2;
     const int step = per_tok * a.units;
     const uint16_t *const q_src = a.q + tok * a.q_stride, *const k_src = a.k + tok * a.k_stride, *const v_src = a.v + tok * a.v_stride;
     struct Rows { int which, h; bool on; const uint16_t* src; };
-    auto rows_of = [&](int g) {                          // this lane's row of group g
+    auto rows_of = [&](int g) {                          // this lane's row of group g: 0 q, 1 k, 2 v
         Rows r;
-        r.which = g < a.gq ? 0 : (g < a.gqk ? 1 : 2);
-        r.h = (g - (r.which == 0 ? 0 : (r.which == 1 ? a.gq : a.gqk))) * RPW + row_in;
-        r.on = g < a.groups && r.h < (r.which == 0 ? a.Hq : (r.which == 1 ? a.Hk : a.Hv));
+        r.h = (g < a.gq ? g : g - a.gq) * RPW + row_in;
+        r.on = g < a.groups && r.h < (g < a.gq ? a.Hq : a.Hk + a.Hv);
+        r.which = g < a.gq ? 0 : (r.h < a.Hk ? 1 : 2);
+        if (r.which == 2) r.h -= a.Hk;
         r.src = (r.which == 0 ? q_src : (r.which == 1 ? k_src : v_src)) + r.h * D;
         return r;
     };
@@ -362,8 +365,13 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
             if (i > 0 && g + i * step >= a.groups) break;
             const Rows r = here[i];
             // (values go in as they are; their chunks are where the lane's are)
-            if (r.which != 2) rotate(DEST == DEST_PAGES4 && r.which == 1, ya[i], yb[i], r.src, r.on);
-            if (DEST == DEST_ROWS || r.which == 0) {
+            const int gi = g + i * step;
+            if (gi < a.gq || (gi - a.gq) * RPW < a.Hk) {
+                uint4 za = ya[i], zb = yb[i];
+                rotate(DEST == DEST_PAGES4 && gi >= a.gq, za, zb, r.src, r.on && r.which != 2);
+                if (r.which != 2) { ya[i] = za; yb[i] = zb; }
+            }
+            if (DEST == DEST_ROWS || gi < a.gq) {
                 if (r.on) {
                     uint16_t* dst = (r.which == 0 ? a.q_out + tok * a.q_out_stride : a.k_out + tok * a.k_out_stride) + r.h * D;
                     *reinterpret_cast<uint4*>(dst + ca) = ya[i];
