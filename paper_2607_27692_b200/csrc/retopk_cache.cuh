@@ -548,7 +548,7 @@ __host__ __device__ constexpr int q4_ring_bytes(int d, int shape) {      // the 
 // The tensor core cuts what it adds to an accumulator off at that accumulator's last place: after 150
 // tiles the sums were 5e-6 too small, and where many keys average out to little that is the first thing
 // wrong with the result.  Every Q4_FLUSH steps the sums move on to shared memory, by rounded additions.
-constexpr int Q4_FLUSH = 8;
+constexpr int Q4_FLUSH = 4;
 __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) { return q4_ring_bytes(d, shape) + Q4_WARPS * q4_cols(shape) * d * 4; }
 
 // Few warps with many registers: three tiles at a time keep the ALU and the tensor cores busier than

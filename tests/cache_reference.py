@@ -118,9 +118,9 @@ def attention_bounds(q, k_scale, v_scale, v, scale, n, dtype):
     The exponential: off by e in the score is off by the factor 1 + e; lse adds its own fp32 steps.
 
     Output.  Weights off by 1 + e on both sides of the quotient: 2 e * max |v|; weights as two truncated
-    bf16 parts: 2^-16, likewise.  Sums of codes: at most 24 products in a row in the tensor core, each
+    bf16 parts: 2^-16, likewise.  Sums of codes: at most 12 products in a row in the tensor core, each
     addition off by 2^-23 of a partial sum below 16 * step (bytes up to 255, divided by 16 at the end), for
-    weights that sum to 1; then n / 384 rounded additions, 2^-24 each; joining warps and CTAs is within
+    weights that sum to 1; then n / 192 rounded additions, 2^-24 each; joining warps and CTAs is within
     64 more.  Sums of minima: n / 32 rounded additions to a lane, of partial sums below |minimum|.
     """
     q = q.double()
@@ -133,5 +133,5 @@ def attention_bounds(q, k_scale, v_scale, v, scale, n, dtype):
     vs, vm = v_scale[..., 0].double().abs().max().item(), v_scale[..., 1].double().abs().max().item()
     err = abs(scale) * (15 * ks * rounded + 2.0 ** -20 * sumq * (15 * ks + km))
     vmax = v.abs().max().item() if v.numel() else 0.0
-    out = 2 * (err + 2.0 ** -16) * vmax + (n / 384 + 88) * 2.0 ** -23 * 16 * vs + (n / 32 + 64) * 2.0 ** -24 * vm
+    out = 2 * (err + 2.0 ** -16) * vmax + (n / 384 + 76) * 2.0 ** -23 * 16 * vs + (n / 32 + 64) * 2.0 ** -24 * vm
     return err + 2.0 ** -20 * (1 + abs(math.log(max(n, 2)))), out
