@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
         Rows r;
         r.h = (g < a.gq ? g : g - a.gq) * RPW + row_in;
         r.on = g < a.groups && r.h < (g < a.gq ? a.Hq : a.Hk + a.Hv);
-        r.which = g < a.gq ? 0 : (r.h < a.Hk ? 1 : 2);
+        r.which = g < a.gq ? 0 : (DEST == DEST_ROWS || r.h < a.Hk ? 1 : 2);
         if (r.which == 2) r.h -= a.Hk;
         r.src = (r.which == 0 ? q_src : (r.which == 1 ? k_src : v_src)) + r.h * D;
         return r;
@@ -366,7 +366,9 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
             const Rows r = here[i];
             // (values go in as they are; their chunks are where the lane's are)
             const int gi = g + i * step;
-            if (gi < a.gq || (gi - a.gq) * RPW < a.Hk) {
+            if (DEST == DEST_ROWS) {
+                rotate(false, ya[i], yb[i], r.src, r.on);
+            } else if (gi < a.gq || (gi - a.gq) * RPW < a.Hk) {
                 uint4 za = ya[i], zb = yb[i];
                 rotate(DEST == DEST_PAGES4 && gi >= a.gq, za, zb, r.src, r.on && r.which != 2);
                 if (r.which != 2) { ya[i] = za; yb[i] = zb; }
