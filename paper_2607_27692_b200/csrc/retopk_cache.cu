@@ -174,7 +174,7 @@ template <int SRC, int DT> int launch_gather(const GatherArgs& a, int d, dim3 gr
 }
 
 int q4_shape(int columns) { return columns <= 4 ? COLS_4 : (columns <= 8 ? COLS_8 : COLS_16); }
-int q4_ctas(int d, int shape, int num_sms) { return num_sms * q4_ctas_per_sm(d, shape); }
+int q4_ctas(int shape, int num_sms) { return num_sms * q4_ctas_per_sm(shape); }
 
 int check_q4_shape(int B, int T, int H_q, int H_kv, int d) {
     if (B < 1 || T < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv != 0) return RETOPK_EINVAL;
@@ -382,7 +382,7 @@ int64_t retopk_q4_attention_workspace(int B, int T, int H_q, int H_kv, int d) {
     if (rc == RETOPK_OK) rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
     const int shape = q4_shape(T * (H_q / H_kv));
-    return 2ll * q4_ctas(d, shape, num_sms) * q4_cols(shape) * (d + 2) * 4;
+    return 2ll * q4_ctas(shape, num_sms) * q4_cols(shape) * (d + 2) * 4;
 }
 
 int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int dtype,
@@ -414,9 +414,9 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
     a.B = B; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv;
     const int columns = T * a.G, shape = q4_shape(columns);
     a.col_tiles = (columns + q4_cols(shape) - 1) / q4_cols(shape);
-    if (workspace_bytes < 2ll * q4_ctas(pages->d, shape, num_sms) * q4_cols(shape) * (pages->d + 2) * 4) return RETOPK_EINVAL;
+    if (workspace_bytes < 2ll * q4_ctas(shape, num_sms) * q4_cols(shape) * (pages->d + 2) * 4) return RETOPK_EINVAL;
     const long long most = (long long)B * pages->H_kv * a.col_tiles * ((a.pg.capacity + Q4_UNIT - 1) / Q4_UNIT);
-    const int ctas = q4_ctas(pages->d, shape, num_sms);
+    const int ctas = q4_ctas(shape, num_sms);
     a.grid = (int)(most < ctas ? most : ctas);
     const int items = B * pages->H_kv * a.col_tiles;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -555,8 +555,9 @@ __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) { return q4_ri
 
 // Few warps with many registers: three tiles at a time keep the ALU and the tensor cores busier than
 // more warps with one or two tiles would (4 x 128K keys: 107 us; 16 warps an SM with two tiles 112, 20
-// with one 130).  Accumulators and queries of 16 columns of 128 channels take what two CTAs leave.
-__host__ __device__ constexpr int q4_ctas_per_sm(int d, int shape) { return shape == COLS_16 && d == 128 ? 2 : 3; }
+// with one 130).  16 columns take what two CTAs leave: at d = 128 they need it, at d = 64 four draft tokens
+// over 8K keys take 20.8 us with two CTAs and 22.9 with three.
+__host__ __device__ constexpr int q4_ctas_per_sm(int shape) { return shape == COLS_16 ? 2 : 3; }
 
 struct Q4Args {
     Pages pg;
@@ -700,7 +701,7 @@ struct Q4State {
 // Channels are matched to the fragments so that no code moves between lanes: key codes of lane quarter
 // t are channels 64 g + 16 t .. + 15, value codes of lane group r channels 64 g + 8 r .. + 7.
 template <int DT, int D, int SHAPE>
-__global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(D, SHAPE)) q4_attend_kernel(const __grid_constant__ Q4Args a) {
+__global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_kernel(const __grid_constant__ Q4Args a) {
     constexpr bool PACKED = SHAPE == COLS_4;
     constexpr int NT = SHAPE == COLS_16 ? 2 : 1, U = Q4_STEP;
     constexpr int COLS = q4_cols(SHAPE), NG = D / GROUP, NC = PACKED ? 1 : 2, PARTS = PACKED ? 1 : 2;
