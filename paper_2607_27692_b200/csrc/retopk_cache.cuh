@@ -630,8 +630,9 @@ __device__ __forceinline__ void mma16832_u8s8(int (&c)[4], uint32_t a0, uint32_t
             : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Codes as operands.  The kernel is bound by the ALU, where masks, shifts and byte permutations go, and
-// by the power that all of it takes (at 4 x 128K keys back to back the card is at 1000 W and 1.6 GHz).
+// Codes as operands.  What bounds the kernel short of HBM is instructions, on the ALU most of all, where
+// masks, shifts and byte permutations go, and the power that they take: 4 x 128K keys take 104 us in one
+// call at 1.9 GHz, 90% of the copy rate, and 115 us back to back, where the card is at 1000 W and 1.6 GHz.
 //
 // Keys for up to 4 columns: bytes b = n0 + 16 n1 are unsigned 8-bit operands as they are, and a mask gives
 // n0: one instruction for the eight codes of a word (mma.sync with 8-bit integers).
@@ -644,7 +645,8 @@ __device__ __forceinline__ void mma16832_u8s8(int (&c)[4], uint32_t a0, uint32_t
 //
 // Measured at 4 x 128K keys, with n0, 16 n1 and a shift for the upper bytes of keys and values: 132 us;
 // that shift as a product 142 us (its two issue slots cost more); e4m3 operands for the keys 143 us (mma
-// converts them to fp16, on the ALU).
+// converts them to fp16, on the ALU).  With bytes for the values 120 us, and key bytes as fp16 operands
+// 119 us back to back against 113 as integers.
 __device__ __forceinline__ void code_words(uint32_t x, uint32_t (&c)[4]) {
     const uint32_t y = x >> 8;
     c[0] = x & 0x000f000fu;                      // codes (0,4)
@@ -690,7 +692,7 @@ struct Q4State {
 //     q . k = sum_g ( s_g (q . n)_g + m_g (sum of q)_g )
 // so the codes go into the tensor core as they are and step and minimum are applied to the 16 x 8
 // result.  The same for values: sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j, the weight p_j s_j
-// entering as two bf16 parts (hi + lo, 2^-16 relative).  Keys are the M side of both products (16 keys
+// entering as two bf16 parts (hi + lo, 2^-17 relative).  Keys are the M side of both products (16 keys
 // or 16 channels), the columns the N side: with 4 columns the two parts of a weight fill the 8 columns
 // of one product, so the second part is free.
 //
