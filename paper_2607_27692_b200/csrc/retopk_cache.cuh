@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
         for (int p = 0; p < PASSES; ++p) {
             if (src_row[p] < 0) continue;
             const long long at = (((long long)b * a.pg.H_kv + h) * a.max_rows + row0 + r0 + p * RPP) * D;
-            if (SRC == 2 && DT == TYPE_BF16) {
+            if constexpr (SRC == 2 && DT == TYPE_BF16) {
                 const uint32_t x = x0[kv][p].x, sm = x0[kv][p].y;
                 uint32_t v[4];                           // values (0,4) (1,5) (2,6) (3,7)
 #pragma unroll
@@ -495,31 +495,31 @@ __global__ void __launch_bounds__(GATHER_THREADS) gather_kernel(const __grid_con
                 *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c0) =
                     make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
                                __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
-                continue;
-            }
-            float f[8];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const uint2 x = half ? x1[kv][p] : x0[kv][p];
-                if (SRC == 2) {
-                    const float2 sm = unpack2<TYPE_BF16>(x.y);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {        // 2^23 + n is a mask away too
-                        const float n = __uint_as_float(((x.x >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.f;
-                        f[4 * half + e] = fmaf(n, sm.x, sm.y);
-                    }
-                } else if (SPLIT) {
-                    const float2 lo = unpack2<SRC == 2 ? 0 : SRC>(x.x), hi = unpack2<SRC == 2 ? 0 : SRC>(x.y);
-                    f[4 * half] = lo.x; f[4 * half + 1] = lo.y; f[4 * half + 2] = hi.x; f[4 * half + 3] = hi.y;
-                }
-            }
-            if (SPLIT) {
-                float* o = static_cast<float*>(out) + at;
-                *reinterpret_cast<float4*>(o + c0) = make_float4(f[0], f[1], f[2], f[3]);
-                *reinterpret_cast<float4*>(o + c1) = make_float4(f[4], f[5], f[6], f[7]);
             } else {
-                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c0) =
-                    SRC == 2 ? pack8<SPLIT ? 0 : DT>(f) : make_uint4(x0[kv][p].x, x0[kv][p].y, x1[kv][p].x, x1[kv][p].y);
+                float f[8];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint2 x = half ? x1[kv][p] : x0[kv][p];
+                    if (SRC == 2) {
+                        const float2 sm = unpack2<TYPE_BF16>(x.y);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {        // 2^23 + n is a mask away too
+                            const float n = __uint_as_float(((x.x >> (4 * e)) & 15u) | 0x4b000000u) - 8388608.f;
+                            f[4 * half + e] = fmaf(n, sm.x, sm.y);
+                        }
+                    } else if (SPLIT) {
+                        const float2 lo = unpack2<SRC == 2 ? 0 : SRC>(x.x), hi = unpack2<SRC == 2 ? 0 : SRC>(x.y);
+                        f[4 * half] = lo.x; f[4 * half + 1] = lo.y; f[4 * half + 2] = hi.x; f[4 * half + 3] = hi.y;
+                    }
+                }
+                if (SPLIT) {
+                    float* o = static_cast<float*>(out) + at;
+                    *reinterpret_cast<float4*>(o + c0) = make_float4(f[0], f[1], f[2], f[3]);
+                    *reinterpret_cast<float4*>(o + c1) = make_float4(f[4], f[5], f[6], f[7]);
+                } else {
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c0) =
+                        SRC == 2 ? pack8<SPLIT ? 0 : DT>(f) : make_uint4(x0[kv][p].x, x0[kv][p].y, x1[kv][p].x, x1[kv][p].y);
+                }
             }
         }
     }
