@@ -664,6 +664,8 @@ __device__ __forceinline__ void pair_bytes(uint32_t z, uint32_t (&c)[4]) {
 __device__ __forceinline__ float2 step_min(uint32_t x, uint32_t two16) {
     return make_float2(__uint_as_float(x * two16), __uint_as_float(x & 0xffff0000u));
 }
+// Whether one of two bf16 values is an infinity or NaN.
+__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
     uint32_t x;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
@@ -1084,17 +1086,11 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
 #pragma unroll
                     for (int c = 0; c < NC; ++c) { sc[x][nt][0][c] *= unit[nt][c]; sc[x][nt][1][c] *= unit[nt][c]; }
             if (some_bad || kbase + (U - 1) * Q4_UNIT + Q4_TILE > safe_end || kbase < safe_lo) {
-                // Keys that do not count for a column: score -inf.  Rows that hold no key may hold
-                // anything: their value scales are cleared in the ring.
+                // Keys that do not count for a column: score -inf, so weight 0.
 #pragma unroll
                 for (int x = 0; x < U; ++x) {
                     const int key = kbase + x * Q4_UNIT + r8;
                     const bool none = some_bad && row_of(step * U + x) < 0;
-                    if (t4 < 2 && (none || key + 8 * t4 >= key_end)) {
-                        const uint32_t at = s_addr + ring_at + x * TILE + SB + t4 * (8 * NG * 4);
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) sts32(at + 4 * g, 0u);
-                    }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -1109,7 +1105,38 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
                                 if (none || key + 8 * r >= end || key + 8 * r < low) sc[x][nt][r][c] = -INFINITY;
                         }
                 }
-                __syncwarp();
+                // Rows that do not count may hold anything, and 0 times NaN is NaN: a row whose value step or
+                // minimum is no finite number leaves the ring, and the columns for which it does count get NaN.
+                bool wild = false;
+#pragma unroll
+                for (int x = 0; x < U; ++x)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) wild |= not_finite(lds32(s_addr + ring_at + x * TILE + SB + (r * 8 * NG + g) * 4));
+                if (__any_sync(0xffffffffu, wild)) {
+#pragma unroll
+                    for (int x = 0; x < U; ++x)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t at = s_addr + ring_at + x * TILE + SB + r * (8 * NG * 4);
+                            bool clear[NG];
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) {
+                                clear[g] = not_finite(lds32(at + 4 * g));
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int c = 0; c < NC; ++c)
+                                        if (clear[g] && sc[x][nt][r][c] != -INFINITY) st.msum[g][nt][c] = NAN;
+                            }
+                            __syncwarp();                // the four lanes of a row have read it
+#pragma unroll
+                            for (int g = 0; g < NG; ++g)
+                                if (clear[g] && t4 == 0) sts32(at + 4 * g, 0u);
+                        }
+                    __syncwarp();
+                }
             }
             bool grow = false;
 #pragma unroll
