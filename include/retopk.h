@@ -446,9 +446,9 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * `window` of those.  q row b * T + t with q_stride, out [B,T,H_q,d] contiguous, lse [B,T,H_q] fp32 or
  * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf.  Keys of pages
  * out of range do not count.  Scores, weights, sums and outputs are held in fp32 and rounded once to
- * dtype; weights enter the product with the codes as a sum of two bf16 parts (2^-17).  Queries enter, up
- * to 4 columns T * H_q / H_kv, as whole numbers of a unit of at most 2^-13.99 of the row's largest element
- * (exact above 2^-7 of it in bf16, 2^-4 in fp16), beyond that exactly; elements of q below 2^117.  What
+ * dtype; weights enter the product with the codes as a sum of two bf16 parts (2^-17).  Queries enter
+ * exactly but for 2^-23 of the larger element of a pair of channels and 2^-35 of the row's largest; elements of
+ * q below 2^117.  What
  * rows behind seq_lens hold, NaN patterns among it, has no influence.  Results are bit-reproducible.
  * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant
  * before and after; calls that may overlap on the GPU (two streams, two captured graphs) need one each.

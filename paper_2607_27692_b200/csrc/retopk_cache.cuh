@@ -619,34 +619,25 @@ __device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint3
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// c += a * b, c = a * b: unsigned by signed bytes, 32-bit sums
-template <bool FIRST>
-__device__ __forceinline__ void mma16832_u8s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    if (FIRST)
-        asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-            : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(0));
-    else
-        asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// Codes as operands.  What bounds the kernel short of HBM is instructions, on the ALU most of all, where
-// masks, shifts and byte permutations go, and the power that they take: 4 x 128K keys take 104 us in one
-// call at 1.9 GHz, 90% of the copy rate, and 115 us back to back, where the card is at 1000 W and 1.6 GHz.
-//
-// Keys for up to 4 columns: bytes b = n0 + 16 n1 are unsigned 8-bit operands as they are, and a mask gives
-// n0: one instruction for the eight codes of a word (mma.sync with 8-bit integers).
-//
-// Otherwise: the bits of a code ARE a small number.  In bf16 bits 0..7 count in steps of 2^-133
+// Codes as operands: the bits of a code ARE a small number.  In bf16 bits 0..7 count in steps of 2^-133
 // (subnormals, then the first exponent), in fp16 bits 0..10 in steps of 2^-24, and the tensor core
 // multiplies subnormals exactly.  So a mask makes the operand and no offset has to be taken out of the
-// sums again.  Values take n0 and b: four instructions for the eight codes of a word, and what b brings
-// too much is put right once at the end.
+// sums again.  A byte b = n0 + 16 n1 goes in as n0 and as b: four instructions for the eight codes of a
+// word instead of the seven of four masks and three shifts.  What b brings too much is put right in the
+// other operand (keys) or once at the end (values).
 //
-// Measured at 4 x 128K keys, with n0, 16 n1 and a shift for the upper bytes of keys and values: 132 us;
-// that shift as a product 142 us (its two issue slots cost more); e4m3 operands for the keys 143 us (mma
-// converts them to fp16, on the ALU).  With bytes for the values 120 us, and key bytes as fp16 operands
-// 119 us back to back against 113 as integers.
+// What bounds the kernel short of HBM is instructions, on the ALU most of all, where masks, shifts and byte
+// permutations go, and the power that they take (4 x 128K keys back to back: 1000 W at 1.6 GHz).  Measured
+// there, with n0, 16 n1 and a shift for the upper bytes of keys and values: 132 us; that shift as a product
+// 142 us (its two issue slots cost more); e4m3 operands for the keys 143 us (mma converts them to fp16, on
+// the ALU); queries as whole numbers against 8-bit integer operands 6 us less than this form, but then they
+// hold 2^-15 of a row's largest element only.
+__device__ __forceinline__ void code_bytes(uint32_t x, uint32_t (&c)[4]) {
+    c[0] = x & 0x000f000fu;                      // codes (0,4)
+    c[1] = __byte_perm(x, 0u, 0x4240);           // bytes 0 and 2: (0,4) + 16 (1,5)
+    c[3] = __byte_perm(x, 0u, 0x4341);           // bytes 1 and 3: (2,6) + 16 (3,7)
+    c[2] = c[3] & 0x000f000fu;                   // codes (2,6)
+}
 __device__ __forceinline__ void code_words(uint32_t x, uint32_t (&c)[4]) {
     const uint32_t y = x >> 8;
     c[0] = x & 0x000f000fu;                      // codes (0,4)
@@ -891,11 +882,10 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
         for (int i = 0; i < Q4_STAGES - 1; ++i) issue(i, i);
 
         // ---- query fragments --------------------------------------------------------------------
-        // Fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n).  Queries are scaled by a
-        // power of two that brings the column's largest element to 2^14..2^15.  PACKED they become whole
-        // numbers: elements above 2^-7 of the largest (bf16) or 2^-4 (fp16) are exact, smaller ones off by
-        // at most 2^-15 of it; else fp16, which is exact but for elements below 2^-24 of the largest.
-        uint32_t qf[NT][NG][PACKED ? 3 : 4][2];          // PACKED: [word], then the top digits of both words
+        // Fragment column n of tile nt is column (PACKED: n / 2, else nt * 8 + n).  Queries enter as
+        // fp16, scaled by the power of two that brings the column's largest element to 2^14..2^15: exact
+        // but for elements below 2^-24 of the largest (off by 2^-35 of it).
+        uint32_t qf[NT][NG][4][2];
         float qsum[NT][NG][NC], unit[NT][NC];            // sum of q in units of the products; their value in powers of two
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -916,44 +906,36 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
             // 2^(14 - exponent of the largest), kept within what a float can hold both ways
             int e2 = 141 - (int)(__float_as_uint(big) >> 23);
-            if (PACKED && (__float_as_uint(big) & 0x7fffffu) > 0x7e0000u) --e2;      // at most 32512
             e2 = e2 > 100 ? 100 : (e2 < -103 ? -103 : e2);
             const float to_unit = __uint_as_float((uint32_t)(127 + e2) << 23);
-            const float of_unit = __uint_as_float((uint32_t)(127 + (PACKED ? -4 : 24) - e2) << 23);  // products: 16 n q, or n q 2^-24
-            if (PACKED) {
-                // Whole numbers: 16 (q0 n0 + q1 n1) = (16 q0 - q1) n0 + q1 b, the bytes b as they lie in the
-                // cache.  Coefficients in digits of base 256: the middle one in the even columns, the low
-                // one in the odd ones; the third, top digit that only 16 q0 - q1 has makes a product of
-                // its own over the n0 of both words.
+            const float of_unit = __uint_as_float((uint32_t)(127 + 24 - e2) << 23);      // products: n q 2^-24
+            // PACKED: q0 n0 + q1 n1 = (q0 - q1 / 16) n0 + (q1 / 16) b.  The difference needs more bits than
+            // fp16 has: the odd columns take what it leaves over (2^-23 of the larger of the two is lost).
+            // Otherwise that would be a product more, dearer than the masks it saves: q1 / 16 against 16 n1.
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+            for (int g = 0; g < NG; ++g)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t n_dig = 0, b_dig = 0, top = 0;
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {    // bytes i of the word: codes 2 i and 2 i + 1
-                            const int q0 = __float2int_rn(f[g][j][2 * i] * to_unit), q1 = __float2int_rn(f[g][j][2 * i + 1] * to_unit);
-                            const int c = 16 * q0 - q1, c0 = (int)(signed char)c, r = (c - c0) >> 8, c1 = (int)(signed char)r;
-                            const int b0 = (int)(signed char)q1;
-                            n_dig |= (uint32_t)((r8 & 1 ? c0 : c1) & 0xff) << (8 * i);
-                            b_dig |= (uint32_t)((r8 & 1 ? b0 : (q1 - b0) >> 8) & 0xff) << (8 * i);
-                            top |= (uint32_t)((r8 & 1 ? 0 : (r - c1) >> 8) & 0xff) << (8 * i);
+                    for (int e = 0; e < 2; ++e) {        // channels (0,4) (1,5), then (2,6) (3,7) of the eight
+                        float q0[2], q1[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            q0[i] = f[g][j][2 * e + 4 * i] * to_unit;
+                            q1[i] = f[g][j][2 * e + 4 * i + 1] * (0.0625f * to_unit);
                         }
-                        qf[nt][g][j][0] = n_dig;
-                        qf[nt][g][j][1] = b_dig;
-                        qf[nt][g][2][j] = top;
+                        if (PACKED) {
+                            const float d0 = q0[0] - q1[0], d1 = q0[1] - q1[1];
+                            const uint32_t hi = pack2<TYPE_FP16>(d0, d1);
+                            const float2 hf = unpack2<TYPE_FP16>(hi);
+                            const bool rest = r8 & 1;
+                            qf[nt][g][2 * j + e][0] = rest ? pack2<TYPE_FP16>(d0 - hf.x, d1 - hf.y) : hi;
+                            qf[nt][g][2 * j + e][1] = rest ? 0u : pack2<TYPE_FP16>(q1[0], q1[1]);
+                        } else {
+                            qf[nt][g][2 * j + e][0] = pack2<TYPE_FP16>(q0[0], q0[1]);
+                            qf[nt][g][2 * j + e][1] = pack2<TYPE_FP16>(q1[0], q1[1]);
+                        }
                     }
-            } else {
-#pragma unroll
-                for (int g = 0; g < NG; ++g)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {    // channels (0,4) (1,5) (2,6) (3,7) of the eight; odd ones against 16 n
-                            const float c = e & 1 ? 0.0625f * to_unit : to_unit;
-                            qf[nt][g][PACKED ? 0 : 2 * j + (e >> 1)][e & 1] = pack2<TYPE_FP16>(f[g][j][e] * c, f[g][j][e + 4] * c);
-                        }
-            }
             // lanes hold columns 2 t4 + c of the result
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -1040,29 +1022,21 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
                 for (int g = 0; g < NG; ++g) {
                     const uint2 w0 = lds64(k_addr[g][0] + blk), w8 = lds64(k_addr[g][1] + blk + ROW8);
                     float acc[NT][4];
-                    if (PACKED) {
-                        constexpr uint32_t M = 0x0f0f0f0fu;
-                        int lo[4], hi[4];
-                        const uint32_t x0 = w0.x & M, x8 = w8.x & M, y0 = w0.y & M, y8 = w8.y & M;
-                        mma16832_u8s8<true>(lo, x0, x8, w0.x, w8.x, qf[0][g][0][0], qf[0][g][0][1]);
-                        mma16832_u8s8<true>(hi, x0, x8, y0, y8, qf[0][g][2][0], qf[0][g][2][1]);
-                        mma16832_u8s8<false>(lo, y0, y8, w0.y, w8.y, qf[0][g][1][0], qf[0][g][1][1]);
-                        // below 2^30: 64 channels of 15 * 9 * 2^16 + 15 * 2^15 + 255 * 2^15, half of them bytes
-                        acc[0][0] = (float)((hi[0] * 256 + lo[0]) * 256 + lo[1]);
-                        acc[0][2] = (float)((hi[2] * 256 + lo[2]) * 256 + lo[3]);
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            constexpr int N = PACKED ? 0 : 1;                // (indices that exist in both instances)
-                            uint32_t c0[4], c8[4];
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t c0[4], c8[4];
+                        if (PACKED) {
+                            code_bytes(j ? w0.y : w0.x, c0);
+                            code_bytes(j ? w8.y : w8.x, c8);
+                        } else {
                             code_words(j ? w0.y : w0.x, c0);
                             code_words(j ? w8.y : w8.x, c8);
+                        }
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                if (j == 0) mma16816_first(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][0][0], qf[nt][g][0][1]);
-                                else mma16816<TYPE_FP16>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2][0], qf[nt][g][2][1]);
-                                mma16816<TYPE_FP16>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][N * (2 * j + 1)][0], qf[nt][g][N * (2 * j + 1)][1]);
-                            }
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (j == 0) mma16816_first(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][0][0], qf[nt][g][0][1]);
+                            else mma16816<TYPE_FP16>(acc[nt], c0[0], c8[0], c0[1], c8[1], qf[nt][g][2][0], qf[nt][g][2][1]);
+                            mma16816<TYPE_FP16>(acc[nt], c0[2], c8[2], c0[3], c8[3], qf[nt][g][2 * j + 1][0], qf[nt][g][2 * j + 1][1]);
                         }
                     }
 #pragma unroll
@@ -1072,7 +1046,7 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int c = 0; c < NC; ++c)
-                                sc[x][nt][r][c] = fmaf(s.x, acc[nt][2 * r + c],
+                                sc[x][nt][r][c] = fmaf(s.x, PACKED ? acc[nt][2 * r] + acc[nt][2 * r + 1] : acc[nt][2 * r + c],
                                                        g == 0 ? s.y * qsum[nt][g][c] : fmaf(s.y, qsum[nt][g][c], sc[x][nt][r][c]));
                     }
                 }
