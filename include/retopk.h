@@ -444,7 +444,8 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * for T query tokens per sequence (1 = a decode step, more = draft tokens checked at once), which are
  * its last T positions: token t sees keys j < seq_lens[b] - T + 1 + t, with window > 0 only the last
  * `window` of those.  q row b * T + t with q_stride, out [B,T,H_q,d] contiguous, lse [B,T,H_q] fp32 or
- * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf.  Keys of pages
+ * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf; so does every row of
+ * a sequence whose length is negative or more than max_pages * page_size.  Keys of pages
  * out of range do not count.  Scores, weights, sums and outputs are held in fp32 and rounded once to
  * dtype; weights enter the product with the codes as a sum of two bf16 parts (2^-17).  Queries enter
  * exactly but for 2^-23 of the larger element of a pair of channels and 2^-35 of the row's largest; elements of

@@ -581,9 +581,8 @@ constexpr int Q4_BEGIN = 10;
 struct Span { int lo, len, units, weight; };
 __device__ __forceinline__ Span q4_span(const Q4Args& a, int seq_len) {
     Span s;
-    long long len = seq_len;
-    if (len > a.pg.capacity) len = a.pg.capacity;
-    s.len = len > 0 ? (int)len : 0;
+    // a length that the block table cannot hold does not tell which rows hold keys: none counts
+    s.len = seq_len > 0 && seq_len <= a.pg.capacity ? seq_len : 0;
     long long lo = a.window > 0 ? (long long)s.len - a.T + 1 - a.window : 0;
     if (lo < 0) lo = 0;
     s.lo = (int)lo & ~(Q4_TILE - 1);

@@ -48,3 +48,16 @@ def test_query_elements_far_below_the_largest(paged, dtype, d, G, T):
         # the sum of exponentials and its logarithm: a few fp32 steps of values about ln n, as for whole scores
         assert (off <= e + 2.0 ** -20 * (1 + math.log(n))).all(), f"lse off by {off.max().item()}, scores by {e} at most"
         assert ((out[b].double() - want).abs() <= ref.half_step(dtype) * (1 + 2.0 ** -10) * want.abs() + 2 * (e + 2.0 ** -15) * v.abs().max()).all()
+
+
+@pytest.mark.parametrize("G,T", [(4, 1), (1, 3), (8, 2)])
+def test_lengths_that_the_block_table_cannot_hold(paged, G, T):
+    """They do not say which rows hold keys (cut off at the table they moved the tokens' causal limits): no key counts."""
+    page, d, cap = 16, 64, 64
+    cache, table = filled(paged, [cap] * 4, page, 2, d, 411, wild=False)
+    q = torch.randn(4, T, 2 * G, d, generator=gen(412), device="cuda").to(BF)
+    lse, fits = torch.empty(q.shape[:-1], device="cuda"), torch.empty(q.shape[:-1], device="cuda")
+    want = cache.attend(q, ints([cap] * 4), table, lse=fits)
+    out = cache.attend(q, ints([cap, cap + 1, 2 ** 31 - 1, -2 ** 31]), table, lse=lse)
+    assert torch.equal(out[0], want[0]) and torch.equal(lse[0], fits[0]) and torch.isfinite(lse[0]).all()
+    assert (out[1:] == 0).all() and (lse[1:] == -math.inf).all()
