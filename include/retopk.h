@@ -445,12 +445,15 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * its last T positions: token t sees keys j < seq_lens[b] - T + 1 + t, with window > 0 only the last
  * `window` of those.  q row b * T + t with q_stride, out [B,T,H_q,d] contiguous, lse [B,T,H_q] fp32 or
  * NULL: ln sum_j exp(scale * q . k_j).  A row without keys gives out = 0, lse = -inf; so does every row of
- * a sequence whose length is negative or more than max_pages * page_size.  Keys of pages
- * out of range do not count.  Scores, weights, sums and outputs are held in fp32 and rounded once to
- * dtype; weights enter the product with the codes as a sum of two bf16 parts (2^-17).  Queries enter
- * exactly but for 2^-23 of the larger element of a pair of channels and 2^-35 of the row's largest; elements of
- * q below 2^117.  What
- * rows behind seq_lens hold, NaN patterns among it, has no influence.  Results are bit-reproducible.
+ * a sequence whose length is negative or more than max_pages * page_size.  Keys of pages out of range do
+ * not count.  NaN, infinities and scores beyond the fp32 range are not hidden: a row with such a score is
+ * NaN throughout, its lse too; a value whose step or minimum is not finite makes its 64 channels non-finite
+ * in every row that sees it.  What rows hold that a token does not see (behind seq_lens, before the window,
+ * of later draft tokens), NaN patterns among it, has no influence on it.
+ * Scores, weights, sums and outputs are held in fp32 and rounded once to dtype; weights enter the product
+ * with the codes as a sum of two bf16 parts (2^-17).  Queries enter exactly but for 2^-23 of the larger
+ * element of a pair of channels and 2^-35 of the row's largest; elements of q below 2^117.  Results are
+ * bit-reproducible.
  * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant
  * before and after; calls that may overlap on the GPU (two streams, two captured graphs) need one each.
  * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096, at most 2^20 keys of a sequence (max_pages *

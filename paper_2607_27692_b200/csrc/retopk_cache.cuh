@@ -534,7 +534,7 @@ constexpr int Q4_STEP = 3;               // tiles that a warp takes in one step
 constexpr int Q4_UNIT = Q4_TILE * Q4_WARPS;
 constexpr int Q4_STAGES = 2;             // steps a warp has in flight or in use
 constexpr int Q4_AHEAD = 32 / Q4_STEP * Q4_STEP;   // tiles whose rows the lanes of a warp look up at once
-constexpr float Q4_NONE = -3.0e38f;      // reference of a column that has seen no key
+constexpr float Q4_NONE = -3.402823466e38f;   // reference of a column that has seen no key: no score is below it
 
 // Columns (query token, head of the group) of one CTA by shape: four columns, each as two parts of
 // its weights, or 8 or 16 columns.
@@ -1052,12 +1052,19 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
             }
 
             // ---- weights -------------------------------------------------------------------------
+            // An infinite score becomes NaN (times 0, plus itself): +inf leaves no weights to speak of, and
+            // -inf, which stands for a key that does not count, would drop this one without a trace.
 #pragma unroll
             for (int x = 0; x < U; ++x)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) { sc[x][nt][0][c] *= unit[nt][c]; sc[x][nt][1][c] *= unit[nt][c]; }
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const float y = sc[x][nt][r][c] * unit[nt][c];
+                            sc[x][nt][r][c] = fmaf(y, 0.f, y);
+                        }
             if (some_bad || kbase + (U - 1) * Q4_UNIT + Q4_TILE > safe_end || kbase < safe_lo) {
                 // Keys that do not count for a column: score -inf, so weight 0.
 #pragma unroll
@@ -1297,9 +1304,9 @@ __global__ void __launch_bounds__(Q4_THREADS, q4_ctas_per_sm(SHAPE)) q4_attend_k
             if (whole) {
                 const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
                 const long long row = ((long long)b * a.T + tok) * a.Hq + head;
-                const float y = l > 0.f ? o / l : 0.f;
+                const float y = l == 0.f ? 0.f : o / l;         // (no key; a NaN goes on)
                 a.out[row * D + ch] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
-                if (a.lse && ch == 0) a.lse[row] = l > 0.f ? (mx + 64.f + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                if (a.lse && ch == 0) a.lse[row] = l == 0.f ? -INFINITY : (mx + 64.f + log2f(l)) * 0.6931471805599453f;
             } else {
                 part[col * (D + 2) + ch] = o;
                 if (ch == 0) { part[col * (D + 2) + D] = mx; part[col * (D + 2) + D + 1] = l; }
@@ -1378,9 +1385,9 @@ __global__ void __launch_bounds__(D) q4_combine_kernel(const __grid_constant__ Q
     }
     const int cc = ct * COLS + col, tok = cc / a.G, head = h * a.G + (cc - tok * a.G);
     const long long row = ((long long)b * a.T + tok) * a.Hq + head;
-    const float y = l > 0.f ? o / l : 0.f;
+    const float y = l == 0.f ? 0.f : o / l;         // (no key; a NaN goes on)
     a.out[row * D + tid] = (uint16_t)(pack2<DT>(y, 0.f) & 0xffffu);
-    if (a.lse && tid == 0) a.lse[row] = l > 0.f ? (mx + 64.f + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && tid == 0) a.lse[row] = l == 0.f ? -INFINITY : (mx + 64.f + log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace retopk_cache

@@ -87,3 +87,70 @@ def test_values_that_are_seen(paged, d, group, G, T):
                         assert torch.equal(y[:, other], w[:, other])
                     else:
                         assert torch.equal(y, w)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,T", [(1, 1), (4, 1), (8, 1), (4, 4)])
+def test_queries_that_are_not_finite(paged, dtype, d, G, T):
+    """A row whose query holds NaN or an infinity is NaN, not the row of a sequence without keys; others are as before."""
+    lens, page = [0, T, 50, 1003, 40000], 16
+    cache, table = filled(paged, lens, page, 2, d, 321)
+    q = torch.randn(len(lens), T, 2 * G, d, generator=gen(322), device="cuda").to(dtype)
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    want = cache.attend(q, ints(lens), table, lse=lse)
+    for x in (math.nan, math.inf, -math.inf):
+        wild, got_lse = q.clone(), torch.empty_like(lse)
+        wild[:, T - 1, G, 5] = x
+        got = cache.attend(wild, ints(lens), table, lse=got_lse)
+        hit = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+        hit[1:, T - 1, G] = True
+        assert torch.isnan(got[hit]).all() and torch.isnan(got_lse[hit]).all()
+        assert torch.equal(got[~hit], want[~hit]) and torch.equal(got_lse[~hit], lse[~hit])
+        assert (got[0] == 0).all() and (got_lse[0] == -math.inf).all()
+
+
+@pytest.mark.parametrize("d,group", [(64, 0), (128, 1)])
+@pytest.mark.parametrize("G,T", [(1, 1), (4, 1), (8, 1), (4, 4)])
+def test_keys_that_are_not_finite(paged, d, group, G, T):
+    """One live key without a finite step or minimum: every row that sees it is NaN; an infinite score is never a masked one."""
+    lens, page, H = [T, 50, 1003, 40000], 16, 2
+    cache, table = filled(paged, lens, page, H, d, 331)
+    q = torch.randn(len(lens), T, H * G, d, generator=gen(332), device="cuda").to(BF)
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    want = cache.attend(q, ints(lens), table, lse=lse)
+    start = cache.k_scale.clone()
+    for part, x in ((0, math.nan), (0, math.inf), (0, -math.inf), (1, math.nan), (1, math.inf), (1, -math.inf)):
+        for far in (0.0, 0.4, 1.0):
+            cache.k_scale.copy_(start)
+            rows = [int(far * (n - 1)) for n in lens]
+            for b, r in enumerate(rows):
+                put(cache, table, b, [r], "k_scale", part, x, group)
+            got_lse = torch.empty_like(lse)
+            got = cache.attend(q, ints(lens), table, lse=got_lse)
+            for b, (n, r) in enumerate(zip(lens, rows)):
+                for t in range(T):
+                    if r < n - T + 1 + t:
+                        assert torch.isnan(got[b, t]).all() and torch.isnan(got_lse[b, t]).all()
+                    else:
+                        assert torch.equal(got[b, t], want[b, t]) and torch.equal(got_lse[b, t], lse[b, t])
+
+
+@pytest.mark.parametrize("G", [4, 8])
+@pytest.mark.parametrize("low", [-1.0e38, -2.2e38, 2.2e38])
+def test_scores_near_the_end_of_the_range(paged, G, low):
+    """One key with a score near the largest fp32 number: it has all the weight, whatever its sign."""
+    d = 64
+    cache, table = filled(paged, [1], 16, 1, d, 341, wild=False)
+    row = (table[0, 0].item(), 0, 0)
+    cache.k_scale[row][:, 0] = 0.0
+    cache.k_scale[row][:, 1] = 1.0e36
+    q = torch.full((1, G, d), -1.0, device="cuda").to(BF)
+    scale = -low / (64 * cache.k_scale[row][0, 1].item())
+    lse = torch.empty(1, G, device="cuda")
+    out = cache.attend(q, ints([1]), table, scale=scale, lse=lse)
+    n = torch.stack((cache.v[row] & 15, cache.v[row] >> 4), -1).flatten().double()
+    want = n * cache.v_scale[row][0, 0].double() + cache.v_scale[row][0, 1].double()
+    # the weight is 1 and its two parts are exact; one product and sum in fp32, and the rounding to bf16
+    assert ((out[0].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -20).all()
+    assert ((lse.double() - low).abs() <= 2.0 ** -20 * abs(low)).all()
