@@ -413,8 +413,9 @@ typedef struct {
  * are (then q = NULL).
  * RETOPK_PAGES_Q4 rounds the rotated key to `dtype` and then quantises each group of 64 channels:
  * m = bf16(min), s = bf16((max - m) / 15), n = round((x - m) / s) to nearest, ties to even, within
- * 0..15, n = 0 where s = 0; 32-bit arithmetic, IEEE rounding.  A span max - m above the fp32 range is
- * unspecified.  16-bit pages hold `dtype`; q and keys that stay 16-bit are rounded once from a rotation
+ * 0..15, n = 0 where s = 0; 32-bit arithmetic, IEEE rounding.  A group with NaN or an
+ * infinity in it, or with a span max - m above the fp32 range, has a step of infinity or NaN and code 0
+ * throughout: s * n + m is NaN in all its channels.  16-bit pages hold `dtype`; q and keys that stay 16-bit are rounded once from a rotation
  * within 2^-23 of the exact one, keys that are quantised from one in 64 bits.
  * Rows of k_new from cu_new[B] on, and tokens whose position is negative (an idle sequence of length
  * 0), are left out, their q_out rows too.  A key whose page is not in 0..n_pages-1 or whose position is

@@ -50,6 +50,18 @@ template <int DT> __device__ __forceinline__ uint4 pack8(const float* f) {
     return make_uint4(pack2<DT>(f[0], f[1]), pack2<DT>(f[2], f[3]), pack2<DT>(f[4], f[5]), pack2<DT>(f[6], f[7]));
 }
 
+// Minimum and maximum that are NaN if one operand is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float c;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float c;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
+}
+
 __device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
@@ -326,23 +338,24 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
             float mna = xa[0], mxa = xa[0], mnb = xb[0], mxb = xb[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) {
-                mna = fminf(mna, xa[e]); mxa = fmaxf(mxa, xa[e]);
-                mnb = fminf(mnb, xb[e]); mxb = fmaxf(mxb, xb[e]);
+                mna = min_nan(mna, xa[e]); mxa = max_nan(mxa, xa[e]);
+                mnb = min_nan(mnb, xb[e]); mxb = max_nan(mxb, xb[e]);
             }
             const int ga = ca / GROUP, gb = cb / GROUP;
             float low[NG], step_[NG];
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                float mn = fminf(ga == g ? mna : INFINITY, gb == g ? mnb : INFINITY);
-                float mx = fmaxf(ga == g ? mxa : -INFINITY, gb == g ? mxb : -INFINITY);
+                float mn = min_nan(ga == g ? mna : INFINITY, gb == g ? mnb : INFINITY);
+                float mx = max_nan(ga == g ? mxa : -INFINITY, gb == g ? mxb : -INFINITY);
 #pragma unroll
                 for (int o = 1; o < LANES; o <<= 1) {
-                    mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                    mn = min_nan(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+                    mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 }
                 low[g] = __bfloat162float(__float2bfloat16_rn(mn));
-                // the minimum may have been rounded up past the maximum of a narrow group
-                step_[g] = __bfloat162float(__float2bfloat16_rn(fmaxf(__fdiv_rn(mx - low[g], 15.f), 0.f)));
+                // the minimum may have been rounded up past the maximum of a narrow group; no finite code stands
+                // for NaN or an infinity, so a group that holds one gets a step of NaN or inf, which makes all of it NaN
+                step_[g] = __bfloat162float(__float2bfloat16_rn(max_nan(__fdiv_rn(mx - low[g], 15.f), 0.f)));
             }
             const uint32_t wa = codes_of(xa, ga == 0 ? low[0] : low[NG - 1], ga == 0 ? step_[0] : step_[NG - 1]);
             const uint32_t wb = codes_of(xb, gb == 0 ? low[0] : low[NG - 1], gb == 0 ? step_[0] : step_[NG - 1]);

@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import cache_reference as ref
 from test_gpu_cache_ops import BF, FP, filled, gen, ints
 
 pytestmark = pytest.mark.gpu
@@ -154,3 +155,67 @@ def test_scores_near_the_end_of_the_range(paged, G, low):
     # the weight is 1 and its two parts are exact; one product and sum in fp32, and the rounding to bf16
     assert ((out[0].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -20).all()
     assert ((lse.double() - low).abs() <= 2.0 ** -20 * abs(low)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
+def test_groups_that_hold_no_finite_numbers(paged, dtype, d):
+    """NaN and infinities in keys and values of a 4-bit cache: their 64 channels read back as NaN, all others as ever."""
+    n, H, page = 45, 2, 16
+    x = torch.randn(n, H, d, generator=gen(351), device="cuda").to(dtype)
+    hit = torch.zeros(n, H, d // 64, dtype=torch.bool, device="cuda")
+    row = 0
+    for at in (0, 7, 8, 31, 32, 63):                # channels in different lanes and chunks
+        for v in (math.nan, math.inf, -math.inf):
+            for g in range(d // 64):
+                x[row % n, row // n, 64 * g + at] = v
+                hit[row % n, row // n, g] = True
+                row += 1
+    for v in (math.nan, math.inf, -math.inf):       # a whole group, and both infinities in one
+        x[row % n, row // n, d - 64:] = v
+        hit[row % n, row // n, -1] = True
+        row += 1
+    x[row % n, row // n, :2] = torch.tensor([math.inf, -math.inf])
+    hit[row % n, row // n, 0] = True
+    if dtype == BF:                                 # a span that fp32 does not hold
+        x[row % n, row // n + 1, :2] = torch.tensor([3.0e38, -3.0e38])
+        hit[row % n, row // n + 1, 0] = True
+    assert row < 2 * n - 45 and not hit.all()
+    codes, step, low = ref.quantise(torch.where(hit.repeat_interleave(64, -1), 0, x))
+    table = ints([[2, 0, 1]])
+    cache = paged.KVPages(3, H, page, d, "q4")
+    cache.append(x, x.flip(0).contiguous(), ints([n]), table)
+    want = ref.values(ref.pack(codes), torch.stack((step, low), -1)).unflatten(-1, (-1, 64))
+    for out in (torch.float32, BF, FP):
+        k, v = (torch.zeros(1, H, n, d, dtype=out, device="cuda") for _ in "kv")
+        cache.gather(k, v, ints([n]), table)
+        for got, w, h in ((k, want, hit), (v, want.flip(0), hit.flip(0))):
+            got = got[0].transpose(0, 1).unflatten(-1, (-1, 64))
+            assert torch.isnan(got[h]).all()
+            tol = 2.0 ** -23 if out == torch.float32 else ref.half_step(out) * (1 + 2.0 ** -10)
+            assert ((got[~h].double() - w[~h]).abs() <= tol * w[~h].abs() + 2.0 ** -24).all()
+    # and the attention over them does not hide them
+    q = torch.randn(1, H, d, generator=gen(352), device="cuda").to(dtype)
+    out = cache.attend(q, ints([n]), table)[0]
+    for h in range(H):
+        assert torch.isnan(out[h]).all() if hit[:, h].any() else torch.isfinite(out[h]).all()
+
+
+def test_a_rotated_key_that_is_not_finite(paged):
+    """An infinity in a key spreads to its pair and to their groups, rotated on the way into 4 bits; other heads stay."""
+    n, H, d = 20, 2, 128
+    x = torch.randn(n, H, d, generator=gen(361), device="cuda").to(BF)
+    wild = x.clone()
+    wild[3, 0, 5] = math.inf                        # paired with channel 69: both groups
+    wild[4, 1, 70] = math.nan
+    rope = paged.Rope(d)
+    outs = []
+    for k in (x, wild):
+        cache = paged.KVPages(2, H, 16, d, "q4")
+        cache.append(k, x, ints([n]), ints([[0, 1]]), rope=rope)
+        got = torch.zeros(1, H, n, d, device="cuda")
+        cache.gather(got, None, ints([n]), ints([[0, 1]]))
+        outs.append(got[0])
+    assert torch.isnan(outs[1][0, 3]).all() and torch.isnan(outs[1][1, 4]).all()
+    outs[1][0, 3], outs[1][1, 4] = outs[0][0, 3], outs[0][1, 4]
+    assert torch.equal(outs[0], outs[1])
