@@ -357,7 +357,8 @@ enum { RETOPK_BF16 = 0, RETOPK_FP16 = 1, RETOPK_FP32 = 2 };
  * attn_factor > 0 replaces a.  Zero in low_freq_factor, high_freq_factor, beta_fast or beta_slow
  * stands for 1, 4, 32 and 1.  Angle and rotation are computed in 64 bits (at position 1 Mi an
  * angle in 32 bits is 0.06 rad off) or, the rotation, to within 2^-23 of that; rounded once to the tensor's
- * type.
+ * type.  Infinities and NaN in a pair go through the formula as IEEE arithmetic takes them; finite elements
+ * below 2^127 / a.
  */
 typedef struct retopk_rope retopk_rope;
 enum { RETOPK_ROPE_HALF = 0, RETOPK_ROPE_INTERLEAVED = 1 };

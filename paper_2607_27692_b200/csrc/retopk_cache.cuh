@@ -156,6 +156,17 @@ struct RowsArgs {
     Pages pg;
 };
 
+// x as the sum of a head of 16 (bf16) or 13 (fp16) bits and a rest.  Both have x's sign (cut off, not
+// rounded) and neither is 0 unless x is (a rest of 2^-100 is nothing next to the head), so that an
+// infinity times x is that infinity in both products and in their sum.
+template <int DT> __device__ __forceinline__ float2 head_and_rest(double x) {
+    constexpr uint32_t HEAD = DT == TYPE_BF16 ? 0xffffff00u : 0xfffff800u;
+    const float h = __uint_as_float(__float_as_uint(__double2float_rz(x)) & HEAD);
+    float r = (float)(x - h);
+    if (r == 0.f && h != 0.f) r = copysignf(7.8886091e-31f, h);
+    return make_float2(h, r);
+}
+
 // One row is held by D / 16 lanes, two chunks of 8 channels each, so that a warp has 4 rows (d = 128) or
 // 8; a warp stays with one token, whose cosines and sines it keeps in shared memory, and goes through the
 // heads, the next groups of rows on their way.  Where a half-layout rotation covers a multiple of 16
@@ -266,9 +277,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
         // a lane reads 8 neighbouring pairs one after the other; the exclusive-or keeps the lanes of a
         // row in different banks
         const int at = i ^ ((i >> 3) & 7);
-        constexpr uint32_t HEAD = DT == TYPE_BF16 ? 0xffffff00u : 0xfffff800u;
-        const float ch = __uint_as_float(__float_as_uint((float)cs) & HEAD), sh = __uint_as_float(__float_as_uint((float)sn) & HEAD);
-        s_tab[warp][at] = make_float4(ch, (float)(cs - ch), sh, (float)(sn - sh));
+        const float2 c = head_and_rest<DT>(cs), s = head_and_rest<DT>(sn);
+        s_tab[warp][at] = make_float4(c.x, c.y, s.x, s.y);
         if (DEST == DEST_PAGES4) s_tab64[DEST == DEST_PAGES4 ? warp : 0][at] = make_double2(cs, sn);
     }
     __syncwarp();

@@ -219,3 +219,52 @@ def test_a_rotated_key_that_is_not_finite(paged):
     assert torch.isnan(outs[1][0, 3]).all() and torch.isnan(outs[1][1, 4]).all()
     outs[1][0, 3], outs[1][1, 4] = outs[0][0, 3], outs[0][1, 4]
     assert torch.equal(outs[0], outs[1])
+
+
+def same_numbers(got, want, dtype):
+    """got is `want` (fp64) rounded: NaN where it is, the same infinities, half a step elsewhere."""
+    rounded = want.to(dtype)
+    assert torch.equal(torch.isnan(got), torch.isnan(rounded))
+    wild = torch.isinf(rounded)
+    assert torch.equal(got[wild], rounded[wild]) and torch.equal(torch.isinf(got), wild)
+    ok = torch.isfinite(rounded)
+    assert ((got[ok].double() - want[ok]).abs() <= ref.half_step(dtype) * (1 + 2.0 ** -10) * want[ok].abs() + 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,rot,interleaved", [(128, 128, False), (128, 64, True), (128, 10, False), (64, 64, False), (64, 48, True), (64, 50, False)])
+def test_rotation_of_infinities(paged, dtype, d, rot, interleaved):
+    """x cos - y sin and x sin + y cos as IEEE arithmetic has them; positions whose cosine or sine is 0 or 1 among them."""
+    n, H = 40, 3
+    x = torch.randn(n, H, d, generator=gen(371), device="cuda").to(dtype)
+    g = torch.Generator().manual_seed(372)
+    for i in range(n):
+        for _ in range(4):
+            x[i, int(torch.randint(0, H, (1,), generator=g)), int(torch.randint(0, d, (1,), generator=g))] = \
+                (math.inf, -math.inf, math.nan)[int(torch.randint(0, 3, (1,), generator=g))]
+    x[5] = math.inf
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 97
+    w, _ = ref.frequencies(rot)
+    rope = paged.Rope(d, rot, interleaved=interleaved)
+    for inverse in (False, True):
+        same_numbers(rope.apply(x, pos, inverse=inverse), ref.rotate(x, pos, w, 1.0, interleaved, inverse), dtype)
+    # on the way into a 16-bit cache: token i goes to position i
+    cache = paged.KVPages(1, H, n, d, "bf16" if dtype == BF else "fp16")
+    q = cache.append(x, x, ints([n]), rope=rope, q=x.flip(1).contiguous())
+    want = ref.rotate(x, torch.arange(n, device="cuda"), w, 1.0, interleaved)
+    same_numbers(cache.k[0].transpose(0, 1), want, dtype)
+    same_numbers(q, want.flip(1), dtype)
+    same_numbers(cache.v[0].transpose(0, 1), x.double(), dtype)
+
+
+def test_rotation_that_overflows(paged):
+    """fp16 rows whose rotated values are beyond the type: infinities, of the right sign."""
+    n, H, d = 64, 2, 64
+    x = (60000 * torch.randn(n, H, d, generator=gen(381), device="cuda").sign() * torch.rand(n, H, d, generator=gen(382), device="cuda")).to(FP)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    want = ref.rotate(x, pos, ref.frequencies(d)[0])
+    assert (want.abs() > 65536).any()
+    # within 2^-12 of the border both roundings are right
+    want = torch.where((want.abs() - 65520).abs() < 16, 0.0, want)
+    got = paged.Rope(d).apply(x, pos)
+    same_numbers(torch.where(want == 0, 0, got), want, FP)
