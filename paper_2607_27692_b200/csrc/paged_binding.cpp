@@ -5,6 +5,7 @@
 #include <torch/csrc/Exceptions.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -72,6 +73,18 @@ int64_t sequences(PyObject* lens) {
 at::Tensor empty(at::IntArrayRef shape, const at::Tensor& like, at::ScalarType dt) { return at::empty(shape, like.options().dtype(dt)); }
 void* stream_of(at::Device dev) { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
 
+// Whether autograd would have to record a call on these tensors.
+bool wants_gradient(std::initializer_list<const at::Tensor*> all) {
+    if (!at::GradMode::is_enabled()) return false;
+    for (const at::Tensor* t : all)
+        if (t->defined() && t->requires_grad()) return true;
+    return false;
+}
+// For calls without a backward pass: a gradient that would be lost is refused.
+void no_gradient(const char* what, std::initializer_list<const at::Tensor*> all) {
+    if (wants_gradient(all)) throw Failure{g_error, text(what, " has no gradient, but a tensor requires one: call it under torch.no_grad(), or detach")};
+}
+
 // The pages of one cache, as KVPages made them out.
 struct Cache {
     retopk_pages_t pages;
@@ -112,7 +125,8 @@ bool arity(Py_ssize_t n, Py_ssize_t want) {
     return n == want;
 }
 
-// rope_apply(handle, d, q, k, positions, q_out, k_out, inverse) -> (q_out, k_out)
+// rope_apply(handle, d, q, k, positions, q_out, k_out, inverse) -> (q_out, k_out), or None where autograd has
+// to record the call
 PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (!arity(n_args, 8)) return nullptr;
     return guarded([&]() -> PyObject* {
@@ -126,6 +140,11 @@ PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const Rows qi = rows(q, "q", dev, dt, n, H_q, d);
         const int32_t* pos = ints(a[4], "positions", dev, n);
         const int inverse = PyObject_IsTrue(a[7]);
+        const at::Tensor none, &k_in = given(a[3]) ? tensor(a[3], "k") : none;
+        if (given(a[5]) || given(a[6]))
+            no_gradient("a rotation into given outputs", {&q, &k_in, given(a[5]) ? &tensor(a[5], "q_out") : &none, given(a[6]) ? &tensor(a[6], "k_out") : &none});
+        else if (wants_gradient({&q, &k_in}))
+            return Py_NewRef(Py_None);
         const c10::cuda::CUDAGuard guard(dev);
         const at::Tensor qo = given(a[5]) ? tensor(a[5], "q_out") : empty({n, H_q, d}, q, dt);
         const Rows qr = rows(qo, "q_out", dev, dt, n, H_q, d);
@@ -180,6 +199,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (!cu && B > 0 && n % B) value_error(n, " new tokens do not divide among ", B, " sequences: pass cu_new");
         const auto* rope = static_cast<const retopk_rope*>(PyLong_AsVoidPtr(a[6]));
         const retopk_pages_t pages = pages_of(c, B, a[4]);
+        const at::Tensor none;
+        no_gradient("append", {&k, &v, given(a[8]) ? &tensor(a[8], "q") : &none, given(a[9]) ? &tensor(a[9], "q_out") : &none});
         const c10::cuda::CUDAGuard guard(c.dev);
         at::Tensor qo;
         Rows qi = {nullptr, 0}, qr = {nullptr, 0};
@@ -216,6 +237,7 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                 const at::Tensor& t = tensor(a[1 + i], "k_out, v_out");
                 if (t.device() != c.dev || t.scalar_type() != dt || t.sizes() != ref.sizes() || !t.is_contiguous())
                     type_error("k_out, v_out: contiguous ", dt, " ", ref.sizes(), " on ", c.dev);
+                no_gradient("gather", {&t});
                 out[i] = t.data_ptr();
             }
         const int64_t B = ref.size(0);
@@ -247,6 +269,8 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const int64_t q_stride = B * T <= 1 ? H_q * d : (T == 1 ? q.stride(0) : q.stride(1));
         const int32_t* lens = ints(a[2], "seq_lens", c.dev, B);
         const retopk_pages_t pages = pages_of(c, B, a[3]);
+        const at::Tensor none;
+        no_gradient("attend", {&q, given(a[6]) ? &tensor(a[6], "out") : &none, given(a[7]) ? &tensor(a[7], "lse") : &none});
         const double scale = given(a[4]) ? PyFloat_AsDouble(a[4]) : 1.0 / std::sqrt((double)d);
         const int64_t window = PyLong_AsLongLong(a[5]);
         if (PyErr_Occurred()) throw python_error();

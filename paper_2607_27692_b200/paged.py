@@ -14,6 +14,9 @@ What a decode loop needs around :class:`paper_2607_27692_b200.retopk.ReTopK`::
     q = cache.append(k_new, v_new, seq_lens, block_table, rope=rope, q=q_new)
     out = cache.attend(q, seq_lens, block_table)
 
+The rotation is differentiable.  The calls of a cache are for serving: they have no gradient and refuse
+tensors that require one unless under ``torch.no_grad()``.
+
 The arithmetic runs in ``libretopk.so`` (``include/retopk.h`` states it); ``_paged.so``
 (``csrc/paged_binding.cpp``) checks the tensors and passes pointers.  Work is enqueued on the current stream of the tensors' device; nothing
 is kept between calls, so calls on several streams and captured graphs do not share anything here.
@@ -66,6 +69,26 @@ def _binding():
     return _module
 
 
+class _Rotation(torch.autograd.Function):
+    """The rotation of one or two tensors; its backward pass is the transposed one."""
+
+    @staticmethod
+    def forward(ctx, rope, inverse, positions, *tensors):
+        ctx.rope, ctx.inverse = rope, inverse
+        ctx.save_for_backward(positions)
+        out = rope._call(rope.h, rope.d, tensors[0], tensors[1] if len(tensors) > 1 else None, positions, None, None, inverse)
+        return out[:len(tensors)]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        wanted = [i for i in range(len(grads)) if ctx.needs_input_grad[3 + i]]
+        turned = ctx.rope._rotate([grads[i].contiguous() for i in wanted], ctx.saved_tensors[0], not ctx.inverse)
+        out = [None] * len(grads)
+        for i, g in zip(wanted, turned):
+            out[i] = g
+        return (None, None, None, *out)
+
+
 class Rope:
     """Rotary positions of one model (wraps a ``retopk_rope*``; host memory only, any device).
 
@@ -104,12 +127,24 @@ class Rope:
         return list(w), float(a.value)
 
     def apply(self, x, positions, out=None, inverse=False):
-        """Rotate x [tokens, heads, d] at int32 ``positions``; ``out`` may be x itself."""
-        return self._call(self.h, self.d, x, None, positions, out, None, inverse)[0]
+        """Rotate x [tokens, heads, d] at int32 ``positions``; ``out`` may be x itself.
+
+        Differentiable (twice, too), but not into a given ``out``: that is refused for tensors that
+        require a gradient, unless under ``torch.no_grad()``.
+        """
+        r = self._call(self.h, self.d, x, None, positions, out, None, inverse)
+        return self._rotate([x], positions, inverse)[0] if r is None else r[0]
 
     def apply_pair(self, q, k, positions, q_out=None, k_out=None, inverse=False):
-        """Rotate queries and keys in one launch.  ``inverse``: the transpose, i.e. the gradient."""
-        return self._call(self.h, self.d, q, k, positions, q_out, k_out, inverse)
+        """Rotate queries and keys in one launch.  ``inverse``: the transpose, i.e. the gradient.
+
+        Differentiable as ``apply`` is; the backward pass is one launch, too.
+        """
+        r = self._call(self.h, self.d, q, k, positions, q_out, k_out, inverse)
+        return self._rotate([q, k], positions, inverse) if r is None else r
+
+    def _rotate(self, tensors, positions, inverse):
+        return _Rotation.apply(self, bool(inverse), positions, *tensors)
 
 
 class KVPages:
