@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAStream.h>
 
 #include <map>
+#include <memory>
 #include <sstream>
 #include <tuple>
 
@@ -85,16 +86,25 @@ void no_gradient(const char* what, std::initializer_list<const at::Tensor*> all)
     if (wants_gradient(all)) throw Failure{g_error, text(what, " has no gradient, but a tensor requires one: call it under torch.no_grad(), or detach")};
 }
 
-// The pages of one cache, as KVPages made them out.
+// The pages of one cache, as KVPages made them out.  It owns the tensors that `pages` points into.
 struct Cache {
     retopk_pages_t pages;
     at::Device dev;
+    at::Tensor tensors[4];                   // k, v, and of 4-bit pages k_scale, v_scale
+    void* at[4];
+    int64_t numel[4];
     std::map<std::tuple<int64_t, int64_t, int64_t>, int64_t> needs;      // workspace bytes by (B, T, H_q)
 };
 constexpr const char* CACHE = "retopk_cache";
 Cache& cache_of(PyObject* o) {
     auto* c = static_cast<Cache*>(PyCapsule_GetPointer(o, CACHE));
     if (!c) throw python_error();
+    for (int i = 0; i < 4; ++i) {
+        const at::Tensor& t = c->tensors[i];
+        if (t.defined() && (t.data_ptr() != c->at[i] || t.numel() != c->numel[i] || !t.is_contiguous() ||
+                            t.storage().nbytes() < (size_t)(t.storage_offset() + t.numel()) * t.element_size()))
+            throw Failure{g_error, "a tensor of the cache was resized or given other memory: wrap the tensors again"};
+    }
     return *c;
 }
 retopk_pages_t pages_of(const Cache& c, int64_t B, PyObject* table) {
@@ -169,19 +179,30 @@ PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
-// cache_new(format, H_kv, d, page_size, n_pages, k, v, k_scale, v_scale, tensor of the device) -> capsule
+// cache_new(format, H_kv, d, page_size, n_pages, k, v, k_scale or None, v_scale or None) -> capsule
 PyObject* cache_new(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-    if (!arity(n_args, 10)) return nullptr;
+    if (!arity(n_args, 9)) return nullptr;
     return guarded([&]() -> PyObject* {
-        int64_t v[9];
-        for (int i = 0; i < 9; ++i) {
+        int64_t v[5];
+        for (int i = 0; i < 5; ++i) {
             v[i] = PyLong_AsLongLong(a[i]);
             if (v[i] == -1 && PyErr_Occurred()) throw python_error();
         }
-        auto* c = new Cache{{(int)v[0], (int)v[1], (int)v[2], (int)v[3], v[4], reinterpret_cast<void*>(v[5]), reinterpret_cast<void*>(v[6]),
-                             reinterpret_cast<void*>(v[7]), reinterpret_cast<void*>(v[8]), nullptr, 0},
-                            tensor(a[9], "k").device(), {}};
-        return PyCapsule_New(c, CACHE, [](PyObject* o) { delete static_cast<Cache*>(PyCapsule_GetPointer(o, CACHE)); });
+        auto c = std::unique_ptr<Cache>(new Cache{{(int)v[0], (int)v[1], (int)v[2], (int)v[3], v[4], nullptr, nullptr, nullptr, nullptr, nullptr, 0},
+                                                  tensor(a[5], "k").device(), {}, {}, {}, {}});
+        for (int i = 0; i < 4; ++i)
+            if (given(a[5 + i])) {
+                c->tensors[i] = tensor(a[5 + i], "k, v, k_scale, v_scale");
+                c->at[i] = c->tensors[i].data_ptr();
+                c->numel[i] = c->tensors[i].numel();
+            }
+        c->pages.k = c->at[0];
+        c->pages.v = c->at[1];
+        c->pages.k_scale = c->at[2];
+        c->pages.v_scale = c->at[3];
+        PyObject* capsule = PyCapsule_New(c.get(), CACHE, [](PyObject* o) { delete static_cast<Cache*>(PyCapsule_GetPointer(o, CACHE)); });
+        if (capsule) c.release();
+        return capsule;
     });
 }
 

@@ -190,11 +190,17 @@ class KVPages:
         for t in (k, v, k_scale, v_scale):
             if t is not None and (not t.is_cuda or t.device != k.device or not t.is_contiguous()):
                 raise TypeError("the tensors of a cache have to be contiguous on one CUDA device")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._tensors = (k, v, k_scale, v_scale)
         self.fmt = "q4" if q4 else ("bf16" if k.dtype == torch.bfloat16 else "fp16")
         self.device = k.device
-        self._cache = self._fast.cache_new(_FORMATS[self.fmt][0], self.H_kv, self.d, self.page_size, self.n_pages, k.data_ptr(),
-                                           v.data_ptr(), k_scale.data_ptr() if q4 else 0, v_scale.data_ptr() if q4 else 0, k)
+        self._cache = self._fast.cache_new(_FORMATS[self.fmt][0], self.H_kv, self.d, self.page_size, self.n_pages, k, v, k_scale, v_scale)
+
+    # Read only: the kernels use the memory that these tensors had when the cache was made, and every call
+    # checks that it is still theirs.
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
 
     def append(self, k_new, v_new, seq_lens, block_table=None, cu_new=None, rope=None, q=None, q_out=None):
         """Store new keys and values [tokens, H_kv, d], rotated by ``rope`` on the way.
