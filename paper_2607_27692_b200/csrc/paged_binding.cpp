@@ -86,6 +86,11 @@ void no_gradient(const char* what, std::initializer_list<const at::Tensor*> all)
     if (wants_gradient(all)) throw Failure{g_error, text(what, " has no gradient, but a tensor requires one: call it under torch.no_grad(), or detach")};
 }
 
+// Tells autograd that a tensor was written in place, so that a backward pass that saved it is refused.
+void written(const at::Tensor& t) {
+    if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The pages of one cache, as KVPages made them out.  It owns the tensors that `pages` points into.
 struct Cache {
     retopk_pages_t pages;
@@ -171,6 +176,8 @@ PyObject* rope_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (n > 0)
             check(retopk_rope_apply(rope, type_code(dt), n, pos, qi.p, qi.stride, qr.p, qr.stride, (int)H_q, ki.p, ki.stride, kr.p,
                                     kr.stride, (int)H_k, inverse, stream_of(dev)), "retopk_rope_apply");
+        if (given(a[5])) written(qo);
+        if (given(a[6])) written(ko);
         PyObject* out = PyTuple_New(2);
         PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(qo));
         PyObject* second = ko.defined() ? THPVariable_Wrap(ko) : Py_NewRef(Py_None);
@@ -221,7 +228,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const auto* rope = static_cast<const retopk_rope*>(PyLong_AsVoidPtr(a[6]));
         const retopk_pages_t pages = pages_of(c, B, a[4]);
         const at::Tensor none;
-        no_gradient("append", {&k, &v, given(a[8]) ? &tensor(a[8], "q") : &none, given(a[9]) ? &tensor(a[9], "q_out") : &none});
+        const at::Tensor* pg = c.tensors;
+        no_gradient("append", {&k, &v, &pg[0], &pg[1], &pg[2], &pg[3], given(a[8]) ? &tensor(a[8], "q") : &none, given(a[9]) ? &tensor(a[9], "q_out") : &none});
         const c10::cuda::CUDAGuard guard(c.dev);
         at::Tensor qo;
         Rows qi = {nullptr, 0}, qr = {nullptr, 0};
@@ -237,6 +245,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (n > 0)
             check(retopk_kv_append(&pages, (int)B, lens, cu, n, type_code(dt), kr.p, kr.stride, vr.p, vr.stride, rope, qi.p, qi.stride, qr.p,
                                    qr.stride, (int)H_q, stream_of(c.dev)), "retopk_kv_append");
+        for (const at::Tensor& t : c.tensors) written(t);
+        if (given(a[8]) && given(a[9])) written(qo);
         return qo.defined() ? THPVariable_Wrap(qo) : Py_NewRef(given(a[9]) ? a[9] : Py_None);
     });
 }
@@ -258,7 +268,7 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                 const at::Tensor& t = tensor(a[1 + i], "k_out, v_out");
                 if (t.device() != c.dev || t.scalar_type() != dt || t.sizes() != ref.sizes() || !t.is_contiguous())
                     type_error("k_out, v_out: contiguous ", dt, " ", ref.sizes(), " on ", c.dev);
-                no_gradient("gather", {&t});
+                no_gradient("gather", {&t, &c.tensors[0], &c.tensors[1]});
                 out[i] = t.data_ptr();
             }
         const int64_t B = ref.size(0);
@@ -268,6 +278,8 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (ref.numel() > 0) {
             const c10::cuda::CUDAGuard guard(c.dev);
             check(retopk_kv_gather(&pages, (int)B, lens, first, ref.size(2), type_code(dt), out[0], out[1], stream_of(c.dev)), "retopk_kv_gather");
+            for (int i = 0; i < 2; ++i)
+                if (given(a[1 + i])) written(tensor(a[1 + i], "k_out, v_out"));
         }
         return Py_NewRef(Py_None);
     });
@@ -291,7 +303,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const int32_t* lens = ints(a[2], "seq_lens", c.dev, B);
         const retopk_pages_t pages = pages_of(c, B, a[3]);
         const at::Tensor none;
-        no_gradient("attend", {&q, given(a[6]) ? &tensor(a[6], "out") : &none, given(a[7]) ? &tensor(a[7], "lse") : &none});
+        no_gradient("attend", {&q, &c.tensors[2], &c.tensors[3], given(a[6]) ? &tensor(a[6], "out") : &none, given(a[7]) ? &tensor(a[7], "lse") : &none});
         const double scale = given(a[4]) ? PyFloat_AsDouble(a[4]) : 1.0 / std::sqrt((double)d);
         const int64_t window = PyLong_AsLongLong(a[5]);
         if (PyErr_Occurred()) throw python_error();
@@ -321,6 +333,8 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
             const at::Tensor ws = empty({need}, q, at::kByte);
             check(retopk_q4_attention(&pages, (int)B, (int)T, (int)H_q, lens, type_code(q.scalar_type()), q.data_ptr(), q_stride, (float)scale,
                                       window, out.data_ptr(), lse, ws.data_ptr(), need, stream_of(c.dev)), "retopk_q4_attention");
+            if (given(a[6])) written(out);
+            if (given(a[7])) written(tensor(a[7], "lse"));
         }
         return THPVariable_Wrap(out);
     });

@@ -127,3 +127,56 @@ def test_a_captured_gradient(paged):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(got, rope.apply(up, pos, inverse=True))
+
+
+def test_tensors_written_in_place_are_marked(paged):
+    """A tensor that autograd has saved and a call then writes: the backward pass is refused, as after any operator of torch."""
+    d, H, page = 64, 2, 16
+    rope = paged.Rope(d)
+    pos, lens, table = ints([0, 1, 2]), ints([1, 1, 1]), ints([[0], [1], [2]])
+    w = torch.ones(1, device="cuda", dtype=BF, requires_grad=True)
+
+    def fresh(*shape, dtype=BF):
+        return torch.randn(*(shape or (3, H, d)), generator=gen(541), device="cuda").to(dtype)
+
+    k16, v16 = fresh(3, H, page, d), fresh(3, H, page, d)
+    half, q4 = paged.KVPages.wrap(k16, v16), paged.KVPages(3, H, page, d, "q4")
+    x = fresh()
+    a, b, c, e, f, g, h, lse = (fresh() for _ in range(8))
+    rows = [fresh(3, H, 1, d) for _ in "kv"]
+    lse = fresh(3, H, dtype=torch.float32)
+    writes = [
+        ([a], lambda: rope.apply(a, pos, out=a)), ([b], lambda: rope.apply(x, pos, out=b)),
+        ([c, e], lambda: rope.apply_pair(x, x, pos, q_out=c, k_out=e)), ([f, k16, v16], lambda: half.append(x, x, lens, table, rope=rope, q=x, q_out=f)),
+        ([k16[1:], v16.view(-1)], lambda: half.append(x, x, lens, table)), ([q4.k_scale, q4.v_scale], lambda: q4.append(x, x, lens, table)),
+        (rows, lambda: q4.gather(*rows, lens, table)), ([g, lse], lambda: q4.attend(x, lens, table, out=g, lse=lse)),
+        ([h], lambda: q4.attend(h, lens, table, out=h)),
+    ]
+    for tensors, call in writes:
+        results = [(t * w.to(t.dtype)).sum() for t in tensors]           # the product saves t
+        kept = (x * w).sum()
+        before = [t._version for t in tensors]
+        call()
+        assert all(t._version > n for t, n in zip(tensors, before))
+        for r in results:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                r.backward()
+        kept.backward()                                                  # inputs are not marked
+    codes = [q4.k._version, q4.v._version]
+    q4.append(x, x, lens, table)
+    assert [q4.k._version, q4.v._version] > codes
+    # tensors without a version counter are written all the same
+    with torch.inference_mode():
+        cache = paged.KVPages(3, H, page, d, "bf16")
+        y = fresh()
+    cache.append(x, x, lens, table, rope=rope, q=x, q_out=y)
+    rope.apply(y, pos, out=y)
+    assert torch.equal(cache.v[0, :, 0], x[0])
+    # a cache whose tensors require a gradient
+    leaf = paged.KVPages.wrap(k16.detach().clone().requires_grad_(), v16.detach().clone())
+    with pytest.raises(paged._rt.RetopkError, match="no_grad"):
+        leaf.append(x, x, lens, table)
+    with pytest.raises(paged._rt.RetopkError, match="no_grad"):
+        leaf.gather(*rows, lens, table)
+    with torch.no_grad():
+        leaf.append(x, x, lens, table)
