@@ -421,7 +421,9 @@ typedef struct {
  * Rows of k_new from cu_new[B] on, and tokens whose position is negative (an idle sequence of length
  * 0), are left out, their q_out rows too.  A key whose page is not in 0..n_pages-1 or whose position is
  * beyond the block table is not stored.  All other rows of the cache stay as they are.  Two new
- * tokens that share a row of a page leave that row unspecified.
+ * tokens that share a row of a page leave that row unspecified.  q_out may be q (same pointer and stride);
+ * other overlaps of q_out with the inputs, and any of the pages' tensors with each other or with q, q_out,
+ * k_new and v_new, are EINVAL.
  * Limits: B, H_kv, H_q <= 65535; EUNSUPPORTED beyond.
  */
 int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* cu_new, int64_t n_new,
@@ -435,7 +437,8 @@ int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * those whose page is out of range, are left as they were.  Either output may be NULL.
  * dtype: any for 4-bit pages (fp32 holds s * n + m with one rounding), the pages' own type or
  * RETOPK_FP32 for 16-bit ones.  With max_rows = max_seq_len this fills the cache of
- * retopk_decode_step from pages.  Limits: B, H_kv <= 65535.
+ * retopk_decode_step from pages.  Outputs that overlap each other or the pages are EINVAL.  Limits: B, H_kv
+ * <= 65535.
  */
 int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens, const int32_t* first, int64_t max_rows,
                      int dtype, void* k_out, void* v_out, void* stream);
@@ -456,6 +459,8 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * with the codes as a sum of two bf16 parts (2^-17).  Queries enter exactly but for 2^-23 of the larger
  * element of a pair of channels and 2^-35 of the row's largest; elements of q below 2^117.  Results are
  * bit-reproducible.
+ * out may be q where q is contiguous; other overlaps of out, lse and workspace with each other, q or the pages
+ * are EINVAL.
  * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant
  * before and after; calls that may overlap on the GPU (two streams, two captured graphs) need one each.
  * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096, at most 2^20 keys of a sequence (max_pages *

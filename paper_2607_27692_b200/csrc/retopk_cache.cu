@@ -47,6 +47,27 @@ bool in_place_or_apart(const Strided& in, const Strided& out, long long n, int d
     return (in.p == out.p && in.stride == out.stride) || rows_apart(in, out, n, d);
 }
 
+// A stretch of memory; and whether one that is written keeps clear of others.
+struct Memory { const void* p; uint64_t bytes; };
+bool apart(const Memory& x, const Memory& y) {
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x.p), y0 = reinterpret_cast<uintptr_t>(y.p);
+    return !x.p || !y.p || x0 + x.bytes <= y0 || y0 + y.bytes <= x0;
+}
+template <size_t N> bool all_apart(const Memory& x, const Memory (&others)[N]) {
+    for (const Memory& y : others)
+        if (!apart(x, y)) return false;
+    return true;
+}
+Memory memory_of(const Strided& x, long long n, int d) { return {x.p, ((uint64_t)(n - 1) * x.stride + (uint64_t)x.heads * d) * 2}; }
+void memory_of(const retopk_pages_t* p, Memory (&m)[4]) {
+    const bool q4 = p->format == RETOPK_PAGES_Q4;
+    const uint64_t rows = (uint64_t)p->n_pages * p->H_kv * p->page_size;
+    m[0] = {p->k, rows * (q4 ? p->d / 2 : p->d * 2)};
+    m[1] = {p->v, m[0].bytes};
+    m[2] = {q4 ? p->k_scale : nullptr, rows * (p->d / GROUP * 4)};
+    m[3] = {q4 ? p->v_scale : nullptr, m[2].bytes};
+}
+
 int check_pages(const retopk_pages_t* p, int B) {
     if (!p || B < 1) return RETOPK_EINVAL;
     if (p->format < RETOPK_PAGES_BF16 || p->format > RETOPK_PAGES_Q4) return RETOPK_EINVAL;
@@ -321,6 +342,13 @@ int retopk_kv_append(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     if (n_new == 0) return RETOPK_OK;
     const Strided qi = {q, q_stride, H_q}, qo = {q_out, q_out_stride, H_q}, ki = {k_new, k_stride, H}, vi = {v_new, v_stride, H};
     if (q && !(in_place_or_apart(qi, qo, n_new, d) && rows_apart(qo, ki, n_new, d) && rows_apart(qo, vi, n_new, d))) return RETOPK_EINVAL;
+    Memory pg[4];
+    memory_of(pages, pg);
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j)
+            if (!apart(pg[i], pg[j])) return RETOPK_EINVAL;
+    if (!all_apart(memory_of(ki, n_new, d), pg) || !all_apart(memory_of(vi, n_new, d), pg)) return RETOPK_EINVAL;
+    if (q && (!all_apart(memory_of(qi, n_new, d), pg) || !all_apart(memory_of(qo, n_new, d), pg))) return RETOPK_EINVAL;
     int num_sms = 0;
     rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
@@ -354,6 +382,11 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
     if (!q4 && dtype != RETOPK_FP32 && (pages->format == RETOPK_PAGES_BF16) != (dtype == RETOPK_BF16)) return RETOPK_EINVAL;
     if (B > 65535 || pages->H_kv > 65535) return RETOPK_EUNSUPPORTED;
     if (max_rows == 0) return RETOPK_OK;
+    Memory pg[4];
+    memory_of(pages, pg);
+    const uint64_t out_bytes = (uint64_t)B * pages->H_kv * max_rows * pages->d * (dtype == RETOPK_FP32 ? 4 : 2);
+    const Memory ko = {k_out, out_bytes}, vo = {v_out, out_bytes};
+    if (!all_apart(ko, pg) || !all_apart(vo, pg) || !apart(ko, vo)) return RETOPK_EINVAL;
     GatherArgs a;
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
@@ -399,6 +432,13 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
     if (a.pg.capacity > MAX_KEYS || pages->n_pages > 0xfffffffell / ((long long)pages->H_kv * pages->page_size)) return RETOPK_EUNSUPPORTED;
+    const long long n = (long long)B * T;
+    const Strided qi = {q, q_stride, H_q}, qo = {out, (long long)H_q * pages->d, H_q};
+    Memory pg[4];
+    memory_of(pages, pg);
+    const Memory out_m = memory_of(qo, n, pages->d), lse_m = {lse, (uint64_t)n * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
+    if (!in_place_or_apart(qi, qo, n, pages->d) || !all_apart(out_m, pg) || !all_apart(lse_m, pg) || !all_apart(ws_m, pg)) return RETOPK_EINVAL;
+    if (!all_apart(lse_m, {out_m, memory_of(qi, n, pages->d), ws_m}) || !all_apart(ws_m, {out_m, memory_of(qi, n, pages->d)})) return RETOPK_EINVAL;
     int num_sms = 0;
     rc = device_sms(&num_sms);
     if (rc != RETOPK_OK) return rc;
