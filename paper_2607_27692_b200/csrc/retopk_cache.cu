@@ -448,7 +448,7 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
     a.lse = lse;
     a.part = static_cast<float*>(workspace);
     a.q_stride = q_stride;
-    a.window = window;
+    a.window = window <= MAX_KEYS ? window : 0;         // a wider one leaves no key out (nor may sums with it overflow)
     a.two16 = 1u << 16;
     a.scale_log2 = (float)((double)scale * 1.44269504088896340736);
     a.B = B; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv;

@@ -61,3 +61,16 @@ def test_lengths_that_the_block_table_cannot_hold(paged, G, T):
     out = cache.attend(q, ints([cap, cap + 1, 2 ** 31 - 1, -2 ** 31]), table, lse=lse)
     assert torch.equal(out[0], want[0]) and torch.equal(lse[0], fits[0]) and torch.isfinite(lse[0]).all()
     assert (out[1:] == 0).all() and (lse[1:] == -math.inf).all()
+
+
+@pytest.mark.parametrize("T", [1, 16])
+def test_windows_wider_than_any_sequence(paged, T):
+    """Up to the largest 64-bit number, with sequences shorter than the tokens: as without a window."""
+    lens, d = [0, 1, 5, T, 300], 64
+    cache, table = filled(paged, lens, 16, 1, d, 421)
+    q = torch.randn(len(lens), T, 2, d, generator=gen(422), device="cuda").to(BF)
+    lse = torch.empty(q.shape[:-1], device="cuda")
+    want = cache.attend(q, ints(lens), table, lse=lse)
+    for window in (1 << 20, (1 << 20) + 1, (1 << 31) - 1, 1 << 31, 1 << 62, (1 << 63) - 1):
+        got_lse = torch.empty_like(lse)
+        assert torch.equal(cache.attend(q, ints(lens), table, window=window, lse=got_lse), want) and torch.equal(got_lse, lse)
