@@ -195,12 +195,20 @@ class KVPages:
         self.device = k.device
         self._cache = self._fast.cache_new(_FORMATS[self.fmt][0], self.H_kv, self.d, self.page_size, self.n_pages, k, v, k_scale, v_scale)
 
-    # Read only: the kernels use the memory that these tensors had when the cache was made, and every call
-    # checks that it is still theirs.
-    k = property(lambda self: self._tensors[0])
-    v = property(lambda self: self._tensors[1])
-    k_scale = property(lambda self: self._tensors[2])
-    v_scale = property(lambda self: self._tensors[3])
+    def _part(i):
+        def get(self):
+            return self._tensors[i]
+
+        def set(self, value):
+            if value is not self._tensors[i]:       # cache.k *= 2 assigns the tensor that is there
+                raise AttributeError("a cache keeps its tensors: write into them, or wrap others")
+
+        return property(get, set)
+
+    # The kernels use the memory that these tensors had when the cache was made; every call checks that it is
+    # still theirs.
+    k, v, k_scale, v_scale = _part(0), _part(1), _part(2), _part(3)
+    del _part
 
     def append(self, k_new, v_new, seq_lens, block_table=None, cu_new=None, rope=None, q=None, q_out=None):
         """Store new keys and values [tokens, H_kv, d], rotated by ``rope`` on the way.

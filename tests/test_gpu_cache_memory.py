@@ -105,3 +105,14 @@ def test_outputs_on_inputs_are_refused(paged):
             q4.attend(q, ints([30, 30]), table, out=out)
     want = q4.attend(wide[:2].clone(), ints([30, 30]), table)
     assert torch.equal(q4.attend(wide[:2], ints([30, 30]), table, out=wide[2:4]), want)
+
+
+def test_in_place_operators_on_the_attributes(paged):
+    """cache.k |= 1 assigns the same tensor: fine; another one is refused."""
+    cache = paged.KVPages(1, 1, 16, 64, "q4")
+    cache.k |= 0x11
+    cache.v_scale += 1
+    cache.k = cache.k
+    assert (cache.k == 0x11).all() and (cache.v_scale == 1).all()
+    with pytest.raises(AttributeError):
+        cache.k = cache.k | 1
