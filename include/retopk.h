@@ -456,9 +456,13 @@ int retopk_kv_gather(const retopk_pages_t* pages, int B, const int32_t* seq_lens
  * in every row that sees it.  What rows hold that a token does not see (behind seq_lens, before the window,
  * of later draft tokens), NaN patterns among it, has no influence on it.
  * Scores, weights, sums and outputs are held in fp32 and rounded once to dtype; weights enter the product
- * with the codes as a sum of two bf16 parts (2^-17).  Queries enter exactly but for 2^-23 of the larger
- * element of a pair of channels and 2^-35 of the row's largest; elements of q below 2^117.  Results are
+ * with the codes as a sum of two bf16 parts, off by up to 2^-16 of the weight, and the tensor cores cut the
+ * sums of up to 12 tiles of 16 keys off at 2^-23 of them (longer sums are rounded).  Queries enter exactly but
+ * for 2^-23 of the larger element of a pair of channels and 2^-35 of the row's largest.  Results are
  * bit-reproducible.
+ * Range: elements of q below 2^117; value steps of 0 or 2^-57 to 2^55, value minima below 2^36 (all that fp16
+ * keys and values can give).  Beyond it sums may leave the fp32 range, which shows as NaN or infinity; smaller
+ * steps lose low bits of their codes, all of them below 2^-81, and the minimum stays.
  * out may be q where q is contiguous; other overlaps of out, lse and workspace with each other, q or the pages
  * are EINVAL.
  * workspace: at least retopk_q4_attention_workspace() bytes, 16-byte aligned, contents irrelevant

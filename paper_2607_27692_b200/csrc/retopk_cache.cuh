@@ -691,7 +691,9 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
     return x;
 }
 // Weights carry 2^64 through the reference of their exponentials: it keeps their products with the
-// subnormals in the middle of the fp32 range.
+// subnormals in the middle of the fp32 range.  With steps s, a weight (up to 2^72) times s has to be finite
+// (s < 2^55) and 2^64 s 2^-133 normal (s >= 2^-57); 2^20 weights of 2^72 times minima are below 2^128 for
+// minima below 2^36.
 constexpr float TWO64 = 18446744073709551616.f, TWO69 = 32.f * TWO64;     // 2^-133 * 2^64 = 1 / TWO69
 
 // One warp's running state over the keys that it has seen.
@@ -707,7 +709,7 @@ struct Q4State {
 //     q . k = sum_g ( s_g (q . n)_g + m_g (sum of q)_g )
 // so the codes go into the tensor core as they are and step and minimum are applied to the 16 x 8
 // result.  The same for values: sum_j p_j v_j = sum_j (p_j s_j) n_j + sum_j p_j m_j, the weight p_j s_j
-// entering as two bf16 parts (hi + lo, 2^-17 relative).  Keys are the M side of both products (16 keys
+// entering as two bf16 parts (hi cut off, lo rounded: within 2^-16).  Keys are the M side of both products (16 keys
 // or 16 channels), the columns the N side: with 4 columns the two parts of a weight fill the 8 columns
 // of one product, so the second part is free.
 //
