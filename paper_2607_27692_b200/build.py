@@ -1,8 +1,9 @@
-"""Compile in-tree: the CUDA library ``csrc/*.cu`` -> ``libretopk.so`` (sm_100a) and its torch binding
-``csrc/paged_binding.cpp`` -> ``_paged.so``."""
+"""Compile in-tree: the CUDA library ``csrc/*.cu`` -> ``libretopk.so`` (sm_100a) and, where torch is installed,
+its torch binding ``csrc/paged_binding.cpp`` -> ``_paged.so``."""
 from __future__ import annotations
 
 import fcntl
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -33,8 +34,13 @@ def is_stale() -> bool:
     return _older(LIB_PATH, _sources())
 
 
+def has_torch() -> bool:
+    return importlib.util.find_spec("torch") is not None
+
+
 def binding_is_stale() -> bool:
-    return _older(BINDING_PATH, [BINDING_SRC, _sources()[-1]])
+    """False, too, where there is no torch to bind to."""
+    return has_torch() and _older(BINDING_PATH, [BINDING_SRC, _sources()[-1]])
 
 
 def find_nvcc() -> str:
@@ -80,7 +86,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
                 cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + units
                 subprocess.run(cmd, check=True)
                 os.replace(tmp, LIB_PATH)
-            if force or binding_is_stale():
+            if has_torch() and (force or binding_is_stale()):
                 _build_binding()
         finally:
             fcntl.flock(lock, fcntl.LOCK_UN)
