@@ -7,6 +7,7 @@ import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -14,6 +15,7 @@ SRC_DIR = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libretopk.so")
 BINDING_SRC = os.path.join(SRC_DIR, "paged_binding.cpp")
 BINDING_PATH = os.path.join(_PKG, "_paged.so")
+BINDING_STAMP = BINDING_PATH + ".stamp"      # what the binding was compiled against
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]
 
@@ -38,9 +40,22 @@ def has_torch() -> bool:
     return importlib.util.find_spec("torch") is not None
 
 
+def binding_target() -> str:
+    """Python's and torch's binary interface: a binding of another one does not load, or worse."""
+    import torch
+    return f"{sys.implementation.cache_tag} torch {torch.__version__} cxx11 {int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+
+
+def _stamp() -> str:
+    if not os.path.exists(BINDING_STAMP):
+        return ""
+    with open(BINDING_STAMP) as f:
+        return f.read().strip()
+
+
 def binding_is_stale() -> bool:
     """False, too, where there is no torch to bind to."""
-    return has_torch() and _older(BINDING_PATH, [BINDING_SRC, _sources()[-1]])
+    return has_torch() and (_older(BINDING_PATH, [BINDING_SRC, _sources()[-1]]) or _stamp() != binding_target())
 
 
 def find_nvcc() -> str:
@@ -61,11 +76,17 @@ def _build_binding():
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     tmp = f"{BINDING_PATH}.{os.getpid()}.tmp"
-    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DBUILT_FOR="{binding_target()}"']
     cmd += ["-I" + d for d in include] + [BINDING_SRC, "-o", tmp, "-L" + os.path.join(root, "lib"), "-L" + _PKG]
     cmd += ["-l:libretopk.so", "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
     subprocess.run(cmd, check=True)
+    if os.path.exists(BINDING_STAMP):
+        os.remove(BINDING_STAMP)
     os.replace(tmp, BINDING_PATH)
+    with open(tmp, "w") as f:
+        f.write(binding_target() + "\n")
+    os.replace(tmp, BINDING_STAMP)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -352,4 +352,8 @@ PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "_paged", "Calls around the KV cach
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged() { return PyModule_Create(&MODULE); }
+PyMODINIT_FUNC PyInit__paged() {
+    PyObject* m = PyModule_Create(&MODULE);
+    if (m && PyModule_AddStringConstant(m, "built_for", BUILT_FOR) != 0) Py_CLEAR(m);      // compared by paged.py
+    return m;
+}

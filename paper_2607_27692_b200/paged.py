@@ -63,7 +63,13 @@ def _binding():
         _rt.load()
         if not os.path.exists(_build.BINDING_PATH):
             raise _rt.RetopkError(f"{_build.BINDING_PATH} is missing: build it with `python -m paper_2607_27692_b200.build`")
-        module = importlib.import_module("._paged", __package__)
+        again = "build it again with `python -m paper_2607_27692_b200.build`"
+        try:
+            module = importlib.import_module("._paged", __package__)
+        except ImportError as e:
+            raise _rt.RetopkError(f"{_build.BINDING_PATH} does not load ({e}): {again}") from e
+        if module.built_for != _build.binding_target():
+            raise _rt.RetopkError(f"{_build.BINDING_PATH} was built for {module.built_for}, this is {_build.binding_target()}: {again}")
         module.set_error(_rt.RetopkError)
         _module = module
     return _module
