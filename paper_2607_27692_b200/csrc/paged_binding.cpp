@@ -213,9 +213,9 @@ PyObject* cache_new(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
-// append(cache, k_new, v_new, seq_lens, block_table, cu_new, rope handle or 0, rope's d, q, q_out) -> q_out
+// append(cache, k_new, v_new, seq_lens, block_table, cu_new, rope handle or 0, q, q_out) -> q_out
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-    if (!arity(n_args, 10)) return nullptr;
+    if (!arity(n_args, 9)) return nullptr;
     return guarded([&]() -> PyObject* {
         const Cache& c = cache_of(a[0]);
         const at::Tensor &k = half_rows(a[1], "k_new"), &v = half_rows(a[2], "v_new");
@@ -229,25 +229,25 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const retopk_pages_t pages = pages_of(c, B, a[4]);
         const at::Tensor none;
         const at::Tensor* pg = c.tensors;
-        no_gradient("append", {&k, &v, &pg[0], &pg[1], &pg[2], &pg[3], given(a[8]) ? &tensor(a[8], "q") : &none, given(a[9]) ? &tensor(a[9], "q_out") : &none});
+        no_gradient("append", {&k, &v, &pg[0], &pg[1], &pg[2], &pg[3], given(a[7]) ? &tensor(a[7], "q") : &none, given(a[8]) ? &tensor(a[8], "q_out") : &none});
         const c10::cuda::CUDAGuard guard(c.dev);
         at::Tensor qo;
         Rows qi = {nullptr, 0}, qr = {nullptr, 0};
         int64_t H_q = 0;
-        if (given(a[8])) {
+        if (given(a[7])) {
             if (!rope) value_error("q is rotated with the keys: pass rope");
-            const at::Tensor& q = half_rows(a[8], "q");
+            const at::Tensor& q = half_rows(a[7], "q");
             H_q = q.size(1);
             qi = rows(q, "q", c.dev, dt, n, H_q, d);
-            qo = given(a[9]) ? tensor(a[9], "q_out") : empty({n, H_q, d}, q, dt);
+            qo = given(a[8]) ? tensor(a[8], "q_out") : empty({n, H_q, d}, q, dt);
             qr = rows(qo, "q_out", c.dev, dt, n, H_q, d);
         }
         if (n > 0)
             check(retopk_kv_append(&pages, (int)B, lens, cu, n, type_code(dt), kr.p, kr.stride, vr.p, vr.stride, rope, qi.p, qi.stride, qr.p,
                                    qr.stride, (int)H_q, stream_of(c.dev)), "retopk_kv_append");
         for (const at::Tensor& t : c.tensors) written(t);
-        if (given(a[8]) && given(a[9])) written(qo);
-        return qo.defined() ? THPVariable_Wrap(qo) : Py_NewRef(given(a[9]) ? a[9] : Py_None);
+        if (given(a[7]) && given(a[8])) written(qo);
+        return qo.defined() ? THPVariable_Wrap(qo) : Py_NewRef(given(a[8]) ? a[8] : Py_None);
     });
 }
 

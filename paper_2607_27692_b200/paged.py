@@ -221,16 +221,17 @@ class KVPages:
 
         ``seq_lens`` int32 [B] counts each sequence's keys including the new ones.  Sequence b's new
         tokens are rows cu_new[b]:cu_new[b+1] (int32 [B + 1]); without ``cu_new`` every sequence has
-        the same number.  With ``q`` the queries are rotated in the same launch and returned; rows of
-        ``q_out`` that belong to no token are left as they were.
+        the same number.  With ``q`` the queries are rotated in the same launch and returned.  Rows that
+        belong to no token (of an idle sequence, or behind cu_new[B]) are not written: they stay as they
+        were in ``q_out``, and without ``q_out`` they are uninitialised memory.
         """
         if rope is None:
-            return self._fast.append(self._cache, k_new, v_new, seq_lens, block_table, cu_new, 0, 0, q, q_out)
+            return self._fast.append(self._cache, k_new, v_new, seq_lens, block_table, cu_new, 0, q, q_out)
         if not rope.h:
             raise _rt.RetopkError("the rotation was closed")
         if rope.d != self.d:
             raise ValueError(f"the rotation is of heads of {rope.d}, the cache of {self.d}")
-        return self._fast.append(self._cache, k_new, v_new, seq_lens, block_table, cu_new, rope.h, rope.d, q, q_out)
+        return self._fast.append(self._cache, k_new, v_new, seq_lens, block_table, cu_new, rope.h, q, q_out)
 
     def gather(self, k_out, v_out, seq_lens, block_table=None, first=None):
         """Read rows back into k_out / v_out [B, H_kv, rows, d] (either may be None).
