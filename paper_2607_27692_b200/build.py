@@ -1,9 +1,8 @@
-"""Compile in-tree: the CUDA library ``csrc/*.cu`` -> ``libretopk.so`` (sm_100a) and, where torch is installed,
+"""Compile in-tree: the CUDA library ``csrc/*.cu`` -> ``libretopk.so`` (sm_100a) and, where torch for CUDA is installed,
 its torch binding ``csrc/paged_binding.cpp`` -> ``_paged.so``."""
 from __future__ import annotations
 
 import fcntl
-import importlib.util
 import os
 import shutil
 import subprocess
@@ -37,7 +36,12 @@ def is_stale() -> bool:
 
 
 def has_torch() -> bool:
-    return importlib.util.find_spec("torch") is not None
+    """Whether there is a torch to bind to: one for CUDA."""
+    try:
+        import torch
+    except ImportError:
+        return False
+    return torch.version.cuda is not None
 
 
 def binding_target() -> str:

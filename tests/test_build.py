@@ -8,13 +8,14 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-def test_the_library_needs_no_torch(tmp_path):
-    """The C interface is built without torch; its binding is left out."""
+@pytest.mark.parametrize("torch", ["None", "types.SimpleNamespace(version=types.SimpleNamespace(cuda=None), __file__='', __version__='2')"])
+def test_the_library_needs_no_torch(tmp_path, torch):
+    """The C interface is built without torch, and beside one without CUDA; its binding is left out."""
     from paper_2607_27692_b200 import build
     build.build()
     code = f"""
-import sys
-sys.modules["torch"] = None                     # as if it were not installed
+import sys, types
+sys.modules["torch"] = {torch}                  # None: as if it were not installed
 from paper_2607_27692_b200 import build
 build.BINDING_PATH = {str(tmp_path / "_paged.so")!r}
 build.BINDING_STAMP = build.BINDING_PATH + ".stamp"
