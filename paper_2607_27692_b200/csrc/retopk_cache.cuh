@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, ROWS_CTAS) rows_kernel(const __g
     // Groups of RPW rows of q, then of k and v one after the other (a group may end in k and begin in v),
     // are dealt out in turn to the warps of a token, which take PER of them at a time, the next ones on
     // their way.
-    // (quantising twice over is too much code: 40 against 31 us, 6K tokens; so are partners in other lanes)
+    // (quantising twice over is too much code: 16 against 14.3 us, 5938 tokens of 16 + 4 + 4 heads of 64; so are
+    // partners in other lanes)
     constexpr int PER = DEST == DEST_PAGES4 || ROT == ROT_OTHER ? 1 : 2;
     const int step = per_tok * a.units;
     const uint16_t *const q_src = a.q + tok * a.q_stride, *const k_src = a.k + tok * a.k_stride, *const v_src = a.v + tok * a.v_stride;
@@ -577,9 +578,12 @@ constexpr int Q4_FLUSH = 4;
 __host__ __device__ constexpr int q4_smem_bytes(int d, int shape) { return q4_ring_bytes(d, shape) + Q4_WARPS * q4_cols(shape) * d * 4; }
 
 // Few warps with many registers: three tiles at a time keep the ALU and the tensor cores busier than
-// more warps with one or two tiles would (4 x 128K keys: 107 us; 16 warps an SM with two tiles 112, 20
-// with one 130).  16 columns take what two CTAs leave: at d = 128 they need it, at d = 64 four draft tokens
-// over 8K keys take 20.8 us with two CTAs and 22.9 with three.
+// more warps with one or two tiles would (4 x 131584 keys, graph replays: 4 heads a group 107..115 us, 8 heads 137;
+// 16 warps an SM with two tiles 113..120 and 146; 20 with one 137 and 171).  16 columns take what two CTAs
+// leave.  At d = 128 a third does not fit (86 KB of shared memory each).  At d = 64 it would, in fewer registers,
+// and is better for long shares but not for short ones: 16 heads a group, 4 x 131584 keys 127 us with two and 124
+// with three; four draft tokens, 4 x 64K keys 72 and 70; 8 x 8K 28.7 and 28.7; a window of 8K 22.6 and 24.6;
+// three draft tokens of 8 heads, 8 x 8K 43 and 45.
 __host__ __device__ constexpr int q4_ctas_per_sm(int shape) { return shape == COLS_16 ? 2 : 3; }
 
 struct Q4Args {
@@ -649,11 +653,12 @@ __device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint3
 // other operand (keys) or once at the end (values).
 //
 // What bounds the kernel short of HBM is instructions, on the ALU most of all, where masks, shifts and byte
-// permutations go, and the power that they take (4 x 128K keys back to back: 1000 W at 1.6 GHz).  Measured
-// there, with n0, 16 n1 and a shift for the upper bytes of keys and values: 132 us; that shift as a product
-// 142 us (its two issue slots cost more); e4m3 operands for the keys 143 us (mma converts them to fp16, on
-// the ALU); queries as whole numbers against 8-bit integer operands 6 us less than this form, but then they
-// hold 2^-15 of a row's largest element only.
+// permutations go, and the power that they take: 4 x 131584 keys take 107 us in short runs, 88% of the copy rate,
+// and 118..125 us back to back, where the card is at 1000 W and 1.6 GHz.  Measured when this form was chosen, against
+// its 121 us: n0, 16 n1 and a shift for the upper bytes of keys and values 132 us; that shift as a product 142 us
+// (its two issue slots cost more); e4m3 operands for the keys 143 us (mma converts them to fp16, on the ALU).
+// Queries as whole numbers against 8-bit integer operands take 6% less than this form, but hold only 2^-15 of a
+// row's largest element.
 __device__ __forceinline__ void code_bytes(uint32_t x, uint32_t (&c)[4]) {
     c[0] = x & 0x000f000fu;                      // codes (0,4)
     c[1] = __byte_perm(x, 0u, 0x4240);           // bytes 0 and 2: (0,4) + 16 (1,5)
