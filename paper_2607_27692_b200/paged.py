@@ -109,6 +109,8 @@ class Rope:
             raise ValueError(f"scaling: one of {list(_SCALINGS)}, got {scaling!r}")
         self.lib, self._call = _rt.load(), _binding().rope_apply
         self.d, self.rot_dim = d, d if rot_dim is None else rot_dim
+        self._config = (d, rot_dim, base, interleaved, scaling, factor, original_len, low_freq_factor, high_freq_factor, beta_fast,
+                        beta_slow, attn_factor)
         cfg = _RopeConfig(d, self.rot_dim, int(bool(interleaved)), _SCALINGS[scaling], base, factor, original_len,
                           low_freq_factor, high_freq_factor, beta_fast, beta_slow, attn_factor)
         h = _vp()
@@ -125,6 +127,12 @@ class Rope:
             self.close()
         except Exception:
             pass
+
+    def __reduce__(self):
+        """Copies (and pickles) are made from the settings: each has a handle of its own to destroy."""
+        if not self.h:
+            raise _rt.RetopkError("the rotation was closed")
+        return type(self), self._config
 
     def frequencies(self):
         """Radians per position of each pair (list), and the factor on cosine and sine."""
