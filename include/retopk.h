@@ -354,7 +354,7 @@ enum { RETOPK_BF16 = 0, RETOPK_FP16 = 1, RETOPK_FP32 = 2 };
  *   RETOPK_ROPE_YARN    w_i / factor for pairs that turn fewer than beta_slow times over
  *                       original_len, w_i above beta_fast turns, a linear ramp over the pair index
  *                       between; a = 0.1 ln(factor) + 1
- * attn_factor > 0 replaces a.  Zero in low_freq_factor, high_freq_factor, beta_fast or beta_slow
+ * attn_factor > 0 (up to 1e30) replaces a.  Zero in low_freq_factor, high_freq_factor, beta_fast or beta_slow
  * stands for 1, 4, 32 and 1.  Angle and rotation are computed in 64 bits (at position 1 Mi an
  * angle in 32 bits is 0.06 rad off) or, the rotation, to within 2^-23 of that; rounded once to the tensor's
  * type.  Infinities and NaN in a pair go through the formula as IEEE arithmetic takes them; finite elements

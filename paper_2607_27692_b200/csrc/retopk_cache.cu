@@ -225,7 +225,7 @@ int retopk_rope_create(retopk_rope** rope, const retopk_rope_config_t* c) {
     if (c->rot_dim < 2 || c->rot_dim % 2 != 0 || c->rot_dim > c->d) return RETOPK_EINVAL;
     if (c->layout != RETOPK_ROPE_HALF && c->layout != RETOPK_ROPE_INTERLEAVED) return RETOPK_EINVAL;
     if (c->scaling < RETOPK_ROPE_PLAIN || c->scaling > RETOPK_ROPE_YARN) return RETOPK_EINVAL;
-    if (!(c->base > 1.0) || !isfinite(c->base) || !isfinite(c->attn_factor) || c->attn_factor < 0.0) return RETOPK_EINVAL;
+    if (!(c->base > 1.0) || !isfinite(c->base) || !(c->attn_factor >= 0.0) || c->attn_factor > 1e30) return RETOPK_EINVAL;
     if (c->scaling != RETOPK_ROPE_PLAIN && (!(c->factor >= 1.0) || !isfinite(c->factor))) return RETOPK_EINVAL;
     if (c->scaling == RETOPK_ROPE_NTK && c->rot_dim == 2) return RETOPK_EINVAL;
     const double lowf = c->low_freq_factor != 0.0 ? c->low_freq_factor : 1.0;

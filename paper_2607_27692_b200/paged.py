@@ -254,6 +254,8 @@ class KVPages:
 
         q [B, H_q, d] (one token) or [B, T, H_q, d]; the result has q's shape and type.  ``scale``
         defaults to d ** -0.5; ``window`` > 0 limits a token to its last ``window`` keys; ``lse``
-        fp32, of q's shape without d, takes the logarithm of the sum of exponentials.
+        fp32, of q's shape without d, takes the logarithm of the sum of exponentials; ``out`` may be q
+        where q is contiguous.  Rows without keys, and sequences whose length is negative or more than the
+        block table holds, give 0 and -inf; NaN and infinities in what a token sees show in its row.
         """
         return self._fast.attend(self._cache, q, seq_lens, block_table, scale, window, out, lse)

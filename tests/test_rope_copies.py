@@ -1,6 +1,7 @@
-"""Copies of a rotation (no GPU needed: the handle is host memory)."""
+"""Copies and settings of a rotation (no GPU needed: the handle is host memory)."""
 import copy
 import gc
+import math
 import pickle
 
 import pytest
@@ -27,3 +28,13 @@ def test_copies_have_their_own_handle(make):
     again.close()
     with pytest.raises(paged._rt.RetopkError):
         make(again)
+
+
+@pytest.mark.parametrize("factor", [1.1e30, 1e39, 1e300, math.inf, math.nan, -0.1])
+def test_factors_on_cosine_and_sine_that_fp32_does_not_hold(factor):
+    """The kernels hold cosine and sine times the factor in fp32: beyond it 0 would have turned to NaN."""
+    from paper_2607_27692_b200 import build, paged
+    build.build()
+    with pytest.raises(paged._rt.RetopkError):
+        paged.Rope(64, attn_factor=factor)
+    assert paged.Rope(64, attn_factor=1e30).frequencies()[1] == 1e30
