@@ -20,7 +20,9 @@ tensors that require one unless under ``torch.no_grad()``.
 The arithmetic runs in ``libretopk.so`` (``include/retopk.h`` states it); ``_paged.so``
 (``csrc/paged_binding.cpp``) checks the tensors and passes pointers.  Work is enqueued on the current stream of the tensors' device; nothing
 is kept between calls, so calls on several streams and captured graphs do not share anything here.
-As with any kernel, the library's first call on a device loads code: make it before capturing.
+As with any kernel, the library's first call on a device loads code: make it before capturing.  A rotation's
+backward pass may be captured with its forward pass; as for any operator of torch, no eager graph of the same
+leaves may be alive then (torch's gradient accumulators remember the stream that they were made on).
 """
 from __future__ import annotations
 
