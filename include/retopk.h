@@ -475,6 +475,117 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
                         const void* q, int64_t q_stride, float scale, int64_t window, void* out, float* lse,
                         void* workspace, int64_t workspace_bytes, void* stream);
 
+/* =========================================================================================
+ * Sequences that share a cache: which pages are in use, attention over shared prefixes, attention over
+ * selected blocks.  Conventions as in the section above.
+ * ========================================================================================= */
+
+/*
+ * The pages of a cache (of all layers that use one block table).  refs [n_pages] int32 counts the
+ * entries of block tables that hold a page; a page with 0 or less is free, and new pages are the free
+ * ones with the lowest numbers.  scratch: n_pages + RETOPK_POOL_SCRATCH int32, set to zero once;
+ * scratch[0] counts the pages that calls found missing (the caller may read and clear it), the rest is the
+ * library's.  Both on the device.  A sequence of n rows holds the first ceil(n / page_size) entries of its row
+ * of block_table [B,max_pages].  Results do not depend on the order in which the device works.
+ * A pool and the tables over it are changed by one call at a time: calls on several streams need an
+ * order.  Array arguments that a call writes may not overlap its others (EINVAL).
+ * Limits: n_pages <= 2^20, B and n <= 65535; EUNSUPPORTED beyond.
+ */
+#define RETOPK_POOL_SCRATCH 4
+typedef struct {
+    int32_t *refs, *scratch;
+    int64_t n_pages;
+    int page_size;
+} retopk_pool_t;
+
+/* Give each sequence that grows from old_lens[b] to new_lens[b] rows the pages that it lacks, in the order of
+ * the sequences.  One that finds too few pages, or that block_table has no room for, gets none: its new
+ * entries are -1 and what it lacks is added to scratch[0].  Lengths are read only; negative ones count as 0.
+ * old_lens and new_lens may be one array (then nothing is done). */
+int retopk_pool_reserve(const retopk_pool_t* pool, int B, const int32_t* old_lens, const int32_t* new_lens, int32_t* block_table,
+                        int64_t max_pages, void* stream);
+
+/* Fork i lets the empty row children[i] (length 0 or less) continue sequence parents[i]: it holds the
+ * parent's full pages, a free page in the place of a partial last one, and has its length.  src[i], dst[i]
+ * and rows[i] say what is to be copied (retopk_pages_copy, for each layer): -1, -1 and 0 if nothing.  A fork
+ * is not made where a number is out of range, the parent is empty or does not fit block_table, the child is not
+ * empty, an earlier fork has the same child, the parent is a child in the same call, or no page is
+ * free (which counts in scratch[0]). */
+int retopk_pool_fork(const retopk_pool_t* pool, int B, int32_t* seq_lens, int32_t* block_table, int64_t max_pages, int n,
+                     const int32_t* parents, const int32_t* children, int32_t* src, int32_t* dst, int32_t* rows, void* stream);
+
+/* Give back the pages of sequences rows[0..n-1] (NULL: all, n = B) and set their lengths to 0. */
+int retopk_pool_free(const retopk_pool_t* pool, int B, int32_t* seq_lens, const int32_t* block_table, int64_t max_pages, int n,
+                     const int32_t* rows, void* stream);
+
+/* Renumber the pages so that those in use come first: with U in use, the i-th one from number U on becomes
+ * the i-th free one below U.  block_table follows (its rows have to hold all pages that refs counts), src
+ * and dst [n_pages / 2] take the moves for retopk_pages_copy, -1 behind the last. */
+int retopk_pool_compact(const retopk_pool_t* pool, int B, const int32_t* seq_lens, int32_t* block_table, int64_t max_pages,
+                        int32_t* src, int32_t* dst, void* stream);
+
+/* Copy pages src[i] to dst[i], keys, values and scales; with rows (NULL: all) the first rows[i] rows of each
+ * head only.  Pairs with a number that is no page, and pairs of one page, are left out.  A page that is
+ * written twice, or written and read, is unspecified afterwards.  block_table of `pages` is not read. */
+int retopk_pages_copy(const retopk_pages_t* pages, int64_t n, const int32_t* src, const int32_t* dst, const int32_t* rows, void* stream);
+
+/*
+ * Decode attention over 16-bit pages, all keys, no selection:
+ *     out[b,t,h] = sum_j softmax_j(scale * q . k_j) v_j
+ * T, seq_lens, q, out and lse as in retopk_q4_attention; q and out have the pages' type.  Sequences may come in groups
+ * that share their first rows: group g are sequences cu_groups[g] .. cu_groups[g+1]-1 (cu_groups
+ * [n_groups+1] int32, ascending from 0 to B), whose first shared_lens[g] rows are in the same pages (as retopk_pool_fork
+ * leaves them) or equal.  Those rows are read once for a group, from its first sequence that is not empty; the result is that of
+ * each sequence alone.  A group whose members see fewer rows (seq_lens[b] - T + 1) shares the fewest; empty sequences do not count.
+ * cu_groups that do not ascend from 0 to B stand for no groups at all, as n_groups = 0 does.
+ * Rows without keys give out = 0, lse = -inf, among them those of sequences whose length is negative or more than
+ * max_pages * page_size.  Keys of pages out of range do not count.  Scores go through the formula as IEEE arithmetic takes them: NaN and
+ * +inf make their row NaN, -inf is a weight of 0; what a token does not see has no influence.
+ * Scores, sums and outputs are held in fp32; weights are rounded to the pages' type once for the
+ * product with the values.  Results are bit-reproducible.
+ * out may be q where q is contiguous; other overlaps are EINVAL.  workspace as in retopk_q4_attention.
+ * Limits: as retopk_q4_attention.
+ */
+int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d);   /* bytes, or a negative code */
+int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int n_groups,
+                            const int32_t* cu_groups, const int32_t* shared_lens, const void* q, int64_t q_stride, float scale,
+                            void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Blocks of keys.  Block j of a sequence is rows j * block .. (j + 1) * block - 1; block is 16, 32, 64 or
+ * 128 and divides page_size.  bounds [n_pages,H_kv,page_size/block,2,d], of the pages' type: the least and
+ * the largest key of a block, channel by channel (NaN where a key is NaN).  16-bit pages only.
+ *
+ * retopk_block_update: the bounds of all full blocks that overlap the last n_new rows of each sequence.
+ * retopk_block_copy: the bounds follow their pages (retopk_pages_copy); whole pages.
+ */
+int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, int B, const int32_t* seq_lens, int64_t n_new, void* stream);
+int retopk_block_copy(const retopk_pages_t* pages, int block, void* bounds, int64_t n, const int32_t* src, const int32_t* dst, void* stream);
+
+/*
+ * Select blocks for each token and KV head: blocks [B,T,H_kv,keep] int32, ascending, -1 behind the last.  Token t of T
+ * sees n = seq_lens[b] - T + 1 + t keys in N = ceil(n / block) blocks; all of them if N <= keep.  Otherwise the `first` first
+ * and `last` last ones (last >= 1, first + last <= keep) and of the others those with the largest
+ *     score(j) = max over the heads h of the group of sum_c max(q_hc lo_jc, q_hc hi_jc),
+ * an upper bound of q_h . k over the block; ties to the lower number.  Each head's sum is exact to 2^-50 of its terms and rounded
+ * to fp32 once; a score of NaN counts as +inf, one of a page out of range as -inf.  Bounds of partial blocks are not read.
+ * workspace: retopk_block_select_workspace() bytes with max_blocks = ceil(rows that a sequence can have / block).
+ */
+int64_t retopk_block_select_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_blocks);
+int retopk_block_select(const retopk_pages_t* pages, int block, const void* bounds, int B, int T, int H_q, const int32_t* seq_lens,
+                        const void* q, int64_t q_stride, int keep, int first, int last, int32_t* blocks, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
+/*
+ * retopk_shared_attention over the keys of selected blocks: token t and the heads of KV head h see the keys below
+ * seq_lens[b] - T + 1 + t in blocks[b,t,h,:], of which the first min(keep, N) entries are read.  Entries that are no block of the
+ * sequence (-1) do not count; a block that is named twice counts twice.
+ */
+int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep);
+int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T, int H_q, const int32_t* seq_lens, int keep,
+                           const int32_t* blocks, const void* q, int64_t q_stride, float scale, void* out, float* lse,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Static description of an error code. */
 const char* retopk_strerror(int code);
 

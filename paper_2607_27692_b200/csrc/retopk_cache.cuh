@@ -83,6 +83,35 @@ __device__ __forceinline__ void pdl_start_next() { asm volatile("griddepcontrol.
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Sum over the threads before this one, and over all; every thread of the CTA calls it.
+template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total) {
+    __shared__ int s_part[THREADS / 32 + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int sum = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+    }
+    __syncthreads();                     // the last call's parts have been read
+    if (lane == 31) s_part[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+        int p = lane < THREADS / 32 ? s_part[lane] : 0;
+        const int own = p;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, p, o);
+            if (lane >= o) p += y;
+        }
+        if (lane < THREADS / 32) s_part[lane] = p - own;
+        if (lane == 31) s_part[THREADS / 32] = p;
+    }
+    __syncthreads();
+    *total = s_part[THREADS / 32];
+    return s_part[warp] + sum - x;
+}
+
 // The cache as the kernels see it (retopk_pages_t with 64-bit strides worked out).
 struct Pages {
     unsigned char *k, *v, *ks, *vs;
@@ -122,7 +151,7 @@ __device__ __forceinline__ uint32_t eight_codes(const float* x, float m, float s
     return w;
 }
 // The rare steps below 2^-60 or above 2^60, out of line.
-__device__ __noinline__ uint32_t eight_codes_scaled(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float m, float s) {
+static __device__ __noinline__ uint32_t eight_codes_scaled(float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7, float m, float s) {
     const float c = s < 1.f ? 18446744073709551616.f : 5.4210109e-20f;       // 2^64, 2^-64
     const float x[8] = {x0, x1, x2, x3, x4, x5, x6, x7};
     return eight_codes<true>(x, m, s, s > 0.f ? __frcp_rn(s * c) : 0.f, c);

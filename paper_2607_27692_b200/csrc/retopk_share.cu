@@ -1,0 +1,178 @@
+// Host side of the attention over 16-bit pages and of the selection of blocks: argument checks, launches,
+// C interface.
+#include "retopk_share.cuh"
+
+#include <math.h>
+
+#include "retopk_cache_host.cuh"
+
+using namespace retopk_cache;
+
+namespace {
+
+int check_shape(int B, int T, int H_q, int H_kv, int d) {
+    if (B < 1 || T < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv != 0) return RETOPK_EINVAL;
+    if ((d != 64 && d != 128) || H_q / H_kv > 16 || T > 16 || (long long)B * H_kv > MAX_SEQ_GROUPS) return RETOPK_EUNSUPPORTED;
+    return RETOPK_OK;
+}
+
+// What both attentions refuse alike, and their arguments.
+int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, const void* q, int64_t q_stride,
+                    float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, int64_t need, AttendArgs& a) {
+    if (pages->format == RETOPK_PAGES_Q4 || !seq_lens || !out || !workspace || !isfinite(scale)) return RETOPK_EINVAL;
+    const int d = pages->d;
+    if (!rows_ok(q, q_stride, H_q, d) || !aligned16(workspace) || !aligned16(out)) return RETOPK_EINVAL;
+    memset(&a, 0, sizeof a);
+    a.pg = device_pages(pages);
+    if (a.pg.capacity > MAX_KEYS || pages->n_pages > 0xfffffffell / ((long long)pages->H_kv * pages->page_size)) return RETOPK_EUNSUPPORTED;
+    const long long n = (long long)B * T;
+    const Strided qi = {q, q_stride, H_q}, qo = {out, (long long)H_q * d, H_q};
+    Memory pg[4];
+    memory_of(pages, pg);
+    const Memory q_m = memory_of(qi, n, d), out_m = memory_of(qo, n, d), lse_m = {lse, (uint64_t)n * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
+    if (!in_place_or_apart(qi, qo, n, d) || !all_apart(out_m, pg) || !all_apart(lse_m, pg) || !all_apart(ws_m, pg)) return RETOPK_EINVAL;
+    if (!all_apart(lse_m, {out_m, q_m, ws_m}) || !all_apart(ws_m, {out_m, q_m})) return RETOPK_EINVAL;
+    if (workspace_bytes < need) return RETOPK_EINVAL;
+    a.seq_lens = seq_lens;
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_stride = q_stride;
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    a.scale_log2 = (float)((double)scale * 1.44269504088896340736);
+    a.B = B; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv;
+    return RETOPK_OK;
+}
+
+int launch_attend(const AttendArgs& a, const retopk_pages_t* pages, cudaStream_t s) {
+    const dim3 grid((unsigned)a.Hq, (unsigned)a.T, (unsigned)a.B);
+    if (pages->format == RETOPK_PAGES_BF16)
+        return launch(pages->d == 128 ? attend_kernel<TYPE_BF16, 128> : attend_kernel<TYPE_BF16, 64>, grid, ATTEND_THREADS, 0, s, a);
+    return launch(pages->d == 128 ? attend_kernel<TYPE_FP16, 128> : attend_kernel<TYPE_FP16, 64>, grid, ATTEND_THREADS, 0, s, a);
+}
+
+template <class Args, class F> int by_type(const retopk_pages_t* p, F bf128, F bf64, F fp128, F fp64, dim3 grid, unsigned threads, cudaStream_t s, const Args& a) {
+    const bool bf = p->format == RETOPK_PAGES_BF16, wide = p->d == 128;
+    return launch(bf ? (wide ? bf128 : bf64) : (wide ? fp128 : fp64), grid, threads, 0, s, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d) {
+    const int rc = check_shape(B, T, H_q, H_kv, d);
+    if (rc != RETOPK_OK) return rc;
+    if (n_groups < 0 || n_groups > B) return RETOPK_EINVAL;
+    return 16;
+}
+
+int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int n_groups,
+                            const int32_t* cu_groups, const int32_t* shared_lens, const void* q, int64_t q_stride, float scale,
+                            void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_pages(pages, B);
+    if (rc != RETOPK_OK) return rc;
+    const int64_t need = retopk_shared_attention_workspace(B, n_groups, T, H_q, pages->H_kv, pages->d);
+    if (need < 0) return (int)need;
+    if (n_groups > 0 && (!cu_groups || !shared_lens)) return RETOPK_EINVAL;
+    AttendArgs a;
+    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, need, a);
+    if (rc != RETOPK_OK) return rc;
+    a.block = 16;
+    return launch_attend(a, pages, static_cast<cudaStream_t>(stream));
+}
+
+int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, int B, const int32_t* seq_lens, int64_t n_new, void* stream) {
+    const int rc = check_blocks(pages, B, block, bounds);
+    if (rc != RETOPK_OK) return rc;
+    if (!seq_lens || n_new < 0) return RETOPK_EINVAL;
+    if (B > 65535 || pages->H_kv > 65535) return RETOPK_EUNSUPPORTED;
+    if (n_new == 0) return RETOPK_OK;
+    BoundsArgs a;
+    memset(&a, 0, sizeof a);
+    a.pg = device_pages(pages);
+    a.block = block;
+    a.seq_lens = seq_lens;
+    a.n_new = n_new;
+    a.bounds = static_cast<uint16_t*>(bounds);
+    // whole blocks that n_new rows can touch
+    const long long all = a.pg.capacity / block, some = n_new >= a.pg.capacity ? all : (n_new + block - 2) / block + 1;
+    const long long most = some < all ? some : all;
+    if (most == 0) return RETOPK_OK;
+    const dim3 grid((unsigned)((most + BOUNDS_WARPS - 1) / BOUNDS_WARPS), (unsigned)pages->H_kv, (unsigned)B);
+    return by_type(pages, bounds_kernel<TYPE_BF16, 128>, bounds_kernel<TYPE_BF16, 64>, bounds_kernel<TYPE_FP16, 128>,
+                   bounds_kernel<TYPE_FP16, 64>, grid, BOUNDS_THREADS, static_cast<cudaStream_t>(stream), a);
+}
+
+int64_t retopk_block_select_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_blocks) {
+    const int rc = check_shape(B, T, H_q, H_kv, d);
+    if (rc != RETOPK_OK) return rc;
+    if (max_blocks < 1) return RETOPK_EINVAL;
+    if (max_blocks > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    return (int64_t)B * T * H_kv * max_blocks * 4;
+}
+
+int retopk_block_select(const retopk_pages_t* pages, int block, const void* bounds, int B, int T, int H_q, const int32_t* seq_lens,
+                        const void* q, int64_t q_stride, int keep, int first, int last, int32_t* blocks, void* workspace,
+                        int64_t workspace_bytes, void* stream) {
+    int rc = check_blocks(pages, B, block, bounds);
+    if (rc != RETOPK_OK) return rc;
+    if (!seq_lens || !blocks || !workspace || keep < 1 || first < 0 || last < 1 || first > keep - last) return RETOPK_EINVAL;
+    SelectArgs a;
+    memset(&a, 0, sizeof a);
+    a.pg = device_pages(pages);
+    if (a.pg.capacity > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    a.max_blocks = (a.pg.capacity + block - 1) / block;
+    const int64_t need = retopk_block_select_workspace(B, T, H_q, pages->H_kv, pages->d, a.max_blocks);
+    if (need < 0) return (int)need;
+    if (!rows_ok(q, q_stride, H_q, pages->d) || !aligned16(workspace) || workspace_bytes < need) return RETOPK_EINVAL;
+    if (keep > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    const Memory q_m = memory_of(Strided{q, q_stride, H_q}, (long long)B * T, pages->d), ws_m = {workspace, (uint64_t)workspace_bytes};
+    const Memory bounds_m = bounds_memory(pages, block, bounds), blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
+    if (!all_apart(blocks_m, {q_m, ws_m, bounds_m}) || !all_apart(ws_m, {q_m, bounds_m})) return RETOPK_EINVAL;
+    a.block = block; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv; a.keep = keep; a.first = first; a.last = last;
+    a.seq_lens = seq_lens;
+    a.bounds = static_cast<const uint16_t*>(bounds);
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_stride = q_stride;
+    a.scores = static_cast<float*>(workspace);
+    a.blocks = blocks;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a.max_blocks > keep) {
+        const dim3 grid((unsigned)((a.max_blocks + SCORE_BLOCKS - 1) / SCORE_BLOCKS), (unsigned)pages->H_kv, (unsigned)B);
+        rc = by_type(pages, score_kernel<TYPE_BF16, 128>, score_kernel<TYPE_BF16, 64>, score_kernel<TYPE_FP16, 128>,
+                     score_kernel<TYPE_FP16, 64>, grid, SCORE_THREADS, s, a);
+        if (rc != RETOPK_OK) return rc;
+    }
+    return launch(pick_kernel, dim3((unsigned)pages->H_kv, (unsigned)T, (unsigned)B), PICK_THREADS, 0, s, a);
+}
+
+int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep) {
+    const int rc = check_shape(B, T, H_q, H_kv, d);
+    if (rc != RETOPK_OK) return rc;
+    if (keep < 1) return RETOPK_EINVAL;
+    return 16;
+}
+
+int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T, int H_q, const int32_t* seq_lens, int keep,
+                           const int32_t* blocks, const void* q, int64_t q_stride, float scale, void* out, float* lse,
+                           void* workspace, int64_t workspace_bytes, void* stream) {
+    int rc = check_pages(pages, B);
+    if (rc != RETOPK_OK) return rc;
+    if (block != 16 && block != 32 && block != 64 && block != 128) return RETOPK_EUNSUPPORTED;
+    const int64_t need = retopk_block_attention_workspace(B, T, H_q, pages->H_kv, pages->d, keep);
+    if (need < 0) return (int)need;
+    if (!blocks || pages->page_size % block != 0) return RETOPK_EINVAL;
+    if (keep > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    AttendArgs a;
+    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, need, a);
+    if (rc != RETOPK_OK) return rc;
+    const Memory blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
+    const Memory out_m = {out, (uint64_t)B * T * H_q * pages->d * 2}, lse_m = {lse, (uint64_t)B * T * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
+    if (!all_apart(blocks_m, {out_m, lse_m, ws_m})) return RETOPK_EINVAL;
+    a.blocks = blocks;
+    a.keep = keep;
+    a.block = block;
+    return launch_attend(a, pages, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""Rotary positions, paged key/value caches and attention over a 4-bit cache (binding).
+"""Rotary positions, paged key/value caches that sequences share, and attention over them (binding).
 
 What a decode loop needs around :class:`paper_2607_27692_b200.retopk.ReTopK`::
 
@@ -13,6 +13,18 @@ What a decode loop needs around :class:`paper_2607_27692_b200.retopk.ReTopK`::
     cache = KVPages(n_pages, H_kv, 64, 128, "q4")
     q = cache.append(k_new, v_new, seq_lens, block_table, rope=rope, q=q_new)
     out = cache.attend(q, seq_lens, block_table)
+
+    # sequences that continue one prompt: pages are shared, and so is the work on them
+    pool = PagePool(n_pages, 64)
+    pool.reserve(block_table, old_lens, seq_lens)
+    cache.copy_pages(*pool.fork(block_table, seq_lens, parents, children))
+    out = cache.attend_shared(q, seq_lens, block_table, cu_groups, prompt_lens)
+
+    # attention over the blocks of keys that can score highest
+    index = BlockIndex(cache, 64)
+    index.update(seq_lens, block_table)
+    blocks = index.select(q, seq_lens, block_table, keep=64)
+    out = index.attend(q, seq_lens, blocks, block_table)
 
 The rotation is differentiable.  The calls of a cache are for serving: they have no gradient and refuse
 tensors that require one unless under ``torch.no_grad()``.
@@ -261,3 +273,138 @@ class KVPages:
         block table holds, give 0 and -inf; NaN and infinities in what a token sees show in its row.
         """
         return self._fast.attend(self._cache, q, seq_lens, block_table, scale, window, out, lse)
+
+    def attend_shared(self, q, seq_lens, block_table=None, cu_groups=None, shared_lens=None, scale=None, out=None, lse=None):
+        """Attention of the last T tokens of every sequence over 16-bit pages, shared prefixes read once.
+
+        q, ``out``, ``lse`` and the result as in ``attend``; q has the cache's type.  Sequences
+        cu_groups[g]:cu_groups[g+1] (int32 [groups + 1], from 0 to B) share their first shared_lens[g] rows
+        (int32 [groups]): the same pages, as ``PagePool.fork`` leaves them, or equal rows.  The result is that
+        of each sequence alone, which is also what is computed without ``cu_groups``.
+        """
+        return self._fast.attend_shared(self._cache, q, seq_lens, block_table, cu_groups, shared_lens, scale, out, lse)
+
+    def copy_pages(self, src, dst, rows=None):
+        """Copy pages src[i] to dst[i] (int32 [n]), with ``rows`` the first rows[i] rows of each.
+
+        Pairs with a negative number are left out.  A page that is written twice, or written and read, is
+        unspecified afterwards.
+        """
+        self._fast.copy_pages(self._cache, src, dst, rows)
+
+
+class PagePool:
+    """Which pages of a cache (of all layers over one block table) are in use.
+
+    ``refs`` int32 [n_pages] counts the entries of block tables that hold a page; new pages are the free ones
+    with the lowest numbers.  A sequence of n rows holds the first ceil(n / page_size) entries of its row of
+    ``block_table``.  Everything is on the device and nothing is waited for: pages that were missing are
+    counted in ``missing`` (int32 [1], to read or clear).  One call at a time may change a pool and its tables.
+    """
+
+    def __init__(self, n_pages, page_size, device="cuda"):
+        self._set(torch.zeros(n_pages, dtype=torch.int32, device=device), page_size)
+
+    @classmethod
+    def wrap(cls, refs, page_size):
+        """Use existing counts (int32 [n_pages])."""
+        self = cls.__new__(cls)
+        self._set(refs, page_size)
+        return self
+
+    def _set(self, refs, page_size):
+        self._fast = _binding()
+        if refs.dim() != 1 or refs.numel() < 1 or refs.dtype != torch.int32 or not refs.is_cuda or not refs.is_contiguous():
+            raise TypeError(f"refs: expected a contiguous int32 CUDA tensor [n_pages], got {refs.dtype} {tuple(refs.shape)} on {refs.device}")
+        if page_size < 1:
+            raise ValueError(f"page_size: at least 1, got {page_size}")
+        self.refs, self.page_size, self.n_pages = refs, int(page_size), refs.numel()
+        self._scratch = torch.zeros(self.n_pages + 4, dtype=torch.int32, device=refs.device)      # RETOPK_POOL_SCRATCH
+
+    @property
+    def missing(self):
+        return self._scratch[:1]
+
+    def reserve(self, block_table, old_lens, new_lens):
+        """Enter the pages that sequences lack to grow from ``old_lens`` to ``new_lens`` rows (int32 [B]).
+
+        In the order of the sequences; one that finds too few pages, or no room in its row, gets -1 in its
+        new entries.
+        """
+        self._fast.pool_reserve(self.refs, self._scratch, self.page_size, block_table, old_lens, new_lens)
+
+    def fork(self, block_table, seq_lens, parents, children):
+        """Let the empty rows ``children`` (int32 [n]) continue the sequences ``parents``.
+
+        Full pages are shared, a partial last one gets a page of its own; ``seq_lens`` of the children are set.
+        Returns (src, dst, rows), what ``copy_pages`` has to copy in each layer.  A fork that cannot be made (a child
+        that is not empty, is named twice or is a parent too, an empty parent, no free page) is left out.
+        """
+        return self._fast.pool_fork(self.refs, self._scratch, self.page_size, block_table, seq_lens, parents, children)
+
+    def free(self, block_table, seq_lens, rows=None):
+        """Give back the pages of sequences ``rows`` (int32 [n], default all) and set their lengths to 0."""
+        self._fast.pool_free(self.refs, self._scratch, self.page_size, block_table, seq_lens, rows)
+
+    def compact(self, block_table, seq_lens):
+        """Renumber the pages so that those in use come first; ``block_table`` follows.
+
+        Returns (src, dst), the moves that ``copy_pages`` has to make in each layer, -1 behind the last.  All
+        entries that hold pages have to be in ``block_table``.
+        """
+        return self._fast.pool_compact(self.refs, self._scratch, self.page_size, block_table, seq_lens)
+
+
+class BlockIndex:
+    """Bounds of blocks of ``block`` keys (16, 32, 64 or 128) of a 16-bit cache, and attention over selected blocks.
+
+    ``bounds`` [n_pages, H_kv, page_size / block, 2, d], of the cache's type: least and largest key of each
+    block, channel by channel.
+    """
+
+    def __init__(self, cache, block):
+        if block not in (16, 32, 64, 128) or cache.page_size % block:
+            raise ValueError(f"block: 16, 32, 64 or 128 and a divisor of page_size {cache.page_size}, got {block}")
+        shape = (cache.n_pages, cache.H_kv, cache.page_size // block, 2, cache.d)
+        self._set(cache, torch.zeros(shape, dtype=cache.k.dtype, device=cache.device))
+
+    @classmethod
+    def wrap(cls, cache, bounds):
+        """Use an existing tensor of bounds."""
+        self = cls.__new__(cls)
+        self._set(cache, bounds)
+        return self
+
+    def _set(self, cache, bounds):
+        if cache.fmt == "q4":
+            raise TypeError("a block index reads 16-bit pages, this cache holds 4-bit values")
+        if bounds.dim() != 5 or bounds.shape[2] < 1 or cache.page_size % bounds.shape[2]:
+            raise ValueError(f"bounds: expected [n_pages, H_kv, page_size / block, 2, d], got {tuple(bounds.shape)}")
+        self.cache, self.bounds, self.block = cache, bounds, cache.page_size // bounds.shape[2]
+        if self.block not in (16, 32, 64, 128):
+            raise ValueError(f"bounds: blocks of 16, 32, 64 or 128 keys, got {self.block}")
+        self._fast = _binding()
+
+    def update(self, seq_lens, block_table=None, n_new=None):
+        """Work out the bounds of the full blocks that overlap the last ``n_new`` rows (default: of all)."""
+        self._fast.block_update(self.cache._cache, self.bounds, self.block, seq_lens, block_table, (1 << 62) if n_new is None else n_new)
+
+    def select(self, q, seq_lens, block_table=None, keep=64, first=1, last=2, out=None):
+        """Blocks for each token and KV head, int32 [B, H_kv, keep] or [B, T, H_kv, keep], ascending, -1 behind the last.
+
+        The ``first`` and ``last`` blocks of a sequence are always among them; the others are those with the
+        largest upper bound of a query's products with the block's keys (any head of the group), ties to
+        the lower number.  For a ``scale`` above 0.
+        """
+        return self._fast.block_select(self.cache._cache, self.bounds, self.block, q, seq_lens, block_table, keep, first, last, out)
+
+    def attend(self, q, seq_lens, blocks, block_table=None, scale=None, out=None, lse=None):
+        """Attention over the keys of ``blocks``, as ``select`` returns them; the rest as ``KVPages.attend_shared``.
+
+        Entries that are no block of the sequence do not count, a block that is named twice counts twice.
+        """
+        return self._fast.block_attend(self.cache._cache, self.block, q, seq_lens, blocks, block_table, scale, out, lse)
+
+    def copy_pages(self, src, dst):
+        """The bounds follow ``KVPages.copy_pages``."""
+        self._fast.block_copy(self.cache._cache, self.bounds, self.block, src, dst)
