@@ -546,7 +546,8 @@ int retopk_pages_copy(const retopk_pages_t* pages, int64_t n, const int32_t* src
  * out may be q where q is contiguous; other overlaps are EINVAL.  workspace as in retopk_q4_attention.
  * Limits: as retopk_q4_attention.
  */
-int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d);   /* bytes, or a negative code */
+/* Bytes, or a negative code; max_keys: rows that a sequence can have, max_pages * page_size (page_size without a table). */
+int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys);
 int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int n_groups,
                             const int32_t* cu_groups, const int32_t* shared_lens, const void* q, int64_t q_stride, float scale,
                             void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
@@ -581,7 +582,7 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
  * seq_lens[b] - T + 1 + t in blocks[b,t,h,:], of which the first min(keep, N) entries are read.  Entries that are no block of the
  * sequence (-1) do not count; a block that is named twice counts twice.
  */
-int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep);
+int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep, int block);
 int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T, int H_q, const int32_t* seq_lens, int keep,
                            const int32_t* blocks, const void* q, int64_t q_stride, float scale, void* out, float* lse,
                            void* workspace, int64_t workspace_bytes, void* stream);

@@ -286,6 +286,9 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     });
 }
 
+// Rows that a sequence can have.
+int64_t keys_of(const retopk_pages_t& p) { return p.block_table ? p.max_pages * p.page_size : p.page_size; }
+
 // Queries [B, H_q, d] or [B, T, H_q, d], and results of their shape.
 struct Queries {
     const at::Tensor& q;
@@ -390,7 +393,7 @@ PyObject* attend_shared(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const at::Tensor out = output(a[7], x, c);
         float* lse = log_sums(a[8], x, c);
         if (x.B > 0) {
-            const int64_t need = retopk_shared_attention_workspace((int)x.B, (int)groups, (int)x.T, (int)x.H_q, c.pages.H_kv, c.pages.d);
+            const int64_t need = retopk_shared_attention_workspace((int)x.B, (int)groups, (int)x.T, (int)x.H_q, c.pages.H_kv, c.pages.d, keys_of(pages));
             check(need, "retopk_shared_attention_workspace");
             const at::Tensor ws = workspace(need, x.q);
             check(retopk_shared_attention(&pages, (int)x.B, (int)x.T, (int)x.H_q, lens, (int)groups, cu, shared, x.q.data_ptr(), x.stride,
@@ -469,7 +472,7 @@ PyObject* block_select(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
             out = empty(shape, x.q, at::kInt);
         }
         if (x.B > 0) {
-            const int64_t capacity = pages.block_table ? pages.max_pages * pages.page_size : pages.page_size;
+            const int64_t capacity = keys_of(pages);
             const int64_t need = retopk_block_select_workspace((int)x.B, (int)x.T, (int)x.H_q, c.pages.H_kv, c.pages.d, (capacity + block - 1) / block);
             check(need, "retopk_block_select_workspace");
             const at::Tensor ws = workspace(need, x.q);
@@ -508,7 +511,7 @@ PyObject* block_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const at::Tensor out = output(a[7], x, c);
         float* lse = log_sums(a[8], x, c);
         if (x.B > 0) {
-            const int64_t need = retopk_block_attention_workspace((int)x.B, (int)x.T, (int)x.H_q, c.pages.H_kv, c.pages.d, keep);
+            const int64_t need = retopk_block_attention_workspace((int)x.B, (int)x.T, (int)x.H_q, c.pages.H_kv, c.pages.d, keep, block);
             check(need, "retopk_block_attention_workspace");
             const at::Tensor ws = workspace(need, x.q);
             check(retopk_block_attention(&pages, block, (int)x.B, (int)x.T, (int)x.H_q, lens, keep, blocks.data_ptr<int32_t>(), x.q.data_ptr(),

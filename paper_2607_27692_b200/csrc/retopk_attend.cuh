@@ -1,0 +1,815 @@
+// Attention over 16-bit pages on the fifth-generation tensor cores (sm_100a).
+//
+//   plan_kernel      what there is to do: entries of work, one behind the other on a line
+//   attend_kernel    a CTA takes an equal share of the line
+//   join_kernel      joins the parts of a row
+//
+// An entry is a set of query rows that see the same keys: the members of a group and the rows that they share,
+// the tokens of a sequence and the rows of its own, or one token and the blocks selected for it.  Keys that only some of a sequence's
+// draft tokens see (its last T - 1) are left to join_kernel, so that a tile of 128 keys has one mask for all
+// rows.  For each KV head and 256 query rows an entry has a line of tiles; a piece of a line is what one CTA
+// takes of it, and leaves fp32 sums for its rows in the workspace.
+#pragma once
+#include "retopk_cache.cuh"
+
+namespace retopk_cache {
+
+// Keys that token t of T sees in a sequence of `len` keys; none if the cache cannot hold the sequence.
+__device__ __forceinline__ long long keys_seen(const Pages& pg, long long len, int T, int t) {
+    if (len < 0 || len > pg.capacity) return 0;
+    const long long n = len - T + 1 + t;
+    return n > 0 ? n : 0;
+}
+
+constexpr int ATT_TILE = 128;            // keys of a tile, and query rows of a stream
+constexpr int ATT_CHUNK = 1024;          // tiles whose sums stay in the tensor core at most: it cuts additions off
+constexpr int ATT_START = 2;             // what beginning a line counts, in tiles
+constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // reference of a row without keys; lowest of one with keys
+
+struct Entry {
+    long long u;                // where its lines begin
+    int item;                   // number of its first (line, chunk)
+    int rows, token;            // query rows: heads of a group of the tokens from `token` on
+    int b;                      // sequence whose row of the block table holds the keys
+    int lo, hi, seen;           // keys lo..hi-1 (of the selected blocks one behind the other: 0..hi-1, below `seen`)
+    int tile0, tiles;
+    int row_tiles, chunks;      // lines of a KV head (256 rows each); chunks of a line
+};
+struct AttendHeader { long long units; };
+
+struct AttendArgs {
+    Pages pg;
+    const int32_t* seq_lens;
+    const uint16_t* q;
+    long long q_stride;
+    uint16_t* out;
+    float* lse;
+    float scale_log2;
+    int B, T, Hq, G;
+    int n_groups;
+    const int32_t *cu, *shared_lens;
+    const int32_t* blocks;      // [B, T, H_kv, keep], or null: all keys
+    int keep, block, block_shift;
+    int entries, grid, own_rows;                         // own_rows: rows of a half of a part that belongs to one sequence
+    AttendHeader* head;
+    Entry* entry;
+    int32_t *group_of, *flags;  // group of a sequence or -1; CTAs that gave up
+    float *shared_parts, *own_parts;
+};
+
+// Floats of a half of a part (one stream's): sums [D / 4][rows][4], then reference and weight sum of each row.
+__host__ __device__ constexpr long long half_floats(int rows, int d) { return (long long)rows * d + (2 * rows + 3) / 4 * 4; }
+__device__ __forceinline__ long long line_units(const Entry& e) { return e.tiles > 0 ? e.tiles + ATT_START : 0; }
+__device__ __forceinline__ long long share_begin(long long units, int grid, int cta) { return units * cta / grid; }
+// The CTA whose share holds unit u.
+__device__ __forceinline__ int share_of(long long units, int grid, long long u) { return (int)(((u + 1) * grid - 1) / units); }
+
+// ---------------------------------------------------------------------------------------
+// plan_kernel
+// ---------------------------------------------------------------------------------------
+constexpr int PLAN_THREADS = 1024;
+
+// One CTA.  Groups: the first member that is not empty owns the keys, the fewest rows that any of them sees
+// are shared; a member alone shares nothing.
+__global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constant__ AttendArgs a) {
+    __shared__ long long s_units[PLAN_THREADS / 32 + 1];
+    pdl_wait();
+    pdl_start_next();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    bool bad = false;
+    for (int g = tid; g < a.n_groups; g += PLAN_THREADS)
+        bad |= a.cu[g] < 0 || a.cu[g + 1] < a.cu[g] || a.cu[g + 1] > a.B || (g == 0 && a.cu[0] != 0) || (g == a.n_groups - 1 && a.cu[g + 1] != a.B);
+    const int groups = __syncthreads_or(bad) ? 0 : a.n_groups;
+    for (int g = warp; g < groups; g += PLAN_THREADS / 32) {
+        const int b0 = a.cu[g], b1 = a.cu[g + 1];
+        int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
+        for (int b = b0 + lane; b < b1; b += 32) {
+            a.group_of[b] = g;
+            if (a.seq_lens[b] <= 0 || a.seq_lens[b] > a.pg.capacity) continue;
+            const int n = (int)keys_seen(a.pg, a.seq_lens[b], a.T, 0);
+            owner = b < owner ? b : owner;
+            least = n < least ? n : least;
+            ++members;
+        }
+        owner = __reduce_min_sync(0xffffffffu, owner);
+        least = __reduce_min_sync(0xffffffffu, least);
+        members = __reduce_add_sync(0xffffffffu, members);
+        if (lane == 0) {
+            int n = a.shared_lens[g];
+            n = members < 2 || n < 0 ? 0 : (n < least ? n : least);
+            Entry e;
+            e.rows = (b1 - b0) * a.T * a.G;
+            e.token = b0 * a.T;
+            e.b = n > 0 ? owner : 0;
+            e.lo = 0;
+            e.hi = e.seen = n;
+            a.entry[g] = e;
+        }
+    }
+    __syncthreads();
+    if (groups == 0) {
+        for (int b = tid; b < a.B; b += PLAN_THREADS) a.group_of[b] = -1;
+        for (int g = tid; g < a.n_groups; g += PLAN_THREADS) {
+            Entry e;
+            e.rows = e.token = e.b = e.lo = e.hi = e.seen = 0;
+            a.entry[g] = e;
+        }
+        __syncthreads();
+    }
+    long long units = 0;
+    int shared_items = 0, own_items = 0;
+    for (int e0 = 0; e0 < a.entries; e0 += PLAN_THREADS) {
+        const int i = e0 + tid;
+        const bool on = i < a.entries, own = i >= a.n_groups;
+        Entry e;
+        e.tiles = e.row_tiles = e.chunks = 0;
+        if (on) {
+            if (!own) {
+                e = a.entry[i];
+            } else if (a.blocks) {
+                const int b = i / a.T;
+                const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, i - b * a.T), N = (seen + a.block - 1) / a.block;
+                e.rows = a.G;
+                e.token = i;
+                e.b = b;
+                e.lo = 0;
+                e.seen = (int)seen;
+                e.hi = (int)((N < a.keep ? N : a.keep) * a.block);
+            } else {
+                const int b = i - a.n_groups, g = a.group_of[b];
+                e.rows = a.T * a.G;
+                e.token = b * a.T;
+                e.b = b;
+                e.hi = e.seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, 0);
+                e.lo = g >= 0 ? a.entry[g].hi : 0;
+                if (e.lo > e.hi) e.lo = e.hi;
+            }
+            e.tile0 = e.lo / ATT_TILE;
+            e.tiles = e.hi > e.lo ? (e.hi + ATT_TILE - 1) / ATT_TILE - e.tile0 : 0;
+            e.row_tiles = (e.rows + 2 * ATT_TILE - 1) / (2 * ATT_TILE);
+            e.chunks = (e.tiles + ATT_CHUNK - 1) / ATT_CHUNK;
+        }
+        const int lines = a.pg.H_kv * e.row_tiles, items = lines * e.chunks;
+        int all_items, all_shared;
+        const int before = scan_cta<PLAN_THREADS>(items, &all_items);
+        scan_cta<PLAN_THREADS>(own ? 0 : items, &all_shared);
+        // units: a scan in 64 bits
+        long long mine = (long long)lines * line_units(e), sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
+        }
+        if (lane == 31) s_units[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+            const long long part = s_units[lane];
+            long long p = part;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, p, o);
+                if (lane >= o) p += y;
+            }
+            s_units[lane] = p - part;
+            if (lane == 31) s_units[32] = p;
+        }
+        __syncthreads();
+        if (on) {
+            e.u = units + s_units[warp] + sum - mine;
+            e.item = own ? own_items + before - all_shared : shared_items + before;      // (groups come first)
+            a.entry[i] = e;
+        }
+        units += s_units[32];
+        shared_items += all_shared;
+        own_items += all_items - all_shared;
+        __syncthreads();
+    }
+    if (tid == 0) a.head->units = units;
+}
+
+// ---------------------------------------------------------------------------------------
+// Barriers and the tensor core
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long clock_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for the phase; gives up after two seconds, or when another part of the CTA has.
+__device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    const unsigned long long begin = clock_ns();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (bar_try(bar, parity)) return true;
+        if (*gave_up) return false;
+        if (clock_ns() - begin > 2000000000ull) {
+            *gave_up = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
+    if (bar_try(bar, parity)) return true;
+    return bar_wait_long(bar, parity, gave_up);
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D (+)= A B, 128 x N x 16; A in shared memory or in tensor memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+
+#define TC_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
+#define TC_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+// 32 columns of the lanes of this warp; tc_wait_ld before the values are used.
+__device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : TC_R8(x, 0), TC_R8(x, 8), TC_R8(x, 16), TC_R8(x, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8), TC_W8(x, 16), TC_W8(x, 24) : "memory");
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Shared memory operand with rows of 128 bytes, 16-byte columns exchanged within 8 rows (128-byte swizzle);
+// `lead`: bytes between halves of 64 channels where the operand runs along the channels.
+__device__ __forceinline__ uint64_t tc_operand(uint32_t addr, uint32_t lead) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Accumulators in fp32, operands of one 16-bit type, 128 x n; b_along_n: B lies with its rows along k.
+template <int DT> __host__ __device__ constexpr uint32_t tc_shape(int n, bool b_along_n) {
+    return 1u << 4 | (uint32_t)(DT == TYPE_BF16) << 7 | (uint32_t)(DT == TYPE_BF16) << 10 | (uint32_t)b_along_n << 16 |
+           (uint32_t)(n >> 3) << 17 | (uint32_t)(ATT_TILE >> 4) << 24;
+}
+
+// ---------------------------------------------------------------------------------------
+// attend_kernel
+// ---------------------------------------------------------------------------------------
+constexpr int ATT_SOFT_WARPS = 8, ATT_LOAD_WARPS = 4, ATT_MMA_WARP = ATT_SOFT_WARPS + ATT_LOAD_WARPS;
+constexpr int ATT_THREADS = (ATT_MMA_WARP + 1) * 32;
+constexpr int ATT_PIECES = 32;           // pieces that a CTA lists at once
+constexpr int ATT_MASKS = 8;             // tiles whose masks are kept
+
+struct Piece {
+    int b, h, token, row0, rows, half_rows;
+    int lo, hi, seen, tile0, tile1;
+    int pad;
+    float* part;
+};
+template <int D> struct AttendSmem {
+    static constexpr int TILE_BYTES = ATT_TILE * D * 2;
+    static constexpr int SLOTS = 5 * 128 / D;
+    static constexpr int LAG = SLOTS - 2;                // loads in flight before one is waited for
+    unsigned char q[2][TILE_BYTES];
+    unsigned char ring[SLOTS][TILE_BYTES];
+    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2], p_ready[2], o_ready[2], drained;
+    uint32_t mask[ATT_MASKS][4];
+    Piece piece[ATT_PIECES];
+    int warp_sum[ATT_MMA_WARP + 2];
+    uint32_t tmem;
+    int gave_up;
+};
+
+// Two streams of four warps each take the softmax of 128 query rows: with up to 128 rows both have the same
+// rows and every other tile, with more a stream has 128 of 256 rows and every tile.  While one is at its
+// softmax the tensor core works for the other.  Four warps fetch keys and values, rows of pages wherever they
+// lie, with cp.async into a ring, 5 tiles of 32 KB at d = 128; one thread issues the products: S = Q K^T into tensor memory,
+// O += P V with P over the columns of S.  Rows that are not loaded (masked, pages out of range) are zeros in shared memory.
+template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_constant__ AttendArgs a) {
+    using Smem = AttendSmem<D>;
+    extern __shared__ __align__(1024) unsigned char att_smem[];
+    Smem& sm = *reinterpret_cast<Smem*>(att_smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), cta = blockIdx.x;
+    volatile int* gave_up = &sm.gave_up;
+    if (tid == 0) {
+        sm.gave_up = (smem_of(att_smem) & 1023) != 0;    // operands need the alignment
+        for (int i = 0; i < Smem::SLOTS; ++i) {
+            bar_init(smem_of(&sm.full[i]), ATT_LOAD_WARPS);
+            bar_init(smem_of(&sm.empty[i]), 1);
+        }
+        for (int i = 0; i < ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i]), ATT_LOAD_WARPS);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_of(&sm.q_ready[i]), 4);
+            bar_init(smem_of(&sm.s_ready[i]), 1);
+            bar_init(smem_of(&sm.p_ready[i]), 4);
+            bar_init(smem_of(&sm.o_ready[i]), 1);
+        }
+        bar_init(smem_of(&sm.drained), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_wait();
+    const long long units = a.head->units;
+    const long long u0 = share_begin(units, a.grid, cta), u1 = share_begin(units, a.grid, cta + 1);
+    pdl_start_next();
+    if (u0 == u1) {
+        if (tid == 0) a.flags[cta] = 0;
+        return;
+    }
+    if (warp == ATT_MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sm.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // what the roles keep from piece to piece
+    uint32_t loads = 0, tiles_done = 0;                  // loads issued (or consumed), tiles behind
+    uint32_t turns[2] = {0, 0};                          // tiles of a stream behind
+    uint32_t begun[2] = {0, 0};                          // pieces of a stream begun
+    bool ok = true;
+
+    for (int batch = 0;; ++batch) {
+        // ---- the pieces of this CTA, ATT_PIECES at a time ------------------------------------------
+        int listed = 0;
+        for (int e0 = 0; e0 < a.entries; e0 += ATT_THREADS) {
+            const int i = e0 + tid;
+            Entry e;
+            long long from = 0, to = 0, len = 1;
+            int count = 0, lines0 = 0, lines1 = 0;
+            // tiles of a line that units x0..x1-1 of it stand for
+            auto tiles_of = [&](long long x0, long long x1, int& t0, int& t1) {
+                t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0);
+                t1 = (int)(x1 > ATT_START ? x1 - ATT_START : 0);
+            };
+            auto range_of = [&](int line, int& t0, int& t1) {
+                const long long x0 = from > line * len ? from - line * len : 0, x1 = to < (line + 1) * len ? to - line * len : len;
+                tiles_of(x0, x1, t0, t1);
+            };
+            if (i < a.entries) {
+                e = a.entry[i];
+                len = line_units(e);
+                from = u0 > e.u ? u0 - e.u : 0;
+                const long long all = len * a.pg.H_kv * e.row_tiles;
+                to = u1 - e.u < all ? u1 - e.u : all;
+                if (to > from) {
+                    lines0 = (int)(from / len);
+                    lines1 = (int)((to - 1) / len);
+                    for (int line = lines0; line <= lines1; line = line == lines0 && lines1 > lines0 + 1 ? lines1 : line + 1) {
+                        int t0, t1;
+                        range_of(line, t0, t1);
+                        if (t1 > t0) count += (t1 - 1) / ATT_CHUNK - t0 / ATT_CHUNK + 1;
+                    }
+                    if (lines1 > lines0 + 1) count += (lines1 - lines0 - 1) * e.chunks;
+                }
+            }
+            // ordinal of this entry's first piece
+            int sum = count;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += y;
+            }
+            if (lane == 31) sm.warp_sum[warp] = sum;
+            __syncthreads();
+            int at = listed + sum - count - batch * ATT_PIECES, total = 0;
+            for (int w = 0; w <= ATT_MMA_WARP; ++w) {
+                if (w < warp) at += sm.warp_sum[w];
+                total += sm.warp_sum[w];
+            }
+            listed += total;
+            if (count > 0 && at < ATT_PIECES && at + count > 0) {
+                for (int line = lines0; line <= lines1 && at < ATT_PIECES; ++line) {
+                    int t0, t1;
+                    range_of(line, t0, t1);
+                    for (; t0 < t1; t0 = (t0 / ATT_CHUNK + 1) * ATT_CHUNK, ++at) {
+                        if (at < 0 || at >= ATT_PIECES) continue;
+                        const int chunk = t0 / ATT_CHUNK, end = (chunk + 1) * ATT_CHUNK < t1 ? (chunk + 1) * ATT_CHUNK : t1;
+                        Piece p;
+                        p.b = e.b;
+                        p.h = line / e.row_tiles;
+                        p.token = e.token;
+                        p.row0 = line % e.row_tiles * (2 * ATT_TILE);
+                        p.rows = e.rows - p.row0 < 2 * ATT_TILE ? e.rows - p.row0 : 2 * ATT_TILE;
+                        p.lo = e.lo;
+                        p.hi = e.hi;
+                        p.seen = e.seen;
+                        p.tile0 = e.tile0 + t0;
+                        p.tile1 = e.tile0 + end;
+                        const long long slot = (long long)e.item + (long long)line * e.chunks + chunk + cta;
+                        const bool own = i >= a.n_groups;
+                        p.half_rows = own ? a.own_rows : ATT_TILE;
+                        p.part = (own ? a.own_parts : a.shared_parts) + slot * 2 * half_floats(p.half_rows, D);
+                        sm.piece[at] = p;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        int pieces = listed - batch * ATT_PIECES;
+        pieces = pieces < ATT_PIECES ? pieces : ATT_PIECES;
+        if (batch == 0) {
+            tc_before_sync();
+            __syncthreads();
+            tc_after_sync();
+        }
+        if (pieces <= 0 || !ok) break;                   // (the same for all threads)
+        const uint32_t tmem = sm.tmem;
+
+        if (warp >= ATT_SOFT_WARPS && warp < ATT_MMA_WARP) {
+            // ---- loads ---------------------------------------------------------------------------
+            const int part = warp - ATT_SOFT_WARPS;      // rows 32 * part .. of a tile
+            // number of this lane's row of tile t, or ~0
+            auto look_up = [&](const Piece& p, int t) -> uint32_t {
+                int pos = t * ATT_TILE + part * 32 + lane;
+                if (pos < p.lo || pos >= p.hi) return ~0u;
+                if (a.blocks) {
+                    const int j = a.blocks[((long long)p.token * a.pg.H_kv + p.h) * a.keep + (pos >> a.block_shift)];
+                    if (j < 0 || j > (p.seen - 1) >> a.block_shift) return ~0u;
+                    pos = (j << a.block_shift) + (pos & (a.block - 1));
+                    if (pos >= p.seen) return ~0u;
+                }
+                const long long row = cache_row(a.pg, p.b, pos);
+                return row < 0 ? ~0u : (uint32_t)(row + (long long)p.h * a.pg.page_size);
+            };
+            auto arrive_full = [&](uint32_t load) {
+                fence_async();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_of(&sm.full[load % Smem::SLOTS]));
+            };
+            uint32_t unsignalled = 0;                    // loads of this batch that are not arrived yet
+            auto load = [&](const unsigned char* base, uint32_t row) -> bool {
+                constexpr int LANES = D / 8, RPI = 32 / LANES;          // lanes of a row, rows of an instruction
+                const uint32_t slot = loads % Smem::SLOTS, turn = loads / Smem::SLOTS;
+                if (!__all_sync(0xffffffffu, bar_wait(smem_of(&sm.empty[slot]), (turn & 1) ^ 1, gave_up))) return false;
+                const int c = lane % LANES;
+                const uint32_t dst = smem_of(sm.ring[slot]) + (c >> 3) * (ATT_TILE * 128);
+#pragma unroll
+                for (int i = 0; i < 32 / RPI; ++i) {
+                    const int r = part * 32 + i * RPI + lane / LANES;
+                    const uint32_t from = __shfl_sync(0xffffffffu, row, i * RPI + lane / LANES);
+                    const unsigned char* src = base + (from == ~0u ? 0 : (unsigned long long)from * (D * 2)) + c * 16;
+                    const int bytes = from == ~0u ? 0 : 16;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "l"(src), "r"(bytes) : "memory");
+                }
+                cp_async_commit();
+                ++loads;
+                if (++unsignalled > Smem::LAG) {
+                    cp_async_wait<Smem::LAG>();
+                    arrive_full(loads - unsignalled);
+                    --unsignalled;
+                }
+                return true;
+            };
+            uint32_t next = look_up(sm.piece[0], sm.piece[0].tile0);
+            for (int i = 0; i < pieces && ok; ++i) {
+                const Piece& p = sm.piece[i];
+                uint32_t before = ~0u;
+                for (int t = p.tile0; t < p.tile1 && ok; ++t) {
+                    const uint32_t row = next;
+                    if (t + 1 < p.tile1) next = look_up(p, t + 1);
+                    else if (i + 1 < pieces) next = look_up(sm.piece[i + 1], sm.piece[i + 1].tile0);
+                    // the mask of tile 8 back is no longer read: its softmax was over before the slots of this tile came free
+                    const uint32_t valid = __ballot_sync(0xffffffffu, row != ~0u);
+                    ok = load(a.pg.k, row);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        sm.mask[tiles_done % ATT_MASKS][part] = valid;
+                        bar_arrive(smem_of(&sm.mask_ready[tiles_done % ATT_MASKS]));
+                    }
+                    __syncwarp();
+                    ++tiles_done;
+                    if (t > p.tile0) ok = load(a.pg.v, before);
+                    before = row;
+                }
+                if (ok) ok = load(a.pg.v, before);
+            }
+            cp_async_wait<0>();
+            for (; ok && unsignalled > 0; --unsignalled) arrive_full(loads - unsignalled);
+        } else if (warp == ATT_MMA_WARP) {
+            // ---- products ------------------------------------------------------------------------
+            if (lane == 0) {
+                constexpr uint32_t QK = tc_shape<DT>(ATT_TILE, false), PV = tc_shape<DT>(D, true);
+                auto wait_full = [&](uint32_t load) { return bar_wait(smem_of(&sm.full[load % Smem::SLOTS]), load / Smem::SLOTS & 1, gave_up); };
+                for (int i = 0; i < pieces && ok; ++i) {
+                    const Piece& p = sm.piece[i];
+                    const int n = p.tile1 - p.tile0;
+                    const bool both = p.rows > ATT_TILE;
+                    // loads of a piece: K0, K1, V0, K2, V1, .. , V(n-2), V(n-1)
+                    auto k_load = [&](int t) { return loads + (t == 0 ? 0 : 2 * t - 1); };
+                    auto v_load = [&](int t) { return loads + (t == n - 1 ? 2 * n - 1 : 2 * t + 2); };
+                    auto weigh = [&](int t, int s) -> bool {             // O += P V of tile t
+                        if (!bar_wait(smem_of(&sm.p_ready[s]), turns[s] & 1, gave_up)) return false;
+                        if (!wait_full(v_load(t))) return false;
+                        tc_after_sync();
+                        const uint32_t v = smem_of(sm.ring[v_load(t) % Smem::SLOTS]);
+#pragma unroll
+                        for (int x = 0; x < ATT_TILE / 16; ++x)
+                            tc_mma_ts(tmem + 2 * ATT_TILE + s * D, tmem + s * ATT_TILE + x * 8, tc_operand(v + x * 2048, ATT_TILE * 128), PV,
+                                      x > 0 || t >= (both ? 1 : 2));
+                        tc_commit(smem_of(&sm.o_ready[s]));
+                        if (!both || s == 1) tc_commit(smem_of(&sm.empty[v_load(t) % Smem::SLOTS]));
+                        ++turns[s];
+                        return true;
+                    };
+                    for (int t = 0; t < n && ok; ++t) {
+                        for (int s = both ? 0 : t & 1; s <= (both ? 1 : t & 1) && ok; ++s) {
+                            const int last = both ? t - 1 : t - 2;
+                            if (last >= 0) {
+                                ok = weigh(last, s) && bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up);
+                            } else {
+                                ok = bar_wait(smem_of(&sm.q_ready[s]), begun[s] & 1, gave_up);
+                                ++begun[s];
+                            }
+                            ok = ok && wait_full(k_load(t));
+                            if (!ok) break;
+                            tc_after_sync();
+                            const uint32_t q = smem_of(sm.q[s]), k = smem_of(sm.ring[k_load(t) % Smem::SLOTS]);
+#pragma unroll
+                            for (int x = 0; x < D / 16; ++x) {
+                                const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
+                                tc_mma_ss(tmem + s * ATT_TILE, tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0);
+                            }
+                            tc_commit(smem_of(&sm.s_ready[s]));
+                            if (!both || s == 1) tc_commit(smem_of(&sm.empty[k_load(t) % Smem::SLOTS]));
+                        }
+                    }
+                    if (both) {
+                        ok = ok && weigh(n - 1, 0) && weigh(n - 1, 1);
+                    } else {
+                        if (n > 1) ok = ok && weigh(n - 2, (n - 2) & 1);
+                        ok = ok && weigh(n - 1, (n - 1) & 1);
+                    }
+                    loads += 2 * n;
+                }
+                if (!ok) {                               // what was issued ends before the memory is given back
+                    tc_commit(smem_of(&sm.drained));
+                    *gave_up = 0;
+                    bar_wait(smem_of(&sm.drained), 0, gave_up);
+                    *gave_up = 1;
+                }
+            }
+            __syncwarp();
+        } else {
+            // ---- softmax -------------------------------------------------------------------------
+            const int s = warp >> 2, row = (warp & 3) * 32 + lane;
+            const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+            const uint32_t S = lanes + s * ATT_TILE, O = lanes + 2 * ATT_TILE + s * D;
+            const float scale = fabsf(a.scale_log2);
+            for (int i = 0; i < pieces && ok; ++i) {
+                const Piece& p = sm.piece[i];
+                const int n = p.tile1 - p.tile0;
+                const bool both = p.rows > ATT_TILE;
+                const int mine = both ? (s == 0 ? ATT_TILE : p.rows - ATT_TILE) : p.rows;       // rows of this stream
+                const int turn_count = both ? n : (n + 1 - s) / 2;
+                const bool live = row < mine, warp_live = (warp & 3) * 32 < mine;
+                float* part = p.part + s * half_floats(p.half_rows, D);
+                float ref = ATT_NONE, l = 0.f;
+                if (turn_count > 0) {
+                    // queries; a negative scale turns their signs
+                    if (live) {
+                        const int r = p.row0 + (both ? s * ATT_TILE : 0) + row;
+                        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((long long)p.token + r / a.G) * a.q_stride + (long long)(p.h * a.G + r % a.G) * D);
+                        const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) {
+                            uint4 x = src[c];
+                            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+                            *reinterpret_cast<uint4*>(sm.q[s] + (c >> 3) * (ATT_TILE * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
+                        }
+                    }
+                    fence_async();
+                    tc_before_sync();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_of(&sm.q_ready[s]));
+                }
+                for (int k = 0; k < turn_count && ok; ++k) {
+                    const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.s_ready[s]), turns[s] & 1, gave_up) &&
+                                                     bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up));
+                    if (!ok) break;
+                    ++turns[s];
+                    if (warp_live) {
+                        tc_after_sync();
+                        uint32_t mask[4];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) mask[w] = sm.mask[tile % ATT_MASKS][w];
+                        const bool all = (mask[0] & mask[1] & mask[2] & mask[3]) == ~0u;
+                        uint32_t x[64];
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int w = 0; w < 4; w += 2) {
+                            tc_ld32(S + w * 32, x);
+                            tc_ld32(S + w * 32 + 32, x + 32);
+                            tc_wait_ld();
+                            if (all) {
+#pragma unroll
+                                for (int j = 0; j < 64; ++j) top = fmaxf(top, __uint_as_float(x[j]));
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 64; ++j)
+                                    if (mask[w + j / 32] >> (j % 32) & 1) top = fmaxf(top, __uint_as_float(x[j]));
+                            }
+                        }
+                        top *= scale;
+                        if (all || (mask[0] | mask[1] | mask[2] | mask[3])) top = fmaxf(top, ATT_LOW);
+                        // The reference follows the maximum when that is more than 8 above it: weights up to 2^8 fit
+                        // both types, and the sums in tensor memory are seldom touched.
+                        const bool follow = live && top > (ref == ATT_NONE ? ref : ref + 8.f);
+                        const float f = follow ? exp2_approx(ref - top) : 1.f;
+                        if (follow) ref = top;
+                        l *= f;
+                        if (k > 0 && __any_sync(0xffffffffu, follow)) {
+#pragma unroll
+                            for (int c = 0; c < D; c += 32) {
+                                tc_ld32(O + c, x);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f);
+                                tc_st32(O + c, x);
+                            }
+                        }
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int w = 0; w < 4; w += 2) {
+                            tc_ld32(S + w * 32, x);
+                            tc_ld32(S + w * 32 + 32, x + 32);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 64; j += 2) {
+                                float p0 = exp2_approx(fmaf(__uint_as_float(x[j]), scale, -ref));
+                                float p1 = exp2_approx(fmaf(__uint_as_float(x[j + 1]), scale, -ref));
+                                if (!all) {
+                                    if (!(mask[w + j / 32] >> (j % 32) & 1)) p0 = 0.f;
+                                    if (!(mask[w + j / 32] >> (j % 32 + 1) & 1)) p1 = 0.f;
+                                }
+                                sum[j / 2 & 3] += p0 + p1;
+                                x[j / 2] = pack2<DT>(p0, p1);
+                            }
+                            tc_st32(S + w * 16, x);
+                        }
+                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        tc_wait_st();
+                        tc_before_sync();
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s]));
+                }
+                // ---- the sums of this piece ------------------------------------------------------
+                if (ok && turn_count > 0) {
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up));
+                    if (ok && warp_live) {
+                        tc_after_sync();
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t x[32];
+                            tc_ld32(O + c, x);
+                            tc_wait_ld();
+                            if (live) {
+#pragma unroll
+                                for (int j = 0; j < 32; j += 4)
+                                    *reinterpret_cast<uint4*>(part + ((long long)((c + j) / 4) * p.half_rows + row) * 4) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                            }
+                        }
+                    }
+                }
+                if (live) *reinterpret_cast<float2*>(part + (long long)p.half_rows * D + 2 * row) = make_float2(ref, l);
+                tiles_done += n;
+            }
+        }
+        ok = !__syncthreads_or(!ok) && !*gave_up;
+        if (listed <= (batch + 1) * ATT_PIECES || !ok) break;
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (warp == ATT_MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sm.tmem) : "memory");
+    if (tid == 0) a.flags[cta] = !ok;
+}
+
+// ---------------------------------------------------------------------------------------
+// join_kernel
+// ---------------------------------------------------------------------------------------
+constexpr int JOIN_THREADS = 128;
+
+// A CTA for a KV head of one sequence (or token); four channels of a row to a thread.  The parts of a row
+// come in the order of the line, so that results do not depend on timing.
+template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttendArgs a) {
+    __shared__ float s_late[16 * 15 * 16];               // scores of the keys that the first token does not see
+    __shared__ long long s_late_row[15];
+    pdl_wait();
+    const int h = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
+    bool failed = false;
+    for (int c = tid; c < a.grid; c += JOIN_THREADS) failed |= a.flags[c] != 0;
+    failed = __syncthreads_or(failed);
+    const long long units = a.head->units;
+    const Entry own = a.entry[a.n_groups + i];
+    const int g = a.blocks ? -1 : a.group_of[i];
+    // later draft tokens: all queries are read before the first output is written, which may take their place
+    int late = 0;
+    if (!a.blocks && a.T > 1) {
+        const long long len = a.seq_lens[i], first = keys_seen(a.pg, len, a.T, 0), end = keys_seen(a.pg, len, a.T, a.T - 1);
+        late = (int)(end - first);
+        if (tid < late) {
+            const long long row = cache_row(a.pg, i, first + tid);
+            s_late_row[tid] = row < 0 ? -1 : row + (long long)h * a.pg.page_size;
+        }
+        __syncthreads();
+        for (int x = tid; x < own.rows * late; x += JOIN_THREADS) {
+            const int r = x / late, k = x % late;
+            // token t sees the keys below first + t where all tokens see some, else below len - T + 1 + t
+            if (first + k >= keys_seen(a.pg, len, a.T, r / a.G) || s_late_row[k] < 0) continue;
+            const uint16_t* key = reinterpret_cast<const uint16_t*>(a.pg.k) + s_late_row[k] * D;
+            const uint16_t* q = a.q + ((long long)own.token + r / a.G) * a.q_stride + (long long)(h * a.G + r % a.G) * D;
+            float s = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < D; c += 8) {
+                float kf[8], qf[8];
+                unpack8<DT>(*reinterpret_cast<const uint4*>(key + c), kf);
+                unpack8<DT>(*reinterpret_cast<const uint4*>(q + c), qf);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s = fmaf(qf[e], kf[e], s);
+            }
+            s_late[x] = s * a.scale_log2;
+        }
+        __syncthreads();
+    }
+    for (int x = tid; x < own.rows * (D / 4); x += JOIN_THREADS) {
+        const int r = x % own.rows, c4 = x / own.rows;
+        float M = ATT_NONE, L = 0.f;
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float m, float l, float4 o) {
+            const float top = fmaxf(M, m), f = exp2_approx(M - top), e = exp2_approx(m - top);
+            M = top;
+            L = L * f + l * e;
+            O.x = O.x * f + o.x * e;
+            O.y = O.y * f + o.y * e;
+            O.z = O.z * f + o.z * e;
+            O.w = O.w * f + o.w * e;
+        };
+        auto line_of = [&](const Entry& e, int row, const float* parts, int half_rows) {
+            const long long len = line_units(e);
+            if (len == 0) return;
+            const int m = row / (2 * ATT_TILE), line = h * e.row_tiles + m;
+            row -= m * (2 * ATT_TILE);
+            const int rows = e.rows - m * (2 * ATT_TILE) < 2 * ATT_TILE ? e.rows - m * (2 * ATT_TILE) : 2 * ATT_TILE;
+            const bool both = rows > ATT_TILE;
+            const long long first = e.u + line * len;
+            const int c1 = share_of(units, a.grid, first + len - 1);
+            for (int c = share_of(units, a.grid, first); c <= c1; ++c) {
+                const long long x0 = share_begin(units, a.grid, c) - first, x1 = share_begin(units, a.grid, c + 1) - first;
+                const int t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0), t1 = (int)((x1 < len ? x1 : len) - ATT_START);
+                if (t1 <= t0) continue;
+                for (int chunk = t0 / ATT_CHUNK; chunk <= (t1 - 1) / ATT_CHUNK; ++chunk) {
+                    const float* part = parts + ((long long)e.item + (long long)line * e.chunks + chunk + c) * 2 * half_floats(half_rows, D);
+                    for (int s = both ? row / ATT_TILE : 0; s <= (both ? row / ATT_TILE : 1); ++s) {
+                        const float* half = part + s * half_floats(half_rows, D);
+                        const int at = both ? row - s * ATT_TILE : row;
+                        const float2 ml = *reinterpret_cast<const float2*>(half + (long long)half_rows * D + 2 * at);
+                        if (ml.x == ATT_NONE) continue;
+                        add(ml.x, ml.y, *reinterpret_cast<const float4*>(half + ((long long)c4 * half_rows + at) * 4));
+                    }
+                }
+            }
+        };
+        if (g >= 0) {
+            const Entry e = a.entry[g];
+            if (own.hi >= e.hi) line_of(e, (own.token - e.token) * a.G + r, a.shared_parts, ATT_TILE);      // (not an empty sequence)
+        }
+        line_of(own, r, a.own_parts, a.own_rows);
+        const long long token = own.token + r / a.G;
+        const int hq = h * a.G + r % a.G;
+        if (late > 0) {
+            const long long len = a.seq_lens[i], first = keys_seen(a.pg, len, a.T, 0);
+            const int mine = (int)(keys_seen(a.pg, len, a.T, r / a.G) - first);
+            for (int k = 0; k < mine; ++k) {
+                if (s_late_row[k] < 0) continue;
+                const float s = s_late[r * late + k];
+                const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(a.pg.v) + s_late_row[k] * D + c4 * 4);
+                const float2 v0 = unpack2<DT>(v.x), v1 = unpack2<DT>(v.y);
+                if (s == -INFINITY) add(ATT_LOW, 0.f, make_float4(0.f, 0.f, 0.f, 0.f));
+                else add(s, 1.f, make_float4(v0.x, v0.y, v1.x, v1.y));
+            }
+        }
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (M != ATT_NONE) y = make_float4(O.x / L, O.y / L, O.z / L, O.w / L);
+        if (failed) y.x = y.y = y.z = y.w = __int_as_float(0x7fc00000);
+        const long long at = (token * a.Hq + hq) * D + c4 * 4;
+        *reinterpret_cast<uint2*>(a.out + at) = make_uint2(pack2<DT>(y.x, y.y), pack2<DT>(y.z, y.w));
+        if (a.lse && c4 == 0) a.lse[token * a.Hq + hq] = failed ? y.x : (M == ATT_NONE ? -INFINITY : (M + log2f(L)) * 0.69314718f);
+    }
+}
+
+}  // namespace retopk_cache

@@ -1,21 +1,12 @@
-// Device code for attention over 16-bit pages (sm_100a): groups of sequences that share a prefix, and
-// blocks of keys that a cheap score selects.
+// Device code that selects blocks of keys by a cheap score (sm_100a).
 //
 //   bounds_kernel   least and largest key of each block, channel by channel
 //   score_kernel    upper bound of a block's scores from its bounds
 //   pick_kernel     the blocks with the largest bounds
-//   attend_kernel   attention
 #pragma once
-#include "retopk_cache.cuh"
+#include "retopk_attend.cuh"
 
 namespace retopk_cache {
-
-// Keys that token t of T sees in a sequence of `len` keys; none if the cache cannot hold the sequence.
-__device__ __forceinline__ long long keys_seen(const Pages& pg, long long len, int T, int t) {
-    if (len < 0 || len > pg.capacity) return 0;
-    const long long n = len - T + 1 + t;
-    return n > 0 ? n : 0;
-}
 
 // ---------------------------------------------------------------------------------------
 // bounds_kernel
@@ -237,75 +228,6 @@ __global__ void __launch_bounds__(PICK_THREADS) pick_kernel(const __grid_constan
         taken += total & 65535;
         equal += total >> 16;
     }
-}
-
-// ---------------------------------------------------------------------------------------
-// attend_kernel
-// ---------------------------------------------------------------------------------------
-struct AttendArgs {
-    Pages pg;
-    const int32_t* seq_lens;
-    const uint16_t* q;
-    long long q_stride;
-    uint16_t* out;
-    float* lse;
-    float scale_log2;
-    int B, T, Hq, G;
-    const int32_t* blocks;      // [B, T, H_kv, keep] or null: all keys
-    int keep, block;
-};
-constexpr int ATTEND_THREADS = 128, ATTEND_WARPS = ATTEND_THREADS / 32;
-
-// A CTA for a token and head, a warp for every fourth key.
-template <int DT, int D> __global__ void __launch_bounds__(ATTEND_THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
-    constexpr int PER = D / 32;
-    __shared__ float s_o[ATTEND_WARPS][D], s_m[ATTEND_WARPS], s_l[ATTEND_WARPS];
-    pdl_wait();
-    const int hq = blockIdx.x, t = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int h = hq / a.G;
-    const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, t);
-    const long long N = (seen + a.block - 1) / a.block;
-    const int32_t* list = a.blocks ? a.blocks + (((long long)b * a.T + t) * a.pg.H_kv + h) * a.keep : nullptr;
-    const long long keys = list ? (N < a.keep ? N : a.keep) * a.block : seen;
-    float q[PER], o[PER] = {}, m = -INFINITY, l = 0.f;
-    for (int i = 0; i < PER; ++i) q[i] = to_f32<DT>(a.q[((long long)b * a.T + t) * a.q_stride + hq * D + lane * PER + i]);
-    for (long long i = warp; i < keys; i += ATTEND_WARPS) {
-        long long pos = i;
-        if (list) {
-            const int j = list[i / a.block];
-            if (j < 0 || j >= N) continue;
-            pos = (long long)j * a.block + i % a.block;
-            if (pos >= seen) continue;
-        }
-        const long long row = cache_row(a.pg, b, pos);
-        if (row < 0) continue;
-        const long long at = (row + (long long)h * a.pg.page_size) * D + lane * PER;
-        const uint16_t *k = reinterpret_cast<const uint16_t*>(a.pg.k) + at, *v = reinterpret_cast<const uint16_t*>(a.pg.v) + at;
-        float s = 0.f;
-        for (int e = 0; e < PER; ++e) s = fmaf(q[e], to_f32<DT>(k[e]), s);
-        for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= a.scale_log2;
-        const float top = fmaxf(m, s), f = m == -INFINITY ? 0.f : exp2f(m - top), p = s == -INFINITY ? 0.f : exp2f(s - top);
-        m = top;
-        l = l * f + p;
-        for (int e = 0; e < PER; ++e) o[e] = o[e] * f + p * to_f32<DT>(v[e]);
-    }
-    for (int e = 0; e < PER; ++e) s_o[warp][lane * PER + e] = o[e];
-    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float M = -INFINITY, L = 0.f, O = 0.f;
-    for (int w = 0; w < ATTEND_WARPS; ++w) M = fmaxf(M, s_m[w]);
-    for (int w = 0; w < ATTEND_WARPS; ++w) {
-        const float f = s_m[w] == -INFINITY ? 0.f : exp2f(s_m[w] - M);
-        L += f * s_l[w];
-        O += f * s_o[w][threadIdx.x];
-    }
-    const long long row = ((long long)b * a.T + t) * a.Hq + hq;
-    const float x = L == 0.f ? 0.f : O / L;
-    const uint32_t bits = pack2<DT>(x, x);
-    a.out[row * D + threadIdx.x] = (uint16_t)bits;
-    if (a.lse && threadIdx.x == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718f;
 }
 
 }  // namespace retopk_cache

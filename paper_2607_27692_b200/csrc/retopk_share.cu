@@ -1,8 +1,9 @@
 // Host side of the attention over 16-bit pages and of the selection of blocks: argument checks, launches,
 // C interface.
-#include "retopk_share.cuh"
+#include "retopk_blocks.cuh"
 
 #include <math.h>
+#include <mutex>
 
 #include "retopk_cache_host.cuh"
 
@@ -16,9 +17,55 @@ int check_shape(int B, int T, int H_q, int H_kv, int d) {
     return RETOPK_OK;
 }
 
+// SM count, and the attention kernels' opt-in to large shared memory; once per device.
+constexpr int MAX_DEVICES = 64;
+struct DeviceSetup { bool ready; int num_sms; };
+DeviceSetup g_setup[MAX_DEVICES];
+std::mutex g_setup_mutex;
+
+template <int DT, int D> bool opt_in() {
+    return cudaFuncSetAttribute(attend_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>)) == cudaSuccess;
+}
+int device_sms(int* num_sms) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return RETOPK_ECUDA; }
+    if (dev < 0 || dev >= MAX_DEVICES) return RETOPK_EUNSUPPORTED;
+    std::lock_guard<std::mutex> lock(g_setup_mutex);
+    DeviceSetup& st = g_setup[dev];
+    if (!st.ready) {
+        if (cudaDeviceGetAttribute(&st.num_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            !opt_in<TYPE_BF16, 64>() || !opt_in<TYPE_BF16, 128>() || !opt_in<TYPE_FP16, 64>() || !opt_in<TYPE_FP16, 128>()) {
+            cudaGetLastError();
+            return RETOPK_ECUDA;
+        }
+        st.ready = true;
+    }
+    *num_sms = st.num_sms;
+    return RETOPK_OK;
+}
+
+// The workspace: where its parts begin, and its size.  `sequences`: entries that belong to one sequence or token,
+// `rows` query rows each; `keys`: the most keys that an entry can have.
+struct Workspace { int64_t entry, group_of, flags, shared_parts, own_parts, bytes; };
+Workspace lay_out(int64_t sequences, int64_t rows, int64_t n_groups, int64_t group_rows, int64_t H_kv, int d, int64_t keys, int grid) {
+    auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
+    const int64_t tiles = (keys + ATT_TILE - 1) / ATT_TILE, chunks = (tiles + ATT_CHUNK - 1) / ATT_CHUNK;
+    const int64_t own = sequences * H_kv * chunks + grid;
+    // groups of x rows in all have at most one row tile each more than x / 256
+    const int64_t shared = n_groups ? H_kv * chunks * (n_groups + group_rows / (2 * ATT_TILE)) + grid : 0;
+    Workspace w;
+    w.entry = up(sizeof(AttendHeader));
+    w.group_of = w.entry + up((n_groups + sequences) * (int64_t)sizeof(Entry));
+    w.flags = w.group_of + up(sequences * 4);
+    w.shared_parts = w.flags + up(grid * 4);
+    w.own_parts = w.shared_parts + up(shared * 2 * half_floats(ATT_TILE, d) * 4);
+    w.bytes = w.own_parts + up(own * 2 * half_floats((int)(rows < ATT_TILE ? rows : ATT_TILE), d) * 4);
+    return w;
+}
+
 // What both attentions refuse alike, and their arguments.
 int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, const void* q, int64_t q_stride,
-                    float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, int64_t need, AttendArgs& a) {
+                    float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, AttendArgs& a) {
     if (pages->format == RETOPK_PAGES_Q4 || !seq_lens || !out || !workspace || !isfinite(scale)) return RETOPK_EINVAL;
     const int d = pages->d;
     if (!rows_ok(q, q_stride, H_q, d) || !aligned16(workspace) || !aligned16(out)) return RETOPK_EINVAL;
@@ -32,7 +79,6 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     const Memory q_m = memory_of(qi, n, d), out_m = memory_of(qo, n, d), lse_m = {lse, (uint64_t)n * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
     if (!in_place_or_apart(qi, qo, n, d) || !all_apart(out_m, pg) || !all_apart(lse_m, pg) || !all_apart(ws_m, pg)) return RETOPK_EINVAL;
     if (!all_apart(lse_m, {out_m, q_m, ws_m}) || !all_apart(ws_m, {out_m, q_m})) return RETOPK_EINVAL;
-    if (workspace_bytes < need) return RETOPK_EINVAL;
     a.seq_lens = seq_lens;
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_stride;
@@ -43,11 +89,49 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     return RETOPK_OK;
 }
 
-int launch_attend(const AttendArgs& a, const retopk_pages_t* pages, cudaStream_t s) {
-    const dim3 grid((unsigned)a.Hq, (unsigned)a.T, (unsigned)a.B);
+template <int DT, int D> int launch_attention(const AttendArgs& a, int sequences, cudaStream_t s) {
+    int rc = launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, a);
+    if (rc != RETOPK_OK) return rc;
+    rc = launch(attend_kernel<DT, D>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, a);
+    if (rc != RETOPK_OK) return rc;
+    return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences), JOIN_THREADS, 0, s, a);
+}
+int run_attention(AttendArgs& a, const retopk_pages_t* pages, int sequences, int rows, const Workspace& w, int grid, void* workspace, cudaStream_t s) {
+    char* ws = static_cast<char*>(workspace);
+    a.head = reinterpret_cast<AttendHeader*>(ws);
+    a.entry = reinterpret_cast<Entry*>(ws + w.entry);
+    a.group_of = reinterpret_cast<int32_t*>(ws + w.group_of);
+    a.flags = reinterpret_cast<int32_t*>(ws + w.flags);
+    a.shared_parts = reinterpret_cast<float*>(ws + w.shared_parts);
+    a.own_parts = reinterpret_cast<float*>(ws + w.own_parts);
+    a.entries = a.n_groups + sequences;
+    a.grid = grid;
+    a.own_rows = rows < ATT_TILE ? rows : ATT_TILE;
     if (pages->format == RETOPK_PAGES_BF16)
-        return launch(pages->d == 128 ? attend_kernel<TYPE_BF16, 128> : attend_kernel<TYPE_BF16, 64>, grid, ATTEND_THREADS, 0, s, a);
-    return launch(pages->d == 128 ? attend_kernel<TYPE_FP16, 128> : attend_kernel<TYPE_FP16, 64>, grid, ATTEND_THREADS, 0, s, a);
+        return pages->d == 128 ? launch_attention<TYPE_BF16, 128>(a, sequences, s) : launch_attention<TYPE_BF16, 64>(a, sequences, s);
+    return pages->d == 128 ? launch_attention<TYPE_FP16, 128>(a, sequences, s) : launch_attention<TYPE_FP16, 64>(a, sequences, s);
+}
+
+int shared_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, int* grid) {
+    int rc = check_shape(B, T, H_q, H_kv, d);
+    if (rc != RETOPK_OK) return rc;
+    if (n_groups < 0 || n_groups > B || max_keys < 1) return RETOPK_EINVAL;
+    if (max_keys > MAX_KEYS) return RETOPK_EUNSUPPORTED;
+    rc = device_sms(grid);
+    if (rc != RETOPK_OK) return rc;
+    const int rows = T * (H_q / H_kv);
+    *w = lay_out(B, rows, n_groups, (int64_t)B * rows, H_kv, d, max_keys, *grid);
+    return RETOPK_OK;
+}
+int block_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, int* grid) {
+    int rc = check_shape(B, T, H_q, H_kv, d);
+    if (rc != RETOPK_OK) return rc;
+    if (max_keys < 1) return RETOPK_EINVAL;
+    if (max_keys > MAX_KEYS + 127) return RETOPK_EUNSUPPORTED;
+    rc = device_sms(grid);
+    if (rc != RETOPK_OK) return rc;
+    *w = lay_out((int64_t)B * T, H_q / H_kv, 0, 0, H_kv, d, max_keys, *grid);
+    return RETOPK_OK;
 }
 
 template <class Args, class F> int by_type(const retopk_pages_t* p, F bf128, F bf64, F fp128, F fp64, dim3 grid, unsigned threads, cudaStream_t s, const Args& a) {
@@ -59,11 +143,11 @@ template <class Args, class F> int by_type(const retopk_pages_t* p, F bf128, F b
 
 extern "C" {
 
-int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d) {
-    const int rc = check_shape(B, T, H_q, H_kv, d);
-    if (rc != RETOPK_OK) return rc;
-    if (n_groups < 0 || n_groups > B) return RETOPK_EINVAL;
-    return 16;
+int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys) {
+    Workspace w;
+    int grid;
+    const int rc = shared_workspace(B, n_groups, T, H_q, H_kv, d, max_keys, &w, &grid);
+    return rc == RETOPK_OK ? w.bytes : rc;
 }
 
 int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, int n_groups,
@@ -71,14 +155,22 @@ int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, 
                             void* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
     int rc = check_pages(pages, B);
     if (rc != RETOPK_OK) return rc;
-    const int64_t need = retopk_shared_attention_workspace(B, n_groups, T, H_q, pages->H_kv, pages->d);
-    if (need < 0) return (int)need;
-    if (n_groups > 0 && (!cu_groups || !shared_lens)) return RETOPK_EINVAL;
-    AttendArgs a;
-    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, need, a);
+    rc = check_shape(B, T, H_q, pages->H_kv, pages->d);
     if (rc != RETOPK_OK) return rc;
-    a.block = 16;
-    return launch_attend(a, pages, static_cast<cudaStream_t>(stream));
+    if (n_groups < 0 || n_groups > B || (n_groups > 0 && (!cu_groups || !shared_lens))) return RETOPK_EINVAL;
+    AttendArgs a;
+    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
+    if (rc != RETOPK_OK) return rc;
+    if (workspace_bytes < 4096) return RETOPK_EINVAL;    // (refused without a device too)
+    Workspace w;
+    int grid;
+    rc = shared_workspace(B, n_groups, T, H_q, pages->H_kv, pages->d, a.pg.capacity, &w, &grid);
+    if (rc != RETOPK_OK) return rc;
+    if (workspace_bytes < w.bytes) return RETOPK_EINVAL;
+    a.n_groups = n_groups;
+    a.cu = cu_groups;
+    a.shared_lens = shared_lens;
+    return run_attention(a, pages, B, T * a.G, w, grid, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, int B, const int32_t* seq_lens, int64_t n_new, void* stream) {
@@ -146,11 +238,16 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
     return launch(pick_kernel, dim3((unsigned)pages->H_kv, (unsigned)T, (unsigned)B), PICK_THREADS, 0, s, a);
 }
 
-int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep) {
-    const int rc = check_shape(B, T, H_q, H_kv, d);
-    if (rc != RETOPK_OK) return rc;
-    if (keep < 1) return RETOPK_EINVAL;
-    return 16;
+int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep, int block) {
+    const int rc0 = check_shape(B, T, H_q, H_kv, d);
+    if (rc0 != RETOPK_OK) return rc0;
+    if (keep < 1 || block < 1) return RETOPK_EINVAL;
+    if (keep > MAX_KEYS || block > 128) return RETOPK_EUNSUPPORTED;
+    const int64_t keys = (int64_t)keep * block, most = MAX_KEYS + block - 1;
+    Workspace w;
+    int grid;
+    const int rc = block_workspace(B, T, H_q, H_kv, d, keys < most ? keys : most, &w, &grid);
+    return rc == RETOPK_OK ? w.bytes : rc;
 }
 
 int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T, int H_q, const int32_t* seq_lens, int keep,
@@ -159,20 +256,27 @@ int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T,
     int rc = check_pages(pages, B);
     if (rc != RETOPK_OK) return rc;
     if (block != 16 && block != 32 && block != 64 && block != 128) return RETOPK_EUNSUPPORTED;
-    const int64_t need = retopk_block_attention_workspace(B, T, H_q, pages->H_kv, pages->d, keep);
-    if (need < 0) return (int)need;
-    if (!blocks || pages->page_size % block != 0) return RETOPK_EINVAL;
+    rc = check_shape(B, T, H_q, pages->H_kv, pages->d);
+    if (rc != RETOPK_OK) return rc;
+    if (keep < 1 || !blocks || pages->page_size % block != 0) return RETOPK_EINVAL;
     if (keep > MAX_KEYS) return RETOPK_EUNSUPPORTED;
     AttendArgs a;
-    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, need, a);
+    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
     if (rc != RETOPK_OK) return rc;
     const Memory blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
     const Memory out_m = {out, (uint64_t)B * T * H_q * pages->d * 2}, lse_m = {lse, (uint64_t)B * T * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
-    if (!all_apart(blocks_m, {out_m, lse_m, ws_m})) return RETOPK_EINVAL;
+    if (!all_apart(blocks_m, {out_m, lse_m, ws_m}) || workspace_bytes < 4096) return RETOPK_EINVAL;
+    const int64_t keys = (int64_t)keep * block, most = MAX_KEYS + block - 1;
+    Workspace w;
+    int grid;
+    rc = block_workspace(B, T, H_q, pages->H_kv, pages->d, keys < most ? keys : most, &w, &grid);
+    if (rc != RETOPK_OK) return rc;
+    if (workspace_bytes < w.bytes) return RETOPK_EINVAL;
     a.blocks = blocks;
     a.keep = keep;
     a.block = block;
-    return launch_attend(a, pages, static_cast<cudaStream_t>(stream));
+    a.block_shift = __builtin_ctz((unsigned)block);
+    return run_attention(a, pages, B * T, a.G, w, grid, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

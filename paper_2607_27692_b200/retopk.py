@@ -74,13 +74,13 @@ SIGNATURES = {
     "retopk_pool_free": (_i32, [_vp, _i32, _vp, _vp, _i64, _i32, _vp, _vp]),
     "retopk_pool_compact": (_i32, [_vp, _i32, _vp, _vp, _i64, _vp, _vp, _vp]),
     "retopk_pages_copy": (_i32, [_vp, _i64, _vp, _vp, _vp, _vp]),
-    "retopk_shared_attention_workspace": (_i64, [_i32] * 6),
+    "retopk_shared_attention_workspace": (_i64, [_i32] * 6 + [_i64]),
     "retopk_shared_attention": (_i32, [_vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _i64, _f32, _vp, _vp, _vp, _i64, _vp]),
     "retopk_block_update": (_i32, [_vp, _i32, _vp, _i32, _vp, _i64, _vp]),
     "retopk_block_copy": (_i32, [_vp, _i32, _vp, _i64, _vp, _vp, _vp]),
     "retopk_block_select_workspace": (_i64, [_i32] * 5 + [_i64]),
     "retopk_block_select": (_i32, [_vp, _i32, _vp, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _i64, _vp]),
-    "retopk_block_attention_workspace": (_i64, [_i32] * 6),
+    "retopk_block_attention_workspace": (_i64, [_i32] * 7),
     "retopk_block_attention": (_i32, [_vp, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _f32, _vp, _vp, _vp, _i64, _vp]),
     "retopk_strerror": (C.c_char_p, [_i32]),
 }

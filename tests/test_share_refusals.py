@@ -113,8 +113,8 @@ def test_attention_refusals(lib):  # noqa: F811
     for kw in (dict(keep=0), dict(list=None), dict(block=128), dict(list=X + M), dict(list=X + 2 * M)):
         assert blocks(**kw) == EINVAL, kw
     assert blocks(block=8) == EUNSUPPORTED
-    assert lib.retopk_shared_attention_workspace(3, 4, 1, 4, 2, 128) == EINVAL
-    assert lib.retopk_block_attention_workspace(3, 1, 4, 2, 96, 4) == EUNSUPPORTED
+    assert lib.retopk_shared_attention_workspace(3, 4, 1, 4, 2, 128, 1000) == EINVAL
+    assert lib.retopk_block_attention_workspace(3, 1, 4, 2, 96, 4, 16) == EUNSUPPORTED
 
 
 def test_select_refusals(lib):  # noqa: F811
