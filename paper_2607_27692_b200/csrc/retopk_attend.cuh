@@ -246,6 +246,10 @@ __device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t* x) {
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : TC_R8(x, 0), TC_R8(x, 8), TC_R8(x, 16), TC_R8(x, 24) : "r"(addr));
 }
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8) : "memory");
+}
 __device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* x) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
                  "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
@@ -255,6 +259,20 @@ __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Two fp32 operations at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 
 // Shared memory operand with rows of 128 bytes, 16-byte columns exchanged within 8 rows (128-byte swizzle);
@@ -288,8 +306,8 @@ template <int D> struct AttendSmem {
     static constexpr int LAG = SLOTS - 2;                // loads in flight before one is waited for
     unsigned char q[2][TILE_BYTES];
     unsigned char ring[SLOTS][TILE_BYTES];
-    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2], p_ready[2], o_ready[2], drained;
     uint32_t mask[ATT_MASKS][4];
+    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2], p_ready[2], o_ready[2], drained;
     Piece piece[ATT_PIECES];
     int warp_sum[ATT_MMA_WARP + 2];
     uint32_t tmem;
@@ -533,6 +551,8 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
                             } else {
                                 ok = bar_wait(smem_of(&sm.q_ready[s]), begun[s] & 1, gave_up);
                                 ++begun[s];
+                                // (the weights of the piece before are read)
+                                if (turns[s] > 0) ok = ok && bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up);
                             }
                             ok = ok && wait_full(k_load(t));
                             if (!ok) break;
@@ -568,33 +588,45 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
             const int s = warp >> 2, row = (warp & 3) * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
             const uint32_t S = lanes + s * ATT_TILE, O = lanes + 2 * ATT_TILE + s * D;
-            const float scale = fabsf(a.scale_log2);
+            // (a scale of 0 as the smallest: 0 times the -inf of a hidden key is no number)
+            const float scale = a.scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.scale_log2);
+            // rows and tiles of this stream in a piece
+            auto rows_of = [&](const Piece& p) { return p.rows <= ATT_TILE ? p.rows : (s == 0 ? ATT_TILE : p.rows - ATT_TILE); };
+            auto turns_of = [&](const Piece& p) { return p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
+            auto fetch_q = [&](const Piece& p) {
+                const int r = p.row0 + (p.rows > ATT_TILE ? s * ATT_TILE : 0) + row;
+                const uint16_t* src = a.q + ((long long)p.token + r / a.G) * a.q_stride + (long long)(p.h * a.G + r % a.G) * D;
+                const uint32_t dst = smem_of(sm.q[s]) + row * 128;
+                if (row < rows_of(p)) {
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) cp_async16(dst + (c >> 3) * (ATT_TILE * 128) + (((c & 7) ^ (row & 7)) << 4), src + c * 8);
+                }
+                cp_async_commit();
+            };
+            int fetched = -1;                            // piece whose queries are on their way
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
                 const bool both = p.rows > ATT_TILE;
-                const int mine = both ? (s == 0 ? ATT_TILE : p.rows - ATT_TILE) : p.rows;       // rows of this stream
-                const int turn_count = both ? n : (n + 1 - s) / 2;
+                const int mine = rows_of(p), turn_count = turns_of(p);
                 const bool live = row < mine, warp_live = (warp & 3) * 32 < mine;
                 float* part = p.part + s * half_floats(p.half_rows, D);
                 float ref = ATT_NONE, l = 0.f;
-                if (turn_count > 0) {
-                    // queries; a negative scale turns their signs
-                    if (live) {
-                        const int r = p.row0 + (both ? s * ATT_TILE : 0) + row;
-                        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((long long)p.token + r / a.G) * a.q_stride + (long long)(p.h * a.G + r % a.G) * D);
-                        const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-#pragma unroll
+                auto give_q = [&]() {
+                    cp_async_wait<0>();
+                    if (a.scale_log2 < 0.f && row < rows_of(sm.piece[fetched]))         // a negative scale turns the queries' signs
                         for (int c = 0; c < D / 8; ++c) {
-                            uint4 x = src[c];
-                            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
-                            *reinterpret_cast<uint4*>(sm.q[s] + (c >> 3) * (ATT_TILE * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
+                            uint4* x = reinterpret_cast<uint4*>(sm.q[s] + (c >> 3) * (ATT_TILE * 128) + row * 128 + ((c & 7) << 4));
+                            x->x ^= 0x80008000u; x->y ^= 0x80008000u; x->z ^= 0x80008000u; x->w ^= 0x80008000u;
                         }
-                    }
                     fence_async();
-                    tc_before_sync();
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_of(&sm.q_ready[s]));
+                };
+                if (turn_count > 0 && fetched < i) {
+                    fetched = i;
+                    fetch_q(p);
+                    give_q();
                 }
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
@@ -602,38 +634,78 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
                                                      bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up));
                     if (!ok) break;
                     ++turns[s];
+                    const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
+                    if (ahead) {                         // the queries of this piece have been read: the next one's take their place
+                        fetched = i + 1;
+                        fetch_q(sm.piece[i + 1]);
+                    }
                     if (warp_live) {
                         tc_after_sync();
-                        uint32_t mask[4];
+                        uint32_t x[32], y[32];
+                        const uint4 mask4 = *reinterpret_cast<const uint4*>(sm.mask[tile % ATT_MASKS]);
+                        const bool all = (mask4.x & mask4.y & mask4.z & mask4.w) == ~0u;
+                        auto hide = [&](uint32_t* v, int c) {            // keys that do not count: weight 0
+                            if (all) return;
+                            const uint32_t m = sm.mask[tile % ATT_MASKS][c];
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) mask[w] = sm.mask[tile % ATT_MASKS][w];
-                        const bool all = (mask[0] & mask[1] & mask[2] & mask[3]) == ~0u;
-                        uint32_t x[64];
-                        float top = -INFINITY;
+                            for (int j = 0; j < 32; ++j)
+                                if (!(m >> j & 1)) v[j] = 0xff800000u;
+                        };
+                        // The maximum, 32 columns at a time, the next ones on their way.  (Loops, not all of it unrolled:
+                        // a tile's code once through is otherwise more than the instruction caches feed.)
+                        float top0 = -INFINITY, top1 = -INFINITY;
+                        auto largest = [&](uint32_t* v, int c) {
+                            hide(v, c);
 #pragma unroll
-                        for (int w = 0; w < 4; w += 2) {
-                            tc_ld32(S + w * 32, x);
-                            tc_ld32(S + w * 32 + 32, x + 32);
-                            tc_wait_ld();
-                            if (all) {
-#pragma unroll
-                                for (int j = 0; j < 64; ++j) top = fmaxf(top, __uint_as_float(x[j]));
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 64; ++j)
-                                    if (mask[w + j / 32] >> (j % 32) & 1) top = fmaxf(top, __uint_as_float(x[j]));
+                            for (int j = 0; j < 32; j += 4) {
+                                top0 = fmaxf(top0, fmaxf(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
+                                top1 = fmaxf(top1, fmaxf(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])));
                             }
+                        };
+                        tc_ld32(S, x);
+#pragma unroll 1
+                        for (int c = 0; c < 4; c += 2) {
+                            tc_wait_ld();
+                            tc_ld32(S + c * 32 + 32, y);
+                            largest(x, c);
+                            tc_wait_ld();
+                            tc_ld32(S + (c == 0 ? 64 : 0), x);           // (at the end the first ones again, for the weights)
+                            largest(y, c + 1);
                         }
-                        top *= scale;
-                        if (all || (mask[0] | mask[1] | mask[2] | mask[3])) top = fmaxf(top, ATT_LOW);
+                        float top = fmaxf(top0, top1) * scale;
+                        if (all || (mask4.x | mask4.y | mask4.z | mask4.w)) top = fmaxf(top, ATT_LOW);
                         // The reference follows the maximum when that is more than 8 above it: weights up to 2^8 fit
                         // both types, and the sums in tensor memory are seldom touched.
                         const bool follow = live && top > (ref == ATT_NONE ? ref : ref + 8.f);
                         const float f = follow ? exp2_approx(ref - top) : 1.f;
                         if (follow) ref = top;
-                        l *= f;
-                        if (k > 0 && __any_sync(0xffffffffu, follow)) {
+                        float2 sum = make_float2(0.f, 0.f), more = make_float2(0.f, 0.f);
+                        const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
+                        auto weights = [&](uint32_t* v, int c) {
+                            hide(v, c);
 #pragma unroll
+                            for (int j = 0; j < 32; j += 2) {
+                                float2 p = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale2, ref2);
+                                p.x = exp2_approx(p.x);
+                                p.y = exp2_approx(p.y);
+                                if (j & 2) more = add2(more, p);
+                                else sum = add2(sum, p);
+                                v[j / 2] = pack2<DT>(p.x, p.y);
+                            }
+                            tc_st16(S + c * 16, v);
+                        };
+#pragma unroll 1
+                        for (int c = 0; c < 4; c += 2) {
+                            tc_wait_ld();
+                            tc_ld32(S + c * 32 + 32, y);
+                            weights(x, c);
+                            tc_wait_ld();
+                            if (c == 0) tc_ld32(S + 64, x);
+                            weights(y, c + 1);
+                        }
+                        l = l * f + ((sum.x + sum.y) + (more.x + more.y));
+                        if (k > 0 && __any_sync(0xffffffffu, follow)) {
+#pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 tc_ld32(O + c, x);
                                 tc_wait_ld();
@@ -642,38 +714,19 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
                                 tc_st32(O + c, x);
                             }
                         }
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int w = 0; w < 4; w += 2) {
-                            tc_ld32(S + w * 32, x);
-                            tc_ld32(S + w * 32 + 32, x + 32);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 64; j += 2) {
-                                float p0 = exp2_approx(fmaf(__uint_as_float(x[j]), scale, -ref));
-                                float p1 = exp2_approx(fmaf(__uint_as_float(x[j + 1]), scale, -ref));
-                                if (!all) {
-                                    if (!(mask[w + j / 32] >> (j % 32) & 1)) p0 = 0.f;
-                                    if (!(mask[w + j / 32] >> (j % 32 + 1) & 1)) p1 = 0.f;
-                                }
-                                sum[j / 2 & 3] += p0 + p1;
-                                x[j / 2] = pack2<DT>(p0, p1);
-                            }
-                            tc_st32(S + w * 16, x);
-                        }
-                        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                         tc_wait_st();
                         tc_before_sync();
                     }
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s]));
+                    if (ahead) give_q();
                 }
                 // ---- the sums of this piece ------------------------------------------------------
                 if (ok && turn_count > 0) {
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up));
                     if (ok && warp_live) {
                         tc_after_sync();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             uint32_t x[32];
                             tc_ld32(O + c, x);
@@ -686,6 +739,7 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
                         }
                     }
                 }
+                tc_before_sync();
                 if (live) *reinterpret_cast<float2*>(part + (long long)p.half_rows * D + 2 * row) = make_float2(ref, l);
                 tiles_done += n;
             }
@@ -702,18 +756,19 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
 // ---------------------------------------------------------------------------------------
 // join_kernel
 // ---------------------------------------------------------------------------------------
-constexpr int JOIN_THREADS = 128;
+constexpr int JOIN_THREADS = 512, JOIN_LIST = 256, JOIN_DEEP = 4;
 
-// A CTA for a KV head of one sequence (or token); four channels of a row to a thread.  The parts of a row
-// come in the order of the line, so that results do not depend on timing.
+// A CTA for a KV head of one sequence (or token).  First the parts that hold its rows are listed: those of the
+// group's line (its rows may lie across two), and those of its own.  Then four channels of a row go to a
+// thread, or to several that share the parts.  All orders are fixed, so that results do not depend on timing.
 template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttendArgs a) {
     __shared__ float s_late[16 * 15 * 16];               // scores of the keys that the first token does not see
     __shared__ long long s_late_row[15];
+    __shared__ const float* s_list[3][JOIN_LIST];
+    __shared__ float s_sum[6][JOIN_THREADS];
     pdl_wait();
     const int h = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
-    bool failed = false;
-    for (int c = tid; c < a.grid; c += JOIN_THREADS) failed |= a.flags[c] != 0;
-    failed = __syncthreads_or(failed);
+    const bool failed = __syncthreads_or(tid < a.grid && a.flags[tid] != 0);
     const long long units = a.head->units;
     const Entry own = a.entry[a.n_groups + i];
     const int g = a.blocks ? -1 : a.group_of[i];
@@ -729,7 +784,6 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
         __syncthreads();
         for (int x = tid; x < own.rows * late; x += JOIN_THREADS) {
             const int r = x / late, k = x % late;
-            // token t sees the keys below first + t where all tokens see some, else below len - T + 1 + t
             if (first + k >= keys_seen(a.pg, len, a.T, r / a.G) || s_late_row[k] < 0) continue;
             const uint16_t* key = reinterpret_cast<const uint16_t*>(a.pg.k) + s_late_row[k] * D;
             const uint16_t* q = a.q + ((long long)own.token + r / a.G) * a.q_stride + (long long)(h * a.G + r % a.G) * D;
@@ -744,9 +798,50 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
             }
             s_late[x] = s * a.scale_log2;
         }
-        __syncthreads();
     }
-    for (int x = tid; x < own.rows * (D / 4); x += JOIN_THREADS) {
+    // the parts of row tile m of an entry; how many
+    auto list_line = [&](const Entry& e, int m, const float* parts, int half_rows, const float** list) -> int {
+        const long long len = line_units(e);
+        if (len == 0) return 0;
+        const int line = h * e.row_tiles + m;
+        const long long first = e.u + line * len;
+        const int c0 = share_of(units, a.grid, first), c1 = share_of(units, a.grid, first + len - 1);
+        int count = 0;
+        const int c = c0 + tid;                          // (a CTA of the other kernel to a thread: grid <= JOIN_LIST - 16)
+        int t0 = 0, t1 = 0;
+        if (c <= c1) {
+            const long long x0 = share_begin(units, a.grid, c) - first, x1 = share_begin(units, a.grid, c + 1) - first;
+            t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0);
+            t1 = (int)((x1 < len ? x1 : len) - ATT_START);
+            if (t1 > t0) count = (t1 - 1) / ATT_CHUNK - t0 / ATT_CHUNK + 1;
+        }
+        int total;
+        const int at = scan_cta<JOIN_THREADS>(count, &total);
+        for (int k = 0; k < count; ++k)
+            list[at + k] = parts + ((long long)e.item + (long long)line * e.chunks + t0 / ATT_CHUNK + k + c) * 2 * half_floats(half_rows, D);
+        return total;
+    };
+    int shared_row = 0, n_first = 0, n_second = 0, m0 = 0;
+    Entry group;
+    group.rows = 0;
+    if (g >= 0) {
+        group = a.entry[g];
+        shared_row = (own.token - group.token) * a.G;
+        m0 = shared_row / (2 * ATT_TILE);
+        if (own.hi >= group.hi) {                        // (not an empty sequence)
+            n_first = list_line(group, m0, a.shared_parts, ATT_TILE, s_list[0]);
+            if ((shared_row + own.rows - 1) / (2 * ATT_TILE) > m0) n_second = list_line(group, m0 + 1, a.shared_parts, ATT_TILE, s_list[1]);
+        }
+    }
+    const int n_own = list_line(own, 0, a.own_parts, a.own_rows, s_list[2]);
+    __syncthreads();
+
+    const int work = own.rows * (D / 4);
+    int splits = 1;
+    while (2 * splits * work <= JOIN_THREADS) splits *= 2;
+    for (int x0 = 0; x0 < work; x0 += JOIN_THREADS) {
+        const int split = splits > 1 ? tid / work : 0, x = x0 + (splits > 1 ? tid % work : tid);
+        const bool on = x < work && split < splits;
         const int r = x % own.rows, c4 = x / own.rows;
         float M = ATT_NONE, L = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -759,36 +854,47 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
             O.z = O.z * f + o.z * e;
             O.w = O.w * f + o.w * e;
         };
-        auto line_of = [&](const Entry& e, int row, const float* parts, int half_rows) {
-            const long long len = line_units(e);
-            if (len == 0) return;
-            const int m = row / (2 * ATT_TILE), line = h * e.row_tiles + m;
-            row -= m * (2 * ATT_TILE);
-            const int rows = e.rows - m * (2 * ATT_TILE) < 2 * ATT_TILE ? e.rows - m * (2 * ATT_TILE) : 2 * ATT_TILE;
-            const bool both = rows > ATT_TILE;
-            const long long first = e.u + line * len;
-            const int c1 = share_of(units, a.grid, first + len - 1);
-            for (int c = share_of(units, a.grid, first); c <= c1; ++c) {
-                const long long x0 = share_begin(units, a.grid, c) - first, x1 = share_begin(units, a.grid, c + 1) - first;
-                const int t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0), t1 = (int)((x1 < len ? x1 : len) - ATT_START);
-                if (t1 <= t0) continue;
-                for (int chunk = t0 / ATT_CHUNK; chunk <= (t1 - 1) / ATT_CHUNK; ++chunk) {
-                    const float* part = parts + ((long long)e.item + (long long)line * e.chunks + chunk + c) * 2 * half_floats(half_rows, D);
-                    for (int s = both ? row / ATT_TILE : 0; s <= (both ? row / ATT_TILE : 1); ++s) {
-                        const float* half = part + s * half_floats(half_rows, D);
-                        const int at = both ? row - s * ATT_TILE : row;
-                        const float2 ml = *reinterpret_cast<const float2*>(half + (long long)half_rows * D + 2 * at);
-                        if (ml.x == ATT_NONE) continue;
-                        add(ml.x, ml.y, *reinterpret_cast<const float4*>(half + ((long long)c4 * half_rows + at) * 4));
+        // `halves` of each part from half `h0` on hold the row, at `at`
+        auto add_list = [&](const float** list, int count, int half_rows, int at, int h0, int halves) {
+            const int all = count * halves;
+            for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
+                float2 ml[JOIN_DEEP];
+                float4 o[JOIN_DEEP];
+#pragma unroll
+                for (int d = 0; d < JOIN_DEEP; ++d) {
+                    const int k = k0 + d * splits;
+                    ml[d].x = ATT_NONE;
+                    if (k < all) {
+                        const float* half = list[halves == 2 ? k >> 1 : k] + (h0 + (halves == 2 ? k & 1 : 0)) * half_floats(half_rows, D);
+                        ml[d] = *reinterpret_cast<const float2*>(half + (long long)half_rows * D + 2 * at);
+                        o[d] = *reinterpret_cast<const float4*>(half + ((long long)c4 * half_rows + at) * 4);
                     }
                 }
+#pragma unroll
+                for (int d = 0; d < JOIN_DEEP; ++d)
+                    if (ml[d].x != ATT_NONE) add(ml[d].x, ml[d].y, o[d]);
             }
         };
-        if (g >= 0) {
-            const Entry e = a.entry[g];
-            if (own.hi >= e.hi) line_of(e, (own.token - e.token) * a.G + r, a.shared_parts, ATT_TILE);      // (not an empty sequence)
+        if (on) {
+            if (n_first + n_second > 0) {
+                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), at = row % (2 * ATT_TILE);
+                const bool both = group.rows - (m0 + m) * (2 * ATT_TILE) > ATT_TILE;
+                add_list(s_list[m], m == 0 ? n_first : n_second, ATT_TILE, both ? at % ATT_TILE : at, both ? at / ATT_TILE : 0, both ? 1 : 2);
+            }
+            const bool both = own.rows > ATT_TILE;
+            add_list(s_list[2], n_own, a.own_rows, both ? r % ATT_TILE : r, both ? r / ATT_TILE : 0, both ? 1 : 2);
         }
-        line_of(own, r, a.own_parts, a.own_rows);
+        if (splits > 1) {
+            s_sum[0][tid] = M; s_sum[1][tid] = L;
+            s_sum[2][tid] = O.x; s_sum[3][tid] = O.y; s_sum[4][tid] = O.z; s_sum[5][tid] = O.w;
+            __syncthreads();
+            if (on && split == 0)
+                for (int k = 1; k < splits; ++k) {
+                    const int y = tid + k * work;
+                    if (s_sum[0][y] != ATT_NONE) add(s_sum[0][y], s_sum[1][y], make_float4(s_sum[2][y], s_sum[3][y], s_sum[4][y], s_sum[5][y]));
+                }
+        }
+        if (!on || split > 0) continue;
         const long long token = own.token + r / a.G;
         const int hq = h * a.G + r % a.G;
         if (late > 0) {

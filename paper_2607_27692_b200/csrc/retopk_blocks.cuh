@@ -84,92 +84,315 @@ struct SelectArgs {
     const uint16_t* bounds;
     const uint16_t* q;
     long long q_stride;
-    float* scores;              // [B, T, H_kv, max_blocks]
+    float2* scores;             // [B, T, H_kv, max_blocks]: a score in fp32 and how far it may be off
     long long max_blocks;
     int32_t* blocks;            // [B, T, H_kv, keep]
 };
-constexpr int SCORE_THREADS = 128, SCORE_BLOCKS = 32, SCORE_COLS = 4;
-constexpr int PICK_THREADS = 512;
+constexpr int SCORE_THREADS = 128, SCORE_WARPS = SCORE_THREADS / 32, SCORE_ROWS = 16, SCORE_COLS = 8;
+constexpr int PICK_THREADS = 512, PICK_WARPS = PICK_THREADS / 32, PICK_KEPT = 4096, PICK_LIST = 512;
 
-// Four threads to a block of keys, a share of the channels each; sums of exact products in 64 bits, so that
-// the order of blocks does not hang on the order of additions.
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
+
+// Scores in fp32, and a bound on their errors; pick_kernel works out exactly those that the bound leaves open.
+// (All of them in 64 bits were 22 us at 4 x 8 x 2048 blocks of 128 channels and 4 queries, against 5 for reading the bounds.)
+//
+// max(q lo, q hi) = q+ hi + q- lo with the positive and the negative part of q.  A warp has 16 blocks as the rows
+// of A, up to 8 queries as the columns of B.  The channels that a lane loads at once (8 of 32) are
+// those that it holds in A and in B of two products: sums do not care for their order.
+// Error: products of 16-bit numbers are exact in fp32.  2 D / 16 products of depth 16, each of whose additions cuts off
+// at most 2^-23 of what was summed so far, below sum |q| times the largest |bound| of the block: 2^-23 * 17 * 2 D / 16 <= 2^-14
+// of that for D = 128.
 template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_kernel(const __grid_constant__ SelectArgs a) {
-    __shared__ double s_q[SCORE_COLS][D];
+    constexpr int STEPS = D / 32;
+    __shared__ float s_score[SCORE_WARPS][SCORE_COLS][SCORE_ROWS], s_size[SCORE_WARPS][SCORE_COLS];
     pdl_wait();
     pdl_start_next();
-    const int b = blockIdx.z, h = blockIdx.y, sub = threadIdx.x & 3;
-    const long long j = (long long)blockIdx.x * SCORE_BLOCKS + (threadIdx.x >> 2);
-    const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, a.T - 1), N = (seen + a.block - 1) / a.block;
-    if (N <= a.keep || (long long)blockIdx.x * SCORE_BLOCKS >= N - a.last) return;
-    uint4 lo[D / 32], hi[D / 32];
-    bool on = j < N - a.last;
-    if (on) {
-        const long long row = cache_row(a.pg, b, j * a.block);
-        on = row >= 0;
-        if (on) {
-            const uint16_t* src = a.bounds + (row + (long long)h * a.pg.page_size) / a.block * (2 * D);
+    const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, part = lane & 3;
+    const int j0 = (blockIdx.x * SCORE_WARPS + warp) * SCORE_ROWS;
+    const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, a.T - 1), end = (seen + a.block - 1) / a.block - a.last;
+    if (end + a.last <= a.keep || j0 >= end) return;
+    uint4 lo[2][STEPS], hi[2][STEPS];
+    bool none[2];
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                lo[i] = *reinterpret_cast<const uint4*>(src + (4 * i + sub) * 8);
-                hi[i] = *reinterpret_cast<const uint4*>(src + D + (4 * i + sub) * 8);
+    for (int y = 0; y < 2; ++y) {
+        const int j = j0 + g + 8 * y;
+        const long long r = j < end ? cache_row(a.pg, b, (long long)j * a.block) : -1;
+        none[y] = r < 0;
+        const uint16_t* src = a.bounds + (none[y] ? 0 : (r + (long long)h * a.pg.page_size) / a.block * (2 * D)) + part * 8;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            lo[y][i] = hi[y][i] = make_uint4(0, 0, 0, 0);
+            if (!none[y]) {
+                lo[y][i] = *reinterpret_cast<const uint4*>(src + i * 32);
+                hi[y][i] = *reinterpret_cast<const uint4*>(src + D + i * 32);
             }
         }
     }
-    float best = 0.f;
-    for (int c0 = 0; c0 < a.T * a.G; c0 += SCORE_COLS) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < SCORE_COLS * D; i += SCORE_THREADS) {
-            const int c = c0 + i / D;
-            double x = 0.0;
-            if (c < a.T * a.G) x = to_f32<DT>(a.q[((long long)b * a.T + c / a.G) * a.q_stride + (h * a.G + c % a.G) * D + i % D]);
-            s_q[i / D][i % D] = x;
+    float largest[2];                                     // of the bounds' magnitudes
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = __vmaxu2(__vmaxu2(m, word(lo[y][i], w) & 0x7fff7fffu), word(hi[y][i], w) & 0x7fff7fffu);
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const float2 f = unpack2<DT>(m);
+        largest[y] = f.x != f.x || f.y != f.y ? INFINITY : fmaxf(f.x, f.y);
+    }
+    const int cols = a.T * a.G;
+    float best = 0.f, size = 0.f;
+    for (int c0 = 0; c0 < cols; c0 += SCORE_COLS) {
+        float c[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+        const int col = c0 + g;
+        const uint16_t* q = a.q + ((long long)b * a.T + col / a.G) * a.q_stride + (h * a.G + col % a.G) * D + part * 8;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const uint4 x = col < cols ? *reinterpret_cast<const uint4*>(q + i * 32) : make_uint4(0, 0, 0, 0);
+            uint32_t up[4], down[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                up[w] = max2_nan<DT>(word(x, w), 0u);
+                down[w] = min2_nan<DT>(word(x, w), 0u);
+                const float2 f = unpack2<DT>(word(x, w));
+                sum += fabsf(f.x) + fabsf(f.y);
+            }
+#pragma unroll
+            for (int w = 0; w < 4; w += 2) {
+                mma16816<DT>(c, word(hi[0][i], w), word(hi[1][i], w), word(hi[0][i], w + 1), word(hi[1][i], w + 1), up[w], up[w + 1]);
+                mma16816<DT>(c, word(lo[0][i], w), word(lo[1][i], w), word(lo[0][i], w + 1), word(lo[1][i], w + 1), down[w], down[w + 1]);
+            }
         }
-        __syncthreads();
-        double acc[SCORE_COLS] = {};
-        if (on) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (part == 0) s_size[warp][g] = sum;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                float l[8], u[8];
-                unpack8<DT>(lo[i], l);
-                unpack8<DT>(hi[i], u);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const double dl = l[e], du = u[e];
-#pragma unroll
-                    for (int c = 0; c < SCORE_COLS; ++c) {
-                        const double q = s_q[c][(4 * i + sub) * 8 + e];
-                        acc[c] = fma(q, q < 0.0 ? dl : du, acc[c]);
-                    }
+        for (int y = 0; y < 2; ++y) {
+            s_score[warp][2 * part][g + 8 * y] = c[2 * y];
+            s_score[warp][2 * part + 1][g + 8 * y] = c[2 * y + 1];
+        }
+        __syncwarp();
+        // lane x < 16: block x of the warp
+        const int from = (lane & 7) * 4;
+        const float most0 = __shfl_sync(0xffffffffu, largest[0], from), most1 = __shfl_sync(0xffffffffu, largest[1], from);
+        const int none0 = __shfl_sync(0xffffffffu, (int)none[0], from), none1 = __shfl_sync(0xffffffffu, (int)none[1], from);
+        if (lane < SCORE_ROWS && j0 + lane < end) {
+            const float most = lane & 8 ? most1 : most0;
+            const bool out = (lane & 8 ? none1 : none0) != 0;
+            for (int k = 0; k < SCORE_COLS && c0 + k < cols; ++k) {
+                const int head = (c0 + k) % a.G;
+                const float s = s_score[warp][k][lane], z = s_size[warp][k];
+                best = head == 0 ? s : fmaxf(best, s);
+                size = head == 0 ? z : (z != z ? z : fmaxf(size, z));
+                if (head == a.G - 1) {
+                    float off = size * most * 0x1p-14f + 1e-35f;
+                    if (!(off < 1e37f) || !(fabsf(best) < 1e37f)) off = INFINITY;
+                    a.scores[(((long long)b * a.T + (c0 + k) / a.G) * a.pg.H_kv + h) * a.max_blocks + j0 + lane] =
+                        out ? make_float2(-INFINITY, 0.f) : (off == INFINITY ? make_float2(0.f, INFINITY) : make_float2(best, off));
                 }
             }
         }
-#pragma unroll
-        for (int c = 0; c < SCORE_COLS; ++c) {
-            acc[c] += __shfl_xor_sync(0xffffffffu, acc[c], 1);
-            acc[c] += __shfl_xor_sync(0xffffffffu, acc[c], 2);
-            if (c0 + c >= a.T * a.G) break;
-            float s = (float)acc[c];
-            if (!on) s = -INFINITY;
-            else if (s != s) s = INFINITY;
-            const int g = (c0 + c) % a.G;
-            best = g == 0 ? s : fmaxf(best, s);
-            if (g == a.G - 1 && sub == 0 && j < N - a.last)
-                a.scores[(((long long)b * a.T + (c0 + c) / a.G) * a.pg.H_kv + h) * a.max_blocks + j] = best;
-        }
+        __syncwarp();
     }
 }
 
-// Order of scores as unsigned numbers.
+// Order of scores as unsigned numbers, from 1 on.
 __device__ __forceinline__ uint32_t order_of(float s) {
     const uint32_t u = __float_as_uint(s + 0.f);          // (-0 becomes 0)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One CTA for a token and KV head: the threshold byte by byte, then the numbers above it, ascending.
-__global__ void __launch_bounds__(PICK_THREADS) pick_kernel(const __grid_constant__ SelectArgs a) {
-    __shared__ int s_hist[256], s_digit, s_above;
+// The want-th largest of the CTA's numbers: `limit`, and how many of those equal to it are among the want.  Each thread calls
+// f for its numbers.  Digits of what the numbers have above the least of them, 8 bits at a time; without EXACT over when
+// a digit's numbers are all taken (then the limit is at most the want-th largest, and above all that are smaller).
+template <bool EXACT, class Each> __device__ __forceinline__ void find_limit(Each each, int want, uint32_t* limit, int* rest_out) {
+    __shared__ int s_hist[256], s_digit, s_above, s_inside;
+    __shared__ uint32_t s_low[PICK_WARPS], s_high[PICK_WARPS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t low = ~0u, high = 0;
+    each([&](uint32_t u) {
+        low = u < low ? u : low;
+        high = u > high ? u : high;
+    });
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    __syncthreads();
+    if (lane == 0) { s_low[warp] = low; s_high[warp] = high; }
+    __syncthreads();
+    low = __reduce_min_sync(0xffffffffu, s_low[lane % PICK_WARPS]);
+    high = __reduce_max_sync(0xffffffffu, s_high[lane % PICK_WARPS]);
+    int bits = high > low ? 32 - __clz(high - low) : 0;
+    uint32_t prefix = 0;                                  // digits known so far, of u - low
+    int rest = want, shift = bits;
+    while (shift > 0) {
+        const int width = shift < 8 ? shift : 8, next = shift - width;
+        for (int i = tid; i < 256; i += PICK_THREADS) s_hist[i] = 0;
+        __syncthreads();
+        each([&](uint32_t u) {
+            u -= low;
+            if (shift == bits || u >> shift == prefix) atomicAdd(&s_hist[(u >> next) & ((1 << width) - 1)], 1);
+        });
+        __syncthreads();
+        if (warp == 0) {                                  // from the largest digit down, 8 digits to a lane
+            int digits[8], mine = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) mine += digits[k] = s_hist[255 - (lane * 8 + k)];
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += y;
+            }
+            int above = sum - mine;
+            if (above < rest && rest <= sum) {
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (!found && above + digits[k] >= rest) {
+                        found = true;
+                        s_digit = 255 - (lane * 8 + k);
+                        s_above = above;
+                        s_inside = digits[k];
+                    }
+                    above += digits[k];
+                }
+            }
+        }
+        __syncthreads();
+        prefix = prefix << width | (uint32_t)s_digit;
+        rest -= s_above;
+        shift = next;
+        if (!EXACT && s_inside == rest) break;                      // all that share the digits so far: the limit is the least of them
+        __syncthreads();
+    }
+    *limit = low + (prefix << shift);
+    // cut short: numbers of the last digit may lie above the limit; they are taken as larger ones, none as equal
+    *rest_out = shift > 0 ? 0x7fffffff : rest;
+}
+
+// The score of block j for the heads of a group, in 64 bits and rounded once to fp32; by a warp.
+template <int DT, int D> __device__ __forceinline__ float exact_score(const SelectArgs& a, int b, int t, int h, int j) {
+    constexpr int PER = D / 32, HEADS = 4;
+    const int lane = threadIdx.x & 31;
+    const long long r = cache_row(a.pg, b, (long long)j * a.block);
+    if (r < 0) return -INFINITY;
+    const uint16_t* src = a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + lane * PER;
+    const uint16_t* q = a.q + ((long long)b * a.T + t) * a.q_stride + (long long)h * a.G * D + lane * PER;
+    double lo[PER], hi[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        lo[e] = to_f32<DT>(src[e]);
+        hi[e] = to_f32<DT>(src[D + e]);
+    }
+    float score = 0.f;
+    for (int g0 = 0; g0 < a.G; g0 += HEADS) {
+        uint16_t x[HEADS][PER];
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[k][e] = g0 + k < a.G ? q[(g0 + k) * D + e] : 0;
+        double sum[HEADS] = {};
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const double y = to_f32<DT>(x[k][e]), p = y * lo[e], z = y * hi[e];
+                sum[k] += p != p || z != z ? p + z : (p > z ? p : z);
+            }
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < HEADS; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            float f = (float)sum[k];
+            f = f != f ? INFINITY : f;
+            if (g0 + k < a.G) score = g0 + k == 0 ? f : fmaxf(score, f);
+        }
+    }
+    return score;
+}
+
+// Scores i of a token and KV head: the first ones in shared memory.
+struct Scores {
+    float2 *kept, *rest;
+    __device__ __forceinline__ float2& operator[](int i) const { return i < PICK_KEPT ? kept[i] : rest[i]; }
+};
+
+// Any number of blocks to choose from, any number of equal scores.  A block whose upper end
+// is below the want-th largest lower end is out, and one whose lower end is above the (want + 1)-th largest
+// upper end is in; those between are scored exactly.
+template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs& a, Scores at, int b, int t, int h, int m, int want, int32_t* out) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    uint32_t lowest, limit;
+    int rest;
+    find_limit<false>([&](auto f) {
+        for (int i = tid; i < m; i += PICK_THREADS) f(order_of(__fsub_rd(at[i].x, at[i].y)));
+    }, want, &lowest, &rest);
+    int left = 0, all_left;
+    for (int i = tid; i < m; i += PICK_THREADS) left += order_of(__fadd_ru(at[i].x, at[i].y)) >= lowest;
+    scan_cta<PICK_THREADS>(left, &all_left);
+    uint32_t highest = 0;                                 // (as many left as wanted: all of them are in)
+    if (all_left > want)
+        find_limit<true>([&](auto f) {
+            for (int i = tid; i < m; i += PICK_THREADS) {
+                const uint32_t u = order_of(__fadd_ru(at[i].x, at[i].y));
+                if (u >= lowest) f(u);
+            }
+        }, want + 1, &highest, &rest);
+
+    // From here on x holds a number's bits: 0 for a block that is out, the largest for one that is in, else the order
+    // of its exact score.
+#pragma unroll 1
+    for (int i0 = 0; i0 < m; i0 += PICK_THREADS) {
+        const int i = i0 + tid;
+        const float2 s = i < m ? at[i] : make_float2(0.f, 0.f);
+        const bool some = i < m && order_of(__fadd_ru(s.x, s.y)) >= lowest, in = some && order_of(__fsub_rd(s.x, s.y)) > highest;
+        uint32_t mine = in ? ~0u : 0u;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, some && !in); todo; todo &= todo - 1) {
+            const int x = __ffs(todo) - 1, j = a.first + (i - lane) + x;
+            const float score = exact_score<DT, D>(a, b, t, h, j);
+            if (lane == x) mine = order_of(score);
+        }
+        if (i < m) at[i].x = __uint_as_float(mine);
+    }
+    __syncthreads();
+    limit = 1;
+    rest = 0x7fffffff;
+    if (all_left > want)
+        find_limit<false>([&](auto f) {
+            for (int i = tid; i < m; i += PICK_THREADS) {
+                const uint32_t u = __float_as_uint(at[i].x);
+                if (u) f(u);
+            }
+        }, want, &limit, &rest);
+    // taken: above the limit, or equal to it and among the first `rest` of those
+    int taken = 0, equal = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < m; i0 += PICK_THREADS) {
+        const int i = i0 + tid;
+        const uint32_t u = i < m ? __float_as_uint(at[i].x) : 0;
+        const bool eq = i < m && u == limit, gt = i < m && u > limit;
+        int total;
+        const int before = scan_cta<PICK_THREADS>((int)gt | (int)eq << 16, &total);
+        const int e = equal + (before >> 16), place = taken + (before & 65535) + (e < rest ? e : rest);
+        if (gt || (eq && e < rest)) out[a.first + place] = a.first + i;
+        taken += total & 65535;
+        equal += total >> 16;
+    }
+}
+
+// One CTA for a token and KV head; `want` blocks are to be chosen, whose scores are known as intervals.  A bin of the want-th
+// largest lower end gives a limit that few blocks reach with their upper end; among those, each is compared with
+// all others, and those that stay open are scored exactly.
+template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick_kernel(const __grid_constant__ SelectArgs a) {
+    constexpr int BITS = 10, BINS = 1 << BITS, DEEP = PICK_KEPT / PICK_THREADS;
+    __shared__ float2 s_kept[PICK_KEPT];
+    __shared__ int s_bin[BINS], s_cand[PICK_LIST], s_count, s_found[3];
+    __shared__ uint32_t s_lower[PICK_LIST], s_upper[PICK_LIST], s_key[PICK_LIST], s_low[PICK_WARPS], s_high[PICK_WARPS];
     pdl_wait();
-    const int h = blockIdx.x, t = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+    const int h = blockIdx.x, t = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, t);
     const int N = (int)((seen + a.block - 1) / a.block);
     const long long item = ((long long)b * a.T + t) * a.pg.H_kv + h;
@@ -182,51 +405,122 @@ __global__ void __launch_bounds__(PICK_THREADS) pick_kernel(const __grid_constan
     for (int i = tid; i < a.first; i += PICK_THREADS) out[i] = i;
     for (int i = tid; i < a.last; i += PICK_THREADS) out[a.keep - a.last + i] = N - a.last + i;
     if (want == 0) return;
-    const float* scores = a.scores + item * a.max_blocks + a.first;
-    uint32_t limit = 0;                                   // digits of the want-th largest, as far as they are known
-    int rest = want;                                      // how many of those that share them are taken
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += PICK_THREADS) s_hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < m; i += PICK_THREADS) {
-            const uint32_t u = order_of(scores[i]);
-            if (shift == 24 || u >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&s_hist[(u >> shift) & 255], 1);
-        }
-        __syncthreads();
-        if (tid < 32) {                                   // from the largest digit down, 8 digits to a lane
-            int mine = 0;
-            for (int k = 0; k < 8; ++k) mine += s_hist[255 - (tid * 8 + k)];
-            int sum = mine;
+    const Scores at = {s_kept, a.scores + item * a.max_blocks + a.first};
+    auto lower = [](float2 s) { return order_of(__fsub_rd(s.x, s.y)); };
+    auto upper = [](float2 s) { return order_of(__fadd_ru(s.x, s.y)); };
+    {
+        uint32_t low = ~0u, high = 0;
+        float2 x[DEEP];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, sum, o);
-                if (tid >= o) sum += y;
+        for (int k = 0; k < DEEP; ++k)
+            if (k * PICK_THREADS + tid < m) x[k] = at.rest[k * PICK_THREADS + tid];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+            if (k * PICK_THREADS + tid < m) {
+                s_kept[k * PICK_THREADS + tid] = x[k];
+                low = min(low, lower(x[k]));
+                high = max(high, lower(x[k]));
             }
-            int above = sum - mine;
-            if (above < rest && rest <= sum) {
-                int k = 0;
-                while (above + s_hist[255 - (tid * 8 + k)] < rest) above += s_hist[255 - (tid * 8 + k++)];
-                s_digit = 255 - (tid * 8 + k);
-                s_above = above;
-            }
+        for (int i = PICK_KEPT + tid; i < m; i += PICK_THREADS) {
+            low = min(low, lower(at.rest[i]));
+            high = max(high, lower(at.rest[i]));
+        }
+        low = __reduce_min_sync(0xffffffffu, low);
+        high = __reduce_max_sync(0xffffffffu, high);
+        if (lane == 0) { s_low[warp] = low; s_high[warp] = high; }
+    }
+    for (int i = tid; i < BINS; i += PICK_THREADS) s_bin[i] = 0;
+    if (tid == 0) s_count = 0;
+    __syncthreads();
+    const uint32_t low = __reduce_min_sync(0xffffffffu, s_low[lane % PICK_WARPS]), high = __reduce_max_sync(0xffffffffu, s_high[lane % PICK_WARPS]);
+    // bins, BITS of what the lower ends have above the least of them at a time, until one holds few
+    const int bits = high > low ? 32 - __clz(high - low) : 0;
+    uint32_t prefix = 0;
+    int rest = want, shift = bits;
+    while (shift > 0) {
+        const int width = shift < BITS ? shift : BITS, next = shift - width;
+        for (int i = tid; i < m; i += PICK_THREADS) {
+            const uint32_t u = lower(at[i]) - low;
+            if (shift == bits || u >> shift == prefix) atomicAdd(&s_bin[(u >> next) & (BINS - 1)], 1);
         }
         __syncthreads();
-        limit |= (uint32_t)s_digit << shift;
-        rest -= s_above;
+        constexpr int PER = BINS / PICK_THREADS;          // bins of a thread, from the largest down
+        int n[PER], mine = 0, total;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            mine += n[k] = s_bin[BINS - 1 - (tid * PER + k)];
+            s_bin[BINS - 1 - (tid * PER + k)] = 0;
+        }
+        int above = scan_cta<PICK_THREADS>(mine, &total);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (above < rest && rest <= above + n[k]) {
+                s_found[0] = BINS - 1 - (tid * PER + k);
+                s_found[1] = above;
+                s_found[2] = n[k];
+            }
+            above += n[k];
+        }
+        __syncthreads();
+        prefix = prefix << width | (uint32_t)s_found[0];
+        rest -= s_found[1];
+        shift = next;
+        if (s_found[2] <= 32) break;
         __syncthreads();
     }
-    // taken: above the limit, or equal to it and among the first `rest` of those
-    int taken = 0, equal = 0;
+    const uint32_t limit = low + (prefix << shift);
+    // the blocks that reach the limit
     for (int i0 = 0; i0 < m; i0 += PICK_THREADS) {
         const int i = i0 + tid;
-        const uint32_t u = i < m ? order_of(scores[i]) : 0;
-        const bool eq = i < m && u == limit, gt = i < m && u > limit;
-        int total;
-        const int before = scan_cta<PICK_THREADS>((int)gt | (int)eq << 16, &total);
-        const int e = equal + (before >> 16), at = taken + (before & 65535) + (e < rest ? e : rest);
-        if (gt || (eq && e < rest)) out[a.first + at] = a.first + i;
-        taken += total & 65535;
-        equal += total >> 16;
+        const float2 s = i < m ? at[i] : make_float2(0.f, 0.f);
+        const bool in = i < m && upper(s) >= limit;
+        const uint32_t who = __ballot_sync(0xffffffffu, in);
+        int base = 0;
+        if (lane == 0 && who) base = atomicAdd(&s_count, __popc(who));
+        base = __shfl_sync(0xffffffffu, base, 0) + __popc(who & ((1u << lane) - 1));
+        if (in && base < PICK_LIST) {
+            s_cand[base] = i;
+            s_lower[base] = lower(s);
+            s_upper[base] = upper(s);
+        }
+    }
+    __syncthreads();
+    const int C = s_count;
+    if (C > PICK_LIST) {
+        pick_any<DT, D>(a, at, b, t, h, m, want, out);
+        return;
+    }
+    // a key for each: the largest for one that is in, 0 for one that is out, 1 for one that is open
+    for (int c = tid; c < C; c += PICK_THREADS) {
+        int rivals = 0, better = 0;
+        if (C > want)
+            for (int k = 0; k < C; ++k) {
+                rivals += s_upper[k] >= s_lower[c];
+                better += s_lower[k] > s_upper[c];
+            }
+        s_key[c] = rivals <= want ? ~0u : (better >= want ? 0u : 1u);
+    }
+    __syncthreads();
+    for (int c = warp; c < C; c += PICK_WARPS)
+        if (s_key[c] == 1u) {
+            const float score = exact_score<DT, D>(a, b, t, h, a.first + s_cand[c]);
+            __syncwarp();
+            if (lane == 0) s_key[c] = order_of(score);
+        }
+    __syncthreads();
+    for (int c = tid; c < C; c += PICK_THREADS) {
+        const uint32_t u = s_key[c];
+        int rank = 0;
+        if (C > want)
+            for (int k = 0; k < C; ++k) rank += s_key[k] > u || (s_key[k] == u && s_cand[k] < s_cand[c]);
+        s_lower[c] = rank < want;
+    }
+    __syncthreads();
+    for (int c = tid; c < C; c += PICK_THREADS) {
+        if (!s_lower[c]) continue;
+        int place = 0;
+        for (int k = 0; k < C; ++k) place += s_lower[k] && s_cand[k] < s_cand[c];
+        out[a.first + place] = a.first + s_cand[c];
     }
 }
 

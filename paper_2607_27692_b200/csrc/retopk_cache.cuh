@@ -85,7 +85,7 @@ template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile(
 
 // Sum over the threads before this one, and over all; every thread of the CTA calls it.
 template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total) {
-    __shared__ int s_part[THREADS / 32 + 1];
+    __shared__ int s_part[THREADS / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int sum = x;
 #pragma unroll
@@ -96,20 +96,9 @@ template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total
     __syncthreads();                     // the last call's parts have been read
     if (lane == 31) s_part[warp] = sum;
     __syncthreads();
-    if (warp == 0) {
-        int p = lane < THREADS / 32 ? s_part[lane] : 0;
-        const int own = p;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, p, o);
-            if (lane >= o) p += y;
-        }
-        if (lane < THREADS / 32) s_part[lane] = p - own;
-        if (lane == 31) s_part[THREADS / 32] = p;
-    }
-    __syncthreads();
-    *total = s_part[THREADS / 32];
-    return s_part[warp] + sum - x;
+    const int part = lane < THREADS / 32 ? s_part[lane] : 0;
+    *total = __reduce_add_sync(0xffffffffu, part);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? part : 0) + sum - x;
 }
 
 // The cache as the kernels see it (retopk_pages_t with 64-bit strides worked out).

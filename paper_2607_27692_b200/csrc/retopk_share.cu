@@ -17,7 +17,7 @@ int check_shape(int B, int T, int H_q, int H_kv, int d) {
     return RETOPK_OK;
 }
 
-// SM count, and the attention kernels' opt-in to large shared memory; once per device.
+// SM count, and the kernels' opt-in to large shared memory; once per device.
 constexpr int MAX_DEVICES = 64;
 struct DeviceSetup { bool ready; int num_sms; };
 DeviceSetup g_setup[MAX_DEVICES];
@@ -38,6 +38,7 @@ int device_sms(int* num_sms) {
             cudaGetLastError();
             return RETOPK_ECUDA;
         }
+        if (st.num_sms > JOIN_LIST - 16) st.num_sms = JOIN_LIST - 16;        // (CTAs of the attention)
         st.ready = true;
     }
     *num_sms = st.num_sms;
@@ -134,7 +135,8 @@ int block_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_keys, Wo
     return RETOPK_OK;
 }
 
-template <class Args, class F> int by_type(const retopk_pages_t* p, F bf128, F bf64, F fp128, F fp64, dim3 grid, unsigned threads, cudaStream_t s, const Args& a) {
+template <class Args, class F>
+int by_type(const retopk_pages_t* p, F bf128, F bf64, F fp128, F fp64, dim3 grid, unsigned threads, cudaStream_t s, const Args& a) {
     const bool bf = p->format == RETOPK_PAGES_BF16, wide = p->d == 128;
     return launch(bf ? (wide ? bf128 : bf64) : (wide ? fp128 : fp64), grid, threads, 0, s, a);
 }
@@ -200,7 +202,7 @@ int64_t retopk_block_select_workspace(int B, int T, int H_q, int H_kv, int d, in
     if (rc != RETOPK_OK) return rc;
     if (max_blocks < 1) return RETOPK_EINVAL;
     if (max_blocks > MAX_KEYS) return RETOPK_EUNSUPPORTED;
-    return (int64_t)B * T * H_kv * max_blocks * 4;
+    return (int64_t)B * T * H_kv * max_blocks * 8;
 }
 
 int retopk_block_select(const retopk_pages_t* pages, int block, const void* bounds, int B, int T, int H_q, const int32_t* seq_lens,
@@ -226,16 +228,18 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
     a.bounds = static_cast<const uint16_t*>(bounds);
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_stride;
-    a.scores = static_cast<float*>(workspace);
+    a.scores = static_cast<float2*>(workspace);
     a.blocks = blocks;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (a.max_blocks > keep) {
-        const dim3 grid((unsigned)((a.max_blocks + SCORE_BLOCKS - 1) / SCORE_BLOCKS), (unsigned)pages->H_kv, (unsigned)B);
+        constexpr int PER_CTA = SCORE_WARPS * SCORE_ROWS;
+        const dim3 grid((unsigned)((a.max_blocks + PER_CTA - 1) / PER_CTA), (unsigned)pages->H_kv, (unsigned)B);
         rc = by_type(pages, score_kernel<TYPE_BF16, 128>, score_kernel<TYPE_BF16, 64>, score_kernel<TYPE_FP16, 128>,
                      score_kernel<TYPE_FP16, 64>, grid, SCORE_THREADS, s, a);
         if (rc != RETOPK_OK) return rc;
     }
-    return launch(pick_kernel, dim3((unsigned)pages->H_kv, (unsigned)T, (unsigned)B), PICK_THREADS, 0, s, a);
+    return by_type(pages, pick_kernel<TYPE_BF16, 128>, pick_kernel<TYPE_BF16, 64>, pick_kernel<TYPE_FP16, 128>, pick_kernel<TYPE_FP16, 64>,
+                   dim3((unsigned)pages->H_kv, (unsigned)T, (unsigned)B), PICK_THREADS, s, a);
 }
 
 int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d, int keep, int block) {
