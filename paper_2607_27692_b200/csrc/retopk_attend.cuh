@@ -10,6 +10,8 @@
 // rows.  For each KV head and 256 query rows an entry has a line of tiles; a piece of a line is what one CTA
 // takes of it, and leaves fp32 sums for its rows in the workspace.
 #pragma once
+#include <cuda.h>
+
 #include "retopk_cache.cuh"
 
 namespace retopk_cache {
@@ -37,6 +39,9 @@ struct Entry {
 };
 struct AttendHeader { long long units; };
 
+// Keys and values as [rows of all pages, d] for copies of `box_rows` rows (which lie in one page) and of single rows.
+struct AttendMaps { CUtensorMap k, v, v_row; };
+
 struct AttendArgs {
     Pages pg;
     const int32_t* seq_lens;
@@ -55,6 +60,11 @@ struct AttendArgs {
     Entry* entry;
     int32_t *group_of, *flags;  // group of a sequence or -1; CTAs that gave up
     float *shared_parts, *own_parts;
+    int box_rows, total_rows;
+};
+struct AttendParams {
+    AttendMaps maps;
+    AttendArgs a;
 };
 
 // Floats of a half of a part (one stream's): sums [D / 4][rows][4], then reference and weight sum of each row.
@@ -250,10 +260,9 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* x) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8) : "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* x) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8), TC_W8(x, 16), TC_W8(x, 24) : "memory");
+__device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t* x) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : TC_R8(x, 0), TC_R8(x, 8) : "r"(addr));
 }
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -289,10 +298,19 @@ template <int DT> __host__ __device__ constexpr uint32_t tc_shape(int n, bool b_
 // ---------------------------------------------------------------------------------------
 // attend_kernel
 // ---------------------------------------------------------------------------------------
-constexpr int ATT_SOFT_WARPS = 8, ATT_LOAD_WARPS = 4, ATT_MMA_WARP = ATT_SOFT_WARPS + ATT_LOAD_WARPS;
-constexpr int ATT_THREADS = (ATT_MMA_WARP + 1) * 32;
+constexpr int ATT_SOFT_WARPS = 8, ATT_LOAD_WARP = ATT_SOFT_WARPS, ATT_MMA_WARP = ATT_LOAD_WARP + 2;      // (two of each)
+constexpr int ATT_WARPS = ATT_MMA_WARP + 2, ATT_THREADS = ATT_WARPS * 32;
 constexpr int ATT_PIECES = 32;           // pieces that a CTA lists at once
 constexpr int ATT_MASKS = 8;             // tiles whose masks are kept
+
+// With few query rows, copies of them fill the 128 of a stream: each copy has a share of a tile's keys to itself,
+// so that four warps have the work of one.
+__host__ __device__ constexpr int copies_of(int rows) { return rows <= ATT_TILE / 4 ? 4 : (rows <= ATT_TILE / 2 ? 2 : 1); }
+
+// Loads of a piece of n tiles, j = 0 .. 2 n - 1: K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1).
+__device__ __forceinline__ int k_load(int t) { return t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ int v_load(int t, int n) { return t == n - 1 ? 2 * n - 1 : 2 * t + 2; }
+__device__ __forceinline__ int tile_of_load(int j, int n) { return j == 0 ? 0 : (j == 2 * n - 1 ? n - 1 : (j & 1 ? (j + 1) >> 1 : (j >> 1) - 1)); }
 
 struct Piece {
     int b, h, token, row0, rows, half_rows;
@@ -303,24 +321,29 @@ struct Piece {
 template <int D> struct AttendSmem {
     static constexpr int TILE_BYTES = ATT_TILE * D * 2;
     static constexpr int SLOTS = 5 * 128 / D;
-    static constexpr int LAG = SLOTS - 2;                // loads in flight before one is waited for
     unsigned char q[2][TILE_BYTES];
     unsigned char ring[SLOTS][TILE_BYTES];
     uint32_t mask[ATT_MASKS][4];
-    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2], p_ready[2], o_ready[2], drained;
+    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2][2], p_ready[2][2], o_ready[2][2], drained[2];      // [stream][half of a tile]
     Piece piece[ATT_PIECES];
-    int warp_sum[ATT_MMA_WARP + 2];
+    int warp_sum[ATT_WARPS];
+    uint32_t issued[SLOTS];     // last load into a slot
     uint32_t tmem;
     int gave_up;
 };
 
 // Two streams of four warps each take the softmax of 128 query rows: with up to 128 rows both have the same
 // rows and every other tile, with more a stream has 128 of 256 rows and every tile.  While one is at its
-// softmax the tensor core works for the other.  Four warps fetch keys and values, rows of pages wherever they
-// lie, with cp.async into a ring, 5 tiles of 32 KB at d = 128; one thread issues the products: S = Q K^T into tensor memory,
-// O += P V with P over the columns of S.  Rows that are not loaded (masked, pages out of range) are zeros in shared memory.
-template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_constant__ AttendArgs a) {
+// softmax the tensor core works for the other.  One warp fetches keys, one values, by copies of as many rows as
+// lie in a page together, into a ring of 5 tiles of 32 KB at d = 128; for each stream one thread issues the products: S = Q K^T into
+// tensor memory, O += P V with P over the columns of S, half a tile of keys at a time, so that the other half is at its
+// softmax.  Rows of values that do not count (masked, pages out of range) are read from behind the last row, where a copy
+// finds zeros; a weight of 0 would not hide a NaN.
+template <int DT, int D>
+__global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_constant__ AttendParams params) {
     using Smem = AttendSmem<D>;
+    const AttendArgs& a = params.a;
+    const AttendMaps& maps = params.maps;
     extern __shared__ __align__(1024) unsigned char att_smem[];
     Smem& sm = *reinterpret_cast<Smem*>(att_smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), cta = blockIdx.x;
@@ -328,17 +351,20 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
     if (tid == 0) {
         sm.gave_up = (smem_of(att_smem) & 1023) != 0;    // operands need the alignment
         for (int i = 0; i < Smem::SLOTS; ++i) {
-            bar_init(smem_of(&sm.full[i]), ATT_LOAD_WARPS);
-            bar_init(smem_of(&sm.empty[i]), 1);
+            bar_init(smem_of(&sm.full[i]), 1);
+            sm.issued[i] = ~0u;
+            bar_init(smem_of(&sm.empty[i]), 2);           // one of each stream
         }
-        for (int i = 0; i < ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i]), ATT_LOAD_WARPS);
+        for (int i = 0; i < ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i]), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_of(&sm.q_ready[i]), 4);
-            bar_init(smem_of(&sm.s_ready[i]), 1);
-            bar_init(smem_of(&sm.p_ready[i]), 4);
-            bar_init(smem_of(&sm.o_ready[i]), 1);
+            for (int h = 0; h < 2; ++h) {
+                bar_init(smem_of(&sm.s_ready[i][h]), 1);
+                bar_init(smem_of(&sm.p_ready[i][h]), 4);
+                bar_init(smem_of(&sm.o_ready[i][h]), 1);
+            }
         }
-        bar_init(smem_of(&sm.drained), 1);
+        for (int i = 0; i < 2; ++i) bar_init(smem_of(&sm.drained[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
@@ -356,8 +382,7 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
 
     // what the roles keep from piece to piece
     uint32_t loads = 0, tiles_done = 0;                  // loads issued (or consumed), tiles behind
-    uint32_t turns[2] = {0, 0};                          // tiles of a stream behind
-    uint32_t begun[2] = {0, 0};                          // pieces of a stream begun
+    uint32_t turns = 0, begun = 0;                       // of a stream: tiles behind, pieces begun
     bool ok = true;
 
     for (int batch = 0;; ++batch) {
@@ -404,7 +429,7 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
             if (lane == 31) sm.warp_sum[warp] = sum;
             __syncthreads();
             int at = listed + sum - count - batch * ATT_PIECES, total = 0;
-            for (int w = 0; w <= ATT_MMA_WARP; ++w) {
+            for (int w = 0; w < ATT_WARPS; ++w) {
                 if (w < warp) at += sm.warp_sum[w];
                 total += sm.warp_sum[w];
             }
@@ -447,138 +472,177 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
         if (pieces <= 0 || !ok) break;                   // (the same for all threads)
         const uint32_t tmem = sm.tmem;
 
-        if (warp >= ATT_SOFT_WARPS && warp < ATT_MMA_WARP) {
-            // ---- loads ---------------------------------------------------------------------------
-            const int part = warp - ATT_SOFT_WARPS;      // rows 32 * part .. of a tile
-            // number of this lane's row of tile t, or ~0
-            auto look_up = [&](const Piece& p, int t) -> uint32_t {
-                int pos = t * ATT_TILE + part * 32 + lane;
-                if (pos < p.lo || pos >= p.hi) return ~0u;
-                if (a.blocks) {
-                    const int j = a.blocks[((long long)p.token * a.pg.H_kv + p.h) * a.keep + (pos >> a.block_shift)];
-                    if (j < 0 || j > (p.seen - 1) >> a.block_shift) return ~0u;
-                    pos = (j << a.block_shift) + (pos & (a.block - 1));
-                    if (pos >= p.seen) return ~0u;
-                }
-                const long long row = cache_row(a.pg, p.b, pos);
-                return row < 0 ? ~0u : (uint32_t)(row + (long long)p.h * a.pg.page_size);
-            };
-            auto arrive_full = [&](uint32_t load) {
-                fence_async();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_of(&sm.full[load % Smem::SLOTS]));
-            };
-            uint32_t unsignalled = 0;                    // loads of this batch that are not arrived yet
-            auto load = [&](const unsigned char* base, uint32_t row) -> bool {
-                constexpr int LANES = D / 8, RPI = 32 / LANES;          // lanes of a row, rows of an instruction
-                const uint32_t slot = loads % Smem::SLOTS, turn = loads / Smem::SLOTS;
-                if (!__all_sync(0xffffffffu, bar_wait(smem_of(&sm.empty[slot]), (turn & 1) ^ 1, gave_up))) return false;
-                const int c = lane % LANES;
-                const uint32_t dst = smem_of(sm.ring[slot]) + (c >> 3) * (ATT_TILE * 128);
+        if (warp >= ATT_LOAD_WARP && warp < ATT_MMA_WARP) {
+            // ---- loads: keys by one warp, values by the other ------------------------------------
+            const bool keys = warp == ATT_LOAD_WARP;
+            const CUtensorMap* map = keys ? &maps.k : &maps.v;
+            const int box = a.box_rows;
+            // Four rows of a tile to a lane.  Their numbers: of the first, the others follow where boxes have
+            // four rows or more, else one by one; and which of them count, as bits.
+            struct Rows { int row[4]; uint32_t valid; };
+            auto look_up = [&](int b, int h, int token, int lo, int hi, int seen, int t) -> Rows {
+                Rows r;
+                r.valid = 0;
+                const int pos0 = t * ATT_TILE + lane * 4;
 #pragma unroll
-                for (int i = 0; i < 32 / RPI; ++i) {
-                    const int r = part * 32 + i * RPI + lane / LANES;
-                    const uint32_t from = __shfl_sync(0xffffffffu, row, i * RPI + lane / LANES);
-                    const unsigned char* src = base + (from == ~0u ? 0 : (unsigned long long)from * (D * 2)) + c * 16;
-                    const int bytes = from == ~0u ? 0 : 16;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4)), "l"(src), "r"(bytes) : "memory");
-                }
-                cp_async_commit();
-                ++loads;
-                if (++unsignalled > Smem::LAG) {
-                    cp_async_wait<Smem::LAG>();
-                    arrive_full(loads - unsignalled);
-                    --unsignalled;
-                }
-                return true;
-            };
-            uint32_t next = look_up(sm.piece[0], sm.piece[0].tile0);
-            for (int i = 0; i < pieces && ok; ++i) {
-                const Piece& p = sm.piece[i];
-                uint32_t before = ~0u;
-                for (int t = p.tile0; t < p.tile1 && ok; ++t) {
-                    const uint32_t row = next;
-                    if (t + 1 < p.tile1) next = look_up(p, t + 1);
-                    else if (i + 1 < pieces) next = look_up(sm.piece[i + 1], sm.piece[i + 1].tile0);
-                    // the mask of tile 8 back is no longer read: its softmax was over before the slots of this tile came free
-                    const uint32_t valid = __ballot_sync(0xffffffffu, row != ~0u);
-                    ok = load(a.pg.k, row);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        sm.mask[tiles_done % ATT_MASKS][part] = valid;
-                        bar_arrive(smem_of(&sm.mask_ready[tiles_done % ATT_MASKS]));
+                for (int e = 0; e < 4; ++e) {
+                    r.row[e] = -1;
+                    if ((e > 0 && box >= 4) || pos0 + e >= hi) continue;
+                    int pos = pos0 + e;
+                    if (a.blocks) {
+                        const int j = a.blocks[((long long)token * a.pg.H_kv + h) * a.keep + (pos >> a.block_shift)];
+                        pos = j < 0 || j > (seen - 1) >> a.block_shift ? -1 : (j << a.block_shift) + (pos & (a.block - 1));
                     }
-                    __syncwarp();
-                    ++tiles_done;
-                    if (t > p.tile0) ok = load(a.pg.v, before);
-                    before = row;
+                    // (rows of a box share the page: the first of them may lie before lo)
+                    const long long row = pos + (box >= 4 ? 3 : 0) < lo ? -1 : cache_row(a.pg, b, pos);
+                    if (row >= 0) r.row[e] = (int)(row + (long long)h * a.pg.page_size);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (x == e || (box >= 4 && e == 0)) {
+                            const int at = pos0 + x, p = pos + x - e;            // place among the keys, position in the sequence
+                            if (row >= 0 && at >= lo && at < hi && p < seen) r.valid |= 1u << x;
+                        }
                 }
-                if (ok) ok = load(a.pg.v, before);
-            }
-            cp_async_wait<0>();
-            for (; ok && unsignalled > 0; --unsignalled) arrive_full(loads - unsignalled);
-        } else if (warp == ATT_MMA_WARP) {
-            // ---- products ------------------------------------------------------------------------
-            if (lane == 0) {
-                constexpr uint32_t QK = tc_shape<DT>(ATT_TILE, false), PV = tc_shape<DT>(D, true);
-                auto wait_full = [&](uint32_t load) { return bar_wait(smem_of(&sm.full[load % Smem::SLOTS]), load / Smem::SLOTS & 1, gave_up); };
-                for (int i = 0; i < pieces && ok; ++i) {
-                    const Piece& p = sm.piece[i];
-                    const int n = p.tile1 - p.tile0;
-                    const bool both = p.rows > ATT_TILE;
-                    // loads of a piece: K0, K1, V0, K2, V1, .. , V(n-2), V(n-1)
-                    auto k_load = [&](int t) { return loads + (t == 0 ? 0 : 2 * t - 1); };
-                    auto v_load = [&](int t) { return loads + (t == n - 1 ? 2 * n - 1 : 2 * t + 2); };
-                    auto weigh = [&](int t, int s) -> bool {             // O += P V of tile t
-                        if (!bar_wait(smem_of(&sm.p_ready[s]), turns[s] & 1, gave_up)) return false;
-                        if (!wait_full(v_load(t))) return false;
-                        tc_after_sync();
-                        const uint32_t v = smem_of(sm.ring[v_load(t) % Smem::SLOTS]);
+                return r;
+            };
+            auto copy = [&](const CUtensorMap* m, uint32_t dst, int row, uint32_t bar) {
 #pragma unroll
-                        for (int x = 0; x < ATT_TILE / 16; ++x)
-                            tc_mma_ts(tmem + 2 * ATT_TILE + s * D, tmem + s * ATT_TILE + x * 8, tc_operand(v + x * 2048, ATT_TILE * 128), PV,
-                                      x > 0 || t >= (both ? 1 : 2));
-                        tc_commit(smem_of(&sm.o_ready[s]));
-                        if (!both || s == 1) tc_commit(smem_of(&sm.empty[v_load(t) % Smem::SLOTS]));
-                        ++turns[s];
-                        return true;
-                    };
-                    for (int t = 0; t < n && ok; ++t) {
-                        for (int s = both ? 0 : t & 1; s <= (both ? 1 : t & 1) && ok; ++s) {
-                            const int last = both ? t - 1 : t - 2;
-                            if (last >= 0) {
-                                ok = weigh(last, s) && bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up);
+                for (int c = 0; c < D / 64; ++c)
+                    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                                 ::"r"(dst + c * (ATT_TILE * 128)), "l"(m), "r"(c * 64), "r"(row), "r"(bar) : "memory");
+            };
+            for (int i = 0; i < pieces && ok; ++i) {
+                const Piece p = sm.piece[i];
+                const int n = p.tile1 - p.tile0;
+                Rows next = look_up(p.b, p.h, p.token, p.lo, p.hi, p.seen, p.tile0);
+                for (int t = 0; t < n && ok; ++t) {
+                    const Rows r = next;
+                    if (t + 1 < n) next = look_up(p.b, p.h, p.token, p.lo, p.hi, p.seen, p.tile0 + t + 1);
+                    const uint32_t load = loads + (keys ? k_load(t) : v_load(t, n)), slot = load % Smem::SLOTS, turn = load / Smem::SLOTS;
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.empty[slot]), (turn & 1) ^ 1, gave_up));
+                    if (!ok) break;
+                    const uint32_t bar = smem_of(&sm.full[slot]), dst = smem_of(sm.ring[slot]) + lane * (4 * 128);
+                    if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(Smem::TILE_BYTES) : "memory");
+                    __syncwarp();
+                    if (box >= 4) {
+                        // whether all rows of the box count, and whether any does; its first lane copies it
+                        const int lanes = box / 4, leader = lane & -lanes;
+                        const uint32_t in_box = (lanes == 32 ? ~0u : (1u << lanes) - 1) << leader;
+                        const uint32_t any = __ballot_sync(0xffffffffu, r.valid != 0) & in_box, full = __ballot_sync(0xffffffffu, r.valid == 15u) & in_box;
+                        // (the box's first row, from a lane whose rows count)
+                        const int from = any ? __ffs(any) - 1 : leader, row = __shfl_sync(0xffffffffu, r.row[0], from) - (from - leader) * 4;
+                        if (keys || any == 0 || full == in_box) {
+                            if (lane == leader) copy(map, dst, any ? row : a.total_rows, bar);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) copy(&maps.v_row, dst + e * 128, r.valid >> e & 1 ? r.row[0] + e : a.total_rows, bar);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t mine = r.valid >> e & ((1u << box) - 1);
+                            if (box == 2 && (e & 1)) continue;
+                            const int row = mine & 1 ? r.row[e] : r.row[e | 1] - 1;
+                            if (keys || mine == 0 || mine == (1u << box) - 1) {
+                                copy(map, dst + e * 128, mine ? row : a.total_rows, bar);
                             } else {
-                                ok = bar_wait(smem_of(&sm.q_ready[s]), begun[s] & 1, gave_up);
-                                ++begun[s];
-                                // (the weights of the piece before are read)
-                                if (turns[s] > 0) ok = ok && bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up);
+                                copy(&maps.v_row, dst + e * 128, mine & 1 ? r.row[e] : a.total_rows, bar);
+                                copy(&maps.v_row, dst + (e + 1) * 128, mine & 2 ? r.row[e | 1] : a.total_rows, bar);
                             }
-                            ok = ok && wait_full(k_load(t));
-                            if (!ok) break;
-                            tc_after_sync();
-                            const uint32_t q = smem_of(sm.q[s]), k = smem_of(sm.ring[k_load(t) % Smem::SLOTS]);
-#pragma unroll
-                            for (int x = 0; x < D / 16; ++x) {
-                                const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
-                                tc_mma_ss(tmem + s * ATT_TILE, tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0);
-                            }
-                            tc_commit(smem_of(&sm.s_ready[s]));
-                            if (!both || s == 1) tc_commit(smem_of(&sm.empty[k_load(t) % Smem::SLOTS]));
                         }
                     }
-                    if (both) {
-                        ok = ok && weigh(n - 1, 0) && weigh(n - 1, 1);
-                    } else {
-                        if (n > 1) ok = ok && weigh(n - 2, (n - 2) & 1);
-                        ok = ok && weigh(n - 1, (n - 1) & 1);
+                    if (lane == 0) sm.issued[slot] = load;
+                    if (keys) {
+                        // The mask.  That of 8 tiles back is no longer read: its softmax was over before this slot came free.
+                        uint32_t m = r.valid << (lane % 8 * 4);
+                        m |= __shfl_xor_sync(0xffffffffu, m, 1);
+                        m |= __shfl_xor_sync(0xffffffffu, m, 2);
+                        m |= __shfl_xor_sync(0xffffffffu, m, 4);
+                        if (lane % 8 == 0) sm.mask[tiles_done % ATT_MASKS][lane / 8] = m;
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_of(&sm.mask_ready[tiles_done % ATT_MASKS]));
+                        ++tiles_done;
                     }
+                }
+                loads += 2 * n;
+            }
+            if (!ok && lane == 0) {                      // copies that are under way end before the memory is given back
+                volatile int never = 0;
+                for (int x = 0; x < Smem::SLOTS; ++x)
+                    if (sm.issued[x] != ~0u) bar_wait(smem_of(&sm.full[x]), sm.issued[x] / Smem::SLOTS & 1, &never);
+            }
+            __syncwarp();
+        } else if (warp >= ATT_MMA_WARP) {
+            // ---- products: a warp for each stream ------------------------------------------------
+            if (lane == 0) {
+                constexpr uint32_t QK = tc_shape<DT>(ATT_TILE / 2, false), PV = tc_shape<DT>(D, true);
+                const int s = warp - ATT_MMA_WARP;
+                const uint32_t S = tmem + s * ATT_TILE, O = tmem + 2 * ATT_TILE + s * D, q = smem_of(sm.q[s]);
+                for (int i = 0; i < pieces && ok; ++i) {
+                    const Piece& p = sm.piece[i];
+                    const int n = p.tile1 - p.tile0, step = p.rows > ATT_TILE ? 1 : 2;
+                    auto wait_full = [&](int j) { return bar_wait(smem_of(&sm.full[(loads + j) % Smem::SLOTS]), (loads + j) / Smem::SLOTS & 1, gave_up); };
+                    auto tile_at = [&](int j) { return smem_of(sm.ring[(loads + j) % Smem::SLOTS]); };
+                    auto empty_at = [&](int j) { return smem_of(&sm.empty[(loads + j) % Smem::SLOTS]); };
+                    // Both threads see all loads go by, so that neither runs away from the other: a phase of a
+                    // barrier is told from the one after the next by nothing else.
+                    int seen = 0;
+                    auto see = [&](int j) -> bool {      // the other stream's loads before j
+                        for (; seen < j; ++seen)
+                            if (step == 2 && (tile_of_load(seen, n) & 1) != s) {
+                                if (!wait_full(seen)) return false;
+                                bar_arrive(empty_at(seen));
+                            }
+                        return true;
+                    };
+                    auto score = [&](int t, int h) {     // S = Q K^T of half a tile
+                        const uint32_t k = tile_at(k_load(t)) + h * (ATT_TILE / 2 * 128);
+                        tc_after_sync();
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
+                            tc_mma_ss(S + h * (ATT_TILE / 2), tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0);
+                        }
+                        tc_commit(smem_of(&sm.s_ready[s][h]));
+                        if (h == 1) tc_commit(empty_at(k_load(t)));
+                    };
+                    // weights that S takes the place of have been read
+                    auto wait_o = [&](int h) { return turns == 0 || bar_wait(smem_of(&sm.o_ready[s][h]), (turns - 1) & 1, gave_up); };
+                    const int first = step == 1 ? 0 : s;
+                    if (first < n) {
+                        ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first));
+                        ++begun;
+                        for (int h = 0; h < 2 && ok; ++h) {
+                            ok = wait_o(h);
+                            if (ok) score(first, h);
+                        }
+                    }
+                    for (int t = first; t < n && ok; t += step) {
+                        ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
+                        const uint32_t v = tile_at(v_load(t, n));
+                        for (int h = 0; h < 2 && ok; ++h) {
+                            ok = bar_wait(smem_of(&sm.p_ready[s][h]), turns & 1, gave_up);
+                            if (!ok) break;
+                            tc_after_sync();
+#pragma unroll
+                            for (int x = 0; x < ATT_TILE / 32; ++x)              // O += P V
+                                tc_mma_ts(O, S + h * (ATT_TILE / 2) + x * 8, tc_operand(v + (h * 4 + x) * 2048, ATT_TILE * 128), PV, x > 0 || h > 0 || t >= step);
+                            tc_commit(smem_of(&sm.o_ready[s][h]));
+                            if (h == 1) tc_commit(empty_at(v_load(t, n)));
+                            if (t + step < n) {
+                                ok = (h == 1 || wait_full(k_load(t + step))) && bar_wait(smem_of(&sm.o_ready[s][h]), turns & 1, gave_up);
+                                if (ok) score(t + step, h);
+                            }
+                        }
+                        ++turns;
+                    }
+                    ok = ok && see(2 * n);
                     loads += 2 * n;
                 }
                 if (!ok) {                               // what was issued ends before the memory is given back
-                    tc_commit(smem_of(&sm.drained));
-                    *gave_up = 0;
-                    bar_wait(smem_of(&sm.drained), 0, gave_up);
+                    tc_commit(smem_of(&sm.drained[s]));
+                    volatile int never = 0;
+                    bar_wait(smem_of(&sm.drained[s]), 0, &never);
                     *gave_up = 1;
                 }
             }
@@ -590,140 +654,161 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
             const uint32_t S = lanes + s * ATT_TILE, O = lanes + 2 * ATT_TILE + s * D;
             // (a scale of 0 as the smallest: 0 times the -inf of a hidden key is no number)
             const float scale = a.scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.scale_log2);
-            // rows and tiles of this stream in a piece
-            auto rows_of = [&](const Piece& p) { return p.rows <= ATT_TILE ? p.rows : (s == 0 ? ATT_TILE : p.rows - ATT_TILE); };
+            // tiles of this stream in a piece
             auto turns_of = [&](const Piece& p) { return p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
+            // this thread's query row in a piece, or -1; the copy that it belongs to
+            auto row_of = [&](const Piece& p, int* copy) {
+                const int copies = copies_of(p.rows), stride = ATT_TILE / copies, r = row % stride + (p.rows > ATT_TILE ? s * ATT_TILE : 0);
+                *copy = copies == 1 ? 0 : row / stride;
+                return r < p.rows ? r : -1;
+            };
             auto fetch_q = [&](const Piece& p) {
-                const int r = p.row0 + (p.rows > ATT_TILE ? s * ATT_TILE : 0) + row;
-                const uint16_t* src = a.q + ((long long)p.token + r / a.G) * a.q_stride + (long long)(p.h * a.G + r % a.G) * D;
-                const uint32_t dst = smem_of(sm.q[s]) + row * 128;
-                if (row < rows_of(p)) {
+                int copy;
+                const int r = p.row0 + row_of(p, &copy);
+                if (r >= p.row0) {
+                    const uint16_t* src = a.q + ((long long)p.token + r / a.G) * a.q_stride + (long long)(p.h * a.G + r % a.G) * D;
+                    const uint32_t dst = smem_of(sm.q[s]) + row * 128;
 #pragma unroll
                     for (int c = 0; c < D / 8; ++c) cp_async16(dst + (c >> 3) * (ATT_TILE * 128) + (((c & 7) ^ (row & 7)) << 4), src + c * 8);
                 }
                 cp_async_commit();
             };
-            int fetched = -1;                            // piece whose queries are on their way
+            auto give_q = [&](const Piece& p) {
+                cp_async_wait<0>();
+                int copy;
+                if (a.scale_log2 < 0.f && row_of(p, &copy) >= 0)         // a negative scale turns the queries' signs
+#pragma unroll 1
+                    for (int c = 0; c < D / 8; ++c) {
+                        uint4* x = reinterpret_cast<uint4*>(sm.q[s] + (c >> 3) * (ATT_TILE * 128) + row * 128 + ((c & 7) << 4));
+                        x->x ^= 0x80008000u; x->y ^= 0x80008000u; x->z ^= 0x80008000u; x->w ^= 0x80008000u;
+                    }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_of(&sm.q_ready[s]));
+            };
+            bool fetched = false;                        // the queries of the next piece are there
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
                 const bool both = p.rows > ATT_TILE;
-                const int mine = rows_of(p), turn_count = turns_of(p);
-                const bool live = row < mine, warp_live = (warp & 3) * 32 < mine;
-                float* part = p.part + s * half_floats(p.half_rows, D);
+                const int turn_count = turns_of(p), copies = copies_of(p.rows);
+                int copy;
+                const int r = row_of(p, &copy);
+                const bool live = r >= 0, warp_live = __any_sync(0xffffffffu, live);
+                const int c0 = copy * (4 / copies), c1 = c0 + 4 / copies;        // columns of this warp, in 32s
                 float ref = ATT_NONE, l = 0.f;
-                auto give_q = [&]() {
-                    cp_async_wait<0>();
-                    if (a.scale_log2 < 0.f && row < rows_of(sm.piece[fetched]))         // a negative scale turns the queries' signs
-                        for (int c = 0; c < D / 8; ++c) {
-                            uint4* x = reinterpret_cast<uint4*>(sm.q[s] + (c >> 3) * (ATT_TILE * 128) + row * 128 + ((c & 7) << 4));
-                            x->x ^= 0x80008000u; x->y ^= 0x80008000u; x->z ^= 0x80008000u; x->w ^= 0x80008000u;
-                        }
-                    fence_async();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_of(&sm.q_ready[s]));
-                };
-                if (turn_count > 0 && fetched < i) {
-                    fetched = i;
+                if (turn_count > 0 && !fetched) {
                     fetch_q(p);
-                    give_q();
+                    give_q(p);
                 }
+                fetched = false;
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
-                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.s_ready[s]), turns[s] & 1, gave_up) &&
-                                                     bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up));
-                    if (!ok) break;
-                    ++turns[s];
                     const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
-                    if (ahead) {                         // the queries of this piece have been read: the next one's take their place
-                        fetched = i + 1;
-                        fetch_q(sm.piece[i + 1]);
+#pragma unroll 1
+                    for (int h = 0; h < 2 && ok; ++h) {
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up) &&
+                                                         bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up));
+                        if (!ok) break;
+                        if (ahead && h == 1) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
+                        if (warp_live) {
+                            tc_after_sync();
+                            const uint32_t Sh = S + h * (ATT_TILE / 2);
+                            uint32_t x[32], y[32];
+                            // this copy's columns: both 32s of the half, one, or none
+                            const bool first = 2 * h >= c0 && 2 * h < c1, second = 2 * h + 1 >= c0 && 2 * h + 1 < c1;
+                            uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
+                            if (!first) mx = 0;
+                            if (!second) my = 0;
+                            if (first) tc_ld32(Sh, x);
+                            if (second) tc_ld32(Sh + 32, y);
+                            tc_wait_ld();
+                            auto hide = [&](uint32_t* v, uint32_t m) {           // keys that do not count: weight 0
+                                if (m == ~0u) return;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (!(m >> j & 1)) v[j] = 0xff800000u;
+                            };
+                            hide(x, mx);
+                            hide(y, my);
+                            float top = -INFINITY;
+                            if (mx | my) {
+                                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                                for (int j = 0; j < 32; j += 2) {
+                                    most[j & 2] = fmaxf(most[j & 2], fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 1])));
+                                    most[(j & 2) + 1] = fmaxf(most[(j & 2) + 1], fmaxf(__uint_as_float(y[j]), __uint_as_float(y[j + 1])));
+                                }
+                                top = fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW);
+                            }
+                            // The reference follows the maximum when that is more than 8 above it: weights up to 2^8 fit
+                            // both types, and the sums in tensor memory are seldom touched.
+                            const bool follow = live && top > (ref == ATT_NONE ? ref : ref + 8.f);
+                            float f = 1.f;
+                            if (__any_sync(0xffffffffu, follow)) {
+                                if (follow) {
+                                    f = exp2_approx(ref - top);
+                                    ref = top;
+                                }
+                                if (k > 0 || h > 0) {
+                                    // (the product of the half before may be under way)
+                                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][1 - h]), (h == 0 ? turns - 1 : turns) & 1, gave_up));
+                                    if (!ok) break;
+                                    tc_after_sync();
+#pragma unroll 1
+                                    for (int c = 0; c < D; c += 16) {
+                                        uint32_t o[16];
+                                        tc_ld16(O + c, o);
+                                        tc_wait_ld();
+#pragma unroll
+                                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                        tc_st16(O + c, o);
+                                    }
+                                }
+                            }
+                            float2 sum = make_float2(0.f, 0.f), more = make_float2(0.f, 0.f);
+                            if (first | second) {
+                                const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
+                                auto weigh = [&](uint32_t* v, float2& total) {
+#pragma unroll
+                                    for (int j = 0; j < 32; j += 2) {
+                                        float2 w = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale2, ref2);
+                                        w.x = exp2_approx(w.x);
+                                        w.y = exp2_approx(w.y);
+                                        total = add2(total, w);
+                                        v[j / 2] = pack2<DT>(w.x, w.y);
+                                    }
+                                };
+                                weigh(x, sum);
+                                tc_st16(Sh, x);
+                                weigh(y, more);
+                                tc_st16(Sh + 16, y);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) x[j] = 0;
+                                tc_st16(Sh, x);
+                                tc_st16(Sh + 16, x);
+                            }
+                            l = l * f + ((sum.x + sum.y) + (more.x + more.y));
+                            tc_wait_st();
+                            tc_before_sync();
+                        }
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s][h]));
                     }
-                    if (warp_live) {
-                        tc_after_sync();
-                        uint32_t x[32], y[32];
-                        const uint4 mask4 = *reinterpret_cast<const uint4*>(sm.mask[tile % ATT_MASKS]);
-                        const bool all = (mask4.x & mask4.y & mask4.z & mask4.w) == ~0u;
-                        auto hide = [&](uint32_t* v, int c) {            // keys that do not count: weight 0
-                            if (all) return;
-                            const uint32_t m = sm.mask[tile % ATT_MASKS][c];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!(m >> j & 1)) v[j] = 0xff800000u;
-                        };
-                        // The maximum, 32 columns at a time, the next ones on their way.  (Loops, not all of it unrolled:
-                        // a tile's code once through is otherwise more than the instruction caches feed.)
-                        float top0 = -INFINITY, top1 = -INFINITY;
-                        auto largest = [&](uint32_t* v, int c) {
-                            hide(v, c);
-#pragma unroll
-                            for (int j = 0; j < 32; j += 4) {
-                                top0 = fmaxf(top0, fmaxf(__uint_as_float(v[j]), __uint_as_float(v[j + 1])));
-                                top1 = fmaxf(top1, fmaxf(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])));
-                            }
-                        };
-                        tc_ld32(S, x);
-#pragma unroll 1
-                        for (int c = 0; c < 4; c += 2) {
-                            tc_wait_ld();
-                            tc_ld32(S + c * 32 + 32, y);
-                            largest(x, c);
-                            tc_wait_ld();
-                            tc_ld32(S + (c == 0 ? 64 : 0), x);           // (at the end the first ones again, for the weights)
-                            largest(y, c + 1);
-                        }
-                        float top = fmaxf(top0, top1) * scale;
-                        if (all || (mask4.x | mask4.y | mask4.z | mask4.w)) top = fmaxf(top, ATT_LOW);
-                        // The reference follows the maximum when that is more than 8 above it: weights up to 2^8 fit
-                        // both types, and the sums in tensor memory are seldom touched.
-                        const bool follow = live && top > (ref == ATT_NONE ? ref : ref + 8.f);
-                        const float f = follow ? exp2_approx(ref - top) : 1.f;
-                        if (follow) ref = top;
-                        float2 sum = make_float2(0.f, 0.f), more = make_float2(0.f, 0.f);
-                        const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
-                        auto weights = [&](uint32_t* v, int c) {
-                            hide(v, c);
-#pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                float2 p = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale2, ref2);
-                                p.x = exp2_approx(p.x);
-                                p.y = exp2_approx(p.y);
-                                if (j & 2) more = add2(more, p);
-                                else sum = add2(sum, p);
-                                v[j / 2] = pack2<DT>(p.x, p.y);
-                            }
-                            tc_st16(S + c * 16, v);
-                        };
-#pragma unroll 1
-                        for (int c = 0; c < 4; c += 2) {
-                            tc_wait_ld();
-                            tc_ld32(S + c * 32 + 32, y);
-                            weights(x, c);
-                            tc_wait_ld();
-                            if (c == 0) tc_ld32(S + 64, x);
-                            weights(y, c + 1);
-                        }
-                        l = l * f + ((sum.x + sum.y) + (more.x + more.y));
-                        if (k > 0 && __any_sync(0xffffffffu, follow)) {
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                tc_ld32(O + c, x);
-                                tc_wait_ld();
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f);
-                                tc_st32(O + c, x);
-                            }
-                        }
-                        tc_wait_st();
-                        tc_before_sync();
+                    ++turns;
+                    if (ok && ahead) {
+                        give_q(sm.piece[i + 1]);
+                        fetched = true;
                     }
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s]));
-                    if (ahead) give_q();
                 }
                 // ---- the sums of this piece ------------------------------------------------------
+                float* part = p.part + s * half_floats(p.half_rows, D);
+                const int at = copy * (p.half_rows / copies) + row % (ATT_TILE / copies);
+                if (live) *reinterpret_cast<float2*>(part + (long long)p.half_rows * D + 2 * at) = make_float2(ref, l);
                 if (ok && turn_count > 0) {
-                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s]), (turns[s] - 1) & 1, gave_up));
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][0]), (turns - 1) & 1, gave_up) &&
+                                                     bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up));
                     if (ok && warp_live) {
                         tc_after_sync();
 #pragma unroll 1
@@ -734,13 +819,12 @@ template <int DT, int D> __global__ void __launch_bounds__(ATT_THREADS, 1) atten
                             if (live) {
 #pragma unroll
                                 for (int j = 0; j < 32; j += 4)
-                                    *reinterpret_cast<uint4*>(part + ((long long)((c + j) / 4) * p.half_rows + row) * 4) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                                    *reinterpret_cast<uint4*>(part + ((long long)((c + j) / 4) * p.half_rows + at) * 4) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
                             }
                         }
                     }
+                    tc_before_sync();
                 }
-                tc_before_sync();
-                if (live) *reinterpret_cast<float2*>(part + (long long)p.half_rows * D + 2 * row) = make_float2(ref, l);
                 tiles_done += n;
             }
         }
@@ -854,9 +938,12 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
             O.z = O.z * f + o.z * e;
             O.w = O.w * f + o.w * e;
         };
-        // `halves` of each part from half `h0` on hold the row, at `at`
-        auto add_list = [&](const float** list, int count, int half_rows, int at, int h0, int halves) {
-            const int all = count * halves;
+        // The row `row` of `rows` in a row tile: with more than 128 rows in one half of each part, with fewer in
+        // both, in `copies` places.
+        auto add_list = [&](const float** list, int count, int half_rows, int row, int rows) {
+            const bool both = rows > ATT_TILE;
+            const int copies = copies_of(rows), places = both ? 1 : 2 * copies, all = count * places, apart = half_rows / copies;
+            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row;
             for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
                 float2 ml[JOIN_DEEP];
                 float4 o[JOIN_DEEP];
@@ -865,7 +952,8 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
                     const int k = k0 + d * splits;
                     ml[d].x = ATT_NONE;
                     if (k < all) {
-                        const float* half = list[halves == 2 ? k >> 1 : k] + (h0 + (halves == 2 ? k & 1 : 0)) * half_floats(half_rows, D);
+                        const int part = k / places, place = k - part * places, at = at0 + place / 2 * apart;
+                        const float* half = list[part] + (h0 + (place & 1)) * half_floats(half_rows, D);
                         ml[d] = *reinterpret_cast<const float2*>(half + (long long)half_rows * D + 2 * at);
                         o[d] = *reinterpret_cast<const float4*>(half + ((long long)c4 * half_rows + at) * 4);
                     }
@@ -877,12 +965,10 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
         };
         if (on) {
             if (n_first + n_second > 0) {
-                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), at = row % (2 * ATT_TILE);
-                const bool both = group.rows - (m0 + m) * (2 * ATT_TILE) > ATT_TILE;
-                add_list(s_list[m], m == 0 ? n_first : n_second, ATT_TILE, both ? at % ATT_TILE : at, both ? at / ATT_TILE : 0, both ? 1 : 2);
+                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), rows = group.rows - (m0 + m) * (2 * ATT_TILE);
+                add_list(s_list[m], m == 0 ? n_first : n_second, ATT_TILE, row % (2 * ATT_TILE), rows < 2 * ATT_TILE ? rows : 2 * ATT_TILE);
             }
-            const bool both = own.rows > ATT_TILE;
-            add_list(s_list[2], n_own, a.own_rows, both ? r % ATT_TILE : r, both ? r / ATT_TILE : 0, both ? 1 : 2);
+            add_list(s_list[2], n_own, a.own_rows, r, own.rows);
         }
         if (splits > 1) {
             s_sum[0][tid] = M; s_sum[1][tid] = L;

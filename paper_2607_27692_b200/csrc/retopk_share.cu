@@ -19,14 +19,16 @@ int check_shape(int B, int T, int H_q, int H_kv, int d) {
 
 // SM count, and the kernels' opt-in to large shared memory; once per device.
 constexpr int MAX_DEVICES = 64;
-struct DeviceSetup { bool ready; int num_sms; };
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+struct DeviceSetup { bool ready; int num_sms; EncodeTiled encode; };
 DeviceSetup g_setup[MAX_DEVICES];
 std::mutex g_setup_mutex;
 
 template <int DT, int D> bool opt_in() {
     return cudaFuncSetAttribute(attend_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>)) == cudaSuccess;
 }
-int device_sms(int* num_sms) {
+int device_setup(DeviceSetup* setup) {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return RETOPK_ECUDA; }
     if (dev < 0 || dev >= MAX_DEVICES) return RETOPK_EUNSUPPORTED;
@@ -38,12 +40,23 @@ int device_sms(int* num_sms) {
             cudaGetLastError();
             return RETOPK_ECUDA;
         }
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn) {
+            cudaGetLastError();
+            return RETOPK_ECUDA;
+        }
+        st.encode = reinterpret_cast<EncodeTiled>(fn);
         if (st.num_sms > JOIN_LIST - 16) st.num_sms = JOIN_LIST - 16;        // (CTAs of the attention)
         st.ready = true;
     }
-    *num_sms = st.num_sms;
+    *setup = st;
     return RETOPK_OK;
 }
+
+// Rows of a half of a part that belongs to one sequence with `rows` query rows: all copies of them.
+int half_rows(int rows) { return rows < ATT_TILE ? rows * copies_of(rows) : ATT_TILE; }
 
 // The workspace: where its parts begin, and its size.  `sequences`: entries that belong to one sequence or token,
 // `rows` query rows each; `keys`: the most keys that an entry can have.
@@ -60,7 +73,7 @@ Workspace lay_out(int64_t sequences, int64_t rows, int64_t n_groups, int64_t gro
     w.flags = w.group_of + up(sequences * 4);
     w.shared_parts = w.flags + up(grid * 4);
     w.own_parts = w.shared_parts + up(shared * 2 * half_floats(ATT_TILE, d) * 4);
-    w.bytes = w.own_parts + up(own * 2 * half_floats((int)(rows < ATT_TILE ? rows : ATT_TILE), d) * 4);
+    w.bytes = w.own_parts + up(own * 2 * half_floats(half_rows((int)rows), d) * 4);
     return w;
 }
 
@@ -72,7 +85,7 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     if (!rows_ok(q, q_stride, H_q, d) || !aligned16(workspace) || !aligned16(out)) return RETOPK_EINVAL;
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
-    if (a.pg.capacity > MAX_KEYS || pages->n_pages > 0xfffffffell / ((long long)pages->H_kv * pages->page_size)) return RETOPK_EUNSUPPORTED;
+    if (a.pg.capacity > MAX_KEYS || pages->n_pages > 0x7fffff00ll / ((long long)pages->H_kv * pages->page_size)) return RETOPK_EUNSUPPORTED;
     const long long n = (long long)B * T;
     const Strided qi = {q, q_stride, H_q}, qo = {out, (long long)H_q * d, H_q};
     Memory pg[4];
@@ -90,14 +103,34 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     return RETOPK_OK;
 }
 
-template <int DT, int D> int launch_attention(const AttendArgs& a, int sequences, cudaStream_t s) {
-    int rc = launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, a);
+template <int DT, int D> int launch_attention(const AttendParams& p, int sequences, cudaStream_t s) {
+    int rc = launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, p.a);
     if (rc != RETOPK_OK) return rc;
-    rc = launch(attend_kernel<DT, D>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, a);
+    rc = launch(attend_kernel<DT, D>, dim3((unsigned)p.a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
     if (rc != RETOPK_OK) return rc;
-    return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences), JOIN_THREADS, 0, s, a);
+    return launch(join_kernel<DT, D>, dim3((unsigned)p.a.pg.H_kv, (unsigned)sequences), JOIN_THREADS, 0, s, p.a);
 }
-int run_attention(AttendArgs& a, const retopk_pages_t* pages, int sequences, int rows, const Workspace& w, int grid, void* workspace, cudaStream_t s) {
+
+// Rows of 64 channels each, `box` rows to a copy, into shared memory as the tensor cores' operands lie there.
+bool encode_rows(EncodeTiled encode, CUtensorMap* map, const retopk_pages_t* pages, void* base, int64_t rows, int box) {
+    const cuuint64_t dims[2] = {(cuuint64_t)pages->d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pages->d * 2};
+    const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, steps[2] = {1, 1};
+    const CUtensorMapDataType type = pages->format == RETOPK_PAGES_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return encode(map, type, 2, base, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, int rows, const Workspace& w, const DeviceSetup& dev, void* workspace, cudaStream_t s) {
+    AttendArgs& a = p.a;
+    // rows that lie together wherever a tile or a block begins: the power of two in a page's size, or a block
+    int box = pages->page_size & -pages->page_size;
+    if (a.blocks && box > a.block) box = a.block;
+    if (box > ATT_TILE) box = ATT_TILE;
+    const int64_t rows_in_all = pages->n_pages * pages->H_kv * pages->page_size;
+    if (!encode_rows(dev.encode, &p.maps.k, pages, pages->k, rows_in_all, box) || !encode_rows(dev.encode, &p.maps.v, pages, pages->v, rows_in_all, box) ||
+        !encode_rows(dev.encode, &p.maps.v_row, pages, pages->v, rows_in_all, 1))
+        return RETOPK_ECUDA;
+    a.box_rows = box;
+    a.total_rows = (int)rows_in_all;
     char* ws = static_cast<char*>(workspace);
     a.head = reinterpret_cast<AttendHeader*>(ws);
     a.entry = reinterpret_cast<Entry*>(ws + w.entry);
@@ -106,32 +139,32 @@ int run_attention(AttendArgs& a, const retopk_pages_t* pages, int sequences, int
     a.shared_parts = reinterpret_cast<float*>(ws + w.shared_parts);
     a.own_parts = reinterpret_cast<float*>(ws + w.own_parts);
     a.entries = a.n_groups + sequences;
-    a.grid = grid;
-    a.own_rows = rows < ATT_TILE ? rows : ATT_TILE;
+    a.grid = dev.num_sms;
+    a.own_rows = half_rows(rows);
     if (pages->format == RETOPK_PAGES_BF16)
-        return pages->d == 128 ? launch_attention<TYPE_BF16, 128>(a, sequences, s) : launch_attention<TYPE_BF16, 64>(a, sequences, s);
-    return pages->d == 128 ? launch_attention<TYPE_FP16, 128>(a, sequences, s) : launch_attention<TYPE_FP16, 64>(a, sequences, s);
+        return pages->d == 128 ? launch_attention<TYPE_BF16, 128>(p, sequences, s) : launch_attention<TYPE_BF16, 64>(p, sequences, s);
+    return pages->d == 128 ? launch_attention<TYPE_FP16, 128>(p, sequences, s) : launch_attention<TYPE_FP16, 64>(p, sequences, s);
 }
 
-int shared_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, int* grid) {
+int shared_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, DeviceSetup* dev) {
     int rc = check_shape(B, T, H_q, H_kv, d);
     if (rc != RETOPK_OK) return rc;
     if (n_groups < 0 || n_groups > B || max_keys < 1) return RETOPK_EINVAL;
     if (max_keys > MAX_KEYS) return RETOPK_EUNSUPPORTED;
-    rc = device_sms(grid);
+    rc = device_setup(dev);
     if (rc != RETOPK_OK) return rc;
     const int rows = T * (H_q / H_kv);
-    *w = lay_out(B, rows, n_groups, (int64_t)B * rows, H_kv, d, max_keys, *grid);
+    *w = lay_out(B, rows, n_groups, (int64_t)B * rows, H_kv, d, max_keys, dev->num_sms);
     return RETOPK_OK;
 }
-int block_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, int* grid) {
+int block_workspace(int B, int T, int H_q, int H_kv, int d, int64_t max_keys, Workspace* w, DeviceSetup* dev) {
     int rc = check_shape(B, T, H_q, H_kv, d);
     if (rc != RETOPK_OK) return rc;
     if (max_keys < 1) return RETOPK_EINVAL;
     if (max_keys > MAX_KEYS + 127) return RETOPK_EUNSUPPORTED;
-    rc = device_sms(grid);
+    rc = device_setup(dev);
     if (rc != RETOPK_OK) return rc;
-    *w = lay_out((int64_t)B * T, H_q / H_kv, 0, 0, H_kv, d, max_keys, *grid);
+    *w = lay_out((int64_t)B * T, H_q / H_kv, 0, 0, H_kv, d, max_keys, dev->num_sms);
     return RETOPK_OK;
 }
 
@@ -147,8 +180,8 @@ extern "C" {
 
 int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys) {
     Workspace w;
-    int grid;
-    const int rc = shared_workspace(B, n_groups, T, H_q, H_kv, d, max_keys, &w, &grid);
+    DeviceSetup dev;
+    const int rc = shared_workspace(B, n_groups, T, H_q, H_kv, d, max_keys, &w, &dev);
     return rc == RETOPK_OK ? w.bytes : rc;
 }
 
@@ -160,19 +193,20 @@ int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, 
     rc = check_shape(B, T, H_q, pages->H_kv, pages->d);
     if (rc != RETOPK_OK) return rc;
     if (n_groups < 0 || n_groups > B || (n_groups > 0 && (!cu_groups || !shared_lens))) return RETOPK_EINVAL;
-    AttendArgs a;
+    AttendParams p;
+    AttendArgs& a = p.a;
     rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
     if (rc != RETOPK_OK) return rc;
     if (workspace_bytes < 4096) return RETOPK_EINVAL;    // (refused without a device too)
     Workspace w;
-    int grid;
-    rc = shared_workspace(B, n_groups, T, H_q, pages->H_kv, pages->d, a.pg.capacity, &w, &grid);
+    DeviceSetup dev;
+    rc = shared_workspace(B, n_groups, T, H_q, pages->H_kv, pages->d, a.pg.capacity, &w, &dev);
     if (rc != RETOPK_OK) return rc;
     if (workspace_bytes < w.bytes) return RETOPK_EINVAL;
     a.n_groups = n_groups;
     a.cu = cu_groups;
     a.shared_lens = shared_lens;
-    return run_attention(a, pages, B, T * a.G, w, grid, workspace, static_cast<cudaStream_t>(stream));
+    return run_attention(p, pages, B, T * a.G, w, dev, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, int B, const int32_t* seq_lens, int64_t n_new, void* stream) {
@@ -249,8 +283,8 @@ int64_t retopk_block_attention_workspace(int B, int T, int H_q, int H_kv, int d,
     if (keep > MAX_KEYS || block > 128) return RETOPK_EUNSUPPORTED;
     const int64_t keys = (int64_t)keep * block, most = MAX_KEYS + block - 1;
     Workspace w;
-    int grid;
-    const int rc = block_workspace(B, T, H_q, H_kv, d, keys < most ? keys : most, &w, &grid);
+    DeviceSetup dev;
+    const int rc = block_workspace(B, T, H_q, H_kv, d, keys < most ? keys : most, &w, &dev);
     return rc == RETOPK_OK ? w.bytes : rc;
 }
 
@@ -264,7 +298,8 @@ int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T,
     if (rc != RETOPK_OK) return rc;
     if (keep < 1 || !blocks || pages->page_size % block != 0) return RETOPK_EINVAL;
     if (keep > MAX_KEYS) return RETOPK_EUNSUPPORTED;
-    AttendArgs a;
+    AttendParams p;
+    AttendArgs& a = p.a;
     rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
     if (rc != RETOPK_OK) return rc;
     const Memory blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
@@ -272,15 +307,15 @@ int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T,
     if (!all_apart(blocks_m, {out_m, lse_m, ws_m}) || workspace_bytes < 4096) return RETOPK_EINVAL;
     const int64_t keys = (int64_t)keep * block, most = MAX_KEYS + block - 1;
     Workspace w;
-    int grid;
-    rc = block_workspace(B, T, H_q, pages->H_kv, pages->d, keys < most ? keys : most, &w, &grid);
+    DeviceSetup dev;
+    rc = block_workspace(B, T, H_q, pages->H_kv, pages->d, keys < most ? keys : most, &w, &dev);
     if (rc != RETOPK_OK) return rc;
     if (workspace_bytes < w.bytes) return RETOPK_EINVAL;
     a.blocks = blocks;
     a.keep = keep;
     a.block = block;
     a.block_shift = __builtin_ctz((unsigned)block);
-    return run_attention(a, pages, B * T, a.G, w, grid, workspace, static_cast<cudaStream_t>(stream));
+    return run_attention(p, pages, B * T, a.G, w, dev, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"
