@@ -1,6 +1,7 @@
 // Attention over 16-bit pages on the fifth-generation tensor cores (sm_100a).
 //
-//   plan_kernel      what there is to do: entries of work, one behind the other on a line
+//   plan_kernel      what there is to do: entries of work, one behind the other on a line (of many sequences; of few,
+//                    attend_kernel works it out itself)
 //   attend_kernel    a CTA takes an equal share of the line
 //   join_kernel      joins the parts of a row
 //
@@ -29,7 +30,7 @@ constexpr int ATT_START = 2;             // what beginning a line counts, in til
 constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // reference of a row without keys; lowest of one with keys
 
 struct Entry {
-    long long u;                // where its lines begin
+    int u;                      // where its lines begin
     int item;                   // number of its first (line, chunk)
     int rows, token;            // query rows: heads of a group of the tokens from `token` on
     int b;                      // sequence whose row of the block table holds the keys
@@ -37,10 +38,10 @@ struct Entry {
     int tile0, tiles;
     int row_tiles, chunks;      // lines of a KV head (256 rows each); chunks of a line
 };
-struct AttendHeader { long long units; };
+struct AttendHeader { int units; };
 
-// Keys and values as [rows of all pages, d] for copies of `box_rows` rows (which lie in one page) and of single rows.
-struct AttendMaps { CUtensorMap k, v, v_row; };
+// Keys and values as [rows of all pages, d] for copies of `box_rows` rows (which lie in one page), of 8 and of single rows.
+struct AttendMaps { CUtensorMap k, v, v_eight, v_row; };
 
 struct AttendArgs {
     Pages pg;
@@ -61,6 +62,7 @@ struct AttendArgs {
     int32_t *group_of, *flags;  // group of a sequence or -1; CTAs that gave up
     float *shared_parts, *own_parts;
     int box_rows, total_rows;
+    bool planned;               // by plan_kernel
 };
 struct AttendParams {
     AttendMaps maps;
@@ -69,34 +71,40 @@ struct AttendParams {
 
 // Floats of a half of a part (one stream's): sums [D / 4][rows][4], then reference and weight sum of each row.
 __host__ __device__ constexpr long long half_floats(int rows, int d) { return (long long)rows * d + (2 * rows + 3) / 4 * 4; }
-__device__ __forceinline__ long long line_units(const Entry& e) { return e.tiles > 0 ? e.tiles + ATT_START : 0; }
-__device__ __forceinline__ long long share_begin(long long units, int grid, int cta) { return units * cta / grid; }
+__device__ __forceinline__ int line_units(const Entry& e) { return e.tiles > 0 ? e.tiles + ATT_START : 0; }
+// Equal shares of the line; none of them is empty: of a short line fewer CTAs have one.
+__device__ __forceinline__ int share_begin(int units, int grid, int cta) {
+    const int n = units < grid ? units : grid;
+    return cta < n ? (int)((long long)units * cta / n) : units;
+}
 // The CTA whose share holds unit u.
-__device__ __forceinline__ int share_of(long long units, int grid, long long u) { return (int)(((u + 1) * grid - 1) / units); }
+__device__ __forceinline__ int share_of(int units, int grid, int u) { return (int)(((long long)(u + 1) * (units < grid ? units : grid) - 1) / units); }
 
 // ---------------------------------------------------------------------------------------
 // plan_kernel
 // ---------------------------------------------------------------------------------------
 constexpr int PLAN_THREADS = 1024;
 
-// One CTA.  Groups: the first member that is not empty owns the keys, the fewest rows that any of them sees
-// are shared; a member alone shares nothing.
-__global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constant__ AttendArgs a) {
-    __shared__ long long s_units[PLAN_THREADS / 32 + 1];
-    pdl_wait();
-    pdl_start_next();
+// By one CTA: the entries, the group of each sequence, and how long the line is.  Groups: the first member that is not
+// empty owns the keys, the fewest rows that any of them sees are shared; a member alone shares nothing.
+// s_part: a number for each warp.
+template <int THREADS> __device__ __forceinline__ int make_plan(const AttendArgs& a, Entry* entry, int32_t* group_of, int* s_part) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    bool bad = false;
-    for (int g = tid; g < a.n_groups; g += PLAN_THREADS)
-        bad |= a.cu[g] < 0 || a.cu[g + 1] < a.cu[g] || a.cu[g + 1] > a.B || (g == 0 && a.cu[0] != 0) || (g == a.n_groups - 1 && a.cu[g + 1] != a.B);
-    const int groups = __syncthreads_or(bad) ? 0 : a.n_groups;
-    for (int g = warp; g < groups; g += PLAN_THREADS / 32) {
+    int groups = 0;
+    if (a.n_groups > 0) {
+        bool bad = false;
+        for (int g = tid; g < a.n_groups; g += THREADS)
+            bad |= a.cu[g] < 0 || a.cu[g + 1] < a.cu[g] || a.cu[g + 1] > a.B || (g == 0 && a.cu[0] != 0) || (g == a.n_groups - 1 && a.cu[g + 1] != a.B);
+        groups = __syncthreads_or(bad) ? 0 : a.n_groups;
+    }
+    for (int g = warp; g < groups; g += THREADS / 32) {
         const int b0 = a.cu[g], b1 = a.cu[g + 1];
         int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
         for (int b = b0 + lane; b < b1; b += 32) {
-            a.group_of[b] = g;
-            if (a.seq_lens[b] <= 0 || a.seq_lens[b] > a.pg.capacity) continue;
-            const int n = (int)keys_seen(a.pg, a.seq_lens[b], a.T, 0);
+            group_of[b] = g;
+            const int len = a.seq_lens[b];
+            if (len <= 0 || len > a.pg.capacity) continue;
+            const int n = (int)keys_seen(a.pg, len, a.T, 0);
             owner = b < owner ? b : owner;
             least = n < least ? n : least;
             ++members;
@@ -113,45 +121,36 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constan
             e.b = n > 0 ? owner : 0;
             e.lo = 0;
             e.hi = e.seen = n;
-            a.entry[g] = e;
+            entry[g] = e;
         }
     }
+    if (groups == 0 && !a.blocks)
+        for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
     __syncthreads();
-    if (groups == 0) {
-        for (int b = tid; b < a.B; b += PLAN_THREADS) a.group_of[b] = -1;
-        for (int g = tid; g < a.n_groups; g += PLAN_THREADS) {
-            Entry e;
-            e.rows = e.token = e.b = e.lo = e.hi = e.seen = 0;
-            a.entry[g] = e;
-        }
-        __syncthreads();
-    }
-    long long units = 0;
-    int shared_items = 0, own_items = 0;
-    for (int e0 = 0; e0 < a.entries; e0 += PLAN_THREADS) {
+    int units = 0, shared_items = 0, own_items = 0;
+    for (int e0 = 0; e0 < a.entries; e0 += THREADS) {
         const int i = e0 + tid;
         const bool on = i < a.entries, own = i >= a.n_groups;
         Entry e;
-        e.tiles = e.row_tiles = e.chunks = 0;
+        e.rows = e.token = e.b = e.lo = e.hi = e.seen = e.tile0 = e.tiles = e.row_tiles = e.chunks = 0;
         if (on) {
             if (!own) {
-                e = a.entry[i];
+                if (groups > 0) e = entry[i];
             } else if (a.blocks) {
                 const int b = i / a.T;
-                const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, i - b * a.T), N = (seen + a.block - 1) / a.block;
+                const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, i - b * a.T), N = (seen + a.block - 1) >> a.block_shift;
                 e.rows = a.G;
                 e.token = i;
                 e.b = b;
-                e.lo = 0;
-                e.seen = (int)seen;
-                e.hi = (int)((N < a.keep ? N : a.keep) * a.block);
+                e.seen = seen;
+                e.hi = (N < a.keep ? N : a.keep) << a.block_shift;
             } else {
-                const int b = i - a.n_groups, g = a.group_of[b];
+                const int b = i - a.n_groups, g = groups > 0 ? group_of[b] : -1;
                 e.rows = a.T * a.G;
                 e.token = b * a.T;
                 e.b = b;
                 e.hi = e.seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, 0);
-                e.lo = g >= 0 ? a.entry[g].hi : 0;
+                e.lo = g >= 0 ? entry[g].hi : 0;
                 if (e.lo > e.hi) e.lo = e.hi;
             }
             e.tile0 = e.lo / ATT_TILE;
@@ -160,41 +159,28 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constan
             e.chunks = (e.tiles + ATT_CHUNK - 1) / ATT_CHUNK;
         }
         const int lines = a.pg.H_kv * e.row_tiles, items = lines * e.chunks;
-        int all_items, all_shared;
-        const int before = scan_cta<PLAN_THREADS>(items, &all_items);
-        scan_cta<PLAN_THREADS>(own ? 0 : items, &all_shared);
-        // units: a scan in 64 bits
-        long long mine = (long long)lines * line_units(e), sum = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += y;
-        }
-        if (lane == 31) s_units[warp] = sum;
-        __syncthreads();
-        if (warp == 0) {
-            const long long part = s_units[lane];
-            long long p = part;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, p, o);
-                if (lane >= o) p += y;
-            }
-            s_units[lane] = p - part;
-            if (lane == 31) s_units[32] = p;
-        }
-        __syncthreads();
+        int all_items, all_shared = 0, all_units;
+        const int before = scan_cta<THREADS>(items, &all_items, s_part);
+        if (e0 < a.n_groups) scan_cta<THREADS>(own ? 0 : items, &all_shared, s_part);
+        const int units_before = scan_cta<THREADS>(lines * line_units(e), &all_units, s_part);
         if (on) {
-            e.u = units + s_units[warp] + sum - mine;
+            e.u = units + units_before;
             e.item = own ? own_items + before - all_shared : shared_items + before;      // (groups come first)
-            a.entry[i] = e;
+            entry[i] = e;
         }
-        units += s_units[32];
+        units += all_units;
         shared_items += all_shared;
         own_items += all_items - all_shared;
-        __syncthreads();
     }
-    if (tid == 0) a.head->units = units;
+    return units;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constant__ AttendArgs a) {
+    __shared__ int s_part[PLAN_THREADS / 32];
+    pdl_wait();
+    pdl_start_next();
+    const int units = make_plan<PLAN_THREADS>(a, a.entry, a.group_of, s_part);
+    if (threadIdx.x == 0) a.head->units = units;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -367,18 +353,12 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         for (int i = 0; i < 2; ++i) bar_init(smem_of(&sm.drained[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_wait();
-    const long long units = a.head->units;
-    const long long u0 = share_begin(units, a.grid, cta), u1 = share_begin(units, a.grid, cta + 1);
-    pdl_start_next();
-    if (u0 == u1) {
-        if (tid == 0) a.flags[cta] = 0;
-        return;
-    }
     if (warp == ATT_MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sm.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    pdl_wait();
+    pdl_start_next();
 
     // what the roles keep from piece to piece
     uint32_t loads = 0, tiles_done = 0;                  // loads issued (or consumed), tiles behind
@@ -387,30 +367,43 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 
     for (int batch = 0;; ++batch) {
         // ---- the pieces of this CTA, ATT_PIECES at a time ------------------------------------------
+        // (a plan of this CTA's own is laid out where the ring is, which is empty between batches)
+        const Entry* plan = a.entry;
+        int units;
+        if (a.planned) {
+            units = a.head->units;
+        } else {
+            Entry* own_plan = reinterpret_cast<Entry*>(sm.ring);
+            units = make_plan<ATT_THREADS>(a, own_plan, reinterpret_cast<int32_t*>(own_plan + ATT_THREADS), sm.warp_sum);
+            plan = own_plan;
+            __syncthreads();
+            if (cta == 0 && batch == 0) {                // for join_kernel
+                if (tid < a.entries) a.entry[tid] = own_plan[tid];
+                if (tid < a.B && !a.blocks) a.group_of[tid] = reinterpret_cast<int32_t*>(own_plan + ATT_THREADS)[tid];
+                if (tid == 0) a.head->units = units;
+            }
+        }
+        const int u0 = share_begin(units, a.grid, cta), u1 = share_begin(units, a.grid, cta + 1);
         int listed = 0;
-        for (int e0 = 0; e0 < a.entries; e0 += ATT_THREADS) {
+        for (int e0 = 0; e0 < a.entries && u0 < u1; e0 += ATT_THREADS) {
             const int i = e0 + tid;
             Entry e;
-            long long from = 0, to = 0, len = 1;
-            int count = 0, lines0 = 0, lines1 = 0;
-            // tiles of a line that units x0..x1-1 of it stand for
-            auto tiles_of = [&](long long x0, long long x1, int& t0, int& t1) {
-                t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0);
-                t1 = (int)(x1 > ATT_START ? x1 - ATT_START : 0);
-            };
+            int from = 0, to = 0, len = 1, count = 0, lines0 = 0, lines1 = 0;
+            // tiles of this CTA in a line: those that its units stand for
             auto range_of = [&](int line, int& t0, int& t1) {
-                const long long x0 = from > line * len ? from - line * len : 0, x1 = to < (line + 1) * len ? to - line * len : len;
-                tiles_of(x0, x1, t0, t1);
+                const int x0 = from > line * len ? from - line * len : 0, x1 = to - line * len < len ? to - line * len : len;
+                t0 = x0 > ATT_START ? x0 - ATT_START : 0;
+                t1 = x1 > ATT_START ? x1 - ATT_START : 0;
             };
             if (i < a.entries) {
-                e = a.entry[i];
+                e = plan[i];
                 len = line_units(e);
                 from = u0 > e.u ? u0 - e.u : 0;
-                const long long all = len * a.pg.H_kv * e.row_tiles;
+                const int all = len * a.pg.H_kv * e.row_tiles;
                 to = u1 - e.u < all ? u1 - e.u : all;
                 if (to > from) {
-                    lines0 = (int)(from / len);
-                    lines1 = (int)((to - 1) / len);
+                    lines0 = from / len;
+                    lines1 = (to - 1) / len;
                     for (int line = lines0; line <= lines1; line = line == lines0 && lines1 > lines0 + 1 ? lines1 : line + 1) {
                         int t0, t1;
                         range_of(line, t0, t1);
@@ -419,20 +412,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     if (lines1 > lines0 + 1) count += (lines1 - lines0 - 1) * e.chunks;
                 }
             }
-            // ordinal of this entry's first piece
-            int sum = count;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += y;
-            }
-            if (lane == 31) sm.warp_sum[warp] = sum;
-            __syncthreads();
-            int at = listed + sum - count - batch * ATT_PIECES, total = 0;
-            for (int w = 0; w < ATT_WARPS; ++w) {
-                if (w < warp) at += sm.warp_sum[w];
-                total += sm.warp_sum[w];
-            }
+            int total, at = listed + scan_cta<ATT_THREADS>(count, &total, sm.warp_sum) - batch * ATT_PIECES;     // of this entry's first piece
             listed += total;
             if (count > 0 && at < ATT_PIECES && at + count > 0) {
                 for (int line = lines0; line <= lines1 && at < ATT_PIECES; ++line) {
@@ -464,11 +444,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         }
         int pieces = listed - batch * ATT_PIECES;
         pieces = pieces < ATT_PIECES ? pieces : ATT_PIECES;
-        if (batch == 0) {
-            tc_before_sync();
-            __syncthreads();
-            tc_after_sync();
-        }
+        fence_async();                                   // the plan has been read: copies may take its place
+        tc_before_sync();
+        __syncthreads();
+        tc_after_sync();
         if (pieces <= 0 || !ok) break;                   // (the same for all threads)
         const uint32_t tmem = sm.tmem;
 
@@ -531,8 +510,11 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         const uint32_t any = __ballot_sync(0xffffffffu, r.valid != 0) & in_box, full = __ballot_sync(0xffffffffu, r.valid == 15u) & in_box;
                         // (the box's first row, from a lane whose rows count)
                         const int from = any ? __ffs(any) - 1 : leader, row = __shfl_sync(0xffffffffu, r.row[0], from) - (from - leader) * 4;
+                        const uint32_t pair = r.valid | __shfl_xor_sync(0xffffffffu, r.valid, 1) << 4;        // of 8 rows
                         if (keys || any == 0 || full == in_box) {
                             if (lane == leader) copy(map, dst, any ? row : a.total_rows, bar);
+                        } else if (box >= 8 && (pair == 0 || pair == 255u)) {
+                            if (!(lane & 1)) copy(&maps.v_eight, dst, pair ? r.row[0] : a.total_rows, bar);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) copy(&maps.v_row, dst + e * 128, r.valid >> e & 1 ? r.row[0] + e : a.total_rows, bar);
@@ -840,22 +822,29 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 // ---------------------------------------------------------------------------------------
 // join_kernel
 // ---------------------------------------------------------------------------------------
-constexpr int JOIN_THREADS = 512, JOIN_LIST = 256, JOIN_DEEP = 4;
+constexpr int JOIN_THREADS = 256, JOIN_DEEP = 4, JOIN_CTAS = 8;          // (CTAs that share the channels at most)
 
-// A CTA for a KV head of one sequence (or token).  First the parts that hold its rows are listed: those of the
-// group's line (its rows may lie across two), and those of its own.  Then four channels of a row go to a
-// thread, or to several that share the parts.  All orders are fixed, so that results do not depend on timing.
-template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttendArgs a) {
+// A KV head of one sequence (or token), or a share of its channels.  The parts that hold its rows lie one behind
+// the other: a line's, in the order of the CTAs that had it (its group's line, of which its rows may be in two, and its own).
+// Four channels of a row go to a thread, or to several that share the parts.  All orders are fixed, so that
+// results do not depend on timing.
+template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join_kernel(const __grid_constant__ AttendArgs a) {
     __shared__ float s_late[16 * 15 * 16];               // scores of the keys that the first token does not see
     __shared__ long long s_late_row[15];
-    __shared__ const float* s_list[3][JOIN_LIST];
+    __shared__ struct { const float* part; int count; } s_line[3];       // parts of a chunk of a line: the first one, and how many
     __shared__ float s_sum[6][JOIN_THREADS];
     pdl_wait();
     const int h = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
-    const bool failed = __syncthreads_or(tid < a.grid && a.flags[tid] != 0);
-    const long long units = a.head->units;
+    const int flag = tid < a.grid ? a.flags[tid] : 0;
+    const int units = a.head->units;
     const Entry own = a.entry[a.n_groups + i];
     const int g = a.blocks ? -1 : a.group_of[i];
+    Entry group;
+    group.rows = group.hi = group.tiles = group.chunks = 0;
+    if (g >= 0) group = a.entry[g];
+    const bool shared = own.hi >= group.hi && group.tiles > 0;           // (not an empty sequence)
+    const int shared_row = shared ? (own.token - group.token) * a.G : 0, m0 = shared_row / (2 * ATT_TILE);
+    const bool two = shared && (shared_row + own.rows - 1) / (2 * ATT_TILE) > m0;
     // later draft tokens: all queries are read before the first output is written, which may take their place
     int late = 0;
     if (!a.blocks && a.T > 1) {
@@ -883,50 +872,15 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
             s_late[x] = s * a.scale_log2;
         }
     }
-    // the parts of row tile m of an entry; how many
-    auto list_line = [&](const Entry& e, int m, const float* parts, int half_rows, const float** list) -> int {
-        const long long len = line_units(e);
-        if (len == 0) return 0;
-        const int line = h * e.row_tiles + m;
-        const long long first = e.u + line * len;
-        const int c0 = share_of(units, a.grid, first), c1 = share_of(units, a.grid, first + len - 1);
-        int count = 0;
-        const int c = c0 + tid;                          // (a CTA of the other kernel to a thread: grid <= JOIN_LIST - 16)
-        int t0 = 0, t1 = 0;
-        if (c <= c1) {
-            const long long x0 = share_begin(units, a.grid, c) - first, x1 = share_begin(units, a.grid, c + 1) - first;
-            t0 = (int)(x0 > ATT_START ? x0 - ATT_START : 0);
-            t1 = (int)((x1 < len ? x1 : len) - ATT_START);
-            if (t1 > t0) count = (t1 - 1) / ATT_CHUNK - t0 / ATT_CHUNK + 1;
-        }
-        int total;
-        const int at = scan_cta<JOIN_THREADS>(count, &total);
-        for (int k = 0; k < count; ++k)
-            list[at + k] = parts + ((long long)e.item + (long long)line * e.chunks + t0 / ATT_CHUNK + k + c) * 2 * half_floats(half_rows, D);
-        return total;
-    };
-    int shared_row = 0, n_first = 0, n_second = 0, m0 = 0;
-    Entry group;
-    group.rows = 0;
-    if (g >= 0) {
-        group = a.entry[g];
-        shared_row = (own.token - group.token) * a.G;
-        m0 = shared_row / (2 * ATT_TILE);
-        if (own.hi >= group.hi) {                        // (not an empty sequence)
-            n_first = list_line(group, m0, a.shared_parts, ATT_TILE, s_list[0]);
-            if ((shared_row + own.rows - 1) / (2 * ATT_TILE) > m0) n_second = list_line(group, m0 + 1, a.shared_parts, ATT_TILE, s_list[1]);
-        }
-    }
-    const int n_own = list_line(own, 0, a.own_parts, a.own_rows, s_list[2]);
-    __syncthreads();
+    const bool failed = __syncthreads_or(flag != 0);
 
-    const int work = own.rows * (D / 4);
+    const int wide = D / 4 / gridDim.z, work = own.rows * wide;
     int splits = 1;
     while (2 * splits * work <= JOIN_THREADS) splits *= 2;
     for (int x0 = 0; x0 < work; x0 += JOIN_THREADS) {
         const int split = splits > 1 ? tid / work : 0, x = x0 + (splits > 1 ? tid % work : tid);
         const bool on = x < work && split < splits;
-        const int r = x % own.rows, c4 = x / own.rows;
+        const int r = x % own.rows, c4 = blockIdx.z * wide + x / own.rows;
         float M = ATT_NONE, L = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
         auto add = [&](float m, float l, float4 o) {
@@ -940,10 +894,10 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
         };
         // The row `row` of `rows` in a row tile: with more than 128 rows in one half of each part, with fewer in
         // both, in `copies` places.
-        auto add_list = [&](const float** list, int count, int half_rows, int row, int rows) {
+        auto add_parts = [&](const float* parts, int count, int half_rows, int row, int rows) {
             const bool both = rows > ATT_TILE;
             const int copies = copies_of(rows), places = both ? 1 : 2 * copies, all = count * places, apart = half_rows / copies;
-            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row;
+            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row, half_size = (int)half_floats(half_rows, D);
             for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
                 float2 ml[JOIN_DEEP];
                 float4 o[JOIN_DEEP];
@@ -952,10 +906,10 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
                     const int k = k0 + d * splits;
                     ml[d].x = ATT_NONE;
                     if (k < all) {
-                        const int part = k / places, place = k - part * places, at = at0 + place / 2 * apart;
-                        const float* half = list[part] + (h0 + (place & 1)) * half_floats(half_rows, D);
-                        ml[d] = *reinterpret_cast<const float2*>(half + (long long)half_rows * D + 2 * at);
-                        o[d] = *reinterpret_cast<const float4*>(half + ((long long)c4 * half_rows + at) * 4);
+                        const int part = both ? k : k / places, place = k - part * places, at = at0 + (place >> 1) * apart;
+                        const float* half = parts + (2ll * part + h0 + (place & 1)) * half_size;
+                        ml[d] = *reinterpret_cast<const float2*>(half + half_rows * D + 2 * at);
+                        o[d] = *reinterpret_cast<const float4*>(half + (c4 * half_rows + at) * 4);
                     }
                 }
 #pragma unroll
@@ -963,22 +917,39 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS) join_ke
                     if (ml[d].x != ATT_NONE) add(ml[d].x, ml[d].y, o[d]);
             }
         };
-        if (on) {
-            if (n_first + n_second > 0) {
-                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), rows = group.rows - (m0 + m) * (2 * ATT_TILE);
-                add_list(s_list[m], m == 0 ? n_first : n_second, ATT_TILE, row % (2 * ATT_TILE), rows < 2 * ATT_TILE ? rows : 2 * ATT_TILE);
+        // chunk by chunk (of lines of more than ATT_CHUNK tiles)
+        const int chunks = group.chunks > own.chunks ? group.chunks : own.chunks;
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            if (chunk > 0) __syncthreads();
+            if (tid % 32 == 0 && tid < 96) {             // one warp for each: who had the chunk
+                const int which = tid / 32;
+                const Entry& e = which < 2 ? group : own;
+                const int half_rows = which < 2 ? ATT_TILE : a.own_rows;
+                s_line[which].count = 0;
+                if (chunk < e.chunks && (which == 2 || (shared && (which == 0 || two)))) {
+                    const int line = h * e.row_tiles + (which < 2 ? m0 + which : 0), tile0 = chunk * ATT_CHUNK;
+                    const int tiles = e.tiles - tile0 < ATT_CHUNK ? e.tiles - tile0 : ATT_CHUNK, u = e.u + line * line_units(e) + ATT_START + tile0;
+                    const int c0 = share_of(units, a.grid, u), c1 = share_of(units, a.grid, u + tiles - 1);
+                    s_line[which].count = c1 - c0 + 1;
+                    s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
+                                         ((long long)e.item + (long long)line * e.chunks + chunk + c0) * 2 * half_floats(half_rows, D);
+                }
             }
-            add_list(s_list[2], n_own, a.own_rows, r, own.rows);
+            __syncthreads();
+            if (on) {
+                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), rows = group.rows - (m0 + m) * (2 * ATT_TILE);
+                if (s_line[m].count > 0)
+                    add_parts(s_line[m].part, s_line[m].count, ATT_TILE, row % (2 * ATT_TILE), rows < 2 * ATT_TILE ? rows : 2 * ATT_TILE);
+                add_parts(s_line[2].part, s_line[2].count, a.own_rows, r, own.rows);
+            }
         }
-        if (splits > 1) {
+        for (int k = splits / 2; k > 0; k /= 2) {        // the upper half of the splits to the lower
+            __syncthreads();
             s_sum[0][tid] = M; s_sum[1][tid] = L;
             s_sum[2][tid] = O.x; s_sum[3][tid] = O.y; s_sum[4][tid] = O.z; s_sum[5][tid] = O.w;
             __syncthreads();
-            if (on && split == 0)
-                for (int k = 1; k < splits; ++k) {
-                    const int y = tid + k * work;
-                    if (s_sum[0][y] != ATT_NONE) add(s_sum[0][y], s_sum[1][y], make_float4(s_sum[2][y], s_sum[3][y], s_sum[4][y], s_sum[5][y]));
-                }
+            const int y = tid + k * work;
+            if (on && split < k && s_sum[0][y] != ATT_NONE) add(s_sum[0][y], s_sum[1][y], make_float4(s_sum[2][y], s_sum[3][y], s_sum[4][y], s_sum[5][y]));
         }
         if (!on || split > 0) continue;
         const long long token = own.token + r / a.G;

@@ -83,9 +83,9 @@ __device__ __forceinline__ void pdl_start_next() { asm volatile("griddepcontrol.
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Sum over the threads before this one, and over all; every thread of the CTA calls it.
-template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total) {
-    __shared__ int s_part[THREADS / 32];
+// Sum over the threads before this one, and over all; every thread of the CTA calls it.  s_part: a number for
+// each warp.
+template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total, int* s_part) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int sum = x;
 #pragma unroll
@@ -99,6 +99,10 @@ template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total
     const int part = lane < THREADS / 32 ? s_part[lane] : 0;
     *total = __reduce_add_sync(0xffffffffu, part);
     return __reduce_add_sync(0xffffffffu, lane < warp ? part : 0) + sum - x;
+}
+template <int THREADS> __device__ __forceinline__ int scan_cta(int x, int* total) {
+    __shared__ int s_part[THREADS / 32];
+    return scan_cta<THREADS>(x, total, s_part);
 }
 
 // The cache as the kernels see it (retopk_pages_t with 64-bit strides worked out).

@@ -48,7 +48,7 @@ int device_setup(DeviceSetup* setup) {
             return RETOPK_ECUDA;
         }
         st.encode = reinterpret_cast<EncodeTiled>(fn);
-        if (st.num_sms > JOIN_LIST - 16) st.num_sms = JOIN_LIST - 16;        // (CTAs of the attention)
+        if (st.num_sms > JOIN_THREADS) st.num_sms = JOIN_THREADS;        // (CTAs of the attention, each with a flag that a thread reads)
         st.ready = true;
     }
     *setup = st;
@@ -104,11 +104,14 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
 }
 
 template <int DT, int D> int launch_attention(const AttendParams& p, int sequences, cudaStream_t s) {
-    int rc = launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, p.a);
+    int rc = p.a.planned ? launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, p.a) : RETOPK_OK;
     if (rc != RETOPK_OK) return rc;
     rc = launch(attend_kernel<DT, D>, dim3((unsigned)p.a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
     if (rc != RETOPK_OK) return rc;
-    return launch(join_kernel<DT, D>, dim3((unsigned)p.a.pg.H_kv, (unsigned)sequences), JOIN_THREADS, 0, s, p.a);
+    // as many CTAs to a head as give the device something to do; one where outputs take the place of queries that it reads
+    int shares = 1;
+    while ((p.a.T == 1 || p.a.out != p.a.q) && shares < JOIN_CTAS && (long long)p.a.pg.H_kv * sequences * shares < 3ll * p.a.grid) shares *= 2;
+    return launch(join_kernel<DT, D>, dim3((unsigned)p.a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, p.a);
 }
 
 // Rows of 64 channels each, `box` rows to a copy, into shared memory as the tensor cores' operands lie there.
@@ -127,6 +130,7 @@ int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, i
     if (box > ATT_TILE) box = ATT_TILE;
     const int64_t rows_in_all = pages->n_pages * pages->H_kv * pages->page_size;
     if (!encode_rows(dev.encode, &p.maps.k, pages, pages->k, rows_in_all, box) || !encode_rows(dev.encode, &p.maps.v, pages, pages->v, rows_in_all, box) ||
+        !encode_rows(dev.encode, &p.maps.v_eight, pages, pages->v, rows_in_all, 8) ||
         !encode_rows(dev.encode, &p.maps.v_row, pages, pages->v, rows_in_all, 1))
         return RETOPK_ECUDA;
     a.box_rows = box;
@@ -139,6 +143,7 @@ int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, i
     a.shared_parts = reinterpret_cast<float*>(ws + w.shared_parts);
     a.own_parts = reinterpret_cast<float*>(ws + w.own_parts);
     a.entries = a.n_groups + sequences;
+    a.planned = a.entries > ATT_THREADS;
     a.grid = dev.num_sms;
     a.own_rows = half_rows(rows);
     if (pages->format == RETOPK_PAGES_BF16)
