@@ -31,12 +31,12 @@ constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // referenc
 
 struct Entry {
     int u;                      // where its lines begin
-    int item;                   // number of its first (line, chunk)
+    int item;                   // number of its first (line, chunk): in the order of the lines, with places to spare
     int rows, token;            // query rows: heads of a group of the tokens from `token` on
     int b;                      // sequence whose row of the block table holds the keys
     int lo, hi, seen;           // keys lo..hi-1 (of the selected blocks one behind the other: 0..hi-1, below `seen`)
     int tile0, tiles;
-    int row_tiles, chunks;      // lines of a KV head (256 rows each); chunks of a line
+    int row_tiles, chunks;      // 256 query rows each: with the KV heads of each, its lines; chunks of a line
 };
 struct AttendHeader { int units; };
 
@@ -56,7 +56,7 @@ struct AttendArgs {
     const int32_t *cu, *shared_lens;
     const int32_t* blocks;      // [B, T, H_kv, keep], or null: all keys
     int keep, block, block_shift;
-    int entries, grid, own_rows;                         // own_rows: rows of a half of a part that belongs to one sequence
+    int entries, grid, max_chunks, own_rows;             // max_chunks: of a line at most; own_rows: rows of a half of a part that belongs to one sequence
     AttendHeader* head;
     Entry* entry;
     int32_t *group_of, *flags;  // group of a sequence or -1; CTAs that gave up
@@ -85,92 +85,91 @@ __device__ __forceinline__ int share_of(int units, int grid, int u) { return (in
 // ---------------------------------------------------------------------------------------
 constexpr int PLAN_THREADS = 1024;
 
+// Where the plan is made from: in global memory, or copies of it in shared memory.
+struct PlanInput { const int32_t *seq_lens, *cu, *shared_lens; };
+
 // By one CTA: the entries, the group of each sequence, and how long the line is.  Groups: the first member that is not
 // empty owns the keys, the fewest rows that any of them sees are shared; a member alone shares nothing.
 // s_part: a number for each warp.
-template <int THREADS> __device__ __forceinline__ int make_plan(const AttendArgs& a, Entry* entry, int32_t* group_of, int* s_part) {
+template <int THREADS>
+__device__ __forceinline__ int make_plan(const AttendArgs& a, const PlanInput& in, Entry* entry, int32_t* group_of, int* s_part) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int groups = 0;
     if (a.n_groups > 0) {
         bool bad = false;
         for (int g = tid; g < a.n_groups; g += THREADS)
-            bad |= a.cu[g] < 0 || a.cu[g + 1] < a.cu[g] || a.cu[g + 1] > a.B || (g == 0 && a.cu[0] != 0) || (g == a.n_groups - 1 && a.cu[g + 1] != a.B);
+            bad |= in.cu[g] < 0 || in.cu[g + 1] < in.cu[g] || in.cu[g + 1] > a.B || (g == 0 && in.cu[0] != 0) || (g == a.n_groups - 1 && in.cu[g + 1] != a.B);
         groups = __syncthreads_or(bad) ? 0 : a.n_groups;
-    }
-    for (int g = warp; g < groups; g += THREADS / 32) {
-        const int b0 = a.cu[g], b1 = a.cu[g + 1];
-        int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
-        for (int b = b0 + lane; b < b1; b += 32) {
-            group_of[b] = g;
-            const int len = a.seq_lens[b];
-            if (len <= 0 || len > a.pg.capacity) continue;
-            const int n = (int)keys_seen(a.pg, len, a.T, 0);
-            owner = b < owner ? b : owner;
-            least = n < least ? n : least;
-            ++members;
+        for (int g = warp; g < groups; g += THREADS / 32) {
+            const int b0 = in.cu[g], b1 = in.cu[g + 1];
+            int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
+            for (int b = b0 + lane; b < b1; b += 32) {
+                group_of[b] = g;
+                const int len = in.seq_lens[b];
+                if (len <= 0 || len > a.pg.capacity) continue;
+                const int n = (int)keys_seen(a.pg, len, a.T, 0);
+                owner = b < owner ? b : owner;
+                least = n < least ? n : least;
+                ++members;
+            }
+            owner = __reduce_min_sync(0xffffffffu, owner);
+            least = __reduce_min_sync(0xffffffffu, least);
+            members = __reduce_add_sync(0xffffffffu, members);
+            if (lane == 0) {
+                int n = in.shared_lens[g];
+                n = members < 2 || n < 0 ? 0 : (n < least ? n : least);
+                Entry e;
+                e.rows = (b1 - b0) * a.T * a.G;
+                e.token = b0 * a.T;
+                e.b = n > 0 ? owner : 0;
+                e.hi = n;
+                entry[g] = e;
+            }
         }
-        owner = __reduce_min_sync(0xffffffffu, owner);
-        least = __reduce_min_sync(0xffffffffu, least);
-        members = __reduce_add_sync(0xffffffffu, members);
-        if (lane == 0) {
-            int n = a.shared_lens[g];
-            n = members < 2 || n < 0 ? 0 : (n < least ? n : least);
-            Entry e;
-            e.rows = (b1 - b0) * a.T * a.G;
-            e.token = b0 * a.T;
-            e.b = n > 0 ? owner : 0;
-            e.lo = 0;
-            e.hi = e.seen = n;
-            entry[g] = e;
-        }
-    }
-    if (groups == 0 && !a.blocks)
+        if (groups == 0)
+            for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
+        __syncthreads();
+    } else if (!a.blocks) {
         for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
-    __syncthreads();
-    int units = 0, shared_items = 0, own_items = 0;
+    }
+    int units = 0;
     for (int e0 = 0; e0 < a.entries; e0 += THREADS) {
         const int i = e0 + tid;
-        const bool on = i < a.entries, own = i >= a.n_groups;
+        const bool on = i < a.entries;
         Entry e;
-        e.rows = e.token = e.b = e.lo = e.hi = e.seen = e.tile0 = e.tiles = e.row_tiles = e.chunks = 0;
-        if (on) {
-            if (!own) {
-                if (groups > 0) e = entry[i];
-            } else if (a.blocks) {
-                const int b = i / a.T;
-                const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, i - b * a.T), N = (seen + a.block - 1) >> a.block_shift;
+        e.rows = e.token = e.b = e.lo = e.hi = e.item = 0;
+        if (i < a.n_groups) {
+            if (groups > 0) e = entry[i];
+            e.lo = 0;
+            e.seen = e.hi;
+            // (groups of x rows in all have at most one row tile each more than x / 256, and so do the first of them)
+            e.item = (i + e.token * a.G / (2 * ATT_TILE)) * a.pg.H_kv * a.max_chunks;
+        } else if (on) {
+            const int at = i - a.n_groups, b = a.blocks ? at / a.T : at;
+            e.b = b;
+            e.item = at * a.pg.H_kv * a.max_chunks;
+            e.seen = (int)keys_seen(a.pg, in.seq_lens[b], a.T, a.blocks ? at - b * a.T : 0);
+            if (a.blocks) {
+                const int N = (e.seen + a.block - 1) >> a.block_shift;
                 e.rows = a.G;
-                e.token = i;
-                e.b = b;
-                e.seen = seen;
+                e.token = at;
                 e.hi = (N < a.keep ? N : a.keep) << a.block_shift;
             } else {
-                const int b = i - a.n_groups, g = groups > 0 ? group_of[b] : -1;
                 e.rows = a.T * a.G;
                 e.token = b * a.T;
-                e.b = b;
-                e.hi = e.seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, 0);
-                e.lo = g >= 0 ? entry[g].hi : 0;
+                e.hi = e.seen;
+                if (groups > 0) e.lo = entry[group_of[b]].hi;
                 if (e.lo > e.hi) e.lo = e.hi;
             }
-            e.tile0 = e.lo / ATT_TILE;
-            e.tiles = e.hi > e.lo ? (e.hi + ATT_TILE - 1) / ATT_TILE - e.tile0 : 0;
-            e.row_tiles = (e.rows + 2 * ATT_TILE - 1) / (2 * ATT_TILE);
-            e.chunks = (e.tiles + ATT_CHUNK - 1) / ATT_CHUNK;
         }
-        const int lines = a.pg.H_kv * e.row_tiles, items = lines * e.chunks;
-        int all_items, all_shared = 0, all_units;
-        const int before = scan_cta<THREADS>(items, &all_items, s_part);
-        if (e0 < a.n_groups) scan_cta<THREADS>(own ? 0 : items, &all_shared, s_part);
-        const int units_before = scan_cta<THREADS>(lines * line_units(e), &all_units, s_part);
-        if (on) {
-            e.u = units + units_before;
-            e.item = own ? own_items + before - all_shared : shared_items + before;      // (groups come first)
-            entry[i] = e;
-        }
-        units += all_units;
-        shared_items += all_shared;
-        own_items += all_items - all_shared;
+        e.tile0 = e.lo / ATT_TILE;
+        e.tiles = e.hi > e.lo ? (e.hi + ATT_TILE - 1) / ATT_TILE - e.tile0 : 0;
+        e.row_tiles = (e.rows + 2 * ATT_TILE - 1) / (2 * ATT_TILE);
+        e.chunks = (e.tiles + ATT_CHUNK - 1) / ATT_CHUNK;
+        int all;
+        e.u = units + scan_cta<THREADS>(a.pg.H_kv * e.row_tiles * line_units(e), &all, s_part);
+        if (on) entry[i] = e;
+        units += all;
     }
     return units;
 }
@@ -179,7 +178,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const __grid_constan
     __shared__ int s_part[PLAN_THREADS / 32];
     pdl_wait();
     pdl_start_next();
-    const int units = make_plan<PLAN_THREADS>(a, a.entry, a.group_of, s_part);
+    const int units = make_plan<PLAN_THREADS>(a, {a.seq_lens, a.cu, a.shared_lens}, a.entry, a.group_of, s_part);
     if (threadIdx.x == 0) a.head->units = units;
 }
 
@@ -220,18 +219,26 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t issue) {
+    asm volatile("{\n.reg .pred q;\nsetp.ne.u32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(issue) : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// D (+)= A B, 128 x N x 16; A in shared memory or in tensor memory.
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// D (+)= A B, 128 x N x 16; A in shared memory or in tensor memory.  The whole warp comes here, the one lane with
+// `issue` issues: operands that are the same for all lanes stay in uniform registers, where the instruction takes them from.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, uint32_t issue) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(issue) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add, uint32_t issue) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"(issue) : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one;
 }
 
 #define TC_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
@@ -249,6 +256,11 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* x) {
 __device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t* x) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : TC_R8(x, 0), TC_R8(x, 8) : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* x) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8), TC_W8(x, 16), TC_W8(x, 24) : "memory");
 }
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -353,6 +365,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         for (int i = 0; i < 2; ++i) bar_init(smem_of(&sm.drained[i]), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (tid == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+    }
     if (warp == ATT_MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sm.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -374,12 +390,18 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             units = a.head->units;
         } else {
             Entry* own_plan = reinterpret_cast<Entry*>(sm.ring);
-            units = make_plan<ATT_THREADS>(a, own_plan, reinterpret_cast<int32_t*>(own_plan + ATT_THREADS), sm.warp_sum);
-            plan = own_plan;
+            int32_t* const lens = reinterpret_cast<int32_t*>(own_plan + ATT_THREADS);
+            int32_t *const cu = lens + ATT_THREADS, *const shared_lens = cu + ATT_THREADS, *const group_of = shared_lens + ATT_THREADS;
+            if (tid < a.B) lens[tid] = a.seq_lens[tid];
+            if (tid <= a.n_groups && a.n_groups > 0) cu[tid] = a.cu[tid];
+            if (tid < a.n_groups) shared_lens[tid] = a.shared_lens[tid];
             __syncthreads();
+            units = make_plan<ATT_THREADS>(a, {lens, cu, shared_lens}, own_plan, group_of, sm.warp_sum);
+            plan = own_plan;
             if (cta == 0 && batch == 0) {                // for join_kernel
+                __syncthreads();
                 if (tid < a.entries) a.entry[tid] = own_plan[tid];
-                if (tid < a.B && !a.blocks) a.group_of[tid] = reinterpret_cast<int32_t*>(own_plan + ATT_THREADS)[tid];
+                if (tid < a.B && !a.blocks) a.group_of[tid] = group_of[tid];
                 if (tid == 0) a.head->units = units;
             }
         }
@@ -423,16 +445,16 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         const int chunk = t0 / ATT_CHUNK, end = (chunk + 1) * ATT_CHUNK < t1 ? (chunk + 1) * ATT_CHUNK : t1;
                         Piece p;
                         p.b = e.b;
-                        p.h = line / e.row_tiles;
+                        p.h = line % a.pg.H_kv;
                         p.token = e.token;
-                        p.row0 = line % e.row_tiles * (2 * ATT_TILE);
+                        p.row0 = line / a.pg.H_kv * (2 * ATT_TILE);
                         p.rows = e.rows - p.row0 < 2 * ATT_TILE ? e.rows - p.row0 : 2 * ATT_TILE;
                         p.lo = e.lo;
                         p.hi = e.hi;
                         p.seen = e.seen;
                         p.tile0 = e.tile0 + t0;
                         p.tile1 = e.tile0 + end;
-                        const long long slot = (long long)e.item + (long long)line * e.chunks + chunk + cta;
+                        const long long slot = (long long)e.item + (long long)line * a.max_chunks + chunk + cta;
                         const bool own = i >= a.n_groups;
                         p.half_rows = own ? a.own_rows : ATT_TILE;
                         p.part = (own ? a.own_parts : a.shared_parts) + slot * 2 * half_floats(p.half_rows, D);
@@ -556,77 +578,81 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             __syncwarp();
         } else if (warp >= ATT_MMA_WARP) {
             // ---- products: a warp for each stream ------------------------------------------------
-            if (lane == 0) {
-                constexpr uint32_t QK = tc_shape<DT>(ATT_TILE / 2, false), PV = tc_shape<DT>(D, true);
-                const int s = warp - ATT_MMA_WARP;
-                const uint32_t S = tmem + s * ATT_TILE, O = tmem + 2 * ATT_TILE + s * D, q = smem_of(sm.q[s]);
-                for (int i = 0; i < pieces && ok; ++i) {
-                    const Piece& p = sm.piece[i];
-                    const int n = p.tile1 - p.tile0, step = p.rows > ATT_TILE ? 1 : 2;
-                    auto wait_full = [&](int j) { return bar_wait(smem_of(&sm.full[(loads + j) % Smem::SLOTS]), (loads + j) / Smem::SLOTS & 1, gave_up); };
-                    auto tile_at = [&](int j) { return smem_of(sm.ring[(loads + j) % Smem::SLOTS]); };
-                    auto empty_at = [&](int j) { return smem_of(&sm.empty[(loads + j) % Smem::SLOTS]); };
-                    // Both threads see all loads go by, so that neither runs away from the other: a phase of a
-                    // barrier is told from the one after the next by nothing else.
-                    int seen = 0;
-                    auto see = [&](int j) -> bool {      // the other stream's loads before j
+            constexpr uint32_t QK = tc_shape<DT>(ATT_TILE / 2, false), PV = tc_shape<DT>(D, true);
+            const uint32_t issue = elect_one();          // always the same lane
+            const int s = warp - ATT_MMA_WARP;
+            const uint32_t S = tmem + s * ATT_TILE, O = tmem + 2 * ATT_TILE + s * D, q = smem_of(sm.q[s]);
+            for (int i = 0; i < pieces && ok; ++i) {
+                const Piece& p = sm.piece[i];
+                const int n = __shfl_sync(0xffffffffu, p.tile1 - p.tile0, 0), step = __shfl_sync(0xffffffffu, p.rows > ATT_TILE ? 1 : 2, 0);
+                auto wait_full = [&](int j) { return bar_wait(smem_of(&sm.full[(loads + j) % Smem::SLOTS]), (loads + j) / Smem::SLOTS & 1, gave_up); };
+                auto tile_at = [&](int j) { return __shfl_sync(0xffffffffu, smem_of(sm.ring[(loads + j) % Smem::SLOTS]), 0); };
+                auto empty_at = [&](int j) { return smem_of(&sm.empty[(loads + j) % Smem::SLOTS]); };
+                // Both warps see all loads go by, so that neither runs away from the other: a phase of a
+                // barrier is told from the one after the next by nothing else.
+                int seen = 0;
+                auto see = [&](int j) -> bool {          // the other stream's loads before j
+                    if (step == 2)
                         for (; seen < j; ++seen)
-                            if (step == 2 && (tile_of_load(seen, n) & 1) != s) {
+                            if ((tile_of_load(seen, n) & 1) != s) {
                                 if (!wait_full(seen)) return false;
-                                bar_arrive(empty_at(seen));
+                                if (issue) bar_arrive(empty_at(seen));
                             }
-                        return true;
-                    };
-                    auto score = [&](int t, int h) {     // S = Q K^T of half a tile
-                        const uint32_t k = tile_at(k_load(t)) + h * (ATT_TILE / 2 * 128);
+                    return true;
+                };
+                auto score = [&](int t, int h) {         // S = Q K^T of half a tile
+                    const uint32_t k = tile_at(k_load(t)) + h * (ATT_TILE / 2 * 128);
+                    tc_after_sync();
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
+                        tc_mma_ss(S + h * (ATT_TILE / 2), tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0, issue);
+                    }
+                    tc_commit(smem_of(&sm.s_ready[s][h]), issue);
+                    if (h == 1) tc_commit(empty_at(k_load(t)), issue);
+                };
+                // weights that S takes the place of have been read
+                auto wait_o = [&](int h) { return turns == 0 || bar_wait(smem_of(&sm.o_ready[s][h]), (turns - 1) & 1, gave_up); };
+                const int first = step == 1 ? 0 : s;
+                if (first < n) {
+                    ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first));
+                    ++begun;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        ok = ok && wait_o(h);
+                        if (__all_sync(0xffffffffu, ok)) score(first, h);
+                    }
+                }
+                for (int t = first; t < n && __all_sync(0xffffffffu, ok); t += step) {
+                    ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
+                    const uint32_t v = tile_at(v_load(t, n));
+                    const bool more = t + step < n;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.p_ready[s][h]), turns & 1, gave_up));
+                        if (!ok) break;
                         tc_after_sync();
 #pragma unroll
-                        for (int x = 0; x < D / 16; ++x) {
-                            const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
-                            tc_mma_ss(S + h * (ATT_TILE / 2), tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0);
-                        }
-                        tc_commit(smem_of(&sm.s_ready[s][h]));
-                        if (h == 1) tc_commit(empty_at(k_load(t)));
-                    };
-                    // weights that S takes the place of have been read
-                    auto wait_o = [&](int h) { return turns == 0 || bar_wait(smem_of(&sm.o_ready[s][h]), (turns - 1) & 1, gave_up); };
-                    const int first = step == 1 ? 0 : s;
-                    if (first < n) {
-                        ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first));
-                        ++begun;
-                        for (int h = 0; h < 2 && ok; ++h) {
-                            ok = wait_o(h);
-                            if (ok) score(first, h);
+                        for (int x = 0; x < ATT_TILE / 32; ++x)                  // O += P V
+                            tc_mma_ts(O, S + h * (ATT_TILE / 2) + x * 8, tc_operand(v + (h * 4 + x) * 2048, ATT_TILE * 128), PV, x > 0 || h > 0 || t >= step, issue);
+                        tc_commit(smem_of(&sm.o_ready[s][h]), issue);
+                        if (h == 1) tc_commit(empty_at(v_load(t, n)), issue);
+                        if (more) {
+                            ok = __all_sync(0xffffffffu, (h == 1 || wait_full(k_load(t + step))) && bar_wait(smem_of(&sm.o_ready[s][h]), turns & 1, gave_up));
+                            if (ok) score(t + step, h);
                         }
                     }
-                    for (int t = first; t < n && ok; t += step) {
-                        ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
-                        const uint32_t v = tile_at(v_load(t, n));
-                        for (int h = 0; h < 2 && ok; ++h) {
-                            ok = bar_wait(smem_of(&sm.p_ready[s][h]), turns & 1, gave_up);
-                            if (!ok) break;
-                            tc_after_sync();
-#pragma unroll
-                            for (int x = 0; x < ATT_TILE / 32; ++x)              // O += P V
-                                tc_mma_ts(O, S + h * (ATT_TILE / 2) + x * 8, tc_operand(v + (h * 4 + x) * 2048, ATT_TILE * 128), PV, x > 0 || h > 0 || t >= step);
-                            tc_commit(smem_of(&sm.o_ready[s][h]));
-                            if (h == 1) tc_commit(empty_at(v_load(t, n)));
-                            if (t + step < n) {
-                                ok = (h == 1 || wait_full(k_load(t + step))) && bar_wait(smem_of(&sm.o_ready[s][h]), turns & 1, gave_up);
-                                if (ok) score(t + step, h);
-                            }
-                        }
-                        ++turns;
-                    }
-                    ok = ok && see(2 * n);
-                    loads += 2 * n;
+                    ++turns;
                 }
-                if (!ok) {                               // what was issued ends before the memory is given back
-                    tc_commit(smem_of(&sm.drained[s]));
-                    volatile int never = 0;
-                    bar_wait(smem_of(&sm.drained[s]), 0, &never);
-                    *gave_up = 1;
-                }
+                ok = ok && see(2 * n);
+                ok = __all_sync(0xffffffffu, ok);
+                loads += 2 * n;
+            }
+            if (!ok) {                                   // what was issued ends before the memory is given back
+                tc_commit(smem_of(&sm.drained[s]), issue);
+                volatile int never = 0;
+                bar_wait(smem_of(&sm.drained[s]), 0, &never);
+                *gave_up = 1;
             }
             __syncwarp();
         } else {
@@ -702,76 +728,82 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
                             if (!first) mx = 0;
                             if (!second) my = 0;
-                            if (first) tc_ld32(Sh, x);
-                            if (second) tc_ld32(Sh + 32, y);
-                            tc_wait_ld();
-                            auto hide = [&](uint32_t* v, uint32_t m) {           // keys that do not count: weight 0
-                                if (m == ~0u) return;
-#pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (!(m >> j & 1)) v[j] = 0xff800000u;
-                            };
-                            hide(x, mx);
-                            hide(y, my);
-                            float top = -INFINITY;
-                            if (mx | my) {
-                                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                                for (int j = 0; j < 32; j += 2) {
-                                    most[j & 2] = fmaxf(most[j & 2], fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 1])));
-                                    most[(j & 2) + 1] = fmaxf(most[(j & 2) + 1], fmaxf(__uint_as_float(y[j]), __uint_as_float(y[j + 1])));
-                                }
-                                top = fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW);
-                            }
-                            // The reference follows the maximum when that is more than 8 above it: weights up to 2^8 fit
-                            // both types, and the sums in tensor memory are seldom touched.
-                            const bool follow = live && top > (ref == ATT_NONE ? ref : ref + 8.f);
-                            float f = 1.f;
-                            if (__any_sync(0xffffffffu, follow)) {
-                                if (follow) {
-                                    f = exp2_approx(ref - top);
-                                    ref = top;
-                                }
-                                if (k > 0 || h > 0) {
-                                    // (the product of the half before may be under way)
-                                    ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][1 - h]), (h == 0 ? turns - 1 : turns) & 1, gave_up));
-                                    if (!ok) break;
-                                    tc_after_sync();
-#pragma unroll 1
-                                    for (int c = 0; c < D; c += 16) {
-                                        uint32_t o[16];
-                                        tc_ld16(O + c, o);
-                                        tc_wait_ld();
-#pragma unroll
-                                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                        tc_st16(O + c, o);
-                                    }
-                                }
-                            }
-                            float2 sum = make_float2(0.f, 0.f), more = make_float2(0.f, 0.f);
                             if (first | second) {
-                                const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
-                                auto weigh = [&](uint32_t* v, float2& total) {
+                                if (first) tc_ld32(Sh, x);
+                                if (second) tc_ld32(Sh + 32, y);
+                                tc_wait_ld();
+                                auto hide = [&](uint32_t* v, uint32_t m) {       // keys that do not count: weight 0
+                                    if (m == ~0u) return;
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j)
+                                        if (!(m >> j & 1)) v[j] = 0xff800000u;
+                                };
+                                hide(x, mx);
+                                hide(y, my);
+                                uint32_t w[32];
+                                float2 sum, more;
+                                auto weigh = [&]() {
+                                    const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
+                                    sum = more = make_float2(0.f, 0.f);
 #pragma unroll
                                     for (int j = 0; j < 32; j += 2) {
-                                        float2 w = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), scale2, ref2);
-                                        w.x = exp2_approx(w.x);
-                                        w.y = exp2_approx(w.y);
-                                        total = add2(total, w);
-                                        v[j / 2] = pack2<DT>(w.x, w.y);
+                                        float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), scale2, ref2);
+                                        float2 v = fma2(make_float2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), scale2, ref2);
+                                        u.x = exp2_approx(u.x);
+                                        u.y = exp2_approx(u.y);
+                                        v.x = exp2_approx(v.x);
+                                        v.y = exp2_approx(v.y);
+                                        sum = add2(sum, u);
+                                        more = add2(more, v);
+                                        w[j / 2] = pack2<DT>(u.x, u.y);
+                                        w[16 + j / 2] = pack2<DT>(v.x, v.y);
                                     }
                                 };
-                                weigh(x, sum);
-                                tc_st16(Sh, x);
-                                weigh(y, more);
-                                tc_st16(Sh + 16, y);
-                            } else {
+                                // Weights come first, against the reference that is there: it need not be the maximum, as long
+                                // as no sum leaves 2^14 (what fp16 weights can hold).  Where one does, or there was none
+                                // before, the reference becomes the maximum, and sums so far and weights follow.
+                                weigh();
+                                float total = (sum.x + sum.y) + (more.x + more.y);
+                                const bool low = live && (!(total <= 16384.f) || (ref == ATT_NONE && (mx | my)));
+                                if (__any_sync(0xffffffffu, low)) {
+                                    float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) x[j] = 0;
-                                tc_st16(Sh, x);
-                                tc_st16(Sh + 16, x);
+                                    for (int j = 0; j < 32; j += 2) {
+                                        most[j & 2] = fmaxf(most[j & 2], fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 1])));
+                                        most[(j & 2) + 1] = fmaxf(most[(j & 2) + 1], fmaxf(__uint_as_float(y[j]), __uint_as_float(y[j + 1])));
+                                    }
+                                    const float top = fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW);
+                                    float f = 1.f;
+                                    if (low && top > ref) {
+                                        f = exp2_approx(ref - top);
+                                        ref = top;
+                                        l *= f;
+                                    }
+                                    if (k > 0 || h > 0) {
+                                        // (the product of the half before may be under way)
+                                        ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][1 - h]), (h == 0 ? turns - 1 : turns) & 1, gave_up));
+                                        if (!ok) break;
+                                        tc_after_sync();
+#pragma unroll 1
+                                        for (int c = 0; c < D; c += 16) {
+                                            uint32_t o[16];
+                                            tc_ld16(O + c, o);
+                                            tc_wait_ld();
+#pragma unroll
+                                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                            tc_st16(O + c, o);
+                                        }
+                                    }
+                                    weigh();
+                                    total = (sum.x + sum.y) + (more.x + more.y);
+                                }
+                                l += total;
+                                tc_st32(Sh, w);
+                            } else {                     // another copy's keys
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) x[j] = 0;
+                                tc_st32(Sh, x);
                             }
-                            l = l * f + ((sum.x + sum.y) + (more.x + more.y));
                             tc_wait_st();
                             tc_before_sync();
                         }
@@ -927,12 +959,12 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                 const int half_rows = which < 2 ? ATT_TILE : a.own_rows;
                 s_line[which].count = 0;
                 if (chunk < e.chunks && (which == 2 || (shared && (which == 0 || two)))) {
-                    const int line = h * e.row_tiles + (which < 2 ? m0 + which : 0), tile0 = chunk * ATT_CHUNK;
+                    const int line = (which < 2 ? m0 + which : 0) * a.pg.H_kv + h, tile0 = chunk * ATT_CHUNK;
                     const int tiles = e.tiles - tile0 < ATT_CHUNK ? e.tiles - tile0 : ATT_CHUNK, u = e.u + line * line_units(e) + ATT_START + tile0;
                     const int c0 = share_of(units, a.grid, u), c1 = share_of(units, a.grid, u + tiles - 1);
                     s_line[which].count = c1 - c0 + 1;
                     s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
-                                         ((long long)e.item + (long long)line * e.chunks + chunk + c0) * 2 * half_floats(half_rows, D);
+                                         ((long long)e.item + (long long)line * a.max_chunks + chunk + c0) * 2 * half_floats(half_rows, D);
                 }
             }
             __syncthreads();

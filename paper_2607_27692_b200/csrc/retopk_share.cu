@@ -60,7 +60,7 @@ int half_rows(int rows) { return rows < ATT_TILE ? rows * copies_of(rows) : ATT_
 
 // The workspace: where its parts begin, and its size.  `sequences`: entries that belong to one sequence or token,
 // `rows` query rows each; `keys`: the most keys that an entry can have.
-struct Workspace { int64_t entry, group_of, flags, shared_parts, own_parts, bytes; };
+struct Workspace { int64_t entry, group_of, flags, shared_parts, own_parts, bytes, chunks; };
 Workspace lay_out(int64_t sequences, int64_t rows, int64_t n_groups, int64_t group_rows, int64_t H_kv, int d, int64_t keys, int grid) {
     auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
     const int64_t tiles = (keys + ATT_TILE - 1) / ATT_TILE, chunks = (tiles + ATT_CHUNK - 1) / ATT_CHUNK;
@@ -73,6 +73,7 @@ Workspace lay_out(int64_t sequences, int64_t rows, int64_t n_groups, int64_t gro
     w.flags = w.group_of + up(sequences * 4);
     w.shared_parts = w.flags + up(grid * 4);
     w.own_parts = w.shared_parts + up(shared * 2 * half_floats(ATT_TILE, d) * 4);
+    w.chunks = chunks;
     w.bytes = w.own_parts + up(own * 2 * half_floats(half_rows((int)rows), d) * 4);
     return w;
 }
@@ -143,8 +144,9 @@ int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, i
     a.shared_parts = reinterpret_cast<float*>(ws + w.shared_parts);
     a.own_parts = reinterpret_cast<float*>(ws + w.own_parts);
     a.entries = a.n_groups + sequences;
-    a.planned = a.entries > ATT_THREADS;
+    a.planned = a.entries >= ATT_THREADS;
     a.grid = dev.num_sms;
+    a.max_chunks = (int)w.chunks;
     a.own_rows = half_rows(rows);
     if (pages->format == RETOPK_PAGES_BF16)
         return pages->d == 128 ? launch_attention<TYPE_BF16, 128>(p, sequences, s) : launch_attention<TYPE_BF16, 64>(p, sequences, s);
