@@ -268,17 +268,19 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// Two fp32 operations at once.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+// Two fp32 operations at once, on pairs of registers.
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return pair_of(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 d;
-    asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 
@@ -713,10 +715,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
                     const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
+                    ok = bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up);
 #pragma unroll 1
-                    for (int h = 0; h < 2 && ok; ++h) {
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up) &&
-                                                         bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up));
+                    for (int h = 0; h < 2; ++h) {
+                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up));
                         if (!ok) break;
                         if (ahead && h == 1) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
                         if (warp_live) {
@@ -741,29 +743,27 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                 hide(x, mx);
                                 hide(y, my);
                                 uint32_t w[32];
-                                float2 sum, more;
+                                float total;
                                 auto weigh = [&]() {
-                                    const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
-                                    sum = more = make_float2(0.f, 0.f);
+                                    const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
+                                    uint64_t sum = 0, more = 0;
 #pragma unroll
                                     for (int j = 0; j < 32; j += 2) {
-                                        float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), scale2, ref2);
-                                        float2 v = fma2(make_float2(__uint_as_float(y[j]), __uint_as_float(y[j + 1])), scale2, ref2);
-                                        u.x = exp2_approx(u.x);
-                                        u.y = exp2_approx(u.y);
-                                        v.x = exp2_approx(v.x);
-                                        v.y = exp2_approx(v.y);
-                                        sum = add2(sum, u);
-                                        more = add2(more, v);
-                                        w[j / 2] = pack2<DT>(u.x, u.y);
-                                        w[16 + j / 2] = pack2<DT>(v.x, v.y);
+                                        const uint64_t u = fma2(pair_of(x[j], x[j + 1]), scale2, ref2), v = fma2(pair_of(y[j], y[j + 1]), scale2, ref2);
+                                        const float u0 = exp2_approx(low_of(u)), u1 = exp2_approx(high_of(u));
+                                        const float v0 = exp2_approx(low_of(v)), v1 = exp2_approx(high_of(v));
+                                        sum = add2(sum, pair_of(u0, u1));
+                                        more = add2(more, pair_of(v0, v1));
+                                        w[j / 2] = pack2<DT>(u0, u1);
+                                        w[16 + j / 2] = pack2<DT>(v0, v1);
                                     }
+                                    sum = add2(sum, more);
+                                    total = low_of(sum) + high_of(sum);
                                 };
                                 // Weights come first, against the reference that is there: it need not be the maximum, as long
                                 // as no sum leaves 2^14 (what fp16 weights can hold).  Where one does, or there was none
                                 // before, the reference becomes the maximum, and sums so far and weights follow.
                                 weigh();
-                                float total = (sum.x + sum.y) + (more.x + more.y);
                                 const bool low = live && (!(total <= 16384.f) || (ref == ATT_NONE && (mx | my)));
                                 if (__any_sync(0xffffffffu, low)) {
                                     float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -795,7 +795,6 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                         }
                                     }
                                     weigh();
-                                    total = (sum.x + sum.y) + (more.x + more.y);
                                 }
                                 l += total;
                                 tc_st32(Sh, w);
