@@ -99,10 +99,10 @@ __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 
 // max(q lo, q hi) = q+ hi + q- lo with the positive and the negative part of q.  A warp has 16 blocks as the rows
 // of A, up to 8 queries as the columns of B.  The channels that a lane loads at once (8 of 32) are
 // those that it holds in A and in B of two products: sums do not care for their order.
-// Error: products of 16-bit numbers are exact in fp32.  2 D / 16 products of depth 16, each of whose additions cuts off
-// at most 2^-23 of what was summed so far, below sum |q| times the largest |bound| of the block: 2^-23 * 17 * 2 D / 16 <= 2^-14
-// of that for D = 128.
-template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_kernel(const __grid_constant__ SelectArgs a) {
+// Error: products of 16-bit numbers are exact in fp32.  Two products of depth 16 go into a sum, each of whose 34 additions
+// cuts off at most 2^-23 of what was summed so far, below the sum's share of size = sum |q| times the largest |bound| of the
+// block; at most 8 such sums are added with 2^-24 of size each: 34 * 2^-23 + 8 * 2^-24 < 2^-17 of size.
+template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS, 7) score_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int STEPS = D / 32;
     __shared__ float s_score[SCORE_WARPS][SCORE_COLS][SCORE_ROWS], s_size[SCORE_WARPS][SCORE_COLS];
     pdl_wait();
@@ -111,36 +111,16 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_
     const int j0 = (blockIdx.x * SCORE_WARPS + warp) * SCORE_ROWS;
     const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, a.T - 1), end = (seen + a.block - 1) / a.block - a.last;
     if (end + a.last <= a.keep || j0 >= end) return;
-    uint4 lo[2][STEPS], hi[2][STEPS];
-    bool none[2];
+    constexpr int DEEP = 2;                              // groups of 32 channels that are loaded at once
+    const uint16_t* src[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
         const int j = j0 + g + 8 * y;
         const long long r = j < end ? cache_row(a.pg, b, (long long)j * a.block) : -1;
-        none[y] = r < 0;
-        const uint16_t* src = a.bounds + (none[y] ? 0 : (r + (long long)h * a.pg.page_size) / a.block * (2 * D)) + part * 8;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            lo[y][i] = hi[y][i] = make_uint4(0, 0, 0, 0);
-            if (!none[y]) {
-                lo[y][i] = *reinterpret_cast<const uint4*>(src + i * 32);
-                hi[y][i] = *reinterpret_cast<const uint4*>(src + D + i * 32);
-            }
-        }
+        src[y] = r < 0 ? nullptr : a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + part * 8;
     }
-    float largest[2];                                     // of the bounds' magnitudes
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) m = __vmaxu2(__vmaxu2(m, word(lo[y][i], w) & 0x7fff7fffu), word(hi[y][i], w) & 0x7fff7fffu);
-        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const float2 f = unpack2<DT>(m);
-        largest[y] = f.x != f.x || f.y != f.y ? INFINITY : fmaxf(f.x, f.y);
-    }
+    uint32_t largest2[2] = {0, 0};                       // of the bounds' magnitudes
+    float largest[2] = {0.f, 0.f};
     const int cols = a.T * a.G;
     float best = 0.f, size = 0.f;
     for (int c0 = 0; c0 < cols; c0 += SCORE_COLS) {
@@ -148,22 +128,53 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_
         const int col = c0 + g;
         const uint16_t* q = a.q + ((long long)b * a.T + col / a.G) * a.q_stride + (h * a.G + col % a.G) * D + part * 8;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const uint4 x = col < cols ? *reinterpret_cast<const uint4*>(q + i * 32) : make_uint4(0, 0, 0, 0);
-            uint32_t up[4], down[4];
+        for (int i0 = 0; i0 < STEPS; i0 += DEEP) {
+            uint4 lo[2][DEEP], hi[2][DEEP], x[DEEP];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                up[w] = max2_nan<DT>(word(x, w), 0u);
-                down[w] = min2_nan<DT>(word(x, w), 0u);
-                const float2 f = unpack2<DT>(word(x, w));
-                sum += fabsf(f.x) + fabsf(f.y);
+            for (int i = 0; i < DEEP; ++i) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    lo[y][i] = hi[y][i] = make_uint4(0, 0, 0, 0);
+                    if (src[y]) {
+                        lo[y][i] = *reinterpret_cast<const uint4*>(src[y] + (i0 + i) * 32);
+                        hi[y][i] = *reinterpret_cast<const uint4*>(src[y] + D + (i0 + i) * 32);
+                    }
+                }
+                x[i] = col < cols ? *reinterpret_cast<const uint4*>(q + (i0 + i) * 32) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
-            for (int w = 0; w < 4; w += 2) {
-                mma16816<DT>(c, word(hi[0][i], w), word(hi[1][i], w), word(hi[0][i], w + 1), word(hi[1][i], w + 1), up[w], up[w + 1]);
-                mma16816<DT>(c, word(lo[0][i], w), word(lo[1][i], w), word(lo[0][i], w + 1), word(lo[1][i], w + 1), down[w], down[w + 1]);
+            for (int i = 0; i < DEEP; ++i) {
+                uint32_t up[4], down[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    up[w] = max2_nan<DT>(word(x[i], w), 0u);
+                    down[w] = min2_nan<DT>(word(x[i], w), 0u);
+                    const float2 f = unpack2<DT>(word(x[i], w));
+                    sum += fabsf(f.x) + fabsf(f.y);
+                    if (c0 == 0)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+                            largest2[y] = __vmaxu2(__vmaxu2(largest2[y], word(lo[y][i], w) & 0x7fff7fffu), word(hi[y][i], w) & 0x7fff7fffu);
+                }
+                float u[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < 4; w += 2) {
+                    mma16816<DT>(u, word(hi[0][i], w), word(hi[1][i], w), word(hi[0][i], w + 1), word(hi[1][i], w + 1), up[w], up[w + 1]);
+                    mma16816<DT>(v, word(lo[0][i], w), word(lo[1][i], w), word(lo[0][i], w + 1), word(lo[1][i], w + 1), down[w], down[w + 1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[k] += u[k] + v[k];
             }
         }
+        if (c0 == 0)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                uint32_t m = largest2[y];
+                m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const float2 f = unpack2<DT>(m);
+                largest[y] = f.x != f.x || f.y != f.y ? INFINITY : fmaxf(f.x, f.y);
+            }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         if (part == 0) s_size[warp][g] = sum;
@@ -176,7 +187,7 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_
         // lane x < 16: block x of the warp
         const int from = (lane & 7) * 4;
         const float most0 = __shfl_sync(0xffffffffu, largest[0], from), most1 = __shfl_sync(0xffffffffu, largest[1], from);
-        const int none0 = __shfl_sync(0xffffffffu, (int)none[0], from), none1 = __shfl_sync(0xffffffffu, (int)none[1], from);
+        const int none0 = __shfl_sync(0xffffffffu, (int)(src[0] == nullptr), from), none1 = __shfl_sync(0xffffffffu, (int)(src[1] == nullptr), from);
         if (lane < SCORE_ROWS && j0 + lane < end) {
             const float most = lane & 8 ? most1 : most0;
             const bool out = (lane & 8 ? none1 : none0) != 0;
@@ -186,7 +197,7 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS) score_
                 best = head == 0 ? s : fmaxf(best, s);
                 size = head == 0 ? z : (z != z ? z : fmaxf(size, z));
                 if (head == a.G - 1) {
-                    float off = size * most * 0x1p-14f + 1e-35f;
+                    float off = size * most * 0x1p-17f + 1e-35f;
                     if (!(off < 1e37f) || !(fabsf(best) < 1e37f)) off = INFINITY;
                     a.scores[(((long long)b * a.T + (c0 + k) / a.G) * a.pg.H_kv + h) * a.max_blocks + j0 + lane] =
                         out ? make_float2(-INFINITY, 0.f) : (off == INFINITY ? make_float2(0.f, INFINITY) : make_float2(best, off));
@@ -271,45 +282,37 @@ template <bool EXACT, class Each> __device__ __forceinline__ void find_limit(Eac
     *rest_out = shift > 0 ? 0x7fffffff : rest;
 }
 
-// The score of block j for the heads of a group, in 64 bits and rounded once to fp32; by a warp.
+// The score of block j for the heads of a group, in 64 bits and rounded once to fp32; by a warp: 8 lanes with a share of
+// the channels each for a head, four heads at a time.
 template <int DT, int D> __device__ __forceinline__ float exact_score(const SelectArgs& a, int b, int t, int h, int j) {
-    constexpr int PER = D / 32, HEADS = 4;
-    const int lane = threadIdx.x & 31;
+    constexpr int PER = D / 8;
+    const int lane = threadIdx.x & 31, share = lane & 7;
     const long long r = cache_row(a.pg, b, (long long)j * a.block);
     if (r < 0) return -INFINITY;
-    const uint16_t* src = a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + lane * PER;
-    const uint16_t* q = a.q + ((long long)b * a.T + t) * a.q_stride + (long long)h * a.G * D + lane * PER;
-    double lo[PER], hi[PER];
+    const uint16_t* src = a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + share * PER;
+    float score = -INFINITY;
+    for (int g0 = 0; g0 < a.G; g0 += 4) {
+        const int g = g0 + (lane >> 3) < a.G ? g0 + (lane >> 3) : a.G - 1;           // (a head twice does no harm)
+        const uint16_t* q = a.q + ((long long)b * a.T + t) * a.q_stride + ((long long)h * a.G + g) * D + share * PER;
+        double sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        lo[e] = to_f32<DT>(src[e]);
-        hi[e] = to_f32<DT>(src[D + e]);
-    }
-    float score = 0.f;
-    for (int g0 = 0; g0 < a.G; g0 += HEADS) {
-        uint16_t x[HEADS][PER];
+        for (int c = 0; c < PER; c += 8) {
+            float x[8], lo[8], hi[8];
+            unpack8<DT>(*reinterpret_cast<const uint4*>(q + c), x);
+            unpack8<DT>(*reinterpret_cast<const uint4*>(src + c), lo);
+            unpack8<DT>(*reinterpret_cast<const uint4*>(src + D + c), hi);
 #pragma unroll
-        for (int k = 0; k < HEADS; ++k)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) x[k][e] = g0 + k < a.G ? q[(g0 + k) * D + e] : 0;
-        double sum[HEADS] = {};
-#pragma unroll
-        for (int k = 0; k < HEADS; ++k)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const double y = to_f32<DT>(x[k][e]), p = y * lo[e], z = y * hi[e];
-                sum[k] += p != p || z != z ? p + z : (p > z ? p : z);
+            for (int e = 0; e < 8; ++e) {
+                const double y = x[e], p = y * lo[e], z = y * hi[e];
+                sum += p != p || z != z ? p + z : (p > z ? p : z);
             }
-#pragma unroll
-        for (int o = 16; o; o >>= 1)
-#pragma unroll
-            for (int k = 0; k < HEADS; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
-#pragma unroll
-        for (int k = 0; k < HEADS; ++k) {
-            float f = (float)sum[k];
-            f = f != f ? INFINITY : f;
-            if (g0 + k < a.G) score = g0 + k == 0 ? f : fmaxf(score, f);
         }
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        float f = (float)sum;
+        f = f != f ? INFINITY : f;
+        f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 8));
+        score = fmaxf(score, fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 16)));
     }
     return score;
 }
@@ -389,8 +392,9 @@ template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs&
 template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int BITS = 10, BINS = 1 << BITS, DEEP = PICK_KEPT / PICK_THREADS;
     __shared__ float2 s_kept[PICK_KEPT];
-    __shared__ int s_bin[BINS], s_cand[PICK_LIST], s_count, s_found[3];
-    __shared__ uint32_t s_lower[PICK_LIST], s_upper[PICK_LIST], s_key[PICK_LIST], s_low[PICK_WARPS], s_high[PICK_WARPS];
+    __shared__ int s_bin[BINS], s_count, s_found[3];
+    __shared__ __align__(16) uint32_t s_cand[PICK_LIST], s_lower[PICK_LIST], s_upper[PICK_LIST], s_key[PICK_LIST];
+    __shared__ uint32_t s_low[PICK_WARPS], s_high[PICK_WARPS];
     pdl_wait();
     const int h = blockIdx.x, t = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, t);
@@ -490,37 +494,53 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
         pick_any<DT, D>(a, at, b, t, h, m, want, out);
         return;
     }
-    // a key for each: the largest for one that is in, 0 for one that is out, 1 for one that is open
-    for (int c = tid; c < C; c += PICK_THREADS) {
-        int rivals = 0, better = 0;
-        if (C > want)
-            for (int k = 0; k < C; ++k) {
-                rivals += s_upper[k] >= s_lower[c];
-                better += s_lower[k] > s_upper[c];
-            }
-        s_key[c] = rivals <= want ? ~0u : (better >= want ? 0u : 1u);
-    }
-    __syncthreads();
-    for (int c = warp; c < C; c += PICK_WARPS)
-        if (s_key[c] == 1u) {
-            const float score = exact_score<DT, D>(a, b, t, h, a.first + s_cand[c]);
-            __syncwarp();
-            if (lane == 0) s_key[c] = order_of(score);
+    // a candidate to a thread, the others four at a time (filled up with ones that count for nothing)
+    const int C4 = (C + 3) / 4;
+    auto each4 = [&](const uint32_t* x, auto f) {
+#pragma unroll 4
+        for (int k = 0; k < C4; ++k) {
+            const uint4 v = reinterpret_cast<const uint4*>(x)[k];
+            f(v.x, 4 * k); f(v.y, 4 * k + 1); f(v.z, 4 * k + 2); f(v.w, 4 * k + 3);
         }
-    __syncthreads();
-    for (int c = tid; c < C; c += PICK_THREADS) {
-        const uint32_t u = s_key[c];
-        int rank = 0;
-        if (C > want)
-            for (int k = 0; k < C; ++k) rank += s_key[k] > u || (s_key[k] == u && s_cand[k] < s_cand[c]);
-        s_lower[c] = rank < want;
+    };
+    if (tid < 4 * C4 - C) {
+        s_lower[C + tid] = s_upper[C + tid] = s_key[C + tid] = 0;
+        s_cand[C + tid] = ~0u;
     }
     __syncthreads();
-    for (int c = tid; c < C; c += PICK_THREADS) {
-        if (!s_lower[c]) continue;
+    if (C > want) {
+        // a key for each: the largest for one that is in, 0 for one that is out, else the order of its exact score
+        if (tid < C) {
+            const uint32_t lo = s_lower[tid], hi = s_upper[tid];
+            int better = 0, rivals = 0;
+            each4(s_lower, [&](uint32_t u, int) { better += u > hi; });
+            each4(s_upper, [&](uint32_t u, int) { rivals += u >= lo; });
+            s_key[tid] = better >= want ? 0u : (rivals <= want ? ~0u : 1u);
+        }
+        __syncthreads();
+        for (int c = warp; c < C; c += PICK_WARPS)
+            if (s_key[c] == 1u) {
+                const float score = exact_score<DT, D>(a, b, t, h, a.first + (int)s_cand[c]);
+                __syncwarp();
+                if (lane == 0) s_key[c] = order_of(score);
+            }
+        __syncthreads();
+        bool in = false;
+        if (tid < C) {
+            const uint32_t key = s_key[tid], me = s_cand[tid];
+            int rank = 0;
+            each4(s_key, [&](uint32_t u, int k) { rank += u > key || (u == key && s_cand[k] < me); });
+            in = rank < want;
+        }
+        __syncthreads();
+        if (tid < C && !in) s_cand[tid] = ~0u;
+        __syncthreads();
+    }
+    if (tid < C && s_cand[tid] != ~0u) {
+        const uint32_t me = s_cand[tid];
         int place = 0;
-        for (int k = 0; k < C; ++k) place += s_lower[k] && s_cand[k] < s_cand[c];
-        out[a.first + place] = a.first + s_cand[c];
+        each4(s_cand, [&](uint32_t u, int) { place += u < me; });
+        out[a.first + place] = a.first + (int)me;
     }
 }
 

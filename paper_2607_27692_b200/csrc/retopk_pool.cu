@@ -100,7 +100,7 @@ int retopk_pool_fork(const retopk_pool_t* pool, int B, int32_t* seq_lens, int32_
     a.src = src;
     a.dst = dst;
     a.rows = rows;
-    return launch(fork_kernel, dim3((unsigned)n), FORK_THREADS, 0, static_cast<cudaStream_t>(stream), a);
+    return launch(fork_kernel, dim3((unsigned)n + 1), FORK_THREADS, 0, static_cast<cudaStream_t>(stream), a);
 }
 
 int retopk_pool_free(const retopk_pool_t* pool, int B, int32_t* seq_lens, const int32_t* block_table, int64_t max_pages, int n,

@@ -111,53 +111,59 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
     if (missing) atomicAdd(a.scratch + POOL_SHORT, missing);
 }
 
-// One CTA for a fork copies the table row and counts the full pages; the CTA that is done last hands out
-// pages for the partial ones, in the order of the forks.
+// One CTA for a fork copies the table row and counts the full pages, one more finds free pages meanwhile (full pages
+// are in use, so that the counts of free ones stay as they are); the CTA that is done last hands them out
+// for the partial pages, in the order of the forks.
 __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constant__ PoolArgs a) {
+    constexpr int DEEP = 8;
+    __shared__ int s_last;
     pdl_wait();
-    const int i = blockIdx.x, tid = threadIdx.x;
-    const int c = a.children[i], p = a.other[i];
-    // what holds for a fork does not depend on the others' progress: no child is anyone's parent, and of
-    // several forks to one child the first counts
-    bool ok = c >= 0 && c < a.B && p >= 0 && p < a.B;
-    bool clash = false;
-    for (int j = tid; j < a.n; j += FORK_THREADS) {
-        const int x = a.children[j];
-        clash |= (x == c && j < i) || x == p;
-    }
-    ok = !__syncthreads_or(clash) && ok;
-    const int len = ok ? a.lens[p] : 0;
-    ok = ok && len > 0 && len <= a.capacity && a.lens[c] <= 0;
-    const int full = ok ? len / a.page_size : 0, rest = ok ? len % a.page_size : 0;
-    const int32_t* from = a.table + (long long)p * a.max_pages;
-    int32_t* to = a.table + (long long)c * a.max_pages;
-    for (int s = tid; s < full; s += FORK_THREADS) {
-        const int page = from[s];
-        to[s] = page;
-        if (page >= 0 && page < a.n_pages) atomicAdd(a.refs + page, 1);
-    }
-    if (tid == 0) {
-        a.src[i] = rest ? from[full] : -1;
-        a.dst[i] = !ok ? -3 : (rest ? -2 : -1);          // -2: waits for a page, -3: not made
-        a.rows[i] = rest;
+    const int tid = threadIdx.x, i = blockIdx.x;
+    int32_t* list = a.scratch + POOL_LIST;
+    if (i == a.n) {
+        const int found = lowest_free<FORK_THREADS>(a, list, a.n < a.n_pages ? a.n : (int)a.n_pages);
+        if (tid == 0) a.scratch[POOL_USED] = found;
+    } else {
+        const int c = a.children[i], p = a.other[i];
+        // what holds for a fork does not depend on the others' progress: no child is anyone's parent, and of
+        // several forks to one child the first counts
+        bool ok = c >= 0 && c < a.B && p >= 0 && p < a.B;
+        bool clash = false;
+        for (int j = tid; j < a.n; j += FORK_THREADS) {
+            const int x = a.children[j];
+            clash |= (x == c && j < i) || x == p;
+        }
+        ok = !__syncthreads_or(clash) && ok;
+        const int len = ok ? a.lens[p] : 0;
+        ok = ok && len > 0 && len <= a.capacity && a.lens[c] <= 0;
+        const int full = ok ? len / a.page_size : 0, rest = ok ? len % a.page_size : 0;
+        const int32_t* from = a.table + (long long)p * a.max_pages;
+        int32_t* to = a.table + (long long)c * a.max_pages;
+        for (int s0 = tid; s0 < full; s0 += FORK_THREADS * DEEP) {
+            int page[DEEP];
+#pragma unroll
+            for (int k = 0; k < DEEP; ++k) page[k] = s0 + k * FORK_THREADS < full ? from[s0 + k * FORK_THREADS] : -1;
+#pragma unroll
+            for (int k = 0; k < DEEP; ++k) {
+                if (s0 + k * FORK_THREADS < full) to[s0 + k * FORK_THREADS] = page[k];
+                if (page[k] >= 0 && page[k] < a.n_pages) atomicAdd(a.refs + page[k], 1);
+            }
+        }
+        if (tid == 0) {
+            a.src[i] = rest ? from[full] : -1;
+            a.dst[i] = !ok ? -3 : (rest ? -2 : -1);          // -2: waits for a page, -3: not made
+            a.rows[i] = rest;
+        }
     }
     __threadfence();
     __syncthreads();
-    __shared__ int s_last;
     if (tid == 0) s_last = atomicAdd(a.scratch + POOL_TICKET, 1) == (int)gridDim.x - 1;
     __syncthreads();
     if (!s_last) return;
     __threadfence();
     if (tid == 0) a.scratch[POOL_TICKET] = 0;
 
-    int32_t* list = a.scratch + POOL_LIST;
-    int want = 0;
-    for (int i0 = 0; i0 < a.n; i0 += FORK_THREADS) {
-        int total;
-        scan_cta<FORK_THREADS>(i0 + tid < a.n && __ldcg(a.dst + i0 + tid) == -2, &total);
-        want += total;
-    }
-    const int found = lowest_free<FORK_THREADS>(a, list, want < a.n_pages ? want : (int)a.n_pages);
+    const int found = __ldcg(a.scratch + POOL_USED);
     int base = 0, missing = 0;
     for (int i0 = 0; i0 < a.n; i0 += FORK_THREADS) {
         const int k = i0 + tid, state = k < a.n ? __ldcg(a.dst + k) : -3;
@@ -173,7 +179,7 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
         int32_t* row = a.table + (long long)child * a.max_pages;
         if (state == -1 || at < found) {
             if (state == -2) {
-                const int page = list[at];
+                const int page = __ldcg(list + at);
                 row[whole] = page;
                 a.refs[page] = 1;
                 a.dst[k] = page;
