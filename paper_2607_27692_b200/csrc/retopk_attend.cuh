@@ -69,16 +69,32 @@ struct AttendParams {
     AttendArgs a;
 };
 
-// Floats of a half of a part (one stream's): sums [D / 4][rows][4], then reference and weight sum of each row.
-__host__ __device__ constexpr long long half_floats(int rows, int d) { return (long long)rows * d + (2 * rows + 3) / 4 * 4; }
+// Floats of a half of a part (one stream's): the sums of four rows each lie together, [rows / 4][D / 4][4 rows][4], so
+// that join_kernel finds a sequence's rows in one place; then reference and weight sum of each row.
+__host__ __device__ constexpr int half_floats(int rows, int d) { return (rows + 3) / 4 * 4 * (d + 2); }
+__device__ __forceinline__ int sums_at(int row, int c4, int d) { return (row >> 2) * (4 * d) + c4 * 16 + (row & 3) * 4; }
+__device__ __forceinline__ int weight_at(int row, int rows, int d) { return (rows + 3) / 4 * 4 * d + 2 * row; }
 __device__ __forceinline__ int line_units(const Entry& e) { return e.tiles > 0 ? e.tiles + ATT_START : 0; }
-// Equal shares of the line; none of them is empty: of a short line fewer CTAs have one.
-__device__ __forceinline__ int share_begin(int units, int grid, int cta) {
-    const int n = units < grid ? units : grid;
-    return cta < n ? (int)((long long)units * cta / n) : units;
-}
-// The CTA whose share holds unit u.
-__device__ __forceinline__ int share_of(int units, int grid, int u) { return (int)(((long long)(u + 1) * (units < grid ? units : grid) - 1) / units); }
+// Equal shares of the line: that of CTA c begins at floor(units * c / n).  None is empty: of a short line fewer CTAs
+// have one.
+struct Shares {
+    int units, n, whole, rest;
+    __device__ __forceinline__ Shares(int units_, int grid) {
+        units = units_;
+        n = units < grid ? units : grid;
+        whole = n > 0 ? units / n : 0;
+        rest = units - whole * n;
+    }
+    __device__ __forceinline__ int begin(int c) const { return c < n ? whole * c + rest * c / n : units; }
+    // the CTA whose share holds unit u
+    __device__ __forceinline__ int of(int u) const {
+        int c = (int)(__fdividef((float)u, (float)units) * (float)n);
+        c = c < 0 ? 0 : (c < n - 1 ? c : n - 1);
+        while (c > 0 && begin(c) > u) --c;
+        while (c < n - 1 && begin(c + 1) <= u) ++c;
+        return c;
+    }
+};
 
 // ---------------------------------------------------------------------------------------
 // plan_kernel
@@ -407,7 +423,8 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 if (tid == 0) a.head->units = units;
             }
         }
-        const int u0 = share_begin(units, a.grid, cta), u1 = share_begin(units, a.grid, cta + 1);
+        const Shares shares(units, a.grid);
+        const int u0 = shares.begin(cta), u1 = shares.begin(cta + 1);
         int listed = 0;
         for (int e0 = 0; e0 < a.entries && u0 < u1; e0 += ATT_THREADS) {
             const int i = e0 + tid;
@@ -459,7 +476,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         const long long slot = (long long)e.item + (long long)line * a.max_chunks + chunk + cta;
                         const bool own = i >= a.n_groups;
                         p.half_rows = own ? a.own_rows : ATT_TILE;
-                        p.part = (own ? a.own_parts : a.shared_parts) + slot * 2 * half_floats(p.half_rows, D);
+                        p.part = (own ? a.own_parts : a.shared_parts) + slot * (2 * half_floats(p.half_rows, D));
                         sm.piece[at] = p;
                     }
                 }
@@ -818,7 +835,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 // ---- the sums of this piece ------------------------------------------------------
                 float* part = p.part + s * half_floats(p.half_rows, D);
                 const int at = copy * (p.half_rows / copies) + row % (ATT_TILE / copies);
-                if (live) *reinterpret_cast<float2*>(part + (long long)p.half_rows * D + 2 * at) = make_float2(ref, l);
+                if (live) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(ref, l);
                 if (ok && turn_count > 0) {
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][0]), (turns - 1) & 1, gave_up) &&
                                                      bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up));
@@ -832,7 +849,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             if (live) {
 #pragma unroll
                                 for (int j = 0; j < 32; j += 4)
-                                    *reinterpret_cast<uint4*>(part + ((long long)((c + j) / 4) * p.half_rows + at) * 4) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                                    *reinterpret_cast<uint4*>(part + sums_at(at, (c + j) / 4, D)) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
                             }
                         }
                     }
@@ -886,21 +903,26 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
             s_late_row[tid] = row < 0 ? -1 : row + (long long)h * a.pg.page_size;
         }
         __syncthreads();
-        for (int x = tid; x < own.rows * late; x += JOIN_THREADS) {
-            const int r = x / late, k = x % late;
-            if (first + k >= keys_seen(a.pg, len, a.T, r / a.G) || s_late_row[k] < 0) continue;
-            const uint16_t* key = reinterpret_cast<const uint16_t*>(a.pg.k) + s_late_row[k] * D;
-            const uint16_t* q = a.q + ((long long)own.token + r / a.G) * a.q_stride + (long long)(h * a.G + r % a.G) * D;
+        // 8 lanes to a score
+        for (int x0 = 0; x0 < own.rows * late; x0 += JOIN_THREADS / 8) {
+            const int x = x0 + tid / 8, r = x / late, k = x - r * late, share = tid % 8;
             float s = 0.f;
-#pragma unroll 4
-            for (int c = 0; c < D; c += 8) {
-                float kf[8], qf[8];
-                unpack8<DT>(*reinterpret_cast<const uint4*>(key + c), kf);
-                unpack8<DT>(*reinterpret_cast<const uint4*>(q + c), qf);
+            const bool sees = x < own.rows * late && first + k < keys_seen(a.pg, len, a.T, r / a.G) && s_late_row[k] >= 0;
+            if (sees) {
+                const uint16_t* key = reinterpret_cast<const uint16_t*>(a.pg.k) + s_late_row[k] * D + share * 8;
+                const uint16_t* q = a.q + ((long long)own.token + r / a.G) * a.q_stride + (long long)(h * a.G + r % a.G) * D + share * 8;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(qf[e], kf[e], s);
+                for (int c = 0; c < D; c += 64) {
+                    float kf[8], qf[8];
+                    unpack8<DT>(*reinterpret_cast<const uint4*>(key + c), kf);
+                    unpack8<DT>(*reinterpret_cast<const uint4*>(q + c), qf);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s = fmaf(qf[e], kf[e], s);
+                }
             }
-            s_late[x] = s * a.scale_log2;
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (sees && share == 0) s_late[x] = s * a.scale_log2;
         }
     }
     const bool failed = __syncthreads_or(flag != 0);
@@ -927,8 +949,8 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
         // both, in `copies` places.
         auto add_parts = [&](const float* parts, int count, int half_rows, int row, int rows) {
             const bool both = rows > ATT_TILE;
-            const int copies = copies_of(rows), places = both ? 1 : 2 * copies, all = count * places, apart = half_rows / copies;
-            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row, half_size = (int)half_floats(half_rows, D);
+            const int copies = copies_of(rows), places = both ? 1 : 2 * copies, all = count * places, apart = half_rows / copies, shift = __ffs(places) - 1;
+            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row, half_size = half_floats(half_rows, D);
             for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
                 float2 ml[JOIN_DEEP];
                 float4 o[JOIN_DEEP];
@@ -937,10 +959,10 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                     const int k = k0 + d * splits;
                     ml[d].x = ATT_NONE;
                     if (k < all) {
-                        const int part = both ? k : k / places, place = k - part * places, at = at0 + (place >> 1) * apart;
+                        const int part = k >> shift, place = k & (places - 1), at = at0 + (place >> 1) * apart;
                         const float* half = parts + (2ll * part + h0 + (place & 1)) * half_size;
-                        ml[d] = *reinterpret_cast<const float2*>(half + half_rows * D + 2 * at);
-                        o[d] = *reinterpret_cast<const float4*>(half + (c4 * half_rows + at) * 4);
+                        ml[d] = *reinterpret_cast<const float2*>(half + weight_at(at, half_rows, D));
+                        o[d] = *reinterpret_cast<const float4*>(half + sums_at(at, c4, D));
                     }
                 }
 #pragma unroll
@@ -960,10 +982,11 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                 if (chunk < e.chunks && (which == 2 || (shared && (which == 0 || two)))) {
                     const int line = (which < 2 ? m0 + which : 0) * a.pg.H_kv + h, tile0 = chunk * ATT_CHUNK;
                     const int tiles = e.tiles - tile0 < ATT_CHUNK ? e.tiles - tile0 : ATT_CHUNK, u = e.u + line * line_units(e) + ATT_START + tile0;
-                    const int c0 = share_of(units, a.grid, u), c1 = share_of(units, a.grid, u + tiles - 1);
+                    const Shares shares(units, a.grid);
+                    const int c0 = shares.of(u), c1 = shares.of(u + tiles - 1);
                     s_line[which].count = c1 - c0 + 1;
                     s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
-                                         ((long long)e.item + (long long)line * a.max_chunks + chunk + c0) * 2 * half_floats(half_rows, D);
+                                         ((long long)e.item + (long long)line * a.max_chunks + chunk + c0) * (2 * half_floats(half_rows, D));
                 }
             }
             __syncthreads();
