@@ -18,9 +18,9 @@
 namespace retopk_cache {
 
 // Keys that token t of T sees in a sequence of `len` keys; none if the cache cannot hold the sequence.
-__device__ __forceinline__ long long keys_seen(const Pages& pg, long long len, int T, int t) {
+__device__ __forceinline__ int keys_seen(const Pages& pg, int len, int T, int t) {
     if (len < 0 || len > pg.capacity) return 0;
-    const long long n = len - T + 1 + t;
+    const int n = len - T + 1 + t;
     return n > 0 ? n : 0;
 }
 
@@ -63,6 +63,9 @@ struct AttendArgs {
     float *shared_parts, *own_parts;
     int box_rows, total_rows;
     bool planned;               // by plan_kernel
+    // join_kernel: float4s of a row that a CTA has, threads to each, and 1 / rows, 1 / (rows * wide), 1 / G
+    int join_wide, join_splits;
+    float per_row, per_work, per_G;
 };
 struct AttendParams {
     AttendMaps maps;
@@ -86,15 +89,20 @@ struct Shares {
         rest = units - whole * n;
     }
     __device__ __forceinline__ int begin(int c) const { return c < n ? whole * c + rest * c / n : units; }
-    // the CTA whose share holds unit u
-    __device__ __forceinline__ int of(int u) const {
-        int c = (int)(__fdividef((float)u, (float)units) * (float)n);
-        c = c < 0 ? 0 : (c < n - 1 ? c : n - 1);
-        while (c > 0 && begin(c) > u) --c;
-        while (c < n - 1 && begin(c + 1) <= u) ++c;
-        return c;
-    }
 };
+
+// The CTA whose share holds unit u: the last c with floor(units * c / n) <= u.
+__device__ __forceinline__ int share_of(int u, int units, int grid) {
+    const int n = units < grid ? units : grid;
+    const long long end = (u + 1ll) * n;
+    int c = (int)(__fdividef((float)u, (float)units) * (float)n);
+    c = c < 0 ? 0 : (c < n - 1 ? c : n - 1);
+#pragma unroll 1
+    while (c > 0 && (long long)units * c >= end) --c;
+#pragma unroll 1
+    while (c < n - 1 && units * (c + 1ll) < end) ++c;
+    return c;
+}
 
 // ---------------------------------------------------------------------------------------
 // plan_kernel
@@ -113,12 +121,15 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, const PlanInput& i
     int groups = 0;
     if (a.n_groups > 0) {
         bool bad = false;
+#pragma unroll 1
         for (int g = tid; g < a.n_groups; g += THREADS)
             bad |= in.cu[g] < 0 || in.cu[g + 1] < in.cu[g] || in.cu[g + 1] > a.B || (g == 0 && in.cu[0] != 0) || (g == a.n_groups - 1 && in.cu[g + 1] != a.B);
         groups = __syncthreads_or(bad) ? 0 : a.n_groups;
+#pragma unroll 1
         for (int g = warp; g < groups; g += THREADS / 32) {
             const int b0 = in.cu[g], b1 = in.cu[g + 1];
             int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
+#pragma unroll 1
             for (int b = b0 + lane; b < b1; b += 32) {
                 group_of[b] = g;
                 const int len = in.seq_lens[b];
@@ -143,12 +154,15 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, const PlanInput& i
             }
         }
         if (groups == 0)
+#pragma unroll 1
             for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
         __syncthreads();
     } else if (!a.blocks) {
+#pragma unroll 1
         for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
     }
     int units = 0;
+#pragma unroll 1
     for (int e0 = 0; e0 < a.entries; e0 += THREADS) {
         const int i = e0 + tid;
         const bool on = i < a.entries;
@@ -366,11 +380,13 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
     volatile int* gave_up = &sm.gave_up;
     if (tid == 0) {
         sm.gave_up = (smem_of(att_smem) & 1023) != 0;    // operands need the alignment
+#pragma unroll 1
         for (int i = 0; i < Smem::SLOTS; ++i) {
             bar_init(smem_of(&sm.full[i]), 1);
             sm.issued[i] = ~0u;
             bar_init(smem_of(&sm.empty[i]), 2);           // one of each stream
         }
+#pragma unroll 1
         for (int i = 0; i < ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i]), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_of(&sm.q_ready[i]), 4);
@@ -426,6 +442,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         const Shares shares(units, a.grid);
         const int u0 = shares.begin(cta), u1 = shares.begin(cta + 1);
         int listed = 0;
+#pragma unroll 1
         for (int e0 = 0; e0 < a.entries && u0 < u1; e0 += ATT_THREADS) {
             const int i = e0 + tid;
             Entry e;
@@ -445,6 +462,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 if (to > from) {
                     lines0 = from / len;
                     lines1 = (to - 1) / len;
+#pragma unroll 1
                     for (int line = lines0; line <= lines1; line = line == lines0 && lines1 > lines0 + 1 ? lines1 : line + 1) {
                         int t0, t1;
                         range_of(line, t0, t1);
@@ -456,9 +474,11 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             int total, at = listed + scan_cta<ATT_THREADS>(count, &total, sm.warp_sum) - batch * ATT_PIECES;     // of this entry's first piece
             listed += total;
             if (count > 0 && at < ATT_PIECES && at + count > 0) {
+#pragma unroll 1
                 for (int line = lines0; line <= lines1 && at < ATT_PIECES; ++line) {
                     int t0, t1;
                     range_of(line, t0, t1);
+#pragma unroll 1
                     for (; t0 < t1; t0 = (t0 / ATT_CHUNK + 1) * ATT_CHUNK, ++at) {
                         if (at < 0 || at >= ATT_PIECES) continue;
                         const int chunk = t0 / ATT_CHUNK, end = (chunk + 1) * ATT_CHUNK < t1 ? (chunk + 1) * ATT_CHUNK : t1;
@@ -500,28 +520,27 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             // Four rows of a tile to a lane.  Their numbers: of the first, the others follow where boxes have
             // four rows or more, else one by one; and which of them count, as bits.
             struct Rows { int row[4]; uint32_t valid; };
-            auto look_up = [&](int b, int h, int token, int lo, int hi, int seen, int t) -> Rows {
+            auto look_up = [&](const Piece& p, int t) -> Rows {
                 Rows r;
                 r.valid = 0;
-                const int pos0 = t * ATT_TILE + lane * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    r.row[e] = -1;
-                    if ((e > 0 && box >= 4) || pos0 + e >= hi) continue;
-                    int pos = pos0 + e;
-                    if (a.blocks) {
-                        const int j = a.blocks[((long long)token * a.pg.H_kv + h) * a.keep + (pos >> a.block_shift)];
-                        pos = j < 0 || j > (seen - 1) >> a.block_shift ? -1 : (j << a.block_shift) + (pos & (a.block - 1));
+#pragma unroll 1
+                for (int e = 0; e < (box >= 4 ? 1 : 4); ++e) {
+                    const int at = t * ATT_TILE + lane * 4 + e;          // place among the keys
+                    int pos = at;                        // position in the sequence
+                    if (a.blocks && at < p.hi) {
+                        const int j = a.blocks[((long long)p.token * a.pg.H_kv + p.h) * a.keep + (at >> a.block_shift)];
+                        pos = j < 0 || j > (p.seen - 1) >> a.block_shift ? -1 : (j << a.block_shift) + (at & (a.block - 1));
                     }
                     // (rows of a box share the page: the first of them may lie before lo)
-                    const long long row = pos + (box >= 4 ? 3 : 0) < lo ? -1 : cache_row(a.pg, b, pos);
-                    if (row >= 0) r.row[e] = (int)(row + (long long)h * a.pg.page_size);
+                    const long long found = at >= p.hi || at + (box >= 4 ? 3 : 0) < p.lo ? -1 : cache_row(a.pg, p.b, pos);
+                    const int row = found < 0 ? -1 : (int)(found + (long long)p.h * a.pg.page_size);
+                    if (e == 0) r.row[0] = row;
+                    else if (e == 1) r.row[1] = row;
+                    else if (e == 2) r.row[2] = row;
+                    else r.row[3] = row;
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        if (x == e || (box >= 4 && e == 0)) {
-                            const int at = pos0 + x, p = pos + x - e;            // place among the keys, position in the sequence
-                            if (row >= 0 && at >= lo && at < hi && p < seen) r.valid |= 1u << x;
-                        }
+                        if ((x == e || box >= 4) && row >= 0 && at + x - e >= p.lo && at + x - e < p.hi && pos + x - e < p.seen) r.valid |= 1u << x;
                 }
                 return r;
             };
@@ -534,10 +553,12 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
-                Rows next = look_up(p.b, p.h, p.token, p.lo, p.hi, p.seen, p.tile0);
-                for (int t = 0; t < n && ok; ++t) {
+                Rows next;
+#pragma unroll 1
+                for (int t = -1; t < n && ok; ++t) {     // (the numbers of a tile's rows are looked up while the one before is waited for)
                     const Rows r = next;
-                    if (t + 1 < n) next = look_up(p.b, p.h, p.token, p.lo, p.hi, p.seen, p.tile0 + t + 1);
+                    if (t + 1 < n) next = look_up(p, p.tile0 + t + 1);
+                    if (t < 0) continue;
                     const uint32_t load = loads + (keys ? k_load(t) : v_load(t, n)), slot = load % Smem::SLOTS, turn = load / Smem::SLOTS;
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.empty[slot]), (turn & 1) ^ 1, gave_up));
                     if (!ok) break;
@@ -557,20 +578,20 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         } else if (box >= 8 && (pair == 0 || pair == 255u)) {
                             if (!(lane & 1)) copy(&maps.v_eight, dst, pair ? r.row[0] : a.total_rows, bar);
                         } else {
-#pragma unroll
+#pragma unroll 1
                             for (int e = 0; e < 4; ++e) copy(&maps.v_row, dst + e * 128, r.valid >> e & 1 ? r.row[0] + e : a.total_rows, bar);
                         }
                     } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
+#pragma unroll 1
+                        for (int e = 0; e < 4; e += box) {
                             const uint32_t mine = r.valid >> e & ((1u << box) - 1);
-                            if (box == 2 && (e & 1)) continue;
-                            const int row = mine & 1 ? r.row[e] : r.row[e | 1] - 1;
+                            // of the box's first row, and of its second (that of another box of one row does not matter)
+                            const int row0 = e == 0 ? r.row[0] : (e == 1 ? r.row[1] : (e == 2 ? r.row[2] : r.row[3])), row1 = e == 0 ? r.row[1] : r.row[3];
                             if (keys || mine == 0 || mine == (1u << box) - 1) {
-                                copy(map, dst + e * 128, mine ? row : a.total_rows, bar);
+                                copy(map, dst + e * 128, mine == 0 ? a.total_rows : (mine & 1 ? row0 : row1 - 1), bar);
                             } else {
-                                copy(&maps.v_row, dst + e * 128, mine & 1 ? r.row[e] : a.total_rows, bar);
-                                copy(&maps.v_row, dst + (e + 1) * 128, mine & 2 ? r.row[e | 1] : a.total_rows, bar);
+                                copy(&maps.v_row, dst + e * 128, mine & 1 ? row0 : a.total_rows, bar);
+                                copy(&maps.v_row, dst + (e + 1) * 128, mine & 2 ? row1 : a.total_rows, bar);
                             }
                         }
                     }
@@ -601,6 +622,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             const uint32_t issue = elect_one();          // always the same lane
             const int s = warp - ATT_MMA_WARP;
             const uint32_t S = tmem + s * ATT_TILE, O = tmem + 2 * ATT_TILE + s * D, q = smem_of(sm.q[s]);
+#pragma unroll 1
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
                 const int n = __shfl_sync(0xffffffffu, p.tile1 - p.tile0, 0), step = __shfl_sync(0xffffffffu, p.rows > ATT_TILE ? 1 : 2, 0);
@@ -714,6 +736,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 if (lane == 0) bar_arrive(smem_of(&sm.q_ready[s]));
             };
             bool fetched = false;                        // the queries of the next piece are there
+#pragma unroll 1
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
@@ -724,14 +747,18 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 const bool live = r >= 0, warp_live = __any_sync(0xffffffffu, live);
                 const int c0 = copy * (4 / copies), c1 = c0 + 4 / copies;        // columns of this warp, in 32s
                 float ref = ATT_NONE, l = 0.f;
-                if (turn_count > 0 && !fetched) {
-                    fetch_q(p);
-                    give_q(p);
-                }
+                // (the queries of the first tile; those of the next piece are asked for at the last tile, in the same place)
+                bool here = fetched || turn_count == 0;
                 fetched = false;
+#pragma unroll 1
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
                     const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
+                    if (!here) {
+                        fetch_q(p);
+                        give_q(p);
+                        here = true;
+                    }
                     ok = bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up);
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
@@ -872,45 +899,44 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 // ---------------------------------------------------------------------------------------
 constexpr int JOIN_THREADS = 256, JOIN_DEEP = 4, JOIN_CTAS = 8;          // (CTAs that share the channels at most)
 
+// x / n for 0 <= x < 2^13 and n <= x or not much more, from 1 / n: an integer division takes several times as long
+__device__ __forceinline__ int small_div(int x, float per_n) { return (int)(((float)x + 0.5f) * per_n); }
+
 // A KV head of one sequence (or token), or a share of its channels.  The parts that hold its rows lie one behind
 // the other: a line's, in the order of the CTAs that had it (its group's line, of which its rows may be in two, and its own).
 // Four channels of a row go to a thread, or to several that share the parts.  All orders are fixed, so that
-// results do not depend on timing.
+// results do not depend on timing.  What does not need the parts is done before they are there; what is left is a few
+// steps that wait for memory one after the other, so each loads all it can.
 template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join_kernel(const __grid_constant__ AttendArgs a) {
-    __shared__ float s_late[16 * 15 * 16];               // scores of the keys that the first token does not see
-    __shared__ long long s_late_row[15];
+    __shared__ float s_late[16 * 16 * 16];               // scores of the keys that the first token does not see, 16 to a row
+    __shared__ long long s_late_row[16];
     __shared__ struct { const float* part; int count; } s_line[3];       // parts of a chunk of a line: the first one, and how many
-    __shared__ float s_sum[6][JOIN_THREADS];
-    pdl_wait();
+    __shared__ float4 s_o[JOIN_THREADS];
+    __shared__ float2 s_ml[JOIN_THREADS];
     const int h = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
-    const int flag = tid < a.grid ? a.flags[tid] : 0;
-    const int units = a.head->units;
-    const Entry own = a.entry[a.n_groups + i];
-    const int g = a.blocks ? -1 : a.group_of[i];
-    Entry group;
-    group.rows = group.hi = group.tiles = group.chunks = 0;
-    if (g >= 0) group = a.entry[g];
-    const bool shared = own.hi >= group.hi && group.tiles > 0;           // (not an empty sequence)
-    const int shared_row = shared ? (own.token - group.token) * a.G : 0, m0 = shared_row / (2 * ATT_TILE);
-    const bool two = shared && (shared_row + own.rows - 1) / (2 * ATT_TILE) > m0;
+    const int rows = a.blocks ? a.G : a.T * a.G, token0 = a.blocks ? i : i * a.T;
     // later draft tokens: all queries are read before the first output is written, which may take their place
-    int late = 0;
+    int late = 0, first_seen = 0;
     if (!a.blocks && a.T > 1) {
-        const long long len = a.seq_lens[i], first = keys_seen(a.pg, len, a.T, 0), end = keys_seen(a.pg, len, a.T, a.T - 1);
-        late = (int)(end - first);
+        const int len = a.seq_lens[i], end = keys_seen(a.pg, len, a.T, a.T - 1);
+        first_seen = keys_seen(a.pg, len, a.T, 0);
+        late = end - first_seen;
         if (tid < late) {
-            const long long row = cache_row(a.pg, i, first + tid);
+            const long long row = cache_row(a.pg, i, first_seen + tid);
             s_late_row[tid] = row < 0 ? -1 : row + (long long)h * a.pg.page_size;
         }
+        first_seen = len - a.T + 1 - first_seen;         // (below 0 where the first tokens see nothing)
         __syncthreads();
+        const int shift = late > 1 ? 32 - __clz(late - 1) : 0;
         // 8 lanes to a score
-        for (int x0 = 0; x0 < own.rows * late; x0 += JOIN_THREADS / 8) {
-            const int x = x0 + tid / 8, r = x / late, k = x - r * late, share = tid % 8;
+#pragma unroll 1
+        for (int x0 = 0; x0 < rows << shift && late > 0; x0 += JOIN_THREADS / 8) {
+            const int x = x0 + tid / 8, r = x >> shift, k = x - (r << shift), share = tid % 8, t = small_div(r, a.per_G);
             float s = 0.f;
-            const bool sees = x < own.rows * late && first + k < keys_seen(a.pg, len, a.T, r / a.G) && s_late_row[k] >= 0;
+            const bool sees = r < rows && k < late && k < first_seen + t && s_late_row[k] >= 0;
             if (sees) {
                 const uint16_t* key = reinterpret_cast<const uint16_t*>(a.pg.k) + s_late_row[k] * D + share * 8;
-                const uint16_t* q = a.q + ((long long)own.token + r / a.G) * a.q_stride + (long long)(h * a.G + r % a.G) * D + share * 8;
+                const uint16_t* q = a.q + ((long long)token0 + t) * a.q_stride + (long long)(h * a.G + r - t * a.G) * D + share * 8;
 #pragma unroll
                 for (int c = 0; c < D; c += 64) {
                     float kf[8], qf[8];
@@ -922,110 +948,150 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
             }
 #pragma unroll
             for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (sees && share == 0) s_late[x] = s * a.scale_log2;
+            if (sees && share == 0) s_late[r * 16 + k] = s * a.scale_log2;
         }
     }
-    const bool failed = __syncthreads_or(flag != 0);
-
-    const int wide = D / 4 / gridDim.z, work = own.rows * wide;
-    int splits = 1;
-    while (2 * splits * work <= JOIN_THREADS) splits *= 2;
+    pdl_wait();
+    const int flag = tid < a.grid ? a.flags[tid] : 0;
+    const int units = a.head->units;
+    const int g = a.blocks ? -1 : a.group_of[i];
+    const Entry* own = a.entry + a.n_groups + i;
+    const Entry* group = a.entry + (g >= 0 ? g : 0);
+    // (an empty sequence has no part in its group's line)
+    const bool shared = g >= 0 && own->hi >= group->hi && group->tiles > 0;
+    const int shared_row = shared ? (token0 - group->token) * a.G : 0, m0 = shared_row / (2 * ATT_TILE), group_rows = shared ? group->rows : 0;
+    const int group_chunks = shared ? group->chunks : 0, chunks = group_chunks > own->chunks ? group_chunks : own->chunks;
+    bool failed = false;
+    const int work = rows * a.join_wide, splits = a.join_splits;
+#pragma unroll 1
     for (int x0 = 0; x0 < work; x0 += JOIN_THREADS) {
-        const int split = splits > 1 ? tid / work : 0, x = x0 + (splits > 1 ? tid % work : tid);
+        const int split = splits > 1 ? small_div(tid, a.per_work) : 0, x = x0 + tid - split * work, quad = small_div(x, a.per_row);
+        const int r = x - quad * rows, c4 = blockIdx.z * a.join_wide + quad;
         const bool on = x < work && split < splits;
-        const int r = x % own.rows, c4 = blockIdx.z * wide + x / own.rows;
         float M = ATT_NONE, L = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](float m, float l, float4 o) {
-            const float top = fmaxf(M, m), f = exp2_approx(M - top), e = exp2_approx(m - top);
-            M = top;
-            L = L * f + l * e;
-            O.x = O.x * f + o.x * e;
-            O.y = O.y * f + o.y * e;
-            O.z = O.z * f + o.z * e;
-            O.w = O.w * f + o.w * e;
-        };
-        // The row `row` of `rows` in a row tile: with more than 128 rows in one half of each part, with fewer in
-        // both, in `copies` places.
-        auto add_parts = [&](const float* parts, int count, int half_rows, int row, int rows) {
-            const bool both = rows > ATT_TILE;
-            const int copies = copies_of(rows), places = both ? 1 : 2 * copies, all = count * places, apart = half_rows / copies, shift = __ffs(places) - 1;
-            const int h0 = both ? row / ATT_TILE : 0, at0 = both ? row % ATT_TILE : row, half_size = half_floats(half_rows, D);
-            for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
-                float2 ml[JOIN_DEEP];
-                float4 o[JOIN_DEEP];
-#pragma unroll
-                for (int d = 0; d < JOIN_DEEP; ++d) {
-                    const int k = k0 + d * splits;
-                    ml[d].x = ATT_NONE;
-                    if (k < all) {
-                        const int part = k >> shift, place = k & (places - 1), at = at0 + (place >> 1) * apart;
-                        const float* half = parts + (2ll * part + h0 + (place & 1)) * half_size;
-                        ml[d] = *reinterpret_cast<const float2*>(half + weight_at(at, half_rows, D));
-                        o[d] = *reinterpret_cast<const float4*>(half + sums_at(at, c4, D));
-                    }
-                }
-#pragma unroll
-                for (int d = 0; d < JOIN_DEEP; ++d)
-                    if (ml[d].x != ATT_NONE) add(ml[d].x, ml[d].y, o[d]);
-            }
-        };
-        // chunk by chunk (of lines of more than ATT_CHUNK tiles)
-        const int chunks = group.chunks > own.chunks ? group.chunks : own.chunks;
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            if (chunk > 0) __syncthreads();
+        // Chunk by chunk (of lines of more than ATT_CHUNK tiles); a sequence without keys has its late ones
+#pragma unroll 1
+        for (int chunk = 0; chunk == 0 || chunk < chunks; ++chunk) {
+            if (chunk > 0 || x0 > 0) __syncthreads();
             if (tid % 32 == 0 && tid < 96) {             // one warp for each: who had the chunk
                 const int which = tid / 32;
-                const Entry& e = which < 2 ? group : own;
-                const int half_rows = which < 2 ? ATT_TILE : a.own_rows;
-                s_line[which].count = 0;
-                if (chunk < e.chunks && (which == 2 || (shared && (which == 0 || two)))) {
-                    const int line = (which < 2 ? m0 + which : 0) * a.pg.H_kv + h, tile0 = chunk * ATT_CHUNK;
-                    const int tiles = e.tiles - tile0 < ATT_CHUNK ? e.tiles - tile0 : ATT_CHUNK, u = e.u + line * line_units(e) + ATT_START + tile0;
-                    const Shares shares(units, a.grid);
-                    const int c0 = shares.of(u), c1 = shares.of(u + tiles - 1);
-                    s_line[which].count = c1 - c0 + 1;
-                    s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
-                                         ((long long)e.item + (long long)line * a.max_chunks + chunk + c0) * (2 * half_floats(half_rows, D));
+                const Entry* e = which < 2 ? group : own;
+                int count = 0;
+                if (which == 2 || (shared && (which == 0 || (shared_row + rows - 1) / (2 * ATT_TILE) > m0))) {
+                    const int line = (which < 2 ? m0 + which : 0) * a.pg.H_kv + h, tile0 = chunk * ATT_CHUNK, left = e->tiles - tile0;
+                    const int u = e->u + line * line_units(*e) + ATT_START + tile0, tiles = left < ATT_CHUNK ? left : ATT_CHUNK;
+                    if (tiles > 0) {
+                        const int c0 = share_of(u, units, a.grid);
+                        count = share_of(u + tiles - 1, units, a.grid) - c0 + 1;
+                        s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
+                                             ((long long)e->item + (long long)line * a.max_chunks + chunk + c0) * (2 * half_floats(which < 2 ? ATT_TILE : a.own_rows, D));
+                    }
+                }
+                s_line[which].count = count;
+            }
+            failed = __syncthreads_or(flag != 0);
+            if (on) {
+                // Row `row` of a row tile: with more than 128 rows in one half of each part, with fewer in both, in
+                // `copies` places.  Places of the group's line, then of the own one, then the late keys.
+                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), tile_rows = group_rows - (m0 + m) * (2 * ATT_TILE);
+                const bool g_both = tile_rows > ATT_TILE, o_both = rows > ATT_TILE;
+                const int g_copies = copies_of(tile_rows) >> 1, o_copies = copies_of(rows) >> 1;             // as shifts: 0, 1, 2
+                const int g_shift = g_both ? 0 : g_copies + 1, o_shift = o_both ? 0 : o_copies + 1;
+                const int n_group = s_line[m].count << g_shift, n_own = n_group + (s_line[2].count << o_shift);
+                const int sees = chunk == 0 && late > 0 ? first_seen + small_div(r, a.per_G) : 0, all = n_own + (sees < late ? (sees > 0 ? sees : 0) : late);
+                const float *g_part = s_line[m].part, *o_part = s_line[2].part;
+                // (a float2 of the row's reference and sum, and its sums)
+                const int g_row = row % (2 * ATT_TILE) % ATT_TILE, o_row = r % ATT_TILE;
+                const int g_half = half_floats(ATT_TILE, D), o_half = half_floats(a.own_rows, D);
+                const int g_skip = g_both ? row % (2 * ATT_TILE) / ATT_TILE : 0, o_skip = r / ATT_TILE;
+#pragma unroll 1
+                for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
+                    float2 ml[JOIN_DEEP];
+                    float4 o[JOIN_DEEP];
+#pragma unroll
+                    for (int d = 0; d < JOIN_DEEP; ++d) {
+                        const int k = k0 + d * splits;
+                        ml[d] = make_float2(ATT_NONE, 0.f);
+                        o[d] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (k < n_own) {
+                            const bool of_group = k < n_group;
+                            const int shift = of_group ? g_shift : o_shift, j = of_group ? k : k - n_group, place = j & ((1 << shift) - 1);
+                            const int half_rows = of_group ? ATT_TILE : a.own_rows;
+                            const int at = (of_group ? g_row : o_row) + (place >> 1) * (half_rows >> (of_group ? g_copies : o_copies));
+                            const float* half = (of_group ? g_part : o_part) + (long long)(2 * (j >> shift) + (of_group ? g_skip : o_skip) + (place & 1)) * (of_group ? g_half : o_half);
+                            ml[d] = *reinterpret_cast<const float2*>(half + weight_at(at, half_rows, D));
+                            o[d] = *reinterpret_cast<const float4*>(half + sums_at(at, c4, D));
+                        } else if (k < all && s_late_row[k - n_own] >= 0) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(a.pg.v) + s_late_row[k - n_own] * D + c4 * 4);
+                            ml[d] = make_float2(s_late[r * 16 + k - n_own], 1.f);
+                            const float2 v0 = unpack2<DT>(v.x), v1 = unpack2<DT>(v.y);
+                            o[d] = make_float4(v0.x, v0.y, v1.x, v1.y);
+                        }
+                    }
+                    float top = M;
+#pragma unroll
+                    for (int d = 0; d < JOIN_DEEP; ++d) {
+                        if (ml[d].x == -INFINITY) ml[d] = make_float2(ATT_LOW, 0.f), o[d] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (ml[d].x == ATT_NONE) o[d] = make_float4(0.f, 0.f, 0.f, 0.f);             // (never written)
+                        top = fmaxf(top, ml[d].x);
+                    }
+                    const float f = exp2_approx(M - top);
+                    M = top;
+                    L *= f;
+                    O = make_float4(O.x * f, O.y * f, O.z * f, O.w * f);
+#pragma unroll
+                    for (int d = 0; d < JOIN_DEEP; ++d) {
+                        const float e = exp2_approx(ml[d].x - top);
+                        L = fmaf(ml[d].y, e, L);
+                        O = make_float4(fmaf(o[d].x, e, O.x), fmaf(o[d].y, e, O.y), fmaf(o[d].z, e, O.z), fmaf(o[d].w, e, O.w));
+                    }
                 }
             }
+        }
+        // the splits of an item: by 2 or 4 neighbouring threads, and these by shuffles
+        int item = x;
+        bool writes = on;
+        if (splits > 1) {
+            s_ml[tid] = make_float2(M, L);
+            s_o[tid] = O;
             __syncthreads();
-            if (on) {
-                const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), rows = group.rows - (m0 + m) * (2 * ATT_TILE);
-                if (s_line[m].count > 0)
-                    add_parts(s_line[m].part, s_line[m].count, ATT_TILE, row % (2 * ATT_TILE), rows < 2 * ATT_TILE ? rows : 2 * ATT_TILE);
-                add_parts(s_line[2].part, s_line[2].count, a.own_rows, r, own.rows);
+            const int fan = splits < 4 ? 1 : 2;          // as a shift
+            item = tid >> fan;
+            writes = item < work && (tid & ((1 << fan) - 1)) == 0;
+            M = ATT_NONE, L = 0.f;
+            O = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int first = item < work ? tid & ((1 << fan) - 1) : splits;
+#pragma unroll 4
+            for (int k = first; k < splits; k += 1 << fan) M = fmaxf(M, s_ml[item + k * work].x);
+#pragma unroll 1
+            for (int o = 1; o < 1 << fan; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+#pragma unroll 4
+            for (int k = first; k < splits; k += 1 << fan) {
+                const float2 ml = s_ml[item + k * work];
+                const float4 o = s_o[item + k * work];
+                const float e = exp2_approx(ml.x - M);
+                L = fmaf(ml.y, e, L);
+                O = make_float4(fmaf(o.x, e, O.x), fmaf(o.y, e, O.y), fmaf(o.z, e, O.z), fmaf(o.w, e, O.w));
+            }
+#pragma unroll 1
+            for (int o = 1; o < 1 << fan; o <<= 1) {
+                L += __shfl_xor_sync(0xffffffffu, L, o);
+                O.x += __shfl_xor_sync(0xffffffffu, O.x, o);
+                O.y += __shfl_xor_sync(0xffffffffu, O.y, o);
+                O.z += __shfl_xor_sync(0xffffffffu, O.z, o);
+                O.w += __shfl_xor_sync(0xffffffffu, O.w, o);
             }
         }
-        for (int k = splits / 2; k > 0; k /= 2) {        // the upper half of the splits to the lower
-            __syncthreads();
-            s_sum[0][tid] = M; s_sum[1][tid] = L;
-            s_sum[2][tid] = O.x; s_sum[3][tid] = O.y; s_sum[4][tid] = O.z; s_sum[5][tid] = O.w;
-            __syncthreads();
-            const int y = tid + k * work;
-            if (on && split < k && s_sum[0][y] != ATT_NONE) add(s_sum[0][y], s_sum[1][y], make_float4(s_sum[2][y], s_sum[3][y], s_sum[4][y], s_sum[5][y]));
-        }
-        if (!on || split > 0) continue;
-        const long long token = own.token + r / a.G;
-        const int hq = h * a.G + r % a.G;
-        if (late > 0) {
-            const long long len = a.seq_lens[i], first = keys_seen(a.pg, len, a.T, 0);
-            const int mine = (int)(keys_seen(a.pg, len, a.T, r / a.G) - first);
-            for (int k = 0; k < mine; ++k) {
-                if (s_late_row[k] < 0) continue;
-                const float s = s_late[r * late + k];
-                const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(a.pg.v) + s_late_row[k] * D + c4 * 4);
-                const float2 v0 = unpack2<DT>(v.x), v1 = unpack2<DT>(v.y);
-                if (s == -INFINITY) add(ATT_LOW, 0.f, make_float4(0.f, 0.f, 0.f, 0.f));
-                else add(s, 1.f, make_float4(v0.x, v0.y, v1.x, v1.y));
-            }
-        }
+        if (!writes) continue;
+        const int column = small_div(item, a.per_row), out_row = item - column * rows, out_c4 = blockIdx.z * a.join_wide + column, t = small_div(out_row, a.per_G);
+        const long long at = ((long long)token0 + t) * a.Hq + h * a.G + out_row - t * a.G;
+        const float per_L = 1.f / L;
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (M != ATT_NONE) y = make_float4(O.x / L, O.y / L, O.z / L, O.w / L);
+        if (M != ATT_NONE) y = make_float4(O.x * per_L, O.y * per_L, O.z * per_L, O.w * per_L);
         if (failed) y.x = y.y = y.z = y.w = __int_as_float(0x7fc00000);
-        const long long at = (token * a.Hq + hq) * D + c4 * 4;
-        *reinterpret_cast<uint2*>(a.out + at) = make_uint2(pack2<DT>(y.x, y.y), pack2<DT>(y.z, y.w));
-        if (a.lse && c4 == 0) a.lse[token * a.Hq + hq] = failed ? y.x : (M == ATT_NONE ? -INFINITY : (M + log2f(L)) * 0.69314718f);
+        *reinterpret_cast<uint2*>(a.out + at * D + out_c4 * 4) = make_uint2(pack2<DT>(y.x, y.y), pack2<DT>(y.z, y.w));
+        if (a.lse && out_c4 == 0) a.lse[at] = failed ? y.x : (M == ATT_NONE ? -INFINITY : (M + log2f(L)) * 0.69314718f);
     }
 }
 

@@ -109,10 +109,18 @@ template <int DT, int D> int launch_attention(const AttendParams& p, int sequenc
     if (rc != RETOPK_OK) return rc;
     rc = launch(attend_kernel<DT, D>, dim3((unsigned)p.a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
     if (rc != RETOPK_OK) return rc;
-    // as many CTAs to a head as give the device something to do; one where outputs take the place of queries that it reads
+    // As many CTAs to a head as run at once (4 on an SM); one where outputs take the place of queries that it reads.
+    AttendArgs a = p.a;
+    const int rows = a.blocks ? a.G : a.T * a.G;
     int shares = 1;
-    while ((p.a.T == 1 || p.a.out != p.a.q) && shares < JOIN_CTAS && (long long)p.a.pg.H_kv * sequences * shares < 3ll * p.a.grid) shares *= 2;
-    return launch(join_kernel<DT, D>, dim3((unsigned)p.a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, p.a);
+    while ((a.T == 1 || a.out != a.q) && shares < JOIN_CTAS && 2ll * shares * a.pg.H_kv * sequences <= 4ll * a.grid) shares *= 2;
+    a.join_wide = D / 4 / shares;
+    a.join_splits = 1;
+    while (2 * a.join_splits * rows * a.join_wide <= JOIN_THREADS) a.join_splits *= 2;
+    a.per_row = 1.f / rows;
+    a.per_work = 1.f / (rows * a.join_wide);
+    a.per_G = 1.f / a.G;
+    return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, a);
 }
 
 // Rows of 64 channels each, `box` rows to a copy, into shared memory as the tensor cores' operands lie there.
