@@ -26,7 +26,9 @@ __device__ __forceinline__ int keys_seen(const Pages& pg, int len, int T, int t)
 
 constexpr int ATT_TILE = 128;            // keys of a tile, and query rows of a stream
 constexpr int ATT_CHUNK = 1024;          // tiles whose sums stay in the tensor core at most: it cuts additions off
-constexpr int ATT_START = 2;             // what beginning a line counts, in tiles
+// What a CTA's work counts: a tile of up to 128 query rows 1 (two of them are at work at once), one of more rows 2, and the
+// beginning of a line 3.
+constexpr int ATT_START = 3;
 constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // reference of a row without keys; lowest of one with keys
 
 struct Entry {
@@ -77,14 +79,15 @@ struct AttendParams {
 __host__ __device__ constexpr int half_floats(int rows, int d) { return (rows + 3) / 4 * 4 * (d + 2); }
 __device__ __forceinline__ int sums_at(int row, int c4, int d) { return (row >> 2) * (4 * d) + c4 * 16 + (row & 3) * 4; }
 __device__ __forceinline__ int weight_at(int row, int rows, int d) { return (rows + 3) / 4 * 4 * d + 2 * row; }
-__device__ __forceinline__ int line_units(const Entry& e) { return e.tiles > 0 ? e.tiles + ATT_START : 0; }
-// Equal shares of the line: that of CTA c begins at floor(units * c / n).  None is empty: of a short line fewer CTAs
-// have one.
+__device__ __forceinline__ int tile_shift(int rows) { return rows > ATT_TILE ? 1 : 0; }
+__device__ __forceinline__ int line_units(const Entry& e) { return e.tiles > 0 ? (e.tiles << tile_shift(e.rows)) + ATT_START : 0; }
+// Equal shares of the line: that of CTA c begins at floor(units * c / n).  None is below 2 units, of a short line fewer
+// CTAs have one: so each that lies between two tiles of a line has a tile of it too, and the parts are without holes.
 struct Shares {
     int units, n, whole, rest;
     __device__ __forceinline__ Shares(int units_, int grid) {
         units = units_;
-        n = units < grid ? units : grid;
+        n = units / 2 < grid ? units / 2 : grid;
         whole = n > 0 ? units / n : 0;
         rest = units - whole * n;
     }
@@ -93,7 +96,7 @@ struct Shares {
 
 // The CTA whose share holds unit u: the last c with floor(units * c / n) <= u.
 __device__ __forceinline__ int share_of(int u, int units, int grid) {
-    const int n = units < grid ? units : grid;
+    const int n = units / 2 < grid ? units / 2 : grid;
     const long long end = (u + 1ll) * n;
     int c = (int)(__fdividef((float)u, (float)units) * (float)n);
     c = c < 0 ? 0 : (c < n - 1 ? c : n - 1);
@@ -446,16 +449,17 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         for (int e0 = 0; e0 < a.entries && u0 < u1; e0 += ATT_THREADS) {
             const int i = e0 + tid;
             Entry e;
-            int from = 0, to = 0, len = 1, count = 0, lines0 = 0, lines1 = 0;
+            int from = 0, to = 0, len = 1, shift = 0, count = 0, lines0 = 0, lines1 = 0;
             // tiles of this CTA in a line: those that its units stand for
             auto range_of = [&](int line, int& t0, int& t1) {
                 const int x0 = from > line * len ? from - line * len : 0, x1 = to - line * len < len ? to - line * len : len;
-                t0 = x0 > ATT_START ? x0 - ATT_START : 0;
-                t1 = x1 > ATT_START ? x1 - ATT_START : 0;
+                t0 = x0 > ATT_START ? (x0 - ATT_START + (1 << shift) - 1) >> shift : 0;
+                t1 = x1 > ATT_START ? (x1 - ATT_START + (1 << shift) - 1) >> shift : 0;
             };
             if (i < a.entries) {
                 e = plan[i];
                 len = line_units(e);
+                shift = tile_shift(e.rows);
                 from = u0 > e.u ? u0 - e.u : 0;
                 const int all = len * a.pg.H_kv * e.row_tiles;
                 to = u1 - e.u < all ? u1 - e.u : all;
@@ -980,10 +984,10 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                 int count = 0;
                 if (which == 2 || (shared && (which == 0 || (shared_row + rows - 1) / (2 * ATT_TILE) > m0))) {
                     const int line = (which < 2 ? m0 + which : 0) * a.pg.H_kv + h, tile0 = chunk * ATT_CHUNK, left = e->tiles - tile0;
-                    const int u = e->u + line * line_units(*e) + ATT_START + tile0, tiles = left < ATT_CHUNK ? left : ATT_CHUNK;
+                    const int tiles = left < ATT_CHUNK ? left : ATT_CHUNK, shift = tile_shift(e->rows), u = e->u + line * line_units(*e) + ATT_START + (tile0 << shift);
                     if (tiles > 0) {
                         const int c0 = share_of(u, units, a.grid);
-                        count = share_of(u + tiles - 1, units, a.grid) - c0 + 1;
+                        count = share_of(u + ((tiles - 1) << shift), units, a.grid) - c0 + 1;
                         s_line[which].part = (which < 2 ? a.shared_parts : a.own_parts) +
                                              ((long long)e->item + (long long)line * a.max_chunks + chunk + c0) * (2 * half_floats(which < 2 ? ATT_TILE : a.own_rows, D));
                     }
