@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
                     const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
-                    if (!here) {
+                    if (__builtin_expect(!here, 0)) {
                         fetch_q(p);
                         give_q(p);
                         here = true;
@@ -768,7 +768,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     for (int h = 0; h < 2; ++h) {
                         ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up));
                         if (!ok) break;
-                        if (ahead && h == 1) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
+                        if (__builtin_expect(ahead && h == 1, 0)) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
                         if (warp_live) {
                             tc_after_sync();
                             const uint32_t Sh = S + h * (ATT_TILE / 2);
@@ -778,12 +778,12 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
                             if (!first) mx = 0;
                             if (!second) my = 0;
-                            if (first | second) {
-                                if (first) tc_ld32(Sh, x);
-                                if (second) tc_ld32(Sh + 32, y);
+                            if (__builtin_expect(first | second, 1)) {
+                                if (__builtin_expect(first, 1)) tc_ld32(Sh, x);
+                                if (__builtin_expect(second, 1)) tc_ld32(Sh + 32, y);
                                 tc_wait_ld();
                                 auto hide = [&](uint32_t* v, uint32_t m) {       // keys that do not count: weight 0
-                                    if (m == ~0u) return;
+                                    if (__builtin_expect(m == ~0u, 1)) return;
 #pragma unroll
                                     for (int j = 0; j < 32; ++j)
                                         if (!(m >> j & 1)) v[j] = 0xff800000u;
@@ -813,7 +813,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                 // before, the reference becomes the maximum, and sums so far and weights follow.
                                 weigh();
                                 const bool low = live && (!(total <= 16384.f) || (ref == ATT_NONE && (mx | my)));
-                                if (__any_sync(0xffffffffu, low)) {
+                                if (__builtin_expect(__any_sync(0xffffffffu, low), 0)) {
                                     float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                                     for (int j = 0; j < 32; j += 2) {
@@ -858,7 +858,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s][h]));
                     }
                     ++turns;
-                    if (ok && ahead) {
+                    if (__builtin_expect(ok && ahead, 0)) {
                         give_q(sm.piece[i + 1]);
                         fetched = true;
                     }
