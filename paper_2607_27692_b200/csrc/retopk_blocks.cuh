@@ -26,7 +26,7 @@ template <int DT> __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint3
 
 struct BoundsArgs {
     Pages pg;
-    int block;                  // rows of a block
+    int block, shift;           // rows of a block, and as a power of two
     const int32_t* seq_lens;
     long long n_new;            // blocks that overlap the last n_new rows
     uint16_t* bounds;           // [n_pages, H_kv, page_size / block, 2, d]
@@ -38,11 +38,10 @@ template <int DT, int D> __global__ void __launch_bounds__(BOUNDS_THREADS) bound
     constexpr int LANES = D / 8, RPW = 32 / LANES;       // lanes per row, rows per load of the warp
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.z, h = blockIdx.y;
-    const long long n = keys_seen(a.pg, a.seq_lens[b], 1, 0);
-    const long long first = a.n_new < n ? n - a.n_new : 0;
-    const long long j = first / a.block + (long long)blockIdx.x * BOUNDS_WARPS + warp;
-    if (j >= n / a.block) return;
-    const long long row0 = cache_row(a.pg, b, j * a.block);
+    const int n = keys_seen(a.pg, a.seq_lens[b], 1, 0), first = a.n_new < n ? n - (int)a.n_new : 0;
+    const int j = (first >> a.shift) + (int)blockIdx.x * BOUNDS_WARPS + warp;
+    if (j >= n >> a.shift) return;
+    const long long row0 = cache_row(a.pg, b, j << a.shift);
     if (row0 < 0) return;
     const unsigned char* src = a.pg.k + (row0 + (long long)h * a.pg.page_size) * (D * 2) + lane * 16;
     uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
@@ -69,7 +68,7 @@ template <int DT, int D> __global__ void __launch_bounds__(BOUNDS_THREADS) bound
         hi = make_uint4(max2_nan<DT>(hi.x, other(hi.x)), max2_nan<DT>(hi.y, other(hi.y)), max2_nan<DT>(hi.z, other(hi.z)), max2_nan<DT>(hi.w, other(hi.w)));
     }
     // blocks of a page and head follow one another, as its rows do
-    uint16_t* dst = a.bounds + (row0 + (long long)h * a.pg.page_size) / a.block * (2 * D);
+    uint16_t* dst = a.bounds + ((row0 + (long long)h * a.pg.page_size) >> a.shift) * (2 * D);
     if (lane < LANES) *reinterpret_cast<uint4*>(dst + lane * 8) = lo;
     else if (lane < 2 * LANES) *reinterpret_cast<uint4*>(dst + D + (lane - LANES) * 8) = hi;
 }
@@ -79,7 +78,8 @@ template <int DT, int D> __global__ void __launch_bounds__(BOUNDS_THREADS) bound
 // ---------------------------------------------------------------------------------------
 struct SelectArgs {
     Pages pg;
-    int block, T, Hq, G, keep, first, last;
+    int block, shift, T, Hq, G, keep, first, last;       // (block: 1 << shift)
+    float per_G;                // 1 / G
     const int32_t* seq_lens;
     const uint16_t* bounds;
     const uint16_t* q;
@@ -87,6 +87,7 @@ struct SelectArgs {
     float2* scores;             // [B, T, H_kv, max_blocks]: a score in fp32 and how far it may be off
     long long max_blocks;
     int32_t* blocks;            // [B, T, H_kv, keep]
+    bool scored;                // score_kernel runs before
 };
 constexpr int SCORE_THREADS = 128, SCORE_WARPS = SCORE_THREADS / 32, SCORE_ROWS = 16, SCORE_COLS = 8;
 constexpr int PICK_THREADS = 512, PICK_WARPS = PICK_THREADS / 32, PICK_KEPT = 4096, PICK_LIST = 512;
@@ -109,15 +110,15 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS, 7) sco
     pdl_start_next();
     const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, part = lane & 3;
     const int j0 = (blockIdx.x * SCORE_WARPS + warp) * SCORE_ROWS;
-    const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, a.T - 1), end = (seen + a.block - 1) / a.block - a.last;
+    const int seen = (int)keys_seen(a.pg, a.seq_lens[b], a.T, a.T - 1), end = ((seen + a.block - 1) >> a.shift) - a.last;
     if (end + a.last <= a.keep || j0 >= end) return;
     constexpr int DEEP = 2;                              // groups of 32 channels that are loaded at once
     const uint16_t* src[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
         const int j = j0 + g + 8 * y;
-        const long long r = j < end ? cache_row(a.pg, b, (long long)j * a.block) : -1;
-        src[y] = r < 0 ? nullptr : a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + part * 8;
+        const long long r = j < end ? cache_row(a.pg, b, j << a.shift) : -1;
+        src[y] = r < 0 ? nullptr : a.bounds + ((r + (long long)h * a.pg.page_size) >> a.shift) * (2 * D) + part * 8;
     }
     uint32_t largest2[2] = {0, 0};                       // of the bounds' magnitudes
     float largest[2] = {0.f, 0.f};
@@ -125,8 +126,8 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS, 7) sco
     float best = 0.f, size = 0.f;
     for (int c0 = 0; c0 < cols; c0 += SCORE_COLS) {
         float c[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-        const int col = c0 + g;
-        const uint16_t* q = a.q + ((long long)b * a.T + col / a.G) * a.q_stride + (h * a.G + col % a.G) * D + part * 8;
+        const int col = c0 + g, t = small_div(col, a.per_G);
+        const uint16_t* q = a.q + ((long long)b * a.T + t) * a.q_stride + (h * a.G + col - t * a.G) * D + part * 8;
 #pragma unroll
         for (int i0 = 0; i0 < STEPS; i0 += DEEP) {
             uint4 lo[2][DEEP], hi[2][DEEP], x[DEEP];
@@ -192,14 +193,14 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS, 7) sco
             const float most = lane & 8 ? most1 : most0;
             const bool out = (lane & 8 ? none1 : none0) != 0;
             for (int k = 0; k < SCORE_COLS && c0 + k < cols; ++k) {
-                const int head = (c0 + k) % a.G;
+                const int t = small_div(c0 + k, a.per_G), head = c0 + k - t * a.G;
                 const float s = s_score[warp][k][lane], z = s_size[warp][k];
                 best = head == 0 ? s : fmaxf(best, s);
                 size = head == 0 ? z : (z != z ? z : fmaxf(size, z));
                 if (head == a.G - 1) {
                     float off = size * most * 0x1p-17f + 1e-35f;
                     if (!(off < 1e37f) || !(fabsf(best) < 1e37f)) off = INFINITY;
-                    a.scores[(((long long)b * a.T + (c0 + k) / a.G) * a.pg.H_kv + h) * a.max_blocks + j0 + lane] =
+                    a.scores[(((long long)b * a.T + t) * a.pg.H_kv + h) * a.max_blocks + j0 + lane] =
                         out ? make_float2(-INFINITY, 0.f) : (off == INFINITY ? make_float2(0.f, INFINITY) : make_float2(best, off));
                 }
             }
@@ -282,39 +283,28 @@ template <bool EXACT, class Each> __device__ __forceinline__ void find_limit(Eac
     *rest_out = shift > 0 ? 0x7fffffff : rest;
 }
 
-// The score of block j for the heads of a group, in 64 bits and rounded once to fp32; by a warp: 8 lanes with a share of
-// the channels each for a head, four heads at a time.
-template <int DT, int D> __device__ __forceinline__ float exact_score(const SelectArgs& a, int b, int t, int h, int j) {
-    constexpr int PER = D / 8;
-    const int lane = threadIdx.x & 31, share = lane & 7;
-    const long long r = cache_row(a.pg, b, (long long)j * a.block);
+// The score of block j for a head, in 64 bits and rounded once to fp32, by a warp: D / 32 channels to a lane.
+template <int DT, int D> __device__ __forceinline__ float exact_score(const SelectArgs& a, int b, int t, int h, int g, int j) {
+    constexpr int WORDS = D / 64;
+    const int lane = threadIdx.x & 31;
+    const long long r = cache_row(a.pg, b, j << a.shift);
     if (r < 0) return -INFINITY;
-    const uint16_t* src = a.bounds + (r + (long long)h * a.pg.page_size) / a.block * (2 * D) + share * PER;
-    float score = -INFINITY;
-    for (int g0 = 0; g0 < a.G; g0 += 4) {
-        const int g = g0 + (lane >> 3) < a.G ? g0 + (lane >> 3) : a.G - 1;           // (a head twice does no harm)
-        const uint16_t* q = a.q + ((long long)b * a.T + t) * a.q_stride + ((long long)h * a.G + g) * D + share * PER;
-        double sum = 0.0;
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(a.bounds + ((r + (long long)h * a.pg.page_size) >> a.shift) * (2 * D)) + lane;
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + ((long long)b * a.T + t) * a.q_stride + ((long long)h * a.G + g) * D) + lane;
+    double sum = 0.0;
 #pragma unroll
-        for (int c = 0; c < PER; c += 8) {
-            float x[8], lo[8], hi[8];
-            unpack8<DT>(*reinterpret_cast<const uint4*>(q + c), x);
-            unpack8<DT>(*reinterpret_cast<const uint4*>(src + c), lo);
-            unpack8<DT>(*reinterpret_cast<const uint4*>(src + D + c), hi);
+    for (int w = 0; w < WORDS; ++w) {
+        const float2 x = unpack2<DT>(q[w * 32]), lo = unpack2<DT>(src[w * 32]), hi = unpack2<DT>(src[D / 2 + w * 32]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double y = x[e], p = y * lo[e], z = y * hi[e];
-                sum += p != p || z != z ? p + z : (p > z ? p : z);
-            }
+        for (int e = 0; e < 2; ++e) {
+            const double y = e ? x.y : x.x, p = y * (e ? lo.y : lo.x), z = y * (e ? hi.y : hi.x);
+            sum += p != p || z != z ? p + z : (p > z ? p : z);
         }
-#pragma unroll
-        for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        float f = (float)sum;
-        f = f != f ? INFINITY : f;
-        f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 8));
-        score = fmaxf(score, fmaxf(f, __shfl_xor_sync(0xffffffffu, f, 16)));
     }
-    return score;
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float f = (float)sum;
+    return f != f ? INFINITY : f;
 }
 
 // Scores i of a token and KV head: the first ones in shared memory.
@@ -355,7 +345,9 @@ template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs&
         uint32_t mine = in ? ~0u : 0u;
         for (uint32_t todo = __ballot_sync(0xffffffffu, some && !in); todo; todo &= todo - 1) {
             const int x = __ffs(todo) - 1, j = a.first + (i - lane) + x;
-            const float score = exact_score<DT, D>(a, b, t, h, j);
+            float score = -INFINITY;
+#pragma unroll 1
+            for (int g = 0; g < a.G; ++g) score = fmaxf(score, exact_score<DT, D>(a, b, t, h, g, j));
             if (lane == x) mine = order_of(score);
         }
         if (i < m) at[i].x = __uint_as_float(mine);
@@ -395,20 +387,28 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     __shared__ int s_bin[BINS], s_count, s_found[3];
     __shared__ __align__(16) uint32_t s_cand[PICK_LIST], s_lower[PICK_LIST], s_upper[PICK_LIST], s_key[PICK_LIST];
     __shared__ uint32_t s_low[PICK_WARPS], s_high[PICK_WARPS];
-    pdl_wait();
+    __shared__ int s_opened;
+    int* const s_open = s_bin;                           // (the bins are done with by then)
     const int h = blockIdx.x, t = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const long long seen = keys_seen(a.pg, a.seq_lens[b], a.T, t);
-    const int N = (int)((seen + a.block - 1) / a.block);
+    if (!a.scored) pdl_wait();                           // (else score_kernel has waited for all but its own scores)
+    const int seen = keys_seen(a.pg, a.seq_lens[b], a.T, t), N = (seen + a.block - 1) >> a.shift;
     const long long item = ((long long)b * a.T + t) * a.pg.H_kv + h;
     int32_t* out = a.blocks + item * a.keep;
     if (N <= a.keep) {
+#pragma unroll 1
         for (int i = tid; i < a.keep; i += PICK_THREADS) out[i] = i < N ? i : -1;
         return;
     }
     const int want = a.keep - a.first - a.last, m = N - a.first - a.last;
+#pragma unroll 1
     for (int i = tid; i < a.first; i += PICK_THREADS) out[i] = i;
+#pragma unroll 1
     for (int i = tid; i < a.last; i += PICK_THREADS) out[a.keep - a.last + i] = N - a.last + i;
     if (want == 0) return;
+#pragma unroll
+    for (int i = 0; i < BINS / PICK_THREADS; ++i) s_bin[i * PICK_THREADS + tid] = 0;
+    if (tid == 0) s_count = s_opened = 0;
+    if (a.scored) pdl_wait();
     const Scores at = {s_kept, a.scores + item * a.max_blocks + a.first};
     auto lower = [](float2 s) { return order_of(__fsub_rd(s.x, s.y)); };
     auto upper = [](float2 s) { return order_of(__fadd_ru(s.x, s.y)); };
@@ -433,8 +433,6 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
         high = __reduce_max_sync(0xffffffffu, high);
         if (lane == 0) { s_low[warp] = low; s_high[warp] = high; }
     }
-    for (int i = tid; i < BINS; i += PICK_THREADS) s_bin[i] = 0;
-    if (tid == 0) s_count = 0;
     __syncthreads();
     const uint32_t low = __reduce_min_sync(0xffffffffu, s_low[lane % PICK_WARPS]), high = __reduce_max_sync(0xffffffffu, s_high[lane % PICK_WARPS]);
     // bins, BITS of what the lower ends have above the least of them at a time, until one holds few
@@ -443,6 +441,7 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     int rest = want, shift = bits;
     while (shift > 0) {
         const int width = shift < BITS ? shift : BITS, next = shift - width;
+#pragma unroll 2
         for (int i = tid; i < m; i += PICK_THREADS) {
             const uint32_t u = lower(at[i]) - low;
             if (shift == bits || u >> shift == prefix) atomicAdd(&s_bin[(u >> next) & (BINS - 1)], 1);
@@ -474,6 +473,7 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     }
     const uint32_t limit = low + (prefix << shift);
     // the blocks that reach the limit
+#pragma unroll 1
     for (int i0 = 0; i0 < m; i0 += PICK_THREADS) {
         const int i = i0 + tid;
         const float2 s = i < m ? at[i] : make_float2(0.f, 0.f);
@@ -497,7 +497,7 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     // a candidate to a thread, the others four at a time (filled up with ones that count for nothing)
     const int C4 = (C + 3) / 4;
     auto each4 = [&](const uint32_t* x, auto f) {
-#pragma unroll 4
+#pragma unroll 2
         for (int k = 0; k < C4; ++k) {
             const uint4 v = reinterpret_cast<const uint4*>(x)[k];
             f(v.x, 4 * k); f(v.y, 4 * k + 1); f(v.z, 4 * k + 2); f(v.w, 4 * k + 3);
@@ -515,15 +515,18 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
             int better = 0, rivals = 0;
             each4(s_lower, [&](uint32_t u, int) { better += u > hi; });
             each4(s_upper, [&](uint32_t u, int) { rivals += u >= lo; });
-            s_key[tid] = better >= want ? 0u : (rivals <= want ? ~0u : 1u);
+            const bool out_of_it = better >= want, in_it = rivals <= want;
+            s_key[tid] = !out_of_it && in_it ? ~0u : 0u;
+            if (!out_of_it && !in_it) s_open[atomicAdd(&s_opened, 1)] = tid;
         }
         __syncthreads();
-        for (int c = warp; c < C; c += PICK_WARPS)
-            if (s_key[c] == 1u) {
-                const float score = exact_score<DT, D>(a, b, t, h, a.first + (int)s_cand[c]);
-                __syncwarp();
-                if (lane == 0) s_key[c] = order_of(score);
-            }
+        // the largest of the heads' scores
+#pragma unroll 1
+        for (int x = warp; x < s_opened * a.G; x += PICK_WARPS) {
+            const int y = small_div(x, a.per_G), c = s_open[y];
+            const float score = exact_score<DT, D>(a, b, t, h, x - y * a.G, a.first + (int)s_cand[c]);
+            if (lane == 0) atomicMax(&s_key[c], order_of(score));
+        }
         __syncthreads();
         bool in = false;
         if (tid < C) {

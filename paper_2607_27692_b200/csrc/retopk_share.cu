@@ -234,6 +234,7 @@ int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, in
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
     a.block = block;
+    a.shift = __builtin_ctz((unsigned)block);
     a.seq_lens = seq_lens;
     a.n_new = n_new;
     a.bounds = static_cast<uint16_t*>(bounds);
@@ -272,7 +273,8 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
     const Memory q_m = memory_of(Strided{q, q_stride, H_q}, (long long)B * T, pages->d), ws_m = {workspace, (uint64_t)workspace_bytes};
     const Memory bounds_m = bounds_memory(pages, block, bounds), blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
     if (!all_apart(blocks_m, {q_m, ws_m, bounds_m}) || !all_apart(ws_m, {q_m, bounds_m})) return RETOPK_EINVAL;
-    a.block = block; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv; a.keep = keep; a.first = first; a.last = last;
+    a.block = block; a.shift = __builtin_ctz((unsigned)block); a.per_G = 1.f / (float)(H_q / pages->H_kv); a.scored = a.max_blocks > keep;
+    a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv; a.keep = keep; a.first = first; a.last = last;
     a.seq_lens = seq_lens;
     a.bounds = static_cast<const uint16_t*>(bounds);
     a.q = static_cast<const uint16_t*>(q);
@@ -280,7 +282,7 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
     a.scores = static_cast<float2*>(workspace);
     a.blocks = blocks;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.max_blocks > keep) {
+    if (a.scored) {
         constexpr int PER_CTA = SCORE_WARPS * SCORE_ROWS;
         const dim3 grid((unsigned)((a.max_blocks + PER_CTA - 1) / PER_CTA), (unsigned)pages->H_kv, (unsigned)B);
         rc = by_type(pages, score_kernel<TYPE_BF16, 128>, score_kernel<TYPE_BF16, 64>, score_kernel<TYPE_FP16, 128>,
