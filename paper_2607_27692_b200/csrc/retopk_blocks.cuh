@@ -90,7 +90,7 @@ struct SelectArgs {
     bool scored;                // score_kernel runs before
 };
 constexpr int SCORE_THREADS = 128, SCORE_WARPS = SCORE_THREADS / 32, SCORE_ROWS = 16, SCORE_COLS = 8;
-constexpr int PICK_THREADS = 512, PICK_WARPS = PICK_THREADS / 32, PICK_KEPT = 4096, PICK_LIST = 512;
+constexpr int PICK_THREADS = 512, PICK_WARPS = PICK_THREADS / 32, PICK_DEEP = 8, PICK_LIST = 512;
 
 __device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
 
@@ -307,16 +307,10 @@ template <int DT, int D> __device__ __forceinline__ float exact_score(const Sele
     return f != f ? INFINITY : f;
 }
 
-// Scores i of a token and KV head: the first ones in shared memory.
-struct Scores {
-    float2 *kept, *rest;
-    __device__ __forceinline__ float2& operator[](int i) const { return i < PICK_KEPT ? kept[i] : rest[i]; }
-};
-
 // Any number of blocks to choose from, any number of equal scores.  A block whose upper end
 // is below the want-th largest lower end is out, and one whose lower end is above the (want + 1)-th largest
 // upper end is in; those between are scored exactly.
-template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs& a, Scores at, int b, int t, int h, int m, int want, int32_t* out) {
+template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs& a, float2* at, int b, int t, int h, int m, int want, int32_t* out) {
     const int tid = threadIdx.x, lane = tid & 31;
     uint32_t lowest, limit;
     int rest;
@@ -382,8 +376,7 @@ template <int DT, int D> __device__ __noinline__ void pick_any(const SelectArgs&
 // largest lower end gives a limit that few blocks reach with their upper end; among those, each is compared with
 // all others, and those that stay open are scored exactly.
 template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick_kernel(const __grid_constant__ SelectArgs a) {
-    constexpr int BITS = 10, BINS = 1 << BITS, DEEP = PICK_KEPT / PICK_THREADS;
-    __shared__ float2 s_kept[PICK_KEPT];
+    constexpr int BITS = 10, BINS = 1 << BITS, DEEP = PICK_DEEP;
     __shared__ int s_bin[BINS], s_count, s_found[3];
     __shared__ __align__(16) uint32_t s_cand[PICK_LIST], s_lower[PICK_LIST], s_upper[PICK_LIST], s_key[PICK_LIST];
     __shared__ uint32_t s_low[PICK_WARPS], s_high[PICK_WARPS];
@@ -409,26 +402,26 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     for (int i = 0; i < BINS / PICK_THREADS; ++i) s_bin[i * PICK_THREADS + tid] = 0;
     if (tid == 0) s_count = s_opened = 0;
     if (a.scored) pdl_wait();
-    const Scores at = {s_kept, a.scores + item * a.max_blocks + a.first};
+    float2* const at = a.scores + item * a.max_blocks + a.first;
     auto lower = [](float2 s) { return order_of(__fsub_rd(s.x, s.y)); };
     auto upper = [](float2 s) { return order_of(__fadd_ru(s.x, s.y)); };
+    float2 x[DEEP];                                      // the first scores of this thread; others are read again where they are wanted
+#pragma unroll
+    for (int k = 0; k < DEEP; ++k)
+        if (k * PICK_THREADS + tid < m) x[k] = at[k * PICK_THREADS + tid];
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+            if (k * PICK_THREADS + tid < m) f(k * PICK_THREADS + tid, x[k]);
+#pragma unroll 1
+        for (int i = DEEP * PICK_THREADS + tid; i < m; i += PICK_THREADS) f(i, at[i]);
+    };
     {
         uint32_t low = ~0u, high = 0;
-        float2 x[DEEP];
-#pragma unroll
-        for (int k = 0; k < DEEP; ++k)
-            if (k * PICK_THREADS + tid < m) x[k] = at.rest[k * PICK_THREADS + tid];
-#pragma unroll
-        for (int k = 0; k < DEEP; ++k)
-            if (k * PICK_THREADS + tid < m) {
-                s_kept[k * PICK_THREADS + tid] = x[k];
-                low = min(low, lower(x[k]));
-                high = max(high, lower(x[k]));
-            }
-        for (int i = PICK_KEPT + tid; i < m; i += PICK_THREADS) {
-            low = min(low, lower(at.rest[i]));
-            high = max(high, lower(at.rest[i]));
-        }
+        each([&](int, float2 v) {
+            low = min(low, lower(v));
+            high = max(high, lower(v));
+        });
         low = __reduce_min_sync(0xffffffffu, low);
         high = __reduce_max_sync(0xffffffffu, high);
         if (lane == 0) { s_low[warp] = low; s_high[warp] = high; }
@@ -439,13 +432,13 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     const int bits = high > low ? 32 - __clz(high - low) : 0;
     uint32_t prefix = 0;
     int rest = want, shift = bits;
+#pragma unroll 1
     while (shift > 0) {
         const int width = shift < BITS ? shift : BITS, next = shift - width;
-#pragma unroll 2
-        for (int i = tid; i < m; i += PICK_THREADS) {
-            const uint32_t u = lower(at[i]) - low;
+        each([&](int, float2 v) {
+            const uint32_t u = lower(v) - low;
             if (shift == bits || u >> shift == prefix) atomicAdd(&s_bin[(u >> next) & (BINS - 1)], 1);
-        }
+        });
         __syncthreads();
         constexpr int PER = BINS / PICK_THREADS;          // bins of a thread, from the largest down
         int n[PER], mine = 0, total;
@@ -472,79 +465,77 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
         __syncthreads();
     }
     const uint32_t limit = low + (prefix << shift);
-    // the blocks that reach the limit
-#pragma unroll 1
-    for (int i0 = 0; i0 < m; i0 += PICK_THREADS) {
-        const int i = i0 + tid;
-        const float2 s = i < m ? at[i] : make_float2(0.f, 0.f);
-        const bool in = i < m && upper(s) >= limit;
-        const uint32_t who = __ballot_sync(0xffffffffu, in);
-        int base = 0;
-        if (lane == 0 && who) base = atomicAdd(&s_count, __popc(who));
-        base = __shfl_sync(0xffffffffu, base, 0) + __popc(who & ((1u << lane) - 1));
-        if (in && base < PICK_LIST) {
-            s_cand[base] = i;
-            s_lower[base] = lower(s);
-            s_upper[base] = upper(s);
-        }
-    }
+    // the blocks that reach the limit, in any order
+    each([&](int i, float2 v) {
+        const uint32_t u = upper(v);
+        if (u < limit) return;
+        const int c = atomicAdd(&s_count, 1);
+        if (c >= PICK_LIST) return;
+        s_cand[c] = i;
+        s_lower[c] = lower(v);
+        s_upper[c] = u;
+    });
     __syncthreads();
     const int C = s_count;
     if (C > PICK_LIST) {
         pick_any<DT, D>(a, at, b, t, h, m, want, out);
         return;
     }
-    // a candidate to a thread, the others four at a time (filled up with ones that count for nothing)
-    const int C4 = (C + 3) / 4;
-    auto each4 = [&](const uint32_t* x, auto f) {
-#pragma unroll 2
-        for (int k = 0; k < C4; ++k) {
-            const uint4 v = reinterpret_cast<const uint4*>(x)[k];
-            f(v.x, 4 * k); f(v.y, 4 * k + 1); f(v.z, 4 * k + 2); f(v.w, 4 * k + 3);
-        }
+    // 1 to 4 threads to a candidate, who go through the others four at a time (filled up with ones that count for nothing)
+    const int C4 = (C + 3) / 4, fan = C <= PICK_THREADS / 4 ? 2 : (C <= PICK_THREADS / 2 ? 1 : 0), mine = tid >> fan, share = tid & ((1 << fan) - 1);
+    const bool on = mine < C;
+    auto count = [&](const uint32_t* list, auto f) {
+        int n = 0;
+        if (on)
+#pragma unroll 4
+            for (int k = share; k < C4; k += 1 << fan) {
+                const uint4 v = reinterpret_cast<const uint4*>(list)[k];
+                n += (int)f(v.x) + (int)f(v.y) + (int)f(v.z) + (int)f(v.w);
+            }
+        if (fan > 0) n += __shfl_xor_sync(0xffffffffu, n, 1);
+        if (fan > 1) n += __shfl_xor_sync(0xffffffffu, n, 2);
+        return n;
     };
     if (tid < 4 * C4 - C) {
-        s_lower[C + tid] = s_upper[C + tid] = s_key[C + tid] = 0;
+        s_lower[C + tid] = s_upper[C + tid] = 0;
         s_cand[C + tid] = ~0u;
     }
     __syncthreads();
+    const uint32_t me = on ? s_cand[mine] : ~0u;
+    bool in = on;
     if (C > want) {
-        // a key for each: the largest for one that is in, 0 for one that is out, else the order of its exact score
-        if (tid < C) {
-            const uint32_t lo = s_lower[tid], hi = s_upper[tid];
-            int better = 0, rivals = 0;
-            each4(s_lower, [&](uint32_t u, int) { better += u > hi; });
-            each4(s_upper, [&](uint32_t u, int) { rivals += u >= lo; });
-            const bool out_of_it = better >= want, in_it = rivals <= want;
-            s_key[tid] = !out_of_it && in_it ? ~0u : 0u;
-            if (!out_of_it && !in_it) s_open[atomicAdd(&s_opened, 1)] = tid;
-        }
+        const uint32_t lo = on ? s_lower[mine] : 0, hi = on ? s_upper[mine] : 0;
+        const int better = count(s_lower, [&](uint32_t u) { return u > hi; }), rivals = count(s_upper, [&](uint32_t u) { return u >= lo; });
+        in = on && rivals <= want;
+        const bool open = on && better < want && rivals > want;
+        if (open && share == 0) s_open[atomicAdd(&s_opened, 1)] = mine;
+        const int free = want - __syncthreads_count(in && share == 0), opened = s_opened;
+        // those that stay open: the largest of the heads' exact scores
+        if (tid < opened) s_key[s_open[tid]] = 0;
         __syncthreads();
-        // the largest of the heads' scores
 #pragma unroll 1
-        for (int x = warp; x < s_opened * a.G; x += PICK_WARPS) {
-            const int y = small_div(x, a.per_G), c = s_open[y];
-            const float score = exact_score<DT, D>(a, b, t, h, x - y * a.G, a.first + (int)s_cand[c]);
+        for (int y = warp; y < opened * a.G; y += PICK_WARPS) {
+            const int k = small_div(y, a.per_G), c = s_open[k];
+            const float score = exact_score<DT, D>(a, b, t, h, y - k * a.G, a.first + (int)s_cand[c]);
             if (lane == 0) atomicMax(&s_key[c], order_of(score));
         }
         __syncthreads();
-        bool in = false;
-        if (tid < C) {
-            const uint32_t key = s_key[tid], me = s_cand[tid];
+        if (open) {
+            const uint32_t key = s_key[mine];
             int rank = 0;
-            each4(s_key, [&](uint32_t u, int k) { rank += u > key || (u == key && s_cand[k] < me); });
-            in = rank < want;
+#pragma unroll 1
+            for (int k = 0; k < opened; ++k) {
+                const int c = s_open[k];
+                rank += s_key[c] > key || (s_key[c] == key && s_cand[c] < me);
+            }
+            in = rank < free;
         }
         __syncthreads();
-        if (tid < C && !in) s_cand[tid] = ~0u;
+        if (on && !in && share == 0) s_cand[mine] = ~0u;
         __syncthreads();
     }
-    if (tid < C && s_cand[tid] != ~0u) {
-        const uint32_t me = s_cand[tid];
-        int place = 0;
-        each4(s_cand, [&](uint32_t u, int) { place += u < me; });
-        out[a.first + place] = a.first + (int)me;
-    }
+    const int place = count(s_cand, [&](uint32_t u) { return u < me; });
+    if (in && share == 0) out[a.first + place] = a.first + (int)me;
 }
 
 }  // namespace retopk_cache
