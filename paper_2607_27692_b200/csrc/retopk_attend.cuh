@@ -42,7 +42,7 @@ struct Entry {
 };
 struct AttendHeader { int units; };
 
-// Keys and values as [rows of all pages, d] for copies of `box_rows` rows (which lie in one page), of 8 and of single rows.
+// Keys and values as [rows of all pages, d] for copies of a box of rows (which lie in one page), of 8 and of single rows.
 struct AttendMaps { CUtensorMap k, v, v_eight, v_row; };
 
 struct AttendArgs {
@@ -63,7 +63,7 @@ struct AttendArgs {
     Entry* entry;
     int32_t *group_of, *flags;  // group of a sequence or -1; CTAs that gave up
     float *shared_parts, *own_parts;
-    int box_rows, total_rows;
+    int box_shift, total_rows;  // rows of a copy: 1 << box_shift
     bool planned;               // by plan_kernel
     // join_kernel: float4s of a row that a CTA has, threads to each, and 1 / rows, 1 / (rows * wide), 1 / G
     int join_wide, join_splits;
@@ -520,33 +520,25 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             // ---- loads: keys by one warp, values by the other ------------------------------------
             const bool keys = warp == ATT_LOAD_WARP;
             const CUtensorMap* map = keys ? &maps.k : &maps.v;
-            const int box = a.box_rows;
-            // Four rows of a tile to a lane.  Their numbers: of the first, the others follow where boxes have
-            // four rows or more, else one by one; and which of them count, as bits.
-            struct Rows { int row[4]; uint32_t valid; };
-            auto look_up = [&](const Piece& p, int t) -> Rows {
-                Rows r;
-                r.valid = 0;
-#pragma unroll 1
-                for (int e = 0; e < (box >= 4 ? 1 : 4); ++e) {
-                    const int at = t * ATT_TILE + lane * 4 + e;          // place among the keys
-                    int pos = at;                        // position in the sequence
-                    if (a.blocks && at < p.hi) {
-                        const int j = a.blocks[((long long)p.token * a.pg.H_kv + p.h) * a.keep + (at >> a.block_shift)];
-                        pos = j < 0 || j > (p.seen - 1) >> a.block_shift ? -1 : (j << a.block_shift) + (at & (a.block - 1));
-                    }
-                    // (rows of a box share the page: the first of them may lie before lo)
-                    const long long found = at >= p.hi || at + (box >= 4 ? 3 : 0) < p.lo ? -1 : cache_row(a.pg, p.b, pos);
-                    const int row = found < 0 ? -1 : (int)(found + (long long)p.h * a.pg.page_size);
-                    if (e == 0) r.row[0] = row;
-                    else if (e == 1) r.row[1] = row;
-                    else if (e == 2) r.row[2] = row;
-                    else r.row[3] = row;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if ((x == e || box >= 4) && row >= 0 && at + x - e >= p.lo && at + x - e < p.hi && pos + x - e < p.seen) r.valid |= 1u << x;
+            const int box_shift = a.box_shift, box = 1 << box_shift;
+            // A box of a copy's rows to a lane, of as many tiles as that makes: at 16 rows of 4 tiles.  Its first row or -1,
+            // and which of its rows count.
+            struct Box { int row, from, to; };
+            auto look_up = [&](const Piece& p, int at) -> Box {          // at: its place among the keys
+                const int lo = p.lo, hi = p.hi, seen = p.seen;
+                int pos = at;                            // position in the sequence
+                if (a.blocks && at < hi) {
+                    const int j = a.blocks[((long long)p.token * a.pg.H_kv + p.h) * a.keep + (at >> a.block_shift)];
+                    pos = j < 0 || j > (seen - 1) >> a.block_shift ? -1 : (j << a.block_shift) + (at & (a.block - 1));
                 }
-                return r;
+                const long long found = at >= hi || at + box <= lo ? -1 : cache_row(a.pg, p.b, pos);
+                Box x;
+                x.row = found < 0 ? -1 : (int)(found + (long long)p.h * a.pg.page_size);
+                x.from = lo > at ? lo - at : 0;
+                x.to = hi - at < seen - pos ? hi - at : seen - pos;
+                x.to = x.to < box ? x.to : box;
+                if (x.row < 0 || x.to <= x.from) x.from = x.to = 0;
+                return x;
             };
             auto copy = [&](const CUtensorMap* m, uint32_t dst, int row, uint32_t bar) {
 #pragma unroll
@@ -554,55 +546,72 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                                  ::"r"(dst + c * (ATT_TILE * 128)), "l"(m), "r"(c * 64), "r"(row), "r"(bar) : "memory");
             };
+            // the copies of a box; of values that do not count none but zeros
+            auto fetch = [&](const Box& x, uint32_t dst, uint32_t bar) {
+                if (x.to == 0 || keys || x.to - x.from == box) {
+                    copy(map, dst, x.to == 0 ? a.total_rows : x.row, bar);
+                    return;
+                }
+                const int step = box < 8 ? box : 8;
+#pragma unroll 1
+                for (int r = 0; r < box; r += step) {
+                    const bool none = x.to <= r || x.from >= r + step, all = x.from <= r && x.to >= r + step;
+                    if (step == 8 && (none || all)) {
+                        copy(&maps.v_eight, dst + r * 128, all ? x.row + r : a.total_rows, bar);
+                    } else {
+#pragma unroll 1
+                        for (int e = r; e < r + step; ++e) copy(&maps.v_row, dst + e * 128, e >= x.from && e < x.to ? x.row + e : a.total_rows, bar);
+                    }
+                }
+            };
+            const int boxes = ATT_TILE >> box_shift, tile_shift = 7 - box_shift;         // of a tile
+            const int ahead = boxes <= 32 ? 32 >> tile_shift : 1;        // tiles that are looked up at once
+            Box next;
+            if (boxes <= 32) next = look_up(sm.piece[0], sm.piece[0].tile0 * ATT_TILE + (lane << box_shift));
+#pragma unroll 1
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
-                Rows next;
+                Box mine;
+                int at = ahead;                          // of the tiles looked up last
 #pragma unroll 1
-                for (int t = -1; t < n && ok; ++t) {     // (the numbers of a tile's rows are looked up while the one before is waited for)
-                    const Rows r = next;
-                    if (t + 1 < n) next = look_up(p, p.tile0 + t + 1);
-                    if (t < 0) continue;
+                for (int t = 0; t < n && ok; ++t, ++at) {
+                    if (at == ahead) {                   // (those after them are looked up meanwhile, of the next piece too)
+                        at = 0;
+                        mine = next;
+                        if (boxes <= 32) {
+                            const bool more = t + ahead < n;
+                            if (more || i + 1 < pieces) {
+                                const Piece& c = sm.piece[more ? i : i + 1];
+                                next = look_up(c, (c.tile0 + (more ? t + ahead : 0)) * ATT_TILE + (lane << box_shift));
+                            }
+                        }
+                    }
                     const uint32_t load = loads + (keys ? k_load(t) : v_load(t, n)), slot = load % Smem::SLOTS, turn = load / Smem::SLOTS;
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.empty[slot]), (turn & 1) ^ 1, gave_up));
                     if (!ok) break;
-                    const uint32_t bar = smem_of(&sm.full[slot]), dst = smem_of(sm.ring[slot]) + lane * (4 * 128);
+                    const uint32_t bar = smem_of(&sm.full[slot]), dst = smem_of(sm.ring[slot]);
                     if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(Smem::TILE_BYTES) : "memory");
                     __syncwarp();
-                    if (box >= 4) {
-                        // whether all rows of the box count, and whether any does; its first lane copies it
-                        const int lanes = box / 4, leader = lane & -lanes;
-                        const uint32_t in_box = (lanes == 32 ? ~0u : (1u << lanes) - 1) << leader;
-                        const uint32_t any = __ballot_sync(0xffffffffu, r.valid != 0) & in_box, full = __ballot_sync(0xffffffffu, r.valid == 15u) & in_box;
-                        // (the box's first row, from a lane whose rows count)
-                        const int from = any ? __ffs(any) - 1 : leader, row = __shfl_sync(0xffffffffu, r.row[0], from) - (from - leader) * 4;
-                        const uint32_t pair = r.valid | __shfl_xor_sync(0xffffffffu, r.valid, 1) << 4;        // of 8 rows
-                        if (keys || any == 0 || full == in_box) {
-                            if (lane == leader) copy(map, dst, any ? row : a.total_rows, bar);
-                        } else if (box >= 8 && (pair == 0 || pair == 255u)) {
-                            if (!(lane & 1)) copy(&maps.v_eight, dst, pair ? r.row[0] : a.total_rows, bar);
-                        } else {
-#pragma unroll 1
-                            for (int e = 0; e < 4; ++e) copy(&maps.v_row, dst + e * 128, r.valid >> e & 1 ? r.row[0] + e : a.total_rows, bar);
-                        }
-                    } else {
+                    uint32_t valid = 0;                  // of rows 4 * lane on
+                    if (boxes <= 32) {
+                        if (lane >> tile_shift == at) fetch(mine, dst + (lane << box_shift) * 128 - at * (ATT_TILE * 128), bar);
+                        const int range = __shfl_sync(0xffffffffu, mine.from | mine.to << 16, (at << tile_shift) + (lane * 4 >> box_shift));
+                        const int first = lane * 4 & (box - 1), from = (range & 0xffff) - first, to = (range >> 16) - first;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) valid |= e >= from && e < to ? 1u << e : 0u;
+                    } else {                             // boxes of one or two rows
 #pragma unroll 1
                         for (int e = 0; e < 4; e += box) {
-                            const uint32_t mine = r.valid >> e & ((1u << box) - 1);
-                            // of the box's first row, and of its second (that of another box of one row does not matter)
-                            const int row0 = e == 0 ? r.row[0] : (e == 1 ? r.row[1] : (e == 2 ? r.row[2] : r.row[3])), row1 = e == 0 ? r.row[1] : r.row[3];
-                            if (keys || mine == 0 || mine == (1u << box) - 1) {
-                                copy(map, dst + e * 128, mine == 0 ? a.total_rows : (mine & 1 ? row0 : row1 - 1), bar);
-                            } else {
-                                copy(&maps.v_row, dst + e * 128, mine & 1 ? row0 : a.total_rows, bar);
-                                copy(&maps.v_row, dst + (e + 1) * 128, mine & 2 ? row1 : a.total_rows, bar);
-                            }
+                            const Box x = look_up(p, (p.tile0 + t) * ATT_TILE + lane * 4 + e);
+                            fetch(x, dst + (lane * 4 + e) * 128, bar);
+                            valid |= ((1u << x.to) - (1u << x.from)) << e;
                         }
                     }
                     if (lane == 0) sm.issued[slot] = load;
                     if (keys) {
                         // The mask.  That of 8 tiles back is no longer read: its softmax was over before this slot came free.
-                        uint32_t m = r.valid << (lane % 8 * 4);
+                        uint32_t m = valid << (lane % 8 * 4);
                         m |= __shfl_xor_sync(0xffffffffu, m, 1);
                         m |= __shfl_xor_sync(0xffffffffu, m, 2);
                         m |= __shfl_xor_sync(0xffffffffu, m, 4);

@@ -142,7 +142,7 @@ int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, i
         !encode_rows(dev.encode, &p.maps.v_eight, pages, pages->v, rows_in_all, 8) ||
         !encode_rows(dev.encode, &p.maps.v_row, pages, pages->v, rows_in_all, 1))
         return RETOPK_ECUDA;
-    a.box_rows = box;
+    a.box_shift = __builtin_ctz((unsigned)box);
     a.total_rows = (int)rows_in_all;
     char* ws = static_cast<char*>(workspace);
     a.head = reinterpret_cast<AttendHeader*>(ws);
