@@ -94,6 +94,17 @@ struct Shares {
     __device__ __forceinline__ int begin(int c) const { return c < n ? whole * c + rest * c / n : units; }
 };
 
+// With few query rows, copies of them fill the 128 of a stream: each copy has a share of a tile's keys to itself,
+// so that four warps have the work of one.
+__host__ __device__ constexpr int copies_of(int rows) { return rows <= ATT_TILE / 4 ? 4 : (rows <= ATT_TILE / 2 ? 2 : 1); }
+// Whether the sums of a part's copies become one before they are written.  That takes 1 to 2 us at the end of a piece; in
+// join_kernel it saves a half or three quarters of the places, in all parts of the line, that the threads which share a row go
+// through.  Done where each of them had 6 or more.  (Group of 8 sequences, 18 parts to a line: 47.9 to 43.5 us; blocks of 4
+// sequences, 5 parts to a line: 38.2 us, 41.7 with it.)
+__device__ __forceinline__ bool merges_copies(const AttendArgs& a, int line_units, int rows, int units) {
+    const int copies = copies_of(rows);
+    return copies > 1 && (long long)line_units * (units / 2 < a.grid ? units / 2 : a.grid) * (2 * copies) >= 6ll * a.join_splits * units;
+}
 // The CTA whose share holds unit u: the last c with floor(units * c / n) <= u.
 __device__ __forceinline__ int share_of(int u, int units, int grid) {
     const int n = units / 2 < grid ? units / 2 : grid;
@@ -336,10 +347,6 @@ constexpr int ATT_WARPS = ATT_MMA_WARP + 2, ATT_THREADS = ATT_WARPS * 32;
 constexpr int ATT_PIECES = 32;           // pieces that a CTA lists at once
 constexpr int ATT_MASKS = 8;             // tiles whose masks are kept
 
-// With few query rows, copies of them fill the 128 of a stream: each copy has a share of a tile's keys to itself,
-// so that four warps have the work of one.
-__host__ __device__ constexpr int copies_of(int rows) { return rows <= ATT_TILE / 4 ? 4 : (rows <= ATT_TILE / 2 ? 2 : 1); }
-
 // Loads of a piece of n tiles, j = 0 .. 2 n - 1: K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1).
 __device__ __forceinline__ int k_load(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int v_load(int t, int n) { return t == n - 1 ? 2 * n - 1 : 2 * t + 2; }
@@ -348,7 +355,7 @@ __device__ __forceinline__ int tile_of_load(int j, int n) { return j == 0 ? 0 : 
 struct Piece {
     int b, h, token, row0, rows, half_rows;
     int lo, hi, seen, tile0, tile1;
-    int pad;
+    int merge;                  // the copies' sums become one
     float* part;
 };
 template <int D> struct AttendSmem {
@@ -357,7 +364,7 @@ template <int D> struct AttendSmem {
     unsigned char q[2][TILE_BYTES];
     unsigned char ring[SLOTS][TILE_BYTES];
     uint32_t mask[ATT_MASKS][4];
-    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2][2], p_ready[2][2], o_ready[2][2], drained[2];      // [stream][half of a tile]
+    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2][2], p_ready[2][2], o_ready[2][2], merged[2], drained[2];         // [stream][half of a tile]
     Piece piece[ATT_PIECES];
     int warp_sum[ATT_WARPS];
     uint32_t issued[SLOTS];     // last load into a slot
@@ -399,7 +406,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 bar_init(smem_of(&sm.o_ready[i][h]), 1);
             }
         }
-        for (int i = 0; i < 2; ++i) bar_init(smem_of(&sm.drained[i]), 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_of(&sm.drained[i]), 1);
+            bar_init(smem_of(&sm.merged[i]), 4);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (tid == 32) {
@@ -415,7 +425,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 
     // what the roles keep from piece to piece
     uint32_t loads = 0, tiles_done = 0;                  // loads issued (or consumed), tiles behind
-    uint32_t turns = 0, begun = 0;                       // of a stream: tiles behind, pieces begun
+    uint32_t turns = 0, begun = 0, merges = 0;           // of a stream: tiles behind, pieces begun, times its warps waited for each other
     bool ok = true;
 
     for (int batch = 0;; ++batch) {
@@ -495,6 +505,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         p.lo = e.lo;
                         p.hi = e.hi;
                         p.seen = e.seen;
+                        p.merge = merges_copies(a, e.tiles << shift, p.rows, units);
                         p.tile0 = e.tile0 + t0;
                         p.tile1 = e.tile0 + end;
                         const long long slot = (long long)e.item + (long long)line * a.max_chunks + chunk + cta;
@@ -766,7 +777,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 #pragma unroll 1
                 for (int k = 0; k < turn_count && ok; ++k) {
                     const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
-                    const bool ahead = k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
+                    const bool ahead = !p.merge && k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
                     if (__builtin_expect(!here, 0)) {
                         fetch_q(p);
                         give_q(p);
@@ -874,13 +885,15 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 }
                 // ---- the sums of this piece ------------------------------------------------------
                 float* part = p.part + s * half_floats(p.half_rows, D);
-                const int at = copy * (p.half_rows / copies) + row % (ATT_TILE / copies);
-                if (live) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(ref, l);
+                const int at = p.merge ? row % (ATT_TILE / copies) : copy * (p.half_rows / copies) + row % (ATT_TILE / copies);
                 if (ok && turn_count > 0) {
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][0]), (turns - 1) & 1, gave_up) &&
                                                      bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up));
-                    if (ok && warp_live) {
-                        tc_after_sync();
+                    tc_after_sync();
+                }
+                if (!p.merge || turn_count == 0) {
+                    if (live && (!p.merge || copy == 0)) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(ref, l);
+                    if (ok && turn_count > 0 && warp_live) {
 #pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
                             uint32_t x[32];
@@ -893,8 +906,62 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             }
                         }
                     }
-                    tc_before_sync();
+                } else {
+                    // The copies' sums become one, in the place of the queries, which have been read: references first, then
+                    // half of the channels at a time.  A copy adds up a share of the channels.  (Written out as they are, they
+                    // would be 2 or 4 times as much to write here and to read in join_kernel.)
+                    auto meet = [&]() {                  // the warps of the stream
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_of(&sm.merged[s]));
+                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.merged[s]), merges & 1, gave_up));
+                        ++merges;
+                    };
+                    constexpr int F4 = D / 8;            // float4s of half a row
+                    float4* const sums = reinterpret_cast<float4*>(sm.q[s]);
+                    float2* const refs = reinterpret_cast<float2*>(sm.q[s]);
+                    if (ok) refs[row] = make_float2(ref, l);
+                    meet();
+                    float top = ATT_NONE, total = 0.f, e[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        e[c] = c < copies ? refs[at + c * (ATT_TILE / copies)].x : ATT_NONE;
+                        top = fmaxf(top, e[c]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        e[c] = e[c] == ATT_NONE ? 0.f : exp2_approx(e[c] - top);
+                        if (c < copies) total = fmaf(refs[at + c * (ATT_TILE / copies)].y, e[c], total);
+                    }
+                    if (ok && live && copy == 0) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(top, total);
+                    meet();
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 2; c += 32) {
+                            uint32_t x[32];
+                            tc_ld32(O + half * (D / 2) + c, x);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4)
+                                *reinterpret_cast<uint4*>(&sums[row * F4 + (((c + j) / 4) ^ (row & 7))]) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                        }
+                        meet();
+                        if (!ok) break;
+#pragma unroll 1
+                        for (int c4 = copy * (F4 / copies); c4 < (copy + 1) * (F4 / copies); ++c4) {
+                            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                if (c >= copies) break;
+                                const float4 v = sums[(at + c * (ATT_TILE / copies)) * F4 + (c4 ^ (row & 7))];
+                                y = make_float4(fmaf(v.x, e[c], y.x), fmaf(v.y, e[c], y.y), fmaf(v.z, e[c], y.z), fmaf(v.w, e[c], y.w));
+                            }
+                            if (live) *reinterpret_cast<float4*>(part + sums_at(at, half * F4 + c4, D)) = y;
+                        }
+                        meet();
+                    }
                 }
+                if (turn_count > 0) tc_before_sync();
                 tiles_done += n;
             }
         }
@@ -974,6 +1041,8 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
     const bool shared = g >= 0 && own->hi >= group->hi && group->tiles > 0;
     const int shared_row = shared ? (token0 - group->token) * a.G : 0, m0 = shared_row / (2 * ATT_TILE), group_rows = shared ? group->rows : 0;
     const int group_chunks = shared ? group->chunks : 0, chunks = group_chunks > own->chunks ? group_chunks : own->chunks;
+    const int group_units = shared ? group->tiles << tile_shift(group->rows) : 0;
+    const bool own_merge = merges_copies(a, own->tiles << tile_shift(rows), rows, units);
     bool failed = false;
     const int work = rows * a.join_wide, splits = a.join_splits;
 #pragma unroll 1
@@ -1008,16 +1077,16 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                 // Row `row` of a row tile: with more than 128 rows in one half of each part, with fewer in both, in
                 // `copies` places.  Places of the group's line, then of the own one, then the late keys.
                 const int row = shared_row + r - m0 * (2 * ATT_TILE), m = row / (2 * ATT_TILE), tile_rows = group_rows - (m0 + m) * (2 * ATT_TILE);
-                const bool g_both = tile_rows > ATT_TILE, o_both = rows > ATT_TILE;
-                const int g_copies = copies_of(tile_rows) >> 1, o_copies = copies_of(rows) >> 1;             // as shifts: 0, 1, 2
-                const int g_shift = g_both ? 0 : g_copies + 1, o_shift = o_both ? 0 : o_copies + 1;
+                const int g_copies = merges_copies(a, group_units, tile_rows, units) ? 0 : copies_of(tile_rows) >> 1;       // as shifts: 0, 1, 2
+                const int o_copies = own_merge ? 0 : copies_of(rows) >> 1;
+                const int g_shift = tile_rows > ATT_TILE ? 0 : g_copies + 1, o_shift = rows > ATT_TILE ? 0 : o_copies + 1;
                 const int n_group = s_line[m].count << g_shift, n_own = n_group + (s_line[2].count << o_shift);
                 const int sees = chunk == 0 && late > 0 ? first_seen + small_div(r, a.per_G) : 0, all = n_own + (sees < late ? (sees > 0 ? sees : 0) : late);
                 const float *g_part = s_line[m].part, *o_part = s_line[2].part;
                 // (a float2 of the row's reference and sum, and its sums)
                 const int g_row = row % (2 * ATT_TILE) % ATT_TILE, o_row = r % ATT_TILE;
                 const int g_half = half_floats(ATT_TILE, D), o_half = half_floats(a.own_rows, D);
-                const int g_skip = g_both ? row % (2 * ATT_TILE) / ATT_TILE : 0, o_skip = r / ATT_TILE;
+                const int g_skip = row % (2 * ATT_TILE) / ATT_TILE, o_skip = r / ATT_TILE;
 #pragma unroll 1
                 for (int k0 = split; k0 < all; k0 += splits * JOIN_DEEP) {
                     float2 ml[JOIN_DEEP];
@@ -1029,10 +1098,11 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                         o[d] = make_float4(0.f, 0.f, 0.f, 0.f);
                         if (k < n_own) {
                             const bool of_group = k < n_group;
-                            const int shift = of_group ? g_shift : o_shift, j = of_group ? k : k - n_group, place = j & ((1 << shift) - 1);
-                            const int half_rows = of_group ? ATT_TILE : a.own_rows;
-                            const int at = (of_group ? g_row : o_row) + (place >> 1) * (half_rows >> (of_group ? g_copies : o_copies));
-                            const float* half = (of_group ? g_part : o_part) + (long long)(2 * (j >> shift) + (of_group ? g_skip : o_skip) + (place & 1)) * (of_group ? g_half : o_half);
+                            const int shift = of_group ? g_shift : o_shift, j = of_group ? k : k - n_group;
+                            const int half_rows = of_group ? ATT_TILE : a.own_rows, place = j & ((1 << shift) - 1);
+                            const int at = of_group ? g_row + (place >> 1) * (ATT_TILE >> g_copies) : o_row + (place >> 1) * (a.own_rows >> o_copies);
+                            const int which = 2 * (j >> shift) + (of_group ? g_skip : o_skip) + (place & 1);
+                            const float* half = (of_group ? g_part : o_part) + (long long)which * (of_group ? g_half : o_half);
                             ml[d] = *reinterpret_cast<const float2*>(half + weight_at(at, half_rows, D));
                             o[d] = *reinterpret_cast<const float4*>(half + sums_at(at, c4, D));
                         } else if (k < all && s_late_row[k - n_own] >= 0) {

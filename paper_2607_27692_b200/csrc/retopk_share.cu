@@ -104,13 +104,9 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     return RETOPK_OK;
 }
 
-template <int DT, int D> int launch_attention(const AttendParams& p, int sequences, cudaStream_t s) {
-    int rc = p.a.planned ? launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, p.a) : RETOPK_OK;
-    if (rc != RETOPK_OK) return rc;
-    rc = launch(attend_kernel<DT, D>, dim3((unsigned)p.a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
-    if (rc != RETOPK_OK) return rc;
-    // As many CTAs to a head as run at once (4 on an SM); one where outputs take the place of queries that it reads.
-    AttendArgs a = p.a;
+template <int DT, int D> int launch_attention(AttendParams& p, int sequences, cudaStream_t s) {
+    AttendArgs& a = p.a;
+    // join_kernel has as many CTAs to a head as run at once (4 on an SM); one where outputs take the place of queries that it reads.
     const int rows = a.blocks ? a.G : a.T * a.G;
     int shares = 1;
     while ((a.T == 1 || a.out != a.q) && shares < JOIN_CTAS && 2ll * shares * a.pg.H_kv * sequences <= 4ll * a.grid) shares *= 2;
@@ -120,6 +116,10 @@ template <int DT, int D> int launch_attention(const AttendParams& p, int sequenc
     a.per_row = 1.f / rows;
     a.per_work = 1.f / (rows * a.join_wide);
     a.per_G = 1.f / a.G;
+    int rc = a.planned ? launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, a) : RETOPK_OK;
+    if (rc != RETOPK_OK) return rc;
+    rc = launch(attend_kernel<DT, D>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
+    if (rc != RETOPK_OK) return rc;
     return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, a);
 }
 
