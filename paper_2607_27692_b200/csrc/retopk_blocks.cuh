@@ -196,7 +196,7 @@ template <int DT, int D> __global__ void __launch_bounds__(SCORE_THREADS, 7) sco
                 const int t = small_div(c0 + k, a.per_G), head = c0 + k - t * a.G;
                 const float s = s_score[warp][k][lane], z = s_size[warp][k];
                 best = head == 0 ? s : fmaxf(best, s);
-                size = head == 0 ? z : (z != z ? z : fmaxf(size, z));
+                size = head == 0 || z != z ? z : (size != size ? size : fmaxf(size, z));          // (NaN stays)
                 if (head == a.G - 1) {
                     float off = size * most * 0x1p-17f + 1e-35f;
                     if (!(off < 1e37f) || !(fabsf(best) < 1e37f)) off = INFINITY;

@@ -231,6 +231,54 @@ def test_attend_long(paged):
     run_shared(paged, [2], [70000], [70100, 70001], 64, 2, 1, 128, 2, FP)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("members,G,T", [(1, 1, 1), (2, 4, 2), (8, 4, 1), (11, 3, 1), (16, 4, 1), (7, 2, 4), (17, 4, 1)])
+def test_attend_lines_in_many_parts(paged, dtype, d, members, G, T):
+    """A few query rows and one head: parts of a line in every CTA, whose copies of the rows become one."""
+    rng = random.Random(members)
+    run_shared(paged, [members], [9000], [9000 + T + rng.randint(0, 300) for _ in range(members)], 32, G, 1, d, T, dtype)
+
+
+@pytest.mark.parametrize("members,T,G", [(3, 2, 2), (2, 1, 16), (70, 1, 4)])
+def test_attend_more_tiles_than_a_chunk(paged, members, T, G):
+    """Lines of more than 1024 tiles of 128 keys: of a group and of one sequence alone."""
+    lens = [132000 + T + 40 * i for i in range(members)] + [140001]
+    run_shared(paged, [members, 1], [132000, 0], lens, 128, G, 1, 64, T, BF)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [2, 5, 16])
+def test_attend_draft_tokens_in_place(paged, d, T):
+    """Outputs in the place of the queries, which are read for the draft tokens' own keys until the last."""
+    lens = [330, T, 900, 301 + T, 0, T - 1]
+    k, v, table, cu, sh = sref.grouped_cache([4, 2], [300, 0], lens, 16, 3, d, BF)
+    cache = paged.KVPages.wrap(k, v)
+    q = randn(4, 6, T, 12, d)
+    results = []
+    for _ in range(5):
+        x = q.clone()
+        assert cache.attend_shared(x, ints(lens), table, cu, sh, out=x) is x
+        sref.check_attention(x, None, q, k, v, table, lens, 16, d ** -0.5)
+        results.append(x)
+    assert all(torch.equal(x, results[0]) for x in results)
+
+
+def test_attend_repeats_itself(paged):
+    """The same call gives the same bits, on a busy device too."""
+    lens = [5000 + 37 * i for i in range(20)]
+    k, v, table, cu, sh = sref.grouped_cache([20], [4900], lens, 16, 2, 128, BF)
+    cache = paged.KVPages.wrap(k, v)
+    q = randn(4, 20, 1, 8, 128)
+    want = cache.attend_shared(q, ints(lens), table, cu, sh)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        with torch.cuda.stream(other):
+            cache.k.sum(dtype=torch.float32)
+        assert torch.equal(cache.attend_shared(q, ints(lens), table, cu, sh), want)
+    torch.cuda.synchronize()
+
+
 def test_attend_idle_and_short_members(paged):
     """Empty sequences, lengths that the table cannot hold, members that are shorter than the shared rows."""
     k, v, table, cu, sh = sref.grouped_cache([4, 3], [64, 80], [90, 64, 130, 100, 200, 81, 80], 16, 2, 64, BF)
@@ -510,6 +558,42 @@ def test_select_many_blocks(paged):
     out = index.attend(q, ints([n]), blocks)
     picks = [[[[x for x in blocks[0, 0, 0].tolist()]]]]
     sref.check_attention(out, None, q, k, cache.v, None, [n], k.shape[2], 64 ** -0.5, picks, 16)
+
+
+@pytest.mark.parametrize("dtype,key,query", [(FP, 2.0 ** -20, 1.0), (FP, 2.0 ** -23, 2.0 ** -20), (BF, 2.0 ** -130, 1.0), (BF, 2.0 ** -100, 2.0 ** -30),
+                                             (FP, 2.0 ** 12, 2.0 ** 12), (BF, 2.0 ** 100, 2.0 ** 20), (BF, 2.0 ** 120, 2.0 ** 120)])
+def test_select_small_and_large_numbers(paged, dtype, key, query):
+    """Subnormal numbers and products, sums near and beyond the largest: the order of the scores rounded to fp32 holds."""
+    lens = [16 * 300, 16 * 700 + 3]
+    cache, index, table = make_blocks(paged, lens, 32, 16, 2, 64, dtype)
+    cache.k.copy_((cache.k.float() * key).to(dtype))
+    index.update(ints(lens), table)
+    q = (randn(9, 2, 1, 6, 64).float() * query).to(dtype)
+    for keep in (20, 250):
+        blocks = index.select(q, ints(lens), table, keep=keep, first=1, last=2)
+        check_select(index, table, q, lens, blocks, keep, 1, 2, 32)
+
+
+def test_select_infinite_queries(paged):
+    """Infinities and NaN in a query: a score that is no number counts as the largest."""
+    lens = [16 * 60, 16 * 60]
+    cache, index, table = make_blocks(paged, lens, 32, 16, 2, 64, BF)
+    q = randn(9, 2, 1, 4, 64)
+    q[0, 0, 1, 5] = math.inf
+    q[0, 0, 2, 7] = -math.inf
+    q[1, 0, 0, 3] = math.nan
+    blocks = index.select(q, ints(lens), table, keep=9, first=1, last=2)
+    check_select(index, table, q, lens, blocks, 9, 1, 2, 32)
+
+
+def test_attend_many_selected_blocks(paged):
+    """One token whose blocks are in many parts."""
+    lens = [16 * 900 + 5]
+    cache, index, table = make_blocks(paged, lens, 64, 16, 1, 128, BF)
+    q = randn(9, 1, 1, 4, 128)
+    blocks = index.select(q, ints(lens), table, keep=700)
+    picks = check_select(index, table, q, lens, blocks, 700, 1, 2, 64)
+    sref.check_attention(index.attend(q, ints(lens), blocks, table), None, q, cache.k, cache.v, table, lens, 64, 128 ** -0.5, picks, 16)
 
 
 def test_attend_lists(paged):
