@@ -57,6 +57,7 @@ int launch_copy(CopyArgs& a, int64_t n, const int32_t* src, const int32_t* dst, 
     long long parts = (2 * ctas + n - 1) / n;
     parts = parts < 4 ? 4 : parts;
     a.parts = (int)(parts < most ? parts : most);
+    a.per_part = ~0ull / (unsigned)a.parts + 1;
     const long long lines = n < (ctas + a.parts - 1) / a.parts ? n : (ctas + a.parts - 1) / a.parts;
     return launch(copy_pages_kernel, dim3((unsigned)(lines * a.parts)), COPY_THREADS, 0, s, a);
 }

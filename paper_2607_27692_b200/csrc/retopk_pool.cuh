@@ -294,6 +294,7 @@ struct CopyArgs {
     long long n_pages;
     long long n;                // pairs
     int parts;                  // a pair is shared by this many CTAs
+    unsigned long long per_part;         // 2^64 / parts, rounded up
     const int32_t *src, *dst, *rows;
 };
 
@@ -317,20 +318,42 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_pages_kernel(const __grid_c
                 using P = decltype(piece);
                 // heads that are copied whole are one run
                 const long long run = (whole ? (long long)a.H * head : (long long)r * a.t[t].row_bytes) / (int)sizeof(P);
-                const long long all = whole ? run : run * a.H;
-                const long long lo = all * part / a.parts, hi = all * (part + 1) / a.parts;
-                for (long long at = lo + threadIdx.x; at < hi; at += COPY_THREADS * COPY_DEEP) {
-                    P x[COPY_DEEP];
-                    long long off[COPY_DEEP];
+                const long long all = whole ? run : run * a.H, share = a.parts > 1 ? (long long)__umul64hi(all, a.per_part) : all, more = all - share * a.parts;
+                const long long lo = share * part + (part < more ? part : more), hi = lo + share + (part < more);
+                if (whole) {
+                    for (long long at = lo + threadIdx.x; at < hi; at += COPY_THREADS * COPY_DEEP) {
+                        P x[COPY_DEEP];
 #pragma unroll
-                    for (int k = 0; k < COPY_DEEP; ++k) {
-                        const long long v = at + k * COPY_THREADS;
-                        off[k] = whole ? v * (int)sizeof(P) : (v / run) * head + (v % run) * (int)sizeof(P);
-                        if (v < hi) x[k] = *reinterpret_cast<const P*>(s + off[k]);
+                        for (int k = 0; k < COPY_DEEP; ++k)
+                            if (at + k * COPY_THREADS < hi) x[k] = reinterpret_cast<const P*>(s)[at + k * COPY_THREADS];
+#pragma unroll
+                        for (int k = 0; k < COPY_DEEP; ++k)
+                            if (at + k * COPY_THREADS < hi) reinterpret_cast<P*>(d)[at + k * COPY_THREADS] = x[k];
+                    }
+                    return;
+                }
+                // of a thread's pieces: the run (head), and the place in it, one after the other without further divisions
+                const long long skip = head - run * (int)sizeof(P);
+                const int step_run = run > COPY_THREADS ? 0 : COPY_THREADS / (int)run, step_at = COPY_THREADS - step_run * (int)(run > COPY_THREADS ? 0 : run);
+                long long at = lo + threadIdx.x, h = at / run, in_run = at - h * run;
+                while (at < hi) {
+                    P x[COPY_DEEP / 2];
+                    long long off[COPY_DEEP / 2];
+#pragma unroll
+                    for (int k = 0; k < COPY_DEEP / 2; ++k) {
+                        off[k] = at < hi ? at * (int)sizeof(P) + h * skip : -1;
+                        if (off[k] >= 0) x[k] = *reinterpret_cast<const P*>(s + off[k]);
+                        at += COPY_THREADS;
+                        h += step_run;
+                        in_run += step_at;
+                        if (in_run >= run) {
+                            in_run -= run;
+                            ++h;
+                        }
                     }
 #pragma unroll
-                    for (int k = 0; k < COPY_DEEP; ++k)
-                        if (at + k * COPY_THREADS < hi) *reinterpret_cast<P*>(d + off[k]) = x[k];
+                    for (int k = 0; k < COPY_DEEP / 2; ++k)
+                        if (off[k] >= 0) *reinterpret_cast<P*>(d + off[k]) = x[k];
                 }
             };
             if (whole || a.t[t].row_bytes % 16 == 0) move(uint4());
