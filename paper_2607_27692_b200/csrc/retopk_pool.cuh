@@ -30,27 +30,33 @@ constexpr int FORK_THREADS = 256;
 
 __device__ __forceinline__ long long pages_held(long long len, int page_size) { return len <= 0 ? 0 : (len + page_size - 1) / page_size; }
 
-// The lowest `want` free pages, ascending, into `list`; how many there are.  One CTA.
+// The lowest `want` free pages, ascending, into `list`; how many there are.  One CTA: a warp has 512 pages at a time, 32 of
+// them side by side, so that a CTA of 256 threads looks through 4096 with one wait for memory and one barrier.
 template <int THREADS> __device__ int lowest_free(const PoolArgs& a, int32_t* list, int want) {
-    constexpr int PER = 4;
-    int found = 0;
-    for (long long at = 0; at < a.n_pages && found < want; at += (long long)THREADS * PER) {
-        const long long p0 = at + (long long)threadIdx.x * PER;
-        bool free[PER];
-        int mine = 0, total;
+    constexpr int PER = 16, WARPS = THREADS / 32;
+    __shared__ int s_found[2][WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int found = 0, turn = 0;
+#pragma unroll 1
+    for (long long at = 0; at < a.n_pages && found < want; at += (long long)THREADS * PER, turn ^= 1) {
+        const long long p0 = at + warp * (32 * PER) + lane;
+        int refs[PER], mine = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            free[i] = p0 + i < a.n_pages && __ldcg(a.refs + p0 + i) <= 0;
-            mine += free[i];
+        for (int k = 0; k < PER; ++k) refs[k] = p0 + k * 32 < a.n_pages ? __ldcg(a.refs + p0 + k * 32) : 1;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) mine += __popc(__ballot_sync(0xffffffffu, refs[k] <= 0));
+        if (lane == 0) s_found[turn][warp] = mine;
+        __syncthreads();
+        const int n = lane < WARPS ? s_found[turn][lane] : 0;
+        int r = found + __reduce_add_sync(0xffffffffu, lane < warp ? n : 0);
+        found += __reduce_add_sync(0xffffffffu, n);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const uint32_t who = __ballot_sync(0xffffffffu, refs[k] <= 0);
+            const int place = r + __popc(who & ((1u << lane) - 1));
+            if (refs[k] <= 0 && place < want) list[place] = (int)(p0 + k * 32);
+            r += __popc(who);
         }
-        int r = found + scan_cta<THREADS>(mine, &total);
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (free[i]) {
-                if (r < want) list[r] = (int)(p0 + i);
-                ++r;
-            }
-        found += total;
     }
     __syncthreads();
     return found < want ? found : want;
