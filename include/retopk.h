@@ -542,9 +542,12 @@ int retopk_pages_copy(const retopk_pages_t* pages, int64_t n, const int32_t* src
  * max_pages * page_size.  Keys of pages out of range do not count.  Scores go through the formula as IEEE arithmetic takes them: NaN and
  * +inf make their row NaN, -inf is a weight of 0; what a token does not see has no influence.
  * Scores, sums and outputs are held in fp32; weights are rounded to the pages' type once for the
- * product with the values.  Results are bit-reproducible.
+ * product with the values.  Values that are not finite make the outputs of those who see them NaN or infinite.
+ * A scale of 0 counts as the smallest normal number.  Results are bit-reproducible; in place they may differ from others in
+ * the last bits.
  * out may be q where q is contiguous; other overlaps are EINVAL.  workspace as in retopk_q4_attention.
- * Limits: as retopk_q4_attention.
+ * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096, at most 2^20 keys of a sequence (max_pages * page_size) and
+ * 2^31 - 256 rows n_pages * H_kv * page_size; EUNSUPPORTED beyond.
  */
 /* Bytes, or a negative code; max_keys: rows that a sequence can have, max_pages * page_size (page_size without a table). */
 int64_t retopk_shared_attention_workspace(int B, int n_groups, int T, int H_q, int H_kv, int d, int64_t max_keys);

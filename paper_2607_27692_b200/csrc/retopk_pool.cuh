@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
     if (missing) atomicAdd(a.scratch + POOL_SHORT, missing);
 }
 
+// Bound by waiting, about ten times for memory one after the other: 4.6 us for 3 forks, 8 for 64 of up to 2048 pages.
 // One CTA for a fork copies the table row and counts the full pages, one more finds free pages meanwhile (full pages
 // are in use, so that the counts of free ones stay as they are); the CTA that is done last hands them out
 // for the partial pages, in the order of the forks.
@@ -305,7 +306,8 @@ struct CopyArgs {
 };
 
 // A pair's rows are one line of pieces of 16 bytes (4 for scales of a partial page), tensor by tensor and
-// head by head; `parts` CTAs take equal shares of it.  Bound: HBM.
+// head by head; `parts` CTAs take equal shares of it.  Bound by memory: 826 MB read and written by a compaction in
+// 130 us, 6.4 TB/s; of a few partial pages 3 us.  (Whole pages and partial ones in one loop, with a 64-bit division and remainder for each piece, took 136 and 5.3.)
 __global__ void __launch_bounds__(COPY_THREADS) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
     pdl_wait();
     const int part = blockIdx.x % a.parts;
