@@ -393,6 +393,7 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     if (N <= a.keep) {
 #pragma unroll 1
         for (int i = tid; i < a.keep; i += PICK_THREADS) out[i] = i < N ? i : -1;
+        if (a.scored) pdl_wait();                        // (no CTA ends before score_kernel has: what follows may rely on it)
         return;
     }
     const int want = a.keep - a.first - a.last, m = N - a.first - a.last;
@@ -400,11 +401,11 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     for (int i = tid; i < a.first; i += PICK_THREADS) out[i] = i;
 #pragma unroll 1
     for (int i = tid; i < a.last; i += PICK_THREADS) out[a.keep - a.last + i] = N - a.last + i;
-    if (want == 0) return;
 #pragma unroll
     for (int i = 0; i < BINS / PICK_THREADS; ++i) s_bin[i * PICK_THREADS + tid] = 0;
     if (tid == 0) s_count = s_opened = 0;
     if (a.scored) pdl_wait();
+    if (want == 0) return;
     float2* const at = a.scores + item * a.max_blocks + a.first;
     auto lower = [](float2 s) { return order_of(__fsub_rd(s.x, s.y)); };
     auto upper = [](float2 s) { return order_of(__fadd_ru(s.x, s.y)); };
