@@ -142,12 +142,11 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, const PlanInput& i
     if (a.n_groups > 0) {
         bool bad = false;
 #pragma unroll 1
-        for (int g = tid; g < a.n_groups; g += THREADS)
-            bad |= in.cu[g] < 0 || in.cu[g + 1] < in.cu[g] || in.cu[g + 1] > a.B || (g == 0 && in.cu[0] != 0) || (g == a.n_groups - 1 && in.cu[g + 1] != a.B);
-        groups = __syncthreads_or(bad) ? 0 : a.n_groups;
-#pragma unroll 1
-        for (int g = warp; g < groups; g += THREADS / 32) {
-            const int b0 = in.cu[g], b1 = in.cu[g + 1];
+        for (int g = warp; g < a.n_groups; g += THREADS / 32) {
+            int b0 = in.cu[g], b1 = in.cu[g + 1];
+            const bool wrong = (b0 < 0) | (b1 < b0) | (b1 > a.B) | ((g == 0) & (b0 != 0)) | ((g == a.n_groups - 1) & (b1 != a.B));
+            bad |= wrong;
+            if (wrong) b0 = b1 = 0;
             int owner = 0x7fffffff, least = 0x7fffffff, members = 0;
 #pragma unroll 1
             for (int b = b0 + lane; b < b1; b += 32) {
@@ -173,10 +172,12 @@ __device__ __forceinline__ int make_plan(const AttendArgs& a, const PlanInput& i
                 entry[g] = e;
             }
         }
-        if (groups == 0)
+        groups = __syncthreads_or(bad) ? 0 : a.n_groups;
+        if (groups == 0) {
 #pragma unroll 1
             for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
-        __syncthreads();
+            __syncthreads();
+        }
     } else if (!a.blocks) {
 #pragma unroll 1
         for (int b = tid; b < a.B; b += THREADS) group_of[b] = -1;
@@ -506,9 +507,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         const int chunk = t0 / ATT_CHUNK, end = (chunk + 1) * ATT_CHUNK < t1 ? (chunk + 1) * ATT_CHUNK : t1;
                         Piece p;
                         p.b = e.b;
-                        p.h = line % a.pg.H_kv;
+                        const int row_tile = line / a.pg.H_kv;
+                        p.h = line - row_tile * a.pg.H_kv;
                         p.token = e.token;
-                        p.row0 = line / a.pg.H_kv * (2 * ATT_TILE);
+                        p.row0 = row_tile * (2 * ATT_TILE);
                         p.rows = e.rows - p.row0 < 2 * ATT_TILE ? e.rows - p.row0 : 2 * ATT_TILE;
                         p.lo = e.lo;
                         p.hi = e.hi;
