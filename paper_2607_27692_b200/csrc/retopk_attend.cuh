@@ -31,6 +31,7 @@ __device__ __forceinline__ int keys_seen(const Pages& pg, int len, int T, int t)
 }
 
 constexpr int ATT_TILE = 128;            // keys of a tile, and query rows of a stream
+constexpr int ATT_FEW = 64;              // query rows up to which tiles are taken whole
 constexpr int ATT_CHUNK = 1024;          // tiles whose sums stay in the tensor core at most: it cuts additions off
 // What a CTA's work counts: a tile of up to 128 query rows 1 (two of them are at work at once), one of more rows 2, and the
 // beginning of a line 3.
@@ -71,6 +72,7 @@ struct AttendArgs {
     float *shared_parts, *own_parts;
     int box_shift, total_rows;  // rows of a copy: 1 << box_shift
     bool planned;               // by plan_kernel
+    bool few_rows;              // no line has more than ATT_FEW query rows
     // join_kernel: float4s of a row that a CTA has, threads to each, and 1 / rows, 1 / (rows * wide), 1 / G
     int join_wide, join_splits;
     float per_row, per_work, per_G;
@@ -383,12 +385,15 @@ template <int D> struct AttendSmem {
 // rows and every other tile, with more a stream has 128 of 256 rows and every tile.  While one is at its
 // softmax the tensor core works for the other.  One warp fetches keys, one values, by copies of as many rows as
 // lie in a page together, into a ring of 5 tiles of 32 KB at d = 128; for each stream one thread issues the products: S = Q K^T into
-// tensor memory, O += P V with P over the columns of S, half a tile of keys at a time, so that the other half is at its
-// softmax.  Rows of values that do not count (masked, pages out of range) are read from behind the last row, where a copy
+// tensor memory, O += P V with P over the columns of S.  With many rows half a tile of keys at a time, so that the other half
+// is at its softmax; WHOLE, for calls without a line of more than 64 rows (whose copies leave each warp 32 or 64 of a tile's keys): all
+// of it at once, with fewer waits.  (us, whole and halves: blocks of 4 sequences 37.3 and 39.4, of ragged ones 35.9 and 39.4, 4 short sequences
+// 15.5 and 16.9; with the maxima that it takes, 32 sequences of 128 rows in all would be 56 and 52, 64 of 256 rows 222 and 188.)
+// Rows of values that do not count (masked, pages out of range) are read from behind the last row, where a copy
 // finds zeros; a weight of 0 would not hide a NaN.
-// Weights are taken against a reference that need not be the maximum (as long as their sum stays below 2^14), so that most halves
-// need neither maxima nor a rescaling of O; they are rounded to 16 bits once, for the tensor core.
-template <int DT, int D>
+// Weights are taken against a reference that need not be the maximum (halves: as long as their sum stays below 2^14; WHOLE: each below
+// 2^8), so that most halves need neither maxima nor a rescaling of O; they are rounded to 16 bits once, for the tensor core.
+template <int DT, int D, bool WHOLE>
 __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_constant__ AttendParams params) {
     using Smem = AttendSmem<D>;
     const AttendArgs& a = params.a;
@@ -652,14 +657,14 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             __syncwarp();
         } else if (warp >= ATT_MMA_WARP) {
             // ---- products: a warp for each stream ------------------------------------------------
-            constexpr uint32_t QK = tc_shape<DT>(ATT_TILE / 2, false), PV = tc_shape<DT>(D, true);
+            constexpr uint32_t QK = tc_shape<DT>(WHOLE ? ATT_TILE : ATT_TILE / 2, false), PV = tc_shape<DT>(D, true);
             const uint32_t issue = elect_one();          // always the same lane
             const int s = warp - ATT_MMA_WARP;
             const uint32_t S = tmem + s * ATT_TILE, O = tmem + 2 * ATT_TILE + s * D, q = smem_of(sm.q[s]);
 #pragma unroll 1
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
-                const int n = __shfl_sync(0xffffffffu, p.tile1 - p.tile0, 0), step = __shfl_sync(0xffffffffu, p.rows > ATT_TILE ? 1 : 2, 0);
+                const int n = __shfl_sync(0xffffffffu, p.tile1 - p.tile0, 0), step = WHOLE ? 2 : __shfl_sync(0xffffffffu, p.rows > ATT_TILE ? 1 : 2, 0);
                 auto wait_full = [&](int j) { return bar_wait(smem_of(&sm.full[(loads + j) % Smem::SLOTS]), (loads + j) / Smem::SLOTS & 1, gave_up); };
                 auto tile_at = [&](int j) { return __shfl_sync(0xffffffffu, smem_of(sm.ring[(loads + j) % Smem::SLOTS]), 0); };
                 auto empty_at = [&](int j) { return smem_of(&sm.empty[(loads + j) % Smem::SLOTS]); };
@@ -675,49 +680,87 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             }
                     return true;
                 };
-                auto score = [&](int t, int h) {         // S = Q K^T of half a tile
-                    const uint32_t k = tile_at(k_load(t)) + h * (ATT_TILE / 2 * 128);
-                    tc_after_sync();
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
-                        tc_mma_ss(S + h * (ATT_TILE / 2), tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0, issue);
-                    }
-                    tc_commit(smem_of(&sm.s_ready[s][h]), issue);
-                    if (h == 1) tc_commit(empty_at(k_load(t)), issue);
-                };
-                // weights that S takes the place of have been read
-                auto wait_o = [&](int h) { return turns == 0 || bar_wait(smem_of(&sm.o_ready[s][h]), (turns - 1) & 1, gave_up); };
                 const int first = step == 1 ? 0 : s;
-                if (first < n) {
-                    ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first));
-                    ++begun;
+                if constexpr (WHOLE) {
+                    auto score = [&](int t) {                // S = Q K^T
+                        const uint32_t k = tile_at(k_load(t));
+                        tc_after_sync();
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        ok = ok && wait_o(h);
-                        if (__all_sync(0xffffffffu, ok)) score(first, h);
+                        for (int x = 0; x < D / 16; ++x) {
+                            const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
+                            tc_mma_ss(S, tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0, issue);
+                        }
+                        tc_commit(smem_of(&sm.s_ready[s][0]), issue);
+                        tc_commit(empty_at(k_load(t)), issue);
+                    };
+                    if (first < n) {
+                        // (weights that S takes the place of have been read)
+                        ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first)) &&
+                             (turns == 0 || bar_wait(smem_of(&sm.o_ready[s][0]), (turns - 1) & 1, gave_up));
+                        ++begun;
+                        if (__all_sync(0xffffffffu, ok)) score(first);
                     }
-                }
-                for (int t = first; t < n && __all_sync(0xffffffffu, ok); t += step) {
-                    ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
-                    const uint32_t v = tile_at(v_load(t, n));
-                    const bool more = t + step < n;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.p_ready[s][h]), turns & 1, gave_up));
+                    for (int t = first; t < n && __all_sync(0xffffffffu, ok); t += step) {
+                        ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
+                        const uint32_t v = tile_at(v_load(t, n));
+                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.p_ready[s][0]), turns & 1, gave_up));
                         if (!ok) break;
                         tc_after_sync();
 #pragma unroll
-                        for (int x = 0; x < ATT_TILE / 32; ++x)                  // O += P V
-                            tc_mma_ts(O, S + h * (ATT_TILE / 2) + x * 8, tc_operand(v + (h * 4 + x) * 2048, ATT_TILE * 128), PV, x > 0 || h > 0 || t >= step, issue);
-                        tc_commit(smem_of(&sm.o_ready[s][h]), issue);
-                        if (h == 1) tc_commit(empty_at(v_load(t, n)), issue);
-                        if (more) {
-                            ok = __all_sync(0xffffffffu, (h == 1 || wait_full(k_load(t + step))) && bar_wait(smem_of(&sm.o_ready[s][h]), turns & 1, gave_up));
-                            if (ok) score(t + step, h);
+                        for (int x = 0; x < ATT_TILE / 16; ++x)              // O += P V
+                            tc_mma_ts(O, S + x * 8, tc_operand(v + x * 2048, ATT_TILE * 128), PV, x > 0 || t >= step, issue);
+                        tc_commit(smem_of(&sm.o_ready[s][0]), issue);
+                        tc_commit(empty_at(v_load(t, n)), issue);
+                        if (t + step < n) {
+                            ok = __all_sync(0xffffffffu, wait_full(k_load(t + step)) && bar_wait(smem_of(&sm.o_ready[s][0]), turns & 1, gave_up));
+                            if (ok) score(t + step);
+                        }
+                        ++turns;
+                    }
+                } else {
+                    auto score = [&](int t, int h) {         // S = Q K^T of half a tile
+                        const uint32_t k = tile_at(k_load(t)) + h * (ATT_TILE / 2 * 128);
+                        tc_after_sync();
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            const uint32_t off = (x >> 2) * (ATT_TILE * 128) + (x & 3) * 32;
+                            tc_mma_ss(S + h * (ATT_TILE / 2), tc_operand(q + off, 0), tc_operand(k + off, 0), QK, x > 0, issue);
+                        }
+                        tc_commit(smem_of(&sm.s_ready[s][h]), issue);
+                        if (h == 1) tc_commit(empty_at(k_load(t)), issue);
+                    };
+                    // weights that S takes the place of have been read
+                    auto wait_o = [&](int h) { return turns == 0 || bar_wait(smem_of(&sm.o_ready[s][h]), (turns - 1) & 1, gave_up); };
+                    if (first < n) {
+                        ok = see(k_load(first)) && bar_wait(smem_of(&sm.q_ready[s]), begun & 1, gave_up) && wait_full(k_load(first));
+                        ++begun;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            ok = ok && wait_o(h);
+                            if (__all_sync(0xffffffffu, ok)) score(first, h);
                         }
                     }
-                    ++turns;
+                    for (int t = first; t < n && __all_sync(0xffffffffu, ok); t += step) {
+                        ok = see(v_load(t, n) < k_load(t + step) ? v_load(t, n) : k_load(t + step)) && wait_full(v_load(t, n));
+                        const uint32_t v = tile_at(v_load(t, n));
+                        const bool more = t + step < n;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.p_ready[s][h]), turns & 1, gave_up));
+                            if (!ok) break;
+                            tc_after_sync();
+#pragma unroll
+                            for (int x = 0; x < ATT_TILE / 32; ++x)                  // O += P V
+                                tc_mma_ts(O, S + h * (ATT_TILE / 2) + x * 8, tc_operand(v + (h * 4 + x) * 2048, ATT_TILE * 128), PV, x > 0 || h > 0 || t >= step, issue);
+                            tc_commit(smem_of(&sm.o_ready[s][h]), issue);
+                            if (h == 1) tc_commit(empty_at(v_load(t, n)), issue);
+                            if (more) {
+                                ok = __all_sync(0xffffffffu, (h == 1 || wait_full(k_load(t + step))) && bar_wait(smem_of(&sm.o_ready[s][h]), turns & 1, gave_up));
+                                if (ok) score(t + step, h);
+                            }
+                        }
+                        ++turns;
+                    }
                 }
                 ok = ok && see(2 * n);
                 ok = __all_sync(0xffffffffu, ok);
@@ -738,7 +781,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             // (a scale of 0 as the smallest: 0 times the -inf of a hidden key is no number)
             const float scale = a.scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.scale_log2);
             // tiles of this stream in a piece
-            auto turns_of = [&](const Piece& p) { return p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
+            auto turns_of = [&](const Piece& p) { return !WHOLE && p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
             // this thread's query row in a piece, or -1; the copy that it belongs to
             auto row_of = [&](const Piece& p, int* copy) {
                 const int copies = copies_of(p.rows), stride = ATT_TILE / copies, r = row % stride + (p.rows > ATT_TILE ? s * ATT_TILE : 0);
@@ -774,7 +817,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
-                const bool both = p.rows > ATT_TILE;
+                const bool both = !WHOLE && p.rows > ATT_TILE;           // (WHOLE: there are no more than ATT_FEW)
                 const int turn_count = turns_of(p), copies = copies_of(p.rows);
                 int copy;
                 const int r = row_of(p, &copy);
@@ -794,98 +837,182 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         here = true;
                     }
                     ok = bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up);
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up));
+                    if constexpr (WHOLE) {
+                        ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][0]), turns & 1, gave_up));
                         if (!ok) break;
-                        if (__builtin_expect(ahead && h == 1, 0)) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
+                        if (__builtin_expect(ahead, 0)) fetch_q(sm.piece[i + 1]);        // the queries of this piece have been read
                         if (warp_live) {
                             tc_after_sync();
-                            const uint32_t Sh = S + h * (ATT_TILE / 2);
-                            uint32_t x[32], y[32];
-                            // this copy's columns: both 32s of the half, one, or none
-                            const bool first = 2 * h >= c0 && 2 * h < c1, second = 2 * h + 1 >= c0 && 2 * h + 1 < c1;
-                            uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
-                            if (!first) mx = 0;
-                            if (!second) my = 0;
-                            if (__builtin_expect(first | second, 1)) {
-                                if (__builtin_expect(first, 1)) tc_ld32(Sh, x);
-                                if (__builtin_expect(second, 1)) tc_ld32(Sh + 32, y);
-                                tc_wait_ld();
-                                auto hide = [&](uint32_t* v, uint32_t m) {       // keys that do not count: weight 0
-                                    if (__builtin_expect(m == ~0u, 1)) return;
+                            // this copy's columns, 32 or 64 of them
+                            const uint32_t* masks = sm.mask[tile % ATT_MASKS] + c0;
+                            const bool two = c1 - c0 > 1;
+                            uint32_t x[64];
+                            tc_ld32(S + c0 * 32, x);
+                            if (two) tc_ld32(S + c0 * 32 + 32, x + 32);
+                            const uint32_t m0 = masks[0], m1 = two ? masks[1] : 0, any = m0 | m1;
+                            tc_wait_ld();
+                            auto hide = [&](uint32_t* v, uint32_t m) {   // keys that do not count: weight 0
+                                if (__builtin_expect(m == ~0u, 1)) return;
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j)
-                                        if (!(m >> j & 1)) v[j] = 0xff800000u;
-                                };
-                                hide(x, mx);
-                                hide(y, my);
-                                uint32_t w[32];
-                                float total;
-                                auto weigh = [&]() {
-                                    const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
-                                    uint64_t sum = 0, more = 0;
+                                for (int j = 0; j < 32; ++j)
+                                    if (!(m >> j & 1)) v[j] = 0xff800000u;
+                            };
+                            hide(x, m0);
+                            hide(x + 32, m1);
+                            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                            auto larger = [&](const uint32_t* v) {
 #pragma unroll
-                                    for (int j = 0; j < 32; j += 2) {
-                                        const uint64_t u = fma2(pair_of(x[j], x[j + 1]), scale2, ref2), v = fma2(pair_of(y[j], y[j + 1]), scale2, ref2);
-                                        const float u0 = exp2_approx(low_of(u)), u1 = exp2_approx(high_of(u));
-                                        const float v0 = exp2_approx(low_of(v)), v1 = exp2_approx(high_of(v));
-                                        sum = add2(sum, pair_of(u0, u1));
-                                        more = add2(more, pair_of(v0, v1));
-                                        w[j / 2] = pack2<DT>(u0, u1);
-                                        w[16 + j / 2] = pack2<DT>(v0, v1);
-                                    }
-                                    sum = add2(sum, more);
-                                    total = low_of(sum) + high_of(sum);
-                                };
-                                // Weights come first, against the reference that is there: it need not be the maximum, as long
-                                // as no sum leaves 2^14 (what fp16 weights can hold).  Where one does, or there was none
-                                // before, the reference becomes the maximum, and sums so far and weights follow.
-                                weigh();
-                                const bool low = live && (!(total <= 16384.f) || (ref == ATT_NONE && (mx | my)));
-                                if (__builtin_expect(__any_sync(0xffffffffu, low), 0)) {
-                                    float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                                for (int j = 0; j < 32; j += 8)
 #pragma unroll
-                                    for (int j = 0; j < 32; j += 2) {
-                                        most[j & 2] = fmaxf(most[j & 2], fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 1])));
-                                        most[(j & 2) + 1] = fmaxf(most[(j & 2) + 1], fmaxf(__uint_as_float(y[j]), __uint_as_float(y[j + 1])));
-                                    }
-                                    const float top = fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW);
-                                    float f = 1.f;
-                                    if (low && top > ref) {
-                                        f = exp2_approx(ref - top);
-                                        ref = top;
-                                        l *= f;
-                                    }
-                                    if (k > 0 || h > 0) {
-                                        // (the product of the half before may be under way)
-                                        ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][1 - h]), (h == 0 ? turns - 1 : turns) & 1, gave_up));
-                                        if (!ok) break;
-                                        tc_after_sync();
+                                    for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], fmaxf(__uint_as_float(v[j + e]), __uint_as_float(v[j + e + 4])));
+                            };
+                            larger(x);
+                            if (two) larger(x + 32);
+                            // The reference need not be the maximum, as long as weights stay below 2^8: where the maximum is 8 above it
+                            // (in powers of two), it becomes that, and sums so far follow.
+                            const float top = any ? fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW) : ATT_NONE;
+                            const bool low = live && (top > ref + 8.f || (ref == ATT_NONE && any));
+                            if (__builtin_expect(__any_sync(0xffffffffu, low), 0)) {
+                                const float f = low ? exp2_approx(ref - top) : 1.f;
+                                if (low) ref = top;
+                                l *= f;
+                                if (k > 0) {             // (scores are there: the product of the tile before is over)
 #pragma unroll 1
-                                        for (int c = 0; c < D; c += 16) {
-                                            uint32_t o[16];
-                                            tc_ld16(O + c, o);
-                                            tc_wait_ld();
+                                    for (int c = 0; c < D; c += 16) {
+                                        uint32_t o[16];
+                                        tc_ld16(O + c, o);
+                                        tc_wait_ld();
 #pragma unroll
-                                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                            tc_st16(O + c, o);
-                                        }
+                                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                        tc_st16(O + c, o);
                                     }
-                                    weigh();
                                 }
-                                l += total;
-                                tc_st32(Sh, w);
-                            } else {                     // another copy's keys
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) x[j] = 0;
-                                tc_st32(Sh, x);
                             }
+                            const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
+                            uint64_t sum = 0, more = 0;
+                            auto weigh = [&](const uint32_t* y, int c) {
+                                uint32_t w[16];
+#pragma unroll
+                                for (int j = 0; j < 32; j += 4) {
+                                    const uint64_t u = fma2(pair_of(y[j], y[j + 1]), scale2, ref2), v = fma2(pair_of(y[j + 2], y[j + 3]), scale2, ref2);
+                                    const float u0 = exp2_approx(low_of(u)), u1 = exp2_approx(high_of(u));
+                                    const float v0 = exp2_approx(low_of(v)), v1 = exp2_approx(high_of(v));
+                                    sum = add2(sum, pair_of(u0, u1));
+                                    more = add2(more, pair_of(v0, v1));
+                                    w[j / 2] = pack2<DT>(u0, u1);
+                                    w[j / 2 + 1] = pack2<DT>(v0, v1);
+                                }
+                                tc_st16(S + c * 16, w);
+                            };
+                            weigh(x, c0);
+                            if (two) weigh(x + 32, c0 + 1);
+                            sum = add2(sum, more);
+                            l += low_of(sum) + high_of(sum);
+                            uint32_t none[16];           // other copies' keys
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) none[j] = 0;
+#pragma unroll 1
+                            for (int c = 0; c < 4; ++c)
+                                if (c < c0 || c >= c1) tc_st16(S + c * 16, none);
                             tc_wait_st();
                             tc_before_sync();
                         }
                         __syncwarp();
-                        if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s][h]));
+                        if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s][0]));
+                    } else {
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][h]), turns & 1, gave_up));
+                            if (!ok) break;
+                            if (__builtin_expect(ahead && h == 1, 0)) fetch_q(sm.piece[i + 1]);   // the queries of this piece have been read: the next one's take their place
+                            if (warp_live) {
+                                tc_after_sync();
+                                const uint32_t Sh = S + h * (ATT_TILE / 2);
+                                uint32_t x[32], y[32];
+                                // this copy's columns: both 32s of the half, one, or none
+                                const bool first = 2 * h >= c0 && 2 * h < c1, second = 2 * h + 1 >= c0 && 2 * h + 1 < c1;
+                                uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
+                                if (!first) mx = 0;
+                                if (!second) my = 0;
+                                if (__builtin_expect(first | second, 1)) {
+                                    if (__builtin_expect(first, 1)) tc_ld32(Sh, x);
+                                    if (__builtin_expect(second, 1)) tc_ld32(Sh + 32, y);
+                                    tc_wait_ld();
+                                    auto hide = [&](uint32_t* v, uint32_t m) {       // keys that do not count: weight 0
+                                        if (__builtin_expect(m == ~0u, 1)) return;
+#pragma unroll
+                                        for (int j = 0; j < 32; ++j)
+                                            if (!(m >> j & 1)) v[j] = 0xff800000u;
+                                    };
+                                    hide(x, mx);
+                                    hide(y, my);
+                                    uint32_t w[32];
+                                    float total;
+                                    auto weigh = [&]() {
+                                        const uint64_t scale2 = pair_of(scale, scale), ref2 = pair_of(-ref, -ref);
+                                        uint64_t sum = 0, more = 0;
+#pragma unroll
+                                        for (int j = 0; j < 32; j += 2) {
+                                            const uint64_t u = fma2(pair_of(x[j], x[j + 1]), scale2, ref2), v = fma2(pair_of(y[j], y[j + 1]), scale2, ref2);
+                                            const float u0 = exp2_approx(low_of(u)), u1 = exp2_approx(high_of(u));
+                                            const float v0 = exp2_approx(low_of(v)), v1 = exp2_approx(high_of(v));
+                                            sum = add2(sum, pair_of(u0, u1));
+                                            more = add2(more, pair_of(v0, v1));
+                                            w[j / 2] = pack2<DT>(u0, u1);
+                                            w[16 + j / 2] = pack2<DT>(v0, v1);
+                                        }
+                                        sum = add2(sum, more);
+                                        total = low_of(sum) + high_of(sum);
+                                    };
+                                    // Weights come first, against the reference that is there: it need not be the maximum, as long
+                                    // as no sum leaves 2^14 (what fp16 weights can hold).  Where one does, or there was none
+                                    // before, the reference becomes the maximum, and sums so far and weights follow.
+                                    weigh();
+                                    const bool low = live && (!(total <= 16384.f) || (ref == ATT_NONE && (mx | my)));
+                                    if (__builtin_expect(__any_sync(0xffffffffu, low), 0)) {
+                                        float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                                        for (int j = 0; j < 32; j += 2) {
+                                            most[j & 2] = fmaxf(most[j & 2], fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 1])));
+                                            most[(j & 2) + 1] = fmaxf(most[(j & 2) + 1], fmaxf(__uint_as_float(y[j]), __uint_as_float(y[j + 1])));
+                                        }
+                                        const float top = fmaxf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale, ATT_LOW);
+                                        float f = 1.f;
+                                        if (low && top > ref) {
+                                            f = exp2_approx(ref - top);
+                                            ref = top;
+                                            l *= f;
+                                        }
+                                        if (k > 0 || h > 0) {
+                                            // (the product of the half before may be under way)
+                                            ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][1 - h]), (h == 0 ? turns - 1 : turns) & 1, gave_up));
+                                            if (!ok) break;
+                                            tc_after_sync();
+#pragma unroll 1
+                                            for (int c = 0; c < D; c += 16) {
+                                                uint32_t o[16];
+                                                tc_ld16(O + c, o);
+                                                tc_wait_ld();
+#pragma unroll
+                                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                                tc_st16(O + c, o);
+                                            }
+                                        }
+                                        weigh();
+                                    }
+                                    l += total;
+                                    tc_st32(Sh, w);
+                                } else {                     // another copy's keys
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j) x[j] = 0;
+                                    tc_st32(Sh, x);
+                                }
+                                tc_wait_st();
+                                tc_before_sync();
+                            }
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(smem_of(&sm.p_ready[s][h]));
+                        }
                     }
                     ++turns;
                     if (__builtin_expect(ok && ahead, 0)) {
@@ -898,7 +1025,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 const int at = p.merge ? row % (ATT_TILE / copies) : copy * (p.half_rows / copies) + row % (ATT_TILE / copies);
                 if (ok && turn_count > 0) {
                     ok = __all_sync(0xffffffffu, bar_wait(smem_of(&sm.o_ready[s][0]), (turns - 1) & 1, gave_up) &&
-                                                     bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up));
+                                                     (WHOLE || bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up)));
                     tc_after_sync();
                 }
                 if (!p.merge || turn_count == 0) {

@@ -26,7 +26,8 @@ DeviceSetup g_setup[MAX_DEVICES];
 std::mutex g_setup_mutex;
 
 template <int DT, int D> bool opt_in() {
-    return cudaFuncSetAttribute(attend_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>)) == cudaSuccess;
+    return cudaFuncSetAttribute(attend_kernel<DT, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>)) == cudaSuccess &&
+           cudaFuncSetAttribute(attend_kernel<DT, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>)) == cudaSuccess;
 }
 int device_setup(DeviceSetup* setup) {
     int dev = -1;
@@ -118,7 +119,7 @@ template <int DT, int D> int launch_attention(AttendParams& p, int sequences, cu
     a.per_G = 1.f / a.G;
     int rc = a.planned ? launch(plan_kernel, dim3(1), PLAN_THREADS, 0, s, a) : RETOPK_OK;
     if (rc != RETOPK_OK) return rc;
-    rc = launch(attend_kernel<DT, D>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
+    rc = launch(a.few_rows ? attend_kernel<DT, D, true> : attend_kernel<DT, D, false>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
     if (rc != RETOPK_OK) return rc;
     return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, a);
 }
@@ -156,6 +157,7 @@ int run_attention(AttendParams& p, const retopk_pages_t* pages, int sequences, i
     a.grid = dev.num_sms;
     a.max_chunks = (int)w.chunks;
     a.own_rows = half_rows(rows);
+    a.few_rows = (a.n_groups > 0 ? (long long)a.B : 1) * rows <= ATT_FEW;
     if (pages->format == RETOPK_PAGES_BF16)
         return pages->d == 128 ? launch_attention<TYPE_BF16, 128>(p, sequences, s) : launch_attention<TYPE_BF16, 64>(p, sequences, s);
     return pages->d == 128 ? launch_attention<TYPE_FP16, 128>(p, sequences, s) : launch_attention<TYPE_FP16, 64>(p, sequences, s);
