@@ -296,12 +296,16 @@ __device__ __forceinline__ uint32_t elect_one() {
 
 #define TC_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define TC_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
-// 32 columns of the lanes of this warp; tc_wait_ld before the values are used.
+#define TC_RW8(x, i) "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7])
+// 32 columns of the lanes of this warp; tc_wait_ld and tc_loaded before the values are used.
 __device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t* x) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : TC_R8(x, 0), TC_R8(x, 8), TC_R8(x, 16), TC_R8(x, 24) : "r"(addr));
 }
+// Behind the wait: without it the compiler sees nothing that keeps what uses x from being moved before the wait.
+__device__ __forceinline__ void tc_loaded16(uint32_t* x) { asm volatile("" : TC_RW8(x, 0), TC_RW8(x, 8)); }
+__device__ __forceinline__ void tc_loaded32(uint32_t* x) { asm volatile("" : TC_RW8(x, 0), TC_RW8(x, 8), TC_RW8(x, 16), TC_RW8(x, 24)); }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* x) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(addr), TC_W8(x, 0), TC_W8(x, 8) : "memory");
@@ -851,6 +855,8 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             if (two) tc_ld32(S + c0 * 32 + 32, x + 32);
                             const uint32_t m0 = masks[0], m1 = two ? masks[1] : 0, any = m0 | m1;
                             tc_wait_ld();
+                            tc_loaded32(x);
+                            tc_loaded32(x + 32);
                             auto hide = [&](uint32_t* v, uint32_t m) {   // keys that do not count: weight 0
                                 if (__builtin_expect(m == ~0u, 1)) return;
 #pragma unroll
@@ -882,6 +888,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                         uint32_t o[16];
                                         tc_ld16(O + c, o);
                                         tc_wait_ld();
+                                        tc_loaded16(o);
 #pragma unroll
                                         for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
                                         tc_st16(O + c, o);
@@ -938,6 +945,8 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                     if (__builtin_expect(first, 1)) tc_ld32(Sh, x);
                                     if (__builtin_expect(second, 1)) tc_ld32(Sh + 32, y);
                                     tc_wait_ld();
+                                    tc_loaded32(x);
+                                    tc_loaded32(y);
                                     auto hide = [&](uint32_t* v, uint32_t m) {       // keys that do not count: weight 0
                                         if (__builtin_expect(m == ~0u, 1)) return;
 #pragma unroll
@@ -993,6 +1002,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                                 uint32_t o[16];
                                                 tc_ld16(O + c, o);
                                                 tc_wait_ld();
+                                                tc_loaded16(o);
 #pragma unroll
                                                 for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
                                                 tc_st16(O + c, o);
@@ -1036,6 +1046,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             uint32_t x[32];
                             tc_ld32(O + c, x);
                             tc_wait_ld();
+                            tc_loaded32(x);
                             if (live) {
 #pragma unroll
                                 for (int j = 0; j < 32; j += 4)
@@ -1078,6 +1089,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             uint32_t x[32];
                             tc_ld32(O + half * (D / 2) + c, x);
                             tc_wait_ld();
+                            tc_loaded32(x);
 #pragma unroll
                             for (int j = 0; j < 32; j += 4)
                                 *reinterpret_cast<uint4*>(&sums[row * F4 + (((c + j) / 4) ^ (row & 7))]) = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
