@@ -405,6 +405,7 @@ template <int DT, int D> __global__ void __launch_bounds__(PICK_THREADS, 1) pick
     for (int i = 0; i < BINS / PICK_THREADS; ++i) s_bin[i * PICK_THREADS + tid] = 0;
     if (tid == 0) s_count = s_opened = 0;
     if (a.scored) pdl_wait();
+    pdl_start_next();
     if (want == 0) return;
     float2* const at = a.scores + item * a.max_blocks + a.first;
     auto lower = [](float2 s) { return order_of(__fsub_rd(s.x, s.y)); };
