@@ -239,6 +239,16 @@ def test_attend_lines_in_many_parts(paged, dtype, d, members, G, T):
     run_shared(paged, [members], [9000], [9000 + T + rng.randint(0, 300) for _ in range(members)], 32, G, 1, d, T, dtype)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("T,G", [(1, 4), (2, 4), (4, 4), (3, 1)])
+def test_attend_small_group_in_large_batch(paged, dtype, d, T, G):
+    """Two sequences with a long prefix next to many with a short one."""
+    rng = random.Random(T)
+    sizes, shared = [2, 66], [9000, 300]
+    lens = [n + T + rng.randint(0, 200) for m, n in zip(sizes, shared) for _ in range(m)]
+    run_shared(paged, sizes, shared, lens, 16, G, 1, d, T, dtype)
+
+
 @pytest.mark.parametrize("members,T,G", [(3, 2, 2), (2, 1, 16), (70, 1, 4)])
 def test_attend_more_tiles_than_a_chunk(paged, members, T, G):
     """Lines of more than 1024 tiles of 128 keys: of a group and of one sequence alone."""
