@@ -11,8 +11,8 @@
 // rows.  For each KV head and 256 query rows an entry has a line of tiles; a piece of a line is what one CTA
 // takes of it, and leaves fp32 sums for its rows in the workspace.
 //
-// Measured (bf16, d = 128, 8 KV heads of 4 queries).  Four sequences of up to 128K keys on their own, 1.5 GB: 242 us, 6.3 TB/s, near a copy.
-// Eight sequences that share 32K keys: 44 us, of which 21 are the floor of reading them; 3 pass until all CTAs know their work,
+// Measured (bf16, d = 128, 8 KV heads of 4 queries).  Four sequences of up to 128K keys on their own, 1.5 GB: 238 us, 6.4 TB/s, as fast as a copy.
+// Eight sequences that share 32K keys: 42 us, of which 21 are the floor of reading them; 3 pass until all CTAs know their work,
 // 3 until the first scores, 8 in join_kernel.  Of 64 sequences that share 128K: 188 us, 730 TFLOP/s; there the softmax bounds it.  256
 // rows of a tile take 4900 cycles: 2048 for the exponentials alone (16 a cycle), about 2560 of the tensor
 // core (half tiles of keys read Q anew for 64 keys), and neither is hidden wholly behind the other.
