@@ -358,7 +358,7 @@ template <int DT> __host__ __device__ constexpr uint32_t tc_shape(int n, bool b_
 constexpr int ATT_SOFT_WARPS = 8, ATT_LOAD_WARP = ATT_SOFT_WARPS, ATT_MMA_WARP = ATT_LOAD_WARP + 2;      // (two of each)
 constexpr int ATT_WARPS = ATT_MMA_WARP + 2, ATT_THREADS = ATT_WARPS * 32;
 constexpr int ATT_PIECES = 32;           // pieces that a CTA lists at once
-constexpr int ATT_MASKS = 8;             // tiles whose masks are kept
+constexpr int ATT_MASKS = 8;             // tiles of a stream whose masks are kept
 
 // Loads of a piece of n tiles, j = 0 .. 2 n - 1: K0, K1, V0, K2, V1, .., K(n-1), V(n-2), V(n-1).
 __device__ __forceinline__ int k_load(int t) { return t == 0 ? 0 : 2 * t - 1; }
@@ -376,8 +376,8 @@ template <int D> struct AttendSmem {
     static constexpr int SLOTS = 5 * 128 / D;
     unsigned char q[2][TILE_BYTES];
     unsigned char ring[SLOTS][TILE_BYTES];
-    uint32_t mask[ATT_MASKS][4];
-    uint64_t full[SLOTS], empty[SLOTS], mask_ready[ATT_MASKS], q_ready[2], s_ready[2][2], p_ready[2][2], o_ready[2][2], merged[2], drained[2];         // [stream][half of a tile]
+    uint32_t mask[2][ATT_MASKS][4];                      // of each stream's own tiles, one after the other
+    uint64_t full[SLOTS], empty[SLOTS], mask_ready[2][ATT_MASKS], q_ready[2], s_ready[2][2], p_ready[2][2], o_ready[2][2], merged[2], drained[2];         // [stream][half of a tile]
     Piece piece[ATT_PIECES];
     int warp_sum[ATT_WARPS];
     uint32_t issued[SLOTS];     // last load into a slot
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             bar_init(smem_of(&sm.empty[i]), 2);           // one of each stream
         }
 #pragma unroll 1
-        for (int i = 0; i < ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i]), 1);
+        for (int i = 0; i < 2 * ATT_MASKS; ++i) bar_init(smem_of(&sm.mask_ready[i / ATT_MASKS][i % ATT_MASKS]), 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_of(&sm.q_ready[i]), 4);
             for (int h = 0; h < 2; ++h) {
@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
     pdl_start_next();
 
     // what the roles keep from piece to piece
-    uint32_t loads = 0, tiles_done = 0;                  // loads issued (or consumed), tiles behind
+    uint32_t loads = 0, masks[2] = {0, 0};               // loads issued (or consumed), masks written for each stream
     uint32_t turns = 0, begun = 0, merges = 0;           // of a stream: tiles behind, pieces begun, times its warps waited for each other
     bool ok = true;
 
@@ -602,6 +602,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece p = sm.piece[i];
                 const int n = p.tile1 - p.tile0;
+                const bool both = !WHOLE && p.rows > ATT_TILE;           // every tile is both streams'
                 Box mine;
                 int at = ahead;                          // of the tiles looked up last
 #pragma unroll 1
@@ -640,15 +641,21 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     }
                     if (lane == 0) sm.issued[slot] = load;
                     if (keys) {
-                        // The mask.  That of 8 tiles back is no longer read: its softmax was over before this slot came free.
+                        // The mask, for the stream or the two that take the tile.  A stream's masks are numbered as its turns are, so that
+                        // it waits for each of them and a phase of a barrier cannot be taken for the one before.  That of its turn
+                        // 8 back is no longer read: the softmax of that was over before this slot came free.
                         uint32_t m = valid << (lane % 8 * 4);
                         m |= __shfl_xor_sync(0xffffffffu, m, 1);
                         m |= __shfl_xor_sync(0xffffffffu, m, 2);
                         m |= __shfl_xor_sync(0xffffffffu, m, 4);
-                        if (lane % 8 == 0) sm.mask[tiles_done % ATT_MASKS][lane / 8] = m;
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_of(&sm.mask_ready[tiles_done % ATT_MASKS]));
-                        ++tiles_done;
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            if (both || (t & 1) == s) {
+                                if (lane % 8 == 0) sm.mask[s][masks[s] % ATT_MASKS][lane / 8] = m;
+                                __syncwarp();
+                                if (lane == 0) bar_arrive(smem_of(&sm.mask_ready[s][masks[s] % ATT_MASKS]));
+                                ++masks[s];
+                            }
                     }
                 }
                 loads += 2 * n;
@@ -784,7 +791,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             const uint32_t S = lanes + s * ATT_TILE, O = lanes + 2 * ATT_TILE + s * D;
             // (a scale of 0 as the smallest: 0 times the -inf of a hidden key is no number)
             const float scale = a.scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.scale_log2);
-            // tiles of this stream in a piece
+            // tiles of this stream in a piece (WHOLE: none has more rows than ATT_FEW)
             auto turns_of = [&](const Piece& p) { return !WHOLE && p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
             // this thread's query row in a piece, or -1; the copy that it belongs to
             auto row_of = [&](const Piece& p, int* copy) {
@@ -820,8 +827,6 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 #pragma unroll 1
             for (int i = 0; i < pieces && ok; ++i) {
                 const Piece& p = sm.piece[i];
-                const int n = p.tile1 - p.tile0;
-                const bool both = !WHOLE && p.rows > ATT_TILE;           // (WHOLE: there are no more than ATT_FEW)
                 const int turn_count = turns_of(p), copies = copies_of(p.rows);
                 int copy;
                 const int r = row_of(p, &copy);
@@ -833,14 +838,13 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 fetched = false;
 #pragma unroll 1
                 for (int k = 0; k < turn_count && ok; ++k) {
-                    const uint32_t tile = tiles_done + (both ? k : 2 * k + s);
                     const bool ahead = !p.merge && k == turn_count - 1 && i + 1 < pieces && turns_of(sm.piece[i + 1]) > 0;
                     if (__builtin_expect(!here, 0)) {
                         fetch_q(p);
                         give_q(p);
                         here = true;
                     }
-                    ok = bar_wait(smem_of(&sm.mask_ready[tile % ATT_MASKS]), tile / ATT_MASKS & 1, gave_up);
+                    ok = bar_wait(smem_of(&sm.mask_ready[s][turns % ATT_MASKS]), turns / ATT_MASKS & 1, gave_up);
                     if constexpr (WHOLE) {
                         ok = __all_sync(0xffffffffu, ok && bar_wait(smem_of(&sm.s_ready[s][0]), turns & 1, gave_up));
                         if (!ok) break;
@@ -848,7 +852,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         if (warp_live) {
                             tc_after_sync();
                             // this copy's columns, 32 or 64 of them
-                            const uint32_t* masks = sm.mask[tile % ATT_MASKS] + c0;
+                            const uint32_t* masks = sm.mask[s][turns % ATT_MASKS] + c0;
                             const bool two = c1 - c0 > 1;
                             uint32_t x[64];
                             tc_ld32(S + c0 * 32, x);
@@ -938,7 +942,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                 uint32_t x[32], y[32];
                                 // this copy's columns: both 32s of the half, one, or none
                                 const bool first = 2 * h >= c0 && 2 * h < c1, second = 2 * h + 1 >= c0 && 2 * h + 1 < c1;
-                                uint32_t mx = sm.mask[tile % ATT_MASKS][2 * h], my = sm.mask[tile % ATT_MASKS][2 * h + 1];
+                                uint32_t mx = sm.mask[s][turns % ATT_MASKS][2 * h], my = sm.mask[s][turns % ATT_MASKS][2 * h + 1];
                                 if (!first) mx = 0;
                                 if (!second) my = 0;
                                 if (__builtin_expect(first | second, 1)) {
@@ -1111,7 +1115,6 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     }
                 }
                 if (turn_count > 0) tc_before_sync();
-                tiles_done += n;
             }
         }
         ok = !__syncthreads_or(!ok) && !*gave_up;
