@@ -680,14 +680,17 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 auto tile_at = [&](int j) { return __shfl_sync(0xffffffffu, smem_of(sm.ring[(loads + j) % Smem::SLOTS]), 0); };
                 auto empty_at = [&](int j) { return smem_of(&sm.empty[(loads + j) % Smem::SLOTS]); };
                 // Both warps see all loads go by, so that neither runs away from the other: a phase of a
-                // barrier is told from the one after the next by nothing else.
+                // barrier is told from the one after the next by nothing else.  What the other stream has loaded is given back
+                // behind the products that this warp has issued, not before they are over: a place of the ring is one warp's
+                // and the other's load in turn, and either takes for granted that what was there two loads before has been
+                // given back when its own load before has (loads are then given back in their order but for neighbours).
                 int seen = 0;
                 auto see = [&](int j) -> bool {          // the other stream's loads before j
                     if (step == 2)
                         for (; seen < j; ++seen)
                             if ((tile_of_load(seen, n) & 1) != s) {
                                 if (!wait_full(seen)) return false;
-                                if (issue) bar_arrive(empty_at(seen));
+                                tc_commit(empty_at(seen), issue);
                             }
                     return true;
                 };

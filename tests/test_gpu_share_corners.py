@@ -44,3 +44,20 @@ def test_attend_many_lines_of_one_tile(paged, dtype, d, T, G):
         sref.check_attention(want[b:b + 1], None, q[b:b + 1], k, v, table[b:b + 1], lens[b:b + 1], 16, d ** -0.5, case=str(b))
     for _ in range(30):
         assert torch.equal(cache.attend_shared(q, ints(lens), table), want)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("T,G", [(1, 4), (10, 8)])
+def test_attend_many_lines_of_a_few_tiles(paged, dtype, d, T, G):
+    """Lines of one to five tiles in any order: what one stream gives back of the ring while the other stream's product
+    still reads the tile before it."""
+    rng = random.Random(T + d)
+    lens = [rng.randint(1, rng.choice([100, 128, 300, 640])) for _ in range(400)]
+    k, v, table, _, _ = sref.grouped_cache([1] * 400, [0] * 400, lens, 16, 8, d, dtype)
+    cache = paged.KVPages.wrap(k, v)
+    q = randn(6, 400, T, 8 * G, d, dtype=dtype)
+    want = cache.attend_shared(q, ints(lens), table)
+    for b in range(0, 400, 5):
+        sref.check_attention(want[b:b + 1], None, q[b:b + 1], k, v, table[b:b + 1], lens[b:b + 1], 16, d ** -0.5, case=str(b))
+    for _ in range(30):
+        assert torch.equal(cache.attend_shared(q, ints(lens), table), want)
