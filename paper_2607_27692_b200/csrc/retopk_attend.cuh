@@ -37,6 +37,7 @@ constexpr int ATT_CHUNK = 1024;          // tiles whose sums stay in the tensor 
 // beginning of a line 3.
 constexpr int ATT_START = 3;
 constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // reference of a row without keys; lowest of one with keys
+constexpr float ATT_LEAST_SCALE = 1.17549435e-38f;        // stands for a scale of 0
 
 struct Entry {
     int u;                      // where its lines begin
@@ -793,7 +794,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
             const uint32_t S = lanes + s * ATT_TILE, O = lanes + 2 * ATT_TILE + s * D;
             // (a scale of 0 as the smallest: 0 times the -inf of a hidden key is no number)
-            const float scale = a.scale_log2 == 0.f ? 1.17549435e-38f : fabsf(a.scale_log2);
+            const float scale = a.scale_log2 == 0.f ? ATT_LEAST_SCALE : fabsf(a.scale_log2);
             // tiles of this stream in a piece (WHOLE: none has more rows than ATT_FEW)
             auto turns_of = [&](const Piece& p) { return !WHOLE && p.rows > ATT_TILE ? p.tile1 - p.tile0 : (p.tile1 - p.tile0 + 1 - s) / 2; };
             // this thread's query row in a piece, or -1; the copy that it belongs to
@@ -1184,7 +1185,7 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
             }
 #pragma unroll
             for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (sees && share == 0) s_late[r * 16 + k] = s * a.scale_log2;
+            if (sees && share == 0) s_late[r * 16 + k] = s * (a.scale_log2 == 0.f ? ATT_LEAST_SCALE : a.scale_log2);
         }
     }
     pdl_wait();
@@ -1263,15 +1264,17 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
                             o[d] = *reinterpret_cast<const float4*>(half + sums_at(at, c4, D));
                         } else if (k < all && s_late_row[k - n_own] >= 0) {
                             const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(a.pg.v) + s_late_row[k - n_own] * D + c4 * 4);
-                            ml[d] = make_float2(s_late[r * 16 + k - n_own], 1.f);
+                            // (a score of -inf is a weight of 0, one of NaN a weight of NaN: the reference stays a number, as a
+                            // tile's does, so that the row is one with keys)
+                            const float score = s_late[r * 16 + k - n_own], w = score == -INFINITY ? 0.f : (score != score ? score : 1.f);
+                            ml[d] = make_float2(fmaxf(score, ATT_LOW), w);
                             const float2 v0 = unpack2<DT>(v.x), v1 = unpack2<DT>(v.y);
-                            o[d] = make_float4(v0.x, v0.y, v1.x, v1.y);
+                            o[d] = make_float4(v0.x * w, v0.y * w, v1.x * w, v1.y * w);
                         }
                     }
                     float top = M;
 #pragma unroll
                     for (int d = 0; d < JOIN_DEEP; ++d) {
-                        if (ml[d].x == -INFINITY) ml[d] = make_float2(ATT_LOW, 0.f), o[d] = make_float4(0.f, 0.f, 0.f, 0.f);
                         if (ml[d].x == ATT_NONE) o[d] = make_float4(0.f, 0.f, 0.f, 0.f);             // (never written)
                         top = fmaxf(top, ml[d].x);
                     }

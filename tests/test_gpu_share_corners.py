@@ -61,3 +61,80 @@ def test_attend_many_lines_of_a_few_tiles(paged, dtype, d, T, G):
         sref.check_attention(want[b:b + 1], None, q[b:b + 1], k, v, table[b:b + 1], lens[b:b + 1], 16, d ** -0.5, case=str(b))
     for _ in range(30):
         assert torch.equal(cache.attend_shared(q, ints(lens), table), want)
+
+
+# ---------------------------------------------------------------------------------------
+# Draft tokens whose keys are late ones, with numbers that are not finite
+# ---------------------------------------------------------------------------------------
+def formula(q, k, v, scale):
+    """The definition as IEEE arithmetic takes it, 64 bits: q [T, H_q, d], k, v [H, n, d] -> out, lse."""
+    T, H_q, d = q.shape
+    H, n, _ = k.shape
+    out, lse = torch.zeros(T, H_q, d, dtype=torch.float64, device="cuda"), torch.full((T, H_q), -math.inf, dtype=torch.float64, device="cuda")
+    for t in range(T):
+        seen = n - T + 1 + t
+        for h in range(H_q):
+            if seen > 0:
+                s = (k[h * H // H_q, :seen].double() * q[t, h].double()).sum(-1) * scale
+                w = torch.exp(s - s.max())
+                out[t, h] = (w.unsqueeze(1) * v[h * H // H_q, :seen].double()).sum(0) / w.sum()
+                lse[t, h] = s.max() + (torch.log(w.sum()) if s.max() > -math.inf else 0.0)
+    return out, lse
+
+
+def check_formula(paged, q, k, v, lens, scale):
+    """k, v [B, H, rows, d], a page for each sequence.  Where values are not finite, outputs are NaN or infinite, as
+    the tensor cores add them up."""
+    lse = torch.full(q.shape[:3], 7.0, device="cuda")
+    out = paged.KVPages.wrap(k, v).attend_shared(q, ints(lens), scale=scale, lse=lse)
+    exact = bool(v.isfinite().all())
+    for b, n in enumerate(lens):
+        want, want_lse = formula(q[b], k[b, :, :n], v[b, :, :n], scale)
+        keys, values = k[b, :, :n].nan_to_num(0, 0, 0), v[b, :, :n].nan_to_num(0, 0, 0)
+        e_lse, e_out = sref.attention_bound(q[b].nan_to_num(0), keys, values, scale, n, q.dtype)
+        assert not exact or torch.equal(out[b].isnan(), want.isnan()), b
+        assert torch.equal(lse[b].isnan(), want_lse.isnan()), b
+        fine = want.isfinite()
+        assert torch.equal(out[b].isfinite(), fine)
+        assert bool(((out[b].double() - want).abs() <= e_out + ref.half_step(q.dtype) * want.abs() + 2.0 ** -25)[fine].all()), b
+        assert torch.equal(lse[b] == -math.inf, want_lse == -math.inf), b
+        fine = want_lse.isfinite()
+        assert bool(((lse[b].double() - want_lse).abs() <= e_lse + 2.0 ** -23 * want_lse.abs())[fine].all()), b
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("T,lens", [(2, [1, 2, 1, 3, 0]), (5, [1, 4, 5, 3, 6]), (16, [15, 1, 16, 9, 200])])
+def test_late_keys_that_are_not_finite(paged, dtype, d, T, lens):
+    """Rows whose only keys are late ones: NaN in a key or a query shows, as it does in a tile; -inf is a weight of 0."""
+    scale = d ** -0.5
+    k, v = randn(1, 5, 2, 256, d, dtype=dtype), randn(2, 5, 2, 256, d, dtype=dtype)
+    q = randn(3, 5, T, 4, d, dtype=dtype)
+    check_formula(paged, q, k, v, lens, scale)
+    for where in (0, max(0, T - 3)):
+        for value in (math.nan, math.inf, -math.inf):
+            x = k.clone()
+            x[:, :, where, 5] = value
+            check_formula(paged, q, x, v, lens, scale)
+            y = v.clone()
+            y[:, :, where, 5] = value
+            check_formula(paged, q, k, y, lens, scale)
+            if not math.isnan(value):                     # a weight of 0 times an infinite value
+                check_formula(paged, q, x, y, lens, scale)
+    x = q.clone()
+    x[:, T - 1, 2, 7] = math.nan
+    check_formula(paged, x, k, v, lens, scale)
+
+
+@pytest.mark.parametrize("where", [0, 1, 4])
+def test_late_keys_with_a_scale_of_zero(paged, where):
+    """0 counts as the smallest normal number, of late keys as of others: a score of -inf is a weight of 0."""
+    q = randn(3, 3, 5, 4, 64).abs()
+    k, v = randn(1, 3, 2, 64, 64), randn(2, 3, 2, 64, 64)
+    k[:, :, where, 9] = -math.inf
+    lens = [3, 5, 9]
+    out = paged.KVPages.wrap(k, v).attend_shared(q, ints(lens), scale=0.0)
+    for b, n in enumerate(lens):
+        want, _ = formula(q[b], k[b, :, :n], v[b, :, :n], 2.0 ** -126)
+        assert torch.equal(out[b].isnan(), want.isnan())
+        fine = want.isfinite()
+        assert bool(((out[b].double() - want).abs()[fine] <= 3 * ref.half_step(BF) * v.abs().max()).all())
