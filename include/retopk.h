@@ -484,7 +484,7 @@ int retopk_q4_attention(const retopk_pages_t* pages, int B, int T, int H_q, cons
  * The pages of a cache (of all layers that use one block table).  refs [n_pages] int32 counts the
  * entries of block tables that hold a page; a page with 0 or less is free, and new pages are the free
  * ones with the lowest numbers.  scratch: n_pages + RETOPK_POOL_SCRATCH int32, set to zero once;
- * scratch[0] counts the pages that calls found missing (the caller may read and clear it), the rest is the
+ * scratch[0] counts the pages that calls found missing, up to 2^31 - 1 (the caller may read and clear it), the rest is the
  * library's.  Both on the device.  A sequence of n rows holds the first ceil(n / page_size) entries of its row
  * of block_table [B,max_pages].  Results do not depend on the order in which the device works.
  * A pool and the tables over it are changed by one call at a time: calls on several streams need an
@@ -500,7 +500,8 @@ typedef struct {
 
 /* Give each sequence that grows from old_lens[b] to new_lens[b] rows the pages that it lacks, in the order of
  * the sequences.  One that finds too few pages, or that block_table has no room for, gets none: its new
- * entries are -1 and what it lacks is added to scratch[0].  Lengths are read only; negative ones count as 0.
+ * entries are -1 and what it lacks is added to scratch[0].  The pages of one that finds too few stay free, but those
+ * behind it that lack any find too few as well.  Lengths are read only; negative ones count as 0.
  * old_lens and new_lens may be one array (then nothing is done). */
 int retopk_pool_reserve(const retopk_pool_t* pool, int B, const int32_t* old_lens, const int32_t* new_lens, int32_t* block_table,
                         int64_t max_pages, void* stream);

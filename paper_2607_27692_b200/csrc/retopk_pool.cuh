@@ -62,50 +62,61 @@ template <int THREADS> __device__ int lowest_free(const PoolArgs& a, int32_t* li
     return found < want ? found : want;
 }
 
+// Pages that were missing, by one thread: the count stays at the largest number.
+__device__ __forceinline__ void count_missing(const PoolArgs& a, long long n) {
+    const int have = __ldcg(a.scratch + POOL_SHORT), room = have > 0 ? 0x7fffffff - have : 0x7fffffff;
+    if (n > 0) atomicAdd(a.scratch + POOL_SHORT, n < room ? (int)n : room);
+}
+
 // One CTA: how many pages each sequence needs, the lowest free ones, and their places in the table.  A
-// sequence gets all of its pages or none: then its new entries are -1.
+// sequence gets all of its pages or none: then its new entries are -1, all of them, however few pages there are.
 __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_constant__ PoolArgs a) {
     __shared__ int s_base[POOL_THREADS], s_need[POOL_THREADS];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t* list = a.scratch + POOL_LIST;
-    // pages that sequence b lacks (n_pages + 1: more than there are); negative: more than its row has places for
-    auto need = [&](int b, int* first) {
+    // A sequence's new places, and the pages that it lacks for them: as a number to add up it is cut at n_pages + 1 (more
+    // than there are); negative: more than its row has places for.
+    struct Need { long long first, places, lack; int n; };
+    auto need_of = [&](int b) {
         const long long had = pages_held(a.lens[b], a.page_size), get = pages_held(a.other[b], a.page_size);
-        *first = (int)(had < a.max_pages ? had : a.max_pages);
-        if (get <= had) return 0;
-        const int lack = (int)(get - had <= a.n_pages ? get - had : a.n_pages + 1);
-        return get > a.max_pages ? -lack : lack;
+        Need x = {had < a.max_pages ? had : a.max_pages, 0, 0, 0};
+        if (get <= had) return x;
+        x.places = (get < a.max_pages ? get : a.max_pages) - x.first;
+        x.lack = get - had;
+        x.n = (int)(x.lack <= a.n_pages ? x.lack : a.n_pages + 1);
+        if (get > a.max_pages) x.n = -x.n;
+        return x;
     };
     long long want = 0;
     for (int b0 = 0; b0 < a.B; b0 += POOL_THREADS) {
         const int b = b0 + threadIdx.x;
-        int first, total;
-        const int n = b < a.B ? need(b, &first) : 0;
+        int total;
+        const int n = b < a.B ? need_of(b).n : 0;
         scan_cta<POOL_THREADS>(n < 0 ? 0 : n, &total);
         want += total;
     }
     const int found = lowest_free<POOL_THREADS>(a, list, (int)(want < a.n_pages ? want : a.n_pages));
+    __shared__ unsigned long long s_missing;
+    if (threadIdx.x == 0) s_missing = 0;
     long long base = 0;
-    int missing = 0;
     for (int b0 = 0; b0 < a.B; b0 += POOL_THREADS) {
         const int b = b0 + threadIdx.x;
-        int first = 0, total;
-        const int n = b < a.B ? need(b, &first) : 0;
-        const int at = scan_cta<POOL_THREADS>(n < 0 ? 0 : n, &total);
-        const bool ok = n >= 0 && base + at + n <= found;
-        if (!ok) missing += n < 0 ? -n : n;
+        int total;
+        Need x = {0, 0, 0, 0};
+        if (b < a.B) x = need_of(b);
+        const int at = scan_cta<POOL_THREADS>(x.n < 0 ? 0 : x.n, &total);
+        const bool ok = x.n >= 0 && base + at + x.n <= found;
+        if (!ok && x.lack > 0) atomicAdd(&s_missing, (unsigned long long)x.lack);
         s_base[threadIdx.x] = ok ? (int)(base + at) : -1;
-        s_need[threadIdx.x] = n;
+        s_need[threadIdx.x] = x.n;
         __syncthreads();
         const int here = a.B - b0 < POOL_THREADS ? a.B - b0 : POOL_THREADS;
         for (int i = warp; i < here; i += POOL_WARPS) {
             if (s_need[i] == 0) continue;
-            int f;
-            need(b0 + i, &f);
-            const long long places = s_need[i] < 0 ? a.max_pages - f : s_need[i];
-            int32_t* row = a.table + (long long)(b0 + i) * a.max_pages + f;
-            for (long long s = lane; s < places; s += 32) {
+            const Need x = need_of(b0 + i);
+            int32_t* row = a.table + (long long)(b0 + i) * a.max_pages + x.first;
+            for (long long s = lane; s < x.places; s += 32) {
                 const int p = s_base[i] < 0 ? -1 : list[s_base[i] + s];
                 row[s] = p;
                 if (p >= 0) a.refs[p] = 1;
@@ -114,7 +125,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
         base += total;
         __syncthreads();
     }
-    if (missing) atomicAdd(a.scratch + POOL_SHORT, missing);
+    if (threadIdx.x == 0) count_missing(a, (long long)s_missing);
 }
 
 // Bound by waiting, about ten times for memory one after the other: 4.6 us for 3 forks, 8 for 64 of up to 2048 pages.
@@ -171,7 +182,7 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
     if (tid == 0) a.scratch[POOL_TICKET] = 0;
 
     const int found = __ldcg(a.scratch + POOL_USED);
-    int base = 0, missing = 0;
+    int base = 0;
     for (int i0 = 0; i0 < a.n; i0 += FORK_THREADS) {
         const int k = i0 + tid, state = k < a.n ? __ldcg(a.dst + k) : -3;
         int total;
@@ -199,10 +210,9 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
             }
             a.src[k] = a.dst[k] = -1;
             a.rows[k] = 0;
-            ++missing;
         }
     }
-    if (missing) atomicAdd(a.scratch + POOL_SHORT, missing);
+    if (tid == 0) count_missing(a, base - found);        // (each fork that found no page lacks one)
 }
 
 // One CTA for a sequence.  Whoever takes the length takes the pages: a row that is named twice is freed once.

@@ -138,3 +138,55 @@ def test_late_keys_with_a_scale_of_zero(paged, where):
         assert torch.equal(out[b].isnan(), want.isnan())
         fine = want.isfinite()
         assert bool(((out[b].double() - want).abs()[fine] <= 3 * ref.half_step(BF) * v.abs().max()).all())
+
+
+# ---------------------------------------------------------------------------------------
+# Pages
+# ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_pages,width,page,old,new", [(3, 12, 4, [0, 1], [36, 1]), (10, 32, 16, [1, 40], [321, 40]), (1, 300, 1, [0, 0], [300, 0]),
+                                                        (3, 12, 4, [0, 1], [49, 1])])
+def test_reserve_more_than_there_are(paged, n_pages, width, page, old, new):
+    """A growth by more pages than the pool has, whose row has room for it or not: none of its new entries keeps a number of
+    another sequence's page, and what is missing is counted whole."""
+    pool = paged.PagePool(n_pages, page)
+    table, lens = torch.zeros(2, width, dtype=torch.int32, device="cuda"), ints(old)
+    pool.reserve(table, ints([0, 0]), lens)
+    had = [-(-n // page) for n in old]
+    table[0, had[0]:] = n_pages - 1                       # left from an earlier sequence
+    refs, keep = pool.refs.clone(), table.clone()
+    pool.reserve(table, lens, ints(new))
+    get = -(-new[0] // page)
+    keep[0, had[0]:min(get, width)] = -1
+    assert torch.equal(table, keep) and torch.equal(pool.refs, refs)
+    assert pool.missing.item() == get - had[0]
+    pool.free(table, ints(new), ints([0]))
+    refs[table[0, :had[0]].long()] -= 1
+    assert torch.equal(pool.refs, refs)
+
+
+def test_missing_pages_stay_at_the_largest_number(paged):
+    pool = paged.PagePool(4, 1)
+    table, zero, many = torch.zeros(3, 4, dtype=torch.int32, device="cuda"), ints([0, 0, 0]), ints([2 ** 31 - 1] * 3)
+    for _ in range(3):
+        pool.reserve(table, zero, many)
+        assert pool.missing.item() == 2 ** 31 - 1 and bool((table == -1).all()) and not pool.refs.any()
+    pool.missing.zero_()
+    pool.reserve(table, zero, ints([4, 1, 2]))            # the second finds none, nor does the third
+    assert table.tolist() == [[0, 1, 2, 3], [-1] * 4, [-1] * 4] and pool.missing.item() == 3
+    pool.missing.zero_()
+    pool.reserve(table, ints([4, 0, 0]), ints([4, 2, 0]))
+    assert pool.missing.item() == 2
+
+
+def test_forks_that_find_no_page_are_counted(paged):
+    pool = paged.PagePool(6, 4)
+    table, lens = torch.zeros(8, 2, dtype=torch.int32, device="cuda"), ints([5, 3] + [0] * 6)
+    pool.reserve(table, torch.zeros_like(lens), lens)
+    refs = pool.refs.clone()
+    pool.missing.fill_(2 ** 31 - 2)
+    src, dst, rows = pool.fork(table, lens, ints([0, 1, 0, 1, 0]), ints([2, 3, 4, 5, 6]))
+    assert dst.tolist() == [3, 4, 5, -1, -1] and rows.tolist() == [1, 3, 1, 0, 0] and lens.tolist() == [5, 3, 5, 3, 5, 0, 0, 0]
+    assert pool.missing.item() == 2 ** 31 - 1
+    assert pool.refs.tolist() == [3, 1, 1, 1, 1, 1]
+    pool.free(table, lens, ints([2, 3, 4]))
+    assert torch.equal(pool.refs, refs)
