@@ -328,14 +328,15 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_pages_kernel(const __grid_c
         if (r > a.page_rows) r = a.page_rows;
         if (r <= 0) continue;
         for (int t = 0; t < a.tensors; ++t) {
-            const int head = a.page_rows * a.t[t].row_bytes;           // bytes from one head to the next
+            // bytes from one head to the next; 2^31 and more where a page is a long sequence
+            const long long head = (long long)a.page_rows * a.t[t].row_bytes;
             const bool whole = r == a.page_rows;
             const unsigned char* const s = a.t[t].p + (long long)from * a.H * head;
             unsigned char* const d = a.t[t].p + (long long)to * a.H * head;
             auto move = [&](auto piece) {
                 using P = decltype(piece);
                 // heads that are copied whole are one run
-                const long long run = (whole ? (long long)a.H * head : (long long)r * a.t[t].row_bytes) / (int)sizeof(P);
+                const long long run = (whole ? a.H * head : (long long)r * a.t[t].row_bytes) / (int)sizeof(P);
                 const long long all = whole ? run : run * a.H, share = a.parts > 1 ? (long long)__umul64hi(all, a.per_part) : all, more = all - share * a.parts;
                 const long long lo = share * part + (part < more ? part : more), hi = lo + share + (part < more);
                 if (whole) {

@@ -190,3 +190,21 @@ def test_forks_that_find_no_page_are_counted(paged):
     assert pool.refs.tolist() == [3, 1, 1, 1, 1, 1]
     pool.free(table, lens, ints([2, 3, 4]))
     assert torch.equal(pool.refs, refs)
+
+
+def test_copy_pages_of_more_than_2_gib_a_head(paged):
+    """Pages as long as a sequence: whole ones, and the first rows of one."""
+    page = (1 << 23) + 5
+    k, v = (torch.empty(2, 2, page, 128, dtype=BF, device="cuda") for _ in range(2))           # 8.6 GB each
+    for x, seed in ((k, 1), (v, 2)):
+        x.view(torch.int16).random_(-2 ** 15, 2 ** 15, generator=torch.Generator(device="cuda").manual_seed(seed))
+    cache = paged.KVPages.wrap(k, v)
+    last = [x[1, :, page - 3:].clone().view(torch.int16) for x in (k, v)]
+    cache.copy_pages(ints([0]), ints([1]), ints([page - 3]))
+    for x, tail in zip((k, v), last):
+        bits = x.view(torch.int16)
+        assert torch.equal(bits[0, :, :page - 3], bits[1, :, :page - 3]) and torch.equal(bits[1, :, page - 3:], tail)
+        assert not torch.equal(bits[0, :, page - 3:], tail)
+    cache.copy_pages(ints([1]), ints([0]))
+    for x in (k, v):
+        assert torch.equal(x[0].view(torch.int16), x[1].view(torch.int16))
