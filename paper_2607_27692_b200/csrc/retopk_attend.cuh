@@ -1150,7 +1150,7 @@ template <int DT, int D> __global__ void __launch_bounds__(JOIN_THREADS, 4) join
     __shared__ struct { const float* part; int count; } s_line[3];       // parts of a chunk of a line: the first one, and how many
     __shared__ float4 s_o[JOIN_THREADS];
     __shared__ float2 s_ml[JOIN_THREADS];
-    const int h = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
+    const int i = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;         // entry a.n_groups + i
     const int rows = a.blocks ? a.G : a.T * a.G, token0 = a.blocks ? i : i * a.T;
     // later draft tokens: all queries are read before the first output is written, which may take their place
     int late = 0, first_seen = 0;

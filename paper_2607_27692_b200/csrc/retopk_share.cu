@@ -121,7 +121,8 @@ template <int DT, int D> int launch_attention(AttendParams& p, int sequences, cu
     if (rc != RETOPK_OK) return rc;
     rc = launch(a.few_rows ? attend_kernel<DT, D, true> : attend_kernel<DT, D, false>, dim3((unsigned)a.grid), ATT_THREADS, sizeof(AttendSmem<D>), s, p);
     if (rc != RETOPK_OK) return rc;
-    return launch(join_kernel<DT, D>, dim3((unsigned)a.pg.H_kv, (unsigned)sequences, (unsigned)shares), JOIN_THREADS, 0, s, a);
+    // (tokens with blocks of their own can be 65536, one more than a grid has room for in any dimension but the first)
+    return launch(join_kernel<DT, D>, dim3((unsigned)sequences, (unsigned)a.pg.H_kv, (unsigned)shares), JOIN_THREADS, 0, s, a);
 }
 
 // Rows of 64 channels each, `box` rows to a copy, into shared memory as the tensor cores' operands lie there.

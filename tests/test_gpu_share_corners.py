@@ -208,3 +208,29 @@ def test_copy_pages_of_more_than_2_gib_a_head(paged):
     cache.copy_pages(ints([1]), ints([0]))
     for x in (k, v):
         assert torch.equal(x[0].view(torch.int16), x[1].view(torch.int16))
+
+
+# ---------------------------------------------------------------------------------------
+# Many tokens with blocks of their own
+# ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("B,T,H,G,keep", [(4096, 16, 1, 1, 2), (4095, 16, 1, 2, 1), (512, 1, 2, 4, 3), (100, 4, 3, 2, 5)])
+def test_block_attention_of_many_tokens(paged, B, T, H, G, keep):
+    """Up to the stated limits: 4096 sequences of one KV head, 16 tokens each."""
+    rng = random.Random(B)
+    lens = [rng.randint(0, 95) for _ in range(B)]
+    pages = 97
+    k, v = randn(1, pages, H, 16, 64), randn(2, pages, H, 16, 64)
+    table = ints([[rng.randrange(pages) for _ in range(6)] for _ in range(B)])
+    cache = paged.KVPages.wrap(k, v)
+    index = paged.BlockIndex.wrap(cache, sref.bounds_of(k, 16))
+    q = randn(3, B, T, H * G, 64)
+    blocks = index.select(q, ints(lens), table, keep=keep, first=0, last=1)
+    lse = torch.full((B, T, H * G), 7.0, device="cuda")
+    out = index.attend(q, ints(lens), blocks, table, lse=lse)
+    some = sorted({*range(0, B, max(1, B // 40)), B - 1})
+    for b in some:
+        picks = [[sref.select(q[b, t], index.bounds, table, b, lens[b] - T + 1 + t, 16, 16, keep, 0, 1) for t in range(T)]]
+        assert [[x.tolist() for x in row] for row in blocks[b]] == [[x + [-1] * (keep - len(x)) for x in row] for row in picks[0]], b
+        sref.check_attention(out[b:b + 1], lse[b:b + 1], q[b:b + 1], k, v, table[b:b + 1], [lens[b]], 16, 0.125, picks, 16, case=str(b))
+    assert torch.equal(out, index.attend(q, ints(lens), blocks, table))
+    assert bool((out.isfinite()).all())
