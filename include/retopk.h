@@ -499,9 +499,11 @@ typedef struct {
 } retopk_pool_t;
 
 /* Give each sequence that grows from old_lens[b] to new_lens[b] rows the pages that it lacks, in the order of
- * the sequences.  One that finds too few pages, or that block_table has no room for, gets none: its new
+ * the sequences.  Before that, each one that shrinks (draft tokens that were not accepted) gives back the pages behind its new
+ * length, whose entries become -1.  One that finds too few pages, or that block_table has no room for, gets none: its new
  * entries are -1 and what it lacks is added to scratch[0].  The pages of one that finds too few stay free, but those
- * behind it that lack any find too few as well.  Lengths are read only; negative ones count as 0.
+ * behind it that lack any find too few as well.  A sequence that shrinks to a length inside a page that others hold too must
+ * not be appended to there: a fork of it has that page's rows in a page of its own.  Lengths are read only; negative ones count as 0.
  * old_lens and new_lens may be one array (then nothing is done). */
 int retopk_pool_reserve(const retopk_pool_t* pool, int B, const int32_t* old_lens, const int32_t* new_lens, int32_t* block_table,
                         int64_t max_pages, void* stream);

@@ -69,32 +69,53 @@ __device__ __forceinline__ void count_missing(const PoolArgs& a, long long n) {
 }
 
 // One CTA: how many pages each sequence needs, the lowest free ones, and their places in the table.  A
-// sequence gets all of its pages or none: then its new entries are -1, all of them, however few pages there are.
+// sequence gets all of its pages or none: then its new entries are -1, all of them, however few pages there are.  Before that
+// sequences that shrink give back what they no longer hold, so that a page may go from one to another in a call.
 __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_constant__ PoolArgs a) {
     __shared__ int s_base[POOL_THREADS], s_need[POOL_THREADS];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t* list = a.scratch + POOL_LIST;
     // A sequence's new places, and the pages that it lacks for them: as a number to add up it is cut at n_pages + 1 (more
-    // than there are); negative: more than its row has places for.
-    struct Need { long long first, places, lack; int n; };
+    // than there are); negative: more than its row has places for.  `gone`: the places from `first` on that it no longer holds.
+    struct Need { long long first, places, lack, gone; int n; };
     auto need_of = [&](int b) {
         const long long had = pages_held(a.lens[b], a.page_size), get = pages_held(a.other[b], a.page_size);
-        Need x = {had < a.max_pages ? had : a.max_pages, 0, 0, 0};
-        if (get <= had) return x;
-        x.places = (get < a.max_pages ? get : a.max_pages) - x.first;
+        const long long from = had < a.max_pages ? had : a.max_pages, to = get < a.max_pages ? get : a.max_pages;
+        Need x = {from, 0, 0, 0, 0};
+        if (get <= had) {
+            x.first = to;
+            x.gone = from - to;
+            return x;
+        }
+        x.places = to - from;
         x.lack = get - had;
         x.n = (int)(x.lack <= a.n_pages ? x.lack : a.n_pages + 1);
         if (get > a.max_pages) x.n = -x.n;
         return x;
     };
     long long want = 0;
+    bool less = false;
     for (int b0 = 0; b0 < a.B; b0 += POOL_THREADS) {
         const int b = b0 + threadIdx.x;
         int total;
-        const int n = b < a.B ? need_of(b).n : 0;
-        scan_cta<POOL_THREADS>(n < 0 ? 0 : n, &total);
+        Need x = {0, 0, 0, 0, 0};
+        if (b < a.B) x = need_of(b);
+        less |= x.gone > 0;
+        scan_cta<POOL_THREADS>(x.n < 0 ? 0 : x.n, &total);
         want += total;
+    }
+    if (__syncthreads_or(less)) {
+        for (int b = warp; b < a.B; b += POOL_WARPS) {
+            const Need x = need_of(b);
+            int32_t* row = a.table + (long long)b * a.max_pages + x.first;
+            for (long long s = lane; s < x.gone; s += 32) {
+                const int p = row[s];
+                if (p >= 0 && p < a.n_pages) atomicSub(a.refs + p, 1);
+                row[s] = -1;
+            }
+        }
+        __syncthreads();
     }
     const int found = lowest_free<POOL_THREADS>(a, list, (int)(want < a.n_pages ? want : a.n_pages));
     __shared__ unsigned long long s_missing;
@@ -103,7 +124,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
     for (int b0 = 0; b0 < a.B; b0 += POOL_THREADS) {
         const int b = b0 + threadIdx.x;
         int total;
-        Need x = {0, 0, 0, 0};
+        Need x = {0, 0, 0, 0, 0};
         if (b < a.B) x = need_of(b);
         const int at = scan_cta<POOL_THREADS>(x.n < 0 ? 0 : x.n, &total);
         const bool ok = x.n >= 0 && base + at + x.n <= found;

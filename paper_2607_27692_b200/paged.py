@@ -328,8 +328,10 @@ class PagePool:
     def reserve(self, block_table, old_lens, new_lens):
         """Enter the pages that sequences lack to grow from ``old_lens`` to ``new_lens`` rows (int32 [B]).
 
-        In the order of the sequences; one that finds too few pages, or no room in its row, gets -1 in its
-        new entries.
+        Those that shrink (draft tokens that were not accepted) give back the pages behind their new length first.  In the
+        order of the sequences; one that finds too few pages, or no room in its row, gets -1 in its new entries, and so do
+        those behind one that finds too few.  A sequence that shrinks to a length inside a page that others hold too is not
+        to be appended to there; a fork of it has a page of its own.
         """
         self._fast.pool_reserve(self.refs, self._scratch, self.page_size, block_table, old_lens, new_lens)
 

@@ -234,3 +234,78 @@ def test_block_attention_of_many_tokens(paged, B, T, H, G, keep):
         sref.check_attention(out[b:b + 1], lse[b:b + 1], q[b:b + 1], k, v, table[b:b + 1], [lens[b]], 16, 0.125, picks, 16, case=str(b))
     assert torch.equal(out, index.attend(q, ints(lens), blocks, table))
     assert bool((out.isfinite()).all())
+
+
+# ---------------------------------------------------------------------------------------
+# Sequences that shrink
+# ---------------------------------------------------------------------------------------
+class Rows:
+    """The pool on the host, with lengths that go either way."""
+
+    def __init__(self, paged, n_pages, page, B, width):
+        self.host = sref.Pool(n_pages, page, B, width)
+        self.pool = paged.PagePool(n_pages, page)
+        self.table, self.lens = ints(self.host.table), ints(self.host.lens)
+
+    def reserve(self, new):
+        """New lengths are taken where there was room."""
+        h = self.host
+        self.pool.reserve(self.table, self.lens, ints(new))
+        for b, (o, n) in enumerate(zip(h.lens, new)):
+            for s in range(min(h.held(n), h.width), min(h.held(o), h.width)):
+                if 0 <= h.table[b][s] < len(h.refs):
+                    h.refs[h.table[b][s]] -= 1
+                h.table[b][s] = -1
+        h.reserve(h.lens, new)
+        assert self.table.tolist() == h.table and self.pool.refs.tolist() == h.refs and self.pool.missing.item() == h.missing
+        for b, n in enumerate(new):
+            if h.held(n) <= h.width and -1 not in h.table[b][:h.held(n)]:
+                h.lens[b] = n
+        self.lens.copy_(ints(h.lens))
+
+
+@pytest.mark.parametrize("n_pages,page,B,width", [(7, 4, 3, 5), (64, 16, 9, 12), (3000, 16, 40, 100), (5000, 8, 1100, 20)])
+def test_reserve_for_rows_that_shrink(paged, n_pages, page, B, width):
+    rng = random.Random(n_pages)
+    rows = Rows(paged, n_pages, page, B, width)
+    for step in range(40):
+        rows.reserve([rng.choice([n, n, n + rng.randint(0, 3 * page), max(0, n - rng.randint(0, 3 * page)), rng.randint(-1, width * page)]) for n in rows.host.lens])
+        idle = [b for b, n in enumerate(rows.host.lens) if n <= 0]
+        busy = [b for b, n in enumerate(rows.host.lens) if n > 0]
+        if step % 3 == 0 and idle and busy:               # shared pages: one holder less
+            p, c = rng.choice(busy), rng.choice(idle)
+            rows.pool.fork(rows.table, rows.lens, ints([p]), ints([c]))
+            rows.host.fork([p], [c])
+            assert rows.table.tolist() == rows.host.table and rows.lens.tolist() == rows.host.lens
+    rows.pool.free(rows.table, rows.lens)
+    assert not rows.pool.refs.any()
+
+
+def test_draft_tokens_that_are_not_accepted(paged):
+    """Eight rows more in every step, of which some stay: no page is lost, and a page may go to another sequence at once."""
+    rows, page = Rows(paged, 12, 4, 2, 12), 4
+    rng = random.Random(3)
+    lens = [5, 9]
+    rows.reserve(lens)
+    while max(lens) <= 16:
+        rows.reserve([n + 8 for n in lens])
+        lens = [n + rng.randint(1, 3) for n in lens]
+        rows.reserve(lens)
+        assert rows.pool.missing.item() == 0 and int(rows.pool.refs.sum()) == sum(-(-n // page) for n in lens)
+    rows.reserve([48, 0])                                 # all pages, the other's among them
+    assert rows.pool.missing.item() == 0 and rows.pool.refs.tolist() == [1] * 12 and rows.table[1].tolist() == [-1] * 5 + rows.table[1, 5:].tolist()
+    rows.reserve([-3, 48])
+    assert rows.pool.missing.item() == 0 and rows.pool.refs.tolist() == [1] * 12
+
+
+def test_lengths_beyond_the_row_that_shrink(paged):
+    pool = paged.PagePool(8, 4)
+    table = torch.zeros(1, 3, dtype=torch.int32, device="cuda")
+    pool.reserve(table, ints([0]), ints([12]))
+    pool.reserve(table, ints([400]), ints([30]))          # both beyond: nothing is held less
+    assert table.tolist() == [[0, 1, 2]] and pool.refs.tolist() == [1, 1, 1] + [0] * 5
+    pool.reserve(table, ints([400]), ints([5]))
+    assert table.tolist() == [[0, 1, -1]] and pool.refs.tolist() == [1, 1] + [0] * 6
+    table[0, 1] = 99                                      # no page
+    pool.reserve(table, ints([8]), ints([0]))
+    assert table.tolist() == [[-1] * 3] and pool.refs.tolist() == [0, 1] + [0] * 6 and pool.missing.item() == 0
