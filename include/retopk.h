@@ -548,7 +548,8 @@ int retopk_pages_copy(const retopk_pages_t* pages, int64_t n, const int32_t* src
  * product with the values.  Values that are not finite make the outputs of those who see them NaN or infinite.
  * A scale of 0 counts as the smallest normal number.  Results are bit-reproducible; in place they may differ from others in
  * the last bits.
- * out may be q where q is contiguous; other overlaps are EINVAL.  workspace as in retopk_q4_attention.
+ * out may be q where q is contiguous; other overlaps of out, lse and workspace with each other or with what is read, lengths, groups
+ * and block_table among it, are EINVAL.  workspace as in retopk_q4_attention.
  * Limits: H_q / H_kv <= 16, 1 <= T <= 16, B * H_kv <= 4096, at most 2^20 keys of a sequence (max_pages * page_size) and
  * 2^31 - 256 rows n_pages * H_kv * page_size; EUNSUPPORTED beyond.
  */
@@ -561,7 +562,8 @@ int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, 
 /*
  * Blocks of keys.  Block j of a sequence is rows j * block .. (j + 1) * block - 1; block is 16, 32, 64 or
  * 128 and divides page_size.  bounds [n_pages,H_kv,page_size/block,2,d], of the pages' type: the least and
- * the largest key of a block, channel by channel (NaN where a key is NaN).  16-bit pages only.
+ * the largest key of a block, channel by channel (NaN where a key is NaN).  16-bit pages only.  What a call writes, its
+ * workspace too, may not overlap what it reads (EINVAL).
  *
  * retopk_block_update: the bounds of all full blocks that overlap the last n_new rows of each sequence.
  * retopk_block_copy: the bounds follow their pages (retopk_pages_copy); whole pages.

@@ -88,6 +88,10 @@ inline Pages device_pages(const retopk_pages_t* p) {
     return g;
 }
 
+// What a call reads of the sequences: their lengths and their rows of the block table.
+inline Memory lens_memory(const int32_t* seq_lens, int B) { return {seq_lens, (uint64_t)B * 4}; }
+inline Memory table_memory(const retopk_pages_t* p, int B) { return {p->block_table, (uint64_t)B * p->max_pages * 4}; }
+
 // Bounds of blocks of keys, and the 16-bit pages that they belong to.
 inline Memory bounds_memory(const retopk_pages_t* p, int block, const void* bounds) {
     return {bounds, (uint64_t)p->n_pages * p->H_kv * (p->page_size / block) * p->d * 4};

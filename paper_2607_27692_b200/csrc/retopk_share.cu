@@ -79,9 +79,10 @@ Workspace lay_out(int64_t sequences, int64_t rows, int64_t n_groups, int64_t gro
     return w;
 }
 
-// What both attentions refuse alike, and their arguments.
-int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, const void* q, int64_t q_stride,
-                    float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes, AttendArgs& a) {
+// What both attentions refuse alike, and their arguments.  cu, shared and blocks: what else is read, or nothing.
+int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const int32_t* seq_lens, const Memory& cu_m, const Memory& shared_m,
+                    const Memory& blocks_m, const void* q, int64_t q_stride, float scale, void* out, float* lse, void* workspace,
+                    int64_t workspace_bytes, AttendArgs& a) {
     if (pages->format == RETOPK_PAGES_Q4 || !seq_lens || !out || !workspace || !isfinite(scale)) return RETOPK_EINVAL;
     const int d = pages->d;
     if (!rows_ok(q, q_stride, H_q, d) || !aligned16(workspace) || !aligned16(out)) return RETOPK_EINVAL;
@@ -95,6 +96,9 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     const Memory q_m = memory_of(qi, n, d), out_m = memory_of(qo, n, d), lse_m = {lse, (uint64_t)n * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
     if (!in_place_or_apart(qi, qo, n, d) || !all_apart(out_m, pg) || !all_apart(lse_m, pg) || !all_apart(ws_m, pg)) return RETOPK_EINVAL;
     if (!all_apart(lse_m, {out_m, q_m, ws_m}) || !all_apart(ws_m, {out_m, q_m})) return RETOPK_EINVAL;
+    const Memory lens_m = lens_memory(seq_lens, B), table_m = table_memory(pages, B);
+    for (const Memory& written : {out_m, lse_m, ws_m})
+        if (!all_apart(written, {lens_m, table_m, cu_m, shared_m, blocks_m})) return RETOPK_EINVAL;
     a.seq_lens = seq_lens;
     a.q = static_cast<const uint16_t*>(q);
     a.q_stride = q_stride;
@@ -213,7 +217,8 @@ int retopk_shared_attention(const retopk_pages_t* pages, int B, int T, int H_q, 
     if (n_groups < 0 || n_groups > B || (n_groups > 0 && (!cu_groups || !shared_lens))) return RETOPK_EINVAL;
     AttendParams p;
     AttendArgs& a = p.a;
-    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
+    rc = check_attention(pages, B, T, H_q, seq_lens, {n_groups > 0 ? cu_groups : nullptr, (n_groups + 1ull) * 4},
+                         {n_groups > 0 ? shared_lens : nullptr, n_groups * 4ull}, {nullptr, 0}, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
     if (rc != RETOPK_OK) return rc;
     if (workspace_bytes < 4096) return RETOPK_EINVAL;    // (refused without a device too)
     Workspace w;
@@ -233,6 +238,7 @@ int retopk_block_update(const retopk_pages_t* pages, int block, void* bounds, in
     if (!seq_lens || n_new < 0) return RETOPK_EINVAL;
     if (B > 65535 || pages->H_kv > 65535) return RETOPK_EUNSUPPORTED;
     if (n_new == 0) return RETOPK_OK;
+    if (!all_apart(bounds_memory(pages, block, bounds), {lens_memory(seq_lens, B), table_memory(pages, B)})) return RETOPK_EINVAL;
     BoundsArgs a;
     memset(&a, 0, sizeof a);
     a.pg = device_pages(pages);
@@ -276,6 +282,8 @@ int retopk_block_select(const retopk_pages_t* pages, int block, const void* boun
     const Memory q_m = memory_of(Strided{q, q_stride, H_q}, (long long)B * T, pages->d), ws_m = {workspace, (uint64_t)workspace_bytes};
     const Memory bounds_m = bounds_memory(pages, block, bounds), blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
     if (!all_apart(blocks_m, {q_m, ws_m, bounds_m}) || !all_apart(ws_m, {q_m, bounds_m})) return RETOPK_EINVAL;
+    const Memory lens_m = lens_memory(seq_lens, B), table_m = table_memory(pages, B);
+    if (!all_apart(blocks_m, {lens_m, table_m}) || !all_apart(ws_m, {lens_m, table_m})) return RETOPK_EINVAL;
     a.block = block; a.shift = __builtin_ctz((unsigned)block); a.per_G = 1.f / (float)(H_q / pages->H_kv); a.scored = a.max_blocks > keep;
     a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv; a.keep = keep; a.first = first; a.last = last;
     a.seq_lens = seq_lens;
@@ -320,11 +328,10 @@ int retopk_block_attention(const retopk_pages_t* pages, int block, int B, int T,
     if (keep > MAX_KEYS) return RETOPK_EUNSUPPORTED;
     AttendParams p;
     AttendArgs& a = p.a;
-    rc = check_attention(pages, B, T, H_q, seq_lens, q, q_stride, scale, out, lse, workspace, workspace_bytes, a);
+    rc = check_attention(pages, B, T, H_q, seq_lens, {nullptr, 0}, {nullptr, 0}, {blocks, (uint64_t)B * T * pages->H_kv * keep * 4}, q, q_stride,
+                         scale, out, lse, workspace, workspace_bytes, a);
     if (rc != RETOPK_OK) return rc;
-    const Memory blocks_m = {blocks, (uint64_t)B * T * pages->H_kv * keep * 4};
-    const Memory out_m = {out, (uint64_t)B * T * H_q * pages->d * 2}, lse_m = {lse, (uint64_t)B * T * H_q * 4}, ws_m = {workspace, (uint64_t)workspace_bytes};
-    if (!all_apart(blocks_m, {out_m, lse_m, ws_m}) || workspace_bytes < 4096) return RETOPK_EINVAL;
+    if (workspace_bytes < 4096) return RETOPK_EINVAL;
     const int64_t keys = (int64_t)keep * block, most = MAX_KEYS + block - 1;
     Workspace w;
     DeviceSetup dev;
