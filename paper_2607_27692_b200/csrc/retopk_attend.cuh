@@ -32,7 +32,7 @@ __device__ __forceinline__ int keys_seen(const Pages& pg, int len, int T, int t)
 
 constexpr int ATT_TILE = 128;            // keys of a tile, and query rows of a stream
 constexpr int ATT_FEW = 64;              // query rows up to which tiles are taken whole
-constexpr int ATT_CHUNK = 1024;          // tiles whose sums stay in the tensor core at most: it cuts additions off
+constexpr int ATT_CHUNK = 1024;          // tiles of a line whose sums one part of a CTA holds at most
 // What a CTA's work counts: a tile of up to 128 query rows 1 (two of them are at work at once), one of more rows 2, and the
 // beginning of a line 3.
 constexpr int ATT_START = 3;
@@ -106,6 +106,15 @@ struct Shares {
 // With few query rows, copies of them fill the 128 of a stream: each copy has a share of a tile's keys to itself,
 // so that four warps have the work of one.
 __host__ __device__ constexpr int copies_of(int rows) { return rows <= ATT_TILE / 4 ? 4 : (rows <= ATT_TILE / 2 ? 2 : 1); }
+// Tiles of a piece at most, as a power of two: their sums stay in the tensor core, which cuts each addition off, 2^-23.5 of a
+// sum of one sign on average.  8192 additions (1024 tiles of more than 128 rows; both streams and all copies share those of fewer) are
+// 6e-4 of the sum: little next to half a step of bf16, 4e-3, but more than one of fp16, 5e-4.  fp16: up to 1024 additions, 1.1e-4, after which
+// the next piece of the same part adds its sums to what is there, rounded in fp32.  (152 lines of 1024 tiles of 256 rows, d = 64: 5.9e-4
+// and 2505 us without, 1.1e-4 and 2547 us with it.)
+template <int DT> __device__ __forceinline__ int piece_shift(int rows) {
+    return DT == TYPE_BF16 ? 10 : 7 + (rows <= ATT_TILE) + (copies_of(rows) >> 1);
+}
+static_assert(ATT_CHUNK == 1 << 10, "pieces divide chunks");
 // Whether the sums of a part's copies become one before they are written.  That takes 1 to 2 us at the end of a piece; in
 // join_kernel it saves a half or three quarters of the places, in all parts of the line, that the threads which share a row go
 // through.  Done where each of them had 6 or more.  (Group of 8 sequences, 18 parts to a line: 47.9 to 43.5 us; blocks of 4
@@ -369,7 +378,8 @@ __device__ __forceinline__ int tile_of_load(int j, int n) { return j == 0 ? 0 : 
 struct Piece {
     int b, h, token, row0, rows, half_rows;
     int lo, hi, seen, tile0, tile1;
-    int merge;                  // the copies' sums become one
+    bool merge;                 // the copies' sums become one
+    bool more;                  // its sums are added to those that the CTA's piece before left in the same part
     float* part;
 };
 template <int D> struct AttendSmem {
@@ -478,7 +488,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
         for (int e0 = 0; e0 < a.entries && u0 < u1; e0 += ATT_THREADS) {
             const int i = e0 + tid;
             Entry e;
-            int from = 0, to = 0, len = 1, shift = 0, count = 0, lines0 = 0, lines1 = 0;
+            int from = 0, to = 0, len = 1, shift = 0, cut = 0, count = 0, lines0 = 0, lines1 = 0;
             // tiles of this CTA in a line: those that its units stand for
             auto range_of = [&](int line, int& t0, int& t1) {
                 const int x0 = from > line * len ? from - line * len : 0, x1 = to - line * len < len ? to - line * len : len;
@@ -489,6 +499,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                 e = plan[i];
                 len = line_units(e);
                 shift = tile_shift(e.rows);
+                cut = piece_shift<DT>(e.rows);
                 from = u0 > e.u ? u0 - e.u : 0;
                 const int all = len * a.pg.H_kv * e.row_tiles;
                 to = u1 - e.u < all ? u1 - e.u : all;
@@ -499,9 +510,9 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                     for (int line = lines0; line <= lines1; line = line == lines0 && lines1 > lines0 + 1 ? lines1 : line + 1) {
                         int t0, t1;
                         range_of(line, t0, t1);
-                        if (t1 > t0) count += (t1 - 1) / ATT_CHUNK - t0 / ATT_CHUNK + 1;
+                        if (t1 > t0) count += ((t1 - 1) >> cut) - (t0 >> cut) + 1;
                     }
-                    if (lines1 > lines0 + 1) count += (lines1 - lines0 - 1) * e.chunks;
+                    if (lines1 > lines0 + 1) count += (lines1 - lines0 - 1) * (((e.tiles - 1) >> cut) + 1);
                 }
             }
             int total, at = listed + scan_cta<ATT_THREADS>(count, &total, sm.warp_sum) - batch * ATT_PIECES;     // of this entry's first piece
@@ -509,12 +520,12 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
             if (count > 0 && at < ATT_PIECES && at + count > 0) {
 #pragma unroll 1
                 for (int line = lines0; line <= lines1 && at < ATT_PIECES; ++line) {
-                    int t0, t1;
-                    range_of(line, t0, t1);
+                    int first, t1;
+                    range_of(line, first, t1);
 #pragma unroll 1
-                    for (; t0 < t1; t0 = (t0 / ATT_CHUNK + 1) * ATT_CHUNK, ++at) {
+                    for (int t0 = first; t0 < t1; t0 = ((t0 >> cut) + 1) << cut, ++at) {
                         if (at < 0 || at >= ATT_PIECES) continue;
-                        const int chunk = t0 / ATT_CHUNK, end = (chunk + 1) * ATT_CHUNK < t1 ? (chunk + 1) * ATT_CHUNK : t1;
+                        const int chunk = t0 / ATT_CHUNK, next = ((t0 >> cut) + 1) << cut, end = next < t1 ? next : t1;
                         Piece p;
                         p.b = e.b;
                         const int row_tile = line / a.pg.H_kv;
@@ -526,6 +537,7 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         p.hi = e.hi;
                         p.seen = e.seen;
                         p.merge = merges_copies(a, e.tiles << shift, p.rows, units);
+                        p.more = t0 > first && t0 % ATT_CHUNK != 0;
                         p.tile0 = e.tile0 + t0;
                         p.tile1 = e.tile0 + end;
                         const long long slot = (long long)e.item + (long long)line * a.max_chunks + chunk + cta;
@@ -1046,8 +1058,22 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                                                      (WHOLE || bar_wait(smem_of(&sm.o_ready[s][1]), (turns - 1) & 1, gave_up)));
                     tc_after_sync();
                 }
+                // What is there of the part's rows already (with `more`): reference and weight sum, and the factors for its sums and for this piece's.
+                const bool adds = DT == TYPE_FP16 && p.more && turn_count > 0;
+                float2 old = make_float2(ATT_NONE, 0.f);
+                float keep = 0.f, take = 1.f;
+                auto add_weights = [&](float& top, float& sum) {
+                    if (old.x == ATT_NONE) return;
+                    const float now = fmaxf(old.x, top);
+                    keep = exp2_approx(old.x - now);
+                    take = exp2_approx(top - now);
+                    top = now;
+                    sum = fmaf(old.y, keep, sum * take);
+                };
+                if (adds && live) old = *reinterpret_cast<const float2*>(part + weight_at(at, p.half_rows, D));
                 if (!p.merge || turn_count == 0) {
-                    if (live && (!p.merge || copy == 0)) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(ref, l);
+                    if (adds) add_weights(ref, l);
+                    if (live && (!p.merge || copy == 0) && (turn_count > 0 || !p.more)) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(ref, l);
                     if (ok && turn_count > 0 && warp_live) {
 #pragma unroll 1
                         for (int c = 0; c < D; c += 32) {
@@ -1055,6 +1081,16 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                             tc_ld32(O + c, x);
                             tc_wait_ld();
                             tc_loaded32(x);
+                            if (adds && old.x != ATT_NONE) {
+#pragma unroll
+                                for (int j = 0; j < 32; j += 4) {
+                                    const float4 y = *reinterpret_cast<const float4*>(part + sums_at(at, (c + j) / 4, D));
+                                    x[j] = __float_as_uint(fmaf(y.x, keep, __uint_as_float(x[j]) * take));
+                                    x[j + 1] = __float_as_uint(fmaf(y.y, keep, __uint_as_float(x[j + 1]) * take));
+                                    x[j + 2] = __float_as_uint(fmaf(y.z, keep, __uint_as_float(x[j + 2]) * take));
+                                    x[j + 3] = __float_as_uint(fmaf(y.w, keep, __uint_as_float(x[j + 3]) * take));
+                                }
+                            }
                             if (live) {
 #pragma unroll
                                 for (int j = 0; j < 32; j += 4)
@@ -1088,6 +1124,11 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
                         e[c] = e[c] == ATT_NONE ? 0.f : exp2_approx(e[c] - top);
                         if (c < copies) total = fmaf(refs[at + c * (ATT_TILE / copies)].y, e[c], total);
                     }
+                    if (adds) {                          // (all copies have read what copy 0 writes now)
+                        add_weights(top, total);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) e[c] *= take;
+                    }
                     if (ok && live && copy == 0) *reinterpret_cast<float2*>(part + weight_at(at, p.half_rows, D)) = make_float2(top, total);
                     meet();
 #pragma unroll 1
@@ -1107,6 +1148,10 @@ __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_con
 #pragma unroll 1
                         for (int c4 = copy * (F4 / copies); c4 < (copy + 1) * (F4 / copies); ++c4) {
                             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (adds && old.x != ATT_NONE) {
+                                y = *reinterpret_cast<const float4*>(part + sums_at(at, half * F4 + c4, D));
+                                y = make_float4(y.x * keep, y.y * keep, y.z * keep, y.w * keep);
+                            }
 #pragma unroll
                             for (int c = 0; c < 4; ++c) {
                                 if (c >= copies) break;
