@@ -547,7 +547,7 @@ int retopk_pages_copy(const retopk_pages_t* pages, int64_t n, const int32_t* src
  * Scores, sums and outputs are held in fp32; weights are rounded to the pages' type once for the
  * product with the values, and the tensor cores cut the sums of up to 8192 (bf16) or 1024 (fp16) products of 16 keys off, each at
  * 2^-23 of the sum so far (longer sums are rounded): 6e-4 or 1e-4 of the output where values have one sign.  Values that are not finite make the outputs of those who see them NaN or infinite.
- * A scale of 0 counts as the smallest normal number.  Results are bit-reproducible; in place they may differ from others in
+ * A scale of 0 counts as the smallest normal number; one of 2^127 and more is EINVAL where its product with log2(e) leaves fp32.  Results are bit-reproducible; in place they may differ from others in
  * the last bits.
  * out may be q where q is contiguous; other overlaps of out, lse and workspace with each other or with what is read, lengths, groups
  * and block_table among it, are EINVAL.  workspace as in retopk_q4_attention.

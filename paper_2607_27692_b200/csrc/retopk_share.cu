@@ -84,6 +84,8 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
                     const Memory& blocks_m, const void* q, int64_t q_stride, float scale, void* out, float* lse, void* workspace,
                     int64_t workspace_bytes, AttendArgs& a) {
     if (pages->format == RETOPK_PAGES_Q4 || !seq_lens || !out || !workspace || !isfinite(scale)) return RETOPK_EINVAL;
+    const float scale_log2 = (float)((double)scale * 1.44269504088896340736);
+    if (!isfinite(scale_log2)) return RETOPK_EINVAL;     // (0 times it would be no number)
     const int d = pages->d;
     if (!rows_ok(q, q_stride, H_q, d) || !aligned16(workspace) || !aligned16(out)) return RETOPK_EINVAL;
     memset(&a, 0, sizeof a);
@@ -104,7 +106,7 @@ int check_attention(const retopk_pages_t* pages, int B, int T, int H_q, const in
     a.q_stride = q_stride;
     a.out = static_cast<uint16_t*>(out);
     a.lse = lse;
-    a.scale_log2 = (float)((double)scale * 1.44269504088896340736);
+    a.scale_log2 = scale_log2;
     a.B = B; a.T = T; a.Hq = H_q; a.G = H_q / pages->H_kv;
     return RETOPK_OK;
 }

@@ -50,3 +50,11 @@ def test_update_overlaps(lib):  # noqa: F811
     assert lib.retopk_block_update(half(), 64, X, 3, X + 64, 5, None) == EINVAL
     assert lib.retopk_block_update(half(), 64, TABLE, 3, X, 5, None) == EINVAL
     assert lib.retopk_block_update(half(), 64, X, 3, X, 0, None) == OK
+
+
+@pytest.mark.parametrize("scale", [3.0e38, -2.4e38, 3.4028234e38])
+def test_scale_beyond_fp32(lib, scale):  # noqa: F811
+    """As a power of two it would be infinite, and 0 times it no number."""
+    args = (X, 512, scale, X + 2 * M, None, X + 4 * M, 1 << 20, None)
+    assert lib.retopk_shared_attention(half(), 3, 1, 4, X + M, 0, None, None, *args) == EINVAL
+    assert lib.retopk_block_attention(half(), 16, 3, 1, 4, X + M, 4, X + M + 64, *args) == EINVAL
