@@ -577,6 +577,7 @@ Pooled pooled(PyObject* const* a, const char* lens_name) {
         type_error("block_table: expected a contiguous int32 tensor on ", dev, ", got ", table.scalar_type(), " on ", table.device());
     if (table.dim() != 2) value_error("block_table: expected [sequences, pages], got ", table.sizes());
     const int64_t B = table.size(0);
+    if (B > 0 && table.size(1) == 0) value_error("block_table has no room: ", table.sizes());
     const int32_t* lens = ints(a[4], lens_name, dev, B);
     return {{refs.data_ptr<int32_t>(), scratch.data_ptr<int32_t>(), n, small(a[2], "page_size")}, dev, table, B, const_cast<int32_t*>(lens)};
 }
@@ -587,7 +588,7 @@ PyObject* pool_reserve(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     return guarded([&]() -> PyObject* {
         const Pooled p = pooled(a, "old_lens");
         const int32_t* now = ints(a[5], "new_lens", p.dev, p.B);
-        if (p.table.numel() > 0) {
+        if (p.B > 0) {
             const c10::cuda::CUDAGuard guard(p.dev);
             check(retopk_pool_reserve(&p.pool, (int)p.B, p.lens, now, p.table.data_ptr<int32_t>(), p.table.size(1), stream_of(p.dev)), "retopk_pool_reserve");
             for (int i : {0, 1, 3}) written(tensor(a[i], "refs, block_table"));
@@ -607,12 +608,11 @@ PyObject* pool_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const c10::cuda::CUDAGuard guard(p.dev);
         at::Tensor out[3];
         for (at::Tensor& t : out) t = empty({n}, p.table, at::kInt);
-        if (n > 0 && p.table.numel() > 0) {
+        if (n > 0 && p.B == 0) value_error("forks in a block_table of no sequences");
+        if (n > 0) {
             check(retopk_pool_fork(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, parents, children,
                                    out[0].data_ptr<int32_t>(), out[1].data_ptr<int32_t>(), out[2].data_ptr<int32_t>(), stream_of(p.dev)), "retopk_pool_fork");
             for (int i : {0, 1, 3, 4}) written(tensor(a[i], "refs, block_table, seq_lens"));
-        } else if (n > 0) {
-            value_error("block_table has no room: ", p.table.sizes());
         }
         PyObject* r = PyTuple_New(3);
         for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
@@ -628,7 +628,7 @@ PyObject* pool_free(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const int64_t n = given(a[5]) ? count(a[5], "rows") : p.B;
         const int32_t* rows_ = given(a[5]) ? ints(a[5], "rows", p.dev, n) : nullptr;
         if (n > 2147483647) value_error("rows: too many, ", n);
-        if (n > 0 && p.table.numel() > 0) {
+        if (n > 0 && p.B > 0) {
             const c10::cuda::CUDAGuard guard(p.dev);
             check(retopk_pool_free(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, rows_, stream_of(p.dev)), "retopk_pool_free");
             for (int i : {0, 1, 4}) written(tensor(a[i], "refs, seq_lens"));
@@ -642,7 +642,7 @@ PyObject* pool_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (!arity(n_args, 5)) return nullptr;
     return guarded([&]() -> PyObject* {
         const Pooled p = pooled(a, "seq_lens");
-        if (p.table.numel() == 0) value_error("block_table has no room: ", p.table.sizes());
+        if (p.B == 0) value_error("block_table of no sequences");
         const c10::cuda::CUDAGuard guard(p.dev);
         const at::Tensor src = empty({p.pool.n_pages / 2}, p.table, at::kInt), dst = empty({p.pool.n_pages / 2}, p.table, at::kInt);
         check(retopk_pool_compact(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), src.data_ptr<int32_t>(),

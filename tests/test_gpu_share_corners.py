@@ -309,3 +309,23 @@ def test_lengths_beyond_the_row_that_shrink(paged):
     table[0, 1] = 99                                      # no page
     pool.reserve(table, ints([8]), ints([0]))
     assert table.tolist() == [[-1] * 3] and pool.refs.tolist() == [0, 1] + [0] * 6 and pool.missing.item() == 0
+
+
+def test_tables_without_room(paged):
+    """A table of no places is refused by every call, where lengths would have been left as they were; one of no rows has nothing to do."""
+    pool, lens = paged.PagePool(4, 4), ints([3, 0])
+    table, one = torch.zeros(2, 0, dtype=torch.int32, device="cuda"), ints([0])
+    for call in (lambda: pool.reserve(table, lens, lens), lambda: pool.fork(table, lens, one, ints([1])), lambda: pool.free(table, lens),
+                 lambda: pool.free(table, lens, one), lambda: pool.compact(table, lens)):
+        with pytest.raises(ValueError):
+            call()
+    none, empty = torch.zeros(0, 5, dtype=torch.int32, device="cuda"), ints([])
+    pool.reserve(none, empty, empty)
+    pool.free(none, empty)
+    pool.free(none, empty, one)
+    assert [x.numel() for x in pool.fork(none, empty, empty, empty)] == [0, 0, 0]
+    with pytest.raises(ValueError):
+        pool.fork(none, empty, one, one)
+    with pytest.raises(ValueError):
+        pool.compact(none, empty)
+    assert lens.tolist() == [3, 0] and not pool.refs.any() and pool.missing.item() == 0
