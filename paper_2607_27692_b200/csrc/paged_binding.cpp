@@ -420,6 +420,8 @@ int64_t integer(PyObject* o) {
     if (v == -1 && PyErr_Occurred()) throw python_error();
     return v;
 }
+// A count as the C interface takes it; one that it would not hold is one that it refuses.
+int clipped(int64_t n) { return (int)(n < 2147483647 ? n : 2147483647); }
 int small(PyObject* o, const char* what) {
     const int64_t v = integer(o);
     if (v < -2147483647 || v > 2147483647) value_error(what, ": out of range, got ", v);
@@ -439,7 +441,7 @@ PyObject* block_update(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         no_gradient("update", {&bounds, &c.tensors[0]});
         if (B > 0) {
             const c10::cuda::CUDAGuard guard(c.dev);
-            check(retopk_block_update(&pages, block, bounds.data_ptr(), (int)B, lens, n_new, stream_of(c.dev)), "retopk_block_update");
+            check(retopk_block_update(&pages, block, bounds.data_ptr(), clipped(B), lens, n_new, stream_of(c.dev)), "retopk_block_update");
             written(bounds);
         }
         return Py_NewRef(Py_None);
@@ -590,7 +592,7 @@ PyObject* pool_reserve(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const int32_t* now = ints(a[5], "new_lens", p.dev, p.B);
         if (p.B > 0) {
             const c10::cuda::CUDAGuard guard(p.dev);
-            check(retopk_pool_reserve(&p.pool, (int)p.B, p.lens, now, p.table.data_ptr<int32_t>(), p.table.size(1), stream_of(p.dev)), "retopk_pool_reserve");
+            check(retopk_pool_reserve(&p.pool, clipped(p.B), p.lens, now, p.table.data_ptr<int32_t>(), p.table.size(1), stream_of(p.dev)), "retopk_pool_reserve");
             for (int i : {0, 1, 3}) written(tensor(a[i], "refs, block_table"));
         }
         return Py_NewRef(Py_None);
@@ -610,7 +612,7 @@ PyObject* pool_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         for (at::Tensor& t : out) t = empty({n}, p.table, at::kInt);
         if (n > 0 && p.B == 0) value_error("forks in a block_table of no sequences");
         if (n > 0) {
-            check(retopk_pool_fork(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, parents, children,
+            check(retopk_pool_fork(&p.pool, clipped(p.B), p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, parents, children,
                                    out[0].data_ptr<int32_t>(), out[1].data_ptr<int32_t>(), out[2].data_ptr<int32_t>(), stream_of(p.dev)), "retopk_pool_fork");
             for (int i : {0, 1, 3, 4}) written(tensor(a[i], "refs, block_table, seq_lens"));
         }
@@ -630,7 +632,7 @@ PyObject* pool_free(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (n > 2147483647) value_error("rows: too many, ", n);
         if (n > 0 && p.B > 0) {
             const c10::cuda::CUDAGuard guard(p.dev);
-            check(retopk_pool_free(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, rows_, stream_of(p.dev)), "retopk_pool_free");
+            check(retopk_pool_free(&p.pool, clipped(p.B), p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), (int)n, rows_, stream_of(p.dev)), "retopk_pool_free");
             for (int i : {0, 1, 4}) written(tensor(a[i], "refs, seq_lens"));
         }
         return Py_NewRef(Py_None);
@@ -645,7 +647,7 @@ PyObject* pool_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         if (p.B == 0) value_error("block_table of no sequences");
         const c10::cuda::CUDAGuard guard(p.dev);
         const at::Tensor src = empty({p.pool.n_pages / 2}, p.table, at::kInt), dst = empty({p.pool.n_pages / 2}, p.table, at::kInt);
-        check(retopk_pool_compact(&p.pool, (int)p.B, p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), src.data_ptr<int32_t>(),
+        check(retopk_pool_compact(&p.pool, clipped(p.B), p.lens, p.table.data_ptr<int32_t>(), p.table.size(1), src.data_ptr<int32_t>(),
                                   dst.data_ptr<int32_t>(), stream_of(p.dev)), "retopk_pool_compact");
         for (int i : {0, 1, 3}) written(tensor(a[i], "refs, block_table"));
         PyObject* r = PyTuple_New(2);

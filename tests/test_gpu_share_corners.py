@@ -329,3 +329,19 @@ def test_tables_without_room(paged):
     with pytest.raises(ValueError):
         pool.compact(none, empty)
     assert lens.tolist() == [3, 0] and not pool.refs.any() and pool.missing.item() == 0
+
+
+def test_more_sequences_than_the_interface_counts(paged):
+    """2^32 + 1 rows are not one."""
+    pool = paged.PagePool(4, 4)
+    lens = torch.zeros(2 ** 32 + 1, dtype=torch.int32, device="cuda")
+    lens[0] = 3
+    table = torch.zeros(2 ** 32 + 1, 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(paged._rt.RetopkError):
+        pool.free(table, lens, ints([0]))
+    with pytest.raises(paged._rt.RetopkError):
+        pool.reserve(table, lens, lens)
+    cache = paged.KVPages(4, 1, 16, 64, "bf16")
+    with pytest.raises(paged._rt.RetopkError):
+        paged.BlockIndex(cache, 16).update(lens, table)
+    assert lens[0].item() == 3
