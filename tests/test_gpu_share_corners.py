@@ -345,3 +345,85 @@ def test_more_sequences_than_the_interface_counts(paged):
     with pytest.raises(paged._rt.RetopkError):
         paged.BlockIndex(cache, 16).update(lens, table)
     assert lens[0].item() == 3
+
+
+def test_pool_at_its_limits(paged):
+    """2^20 pages, 65 535 sequences, 65 535 forks, against a model of whole arrays."""
+    import numpy as np
+    n_pages, B, page, width = 1 << 20, 65535, 16, 17
+    rng = np.random.default_rng(1)
+    pool = paged.PagePool(n_pages, page)
+    table_d, lens_d = torch.zeros(B, width, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    table, lens, refs = np.zeros((B, width), np.int64), np.zeros(B, np.int64), np.zeros(n_pages, np.int64)
+    place = np.arange(width)
+
+    def same():
+        assert np.array_equal(table_d.cpu().numpy(), table) and np.array_equal(lens_d.cpu().numpy(), lens)
+        assert np.array_equal(pool.refs.cpu().numpy(), refs)
+
+    def reserve(new):
+        had, get = -(-lens // page), -(-new // page)
+        back = (place >= get[:, None]) & (place < had[:, None])
+        np.subtract.at(refs, table[back], 1)
+        table[back] = -1
+        grown = (place >= had[:, None]) & (place < get[:, None])
+        pages = np.flatnonzero(refs <= 0)[:grown.sum()]
+        table[grown] = pages
+        refs[pages] = 1
+        new_d = torch.from_numpy(new).to(device="cuda", dtype=torch.int32)
+        pool.reserve(table_d, lens_d, new_d)
+        lens[:] = new
+        lens_d.copy_(new_d)
+        same()
+
+    reserve(rng.integers(0, 16 * page, B))
+    reserve(rng.integers(1, 17 * page, B))
+    gone = rng.permutation(B)[:B // 2]
+    np.subtract.at(refs, table[gone][place < (-(-lens[gone] // page))[:, None]], 1)
+    lens[gone] = 0
+    pool.free(table_d, lens_d, torch.from_numpy(gone).to(device="cuda", dtype=torch.int32))
+    same()
+    # every empty row continues a sequence; the other forks have children that are not empty
+    parents = rng.choice(np.flatnonzero(lens > 0), B)
+    children = np.arange(B)
+    made = (lens[children] <= 0) & (lens[parents] > 0)
+    made &= ~np.isin(parents, children)                   # (all rows are children: none is made)
+    moves = pool.fork(table_d, lens_d, *(torch.from_numpy(x).to(device="cuda", dtype=torch.int32) for x in (parents, children)))
+    assert not made.any() and [m.min().item() for m in moves] == [-1, -1, 0] and [m.max().item() for m in moves] == [-1, -1, 0]
+    same()
+    children = np.where(lens <= 0, np.arange(B), -1)      # forks without a child are left out
+    made = children >= 0
+    moves = pool.fork(table_d, lens_d, *(torch.from_numpy(x).to(device="cuda", dtype=torch.int32) for x in (parents, children)))
+    full, rest = lens[parents] // page, lens[parents] % page
+    takes = made & (rest > 0)
+    pages = np.full(B, -1)
+    pages[takes] = np.flatnonzero(refs <= 0)[:takes.sum()]
+    want_src = np.where(takes, table[parents, np.minimum(full, width - 1)], -1)
+    assert np.array_equal(moves[0].cpu().numpy(), want_src) and np.array_equal(moves[1].cpu().numpy(), pages)
+    assert np.array_equal(moves[2].cpu().numpy(), np.where(takes, rest, 0))
+    whole = made[:, None] & (place < full[:, None])
+    shared = table[parents]
+    np.add.at(refs, shared[whole], 1)
+    refs[pages[takes]] = 1
+    for mask, values in ((whole, shared), (takes[:, None] & (place == full[:, None]), np.broadcast_to(pages[:, None], (B, width)))):
+        rows = np.broadcast_to(children[:, None], (B, width))
+        table[rows[mask], np.broadcast_to(place, (B, width))[mask]] = values[mask]
+    lens[children[made]] = lens[parents[made]]
+    same()
+    gone = np.arange(0, B, 3)
+    np.subtract.at(refs, table[gone][place < (-(-lens[gone] // page))[:, None]], 1)
+    lens[gone] = 0
+    pool.free(table_d, lens_d, torch.from_numpy(gone).to(device="cuda", dtype=torch.int32))
+    used = refs > 0
+    U = int(used.sum())
+    movers, holes = np.flatnonzero(used[U:]) + U, np.flatnonzero(~used[:U])
+    to = np.arange(n_pages)
+    to[movers] = holes
+    held = place < (-(-lens // page))[:, None]
+    table[held] = to[table[held]]
+    refs[holes], refs[movers] = refs[movers], 0
+    src, dst = (x.cpu().numpy() for x in pool.compact(table_d, lens_d))
+    assert np.array_equal(src[:len(movers)], movers) and np.array_equal(dst[:len(holes)], holes) and (src[len(movers):] == -1).all()
+    same()
+    reserve(np.minimum(lens + rng.integers(-40, 40, B), width * page).clip(0))
+    assert pool.missing.item() == 0
