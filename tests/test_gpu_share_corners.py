@@ -427,3 +427,36 @@ def test_pool_at_its_limits(paged):
     same()
     reserve(np.minimum(lens + rng.integers(-40, 40, B), width * page).clip(0))
     assert pool.missing.item() == 0
+
+
+# ---------------------------------------------------------------------------------------
+# Caches without a table
+# ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+@pytest.mark.parametrize("rows", [1, 7, 127, 129, 300, 1001])
+def test_contiguous_caches_of_any_size(paged, dtype, d, rows):
+    """Tiles that end behind a sequence's last row, where the next head's and the next sequence's rows follow."""
+    lens = [rows, rows - 1, max(1, rows - 130), rows, 1]
+    k, v = randn(1, 5, 3, rows, d, dtype=dtype), randn(2, 5, 3, rows, d, dtype=dtype)
+    q = randn(3, 5, 2, 6, d, dtype=dtype)
+    cache = paged.KVPages.wrap(k, v)
+    lse = torch.full((5, 2, 6), 7.0, device="cuda")
+    want = cache.attend_shared(q, ints(lens), lse=lse)
+    sref.check_attention(want, lse, q, k, v, None, lens, rows, d ** -0.5)
+    for value in (math.nan, math.inf):                    # other heads and sequences, rows behind the last
+        x, y = k.clone(), v.clone()
+        x[:, 1], y[:, 1] = value, value
+        for b, n in enumerate(lens):
+            x[b, :, n:], y[b, :, n:] = value, value
+        got = paged.KVPages.wrap(x, y).attend_shared(q, ints(lens))
+        assert torch.equal(got[:, :, :2], want[:, :, :2]) and torch.equal(got[:, :, 4:], want[:, :, 4:])
+    if rows % 16 == 0 or rows < 16:
+        return
+    # selected blocks in a cache whose size is a multiple of the block
+    k, v = k[:, :, :rows // 16 * 16].contiguous(), v[:, :, :rows // 16 * 16].contiguous()
+    lens = [min(n, k.shape[2]) for n in lens]
+    index = paged.BlockIndex(paged.KVPages.wrap(k, v), 16)
+    index.update(ints(lens))
+    blocks = index.select(q, ints(lens), keep=4, first=1, last=1)
+    picks = [[sref.select(q[b, t], index.bounds, None, b, n - 1 + t, k.shape[2], 16, 4, 1, 1) for t in range(2)] for b, n in enumerate(lens)]
+    sref.check_attention(index.attend(q, ints(lens), blocks), None, q, k, v, None, lens, k.shape[2], d ** -0.5, picks, 16)
