@@ -11,9 +11,10 @@
 // rows.  For each KV head and 256 query rows an entry has a line of tiles; a piece of a line is what one CTA
 // takes of it, and leaves fp32 sums for its rows in the workspace.
 //
-// Measured (bf16, d = 128, 8 KV heads of 4 queries).  Four sequences of up to 128K keys on their own, 1.5 GB: 238 us, 6.4 TB/s, as fast as a copy.
-// Eight sequences that share 32K keys: 42 us, of which 21 are the floor of reading them; 3 pass until all CTAs know their work,
-// 3 until the first scores, 8 in join_kernel.  Of 64 sequences that share 128K: 188 us, 730 TFLOP/s; there the softmax bounds it.  256
+// Measured (bf16, d = 128, 8 KV heads of 4 queries).  Four sequences of 128K keys on their own, 2.1 GB: 320 us, 6.7 TB/s, as fast as a copy.
+// Eight sequences that share 32K keys: 43 us, of which 21 are the floor of reading them; 3 pass until all CTAs know their work,
+// 3 until the first scores, 8 in join_kernel.  Of 64 sequences that share 128K: 188 us, 730 TFLOP/s, in short runs; 215 to 228 us and 600 to
+// 640 TFLOP/s repeated for seconds, at the power limit.  There the softmax bounds it.  256
 // rows of a tile take 4900 cycles: 2048 for the exponentials alone (16 a cycle), about 2560 of the tensor
 // core (half tiles of keys read Q anew for 64 keys), and neither is hidden wholly behind the other.
 #pragma once
@@ -34,7 +35,7 @@ constexpr int ATT_TILE = 128;            // keys of a tile, and query rows of a 
 constexpr int ATT_FEW = 64;              // query rows up to which tiles are taken whole
 constexpr int ATT_CHUNK = 1024;          // tiles of a line whose sums one part of a CTA holds at most
 // What a CTA's work counts: a tile of up to 128 query rows 1 (two of them are at work at once), one of more rows 2, and the
-// beginning of a line 3.
+// beginning of a line 3.  (64 sequences that share 128K, the one size at which this was varied: 237, 210, 201, 191 and 195 us with 1.5, 2, 2.5, 3 and 4.5.)
 constexpr int ATT_START = 3;
 constexpr float ATT_NONE = -3.402823466e38f, ATT_LOW = -3.3e38f;     // reference of a row without keys; lowest of one with keys
 constexpr float ATT_LEAST_SCALE = 1.17549435e-38f;        // stands for a scale of 0
@@ -117,8 +118,9 @@ template <int DT> __device__ __forceinline__ int piece_shift(int rows) {
 static_assert(ATT_CHUNK == 1 << 10, "pieces divide chunks");
 // Whether the sums of a part's copies become one before they are written.  That takes 1 to 2 us at the end of a piece; in
 // join_kernel it saves a half or three quarters of the places, in all parts of the line, that the threads which share a row go
-// through.  Done where each of them had 6 or more.  (Group of 8 sequences, 18 parts to a line: 47.9 to 43.5 us; blocks of 4
-// sequences, 5 parts to a line: 38.2 us, 41.7 with it.)
+// through.  Done where each of them had 6 or more.  (us without and with it: groups of 2, 4, 8 and 16 sequences that share 32K, 18 parts to
+// a line, 40.9 and 38.4, 44.1 and 41.0, 47.3 and 42.9, 46.7 and 44.8; blocks of 4 sequences, 5 parts to a line, 21.8 and 22.2;
+// 4 sequences that share 704, 19.7 and 20.7.)
 __device__ __forceinline__ bool merges_copies(const AttendArgs& a, int line_units, int rows, int units) {
     const int copies = copies_of(rows);
     return copies > 1 && (long long)line_units * (units / 2 < a.grid ? units / 2 : a.grid) * (2 * copies) >= 6ll * a.join_splits * units;
@@ -407,7 +409,10 @@ template <int D> struct AttendSmem {
 // Rows of values that do not count (masked, pages out of range) are read from behind the last row, where a copy
 // finds zeros; a weight of 0 would not hide a NaN.
 // Weights are taken against a reference that need not be the maximum (halves: as long as their sum stays below 2^14; WHOLE: each below
-// 2^8), so that most halves need neither maxima nor a rescaling of O; they are rounded to 16 bits once, for the tensor core.
+// 2^8), so that most halves need neither maxima nor a rescaling of O; they are rounded to 16 bits once, for the tensor core.  In
+// two parts each, as the attention over 4-bit pages has them, O += P V and the conversions would be twice as much where they and the
+// softmax bound the kernel already; rounded once, outputs are 0.0023 (bf16) and 0.0003 (fp16) off on average, 0.0017 and 0.0002 of which
+// is the rounding of the output itself.  Their sum is that of the weights before they are rounded.
 template <int DT, int D, bool WHOLE>
 __global__ void __launch_bounds__(ATT_THREADS, 1) attend_kernel(const __grid_constant__ AttendParams params) {
     using Smem = AttendSmem<D>;

@@ -71,6 +71,8 @@ __device__ __forceinline__ void count_missing(const PoolArgs& a, long long n) {
 // One CTA: how many pages each sequence needs, the lowest free ones, and their places in the table.  A
 // sequence gets all of its pages or none: then its new entries are -1, all of them, however few pages there are.  Before that
 // sequences that shrink give back what they no longer hold, so that a page may go from one to another in a call.
+// Bound by waiting: 6.5 us for a page each of 64 sequences out of 8192, 3.1 with nothing to do; where nearly all pages are in use the
+// walk over their counts shows, 16 us of 65 536 and 115 of 2^20.
 __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_constant__ PoolArgs a) {
     __shared__ int s_base[POOL_THREADS], s_need[POOL_THREADS];
     pdl_wait();
